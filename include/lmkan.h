@@ -373,6 +373,117 @@ lmkan_status lmkan_conv2d_backward(const lmkan_desc *desc, const lmkan_conv2d *c
                                    const void *coef_dev, const float *grad_y_dev, float *grad_x_dev,
                                    float *grad_coef_dev, void *workspace_dev, size_t workspace_bytes, void *stream);
 
+/*
+ * Dense companions of the layer.  A preconditioned layer (App. E) is
+ *     y = gamma lmKAN(x) + Linear(ReLU(x)),
+ * and a table in the layout of Alg. 1 is itself a batch of (G+1)^2 matrices of
+ * n_in/2 x n_out (the layer is one linear map of the pairs' basis functions for every
+ * table node).  The calls below train such matrices with orthogonalised updates and
+ * answer with the linear term in 8-bit whole numbers.
+ */
+
+/* Largest matrices: the shorter side, the longer side, and the steps of a schedule. */
+#define LMKAN_MAX_MATRIX_SHORT 16384
+#define LMKAN_MAX_MATRIX_LONG (1 << 26)
+#define LMKAN_MAX_ORTHO_STEPS 32
+
+/* A batch of dense matrices, [batch][rows][cols] row-major and contiguous. */
+typedef struct lmkan_matrices {
+    int64_t batch;       /* >= 0                                                       */
+    int32_t rows, cols;  /* >= 1; the shorter up to LMKAN_MAX_MATRIX_SHORT, the longer
+                            up to LMKAN_MAX_MATRIX_LONG                                */
+    int32_t dtype;       /* lmkan_dtype of the matrix (lmkan_muon_step: the gradient)  */
+    float eps;           /* added to the Frobenius norm, > 0                           */
+} lmkan_matrices;
+
+/*
+ * Orthogonalisation by Newton-Schulz products.  For every matrix X of the batch
+ *     X_0 = X / (|X|_F + eps),
+ *     X_{k+1} = a_k X_k + (b_k A + c_k A^2) X_k,  A = X_k X_k^T,
+ * which leaves the singular vectors alone and takes every singular value s in (0, 1] to
+ * a s + b s^3 + c s^5, step after step.
+ *   schedule_host [steps][3]: (a_k, b_k, c_k) on the host, read during the call;
+ *                 0 <= steps <= LMKAN_MAX_ORTHO_STEPS (NULL allowed for none).
+ *                 LMKAN_ERR_UNSUPPORTED when one is not finite, or when a step could
+ *                 bring a singular value beyond 4 or has a factor a + b s^2 + c s^4
+ *                 beyond 64 on its range: the intermediates are scaled by what these
+ *                 bounds allow.
+ *   x_dev, out_dev  desc->dtype; out is overwritten and may be x_dev itself
+ *   workspace_dev / workspace_bytes: at least lmkan_orthogonalize_workspace_bytes(desc)
+ *                 bytes, 256-byte aligned
+ * Every product keeps 22 bits of its factors and is summed in float32, norms are summed
+ * in float64; out is rounded to desc->dtype once.  A matrix of zeros stays zero; one
+ * with a NaN or an infinity becomes NaN (steps > 0) and leaves the others of the batch alone.
+ * The result repeats bit for bit between runs.
+ */
+size_t lmkan_orthogonalize_workspace_bytes(const lmkan_matrices *desc);
+lmkan_status lmkan_orthogonalize(const lmkan_matrices *desc, int32_t steps, const float *schedule_host,
+                                 const void *x_dev, void *out_dev, void *workspace_dev, size_t workspace_bytes,
+                                 void *stream);
+
+/* One step of an optimiser with orthogonalised updates. */
+typedef struct lmkan_muon {
+    float lr;
+    float momentum;      /* beta                                                       */
+    float weight_decay;
+    float scale;         /* of the update, e.g. sqrt(max(1, rows / cols))              */
+    int32_t nesterov;    /* 0 or 1                                                     */
+} lmkan_muon;
+
+/*
+ * For every matrix of the batch, with G its gradient, M its momentum and W its weights:
+ *     M <- beta M + (1 - beta) G
+ *     U  = nesterov ? beta M + (1 - beta) G : M
+ *     W <- (1 - lr weight_decay) W - lr scale orthogonalise(U)
+ * (orthogonalise as above).  grad_dev in desc->dtype, momentum_dev and weight_dev
+ * float32 and changed in place; the three must not overlap.  Workspace as for
+ * lmkan_orthogonalize.
+ */
+lmkan_status lmkan_muon_step(const lmkan_matrices *desc, const lmkan_muon *muon, int32_t steps,
+                             const float *schedule_host, const void *grad_dev, float *momentum_dev,
+                             float *weight_dev, void *workspace_dev, size_t workspace_bytes, void *stream);
+
+/*
+ * Rows to 8 bits: with r = max_e |x[n][e]|,
+ *     codes[n][e] = rint(x[n][e] * f), f = 127 / r rounded to float32 (0 where that is not finite),
+ *     scale[n] = r / 127 rounded to float32,
+ * ties to even, codes in [-127, 127].  With LMKAN_LINEAR_RELU max(x, 0) takes the place
+ * of x.  A row with a NaN or an infinity gets a scale that is not finite and codes of zero.
+ * A matrix of weights [n_out][n_in] quantised this way has a scale for every output.
+ *   x_dtype 16-bit rows are widened to float32 first; cols 1 .. LMKAN_MAX_N_IN
+ *   codes_dev [rows][cols] int8, scale_dev [rows] float32, both overwritten
+ */
+#define LMKAN_LINEAR_RELU 1
+lmkan_status lmkan_quantize_rows(int64_t rows, int32_t cols, int32_t x_dtype, int32_t flags, const void *x_dev,
+                                 int8_t *codes_dev, float *scale_dev, void *stream);
+
+/* The linear term as it answers. */
+typedef struct lmkan_linear {
+    int32_t n_in;     /* 1 .. LMKAN_MAX_N_IN (sums of products of codes fit 32 bits)   */
+    int32_t n_out;    /* 1 .. LMKAN_MAX_N_OUT                                          */
+    int32_t x_dtype;  /* lmkan_dtype of x                                              */
+    int32_t y_dtype;  /* lmkan_dtype of y                                              */
+    int32_t flags;    /* LMKAN_LINEAR_RELU or 0                                        */
+} lmkan_linear;
+
+/*
+ * Linear layer on rows that are quantised on the way (codes and scales of
+ * lmkan_quantize_rows), weights held in 8 bits:
+ *     y[n][j] = beta y[n][j] + xscale[n] wscale[j] sum_e xcode[n][e] wcode[j][e] + bias[j]
+ * The sum is exact; the rest is float32, rounded to y's type once.
+ *   x_dev       [batch][n_in] in x_dtype
+ *   w_codes_dev [n_out][n_in] int8, w_scale_dev [n_out] float32
+ *   bias_dev    [n_out] float32, or NULL
+ *   y_dev       [batch][n_out] in y_dtype; read only when beta != 0 (y = lmKAN(x) and
+ *               beta = gamma make a preconditioned layer of it)
+ *   workspace_dev / workspace_bytes: at least lmkan_linear_i8_workspace_bytes(desc, batch)
+ *               bytes, 256-byte aligned (NULL allowed when 0)
+ */
+size_t lmkan_linear_i8_workspace_bytes(const lmkan_linear *desc, int64_t batch);
+lmkan_status lmkan_linear_i8(const lmkan_linear *desc, int64_t batch, const void *x_dev, const int8_t *w_codes_dev,
+                             const float *w_scale_dev, const float *bias_dev, float beta, void *y_dev,
+                             void *workspace_dev, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -29,6 +29,8 @@ LMKAN_FLAG_WORKSPACE_HAS_RECORDS = 2
 LMKAN_PACK_TILE = 64
 LMKAN_MAX_GRID = 64
 LMKAN_STATIC_SCRATCH_BYTES = 32 << 20
+LMKAN_LINEAR_RELU = 1
+LMKAN_MAX_ORTHO_STEPS = 32
 
 _TORCH_DTYPE = {LMKAN_F32: torch.float32, LMKAN_F16: torch.float16, LMKAN_BF16: torch.bfloat16}
 _DTYPE_CODE = {v: k for k, v in _TORCH_DTYPE.items()}
@@ -93,6 +95,67 @@ class LayerDesc:
         return (self.grid + 1, self.grid + 1, self.pairs, self.n_out)
 
 
+class _Matrices(C.Structure):
+    _fields_ = [("batch", C.c_int64), ("rows", C.c_int32), ("cols", C.c_int32), ("dtype", C.c_int32),
+                ("eps", C.c_float)]
+
+
+class _Muon(C.Structure):
+    _fields_ = [("lr", C.c_float), ("momentum", C.c_float), ("weight_decay", C.c_float), ("scale", C.c_float),
+                ("nesterov", C.c_int32)]
+
+
+class _Linear(C.Structure):
+    _fields_ = [("n_in", C.c_int32), ("n_out", C.c_int32), ("x_dtype", C.c_int32), ("y_dtype", C.c_int32),
+                ("flags", C.c_int32)]
+
+
+@dataclass
+class MatrixDesc:
+    """Mirror of ``lmkan_matrices``: a batch of dense matrices [batch][rows][cols].  A table in the layout of
+    Alg. 1 is one of (G+1)^2 matrices of pairs x n_out."""
+    batch: int
+    rows: int
+    cols: int
+    dtype: int = LMKAN_F32
+    eps: float = 1e-7
+
+    def c(self) -> _Matrices:
+        return _Matrices(self.batch, self.rows, self.cols, self.dtype, self.eps)
+
+    def shape(self):
+        return (self.batch, self.rows, self.cols)
+
+
+@dataclass
+class MuonParams:
+    """Mirror of ``lmkan_muon``."""
+    lr: float
+    momentum: float = 0.95
+    weight_decay: float = 0.0
+    scale: float = 1.0
+    nesterov: bool = True
+
+    def c(self) -> _Muon:
+        return _Muon(self.lr, self.momentum, self.weight_decay, self.scale, int(self.nesterov))
+
+
+@dataclass
+class LinearDesc:
+    """Mirror of ``lmkan_linear``: Linear(x), or Linear(ReLU(x)) with ``relu``."""
+    n_in: int
+    n_out: int
+    x_dtype: int = LMKAN_F32
+    y_dtype: int = LMKAN_F32
+    relu: bool = False
+
+    def c(self) -> _Linear:
+        return _Linear(self.n_in, self.n_out, self.x_dtype, self.y_dtype, LMKAN_LINEAR_RELU if self.relu else 0)
+
+
+# five steps of the quintic that brings singular values from a few thousandths up near one
+QUINTIC_SCHEDULE = ((3.4445, -4.7750, 2.0315),) * 5
+
 _lib = None
 _native = None   # the extension module, once the library is loaded
 
@@ -137,6 +200,23 @@ def lib() -> C.CDLL:
     L.lmkan_time_next_kernel.argtypes = [C.c_void_p, C.c_void_p]
     L.lmkan_microbench.restype = C.c_int
     L.lmkan_microbench.argtypes = [C.c_int32, C.c_void_p, C.c_size_t, C.POINTER(C.c_double), C.c_void_p]
+    mp, up, np_ = C.POINTER(_Matrices), C.POINTER(_Muon), C.POINTER(_Linear)
+    L.lmkan_orthogonalize_workspace_bytes.restype = C.c_size_t
+    L.lmkan_orthogonalize_workspace_bytes.argtypes = [mp]
+    L.lmkan_orthogonalize.restype = C.c_int
+    L.lmkan_orthogonalize.argtypes = [mp, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t,
+                                      C.c_void_p]
+    L.lmkan_muon_step.restype = C.c_int
+    L.lmkan_muon_step.argtypes = [mp, up, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                  C.c_size_t, C.c_void_p]
+    L.lmkan_quantize_rows.restype = C.c_int
+    L.lmkan_quantize_rows.argtypes = [C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p,
+                                      C.c_void_p]
+    L.lmkan_linear_i8_workspace_bytes.restype = C.c_size_t
+    L.lmkan_linear_i8_workspace_bytes.argtypes = [np_, C.c_int64]
+    L.lmkan_linear_i8.restype = C.c_int
+    L.lmkan_linear_i8.argtypes = [np_, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_float,
+                                  C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
     cp = C.POINTER(_Conv2d)
     L.lmkan_conv2d_rows.restype = C.c_int64
     L.lmkan_conv2d_rows.argtypes = [cp, C.POINTER(C.c_int32), C.POINTER(C.c_int32)]
@@ -455,3 +535,97 @@ def lmkan_fold(desc: LayerDesc, coef: torch.Tensor, gamma: float = 1.0, lin_w: t
     tp = _dev(out_shift, torch.float32, (desc.n_out,), "out_shift") if out_shift is not None else None
     _check(lib().lmkan_fold(C.byref(desc.c()), cp, float(gamma), wp, bp, sp, tp, _stream(stream)), "lmkan_fold")
     return coef
+
+
+def _schedule(schedule):
+    """(steps, float32 array [steps][3]) of a sequence of (a, b, c)."""
+    rows = np.asarray(schedule, dtype=np.float32).reshape(-1, 3)
+    return rows.shape[0], np.ascontiguousarray(rows)
+
+
+def _call_workspace(workspace: torch.Tensor | None, need: int, device):
+    """(tensor or None, bytes): the caller's workspace, else a fresh allocation of `need` bytes."""
+    if workspace is not None:
+        if not workspace.is_cuda or not workspace.is_contiguous():
+            raise ValueError("workspace: expected a contiguous device tensor")
+        return workspace, workspace.numel() * workspace.element_size()
+    return (torch.empty(need, dtype=torch.uint8, device=device), need) if need else (None, 0)
+
+
+def _ptr(t: torch.Tensor | None) -> int | None:
+    return None if t is None else t.data_ptr()
+
+
+def lmkan_orthogonalize_workspace_bytes(desc: MatrixDesc) -> int:
+    return lib().lmkan_orthogonalize_workspace_bytes(C.byref(desc.c()))
+
+
+def lmkan_orthogonalize(desc: MatrixDesc, x: torch.Tensor, schedule=QUINTIC_SCHEDULE, out: torch.Tensor | None = None,
+                        stream=None, workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """Each matrix of x [batch][rows][cols] brought near orthonormal rows (columns when rows > cols) by
+    Newton-Schulz steps, one (a, b, c) of ``schedule`` each; ``out`` may be ``x``."""
+    dt = _TORCH_DTYPE[desc.dtype]
+    xp = _dev(x, dt, desc.shape(), "x")
+    if out is None:
+        out = torch.empty(desc.shape(), dtype=dt, device=x.device)
+    op = _dev(out, dt, desc.shape(), "out")
+    steps, rows = _schedule(schedule)
+    ws, wsz = _call_workspace(workspace, lmkan_orthogonalize_workspace_bytes(desc), x.device)
+    _check(lib().lmkan_orthogonalize(C.byref(desc.c()), steps, rows.ctypes.data, xp, op, _ptr(ws), wsz, _stream(stream)),
+           "lmkan_orthogonalize")
+    _used_on(stream, ws, out)
+    return out
+
+
+def lmkan_muon_step(desc: MatrixDesc, muon: MuonParams, grad: torch.Tensor, momentum: torch.Tensor,
+                    weight: torch.Tensor, schedule=QUINTIC_SCHEDULE, stream=None,
+                    workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """One optimiser step in place: ``momentum`` and ``weight`` (float32) change, ``weight`` is returned."""
+    gp = _dev(grad, _TORCH_DTYPE[desc.dtype], desc.shape(), "grad")
+    mp = _dev(momentum, torch.float32, desc.shape(), "momentum")
+    wp = _dev(weight, torch.float32, desc.shape(), "weight")
+    steps, rows = _schedule(schedule)
+    ws, wsz = _call_workspace(workspace, lmkan_orthogonalize_workspace_bytes(desc), grad.device)
+    _check(lib().lmkan_muon_step(C.byref(desc.c()), C.byref(muon.c()), steps, rows.ctypes.data, gp, mp, wp, _ptr(ws),
+                                 wsz, _stream(stream)), "lmkan_muon_step")
+    _used_on(stream, ws)
+    return weight
+
+
+def lmkan_quantize_rows(x: torch.Tensor, relu: bool = False, stream=None):
+    """x [rows][cols] -> (codes int8 [rows][cols], scale float32 [rows])."""
+    if x.dim() != 2 or x.dtype not in _DTYPE_CODE:
+        raise ValueError(f"x: expected a matrix of float32, float16 or bfloat16, got {x.dtype} {tuple(x.shape)}")
+    rows, cols = x.shape
+    xp = _dev(x, x.dtype, (rows, cols), "x")
+    codes = torch.empty((rows, cols), dtype=torch.int8, device=x.device)
+    scale = torch.empty((rows,), dtype=torch.float32, device=x.device)
+    _check(lib().lmkan_quantize_rows(rows, cols, _DTYPE_CODE[x.dtype], LMKAN_LINEAR_RELU if relu else 0, xp,
+                                     codes.data_ptr(), scale.data_ptr(), _stream(stream)), "lmkan_quantize_rows")
+    _used_on(stream, codes, scale)
+    return codes, scale
+
+
+def lmkan_linear_i8_workspace_bytes(desc: LinearDesc, batch: int) -> int:
+    return lib().lmkan_linear_i8_workspace_bytes(C.byref(desc.c()), batch)
+
+
+def lmkan_linear_i8(desc: LinearDesc, x: torch.Tensor, w_codes: torch.Tensor, w_scale: torch.Tensor,
+                    bias: torch.Tensor | None = None, beta: float = 0.0, y: torch.Tensor | None = None, stream=None,
+                    workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """y = beta y + Linear(x) with rows quantised on the way and weights of ``lmkan_quantize_rows``."""
+    batch = x.shape[0]
+    xp = _dev(x, _TORCH_DTYPE[desc.x_dtype], (batch, desc.n_in), "x")
+    wp = _dev(w_codes, torch.int8, (desc.n_out, desc.n_in), "w_codes")
+    sp = _dev(w_scale, torch.float32, (desc.n_out,), "w_scale")
+    bp = _dev(bias, torch.float32, (desc.n_out,), "bias")
+    if y is None:
+        if beta != 0.0:
+            raise ValueError("beta != 0 adds to y: an existing y is needed")
+        y = torch.empty((batch, desc.n_out), dtype=_TORCH_DTYPE[desc.y_dtype], device=x.device)
+    yp = _dev(y, _TORCH_DTYPE[desc.y_dtype], (batch, desc.n_out), "y")
+    ws, wsz = _call_workspace(workspace, lmkan_linear_i8_workspace_bytes(desc, batch), x.device)
+    _check(lib().lmkan_linear_i8(C.byref(desc.c()), batch, xp, wp, sp, bp, beta, yp, _ptr(ws), wsz, _stream(stream)),
+           "lmkan_linear_i8")
+    _used_on(stream, ws, y)
+    return y

@@ -8,6 +8,7 @@
 #include <utility>
 
 #include "lmkan.h"
+#include "lmkan_dense.h"
 #include "lmkan_gather.h"
 #include "lmkan_kernels.h"
 #include "lmkan_sorted.h"
@@ -656,6 +657,131 @@ lmkan_status lmkan_fold(const lmkan_desc *desc, void *coef_dev, float gamma, con
     build_grid(desc->grid, &tab);
     launch_fold(shape_of(desc, 0), tab, static_cast<float *>(coef_dev), gamma, lin_w_dev, lin_b_dev, out_scale_dev,
                 out_shift_dev, static_cast<hipStream_t>(stream));
+    return launch_status();
+}
+
+}  // extern "C"
+
+namespace {
+
+bool known_dtype(int dtype) { return dtype == LMKAN_F32 || dtype == LMKAN_F16 || dtype == LMKAN_BF16; }
+
+lmkan_status check_matrices(const lmkan_matrices *d, MatrixShape *s)
+{
+    if (!d) return LMKAN_ERR_NULL;
+    if (d->batch < 0 || d->batch > LMKAN_MAX_BATCH || d->rows < 1 || d->cols < 1) return LMKAN_ERR_SHAPE;
+    *s = {d->batch, d->rows, d->cols, d->dtype, d->eps};
+    if (s->m() > LMKAN_MAX_MATRIX_SHORT || s->n() > LMKAN_MAX_MATRIX_LONG) return LMKAN_ERR_SHAPE;
+    if (!known_dtype(d->dtype) || !(d->eps > 0.0f) || !isfinite(d->eps)) return LMKAN_ERR_UNSUPPORTED;
+    return LMKAN_OK;
+}
+
+// the checks that the two calls on batches of matrices share
+lmkan_status ortho_impl(const lmkan_matrices *desc, int32_t steps, const float *schedule_host, const UpdateArgs &u,
+                        void *workspace_dev, size_t workspace_bytes, void *stream)
+{
+    MatrixShape s;
+    const lmkan_status st = check_matrices(desc, &s);
+    if (st != LMKAN_OK) return st;
+    if (steps < 0 || steps > LMKAN_MAX_ORTHO_STEPS) return LMKAN_ERR_SHAPE;
+    if (steps > 0 && !schedule_host) return LMKAN_ERR_NULL;
+    ScheduleBounds bounds;
+    if (!schedule_bounds(steps, schedule_host, &bounds)) return LMKAN_ERR_UNSUPPORTED;
+    if (s.batch == 0) return LMKAN_OK;
+    if (!u.grad || (u.momentum ? !u.weight : !u.out)) return LMKAN_ERR_NULL;
+    const size_t item = dtype_size(s.dtype);
+    if (!aligned(u.grad, item) || !aligned(u.out, item) || !aligned(u.momentum, 4) || !aligned(u.weight, 4))
+        return LMKAN_ERR_ALIGN;
+    if (!workspace_dev || workspace_bytes < ortho_workspace_bytes(s)) return LMKAN_ERR_WORKSPACE;
+    if (!aligned(workspace_dev, 256)) return LMKAN_ERR_ALIGN;
+    drop_stale_error();
+    launch_ortho(s, steps, schedule_host, u, workspace_dev, static_cast<hipStream_t>(stream));
+    return launch_status();
+}
+
+lmkan_status check_linear(const lmkan_linear *d, int64_t batch, LinearShape *s)
+{
+    if (!d) return LMKAN_ERR_NULL;
+    if (batch < 0 || batch > LMKAN_MAX_BATCH || d->n_in < 1 || d->n_in > LMKAN_MAX_N_IN || d->n_out < 1 ||
+        d->n_out > LMKAN_MAX_N_OUT)
+        return LMKAN_ERR_SHAPE;
+    if (!known_dtype(d->x_dtype) || !known_dtype(d->y_dtype) || (d->flags & ~LMKAN_LINEAR_RELU)) return LMKAN_ERR_UNSUPPORTED;
+    *s = {batch, d->n_in, d->n_out, d->x_dtype, d->y_dtype, (d->flags & LMKAN_LINEAR_RELU) != 0};
+    return LMKAN_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t lmkan_orthogonalize_workspace_bytes(const lmkan_matrices *desc)
+{
+    MatrixShape s;
+    return check_matrices(desc, &s) == LMKAN_OK && s.batch > 0 ? ortho_workspace_bytes(s) : 0;
+}
+
+lmkan_status lmkan_orthogonalize(const lmkan_matrices *desc, int32_t steps, const float *schedule_host,
+                                 const void *x_dev, void *out_dev, void *workspace_dev, size_t workspace_bytes,
+                                 void *stream)
+{
+    const UpdateArgs u{x_dev, nullptr, nullptr, out_dev, 0.0f, false, 0.0f, 0.0f};
+    return ortho_impl(desc, steps, schedule_host, u, workspace_dev, workspace_bytes, stream);
+}
+
+lmkan_status lmkan_muon_step(const lmkan_matrices *desc, const lmkan_muon *muon, int32_t steps,
+                             const float *schedule_host, const void *grad_dev, float *momentum_dev,
+                             float *weight_dev, void *workspace_dev, size_t workspace_bytes, void *stream)
+{
+    if (!muon) return LMKAN_ERR_NULL;
+    MatrixShape s;
+    const lmkan_status st = check_matrices(desc, &s);
+    if (st != LMKAN_OK) return st;
+    if (s.batch > 0 && (!momentum_dev || !weight_dev)) return LMKAN_ERR_NULL;
+    if (muon->nesterov != 0 && muon->nesterov != 1) return LMKAN_ERR_UNSUPPORTED;
+    const UpdateArgs u{grad_dev, momentum_dev, weight_dev, nullptr, muon->momentum, muon->nesterov != 0,
+                       (float)(1.0 - (double)muon->lr * (double)muon->weight_decay),
+                       (float)(-(double)muon->lr * (double)muon->scale)};
+    return ortho_impl(desc, steps, schedule_host, u, workspace_dev, workspace_bytes, stream);
+}
+
+lmkan_status lmkan_quantize_rows(int64_t rows, int32_t cols, int32_t x_dtype, int32_t flags, const void *x_dev,
+                                 int8_t *codes_dev, float *scale_dev, void *stream)
+{
+    if (rows < 0 || rows > LMKAN_MAX_BATCH || cols < 1 || cols > LMKAN_MAX_N_IN) return LMKAN_ERR_SHAPE;
+    if (!known_dtype(x_dtype) || (flags & ~LMKAN_LINEAR_RELU)) return LMKAN_ERR_UNSUPPORTED;
+    if (rows == 0) return LMKAN_OK;
+    if (!x_dev || !codes_dev || !scale_dev) return LMKAN_ERR_NULL;
+    if (!aligned(x_dev, dtype_size(x_dtype)) || !aligned(scale_dev, 4)) return LMKAN_ERR_ALIGN;
+    drop_stale_error();
+    launch_quantize_rows(rows, cols, x_dtype, (flags & LMKAN_LINEAR_RELU) != 0, x_dev, codes_dev, scale_dev,
+                         static_cast<hipStream_t>(stream));
+    return launch_status();
+}
+
+size_t lmkan_linear_i8_workspace_bytes(const lmkan_linear *desc, int64_t batch)
+{
+    LinearShape s;
+    return check_linear(desc, batch, &s) == LMKAN_OK && batch > 0 ? linear_i8_workspace_bytes(s) : 0;
+}
+
+lmkan_status lmkan_linear_i8(const lmkan_linear *desc, int64_t batch, const void *x_dev, const int8_t *w_codes_dev,
+                             const float *w_scale_dev, const float *bias_dev, float beta, void *y_dev,
+                             void *workspace_dev, size_t workspace_bytes, void *stream)
+{
+    LinearShape s;
+    const lmkan_status st = check_linear(desc, batch, &s);
+    if (st != LMKAN_OK) return st;
+    if (batch == 0) return LMKAN_OK;
+    if (!x_dev || !w_codes_dev || !w_scale_dev || !y_dev) return LMKAN_ERR_NULL;
+    if (!aligned(x_dev, dtype_size(s.x_dtype)) || !aligned(y_dev, dtype_size(s.y_dtype)) || !aligned(w_scale_dev, 4) ||
+        !aligned(bias_dev, 4))
+        return LMKAN_ERR_ALIGN;
+    const size_t need = linear_i8_workspace_bytes(s);
+    if (need > 0 && (!workspace_dev || workspace_bytes < need)) return LMKAN_ERR_WORKSPACE;
+    if (need > 0 && !aligned(workspace_dev, 256)) return LMKAN_ERR_ALIGN;
+    drop_stale_error();
+    launch_linear_i8(s, x_dev, w_codes_dev, w_scale_dev, bias_dev, beta, y_dev, workspace_dev,
+                     static_cast<hipStream_t>(stream));
     return launch_status();
 }
 

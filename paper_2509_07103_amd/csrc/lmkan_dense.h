@@ -1,0 +1,87 @@
+// Host-callable launchers of the dense companions of the layer (lmkan_ortho.hip, lmkan_linear.hip).
+// Every launcher enqueues on the given stream and returns; arguments have been validated by the caller.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "lmkan.h"
+
+namespace lmkan {
+
+// A batch of matrices seen with the shorter side first: m x n, the transpose of what is stored when `flip`.
+struct MatrixShape {
+    int64_t batch;
+    int rows, cols;
+    int dtype;
+    float eps;
+    __host__ __device__ bool flip() const { return rows > cols; }
+    __host__ __device__ int m() const { return rows > cols ? cols : rows; }
+    __host__ __device__ int n() const { return rows > cols ? rows : cols; }
+    __host__ __device__ int64_t elems() const { return (int64_t)rows * cols; }
+};
+
+// What a step does around the products: the update's direction from gradient and momentum, and the weights.
+// Plain orthogonalisation is the case without momentum (null) that writes `out`.
+struct UpdateArgs {
+    const void *grad;   // or x; in the shape's dtype
+    float *momentum;    // null: the direction is `grad` itself
+    float *weight;      // null: the result goes to `out`
+    void *out;          // in the shape's dtype
+    float beta;
+    bool nesterov;
+    float keep;         // W <- keep W + add O
+    float add;
+};
+
+// What the steps of a schedule can make of singular values in [0, 1]; false when a coefficient is not finite or
+// a step exceeds the limits below.
+constexpr double kMaxSingular = 4.0, kMaxFactor = 64.0;
+struct ScheduleBounds {
+    float singular[LMKAN_MAX_ORTHO_STEPS + 1];  // largest singular value before step k (and after the last)
+    float factor[LMKAN_MAX_ORTHO_STEPS];        // largest |a + b s^2 + c s^4| of step k
+};
+bool schedule_bounds(int steps, const float *schedule, ScheduleBounds *bounds);
+
+size_t ortho_workspace_bytes(const MatrixShape &s);
+void launch_ortho(const MatrixShape &s, int steps, const float *schedule, const UpdateArgs &u, void *workspace,
+                  hipStream_t stream);
+
+struct LinearShape {
+    int64_t batch;
+    int n_in, n_out;
+    int x_dtype, y_dtype;
+    bool relu;
+};
+
+void launch_quantize_rows(int64_t rows, int cols, int dtype, bool relu, const void *x, int8_t *codes, float *scale,
+                          hipStream_t stream);
+size_t linear_i8_workspace_bytes(const LinearShape &s);
+void launch_linear_i8(const LinearShape &s, const void *x, const int8_t *w, const float *w_scale, const float *bias,
+                      float beta, void *y, void *workspace, hipStream_t stream);
+
+// Element types by their lmkan_dtype
+__device__ __forceinline__ float load_as_float(const void *p, int64_t i, int dtype)
+{
+    if (dtype == LMKAN_F32) return static_cast<const float *>(p)[i];
+    const uint16_t b = static_cast<const uint16_t *>(p)[i];
+    if (dtype == LMKAN_F16) return (float)__builtin_bit_cast(_Float16, b);
+    return __builtin_bit_cast(float, (uint32_t)b << 16);
+}
+
+// float32 -> bfloat16, to nearest, ties to even; NaN stays NaN
+__device__ __forceinline__ uint16_t bf16_bits(float v)
+{
+    const uint32_t u = __builtin_bit_cast(uint32_t, v);
+    if ((u & 0x7fffffffu) > 0x7f800000u) return (uint16_t)((u >> 16) | 0x40);
+    return (uint16_t)((u + 0x7fffu + ((u >> 16) & 1)) >> 16);
+}
+
+__device__ __forceinline__ void store_from_float(void *p, int64_t i, int dtype, float v)
+{
+    if (dtype == LMKAN_F32) static_cast<float *>(p)[i] = v;
+    else if (dtype == LMKAN_F16) static_cast<uint16_t *>(p)[i] = __builtin_bit_cast(uint16_t, (_Float16)v);
+    else static_cast<uint16_t *>(p)[i] = bf16_bits(v);
+}
+
+}  // namespace lmkan

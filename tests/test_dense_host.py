@@ -1,0 +1,125 @@
+"""Refusals of the calls on dense matrices, found on the host before anything is launched."""
+import ctypes as C
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2509_07103_amd as pkg
+from paper_2509_07103_amd import binding
+
+OK, NULL, SHAPE, UNSUPPORTED, WORKSPACE, ALIGN = 0, 1, 2, 3, 4, 5
+FAKE = C.c_void_p(0x1000)   # never dereferenced: validation comes first
+BIG = C.c_size_t(1 << 60)
+
+
+def _schedule(rows):
+    a = np.ascontiguousarray(np.asarray(rows, dtype=np.float32).reshape(-1, 3))
+    return a.shape[0], a
+
+
+def _ortho(desc=None, schedule=pkg.QUINTIC_SCHEDULE, x=FAKE, out=FAKE, ws=FAKE, nbytes=BIG, **kw):
+    d = (desc or pkg.MatrixDesc(**{**dict(batch=2, rows=8, cols=8), **kw})).c()
+    steps, rows = _schedule(schedule)
+    return pkg.lib().lmkan_orthogonalize(C.byref(d), steps, rows.ctypes.data if steps else None, x, out, ws, nbytes, None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(batch=-1), SHAPE), (dict(rows=0), SHAPE), (dict(cols=0), SHAPE), (dict(rows=16385, cols=16385), SHAPE),
+    (dict(rows=1, cols=(1 << 26) + 1), SHAPE), (dict(dtype=3), UNSUPPORTED), (dict(eps=0.0), UNSUPPORTED),
+    (dict(eps=-1.0), UNSUPPORTED), (dict(eps=float("nan")), UNSUPPORTED), (dict(eps=float("inf")), UNSUPPORTED),
+    (dict(x=None), NULL), (dict(out=None), NULL), (dict(ws=None), WORKSPACE), (dict(nbytes=C.c_size_t(0)), WORKSPACE),
+    (dict(ws=C.c_void_p(0x1010)), ALIGN), (dict(x=C.c_void_p(0x1002)), ALIGN), (dict(out=C.c_void_p(0x1001)), ALIGN),
+    (dict(x=C.c_void_p(0x1001), dtype=pkg.LMKAN_BF16), ALIGN),
+    (dict(schedule=[(1.5, -0.5, float("nan"))]), UNSUPPORTED), (dict(schedule=[(float("inf"), 0, 0)]), UNSUPPORTED),
+    (dict(schedule=[(5.0, 0.0, 0.0)]), UNSUPPORTED),             # singular values beyond 4
+    (dict(schedule=[(2.0, 0.0, 0.0)] * 3), UNSUPPORTED),         # after three steps
+    (dict(schedule=[(70.0, -280.0, 220.0)]), UNSUPPORTED),       # a factor beyond 64
+    (dict(schedule=[(1.5, -0.5, 0.0)] * 33), SHAPE),
+])
+def test_orthogonalize_refuses(kw, status):
+    assert _ortho(**kw) == status
+
+
+def test_missing_descriptors_and_schedules():
+    L = pkg.lib()
+    d, m = pkg.MatrixDesc(2, 8, 8).c(), pkg.MuonParams(0.1).c()
+    assert L.lmkan_orthogonalize(None, 0, None, FAKE, FAKE, FAKE, BIG, None) == NULL
+    assert L.lmkan_orthogonalize(C.byref(d), 3, None, FAKE, FAKE, FAKE, BIG, None) == NULL
+    assert L.lmkan_orthogonalize(C.byref(d), -1, None, FAKE, FAKE, FAKE, BIG, None) == SHAPE
+    assert L.lmkan_muon_step(C.byref(d), None, 0, None, FAKE, FAKE, FAKE, FAKE, BIG, None) == NULL
+    assert L.lmkan_muon_step(None, C.byref(m), 0, None, FAKE, FAKE, FAKE, FAKE, BIG, None) == NULL
+    assert L.lmkan_orthogonalize_workspace_bytes(None) == 0
+    assert L.lmkan_linear_i8_workspace_bytes(None, 4) == 0
+
+
+def _muon(grad=FAKE, momentum=FAKE, weight=FAKE, nesterov=1, **kw):
+    d = pkg.MatrixDesc(**{**dict(batch=2, rows=8, cols=8), **kw}).c()
+    m = binding._Muon(0.1, 0.9, 0.0, 1.0, nesterov)
+    return pkg.lib().lmkan_muon_step(C.byref(d), C.byref(m), 0, None, grad, momentum, weight, FAKE, BIG, None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(grad=None), NULL), (dict(momentum=None), NULL), (dict(weight=None), NULL), (dict(nesterov=2), UNSUPPORTED),
+    (dict(momentum=C.c_void_p(0x1002)), ALIGN), (dict(weight=C.c_void_p(0x1002)), ALIGN), (dict(rows=-4), SHAPE),
+])
+def test_muon_step_refuses(kw, status):
+    assert _muon(**kw) == status
+
+
+def test_empty_batches_need_nothing():
+    L = pkg.lib()
+    d, m, l = pkg.MatrixDesc(0, 8, 8).c(), pkg.MuonParams(0.1).c(), pkg.LinearDesc(8, 4).c()
+    assert L.lmkan_orthogonalize(C.byref(d), 0, None, None, None, None, 0, None) == OK
+    assert L.lmkan_muon_step(C.byref(d), C.byref(m), 0, None, None, None, None, None, 0, None) == OK
+    assert L.lmkan_linear_i8(C.byref(l), 0, None, None, None, None, 0.0, None, None, 0, None) == OK
+    assert L.lmkan_quantize_rows(0, 8, 0, 0, None, None, None, None) == OK
+    assert L.lmkan_orthogonalize_workspace_bytes(C.byref(d)) == 0
+    assert L.lmkan_linear_i8_workspace_bytes(C.byref(l), 0) == 0
+
+
+@pytest.mark.parametrize("kw,batch,status", [
+    (dict(n_in=0), 4, SHAPE), (dict(n_in=131071), 4, SHAPE), (dict(n_out=0), 4, SHAPE), (dict(n_out=4194241), 4, SHAPE),
+    (dict(), -1, SHAPE), (dict(), 1 << 31, SHAPE), (dict(x_dtype=5), 4, UNSUPPORTED), (dict(y_dtype=-1), 4, UNSUPPORTED),
+])
+def test_linear_i8_refuses_shapes_and_types(kw, batch, status):
+    d = pkg.LinearDesc(**{**dict(n_in=8, n_out=4), **kw}).c()
+    assert pkg.lib().lmkan_linear_i8(C.byref(d), batch, FAKE, FAKE, FAKE, None, 0.0, FAKE, FAKE, BIG, None) == status
+    assert pkg.lib().lmkan_linear_i8_workspace_bytes(C.byref(d), batch) == 0
+
+
+def test_linear_i8_and_quantize_refuse_pointers_and_flags():
+    L = pkg.lib()
+    odd, d = C.c_void_p(0x1001), pkg.LinearDesc(8, 4).c()
+
+    def call(x=FAKE, w=FAKE, ws=FAKE, bias=None, y=FAKE):
+        return L.lmkan_linear_i8(C.byref(d), 4, x, w, ws, bias, 0.0, y, FAKE, BIG, None)
+    assert [call(x=None), call(w=None), call(ws=None), call(y=None)] == [NULL] * 4
+    assert [call(x=odd), call(ws=odd), call(y=odd), call(bias=odd)] == [ALIGN] * 4
+    flagged = binding._Linear(8, 4, 0, 0, 2)
+    assert L.lmkan_linear_i8(C.byref(flagged), 4, FAKE, FAKE, FAKE, None, 0.0, FAKE, FAKE, BIG, None) == UNSUPPORTED
+    assert L.lmkan_quantize_rows(4, 0, 0, 0, FAKE, FAKE, FAKE, None) == SHAPE
+    assert L.lmkan_quantize_rows(-1, 8, 0, 0, FAKE, FAKE, FAKE, None) == SHAPE
+    assert L.lmkan_quantize_rows(4, 131071, 0, 0, FAKE, FAKE, FAKE, None) == SHAPE
+    assert L.lmkan_quantize_rows(4, 8, 9, 0, FAKE, FAKE, FAKE, None) == UNSUPPORTED
+    assert L.lmkan_quantize_rows(4, 8, 0, 2, FAKE, FAKE, FAKE, None) == UNSUPPORTED
+    assert L.lmkan_quantize_rows(4, 8, 0, 0, None, FAKE, FAKE, None) == NULL
+    assert L.lmkan_quantize_rows(4, 8, 0, 0, odd, FAKE, FAKE, None) == ALIGN
+    assert L.lmkan_quantize_rows(4, 8, 0, 0, FAKE, FAKE, odd, None) == ALIGN
+
+
+def test_python_refuses_tensors_that_do_not_fit():
+    x = torch.zeros((2, 8, 8))
+    with pytest.raises(ValueError):
+        pkg.lmkan_orthogonalize(pkg.MatrixDesc(2, 8, 8), x)                      # not on the device
+    with pytest.raises(ValueError):
+        pkg.lmkan_muon_step(pkg.MatrixDesc(2, 8, 8), pkg.MuonParams(0.1), x, x, x)
+    with pytest.raises(ValueError):
+        pkg.lmkan_quantize_rows(torch.zeros((2, 8), dtype=torch.float64))
+    with pytest.raises(ValueError):
+        pkg.lmkan_linear_i8(pkg.LinearDesc(8, 4), torch.zeros((2, 8)), torch.zeros((4, 8), dtype=torch.int8), torch.ones(4))
+
+
+def test_workspace_of_large_batches_is_bounded():
+    """A table of 1089 matrices of 2048 x 4096 is worked on in parts."""
+    assert 0 < pkg.lmkan_orthogonalize_workspace_bytes(pkg.MatrixDesc(1089, 2048, 4096)) < 8 << 30
