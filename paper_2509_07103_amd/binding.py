@@ -6,13 +6,14 @@ the current stream.  There is no CPU fallback: if the library is missing or a
 call fails, an exception is raised.
 
 The calls that a program makes per step (forward, backward, pack, the
-convolution) first go to ``_native`` (csrc/lmkan_torch.cpp), which does the same
+convolution, the optimiser's step, the linear term) first go to ``_native`` (csrc/lmkan_torch.cpp), which does the same
 marshalling in native code for the ordinary case and returns None for any
 other; the code here then takes over and raises what there is to raise.
 """
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from dataclasses import dataclass
 
@@ -229,7 +230,8 @@ def lib() -> C.CDLL:
     from . import _native as native   # ImportError when it has not been built
     native.init(*(C.cast(f, C.c_void_p).value for f in (
         L.lmkan_workspace_bytes, L.lmkan_packed_bytes, L.lmkan_forward, L.lmkan_backward, L.lmkan_conv2d_rows,
-        L.lmkan_conv2d_forward, L.lmkan_conv2d_backward, L.lmkan_pack)))
+        L.lmkan_conv2d_forward, L.lmkan_conv2d_backward, L.lmkan_pack, L.lmkan_orthogonalize_workspace_bytes,
+        L.lmkan_orthogonalize, L.lmkan_muon_step, L.lmkan_linear_i8_workspace_bytes, L.lmkan_linear_i8)))
     _native = native
     _lib = L
     return L
@@ -537,10 +539,14 @@ def lmkan_fold(desc: LayerDesc, coef: torch.Tensor, gamma: float = 1.0, lin_w: t
     return coef
 
 
-def _schedule(schedule):
-    """(steps, float32 array [steps][3]) of a sequence of (a, b, c)."""
-    rows = np.asarray(schedule, dtype=np.float32).reshape(-1, 3)
-    return rows.shape[0], np.ascontiguousarray(rows)
+@functools.lru_cache(maxsize=64)
+def _schedule_bytes(schedule: tuple) -> bytes:
+    return np.ascontiguousarray(np.asarray(schedule, dtype=np.float32).reshape(-1, 3)).tobytes()
+
+
+def _schedule(schedule) -> bytes:
+    """float32 [steps][3] of a sequence of (a, b, c)."""
+    return _schedule_bytes(tuple(tuple(float(v) for v in row) for row in schedule))
 
 
 def _call_workspace(workspace: torch.Tensor | None, need: int, device):
@@ -564,14 +570,18 @@ def lmkan_orthogonalize(desc: MatrixDesc, x: torch.Tensor, schedule=QUINTIC_SCHE
                         stream=None, workspace: torch.Tensor | None = None) -> torch.Tensor:
     """Each matrix of x [batch][rows][cols] brought near orthonormal rows (columns when rows > cols) by
     Newton-Schulz steps, one (a, b, c) of ``schedule`` each; ``out`` may be ``x``."""
+    rows = _schedule(schedule)
+    if stream is None:
+        done = (_native or _fast()).orthogonalize(desc, rows, x, out, workspace)
+        if done is not None:
+            return done
     dt = _TORCH_DTYPE[desc.dtype]
     xp = _dev(x, dt, desc.shape(), "x")
     if out is None:
         out = torch.empty(desc.shape(), dtype=dt, device=x.device)
     op = _dev(out, dt, desc.shape(), "out")
-    steps, rows = _schedule(schedule)
     ws, wsz = _call_workspace(workspace, lmkan_orthogonalize_workspace_bytes(desc), x.device)
-    _check(lib().lmkan_orthogonalize(C.byref(desc.c()), steps, rows.ctypes.data, xp, op, _ptr(ws), wsz, _stream(stream)),
+    _check(lib().lmkan_orthogonalize(C.byref(desc.c()), len(rows) // 12, rows, xp, op, _ptr(ws), wsz, _stream(stream)),
            "lmkan_orthogonalize")
     _used_on(stream, ws, out)
     return out
@@ -581,12 +591,16 @@ def lmkan_muon_step(desc: MatrixDesc, muon: MuonParams, grad: torch.Tensor, mome
                     weight: torch.Tensor, schedule=QUINTIC_SCHEDULE, stream=None,
                     workspace: torch.Tensor | None = None) -> torch.Tensor:
     """One optimiser step in place: ``momentum`` and ``weight`` (float32) change, ``weight`` is returned."""
+    rows = _schedule(schedule)
+    if stream is None:
+        done = (_native or _fast()).muon_step(desc, muon, rows, grad, momentum, weight, workspace)
+        if done is not None:
+            return done
     gp = _dev(grad, _TORCH_DTYPE[desc.dtype], desc.shape(), "grad")
     mp = _dev(momentum, torch.float32, desc.shape(), "momentum")
     wp = _dev(weight, torch.float32, desc.shape(), "weight")
-    steps, rows = _schedule(schedule)
     ws, wsz = _call_workspace(workspace, lmkan_orthogonalize_workspace_bytes(desc), grad.device)
-    _check(lib().lmkan_muon_step(C.byref(desc.c()), C.byref(muon.c()), steps, rows.ctypes.data, gp, mp, wp, _ptr(ws),
+    _check(lib().lmkan_muon_step(C.byref(desc.c()), C.byref(muon.c()), len(rows) // 12, rows, gp, mp, wp, _ptr(ws),
                                  wsz, _stream(stream)), "lmkan_muon_step")
     _used_on(stream, ws)
     return weight
@@ -614,6 +628,10 @@ def lmkan_linear_i8(desc: LinearDesc, x: torch.Tensor, w_codes: torch.Tensor, w_
                     bias: torch.Tensor | None = None, beta: float = 0.0, y: torch.Tensor | None = None, stream=None,
                     workspace: torch.Tensor | None = None) -> torch.Tensor:
     """y = beta y + Linear(x) with rows quantised on the way and weights of ``lmkan_quantize_rows``."""
+    if stream is None:
+        done = (_native or _fast()).linear_i8(desc, x, w_codes, w_scale, bias, beta, y, workspace)
+        if done is not None:
+            return done
     batch = x.shape[0]
     xp = _dev(x, _TORCH_DTYPE[desc.x_dtype], (batch, desc.n_in), "x")
     wp = _dev(w_codes, torch.int8, (desc.n_out, desc.n_in), "w_codes")

@@ -84,4 +84,12 @@ __device__ __forceinline__ void store_from_float(void *p, int64_t i, int dtype, 
     else static_cast<uint16_t *>(p)[i] = bf16_bits(v);
 }
 
+// two adjacent 16-bit elements, the first in the lower half
+__device__ __forceinline__ uint32_t two_from_float(int dtype, float a, float b)
+{
+    if (dtype == LMKAN_F16)
+        return (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)a) | (uint32_t)__builtin_bit_cast(uint16_t, (_Float16)b) << 16;
+    return (uint32_t)bf16_bits(a) | (uint32_t)bf16_bits(b) << 16;
+}
+
 }  // namespace lmkan

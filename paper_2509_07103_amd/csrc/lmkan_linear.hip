@@ -1,102 +1,555 @@
 // The linear term in 8-bit whole numbers: rows scaled to codes one by one, products of codes summed exactly,
 //   y = beta y + xscale wscale sum(xcode wcode) + bias.
+//
+// Three kernels.  quantize_kernel reads rows once and writes codes and scales.  linear_kernel multiplies tiles of codes
+// on the matrix cores (lmkan_tile.h); few tiles with a long summed axis are cut along it and joined.  few_rows_kernel
+// answers single rows: it is bound by reading the weights, which every wave has on their way before it scales the rows.
 #include "lmkan_dense.h"
+
+#include "lmkan_kernels.h"
+#include "lmkan_tile.h"
 
 namespace lmkan {
 
 namespace {
 
-// A wave per row.  The largest magnitude is found on the bits (ordered like the values for non-negative
-// floats, NaN above infinity), so that a row with a NaN or an infinity ends with a scale that is not finite.
-__global__ __launch_bounds__(256) void quantize_kernel(int64_t rows, int cols, int dtype, bool relu, const void *x, int8_t *codes, float *scale)
+// ---- rows to codes ---------------------------------------------------------------------------------------------------
+
+// What scales a row to codes, and the codes back: from the bits of its largest magnitude (ordered like the values for
+// non-negative floats, NaN above infinity).  A row with a NaN or an infinity ends with a scale that is not finite.
+struct RowScale {
+    float factor, scale;
+    bool finite;
+    __device__ __forceinline__ explicit RowScale(uint32_t top)
+    {
+        const float r = __builtin_bit_cast(float, top), f = 127.0f / r;
+        finite = top < 0x7f800000u;
+        factor = finite && f < __builtin_inff() ? f : 0.0f;
+        scale = r / 127.0f;
+    }
+    __device__ __forceinline__ int code(float v) const { return finite ? (int)rintf(v * factor) : 0; }
+};
+
+__device__ __forceinline__ uint32_t magnitude(float v) { return __builtin_bit_cast(uint32_t, v) & 0x7fffffffu; }
+__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return a > b ? a : b; }
+__device__ __forceinline__ float rectified(float v, bool relu) { return relu && v < 0.0f ? 0.0f : v; }
+
+__device__ __forceinline__ uint32_t wave_max(uint32_t v)
 {
-    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (row >= rows) return;
-    const int lane = threadIdx.x & 63;
-    const auto value = [&](int e) {
-        const float v = load_as_float(x, row * cols + e, dtype);
-        return relu && v < 0.0f ? 0.0f : v;
-    };
-    uint32_t top = 0;
-    for (int e = lane; e < cols; e += 64) {
-        const uint32_t b = __builtin_bit_cast(uint32_t, value(e)) & 0x7fffffffu;
-        top = b > top ? b : top;
-    }
-    for (int d = 32; d > 0; d >>= 1) {
-        const uint32_t o = (uint32_t)__shfl_xor((int)top, d, 64);
-        top = o > top ? o : top;
-    }
-    const float r = __builtin_bit_cast(float, top);
-    const bool finite = top < 0x7f800000u;
-    const float f = finite && 127.0f / r < INFINITY ? 127.0f / r : 0.0f;
-    for (int e = lane; e < cols; e += 64) codes[row * cols + e] = finite ? (int8_t)(int)rintf(value(e) * f) : (int8_t)0;
-    if (lane == 0) scale[row] = r / 127.0f;
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) v = larger(v, (uint32_t)__shfl_xor((int)v, d, 64));
+    return v;
 }
 
-constexpr int kTile = 32, kDepth = 64;
+__device__ __forceinline__ uint32_t packed(const int (&c)[4])
+{
+    return (uint32_t)(c[0] & 255) | (uint32_t)(c[1] & 255) << 8 | (uint32_t)(c[2] & 255) << 16 | (uint32_t)(c[3] & 255) << 24;
+}
 
-struct Args {
-    const int8_t *x;
-    const float *x_scale;
-    const int8_t *w;
-    const float *w_scale, *bias;
+// four adjacent elements; `whole`: they exist and are aligned to their size together
+template <int DTYPE>
+__device__ __forceinline__ void load_four(const void *x, int64_t at, int left, bool whole, float (&v)[4])
+{
+    if (whole) {
+        if (DTYPE == LMKAN_F32) {
+            const float4 f = *reinterpret_cast<const float4 *>(static_cast<const float *>(x) + at);
+            v[0] = f.x, v[1] = f.y, v[2] = f.z, v[3] = f.w;
+        } else {
+            const uint2 u = *reinterpret_cast<const uint2 *>(static_cast<const uint16_t *>(x) + at);
+            const uint16_t b[4] = {(uint16_t)u.x, (uint16_t)(u.x >> 16), (uint16_t)u.y, (uint16_t)(u.y >> 16)};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = load_as_float(b, e, DTYPE);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = e < left ? load_as_float(x, at + e, DTYPE) : 0.0f;
+    }
+}
+
+constexpr int kHeld = 8;   // fours of a row that a thread keeps; longer rows are read again (from the L2)
+
+struct QuantizeArgs {
+    int64_t rows;
+    int cols, pitch;   // pitch: bytes from one row of codes to the next; what lies between is zeroed when `pad`
+    bool relu, pad, by_four, codes_by_four;
+    const void *x;
+    int8_t *codes;
+    float *scale;
+};
+
+// LANES threads a row (a wave, or a workgroup of 256)
+template <int DTYPE, int LANES>
+__global__ __launch_bounds__(256) void quantize_kernel(QuantizeArgs a)
+{
+    __shared__ uint32_t tops[4];
+    const int64_t row = LANES == 64 ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
+    if (LANES == 64 && row >= a.rows) return;
+    const int t = LANES == 64 ? threadIdx.x & 63 : threadIdx.x;
+    const int fours = (a.cols + 3) / 4;
+    float v[kHeld][4];
+    uint32_t top = 0;
+    const auto load = [&](int f, float (&to)[4]) {
+        const int left = a.cols - 4 * f;
+        load_four<DTYPE>(a.x, row * a.cols + 4 * f, left, a.by_four && left >= 4, to);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) to[e] = rectified(to[e], a.relu);
+    };
+    const auto see = [&](const float (&from)[4]) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) top = larger(top, magnitude(from[e]));
+    };
+#pragma unroll
+    for (int h = 0; h < kHeld; ++h)
+        if (t + h * LANES < fours) load(t + h * LANES, v[h]);
+#pragma unroll
+    for (int h = 0; h < kHeld; ++h)
+        if (t + h * LANES < fours) see(v[h]);
+    for (int f = t + kHeld * LANES; f < fours; f += LANES) {
+        float w[4];
+        load(f, w);
+        see(w);
+    }
+    top = wave_max(top);
+    if (LANES == 256) {
+        if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
+        __syncthreads();
+        top = larger(larger(tops[0], tops[1]), larger(tops[2], tops[3]));
+    }
+    const RowScale s(top);
+    int8_t *to = a.codes + row * a.pitch;
+    const auto store = [&](int f, const float (&from)[4]) {
+        int c[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c[e] = s.code(from[e]);
+        if (a.codes_by_four) {
+            *reinterpret_cast<uint32_t *>(to + 4 * f) = packed(c);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (4 * f + e < a.cols) to[4 * f + e] = (int8_t)c[e];
+        }
+    };
+#pragma unroll
+    for (int h = 0; h < kHeld; ++h)
+        if (t + h * LANES < fours) store(t + h * LANES, v[h]);
+    for (int f = t + kHeld * LANES; f < fours; f += LANES) {
+        float w[4];
+        load(f, w);
+        store(f, w);
+    }
+    if (a.pad)
+        for (int f = fours + t; f < a.pitch / 4; f += LANES) *reinterpret_cast<uint32_t *>(to + 4 * f) = 0;
+    if (t == 0) a.scale[row] = s.scale;
+}
+
+// ---- products of tiles -----------------------------------------------------------------------------------------------
+
+constexpr int kPitch = 36;                                // floats of a row of a wave's tile in LDS
+constexpr int kWaveScratch = 32 * kPitch * (int)sizeof(float);
+
+struct LinearArgs {
+    const int8_t *x, *w;       // codes
+    int64_t x_pitch, w_pitch;
+    const float *x_scale, *w_scale, *bias;
     float beta;
     void *y;
     int64_t batch;
     int n_in, n_out, y_dtype;
+    bool by_four;              // rows of y take accesses of four elements
+    int tiles_across;
+    WorkSplit work;
+    intx4 *parts;
 };
 
-__global__ __launch_bounds__(256) void linear_kernel(Args a)
+template <class T>
+__device__ __forceinline__ void finish_tile(const LinearArgs &a, int64_t tile, const intx4 (&acc)[T::CT][T::RT], char *scratch, int wave)
 {
-    __shared__ int8_t l[kTile][kDepth + 4], r[kTile][kDepth + 4];
-    const unsigned across = (unsigned)((a.n_out + kTile - 1) / kTile);
-    const int64_t i0 = (int64_t)(blockIdx.x / across) * kTile;
-    const int j0 = (int)(blockIdx.x % across) * kTile, tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
-    int acc[4] = {};
-    for (int k0 = 0; k0 < a.n_in; k0 += kDepth) {
-        for (int e = threadIdx.x; e < kTile * kDepth; e += 256) {
-            const int k = e & (kDepth - 1), i = e / kDepth;
-            l[i][k] = i0 + i < a.batch && k0 + k < a.n_in ? a.x[(i0 + i) * a.n_in + k0 + k] : (int8_t)0;
-            r[i][k] = j0 + i < a.n_out && k0 + k < a.n_in ? a.w[(int64_t)(j0 + i) * a.n_in + k0 + k] : (int8_t)0;
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));   // (the addresses below are worked out here, not kept in registers through the main loop)
+    const int r = lane & 15, q = lane >> 4;
+    const int64_t ti = tile / a.tiles_across;
+    const int64_t i0 = ti * T::ROWS;
+    const int j0 = (int)(tile - ti * a.tiles_across) * T::COLS;
+    for_wave_tiles<T>(acc, wave, [&](int row, int col, const intx4 (&v)[4]) {
+        if (i0 + row >= a.batch || j0 + col >= a.n_out) return;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) *reinterpret_cast<intx4 *>(scratch + ((16 * (g >> 1) + r) * kPitch + 16 * (g & 1) + 4 * q) * 4) = v[g];
+        const int j = j0 + col + (lane & 7) * 4;
+        float ws[4], b[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const bool in = j + e < a.n_out;
+            ws[e] = in ? a.w_scale[j + e] : 0.0f;
+            b[e] = in && a.bias ? a.bias[j + e] : 0.0f;
         }
-        __syncthreads();
-        for (int k = 0; k < kDepth; ++k)
-            for (int p = 0; p < 4; ++p) acc[p] += (int)l[ty * 4 + p][k] * (int)r[tx][k];
-        __syncthreads();
-    }
-    for (int p = 0; p < 4; ++p) {
-        const int64_t i = i0 + ty * 4 + p;
-        const int j = j0 + tx;
-        if (i >= a.batch || j >= a.n_out) continue;
-        float v = (float)acc[p] * (a.x_scale[i] * a.w_scale[j]) + (a.bias ? a.bias[j] : 0.0f);
-        if (a.beta != 0.0f) v += a.beta * load_as_float(a.y, i * a.n_out + j, a.y_dtype);
-        store_from_float(a.y, i * a.n_out + j, a.y_dtype, v);
-    }
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const int64_t i = i0 + row + 8 * t + (lane >> 3);
+            const intx4 sum = *reinterpret_cast<const intx4 *>(scratch + ((8 * t + (lane >> 3)) * kPitch + (lane & 7) * 4) * 4);
+            if (i >= a.batch || j >= a.n_out) continue;
+            const float xs = a.x_scale[i];
+            const int64_t at = i * a.n_out + j;
+            float o[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = (float)sum[e] * (xs * ws[e]) + b[e];
+            if (a.by_four) {
+                if (a.y_dtype == LMKAN_F32) {
+                    float4 *to = reinterpret_cast<float4 *>(static_cast<float *>(a.y) + at);
+                    if (a.beta != 0.0f) {
+                        const float4 k = *to;
+                        o[0] += a.beta * k.x, o[1] += a.beta * k.y, o[2] += a.beta * k.z, o[3] += a.beta * k.w;
+                    }
+                    *to = make_float4(o[0], o[1], o[2], o[3]);
+                } else {
+                    uint2 *to = reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.y) + at);
+                    if (a.beta != 0.0f) {
+                        const uint2 k = *to;
+                        const uint16_t h[4] = {(uint16_t)k.x, (uint16_t)(k.x >> 16), (uint16_t)k.y, (uint16_t)(k.y >> 16)};
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[e] += a.beta * load_as_float(h, e, a.y_dtype);
+                    }
+                    *to = make_uint2(two_from_float(a.y_dtype, o[0], o[1]), two_from_float(a.y_dtype, o[2], o[3]));
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (j + e < a.n_out) {
+                        if (a.beta != 0.0f) o[e] += a.beta * load_as_float(a.y, at + e, a.y_dtype);
+                        store_from_float(a.y, at + e, a.y_dtype, o[e]);
+                    }
+            }
+        }
+    });
 }
 
+template <class T>
+__global__ __launch_bounds__(T::THREADS) void linear_kernel(LinearArgs a)
+{
+    extern __shared__ __align__(16) char lds[];
+    for_work(a.work, blockIdx.x, [&](int64_t tile, int from, int to, int slot) {
+        const int64_t ti = tile / a.tiles_across, i0 = ti * T::ROWS;
+        const int j0 = (int)(tile - ti * a.tiles_across) * T::COLS;
+        const int64_t last = a.batch - 1 - i0;
+        const Operand x{reinterpret_cast<const char *>(uniform(a.x + i0 * a.x_pitch)), kLine, uniform((int)(last < T::ROWS ? last : T::ROWS)), false,
+                        (unsigned)a.x_pitch, (int)a.x_pitch - 16};
+        const Operand w{reinterpret_cast<const char *>(uniform(a.w + j0 * a.w_pitch)), kLine, uniform(a.n_out - 1 - j0), false, (unsigned)a.w_pitch,
+                        (int)a.w_pitch - 16};
+        intx4 acc[T::CT][T::RT];
+        multiply<T, CodeProduct>(x, w, from, to, lds, acc);
+        __syncthreads();
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        if (slot < 0) finish_tile<T>(a, tile, acc, lds + wave * kWaveScratch, wave);
+        else store_part<T>(a.parts, slot, acc);
+        __syncthreads();
+    });
+}
+
+// A wave's share of a tile that was cut, a workgroup each
+template <class T>
+__global__ __launch_bounds__(64) void linear_join_kernel(LinearArgs a)
+{
+    __shared__ __align__(16) char lds[kWaveScratch];
+    const int tile = blockIdx.x / T::WAVES, wave = blockIdx.x % T::WAVES;
+    intx4 acc[T::CT][T::RT];
+    if (!join_parts<T>(a.work, tile, wave, a.parts, acc)) return;
+    finish_tile<T>(a, a.work.whole + tile, acc, lds, wave);
+}
+
+// Weights whose rows are not a multiple of 16 bytes, or start anywhere, to rows that are; a dword a thread
+__global__ __launch_bounds__(256) void align_kernel(const int8_t *w, int n_in, int n_out, int pitch, int8_t *to)
+{
+    const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t row = e / (pitch / 4);
+    const int k = (int)(e - row * (pitch / 4)) * 4;
+    if (row >= n_out) return;
+    int c[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c[i] = k + i < n_in ? w[row * n_in + k + i] : 0;
+    *reinterpret_cast<uint32_t *>(to + row * pitch + k) = packed(c);
+}
+
+// ---- few rows --------------------------------------------------------------------------------------------------------
+
+constexpr int kMostRows = 4;             // rows of a call that few_rows_kernel takes
+constexpr int kMostCodes = 48 * 1024;    // bytes of LDS for their codes
+constexpr int kFewHeld = 4;              // fours of a row that a thread keeps
+
+struct FewArgs {
+    const void *x;
+    const int8_t *w;
+    const float *w_scale, *bias;
+    float beta;
+    void *y;
+    int n_in, n_out, x_dtype, y_dtype;
+    bool relu, w_aligned, x_by_four;
+    int padded;                          // n_in rounded up to the codes that a wave reads at a time
+};
+
+// 16 codes of a row from k on, zero beyond its end
+__device__ __forceinline__ intx4 load_codes(const int8_t *row, int k, int n_in, bool aligned)
+{
+    if (k + 16 <= n_in) {
+        if (aligned) return *reinterpret_cast<const intx4 *>(row + k);
+        intx4 v;
+        __builtin_memcpy(&v, row + k, 16);
+        return v;
+    }
+    intx4 v = {0, 0, 0, 0};
+    for (int e = 0; k + e < n_in; ++e) v[e >> 2] |= (int)((uint32_t)(uint8_t)row[k + e] << (8 * (e & 3)));
+    return v;
+}
+
+// A wave takes OUTS outputs of all ROWS rows; CHUNKS pieces of 1024 codes of each output are on their way at a time.
+template <int DTYPE, int ROWS, int OUTS, int CHUNKS>
+__global__ __launch_bounds__(256) void few_rows_kernel(FewArgs a)
+{
+    extern __shared__ __align__(16) char lds[];
+    __shared__ uint32_t tops[ROWS][4];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int j0 = (blockIdx.x * 4 + wave) * OUTS;
+    intx4 w[OUTS][CHUNKS];
+    const auto fetch = [&](int k0) {
+#pragma unroll
+        for (int o = 0; o < OUTS; ++o)
+#pragma unroll
+            for (int c = 0; c < CHUNKS; ++c) {
+                const int k = k0 + c * 1024 + lane * 16, j = j0 + o;
+                w[o][c] = j < a.n_out && k < a.n_in ? load_codes(a.w + (int64_t)j * a.n_in, k, a.n_in, a.w_aligned) : intx4{0, 0, 0, 0};
+            }
+    };
+    fetch(0);
+    // the rows' codes, in LDS; a thread keeps the first kFewHeld fours of each row that it sees
+    const int fours = (a.n_in + 3) / 4;
+    float v[ROWS][kFewHeld][4];
+    const auto load = [&](int r, int f, float (&to)[4]) {
+        const int left = a.n_in - 4 * f;
+        load_four<DTYPE>(a.x, (int64_t)r * a.n_in + 4 * f, left, a.x_by_four && left >= 4, to);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) to[e] = rectified(to[e], a.relu);
+    };
+    uint32_t top[ROWS] = {};
+    const auto see = [&](int r, const float (&from)[4]) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) top[r] = larger(top[r], magnitude(from[e]));
+    };
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+        for (int h = 0; h < kFewHeld; ++h)
+            if ((int)threadIdx.x + h * 256 < fours) load(r, threadIdx.x + h * 256, v[r][h]);
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+#pragma unroll
+        for (int h = 0; h < kFewHeld; ++h)
+            if ((int)threadIdx.x + h * 256 < fours) see(r, v[r][h]);
+#pragma unroll 4
+        for (int f = threadIdx.x + kFewHeld * 256; f < fours; f += 256) {
+            float w[4];
+            load(r, f, w);
+            see(r, w);
+        }
+        top[r] = wave_max(top[r]);
+        if (lane == 0) tops[r][wave] = top[r];
+    }
+    __syncthreads();
+    float scale[ROWS];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+        const RowScale s(larger(larger(tops[r][0], tops[r][1]), larger(tops[r][2], tops[r][3])));
+        scale[r] = s.scale;
+        const auto store = [&](int f, const float (&from)[4]) {
+            int c[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) c[e] = s.code(from[e]);   // (beyond the row's end: of zero)
+            *reinterpret_cast<uint32_t *>(lds + r * a.padded + 4 * f) = packed(c);
+        };
+#pragma unroll
+        for (int h = 0; h < kFewHeld; ++h)
+            if ((int)threadIdx.x + h * 256 < fours) store(threadIdx.x + h * 256, v[r][h]);
+#pragma unroll 4
+        for (int f = threadIdx.x + kFewHeld * 256; f < fours; f += 256) {
+            float w[4];
+            load(r, f, w);
+            store(f, w);
+        }
+        for (int f = fours + threadIdx.x; f < a.padded / 4; f += 256) *reinterpret_cast<uint32_t *>(lds + r * a.padded + 4 * f) = 0;
+    }
+    __syncthreads();
+    int sum[ROWS][OUTS] = {};
+    for (int k0 = 0; k0 < a.n_in; k0 += CHUNKS * 1024) {
+        if (k0) fetch(k0);
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) {
+            if (k0 + c * 1024 >= a.n_in) break;
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) {
+                const intx4 x = *reinterpret_cast<const intx4 *>(lds + r * a.padded + k0 + c * 1024 + lane * 16);
+#pragma unroll
+                for (int o = 0; o < OUTS; ++o)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sum[r][o] = __builtin_amdgcn_sdot4(x[e], w[o][c][e], sum[r][o], false);
+            }
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+        for (int o = 0; o < OUTS; ++o) {
+            int v = sum[r][o];
+#pragma unroll
+            for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d, 64);
+            if (lane == 0 && j0 + o < a.n_out) {
+                const int64_t at = (int64_t)r * a.n_out + j0 + o;
+                float y = (float)v * (scale[r] * a.w_scale[j0 + o]) + (a.bias ? a.bias[j0 + o] : 0.0f);
+                if (a.beta != 0.0f) y += a.beta * load_as_float(a.y, at, a.y_dtype);
+                store_from_float(a.y, at, a.y_dtype, y);
+            }
+        }
+}
+
+// ---- host ------------------------------------------------------------------------------------------------------------
+
 size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
+bool aligned_to(const void *p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+
+int padded_row(int n_in) { return (n_in + kLine - 1) / kLine * kLine; }
+int padded_few(int n_in) { return (n_in + 1023) / 1024 * 1024; }
+
+bool few_rows(const LinearShape &s) { return s.batch <= kMostRows && s.batch * padded_few(s.n_in) <= kMostCodes; }
+
+typedef TileShape<64, 64, 2, 2, 3> Tile64;
+typedef TileShape<128, 128, 2, 2, 2> Tile128;
+
+constexpr int kUnits = 256;   // compute units
+
+template <class T>
+WorkSplit split_work(const LinearShape &s)
+{
+    WorkSplit w;
+    w.tiles = ((s.batch + T::ROWS - 1) / T::ROWS) * ((s.n_out + T::COLS - 1) / T::COLS);
+    w.stages = padded_row(s.n_in) / kLine;
+    w.workers = kUnits * (160 * 1024 / T::LDS);
+    w.whole = w.tiles / w.workers * w.workers;
+    // Tiles are cut only where most compute units would be idle and the summed axis is long: joining the parts takes
+    // 5 us, a stage 0.35 (48 rows of 1024 -> 1024: 17 us cut, 13 whole).
+    const int64_t cut = w.whole == 0 && w.left() * 2 <= kUnits && w.stages >= 24 ? w.left() * w.stages / 8 : 0;
+    w.cutters = (int)(cut < w.left() ? w.left() : cut < kUnits ? cut : kUnits);
+    if (w.whole == 0) w.workers = (w.cutters + 7) / 8 * 8;
+    return w;
+}
+
+// The larger tile reads half as much per product, and needs two tiles a compute unit to keep them busy.  Measured
+// (us, tiles of 64 / 128): 4096 rows of 4096 -> 4096 174 / 104; 8192 of 1024 -> 1024 38 / 35; 5000 of 500 -> 333 16 / 24.
+bool large_tiles(const LinearShape &s) { return ((s.batch + 127) / 128) * ((s.n_out + 127) / 128) >= 2 * kUnits; }
+
+WorkSplit split_work(const LinearShape &s) { return large_tiles(s) ? split_work<Tile128>(s) : split_work<Tile64>(s); }
+
+// the workspace: codes of the rows, their scales, weights in aligned rows, parts of tiles that are cut
+struct Layout {
+    size_t codes, scale, w, parts, total;
+};
+Layout layout_of(const LinearShape &s)
+{
+    Layout l = {};
+    if (few_rows(s)) return l;
+    const WorkSplit w = split_work(s);
+    const size_t tile = (large_tiles(s) ? Tile128::ROWS * Tile128::COLS : Tile64::ROWS * Tile64::COLS) * sizeof(int);
+    size_t at = 0;
+    const auto take = [&](size_t bytes) { const size_t here = at; at += align256(bytes); return here; };
+    l.codes = take((size_t)s.batch * padded_row(s.n_in));
+    l.scale = take((size_t)s.batch * sizeof(float));
+    l.w = take((size_t)s.n_out * padded_row(s.n_in));   // (whether it is needed depends on a pointer)
+    l.parts = take(w.cutters > w.left() ? 2 * w.cutters * tile : 0);
+    l.total = at;
+    return l;
+}
+
+template <class T>
+void launch_tiles(LinearArgs &a, hipStream_t stream)
+{
+    a.tiles_across = (a.n_out + T::COLS - 1) / T::COLS;
+    if (T::LDS > 65536) allow_large_lds(reinterpret_cast<const void *>(linear_kernel<T>), T::LDS);
+    linear_kernel<T><<<a.work.workers, T::THREADS, T::LDS, stream>>>(a);
+    if (a.work.cutters > a.work.left()) linear_join_kernel<T><<<(unsigned)a.work.left() * T::WAVES, 64, 0, stream>>>(a);
+}
+
+template <int DTYPE, int ROWS>
+void launch_few_rows(const FewArgs &a, hipStream_t stream)
+{
+    // one output a wave where four would leave compute units idle
+    if (a.n_out < 2048) few_rows_kernel<DTYPE, ROWS, 1, 8><<<(a.n_out + 3) / 4, 256, ROWS * a.padded, stream>>>(a);
+    else few_rows_kernel<DTYPE, ROWS, 4, 4><<<(a.n_out + 15) / 16, 256, ROWS * a.padded, stream>>>(a);
+}
+template <int DTYPE>
+void launch_few(int64_t rows, const FewArgs &a, hipStream_t stream)
+{
+    if (rows == 1) launch_few_rows<DTYPE, 1>(a, stream);
+    else if (rows == 2) launch_few_rows<DTYPE, 2>(a, stream);
+    else if (rows == 3) launch_few_rows<DTYPE, 3>(a, stream);
+    else launch_few_rows<DTYPE, 4>(a, stream);
+}
+
+template <int DTYPE>
+void launch_quantize(const QuantizeArgs &a, hipStream_t stream)
+{
+    // a wave a row while the row fits what its lanes hold
+    if (a.cols <= 64 * 4 * kHeld) quantize_kernel<DTYPE, 64><<<(unsigned)((a.rows + 3) / 4), 256, 0, stream>>>(a);
+    else quantize_kernel<DTYPE, 256><<<(unsigned)a.rows, 256, 0, stream>>>(a);
+}
+
+void quantize(int64_t rows, int cols, int pitch, int dtype, bool relu, const void *x, int8_t *codes, float *scale, hipStream_t stream)
+{
+    QuantizeArgs a{rows, cols, pitch, relu, pitch > cols, false, false, x, codes, scale};
+    a.by_four = cols % 4 == 0 && aligned_to(x, dtype == LMKAN_F32 ? 16 : 8);
+    a.codes_by_four = pitch % 4 == 0 && aligned_to(codes, 4);
+    if (dtype == LMKAN_F32) launch_quantize<LMKAN_F32>(a, stream);
+    else if (dtype == LMKAN_F16) launch_quantize<LMKAN_F16>(a, stream);
+    else launch_quantize<LMKAN_BF16>(a, stream);
+}
 
 }  // namespace
 
 void launch_quantize_rows(int64_t rows, int cols, int dtype, bool relu, const void *x, int8_t *codes, float *scale, hipStream_t stream)
 {
-    quantize_kernel<<<(unsigned)((rows + 3) / 4), 256, 0, stream>>>(rows, cols, dtype, relu, x, codes, scale);
+    quantize(rows, cols, cols, dtype, relu, x, codes, scale, stream);
 }
 
-size_t linear_i8_workspace_bytes(const LinearShape &s)
-{
-    return align256((size_t)s.batch * s.n_in) + align256((size_t)s.batch * sizeof(float));
-}
+size_t linear_i8_workspace_bytes(const LinearShape &s) { return layout_of(s).total; }
 
 void launch_linear_i8(const LinearShape &s, const void *x, const int8_t *w, const float *w_scale, const float *bias,
                       float beta, void *y, void *workspace, hipStream_t stream)
 {
-    int8_t *codes = static_cast<int8_t *>(workspace);
-    float *scale = reinterpret_cast<float *>(codes + align256((size_t)s.batch * s.n_in));
-    launch_quantize_rows(s.batch, s.n_in, s.x_dtype, s.relu, x, codes, scale, stream);
-    const Args a{codes, scale, w, w_scale, bias, beta, y, s.batch, s.n_in, s.n_out, s.y_dtype};
-    const int64_t tiles = ((s.batch + kTile - 1) / kTile) * ((s.n_out + kTile - 1) / kTile);
-    linear_kernel<<<(unsigned)tiles, 256, 0, stream>>>(a);
+    if (few_rows(s)) {
+        const FewArgs a{x, w, w_scale, bias, beta, y, s.n_in, s.n_out, s.x_dtype, s.y_dtype, s.relu,
+                        s.n_in % 16 == 0 && aligned_to(w, 16), s.n_in % 4 == 0 && aligned_to(x, s.x_dtype == LMKAN_F32 ? 16 : 8),
+                        padded_few(s.n_in)};
+        if (s.x_dtype == LMKAN_F32) launch_few<LMKAN_F32>(s.batch, a, stream);
+        else if (s.x_dtype == LMKAN_F16) launch_few<LMKAN_F16>(s.batch, a, stream);
+        else launch_few<LMKAN_BF16>(s.batch, a, stream);
+        return;
+    }
+    const Layout l = layout_of(s);
+    char *ws = static_cast<char *>(workspace);
+    int8_t *codes = reinterpret_cast<int8_t *>(ws + l.codes);
+    float *scale = reinterpret_cast<float *>(ws + l.scale);
+    const int pitch = padded_row(s.n_in);
+    quantize(s.batch, s.n_in, pitch, s.x_dtype, s.relu, x, codes, scale, stream);
+    LinearArgs a = {};
+    a.x = codes, a.x_pitch = pitch;
+    a.w = w, a.w_pitch = s.n_in;
+    if (s.n_in % 16 != 0 || !aligned_to(w, 16)) {
+        int8_t *to = reinterpret_cast<int8_t *>(ws + l.w);
+        const int64_t dwords = (int64_t)s.n_out * (pitch / 4);
+        align_kernel<<<(unsigned)((dwords + 255) / 256), 256, 0, stream>>>(w, s.n_in, s.n_out, pitch, to);
+        a.w = to, a.w_pitch = pitch;
+    }
+    a.x_scale = scale, a.w_scale = w_scale, a.bias = bias, a.beta = beta;
+    a.y = y, a.batch = s.batch, a.n_in = s.n_in, a.n_out = s.n_out, a.y_dtype = s.y_dtype;
+    a.by_four = s.n_out % 4 == 0 && aligned_to(y, s.y_dtype == LMKAN_F32 ? 16 : 8);
+    a.parts = reinterpret_cast<intx4 *>(ws + l.parts);
+    a.work = split_work(s);
+    if (large_tiles(s)) launch_tiles<Tile128>(a, stream);
+    else launch_tiles<Tile64>(a, stream);
 }
 
 }  // namespace lmkan

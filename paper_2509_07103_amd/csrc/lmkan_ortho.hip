@@ -28,7 +28,7 @@ namespace lmkan {
 namespace {
 
 constexpr int kStepsAtOnce = 3;   // steps on one Gram matrix
-constexpr int kNormParts = 64;    // workgroups that sum the norm of one matrix, at most
+constexpr int kNormParts = 1024;  // workgroups that sum the norm of one matrix, at most
 
 // A batch of matrices of pairs (lmkan_tile.h); element values are held times `scale`
 struct PairMatrix {
@@ -46,11 +46,11 @@ __device__ __forceinline__ float direction(const UpdateArgs &u, int dtype, int64
     return u.nesterov ? u.beta * m + (1.0f - u.beta) * load_as_float(u.grad, i, dtype) : m;
 }
 
-// Sum of `parts` numbers in a fixed order, for all 256 threads
-__device__ __forceinline__ double sum_of_parts(const double *part, int parts, double *shared)
+// Sum over the 256 threads in a fixed order, for all of them
+__device__ __forceinline__ double sum_of_threads(double v, double *shared)
 {
-    shared[threadIdx.x] = (int)threadIdx.x < parts ? part[threadIdx.x] : 0.0;
-    for (int half = kNormParts / 2; half > 0; half >>= 1) {
+    shared[threadIdx.x] = v;
+    for (int half = 128; half > 0; half >>= 1) {
         __syncthreads();
         if ((int)threadIdx.x < half) shared[threadIdx.x] += shared[threadIdx.x + half];
     }
@@ -71,17 +71,15 @@ __global__ __launch_bounds__(256) void norm_kernel(MatrixShape s, UpdateArgs u, 
         const double v = direction(u, s.dtype, base + i);
         sum += v * v;
     }
-    sums[threadIdx.x] = sum;
-    for (int half = 128; half > 0; half >>= 1) {
-        __syncthreads();
-        if ((int)threadIdx.x < half) sums[threadIdx.x] += sums[threadIdx.x + half];
-    }
-    if (threadIdx.x == 0) part[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = sums[0];
+    sum = sum_of_threads(sum, sums);
+    if (threadIdx.x == 0) part[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = sum;
 }
 
 __device__ __forceinline__ float inverse_norm(const MatrixShape &s, const double *part, int parts, int64_t matrix, double *shared)
 {
-    return (float)(1.0 / (sqrt(sum_of_parts(part + matrix * parts, parts, shared)) + (double)s.eps));
+    double sum = 0.0;
+    for (int i = threadIdx.x; i < parts; i += 256) sum += part[matrix * parts + i];
+    return (float)(1.0 / (sqrt(sum_of_threads(sum, shared)) + (double)s.eps));
 }
 
 __device__ __forceinline__ void split(float v, _Float16 *hi, _Float16 *lo)
@@ -137,36 +135,50 @@ __global__ __launch_bounds__(256) void split_kernel(SplitArgs a)
     }
 }
 
-// One value to both halves of a pair, four adjacent columns of a row
-__device__ __forceinline__ void store_four(const PairMatrix &d, int64_t matrix, int row, int col, const float (&v)[4])
+constexpr int kPitch = 36;                                // floats of a row of a wave's tile in LDS
+constexpr int kWaveScratch = 32 * kPitch * (int)sizeof(float);
+
+// A wave's 32 x 32 tile at (row, col) of the output, values as in for_wave_tiles, to a matrix of pairs: by lines
+// through LDS, 1 KiB adjacent at a time
+__device__ __forceinline__ void store_pairs(const PairMatrix &d, char *to, int row, int col, const uint2 (&hi)[4], const uint2 (&lo)[4],
+                                            char *scratch, int lane)
 {
-    char *to = d.base + matrix * d.stride;
-    const int panel = col / kPanel, in = col % kPanel;
-    half4 hi, lo;
+    const int r = lane & 15, q = lane >> 4;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        _Float16 h, l;
-        split(v[e] * d.scale, &h, &l);
-        hi[e] = h, lo[e] = l;
+    for (int g = 0; g < 4; ++g) {
+        const int line = 16 * (g >> 1) + r, chunk = 2 * (g & 1) + (q >> 1);
+        *reinterpret_cast<uint2 *>(scratch + line * kLine + slot_of(line, chunk) * 16 + (q & 1) * 8) = hi[g];
+        *reinterpret_cast<uint2 *>(scratch + line * kLine + slot_of(line, 4 + chunk) * 16 + (q & 1) * 8) = lo[g];
     }
-    *reinterpret_cast<half4 *>(to + pair_at(d.rows, row, panel, in / 8) + in % 8 * 2) = hi;
-    *reinterpret_cast<half4 *>(to + pair_at(d.rows, row, panel, 4 + in / 8) + in % 8 * 2) = lo;
+    char *line = to + ((int64_t)(col / kPanel) * d.rows + row) * kLine;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        const int at = t * 1024 + lane * 16;
+        const uint4 v = *reinterpret_cast<const uint4 *>(scratch + at);
+        if (row + at / kLine < d.rows) *reinterpret_cast<uint4 *>(line + at) = v;
+    }
 }
-__device__ __forceinline__ void store_one(const PairMatrix &d, int64_t matrix, int row, int col, float v)
+
+// the same tile turned: its columns are rows of `d`
+__device__ __forceinline__ void store_turned(const PairMatrix &d, char *to, int row, int col, const uint2 (&hi)[4], const uint2 (&lo)[4], int lane)
 {
-    char *to = d.base + matrix * d.stride;
-    const int panel = col / kPanel, in = col % kPanel;
-    _Float16 h, l;
-    split(v * d.scale, &h, &l);
-    *reinterpret_cast<_Float16 *>(to + pair_at(d.rows, row, panel, in / 8) + in % 8 * 2) = h;
-    *reinterpret_cast<_Float16 *>(to + pair_at(d.rows, row, panel, 4 + in / 8) + in % 8 * 2) = l;
+    const int q = lane >> 4, k = (lane & 15) >> 2;   // the lane's four values along the depth: 4 k ..
+    char *line = to + ((int64_t)(row / kPanel) * d.rows + col) * kLine + (k & 1) * 8;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        const int r = 16 * (g & 1) + 4 * q + (lane & 3), chunk = 2 * (g >> 1) + (k >> 1);
+        const uint2 th = turn_quad(hi[g], lane), tl = turn_quad(lo[g], lane);
+        if (col + r < d.rows) {
+            *reinterpret_cast<uint2 *>(line + r * kLine + slot_of(r, chunk) * 16) = th;
+            *reinterpret_cast<uint2 *>(line + r * kLine + slot_of(r, 4 + chunk) * 16) = tl;
+        }
+    }
 }
 
 // What becomes of a product
 enum Finish {
     kKeep,      // pairs, both ways round
     kPoly,      // a I + b A + c (product), pairs
-    kPartial,   // float32 sums of a part of the summed axis
     kResult,    // the result of the call
 };
 
@@ -181,15 +193,15 @@ struct ProductArgs {
     Product p[2];
     int problems;
     int64_t matrices;
-    int tiles_down, tiles_across;
+    int tiles_across;
     int64_t tiles;             // of one matrix and problem
-    // kPartial
-    float *partial;
-    int parts;
+    WorkSplit work;
+    floatx4 *parts;
     // kResult
     MatrixShape s;
     UpdateArgs u;
     int64_t first;
+    bool by_four;              // rows of the result take accesses of four elements
 };
 
 // Tile t of the upper triangle of n x n tiles, column by column: (0,0) (0,1) (1,1) (0,2) ...
@@ -202,95 +214,135 @@ __device__ __forceinline__ void upper_tile(int t, int *i, int *j)
     *i = t - c * (c + 1) / 2;
 }
 
+// Where a tile of the launch is
+struct Place {
+    int matrix, problem, ti, tj;
+};
+__device__ __forceinline__ Place place_of(const ProductArgs &a, int64_t t)
+{
+    const int64_t which = t / a.tiles;
+    const int tile = (int)(t - which * a.tiles), matrix = (int)(which / a.problems);
+    int ti, tj;
+    if (a.p[0].symmetric) upper_tile(tile, &ti, &tj);
+    else ti = tile / a.tiles_across, tj = tile - ti * a.tiles_across;
+    return Place{uniform(matrix), uniform((int)which - matrix * a.problems), uniform(ti), uniform(tj)};
+}
+
+// (two products at a time are kept ones)
+template <int FINISH>
+__device__ __forceinline__ const Product &product_of(const ProductArgs &a, const Place &w)
+{
+    return FINISH == kKeep && w.problem ? a.p[1] : a.p[0];
+}
+
+// `scratch`: kWaveScratch bytes of LDS of the wave's own
+template <class T, int FINISH>
+__device__ __forceinline__ void finish_tile(const ProductArgs &a, const Place &w, const floatx4 (&acc)[T::CT][T::RT], char *scratch, int wave)
+{
+    const Product &p = product_of<FINISH>(a, w);
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));   // (the addresses below are worked out here, not kept in registers through the main loop)
+    const int r = lane & 15, q = lane >> 4;
+    const float unit = 1.0f / (p.rows.scale * p.cols.scale);
+    const int n_rows = p.rows.rows, n_cols = p.cols.rows;
+    for_wave_tiles<T>(acc, wave, [&](int row, int col, const floatx4 (&v)[4]) {
+        row += w.ti * T::ROWS, col += w.tj * T::COLS;
+        if (FINISH == kResult) {
+            if (row >= n_rows || col >= n_cols) return;
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                *reinterpret_cast<floatx4 *>(scratch + ((16 * (g >> 1) + r) * kPitch + 16 * (g & 1) + 4 * q) * 4) = v[g] * unit;
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                const int i = 8 * t + (lane >> 3), j = (lane & 7) * 4;
+                const float4 o = *reinterpret_cast<const float4 *>(scratch + (i * kPitch + j) * 4);
+                if (row + i >= n_rows || col + j >= n_cols) continue;
+                const int64_t at = (a.first + w.matrix) * a.s.elems() + (int64_t)(row + i) * a.s.cols + col + j;
+                if (a.by_four) {
+                    if (a.u.weight) {
+                        float4 *to = reinterpret_cast<float4 *>(a.u.weight + at);
+                        const float4 k = *to;
+                        *to = make_float4(a.u.keep * k.x + a.u.add * o.x, a.u.keep * k.y + a.u.add * o.y, a.u.keep * k.z + a.u.add * o.z, a.u.keep * k.w + a.u.add * o.w);
+                    } else if (a.s.dtype == LMKAN_F32) {
+                        *reinterpret_cast<float4 *>(static_cast<float *>(a.u.out) + at) = o;
+                    } else {
+                        *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.u.out) + at) =
+                            make_uint2(two_from_float(a.s.dtype, o.x, o.y), two_from_float(a.s.dtype, o.z, o.w));
+                    }
+                } else {
+                    const float one[4] = {o.x, o.y, o.z, o.w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (col + j + e < n_cols) {
+                            if (a.u.weight) a.u.weight[at + e] = a.u.keep * a.u.weight[at + e] + a.u.add * one[e];
+                            else store_from_float(a.u.out, at + e, a.s.dtype, one[e]);
+                        }
+                }
+            }
+            return;
+        }
+        const bool direct = row < n_rows && col < panels(n_cols) * kPanel;
+        const bool turned = p.mirror.base && !(p.symmetric && w.ti == w.tj) && col < n_cols && row < panels(n_rows) * kPanel;
+        if (!direct && !turned) return;
+        uint2 hi[4], lo[4];
+        const float scale = p.out.scale;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int i = row + 16 * (g >> 1) + r, j = col + 16 * (g & 1) + 4 * q;
+            floatx4 f = v[g] * unit;
+            if (FINISH == kPoly && i < n_rows && j < n_cols) {
+                const char *from = p.gram.base + w.matrix * p.gram.stride;
+                const int chunk = 2 * (g & 1) + (q >> 1);
+                const half4 gh = *reinterpret_cast<const half4 *>(from + pair_at(p.gram.rows, i, col / kPanel, chunk) + (q & 1) * 8);
+                const half4 gl = *reinterpret_cast<const half4 *>(from + pair_at(p.gram.rows, i, col / kPanel, 4 + chunk) + (q & 1) * 8);
+                const float s = 1.0f / p.gram.scale;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) f[e] = p.c * f[e] + p.b * (((float)gh[e] + (float)gl[e]) * s) + (i == j + e ? p.a : 0.0f);
+            }
+            half4 vh, vl;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                // what lies beyond the matrix in a panel is zero
+                _Float16 x, y;
+                split(i < n_rows && j + e < n_cols ? f[e] * scale : 0.0f, &x, &y);
+                vh[e] = x, vl[e] = y;
+            }
+            hi[g] = __builtin_bit_cast(uint2, vh), lo[g] = __builtin_bit_cast(uint2, vl);
+        }
+        if (direct) store_pairs(p.out, p.out.base + w.matrix * p.out.stride, row, col, hi, lo, scratch, lane);
+        if (turned) store_turned(p.mirror, p.mirror.base + w.matrix * p.mirror.stride, row, col, hi, lo, lane);
+    });
+}
+
 template <class T, int FINISH>
 __global__ __launch_bounds__(T::THREADS) void product_kernel(ProductArgs a)
 {
     extern __shared__ __align__(16) char lds[];
-    const int64_t each = a.tiles * (FINISH == kPartial ? a.parts : 1), total = each * a.matrices * a.problems;
-    const int64_t place = place_of(blockIdx.x, total);
-    if (place >= total) return;
-    const int64_t which = place / each;
-    const int64_t matrix = which / a.problems;
-    const Product &p = a.p[which - matrix * a.problems];
-    const int64_t rest = place - which * each;
-    const int part = FINISH == kPartial ? (int)(rest / a.tiles) : 0;
-    const int tile = (int)(rest - part * a.tiles);
-    int ti, tj;
-    if (p.symmetric) upper_tile(tile, &ti, &tj);
-    else ti = tile / a.tiles_across, tj = tile - ti * a.tiles_across;
-    const int i0 = ti * T::ROWS, j0 = tj * T::COLS;
-    const auto operand = [&](const PairMatrix &m, int first_row) {
-        return Operand{m.base + matrix * m.stride + (int64_t)first_row * kLine, (int64_t)m.rows * kLine, kLine, m.rows - 1 - first_row, true, 0};
-    };
-    const int stages = panels(p.rows.depth);
-    const int begin = FINISH == kPartial ? (int)((int64_t)stages * part / a.parts) : 0;
-    const int end = FINISH == kPartial ? (int)((int64_t)stages * (part + 1) / a.parts) : stages;
-    floatx16 acc[T::RT][T::CT];
-    multiply<T, PairProduct>(operand(p.rows, i0), operand(p.cols, j0), begin, end, lds, acc);
-    const float unit = 1.0f / (p.rows.scale * p.cols.scale);
-    const int n_rows = p.rows.rows, n_cols = p.cols.rows;
-    for_outputs<T>(acc, [&](int r, int c, float v0, float v1, float v2, float v3) {
-        const int i = i0 + r, j = j0 + c;
-        float v[4] = {v0 * unit, v1 * unit, v2 * unit, v3 * unit};
-        if (FINISH == kPartial) {
-            float *to = a.partial + ((part * a.matrices + matrix) * n_rows + i) * (int64_t)n_cols + j;
-            if (i < n_rows)
-                for (int e = 0; e < 4; ++e)
-                    if (j + e < n_cols) to[e] = v[e];
-            return;
-        }
-        if (FINISH == kResult) {
-            if (i >= n_rows || j >= n_cols) return;
-            const int64_t at = (a.first + matrix) * a.s.elems() + (int64_t)i * a.s.cols + j;
-            for (int e = 0; e < 4; ++e)
-                if (j + e < n_cols) {
-                    if (a.u.weight) a.u.weight[at + e] = a.u.keep * a.u.weight[at + e] + a.u.add * v[e];
-                    else store_from_float(a.u.out, at + e, a.s.dtype, v[e]);
-                }
-            return;
-        }
-        if (FINISH == kPoly && i < n_rows && j < n_cols) {
-            const char *from = p.gram.base + matrix * p.gram.stride;
-            const half4 hi = *reinterpret_cast<const half4 *>(from + pair_at(p.gram.rows, i, j / kPanel, j % kPanel / 8) + j % 8 * 2);
-            const half4 lo = *reinterpret_cast<const half4 *>(from + pair_at(p.gram.rows, i, j / kPanel, 4 + j % kPanel / 8) + j % 8 * 2);
-            const float g = 1.0f / p.gram.scale;
-            for (int e = 0; e < 4; ++e)
-                v[e] = p.c * v[e] + p.b * (((float)hi[e] + (float)lo[e]) * g) + (i == j + e ? p.a : 0.0f);
-        }
-        // what lies beyond the matrix in a panel is zero
-        for (int e = 0; e < 4; ++e)
-            if (i >= n_rows || j + e >= n_cols) v[e] = 0.0f;
-        if (i < n_rows && j < panels(n_cols) * kPanel) store_four(p.out, matrix, i, j, v);
-        if (p.mirror.base && !(p.symmetric && ti == tj) && i < panels(n_rows) * kPanel)
-            for (int e = 0; e < 4; ++e)
-                if (j + e < n_cols) store_one(p.mirror, matrix, j + e, i, v[e]);
+    for_work(a.work, blockIdx.x, [&](int64_t tile, int from, int to, int slot) {
+        const Place w = place_of(a, tile);
+        const Product &p = product_of<FINISH>(a, w);
+        const auto operand = [&](const PairMatrix &m, int first_row) {
+            return Operand{uniform(m.base + w.matrix * m.stride + (int64_t)first_row * kLine), uniform((int64_t)m.rows * kLine), m.rows - 1 - first_row, true, 0, 0};
+        };
+        floatx4 acc[T::CT][T::RT];
+        multiply<T, PairProduct>(operand(p.rows, w.ti * T::ROWS), operand(p.cols, w.tj * T::COLS), from, to, lds, acc);
+        __syncthreads();
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        if (slot < 0) finish_tile<T, FINISH>(a, w, acc, lds + wave * kWaveScratch, wave);
+        else store_part<T>(a.parts, slot, acc);
+        __syncthreads();
     });
 }
 
-// The Gram matrices from their float32 parts (tiles below the diagonal: from above it); a chunk a thread
-__global__ __launch_bounds__(256) void sum_parts_kernel(PairMatrix d, const float *partial, int parts, int64_t matrices, int tile)
+// A wave's share of a tile that was cut, a workgroup each
+template <class T, int FINISH>
+__global__ __launch_bounds__(64) void join_kernel(ProductArgs a)
 {
-    const int m = d.rows, chunks = panels(m) * 4;
-    const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (e >= matrices * m * chunks) return;
-    const int chunk = (int)(e % chunks), i = (int)(e / chunks % m);
-    const int64_t matrix = e / chunks / m;
-    half8 hi, lo;
-    for (int k = 0; k < 8; ++k) {
-        const int j = chunk * 8 + k;
-        float v = 0.0f;
-        if (j < m) {
-            const bool below = j / tile < i / tile;
-            const int64_t at = below ? (int64_t)j * m + i : (int64_t)i * m + j;
-            for (int p = 0; p < parts; ++p) v += partial[(p * matrices + matrix) * m * m + at];
-        }
-        _Float16 h, l;
-        split(v * d.scale, &h, &l);
-        hi[k] = h, lo[k] = l;
-    }
-    char *to = d.base + matrix * d.stride;
-    *reinterpret_cast<half8 *>(to + pair_at(m, i, chunk / 4, chunk % 4)) = hi;
-    *reinterpret_cast<half8 *>(to + pair_at(m, i, chunk / 4, 4 + chunk % 4)) = lo;
+    __shared__ __align__(16) char lds[kWaveScratch];
+    const int tile = blockIdx.x / T::WAVES, wave = blockIdx.x % T::WAVES;
+    floatx4 acc[T::CT][T::RT];
+    if (!join_parts<T>(a.work, tile, wave, a.parts, acc)) return;
+    finish_tile<T, FINISH>(a, place_of(a, a.work.whole + tile), acc, lds, wave);
 }
 
 // No steps: X_0 itself is the result
@@ -306,75 +358,79 @@ __global__ __launch_bounds__(256) void unscaled_kernel(MatrixShape s, UpdateArgs
     }
 }
 
-typedef TileShape<64, 64, 2, 2> Tile64;
-typedef TileShape<128, 128, 2, 2> Tile128;
+typedef TileShape<64, 64, 2, 2, 4> Tile64;
+typedef TileShape<128, 128, 2, 2, 2> Tile128;
+typedef TileShape<256, 256, 4, 2, 2> Tile256;
 
-int64_t upper_tiles(int rows, int tile)
+constexpr int kUnits = 256;      // compute units
+constexpr size_t kPartsBytes = (size_t)128 << 20;   // slots of 256 workgroups with the largest tile
+
+int64_t tiles_of(const Product &p, int tile)
 {
-    const int64_t n = (rows + tile - 1) / tile;
-    return n * (n + 1) / 2;
+    const int64_t down = (p.rows.rows + tile - 1) / tile, across = (p.cols.rows + tile - 1) / tile;
+    return p.symmetric ? down * (down + 1) / 2 : down * across;
 }
-
-// the larger tile reads half as much per product; the smaller one where the larger leaves compute units without work
-bool small_tiles(int64_t large_tiles) { return large_tiles < 256; }
 
 template <class T, int FINISH>
 void launch_product_with(ProductArgs &a, hipStream_t stream)
 {
     const Product &p = a.p[0];
-    a.tiles_down = (p.rows.rows + T::ROWS - 1) / T::ROWS;
     a.tiles_across = (p.cols.rows + T::COLS - 1) / T::COLS;
-    a.tiles = p.symmetric ? upper_tiles(p.rows.rows, T::ROWS) : (int64_t)a.tiles_down * a.tiles_across;
-    const int64_t total = a.tiles * (FINISH == kPartial ? a.parts : 1) * a.matrices * a.problems;
+    a.tiles = tiles_of(p, T::ROWS);
+    WorkSplit &w = a.work;
+    w.tiles = a.tiles * a.matrices * a.problems;
+    w.stages = panels(p.rows.depth);
+    w.workers = kUnits * (T::LDS <= 80 * 1024 ? 2 : 1);
+    w.whole = w.tiles / w.workers * w.workers;
+    // a part shorter than four stages costs more to join than it saves
+    const int64_t cut = w.left() * w.stages / 4;
+    w.cutters = (int)(cut < w.left() ? w.left() : cut < w.workers ? cut : w.workers);
+    if (w.whole == 0) w.workers = (w.cutters + 7) / 8 * 8;
     if (T::LDS > 65536) allow_large_lds(reinterpret_cast<const void *>(product_kernel<T, FINISH>), T::LDS);
-    product_kernel<T, FINISH><<<(unsigned)((total + 7) / 8 * 8), T::THREADS, T::LDS, stream>>>(a);
+    product_kernel<T, FINISH><<<w.workers, T::THREADS, T::LDS, stream>>>(a);
+    if (w.cutters > w.left()) join_kernel<T, FINISH><<<(unsigned)w.left() * T::WAVES, 64, 0, stream>>>(a);
 }
 
-int64_t tiles_of(const Product &p, int tile)
-{
-    return p.symmetric ? upper_tiles(p.rows.rows, tile) : (int64_t)((p.rows.rows + tile - 1) / tile) * ((p.cols.rows + tile - 1) / tile);
-}
-
+// The larger the tile, the less is read per product and the more of a tile that straddles the diagonal or the end is
+// wasted.  Measured (us, tiles of 64 / 128 / 256): 441 of 250 x 333 1900 / 1980 / 2400; 289 of 512 x 1024 7550 /
+// 6240 / 6540; one of 4096 x 4096 6500 / 4900 / 4350; one of 1024 x 1024 348 / 662 / 1020.
 template <int FINISH>
 void launch_product(ProductArgs &a, hipStream_t stream)
 {
-    if (small_tiles(tiles_of(a.p[0], 128) * a.matrices * a.problems)) launch_product_with<Tile64, FINISH>(a, stream);
-    else launch_product_with<Tile128, FINISH>(a, stream);
+    const int64_t n = a.matrices * a.problems;
+    const int shorter = a.s.m();
+    if (shorter > 512 && tiles_of(a.p[0], 256) * n >= kUnits / 2) launch_product_with<Tile256, FINISH>(a, stream);
+    else if (shorter > 256 && tiles_of(a.p[0], 128) * n >= 2 * kUnits) launch_product_with<Tile128, FINISH>(a, stream);
+    else launch_product_with<Tile64, FINISH>(a, stream);
 }
 
-// parts of the summed axis of a Gram matrix: two tiles a compute unit where there are fewer, four lines at least each
-int gram_parts(int m, int n, int64_t matrices)
-{
-    const int64_t tiles = upper_tiles(m, 64) * matrices;
-    const int64_t want = tiles >= 256 ? 1 : (512 + tiles - 1) / tiles, most = panels(n) / 4;
-    return (int)(want < most ? want : most < 1 ? 1 : most);
-}
-
-// matrices that share the workspace at a time: 128 M elements keep every compute unit busy
+// Matrices that share the workspace at a time: the batch in equal parts of at most 256 M elements (parts of 32 M and
+// less leave compute units without work at the end of every launch: 289 of 512 x 1024 took 7.7 ms instead of 6.2)
 int64_t matrices_at_once(const MatrixShape &s)
 {
-    const int64_t some = ((int64_t)128 << 20) / s.elems();
-    return some < 1 ? 1 : some > s.batch ? s.batch : some > 4096 ? 4096 : some;
+    int64_t most = ((int64_t)256 << 20) / s.elems();
+    most = most < 1 ? 1 : most > 16384 ? 16384 : most;
+    const int64_t parts = (s.batch + most - 1) / most;
+    return (s.batch + parts - 1) / parts;
 }
 
 size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // the workspace of `count` matrices
 struct Layout {
-    size_t norm, u, v[2], a, w, b[2], p[2], partial, total;
+    size_t norm, u, v[2], a, w, b[2], p[2], parts, total;
 };
 Layout layout_of(const MatrixShape &s, int64_t count)
 {
     const size_t u = align256(count * pair_bytes(s.m(), s.n())), v = align256(count * pair_bytes(s.n(), s.m()));
     const size_t g = align256(count * pair_bytes(s.m(), s.m()));
-    const int parts = gram_parts(s.m(), s.n(), count);
     Layout l;
     size_t at = 0;
     const auto take = [&](size_t bytes) { const size_t here = at; at += bytes; return here; };
     l.norm = take(align256(count * kNormParts * sizeof(double)));
     l.u = take(u), l.v[0] = take(v), l.v[1] = take(v);
     l.a = take(g), l.w = take(g), l.b[0] = take(g), l.b[1] = take(g), l.p[0] = take(g), l.p[1] = take(g);
-    l.partial = take(parts > 1 ? align256((size_t)parts * count * s.m() * s.m() * sizeof(float)) : 0);
+    l.parts = take(kPartsBytes);
     l.total = at;
     return l;
 }
@@ -457,21 +513,15 @@ void launch_ortho(const MatrixShape &s, int steps, const float *schedule, const 
         args.s = s;
         args.u = u;
         args.first = first;
+        args.by_four = s.cols % 4 == 0 && reinterpret_cast<uintptr_t>(u.weight ? (const void *)u.weight : u.out) % (u.weight || s.dtype == LMKAN_F32 ? 16 : 8) == 0;
+        args.parts = reinterpret_cast<floatx4 *>(ws + l.parts);
         const auto one = [&](const Product &p) { args.p[0] = p, args.problems = 1; };
         for (int k = 0; k < steps;) {
             const int end = k + kStepsAtOnce < steps ? k + kStepsAtOnce : steps;
             const double r = bounds.singular[k];
             PairMatrix gram = pairs(l.a, m, m, r * r), so_far = none;
             one(Product{x, x, gram, gram, none, 0, 0, 0, true});
-            args.parts = gram_parts(m, n, count);
-            if (args.parts > 1) {
-                args.partial = reinterpret_cast<float *>(ws + l.partial);
-                launch_product_with<Tile64, kPartial>(args, stream);
-                const int64_t chunks = count * m * panels(m) * 4;
-                sum_parts_kernel<<<(unsigned)((chunks + 255) / 256), 256, 0, stream>>>(gram, args.partial, args.parts, count, Tile64::ROWS);
-            } else {
-                launch_product<kKeep>(args, stream);
-            }
+            launch_product<kKeep>(args, stream);
             double factor = 1.0;
             for (const int begin = k; k < end; ++k) {
                 const float *abc = schedule + 3 * k;

@@ -1,5 +1,5 @@
 // Tiles of matrix products on the matrix cores: operands whose rows lie along the summed axis, staged through
-// LDS in lines of 128 bytes a row, 16-byte fragments, 32 x 32 matrix instructions.
+// LDS in lines of 128 bytes a row, 16-byte fragments, 16 x 16 matrix instructions.
 //
 // Two kinds of operands:
 //   pairs   a float32 value v held as two float16, v s = hi + lo (s a power of two, 22 bits of v): a line of
@@ -8,7 +8,7 @@
 //           lie panel by panel, [depth / 32][rows][128 bytes]: what a tile reads at a time is one piece.
 //   codes   int8, 128 of them a line, rows `pitch` bytes apart.
 // Chunk c of row r sits in slot c ^ ((r >> 1) & 7) of its line, in LDS and in panels: the 16-byte reads of the
-// lanes of a wave (32 rows, two chunks) then fall on all banks alike.
+// lanes of a wave (16 rows, four chunks) then fall on all banks alike.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -18,8 +18,7 @@ namespace lmkan {
 
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef _Float16 half4 __attribute__((ext_vector_type(4)));
-typedef float floatx16 __attribute__((ext_vector_type(16)));
-typedef int intx16 __attribute__((ext_vector_type(16)));
+typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef int intx4 __attribute__((ext_vector_type(4)));
 
 constexpr int kLine = 128;       // bytes of a row in LDS
@@ -36,12 +35,27 @@ __device__ __forceinline__ int64_t pair_at(int rows, int row, int panel, int chu
     return ((int64_t)panel * rows + row) * kLine + slot_of(row, chunk) * 16;
 }
 
+// The value of the first lane, for one that is the same in all of them but that the compiler cannot tell to be
+template <class V>
+__device__ __forceinline__ V uniform(V v)
+{
+    static_assert(sizeof(V) == 4 || sizeof(V) == 8, "");
+    if constexpr (sizeof(V) == 4) {
+        return __builtin_bit_cast(V, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, v)));
+    } else {
+        const uint64_t u = __builtin_bit_cast(uint64_t, v);
+        const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)u), hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(u >> 32));
+        return __builtin_bit_cast(V, (uint64_t)hi << 32 | lo);
+    }
+}
+
 // 16 bytes per lane from global memory (a wave-uniform base, 32 bits of offset per lane) to LDS at lds + 16 lane.
 // The compiler does not know of the load (it cannot make reads of the other buffer wait for it); it is awaited
 // with landed().  m0 is a reserved register to the compiler, which sets it before any use of its own.
 __device__ __forceinline__ void load_to_lds(const void *base, unsigned offset, unsigned lds)
 {
-    asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(offset), "s"(base), "s"(lds) : "memory");
+    asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" :
+                 : "v"(offset), "s"(uniform(base)), "s"(uniform(lds)) : "memory");
 }
 
 __device__ __forceinline__ unsigned lds_offset(const void *p)
@@ -49,32 +63,35 @@ __device__ __forceinline__ unsigned lds_offset(const void *p)
     return (unsigned)(size_t)(__attribute__((address_space(3))) const void *)p;
 }
 
-// own loads have landed and own reads are done; then all waves' have
+// All but the wave's last `LEFT` loads have landed and its own reads are done; then all waves' have
+template <int LEFT>
 __device__ __forceinline__ void landed()
 {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LEFT) : "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 }
 
-// Tile shape: ROWS x COLS outputs of one workgroup, WR x WC waves.
-template <int ROWS_, int COLS_, int WR_, int WC_>
+// Tile shape: ROWS x COLS outputs of one workgroup, WR x WC waves, stages in BUFFERS buffers
+template <int ROWS_, int COLS_, int WR_, int WC_, int BUFFERS_>
 struct TileShape {
-    static constexpr int ROWS = ROWS_, COLS = COLS_, WR = WR_, WC = WC_;
+    static constexpr int ROWS = ROWS_, COLS = COLS_, WR = WR_, WC = WC_, BUFFERS = BUFFERS_;
     static constexpr int WAVES = WR * WC, THREADS = 64 * WAVES;
-    static constexpr int RT = ROWS / WR / 32, CT = COLS / WC / 32;   // 32 x 32 tiles of a wave
+    static constexpr int RT = ROWS / WR / 16, CT = COLS / WC / 16;   // 16 x 16 tiles of a wave
     static constexpr int STAGE = (ROWS + COLS) * kLine;              // bytes of a stage
-    static constexpr int LDS = 2 * STAGE;
+    static constexpr int LOADS = (ROWS + COLS) / 8 / WAVES;          // loads of a wave a stage
+    static constexpr int LDS = BUFFERS * STAGE;
+    static constexpr int GROUPS = RT * CT;                           // groups of four outputs of a lane
 };
 
-// One operand of a tile: its lines of stage s start at base + s * step, row r of the tile `row_step` bytes apart
+// One operand of a tile: the lines of stage s of its rows start at base + s * step
 struct Operand {
     const char *base;
     int64_t step;
-    unsigned row_step;
-    int last;        // last row of the tile that exists (rows beyond it repeat it: their outputs are dropped)
-    bool swizzled;   // slots are chunks already (panels of pairs)
-    int limit;       // codes: bytes of a row; a chunk beyond reads the row's last one (the other operand is zero there)
+    int last;        // last row of the tile that exists (for rows beyond, others are read: their outputs are dropped)
+    bool panels;     // lines are adjacent, slots in place (pairs); else rows of codes, `pitch` bytes apart
+    unsigned pitch;
+    int limit;       // codes: the last 16 bytes of a row; lines that end beyond read them there (the other operand is zero)
 };
 
 // Brings the lines of a stage of one operand to LDS, N rows, from wave `wave` of WAVES.
@@ -82,135 +99,265 @@ template <int N, int WAVES>
 __device__ __forceinline__ void stage_operand(const Operand &o, int stage, unsigned lds, int wave, int lane)
 {
     const char *base = o.base + stage * o.step;
+    asm volatile("" : "+v"(lane));   // (offsets are worked out again every stage: kept, they take the registers of sums)
 #pragma unroll
     for (int g = 0; g < N / 8 / WAVES; ++g) {
-        const int r0 = (g * WAVES + wave) * 8, r = r0 + (lane >> 3), slot = lane & 7;
-        const unsigned row = (unsigned)(r < o.last ? r : o.last);
+        const int r0 = (g * WAVES + wave) * 8;
         unsigned at;
-        if (o.swizzled) {
-            at = row * o.row_step + slot * 16;
+        if (o.panels) {
+            // one piece; lanes beyond its end read its last bytes
+            const unsigned end = (unsigned)o.last * kLine + kLine - 16;
+            at = (unsigned)(r0 * kLine + lane * 16);
+            at = at < end ? at : end;
         } else {
-            const int c = slot_of(r, slot) * 16, most = o.limit - stage * kLine;
-            at = row * o.row_step + (unsigned)(c < most ? c : most);
+            const int r = r0 + (lane >> 3), c = slot_of(r, lane & 7) * 16, most = o.limit - stage * kLine;
+            at = (unsigned)(r < o.last ? r : o.last) * o.pitch + (unsigned)(c < most ? c : most);
         }
         load_to_lds(base, at, lds + r0 * kLine);
     }
 }
 
-__device__ __forceinline__ const char *fragment_at(const char *lds, int row, int chunk) { return lds + row * kLine + slot_of(row, chunk) * 16; }
+// What a lane holds of a line of 16 rows: row lane & 15, chunk lane >> 4 of the four of each half of the line.
+// (16 rows further on the slots are the same.)
+template <class V>
+struct Fragment {
+    V half[2];
+};
+struct FragmentPlace {
+    unsigned at[2];   // of the first 16 rows
+    __device__ __forceinline__ FragmentPlace(int lane)
+    {
+        const int row = lane & 15, chunk = lane >> 4;
+        at[0] = row * kLine + slot_of(row, chunk) * 16;
+        at[1] = row * kLine + slot_of(row, 4 + chunk) * 16;
+    }
+    template <class V>
+    __device__ __forceinline__ void load(Fragment<V> &f, const char *lds, int sixteens) const
+    {
+        f.half[0] = *reinterpret_cast<const V *>(lds + at[0] + sixteens * 16 * kLine);
+        f.half[1] = *reinterpret_cast<const V *>(lds + at[1] + sixteens * 16 * kLine);
+    }
+};
 
-// acc[r][c] += the tile's products over one stage in LDS, which are summed by themselves first: one rounding at the
-// size of the whole sum for 32 values instead of six (a sum over 1024 is then off by 2^-24 * 6, not * 14).  The instruction's first operand gives the columns of the
-// output (four adjacent ones to a lane), its second the rows (a row a lane).
-template <class T>
+// acc[i] += the products of row fragments i and one column fragment over a line.  The instruction's first operand
+// gives the columns of the output (four adjacent ones to a lane), its second the rows (a row a lane).
 struct PairProduct {
-    typedef floatx16 Acc;
-    static __device__ __forceinline__ void stage(const char *rows, const char *cols, int lane, Acc (&acc)[T::RT][T::CT])
+    typedef half8 Element;
+    typedef floatx4 Acc;
+    // The 96 products of a line are summed by themselves first: one rounding at the size of the whole sum a line
+    // instead of three (over a depth of 1024 the sum is then off by 2^-24 * 6, not * 10)
+    template <int N>
+    static __device__ __forceinline__ void line(const Fragment<half8> (&rows)[N], const Fragment<half8> &cols, Acc (&sum)[N])
     {
-        const int r = lane & 31, h = lane >> 5;
-        half8 rh[T::RT][2], rl[T::RT][2];
 #pragma unroll
-        for (int i = 0; i < T::RT; ++i)
+        for (int i = 0; i < N; ++i) sum[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(cols.half[1], rows[i].half[0], Acc{0, 0, 0, 0}, 0, 0, 0);
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                rh[i][k] = *reinterpret_cast<const half8 *>(fragment_at(rows, 32 * i + r, 2 * k + h));
-                rl[i][k] = *reinterpret_cast<const half8 *>(fragment_at(rows, 32 * i + r, 4 + 2 * k + h));
-            }
+        for (int i = 0; i < N; ++i) sum[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(cols.half[0], rows[i].half[1], sum[i], 0, 0, 0);
 #pragma unroll
-        for (int j = 0; j < T::CT; ++j) {
-            half8 ch[2], cl[2];
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                ch[k] = *reinterpret_cast<const half8 *>(fragment_at(cols, 32 * j + r, 2 * k + h));
-                cl[k] = *reinterpret_cast<const half8 *>(fragment_at(cols, 32 * j + r, 4 + 2 * k + h));
-            }
-#pragma unroll
-            for (int i = 0; i < T::RT; ++i) {
-                Acc t = {};
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    t = __builtin_amdgcn_mfma_f32_32x32x16_f16(ch[k], rl[i][k], t, 0, 0, 0);
-                    t = __builtin_amdgcn_mfma_f32_32x32x16_f16(cl[k], rh[i][k], t, 0, 0, 0);
-                    t = __builtin_amdgcn_mfma_f32_32x32x16_f16(ch[k], rh[i][k], t, 0, 0, 0);
-                }
-                acc[i][j] += t;
-            }
-        }
+        for (int i = 0; i < N; ++i) sum[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(cols.half[0], rows[i].half[0], sum[i], 0, 0, 0);
     }
+    static constexpr bool kBySum = true;
 };
 
-template <class T>
 struct CodeProduct {
-    typedef intx16 Acc;
-    static __device__ __forceinline__ void stage(const char *rows, const char *cols, int lane, Acc (&acc)[T::RT][T::CT])
+    typedef intx4 Element;
+    typedef intx4 Acc;
+    template <int N>
+    static __device__ __forceinline__ void line(const Fragment<intx4> (&rows)[N], const Fragment<intx4> &cols, Acc (&sum)[N])
     {
-        const int r = lane & 31, h = lane >> 5;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            intx4 rf[T::RT];
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int i = 0; i < T::RT; ++i) rf[i] = *reinterpret_cast<const intx4 *>(fragment_at(rows, 32 * i + r, 2 * k + h));
-#pragma unroll
-            for (int j = 0; j < T::CT; ++j) {
-                const intx4 cf = *reinterpret_cast<const intx4 *>(fragment_at(cols, 32 * j + r, 2 * k + h));
-#pragma unroll
-                for (int i = 0; i < T::RT; ++i) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(cf, rf[i], acc[i][j], 0, 0, 0);
-            }
-        }
+            for (int i = 0; i < N; ++i) sum[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(cols.half[h], rows[i].half[h], sum[i], 0, 0, 0);
     }
+    static constexpr bool kBySum = false;
 };
 
-// The main loop: stages [from, to) of both operands.  Two buffers: while one is multiplied the other fills.
-template <class T, template <class> class Product>
+// The main loop: stages [from, to) of both operands, from < to.  While one buffer is multiplied the others fill; the
+// last columns of a stage are multiplied after the barrier that ends it, while the first fragments of the next are
+// on their way.  All waves have read what they need of LDS when it returns after one more barrier.
+template <class T, class Product>
 __device__ __forceinline__ void multiply(const Operand &rows, const Operand &cols, int from, int to, char *lds,
-                                         typename Product<T>::Acc (&acc)[T::RT][T::CT])
+                                         typename Product::Acc (&acc)[T::CT][T::RT])
 {
+    typedef typename Product::Acc Acc;
+    typedef Fragment<typename Product::Element> Frag;
+    constexpr int kAhead = T::BUFFERS - 1;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const unsigned at = lds_offset(lds);
     const int wr = wave / T::WC, wc = wave % T::WC;
 #pragma unroll
-    for (int i = 0; i < T::RT; ++i)
+    for (int j = 0; j < T::CT; ++j)
 #pragma unroll
-        for (int j = 0; j < T::CT; ++j)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0;
+        for (int i = 0; i < T::RT; ++i) acc[j][i] = Acc{0, 0, 0, 0};
     const auto fill = [&](int stage, int buffer) {
         stage_operand<T::ROWS, T::WAVES>(rows, stage, at + buffer * T::STAGE, wave, lane);
         stage_operand<T::COLS, T::WAVES>(cols, stage, at + buffer * T::STAGE + T::ROWS * kLine, wave, lane);
     };
-    if (from >= to) return;
-    fill(from, 0);
-    for (int s = from; s < to; ++s) {
-        const int buffer = (s - from) & 1;
-        landed();
-        if (s + 1 < to) fill(s + 1, buffer ^ 1);
+    const FragmentPlace place(lane);
+    for (int b = 0; b < kAhead; ++b)
+        if (from + b < to) fill(from + b, b);
+    int buffer = 0;
+    Frag r[T::RT], c[2];
+    // the first fragments of a stage that has landed
+    const auto begin = [&]() {
         const char *p = lds + buffer * T::STAGE;
-        Product<T>::stage(p + wr * T::RT * 32 * kLine, p + T::ROWS * kLine + wc * T::CT * 32 * kLine, lane, acc);
+        place.load(c[0], p + (T::ROWS + wc * T::CT * 16) * kLine, 0);
+#pragma unroll
+        for (int i = 0; i < T::RT; ++i) place.load(r[i], p + wr * T::RT * 16 * kLine, i);
+    };
+    // sums of columns j are added while columns j + 1 are multiplied
+    Acc sum[T::RT];
+    const auto multiply_by = [&](const Frag (&rows)[T::RT], const Frag &cols, Acc (&to)[T::RT], Acc (&before)[T::RT]) {
+        if (Product::kBySum) {
+            Acc now[T::RT];
+            Product::line(rows, cols, now);
+#pragma unroll
+            for (int i = 0; i < T::RT; ++i) {
+                before[i] += sum[i], sum[i] = now[i];
+                asm volatile("" : "+v"(before[i]));   // (added here, not when the sum is next needed: that keeps them all)
+            }
+#pragma unroll
+            for (int i = 0; i < T::RT; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 3, 0);   // matrix instructions
+                __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);   // vector instructions
+            }
+        } else {
+            Product::line(rows, cols, to);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+#pragma unroll
+    for (int i = 0; i < T::RT; ++i) sum[i] = Acc{0, 0, 0, 0};
+    if (from + kAhead <= to) landed<(kAhead - 1) * T::LOADS>();
+    else landed<0>();
+    if (from + kAhead < to) fill(from + kAhead, kAhead);
+    begin();
+    for (int s = from; s < to; ++s) {
+        const char *p = lds + buffer * T::STAGE + (T::ROWS + wc * T::CT * 16) * kLine;
+#pragma unroll
+        for (int j = 0; j + 1 < T::CT; ++j) {
+            place.load(c[(j + 1) & 1], p, j + 1);
+            multiply_by(r, c[j & 1], acc[j], acc[j == 0 ? T::CT - 1 : j - 1]);
+        }
+        // own reads are done (told to the compiler: it would wait for the next stage's before the products below)
+        __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0)
+        static_assert(T::CT % 2 == 0, "the last columns of a stage are the second of two");
+        const Frag last = c[1];
+        Frag held[T::RT];
+#pragma unroll
+        for (int i = 0; i < T::RT; ++i) held[i] = r[i];
+        if (s + 1 < to) {
+            // (near the end fewer loads are under way: then all of them are awaited)
+            if (s + 1 + kAhead <= to) landed<(kAhead - 1) * T::LOADS>();
+            else landed<0>();
+            const int done = buffer;
+            buffer = buffer == kAhead ? 0 : buffer + 1;
+            if (s + 1 + kAhead < to) fill(s + 1 + kAhead, done);
+            begin();
+        }
+        multiply_by(held, last, acc[T::CT - 1], acc[T::CT - 2]);
+    }
+    if (Product::kBySum)
+#pragma unroll
+        for (int i = 0; i < T::RT; ++i) acc[T::CT - 1][i] += sum[i];
+}
+
+// A launch of W workgroups on `tiles` products of `stages` stages each.  Each takes whole tiles round by round; the
+// tiles left over for less than a round are cut along the summed axis so that all workgroups get the same number
+// of stages.  What a workgroup has of a tile that it does not own whole goes to one of its two slots of a buffer,
+// where a second kernel joins the parts in order.
+struct WorkSplit {
+    int64_t whole;    // tiles [0, whole) are taken whole, a multiple of `workers`
+    int64_t tiles;
+    int stages;
+    int workers;      // workgroups; a multiple of 8 when there are several rounds
+    int cutters;      // workgroups that share the tiles left over
+    __host__ __device__ int64_t left() const { return tiles - whole; }
+    // stages of the tiles left over, counted through, that workgroup w takes: [begin(w), begin(w + 1))
+    __host__ __device__ int64_t begin(int w) const { return left() * stages * w / cutters; }
+    __host__ __device__ int owner(int64_t stage) const { return (int)(((stage + 1) * cutters - 1) / (left() * stages)); }
+};
+
+// Calls f(tile, from, to, slot) for everything workgroup `id` takes; slot < 0: the whole tile.  Ids that run on the
+// same die (every eighth) take neighbouring tiles.
+template <class F>
+__device__ __forceinline__ void for_work(const WorkSplit &w, int id, F &&f)
+{
+    const int each = w.workers / 8;
+    const int place = w.workers % 8 == 0 ? (id & 7) * each + (id >> 3) : id;
+    for (int64_t t = place; t < w.whole; t += w.workers) f(t, 0, w.stages, -1);
+    if (place >= w.cutters) return;
+    int64_t s = w.begin(place);
+    const int64_t end = w.begin(place + 1);
+    while (s < end) {
+        const int64_t tile = s / w.stages;
+        const int from = (int)(s - tile * w.stages);
+        const int to = end - tile * w.stages < w.stages ? (int)(end - tile * w.stages) : w.stages;
+        f(w.whole + tile, uniform(from), uniform(to), from == 0 && to == w.stages ? -1 : 2 * place + (from == 0));
+        s += to - from;
     }
 }
 
-// Calls f(row, col, values) for every group of four adjacent columns a lane holds; row and col within the tile
-template <class T, class Acc, class F>
-__device__ __forceinline__ void for_outputs(Acc (&acc)[T::RT][T::CT], F &&f)
+template <class T, class Acc>
+__device__ __forceinline__ void store_part(Acc *parts, int slot, const Acc (&acc)[T::CT][T::RT])
 {
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const int row = wave / T::WC * T::RT * 32 + (lane & 31), col = wave % T::WC * T::CT * 32 + 4 * (lane >> 5);
+    Acc *to = parts + (int64_t)slot * T::GROUPS * T::THREADS + threadIdx.x;
 #pragma unroll
-    for (int i = 0; i < T::RT; ++i)
+    for (int j = 0; j < T::CT; ++j)
+#pragma unroll
+        for (int i = 0; i < T::RT; ++i) to[(j * T::RT + i) * T::THREADS] = acc[j][i];
+}
+
+// A wave's share of the parts of tile `tile` (counted from the first that is cut), summed in order; false when the
+// tile was taken whole
+template <class T, class Acc>
+__device__ __forceinline__ bool join_parts(const WorkSplit &w, int64_t tile, int wave, const Acc *parts, Acc (&acc)[T::CT][T::RT])
+{
+    const int64_t first = tile * w.stages;
+    const int from = w.owner(first), to = w.owner(first + w.stages - 1);
+    if (from == to) return false;
+#pragma unroll
+    for (int j = 0; j < T::CT; ++j)
+#pragma unroll
+        for (int i = 0; i < T::RT; ++i) acc[j][i] = Acc{0, 0, 0, 0};
+    for (int k = from; k <= to; ++k) {
+        const Acc *at = parts + (int64_t)(2 * k + (w.begin(k) <= first)) * T::GROUPS * T::THREADS + wave * 64 + (threadIdx.x & 63);
 #pragma unroll
         for (int j = 0; j < T::CT; ++j)
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const auto &a = acc[i][j];
-                f(row + 32 * i, col + 32 * j + 8 * g, a[4 * g], a[4 * g + 1], a[4 * g + 2], a[4 * g + 3]);
-            }
+            for (int i = 0; i < T::RT; ++i) acc[j][i] += at[(j * T::RT + i) * T::THREADS];
+    }
+    return true;
 }
 
-// Workgroup id -> place in the order of work: the ids of one die (every eighth) take neighbouring places
-__device__ __forceinline__ int64_t place_of(unsigned id, int64_t total)
+// Calls f(row, col, values) for every 32 x 32 tile of the wave, one after the other: row and col of its corner within
+// the workgroup's tile.  values[2 i + j][e] of a lane is at row 16 i + (lane & 15), column 16 j + 4 (lane >> 4) + e.
+template <class T, class Acc, class F>
+__device__ __forceinline__ void for_wave_tiles(const Acc (&acc)[T::CT][T::RT], int wave, F &&f)
 {
-    const int64_t each = (total + 7) / 8;
-    return (int64_t)(id & 7) * each + (id >> 3);
+    const int row = wave / T::WC * T::RT * 16, col = wave % T::WC * T::CT * 16;
+#pragma unroll
+    for (int j = 0; j < T::CT; j += 2)
+#pragma unroll
+        for (int i = 0; i < T::RT; i += 2) {
+            const Acc v[4] = {acc[j][i], acc[j + 1][i], acc[j][i + 1], acc[j + 1][i + 1]};
+            f(row + 16 * i, col + 16 * j, v);
+            __builtin_amdgcn_sched_barrier(0);   // (one tile's values at a time in registers)
+        }
+}
+
+// Four rows of a lane quad, four 16-bit values of adjacent columns each -> the lane's column (its place in the quad),
+// four adjacent rows
+__device__ __forceinline__ uint2 turn_quad(uint2 x, int lane)
+{
+    constexpr int kXor1 = 0xb1, kXor2 = 0x4e;   // quad_perm
+    const bool upper = lane & 2;
+    const int got = __builtin_amdgcn_mov_dpp((int)(upper ? x.x : x.y), kXor2, 0xf, 0xf, true);
+    const int y0 = upper ? got : (int)x.x, y1 = upper ? (int)x.y : got;
+    const int r0 = __builtin_amdgcn_mov_dpp(y0, kXor1, 0xf, 0xf, true), r1 = __builtin_amdgcn_mov_dpp(y1, kXor1, 0xf, 0xf, true);
+    const unsigned pick = lane & 1 ? 0x03020706u : 0x05040100u;
+    return make_uint2(__builtin_amdgcn_perm((unsigned)r0, (unsigned)y0, pick), __builtin_amdgcn_perm((unsigned)r1, (unsigned)y1, pick));
 }
 
 }  // namespace lmkan

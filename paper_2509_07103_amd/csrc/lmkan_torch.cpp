@@ -27,12 +27,21 @@ struct Library {
     decltype(&lmkan_conv2d_forward) conv2d_forward;
     decltype(&lmkan_conv2d_backward) conv2d_backward;
     decltype(&lmkan_pack) pack;
+    decltype(&lmkan_orthogonalize_workspace_bytes) orthogonalize_workspace_bytes;
+    decltype(&lmkan_orthogonalize) orthogonalize;
+    decltype(&lmkan_muon_step) muon_step;
+    decltype(&lmkan_linear_i8_workspace_bytes) linear_i8_workspace_bytes;
+    decltype(&lmkan_linear_i8) linear_i8;
 } g_lib;
 
 // attribute names, interned once
 enum { kNIn, kNOut, kGrid, kOrder, kDtype, kLayout, kFlags, kDescNames };
 enum { kN, kH, kW, kCIn, kKh, kKw, kStride, kConvNames };
-PyObject *g_desc_names[kDescNames], *g_conv_names[kConvNames];
+enum { kBatch, kRows, kCols, kMatrixDtype, kMatrixNames };
+enum { kLinIn, kLinOut, kXDtype, kYDtype, kRelu, kLinearNames };
+PyObject *g_desc_names[kDescNames], *g_conv_names[kConvNames], *g_matrix_names[kMatrixNames], *g_linear_names[kLinearNames], *g_eps_name;
+enum { kLr, kMomentum, kDecay, kScale, kNesterov, kMuonNames };
+PyObject *g_muon_names[kMuonNames];
 
 template <int N>
 bool read_ints(PyObject *obj, PyObject *const (&names)[N], int32_t (&out)[N])
@@ -58,10 +67,20 @@ bool read_desc(PyObject *obj, lmkan_desc &d)
     return d.n_in >= 2 && d.n_out >= 1 && d.grid >= 3 && d.grid <= LMKAN_MAX_GRID && d.coef_dtype >= 0 && d.coef_dtype <= 2;
 }
 
-at::ScalarType coef_type(const lmkan_desc &d)
+bool read_double(PyObject *obj, PyObject *name, double &out)
 {
-    return d.coef_dtype == LMKAN_F32 ? at::kFloat : d.coef_dtype == LMKAN_F16 ? at::kHalf : at::kBFloat16;
+    PyObject *v = PyObject_GetAttr(obj, name);
+    out = v ? PyFloat_AsDouble(v) : -1.0;
+    Py_XDECREF(v);
+    if (!PyErr_Occurred()) return true;
+    PyErr_Clear();
+    return false;
 }
+
+at::ScalarType type_of(int dtype) { return dtype == LMKAN_F32 ? at::kFloat : dtype == LMKAN_F16 ? at::kHalf : at::kBFloat16; }
+bool known_dtype(int dtype) { return dtype == LMKAN_F32 || dtype == LMKAN_F16 || dtype == LMKAN_BF16; }
+
+at::ScalarType coef_type(const lmkan_desc &d) { return type_of(d.coef_dtype); }
 
 // the tensor behind a Python object, or nullptr
 const at::Tensor *tensor(PyObject *o) { return THPVariable_Check(o) ? &THPVariable_Unpack(o) : nullptr; }
@@ -244,6 +263,140 @@ PyObject *pack(PyObject *, PyObject *const *args, Py_ssize_t n)
     LMKAN_GUARDED_END
 }
 
+// a batch of matrices, and the (a, b, c) of a schedule's steps as the binding keeps them: bytes of float32
+struct Matrices {
+    lmkan_matrices d;
+    const float *schedule;
+    int32_t steps;
+};
+
+bool read_matrices(PyObject *desc, PyObject *schedule, Matrices &m)
+{
+    int32_t v[kMatrixNames];
+    double eps;
+    if (!read_ints(desc, g_matrix_names, v) || !read_double(desc, g_eps_name, eps) || !PyBytes_Check(schedule)) return false;
+    m.d = {v[kBatch], v[kRows], v[kCols], v[kMatrixDtype], (float)eps};
+    m.steps = (int32_t)(PyBytes_GET_SIZE(schedule) / (3 * sizeof(float)));
+    m.schedule = reinterpret_cast<const float *>(PyBytes_AS_STRING(schedule));
+    return m.d.batch >= 0 && m.d.rows >= 1 && m.d.cols >= 1 && known_dtype(m.d.dtype);
+}
+
+bool any_workspace(PyObject *given, size_t need, const at::Tensor &like, at::Tensor &ws, size_t &bytes)
+{
+    if (given != Py_None) {
+        const at::Tensor *t = tensor(given);
+        if (!t || !t->is_cuda() || !t->is_contiguous()) return false;
+        ws = *t;
+        bytes = t->nbytes();
+        return true;
+    }
+    bytes = need;
+    if (bytes > 0) ws = at::empty({(int64_t)bytes}, like.options().dtype(at::kByte));
+    return true;
+}
+
+// orthogonalize(desc, schedule, x, out, workspace) -> out
+PyObject *orthogonalize(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    if (n != 5) Py_RETURN_NONE;
+    LMKAN_GUARDED_BEGIN
+    Matrices m;
+    if (!read_matrices(args[0], args[1], m)) Py_RETURN_NONE;
+    const at::ScalarType type = type_of(m.d.dtype);
+    const std::array<int64_t, 3> shape = {m.d.batch, m.d.rows, m.d.cols};
+    const at::Tensor *x = tensor(args[2]);
+    if (!fits(x, type, shape)) Py_RETURN_NONE;
+    at::Tensor out, ws;
+    size_t bytes = 0;
+    if (args[3] != Py_None) {
+        const at::Tensor *t = tensor(args[3]);
+        if (!fits(t, type, shape)) Py_RETURN_NONE;
+        out = *t;
+    } else {
+        out = at::empty(shape, x->options());
+    }
+    if (!any_workspace(args[4], g_lib.orthogonalize_workspace_bytes(&m.d), *x, ws, bytes)) Py_RETURN_NONE;
+    lmkan_status st;
+    void *s = current_stream(), *xp = data(*x), *op = data(out), *wp = data(ws);
+    Py_BEGIN_ALLOW_THREADS
+    st = g_lib.orthogonalize(&m.d, m.steps, m.schedule, xp, op, wp, bytes, s);
+    Py_END_ALLOW_THREADS
+    if (st != LMKAN_OK) Py_RETURN_NONE;
+    return wrap(out);
+    LMKAN_GUARDED_END
+}
+
+// muon_step(desc, muon, schedule, grad, momentum, weight, workspace) -> weight
+PyObject *muon_step(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    if (n != 7) Py_RETURN_NONE;
+    LMKAN_GUARDED_BEGIN
+    Matrices m;
+    double p[kMuonNames];
+    if (!read_matrices(args[0], args[2], m)) Py_RETURN_NONE;
+    for (int i = 0; i < kMuonNames; ++i)
+        if (!read_double(args[1], g_muon_names[i], p[i])) Py_RETURN_NONE;
+    const lmkan_muon muon = {(float)p[kLr], (float)p[kMomentum], (float)p[kDecay], (float)p[kScale], p[kNesterov] != 0.0};
+    const std::array<int64_t, 3> shape = {m.d.batch, m.d.rows, m.d.cols};
+    const at::Tensor *grad = tensor(args[3]), *momentum = tensor(args[4]), *weight = tensor(args[5]);
+    if (!fits(grad, type_of(m.d.dtype), shape) || !fits(momentum, at::kFloat, shape) || !fits(weight, at::kFloat, shape)) Py_RETURN_NONE;
+    at::Tensor ws;
+    size_t bytes = 0;
+    if (!any_workspace(args[6], g_lib.orthogonalize_workspace_bytes(&m.d), *grad, ws, bytes)) Py_RETURN_NONE;
+    lmkan_status st;
+    float *mp = static_cast<float *>(data(*momentum)), *wp = static_cast<float *>(data(*weight));
+    void *s = current_stream(), *gp = data(*grad), *sp = data(ws);
+    Py_BEGIN_ALLOW_THREADS
+    st = g_lib.muon_step(&m.d, &muon, m.steps, m.schedule, gp, mp, wp, sp, bytes, s);
+    Py_END_ALLOW_THREADS
+    if (st != LMKAN_OK) Py_RETURN_NONE;
+    Py_INCREF(args[5]);
+    return args[5];
+    LMKAN_GUARDED_END
+}
+
+// linear_i8(desc, x, w_codes, w_scale, bias, beta, y, workspace) -> y
+PyObject *linear_i8(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    if (n != 8) Py_RETURN_NONE;
+    LMKAN_GUARDED_BEGIN
+    int32_t v[kLinearNames];
+    if (!read_ints(args[0], g_linear_names, v) || !known_dtype(v[kXDtype]) || !known_dtype(v[kYDtype])) Py_RETURN_NONE;
+    const lmkan_linear d = {v[kLinIn], v[kLinOut], v[kXDtype], v[kYDtype], v[kRelu] ? LMKAN_LINEAR_RELU : 0};
+    const at::Tensor *x = tensor(args[1]), *w = tensor(args[2]), *scale = tensor(args[3]), *bias = tensor(args[4]);
+    const double beta = PyFloat_AsDouble(args[5]);
+    if (PyErr_Occurred()) {
+        PyErr_Clear();
+        Py_RETURN_NONE;
+    }
+    if (!x || x->dim() != 2) Py_RETURN_NONE;
+    const int64_t batch = x->size(0);
+    if (!fits(x, type_of(d.x_dtype), {batch, d.n_in}) || !fits(w, at::kChar, {d.n_out, d.n_in}) || !fits(scale, at::kFloat, {d.n_out}) ||
+        !(args[4] == Py_None || fits(bias, at::kFloat, {d.n_out})))
+        Py_RETURN_NONE;
+    at::Tensor y, ws;
+    size_t bytes = 0;
+    if (args[6] != Py_None) {
+        const at::Tensor *t = tensor(args[6]);
+        if (!fits(t, type_of(d.y_dtype), {batch, d.n_out})) Py_RETURN_NONE;
+        y = *t;
+    } else {
+        if (beta != 0.0) Py_RETURN_NONE;
+        y = at::empty({batch, d.n_out}, x->options().dtype(type_of(d.y_dtype)));
+    }
+    if (!any_workspace(args[7], g_lib.linear_i8_workspace_bytes(&d, batch), *x, ws, bytes)) Py_RETURN_NONE;
+    lmkan_status st;
+    const int8_t *cp = static_cast<const int8_t *>(data(*w));
+    const float *sp = static_cast<const float *>(data(*scale)), *bp = bias ? static_cast<const float *>(data(*bias)) : nullptr;
+    void *s = current_stream(), *xp = data(*x), *yp = data(y), *wp = data(ws);
+    Py_BEGIN_ALLOW_THREADS
+    st = g_lib.linear_i8(&d, batch, xp, cp, sp, bp, (float)beta, yp, wp, bytes, s);
+    Py_END_ALLOW_THREADS
+    if (st != LMKAN_OK) Py_RETURN_NONE;
+    return wrap(y);
+    LMKAN_GUARDED_END
+}
+
 // init(the addresses, in the order of Library)
 PyObject *init(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
@@ -266,6 +419,9 @@ PyMethodDef g_methods[] = {{"init", (PyCFunction)(void (*)(void))init, METH_FAST
                            {"forward", (PyCFunction)(void (*)(void))forward, METH_FASTCALL, nullptr},
                            {"backward", (PyCFunction)(void (*)(void))backward, METH_FASTCALL, nullptr},
                            {"pack", (PyCFunction)(void (*)(void))pack, METH_FASTCALL, nullptr},
+                           {"orthogonalize", (PyCFunction)(void (*)(void))orthogonalize, METH_FASTCALL, nullptr},
+                           {"muon_step", (PyCFunction)(void (*)(void))muon_step, METH_FASTCALL, nullptr},
+                           {"linear_i8", (PyCFunction)(void (*)(void))linear_i8, METH_FASTCALL, nullptr},
                            {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
@@ -278,5 +434,12 @@ PyMODINIT_FUNC PyInit__native(void)
     static const char *conv[] = {"n", "h", "w", "c_in", "kh", "kw", "stride"};
     for (int i = 0; i < kDescNames; ++i) g_desc_names[i] = PyUnicode_InternFromString(desc[i]);
     for (int i = 0; i < kConvNames; ++i) g_conv_names[i] = PyUnicode_InternFromString(conv[i]);
+    static const char *matrix[] = {"batch", "rows", "cols", "dtype"};
+    static const char *muon[] = {"lr", "momentum", "weight_decay", "scale", "nesterov"};
+    static const char *linear[] = {"n_in", "n_out", "x_dtype", "y_dtype", "relu"};
+    for (int i = 0; i < kMatrixNames; ++i) g_matrix_names[i] = PyUnicode_InternFromString(matrix[i]);
+    for (int i = 0; i < kMuonNames; ++i) g_muon_names[i] = PyUnicode_InternFromString(muon[i]);
+    for (int i = 0; i < kLinearNames; ++i) g_linear_names[i] = PyUnicode_InternFromString(linear[i]);
+    g_eps_name = PyUnicode_InternFromString("eps");
     return PyModule_Create(&g_module);
 }
