@@ -47,6 +47,12 @@ size_t ortho_workspace_bytes(const MatrixShape &s);
 void launch_ortho(const MatrixShape &s, int steps, const float *schedule, const UpdateArgs &u, void *workspace,
                   hipStream_t stream);
 
+// Matrices whose shorter side is at most 64 (lmkan_ortho_small.hip); reached through launch_ortho
+bool ortho_small_applicable(const MatrixShape &s, int steps);
+size_t ortho_small_workspace_bytes(const MatrixShape &s);
+void launch_ortho_small(const MatrixShape &s, int steps, const float *schedule, const UpdateArgs &u, void *workspace,
+                        hipStream_t stream);
+
 struct LinearShape {
     int64_t batch;
     int n_in, n_out;

@@ -478,12 +478,18 @@ bool schedule_bounds(int steps, const float *schedule, ScheduleBounds *bounds)
 size_t ortho_workspace_bytes(const MatrixShape &s)
 {
     const int64_t most = matrices_at_once(s), left = s.batch % most;
+    if (ortho_small_applicable(s, 1)) {
+        // (a call without steps sums norms only)
+        const size_t small = ortho_small_workspace_bytes(s), norms = align256(most * kNormParts * sizeof(double));
+        return small > norms ? small : norms;
+    }
     const size_t whole = layout_of(s, most).total, rest = left ? layout_of(s, left).total : 0;
     return whole > rest ? whole : rest;
 }
 
 void launch_ortho(const MatrixShape &s, int steps, const float *schedule, const UpdateArgs &u, void *workspace, hipStream_t stream)
 {
+    if (ortho_small_applicable(s, steps)) return launch_ortho_small(s, steps, schedule, u, workspace, stream);
     ScheduleBounds bounds;
     (void)schedule_bounds(steps, schedule, &bounds);
     const int m = s.m(), n = s.n();

@@ -1,0 +1,585 @@
+// Orthogonalisation of matrices whose shorter side is at most 64, in float32 matrix instructions.
+//
+// The steps are those of lmkan_ortho.hip: up to three on the m x m Gram matrix, applied together.  Here the Gram
+// matrix and its polynomials fit the LDS of one workgroup, so that a matrix costs
+//   one launch   where X fits LDS too (whole_kernel): X is read once and the result written once;
+//   five         where it is longer (five steps): Gram matrix in parts, polynomial, apply and next Gram matrix in
+//                parts, polynomial, apply.
+// The products with X take 2 m multiply-adds per element and pass; at m = 64 the float32 instructions (157 TFLOP/s)
+// take about as long for that as memory takes for the element, so nothing is gained by splitting factors.
+//
+// Norms: |X|^2 is the trace of the Gram matrix of the raw direction D, A_0 = D D^T / (|D| + eps)^2 and the first
+// polynomial is scaled by 1 / (|D| + eps).  The trace and the sum of the parts are taken in float64.  Elements beyond
+// 2^50, whose squares might exceed float32, are scaled by 2^-100 in the Gram matrix of their part.
+#include "lmkan_dense.h"
+
+#include <math.h>
+
+#include "lmkan_kernels.h"
+#include "lmkan_tile.h"
+
+namespace lmkan {
+
+namespace {
+
+constexpr int kStepsAtOnce = 3;            // steps on one Gram matrix (as for larger matrices)
+constexpr float kLarge = 0x1p50f;          // elements beyond it are scaled in Gram matrices
+constexpr float kDown = 0x1p-100f;
+constexpr int kSmallLds = 150 * 1024;      // of 160 KiB
+constexpr int kMostParts = 512;            // parts of a Gram matrix
+
+// e / d for e < 2^16, d <= 2^12
+struct Divide {
+    unsigned magic, d;
+    __device__ __forceinline__ int quotient(int e) const { return d == 1 ? e : (int)__umulhi((unsigned)e, magic); }
+    static Divide by(int d) { return {(unsigned)(((1ull << 32) + d - 1) / d), (unsigned)d}; }
+};
+
+struct SmallArgs {
+    MatrixShape s;
+    UpdateArgs u;
+    int steps, from, to;                   // steps [from, to) of the schedule
+    float schedule[3 * LMKAN_MAX_ORTHO_STEPS];
+    int columns;                           // of X in LDS at a time, a multiple of 16
+    Divide by_columns, by_m, by_n;
+    int parts;                             // workgroups that share a matrix
+    float *gram;                           // [matrices][parts][M][M], upper tiles
+    unsigned *scaled;                      // [matrices][parts]: whether kDown was applied
+    float *poly;                           // [matrices][M][M]
+    float *x;                              // [matrices][m][n]: X after a polynomial
+};
+
+// element (row, column) of the direction, seen with the shorter side first
+__device__ __forceinline__ int64_t stored_at(const MatrixShape &s, int64_t matrix, int row, int column)
+{
+    return matrix * s.elems() + (s.flip() ? (int64_t)column * s.cols + row : (int64_t)row * s.cols + column);
+}
+
+// The direction's element `at` in two halves, so that many loads can be under way: what it is made of, and the element.
+// `move`: the momentum moves.
+struct Raw {
+    float g, m;
+};
+__device__ __forceinline__ Raw fetch(const UpdateArgs &u, int dtype, int64_t at, bool move)
+{
+    Raw r;
+    r.g = !u.momentum || u.nesterov || move ? load_as_float(u.grad, at, dtype) : 0.0f;
+    r.m = u.momentum ? u.momentum[at] : 0.0f;
+    return r;
+}
+__device__ __forceinline__ float direction(const UpdateArgs &u, Raw r, int64_t at, bool move)
+{
+    if (!u.momentum) return r.g;
+    if (move) u.momentum[at] = r.m = u.beta * r.m + (1.0f - u.beta) * r.g;
+    return u.nesterov ? u.beta * r.m + (1.0f - u.beta) * r.g : r.m;
+}
+
+__device__ __forceinline__ void store_result(const SmallArgs &a, int64_t at, float v)
+{
+    if (a.u.weight) a.u.weight[at] = a.u.keep * a.u.weight[at] + a.u.add * v;
+    else store_from_float(a.u.out, at, a.s.dtype, v);
+}
+
+// M: the shorter side rounded up to 16; WAVES of a workgroup
+template <int M_, int WAVES_>
+struct Small {
+    static constexpr int M = M_, WAVES = WAVES_, THREADS = 64 * WAVES;
+    static constexpr int T = M / 16, TILES = T * (T + 1) / 2;                 // tiles of a symmetric matrix
+    static constexpr int SHARE = TILES < WAVES && TILES == 1 ? WAVES : 1;     // waves that share a tile's summed axis
+    static constexpr int EACH = SHARE > 1 ? 1 : (TILES + WAVES - 1) / WAVES;  // tiles of a wave
+    static constexpr int PITCH = M + 4;
+    static constexpr int SQUARE = M * PITCH;                                  // floats of an M x M matrix in LDS
+
+    // tile t of the upper triangle, column by column
+    static __device__ __forceinline__ void tile(int t, int *i, int *j)
+    {
+        int c = 0;
+        while ((c + 1) * (c + 2) / 2 <= t) ++c;
+        *j = c, *i = t - c * (c + 1) / 2;
+    }
+
+    // a lane's four values along the summed axis of row `row + (lane & 15)`: 4 (lane >> 4) ..
+    static __device__ __forceinline__ floatx4 along(const float *lds, int pitch, int row, int k, int lane)
+    {
+        return *reinterpret_cast<const floatx4 *>(lds + (row + (lane & 15)) * pitch + k + 4 * (lane >> 4));
+    }
+    static __device__ __forceinline__ floatx4 multiply(const floatx4 &cols, const floatx4 &rows, floatx4 acc)
+    {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(cols[e], rows[e], acc, 0, 0, 0);
+        return acc;
+    }
+
+    // X: columns [first, first + columns) of all rows to LDS, zero beyond the matrix; returns whether one is large.
+    // get(row, column) loads, use(loaded, row, column) makes the element of it.
+    template <class G, class U>
+    static __device__ __forceinline__ bool load(float *x, int pitch, const MatrixShape &s, int first, int columns, const Divide &by_columns, G &&get, U &&use)
+    {
+        constexpr int kAtOnce = 8;
+        bool large = false;
+        const int m = s.m(), n = s.n();
+        const bool flip = s.flip();
+        for (int e0 = threadIdx.x; e0 < M * columns; e0 += kAtOnce * THREADS) {
+            Raw raw[kAtOnce];
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u) {
+                // neighbouring lanes take neighbouring elements of what is stored
+                const int e = e0 + u * THREADS, q = flip ? e / M : by_columns.quotient(e);
+                const int r = flip ? e % M : q, c = flip ? q : e - q * columns;
+                if (e < M * columns && r < m && first + c < n) raw[u] = get(r, first + c);
+            }
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u) {
+                const int e = e0 + u * THREADS, q = flip ? e / M : by_columns.quotient(e);
+                const int r = flip ? e % M : q, c = flip ? q : e - q * columns;
+                if (e >= M * columns) break;
+                const float v = r < m && first + c < n ? use(raw[u], r, first + c) : 0.0f;
+                large |= !(fabsf(v) <= kLarge);
+                x[r * pitch + c] = v;
+            }
+        }
+        return large;
+    }
+
+    // acc += X X^T over the columns in LDS, the wave's tiles
+    static __device__ __forceinline__ void gram(const float *x, int pitch, int columns, int wave, int lane, floatx4 (&acc)[EACH])
+    {
+#pragma unroll
+        for (int q = 0; q < EACH; ++q) {
+            const int t = SHARE > 1 ? 0 : wave + q * WAVES;
+            if (t >= TILES) break;
+            int i, j;
+            tile(t, &i, &j);
+            for (int k = SHARE > 1 ? 16 * wave : 0; k < columns; k += 16 * SHARE)
+                acc[q] = multiply(along(x, pitch, 16 * j, k, lane), along(x, pitch, 16 * i, k, lane), acc[q]);
+        }
+    }
+
+    // Calls f(row, col, values): four adjacent columns of a row of the wave's tiles.  SHARE: sums over the waves first,
+    // through `scratch` (4 floats a thread); wave 0 goes on.
+    template <class F>
+    static __device__ __forceinline__ void for_tiles(floatx4 (&acc)[EACH], int wave, int lane, float *scratch, F &&f)
+    {
+        if (SHARE > 1) {
+            *reinterpret_cast<floatx4 *>(scratch + 4 * threadIdx.x) = acc[0];
+            __syncthreads();
+            if (wave != 0) return;
+            for (int w = 1; w < WAVES; ++w) acc[0] += *reinterpret_cast<const floatx4 *>(scratch + 4 * (64 * w + lane));
+        }
+#pragma unroll
+        for (int q = 0; q < EACH; ++q) {
+            const int t = SHARE > 1 ? 0 : wave + q * WAVES;
+            if (t >= TILES) break;
+            int i, j;
+            tile(t, &i, &j);
+            f(16 * i + (lane & 15), 16 * j + 4 * (lane >> 4), i != j, acc[q]);
+        }
+    }
+
+    // D = f(L R), all three symmetric; D may be L or R
+    template <class F>
+    static __device__ __forceinline__ void product(float *d, const float *l, const float *r, int wave, int lane, F &&f)
+    {
+        floatx4 acc[EACH];
+#pragma unroll
+        for (int q = 0; q < EACH; ++q) {
+            acc[q] = floatx4{0, 0, 0, 0};
+            const int t = wave + q * WAVES;
+            if (t >= TILES) break;
+            int i, j;
+            tile(t, &i, &j);
+#pragma unroll
+            for (int k = 0; k < M; k += 16) acc[q] = multiply(along(r, PITCH, 16 * j, k, lane), along(l, PITCH, 16 * i, k, lane), acc[q]);
+        }
+        // (in place: all have read; f may read d at its own element)
+        floatx4 v[EACH];
+#pragma unroll
+        for (int q = 0; q < EACH; ++q) {
+            const int t = wave + q * WAVES;
+            if (t >= TILES) break;
+            int i, j;
+            tile(t, &i, &j);
+            v[q] = f(16 * i + (lane & 15), 16 * j + 4 * (lane >> 4), acc[q]);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < EACH; ++q) {
+            const int t = wave + q * WAVES;
+            if (t >= TILES) break;
+            int i, j;
+            tile(t, &i, &j);
+            const int row = 16 * i + (lane & 15), col = 16 * j + 4 * (lane >> 4);
+            *reinterpret_cast<floatx4 *>(d + row * PITCH + col) = v[q];
+            if (i != j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) d[(col + e) * PITCH + row] = v[q][e];
+        }
+        __syncthreads();
+    }
+
+    // The steps [from, to) of the schedule on the Gram matrix `a` in LDS: leaves their polynomial in `p`
+    static __device__ __forceinline__ void polynomial(const SmallArgs &s, int from, int to, float *a, float *b, float *p, int wave, int lane)
+    {
+        for (int k = from; k < to; ++k) {
+            const float c0 = s.schedule[3 * k], c1 = s.schedule[3 * k + 1], c2 = s.schedule[3 * k + 2];
+            float *step = k == from ? p : b;
+            product(step, a, a, wave, lane, [&](int row, int col, floatx4 v) {
+                const floatx4 g = *reinterpret_cast<const floatx4 *>(a + row * PITCH + col);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = c2 * v[e] + c1 * g[e] + (row == col + e ? c0 : 0.0f);
+                return v;
+            });
+            const auto same = [](int, int, floatx4 v) { return v; };
+            if (k + 1 < to) {
+                product(a, step, a, wave, lane, same);
+                product(a, a, step, wave, lane, same);
+            }
+            if (k > from) product(p, b, p, wave, lane, same);
+        }
+    }
+
+    // X <- P X over the columns in LDS; a wave takes 16 columns at a time, in place
+    static __device__ __forceinline__ void apply(const float *p, float *x, int pitch, int columns, int wave, int lane)
+    {
+        for (int c = 16 * wave; c < columns; c += 16 * WAVES) {
+            floatx4 acc[T];
+#pragma unroll
+            for (int i = 0; i < T; ++i) acc[i] = floatx4{0, 0, 0, 0};
+#pragma unroll
+            for (int k = 0; k < M; k += 16) {
+                floatx4 v;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = x[(k + 4 * (lane >> 4) + e) * pitch + c + (lane & 15)];
+#pragma unroll
+                for (int i = 0; i < T; ++i) acc[i] = multiply(v, along(p, PITCH, 16 * i, k, lane), acc[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < T; ++i) *reinterpret_cast<floatx4 *>(x + (16 * i + (lane & 15)) * pitch + c + 4 * (lane >> 4)) = acc[i];
+        }
+    }
+};
+
+// The Gram matrix of the raw direction to that of X_0, in place, from its trace; returns 1 / (norm + eps).
+// `unit`: what it has to be multiplied by (scaled elements).
+template <class S>
+__device__ __forceinline__ float normalise(float *a, int m, double unit, float eps, double *shared, int lane)
+{
+    __syncthreads();
+    if (threadIdx.x < 64) {
+        double trace = lane < m ? (double)a[lane * S::PITCH + lane] : 0.0;
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) trace += __shfl_xor(trace, d, 64);
+        if (lane == 0) *shared = 1.0 / (sqrt(trace * unit) + (double)eps);
+    }
+    __syncthreads();
+    const double inverse = *shared;
+    const double f = inverse * inverse * unit;
+    for (int e = threadIdx.x; e < S::SQUARE; e += S::THREADS) a[e] = (float)((double)a[e] * f);
+    __syncthreads();
+    return (float)inverse;
+}
+
+template <class S>
+__device__ __forceinline__ void scale_square(float *p, float f)
+{
+    for (int e = threadIdx.x; e < S::SQUARE; e += S::THREADS) p[e] *= f;
+    __syncthreads();
+}
+
+template <class S>
+__device__ __forceinline__ void put_symmetric(float *a, int row, int col, bool mirror, const floatx4 &v)
+{
+    *reinterpret_cast<floatx4 *>(a + row * S::PITCH + col) = v;
+    if (mirror)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) a[(col + e) * S::PITCH + row] = v[e];
+}
+
+template <class S>
+__device__ __forceinline__ void scale_columns(float *x, int pitch, int columns, float f)
+{
+    for (int e = threadIdx.x; e < S::M * pitch; e += S::THREADS) x[e] *= f;
+    __syncthreads();
+}
+
+// A workgroup per matrix, all of it in LDS: X and three M x M matrices
+template <class S>
+__global__ __launch_bounds__(S::THREADS) void whole_kernel(SmallArgs a)
+{
+    extern __shared__ __align__(16) float lds[];
+    __shared__ double shared;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int64_t matrix = blockIdx.x;
+    const int columns = a.columns, pitch = columns + 4, m = a.s.m(), n = a.s.n();
+    float *gram = lds, *b = gram + S::SQUARE, *p = b + S::SQUARE, *x = p + S::SQUARE, *scratch = x + S::M * pitch;
+    const bool large = S::load(
+        x, pitch, a.s, 0, columns, a.by_columns, [&](int r, int c) { return fetch(a.u, a.s.dtype, stored_at(a.s, matrix, r, c), true); },
+        [&](Raw v, int r, int c) { return direction(a.u, v, stored_at(a.s, matrix, r, c), true); });
+    const bool down = __syncthreads_or(large);
+    if (down) scale_columns<S>(x, pitch, columns, kDown);
+    for (int k = 0; k < a.steps;) {
+        const int end = k + kStepsAtOnce < a.steps ? k + kStepsAtOnce : a.steps;
+        floatx4 acc[S::EACH];
+#pragma unroll
+        for (int q = 0; q < S::EACH; ++q) acc[q] = floatx4{0, 0, 0, 0};
+        S::gram(x, pitch, columns, wave, lane, acc);
+        S::for_tiles(acc, wave, lane, scratch, [&](int row, int col, bool mirror, const floatx4 &v) { put_symmetric<S>(gram, row, col, mirror, v); });
+        float inverse = 1.0f;
+        // (the raw direction times 2^-100 has a norm that is so many times smaller, eps with it)
+        if (k == 0) inverse = normalise<S>(gram, m, 1.0, down ? a.s.eps * kDown : a.s.eps, &shared, lane);
+        else __syncthreads();
+        S::polynomial(a, k, end, gram, b, p, wave, lane);
+        if (k == 0) scale_square<S>(p, inverse);
+        S::apply(p, x, pitch, columns, wave, lane);
+        __syncthreads();
+        k = end;
+    }
+    const bool flip = a.s.flip();
+#pragma unroll 4
+    for (int e = threadIdx.x; e < m * n; e += S::THREADS) {
+        const int q = flip ? a.by_m.quotient(e) : a.by_n.quotient(e), left = e - q * (flip ? m : n);
+        store_result(a, matrix * a.s.elems() + e, flip ? x[left * pitch + q] : x[q * pitch + left]);
+    }
+}
+
+// Part of the Gram matrices of the raw direction: grid (parts, matrices)
+template <class S>
+__global__ __launch_bounds__(S::THREADS) void gram_kernel(SmallArgs a)
+{
+    extern __shared__ __align__(16) float lds[];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int64_t matrix = blockIdx.y;
+    const int columns = a.columns, pitch = columns + 4, n = a.s.n();
+    float *x = lds, *scratch = lds + S::M * pitch;
+    floatx4 acc[S::EACH];
+#pragma unroll
+    for (int q = 0; q < S::EACH; ++q) acc[q] = floatx4{0, 0, 0, 0};
+    bool down = false;
+    for (int64_t first = (int64_t)blockIdx.x * columns; first < n; first += (int64_t)a.parts * columns) {
+        const bool large = S::load(
+            x, pitch, a.s, (int)first, columns, a.by_columns, [&](int r, int c) { return fetch(a.u, a.s.dtype, stored_at(a.s, matrix, r, c), true); },
+            [&](Raw v, int r, int c) { return direction(a.u, v, stored_at(a.s, matrix, r, c), true); });
+        const bool now = __syncthreads_or(large);
+        if (now && !down) {
+            down = true;
+#pragma unroll
+            for (int q = 0; q < S::EACH; ++q) acc[q] *= kDown, acc[q] *= kDown;
+        }
+        if (down) scale_columns<S>(x, pitch, columns, kDown);
+        S::gram(x, pitch, columns, wave, lane, acc);
+        __syncthreads();
+    }
+    float *to = a.gram + (matrix * a.parts + blockIdx.x) * S::M * S::M;
+    S::for_tiles(acc, wave, lane, scratch, [&](int row, int col, bool, const floatx4 &v) { *reinterpret_cast<floatx4 *>(to + row * S::M + col) = v; });
+    if (threadIdx.x == 0) a.scaled[matrix * a.parts + blockIdx.x] = down;
+}
+
+// The polynomial of a matrix from the parts of its Gram matrix: a workgroup per matrix.  The first is scaled by the
+// inverse of the norm.
+template <class S>
+__global__ __launch_bounds__(S::THREADS) void polynomial_kernel(SmallArgs a)
+{
+    extern __shared__ __align__(16) float lds[];
+    __shared__ double shared;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int64_t matrix = blockIdx.x;
+    float *gram = lds, *b = gram + S::SQUARE, *p = b + S::SQUARE;
+    const float *from = a.gram + matrix * a.parts * S::M * S::M;
+    const unsigned *scaled = a.scaled + matrix * a.parts;
+    bool any = false;
+    if (a.from == 0)
+        for (int k = threadIdx.x; k < a.parts; k += S::THREADS) any |= scaled[k] != 0;
+    any = __syncthreads_or(any);
+    for (int e = threadIdx.x; e < S::M * S::M; e += S::THREADS) {
+        const int i = e / S::M, j = e % S::M;
+        if (i / 16 > j / 16) continue;
+        double sum = 0.0;
+        if (any) {
+            // all in the units of the scaled ones
+            for (int k = 0; k < a.parts; ++k) sum += (double)from[(int64_t)k * S::M * S::M + e] * (scaled[k] ? 1.0 : 0x1p-200);
+        } else {
+            for (int k = 0; k < a.parts; ++k) sum += (double)from[(int64_t)k * S::M * S::M + e];
+        }
+        gram[i * S::PITCH + j] = (float)sum;
+        if (i / 16 != j / 16) gram[j * S::PITCH + i] = (float)sum;
+    }
+    float inverse = 1.0f;
+    if (a.from == 0) inverse = normalise<S>(gram, a.s.m(), 1.0, any ? a.s.eps * kDown : a.s.eps, &shared, lane);
+    else __syncthreads();
+    S::polynomial(a, a.from, a.to, gram, b, p, wave, lane);
+    if (any) inverse *= kDown;   // (the direction itself is not scaled)
+    float *to = a.poly + matrix * S::M * S::M;
+    for (int e = threadIdx.x; e < S::M * S::M; e += S::THREADS) to[e] = p[e / S::M * S::PITCH + e % S::M] * inverse;
+}
+
+// X <- P X, from the direction (the first time) or from X: with LAST to the result, else to X and to the parts of its
+// Gram matrix.  grid (parts, matrices)
+template <class S, bool LAST>
+__global__ __launch_bounds__(S::THREADS) void apply_kernel(SmallArgs a)
+{
+    extern __shared__ __align__(16) float lds[];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int64_t matrix = blockIdx.y;
+    const int columns = a.columns, pitch = columns + 4, m = a.s.m(), n = a.s.n();
+    float *p = lds, *x = p + S::SQUARE, *scratch = x + S::M * pitch;
+    for (int e = threadIdx.x; e < S::M * S::M; e += S::THREADS) p[e / S::M * S::PITCH + e % S::M] = a.poly[matrix * S::M * S::M + e];
+    floatx4 acc[S::EACH];
+#pragma unroll
+    for (int q = 0; q < S::EACH; ++q) acc[q] = floatx4{0, 0, 0, 0};
+    const float *held = a.x + matrix * (int64_t)m * n;
+    MatrixShape seen = a.s;   // X itself lies with the shorter side first
+    if (a.from != 0) seen.rows = m, seen.cols = n;
+    for (int64_t first = (int64_t)blockIdx.x * columns; first < n; first += (int64_t)a.parts * columns) {
+        S::load(
+            x, pitch, seen, (int)first, columns, a.by_columns,
+            [&](int r, int c) {
+                return a.from != 0 ? Raw{held[(int64_t)r * n + c], 0.0f} : fetch(a.u, a.s.dtype, stored_at(a.s, matrix, r, c), false);
+            },
+            [&](Raw v, int r, int c) { return a.from != 0 ? v.g : direction(a.u, v, 0, false); });
+        __syncthreads();
+        S::apply(p, x, pitch, columns, wave, lane);
+        __syncthreads();
+        const int count = n - first < columns ? (int)(n - first) : columns;
+        if (LAST) {
+            const bool flip = a.s.flip();
+#pragma unroll 4
+            for (int e = threadIdx.x; e < S::M * columns; e += S::THREADS) {
+                const int q = flip ? e / S::M : a.by_columns.quotient(e);
+                const int r = flip ? e % S::M : q, c = flip ? q : e - q * columns;
+                if (r < m && c < count) store_result(a, stored_at(a.s, matrix, r, (int)first + c), x[r * pitch + c]);
+            }
+        } else {
+            float *to = a.x + matrix * (int64_t)m * n + first;
+#pragma unroll 4
+            for (int e = threadIdx.x; e < S::M * columns; e += S::THREADS) {
+                const int r = a.by_columns.quotient(e), c = e - r * columns;
+                if (r < m && c < count) to[(int64_t)r * n + c] = x[r * pitch + c];
+            }
+            S::gram(x, pitch, columns, wave, lane, acc);
+        }
+        __syncthreads();
+    }
+    if (!LAST) {
+        float *to = a.gram + (matrix * a.parts + blockIdx.x) * S::M * S::M;
+        S::for_tiles(acc, wave, lane, scratch, [&](int row, int col, bool, const floatx4 &v) { *reinterpret_cast<floatx4 *>(to + row * S::M + col) = v; });
+    }
+}
+
+int round16(int n) { return (n + 15) / 16 * 16; }
+size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
+
+size_t square_bytes(int M) { return (size_t)M * (M + 4) * sizeof(float); }
+size_t whole_lds(const MatrixShape &s)
+{
+    const size_t M = round16(s.m());
+    // (the waves of a matrix of one tile share its sums)
+    return 3 * square_bytes((int)M) + M * (round16(s.n()) + 4) * sizeof(float) + (M == 16 ? 4 * 256 * sizeof(float) : 0);
+}
+bool whole(const MatrixShape &s) { return s.n() <= 4096 && whole_lds(s) <= kSmallLds; }
+
+// columns in LDS at a time of a long matrix: 16 KiB of X
+int columns_of(int M) { return 4096 / M / 16 * 16; }
+
+int parts_of(const MatrixShape &s, int64_t count)
+{
+    const int columns = columns_of(round16(s.m()));
+    const int64_t blocks = ((int64_t)s.n() + columns - 1) / columns;
+    int64_t parts = (1024 + count - 1) / count;   // four workgroups a compute unit
+    parts = parts < blocks ? parts : blocks;
+    return (int)(parts < kMostParts ? parts : kMostParts);
+}
+
+struct Layout {
+    size_t gram, scaled, poly, x, total;
+};
+Layout layout_of(const MatrixShape &s, int64_t count)
+{
+    Layout l = {};
+    if (whole(s)) return l;
+    const size_t M = round16(s.m()), parts = parts_of(s, count);
+    size_t at = 0;
+    const auto take = [&](size_t bytes) { const size_t here = at; at += align256(bytes); return here; };
+    l.gram = take(count * parts * M * M * sizeof(float));
+    l.scaled = take(count * parts * sizeof(unsigned));
+    l.poly = take(count * M * M * sizeof(float));
+    l.x = take(count * s.elems() * sizeof(float));
+    l.total = at;
+    return l;
+}
+
+// matrices that share the workspace at a time: 512 M elements, and what a grid takes
+int64_t matrices_at_once(const MatrixShape &s)
+{
+    if (whole(s)) return s.batch;
+    int64_t most = ((int64_t)512 << 20) / s.elems();
+    most = most < 1 ? 1 : most > 32768 ? 32768 : most;
+    const int64_t parts = (s.batch + most - 1) / most;
+    return (s.batch + parts - 1) / parts;
+}
+
+template <class S>
+void launch(const MatrixShape &s, const UpdateArgs &update, SmallArgs a, char *ws, hipStream_t stream)
+{
+    if (whole(s)) {
+        a.columns = round16(s.n());
+        a.by_columns = Divide::by(a.columns), a.by_m = Divide::by(s.m()), a.by_n = Divide::by(s.n());
+        const size_t lds = whole_lds(s);
+        if (lds > 65536) allow_large_lds(reinterpret_cast<const void *>(whole_kernel<S>), kSmallLds);
+        whole_kernel<S><<<(unsigned)s.batch, S::THREADS, lds, stream>>>(a);
+        return;
+    }
+    const int64_t most = matrices_at_once(s);
+    const size_t item = s.dtype == LMKAN_F32 ? 4 : 2;
+    a.columns = columns_of(S::M);
+    a.by_columns = Divide::by(a.columns);
+    const size_t block = (size_t)S::M * (a.columns + 4) * sizeof(float), scratch = 4 * S::THREADS * sizeof(float), square = square_bytes(S::M);
+    for (int64_t first = 0; first < s.batch; first += most) {
+        const int64_t count = s.batch - first < most ? s.batch - first : most, skip = first * s.elems();
+        const Layout l = layout_of(s, count);
+        a.parts = parts_of(s, count);
+        a.gram = reinterpret_cast<float *>(ws + l.gram), a.scaled = reinterpret_cast<unsigned *>(ws + l.scaled);
+        a.poly = reinterpret_cast<float *>(ws + l.poly), a.x = reinterpret_cast<float *>(ws + l.x);
+        a.u.grad = static_cast<const char *>(update.grad) + skip * item;
+        a.u.momentum = update.momentum ? update.momentum + skip : nullptr;
+        a.u.weight = update.weight ? update.weight + skip : nullptr;
+        a.u.out = update.out ? static_cast<char *>(update.out) + skip * item : nullptr;
+        const dim3 grid(a.parts, (unsigned)count);
+        a.from = 0;
+        gram_kernel<S><<<grid, S::THREADS, block + scratch, stream>>>(a);
+        for (; a.from < a.steps; a.from = a.to) {
+            a.to = a.from + kStepsAtOnce < a.steps ? a.from + kStepsAtOnce : a.steps;
+            polynomial_kernel<S><<<(unsigned)count, S::THREADS, 3 * square, stream>>>(a);
+            if (a.to == a.steps) apply_kernel<S, true><<<grid, S::THREADS, square + block, stream>>>(a);
+            else apply_kernel<S, false><<<grid, S::THREADS, square + block + scratch, stream>>>(a);
+        }
+    }
+}
+
+}  // namespace
+
+bool ortho_small_applicable(const MatrixShape &s, int steps) { return s.m() <= 64 && steps > 0; }
+
+size_t ortho_small_workspace_bytes(const MatrixShape &s)
+{
+    const int64_t most = matrices_at_once(s), left = s.batch % most;
+    const size_t full = layout_of(s, most).total, rest = left ? layout_of(s, left).total : 0;
+    return full > rest ? full : rest;
+}
+
+void launch_ortho_small(const MatrixShape &s, int steps, const float *schedule, const UpdateArgs &u, void *workspace, hipStream_t stream)
+{
+    SmallArgs a = {};
+    a.s = s;
+    a.u = u;
+    a.steps = steps;
+    for (int k = 0; k < 3 * steps; ++k) a.schedule[k] = schedule[k];
+    char *ws = static_cast<char *>(workspace);
+    // a wave a matrix where there is one tile and little to load
+    if (s.m() <= 16 && s.n() <= 256) launch<Small<16, 1>>(s, u, a, ws, stream);
+    else if (s.m() <= 16) launch<Small<16, 4>>(s, u, a, ws, stream);
+    else if (s.m() <= 32) launch<Small<32, 4>>(s, u, a, ws, stream);
+    else if (s.m() <= 48) launch<Small<48, 4>>(s, u, a, ws, stream);
+    else launch<Small<64, 4>>(s, u, a, ws, stream);
+}
+
+}  // namespace lmkan
