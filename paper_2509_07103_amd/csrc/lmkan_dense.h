@@ -90,6 +90,25 @@ __device__ __forceinline__ void store_from_float(void *p, int64_t i, int dtype, 
     else static_cast<uint16_t *>(p)[i] = bf16_bits(v);
 }
 
+// The direction's element `at` in two halves, so that many loads can be under way: what it is made of, and the element.
+// `move`: the momentum moves.
+struct Raw {
+    float g, m;
+};
+__device__ __forceinline__ Raw fetch(const UpdateArgs &u, int dtype, int64_t at, bool move)
+{
+    Raw r;
+    r.g = !u.momentum || u.nesterov || move ? load_as_float(u.grad, at, dtype) : 0.0f;
+    r.m = u.momentum ? u.momentum[at] : 0.0f;
+    return r;
+}
+__device__ __forceinline__ float direction(const UpdateArgs &u, Raw r, int64_t at, bool move)
+{
+    if (!u.momentum) return r.g;
+    if (move) u.momentum[at] = r.m = u.beta * r.m + (1.0f - u.beta) * r.g;
+    return u.nesterov ? u.beta * r.m + (1.0f - u.beta) * r.g : r.m;
+}
+
 // two adjacent 16-bit elements, the first in the lower half
 __device__ __forceinline__ uint32_t two_from_float(int dtype, float a, float b)
 {

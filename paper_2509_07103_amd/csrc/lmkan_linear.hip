@@ -162,14 +162,14 @@ struct LinearArgs {
 };
 
 template <class T>
-__device__ __forceinline__ void finish_tile(const LinearArgs &a, int64_t tile, const intx4 (&acc)[T::CT][T::RT], char *scratch, int wave)
+__device__ __forceinline__ void finish_tile(const LinearArgs &a, int tile, const intx4 (&acc)[T::CT][T::RT], char *scratch, int wave)
 {
     int lane = threadIdx.x & 63;
     asm volatile("" : "+v"(lane));   // (the addresses below are worked out here, not kept in registers through the main loop)
     const int r = lane & 15, q = lane >> 4;
-    const int64_t ti = tile / a.tiles_across;
-    const int64_t i0 = ti * T::ROWS;
-    const int j0 = (int)(tile - ti * a.tiles_across) * T::COLS;
+    const int ti = tile / a.tiles_across;
+    const int64_t i0 = (int64_t)ti * T::ROWS;
+    const int j0 = (tile - ti * a.tiles_across) * T::COLS;
     for_wave_tiles<T>(acc, wave, [&](int row, int col, const intx4 (&v)[4]) {
         if (i0 + row >= a.batch || j0 + col >= a.n_out) return;
 #pragma unroll
@@ -226,9 +226,10 @@ template <class T>
 __global__ __launch_bounds__(T::THREADS) void linear_kernel(LinearArgs a)
 {
     extern __shared__ __align__(16) char lds[];
-    for_work(a.work, blockIdx.x, [&](int64_t tile, int from, int to, int slot) {
-        const int64_t ti = tile / a.tiles_across, i0 = ti * T::ROWS;
-        const int j0 = (int)(tile - ti * a.tiles_across) * T::COLS;
+    for_work(a.work, blockIdx.x, [&](int tile, int from, int to, int slot) {
+        const int ti = tile / a.tiles_across;
+        const int64_t i0 = (int64_t)ti * T::ROWS;
+        const int j0 = (tile - ti * a.tiles_across) * T::COLS;
         const int64_t last = a.batch - 1 - i0;
         const Operand x{reinterpret_cast<const char *>(uniform(a.x + i0 * a.x_pitch)), kLine, uniform((int)(last < T::ROWS ? last : T::ROWS)), false,
                         (unsigned)a.x_pitch, (int)a.x_pitch - 16};
@@ -425,17 +426,11 @@ constexpr int kUnits = 256;   // compute units
 template <class T>
 WorkSplit split_work(const LinearShape &s)
 {
-    WorkSplit w;
-    w.tiles = ((s.batch + T::ROWS - 1) / T::ROWS) * ((s.n_out + T::COLS - 1) / T::COLS);
-    w.stages = padded_row(s.n_in) / kLine;
-    w.workers = kUnits * (160 * 1024 / T::LDS);
-    w.whole = w.tiles / w.workers * w.workers;
+    const int tiles = (int)(((s.batch + T::ROWS - 1) / T::ROWS) * ((s.n_out + T::COLS - 1) / T::COLS));
+    const int stages = padded_row(s.n_in) / kLine, workers = kUnits * (160 * 1024 / T::LDS);
     // Tiles are cut only where most compute units would be idle and the summed axis is long: joining the parts takes
-    // 5 us, a stage 0.35 (48 rows of 1024 -> 1024: 17 us cut, 13 whole).
-    const int64_t cut = w.whole == 0 && w.left() * 2 <= kUnits && w.stages >= 24 ? w.left() * w.stages / 8 : 0;
-    w.cutters = (int)(cut < w.left() ? w.left() : cut < kUnits ? cut : kUnits);
-    if (w.whole == 0) w.workers = (w.cutters + 7) / 8 * 8;
-    return w;
+    // 5 us, a stage 0.35 (48 rows of 1024 -> 1024: 17 us cut, 11 whole).
+    return WorkSplit::of(tiles, stages, workers, tiles * 2 <= kUnits && stages >= 24 ? 8 : 0);
 }
 
 // The larger tile reads half as much per product, and needs two tiles a compute unit to keep them busy.  Measured
@@ -459,7 +454,7 @@ Layout layout_of(const LinearShape &s)
     l.codes = take((size_t)s.batch * padded_row(s.n_in));
     l.scale = take((size_t)s.batch * sizeof(float));
     l.w = take((size_t)s.n_out * padded_row(s.n_in));   // (whether it is needed depends on a pointer)
-    l.parts = take(w.cutters > w.left() ? 2 * w.cutters * tile : 0);
+    l.parts = take(w.cut() ? 2 * w.cutters * tile : 0);
     l.total = at;
     return l;
 }
@@ -470,7 +465,7 @@ void launch_tiles(LinearArgs &a, hipStream_t stream)
     a.tiles_across = (a.n_out + T::COLS - 1) / T::COLS;
     if (T::LDS > 65536) allow_large_lds(reinterpret_cast<const void *>(linear_kernel<T>), T::LDS);
     linear_kernel<T><<<a.work.workers, T::THREADS, T::LDS, stream>>>(a);
-    if (a.work.cutters > a.work.left()) linear_join_kernel<T><<<(unsigned)a.work.left() * T::WAVES, 64, 0, stream>>>(a);
+    if (a.work.cut()) linear_join_kernel<T><<<(unsigned)a.work.left() * T::WAVES, 64, 0, stream>>>(a);
 }
 
 template <int DTYPE, int ROWS>

@@ -28,6 +28,7 @@ namespace lmkan {
 namespace {
 
 constexpr int kStepsAtOnce = 3;   // steps on one Gram matrix
+constexpr int kAtOnce = 8;        // elements that a thread loads before it uses them
 constexpr int kNormParts = 1024;  // workgroups that sum the norm of one matrix, at most
 
 // A batch of matrices of pairs (lmkan_tile.h); element values are held times `scale`
@@ -35,16 +36,8 @@ struct PairMatrix {
     char *base;
     int64_t stride;  // bytes from one matrix to the next
     int rows, depth;
-    float scale;
+    float scale, inverse;   // a power of two, and one over it
 };
-
-// the direction's element i
-__device__ __forceinline__ float direction(const UpdateArgs &u, int dtype, int64_t i)
-{
-    if (!u.momentum) return load_as_float(u.grad, i, dtype);
-    const float m = u.momentum[i];
-    return u.nesterov ? u.beta * m + (1.0f - u.beta) * load_as_float(u.grad, i, dtype) : m;
-}
 
 // Sum over the 256 threads in a fixed order, for all of them
 __device__ __forceinline__ double sum_of_threads(double v, double *shared)
@@ -66,10 +59,17 @@ __global__ __launch_bounds__(256) void norm_kernel(MatrixShape s, UpdateArgs u, 
     const int64_t each = (per + gridDim.x - 1) / gridDim.x, begin = blockIdx.x * each;
     const int64_t end = begin + each < per ? begin + each : per;
     double sum = 0.0;
-    for (int64_t i = begin + threadIdx.x; i < end; i += 256) {
-        if (u.momentum) u.momentum[base + i] = u.beta * u.momentum[base + i] + (1.0f - u.beta) * load_as_float(u.grad, base + i, s.dtype);
-        const double v = direction(u, s.dtype, base + i);
-        sum += v * v;
+    for (int64_t i0 = begin + threadIdx.x; i0 < end; i0 += 256 * kAtOnce) {
+        Raw raw[kAtOnce];
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k)
+            if (i0 + 256 * k < end) raw[k] = fetch(u, s.dtype, base + i0 + 256 * k, true);
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k)
+            if (i0 + 256 * k < end) {
+                const double v = direction(u, raw[k], base + i0 + 256 * k, true);
+                sum += v * v;
+            }
     }
     sum = sum_of_threads(sum, sums);
     if (threadIdx.x == 0) part[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = sum;
@@ -106,11 +106,22 @@ __global__ __launch_bounds__(256) void split_kernel(SplitArgs a)
     const int across = (a.s.cols + 63) / 64;
     const int r0 = (int)(blockIdx.x / across) * 64, c0 = (int)(blockIdx.x % across) * 64;
     const float f = inverse_norm(a.s, a.part, a.parts, matrix, sums);
-    for (int e = threadIdx.x; e < 64 * 64; e += 256) {
-        const int r = e >> 6, c = e & 63;
-        const bool in = r0 + r < a.s.rows && c0 + c < a.s.cols;
-        // (the scale is a power of two; times the norm's inverse first: the product of both may exceed float32)
-        tile[r][c] = in ? direction(a.u, a.s.dtype, (a.first + matrix) * per + (int64_t)(r0 + r) * a.s.cols + c0 + c) * f * a.by_rows.scale : 0.0f;
+    const int c = threadIdx.x & 63;
+    const int64_t from = (a.first + matrix) * per + (int64_t)r0 * a.s.cols + c0 + c;
+    for (int b = threadIdx.x >> 6; b < 64; b += 4 * kAtOnce) {
+        Raw raw[kAtOnce];
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+            const int r = b + 4 * k;
+            if (r0 + r < a.s.rows && c0 + c < a.s.cols) raw[k] = fetch(a.u, a.s.dtype, from + (int64_t)r * a.s.cols, false);
+        }
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+            const int r = b + 4 * k;
+            const bool in = r0 + r < a.s.rows && c0 + c < a.s.cols;
+            // (the scale is a power of two; times the norm's inverse first: the product of both may exceed float32)
+            tile[r][c] = in ? direction(a.u, raw[k], 0, false) * f * a.by_rows.scale : 0.0f;
+        }
     }
     __syncthreads();
     // a chunk of eight values at a time: 64 lines, two panels, four chunks
@@ -192,9 +203,9 @@ struct Product {
 struct ProductArgs {
     Product p[2];
     int problems;
-    int64_t matrices;
+    int matrices;
     int tiles_across;
-    int64_t tiles;             // of one matrix and problem
+    int tiles;                 // of one matrix and problem
     WorkSplit work;
     floatx4 *parts;
     // kResult
@@ -207,7 +218,7 @@ struct ProductArgs {
 // Tile t of the upper triangle of n x n tiles, column by column: (0,0) (0,1) (1,1) (0,2) ...
 __device__ __forceinline__ void upper_tile(int t, int *i, int *j)
 {
-    int c = (int)((sqrtf(8.0f * t + 1.0f) - 1.0f) * 0.5f);
+    int c = (int)((__builtin_amdgcn_sqrtf(8.0f * t + 1.0f) - 1.0f) * 0.5f);   // (about)
     while ((c + 1) * (c + 2) / 2 <= t) ++c;
     while (c * (c + 1) / 2 > t) --c;
     *j = c;
@@ -218,14 +229,14 @@ __device__ __forceinline__ void upper_tile(int t, int *i, int *j)
 struct Place {
     int matrix, problem, ti, tj;
 };
-__device__ __forceinline__ Place place_of(const ProductArgs &a, int64_t t)
+__device__ __forceinline__ Place place_of(const ProductArgs &a, int t)
 {
-    const int64_t which = t / a.tiles;
-    const int tile = (int)(t - which * a.tiles), matrix = (int)(which / a.problems);
+    const int which = t / a.tiles, tile = t - which * a.tiles;
+    const int matrix = a.problems == 1 ? which : which >> 1;
     int ti, tj;
     if (a.p[0].symmetric) upper_tile(tile, &ti, &tj);
     else ti = tile / a.tiles_across, tj = tile - ti * a.tiles_across;
-    return Place{uniform(matrix), uniform((int)which - matrix * a.problems), uniform(ti), uniform(tj)};
+    return Place{uniform(matrix), uniform(which - matrix * a.problems), uniform(ti), uniform(tj)};
 }
 
 // (two products at a time are kept ones)
@@ -243,7 +254,7 @@ __device__ __forceinline__ void finish_tile(const ProductArgs &a, const Place &w
     int lane = threadIdx.x & 63;
     asm volatile("" : "+v"(lane));   // (the addresses below are worked out here, not kept in registers through the main loop)
     const int r = lane & 15, q = lane >> 4;
-    const float unit = 1.0f / (p.rows.scale * p.cols.scale);
+    const float unit = p.rows.inverse * p.cols.inverse;
     const int n_rows = p.rows.rows, n_cols = p.cols.rows;
     for_wave_tiles<T>(acc, wave, [&](int row, int col, const floatx4 (&v)[4]) {
         row += w.ti * T::ROWS, col += w.tj * T::COLS;
@@ -295,7 +306,7 @@ __device__ __forceinline__ void finish_tile(const ProductArgs &a, const Place &w
                 const int chunk = 2 * (g & 1) + (q >> 1);
                 const half4 gh = *reinterpret_cast<const half4 *>(from + pair_at(p.gram.rows, i, col / kPanel, chunk) + (q & 1) * 8);
                 const half4 gl = *reinterpret_cast<const half4 *>(from + pair_at(p.gram.rows, i, col / kPanel, 4 + chunk) + (q & 1) * 8);
-                const float s = 1.0f / p.gram.scale;
+                const float s = p.gram.inverse;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) f[e] = p.c * f[e] + p.b * (((float)gh[e] + (float)gl[e]) * s) + (i == j + e ? p.a : 0.0f);
             }
@@ -318,7 +329,7 @@ template <class T, int FINISH>
 __global__ __launch_bounds__(T::THREADS) void product_kernel(ProductArgs a)
 {
     extern __shared__ __align__(16) char lds[];
-    for_work(a.work, blockIdx.x, [&](int64_t tile, int from, int to, int slot) {
+    for_work(a.work, blockIdx.x, [&](int tile, int from, int to, int slot) {
         const Place w = place_of(a, tile);
         const Product &p = product_of<FINISH>(a, w);
         const auto operand = [&](const PairMatrix &m, int first_row) {
@@ -352,7 +363,7 @@ __global__ __launch_bounds__(256) void unscaled_kernel(MatrixShape s, UpdateArgs
     const int64_t per = s.elems(), base = (first + blockIdx.y) * per;
     const float f = inverse_norm(s, part, parts, blockIdx.y, sums);
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < per; i += (int64_t)gridDim.x * 256) {
-        const float v = direction(u, s.dtype, base + i) * f;
+        const float v = direction(u, fetch(u, s.dtype, base + i, false), base + i, false) * f;
         if (u.weight) u.weight[base + i] = u.keep * u.weight[base + i] + u.add * v;
         else store_from_float(u.out, base + i, s.dtype, v);
     }
@@ -376,19 +387,15 @@ void launch_product_with(ProductArgs &a, hipStream_t stream)
 {
     const Product &p = a.p[0];
     a.tiles_across = (p.cols.rows + T::COLS - 1) / T::COLS;
-    a.tiles = tiles_of(p, T::ROWS);
-    WorkSplit &w = a.work;
-    w.tiles = a.tiles * a.matrices * a.problems;
-    w.stages = panels(p.rows.depth);
-    w.workers = kUnits * (T::LDS <= 80 * 1024 ? 2 : 1);
-    w.whole = w.tiles / w.workers * w.workers;
+    a.tiles = (int)tiles_of(p, T::ROWS);
+    const int64_t tiles = (int64_t)a.tiles * a.matrices * a.problems;
+    const int workers = kUnits * (T::LDS <= 80 * 1024 ? 2 : 1);
     // a part shorter than four stages costs more to join than it saves
-    const int64_t cut = w.left() * w.stages / 4;
-    w.cutters = (int)(cut < w.left() ? w.left() : cut < w.workers ? cut : w.workers);
-    if (w.whole == 0) w.workers = (w.cutters + 7) / 8 * 8;
+    a.work = WorkSplit::of((int)tiles, panels(p.rows.depth), workers, 4);
+    const WorkSplit &w = a.work;
     if (T::LDS > 65536) allow_large_lds(reinterpret_cast<const void *>(product_kernel<T, FINISH>), T::LDS);
     product_kernel<T, FINISH><<<w.workers, T::THREADS, T::LDS, stream>>>(a);
-    if (w.cutters > w.left()) join_kernel<T, FINISH><<<(unsigned)w.left() * T::WAVES, 64, 0, stream>>>(a);
+    if (w.cut()) join_kernel<T, FINISH><<<(unsigned)w.left() * T::WAVES, 64, 0, stream>>>(a);
 }
 
 // The larger the tile, the less is read per product and the more of a tile that straddles the diagonal or the end is
@@ -499,7 +506,8 @@ void launch_ortho(const MatrixShape &s, int steps, const float *schedule, const 
         const Layout l = layout_of(s, count);
         char *ws = static_cast<char *>(workspace);
         const auto pairs = [&](size_t at, int rows, int depth, double bound) {
-            return PairMatrix{ws + at, pair_bytes(rows, depth), rows, depth, scale_for(bound)};
+            const float scale = scale_for(bound);
+            return PairMatrix{ws + at, pair_bytes(rows, depth), rows, depth, scale, 1.0f / scale};
         };
         double *part = reinterpret_cast<double *>(ws + l.norm);
         const int64_t some = (s.elems() + 4095) / 4096;
@@ -515,7 +523,7 @@ void launch_ortho(const MatrixShape &s, int steps, const float *schedule, const 
         const unsigned tiles = (unsigned)(((s.rows + 63) / 64) * (int64_t)((s.cols + 63) / 64));
         split_kernel<<<dim3(tiles, 1, (unsigned)count), 256, 0, stream>>>(SplitArgs{s, u, first, part, parts, s.flip() ? xt : x, s.flip() ? x : xt});
         ProductArgs args = {};
-        args.matrices = count;
+        args.matrices = (int)count;
         args.s = s;
         args.u = u;
         args.first = first;

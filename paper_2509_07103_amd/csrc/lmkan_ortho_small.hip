@@ -55,25 +55,6 @@ __device__ __forceinline__ int64_t stored_at(const MatrixShape &s, int64_t matri
     return matrix * s.elems() + (s.flip() ? (int64_t)column * s.cols + row : (int64_t)row * s.cols + column);
 }
 
-// The direction's element `at` in two halves, so that many loads can be under way: what it is made of, and the element.
-// `move`: the momentum moves.
-struct Raw {
-    float g, m;
-};
-__device__ __forceinline__ Raw fetch(const UpdateArgs &u, int dtype, int64_t at, bool move)
-{
-    Raw r;
-    r.g = !u.momentum || u.nesterov || move ? load_as_float(u.grad, at, dtype) : 0.0f;
-    r.m = u.momentum ? u.momentum[at] : 0.0f;
-    return r;
-}
-__device__ __forceinline__ float direction(const UpdateArgs &u, Raw r, int64_t at, bool move)
-{
-    if (!u.momentum) return r.g;
-    if (move) u.momentum[at] = r.m = u.beta * r.m + (1.0f - u.beta) * r.g;
-    return u.nesterov ? u.beta * r.m + (1.0f - u.beta) * r.g : r.m;
-}
-
 __device__ __forceinline__ void store_result(const SmallArgs &a, int64_t at, float v)
 {
     if (a.u.weight) a.u.weight[at] = a.u.keep * a.u.weight[at] + a.u.add * v;
@@ -517,15 +498,16 @@ int64_t matrices_at_once(const MatrixShape &s)
     return (s.batch + parts - 1) / parts;
 }
 
-template <class S>
+// W: the shape of workgroups that have a matrix to themselves, S: of those that share one
+template <class W, class S>
 void launch(const MatrixShape &s, const UpdateArgs &update, SmallArgs a, char *ws, hipStream_t stream)
 {
     if (whole(s)) {
         a.columns = round16(s.n());
         a.by_columns = Divide::by(a.columns), a.by_m = Divide::by(s.m()), a.by_n = Divide::by(s.n());
         const size_t lds = whole_lds(s);
-        if (lds > 65536) allow_large_lds(reinterpret_cast<const void *>(whole_kernel<S>), kSmallLds);
-        whole_kernel<S><<<(unsigned)s.batch, S::THREADS, lds, stream>>>(a);
+        if (lds > 65536) allow_large_lds(reinterpret_cast<const void *>(whole_kernel<W>), kSmallLds);
+        whole_kernel<W><<<(unsigned)s.batch, W::THREADS, lds, stream>>>(a);
         return;
     }
     const int64_t most = matrices_at_once(s);
@@ -548,7 +530,7 @@ void launch(const MatrixShape &s, const UpdateArgs &update, SmallArgs a, char *w
         gram_kernel<S><<<grid, S::THREADS, block + scratch, stream>>>(a);
         for (; a.from < a.steps; a.from = a.to) {
             a.to = a.from + kStepsAtOnce < a.steps ? a.from + kStepsAtOnce : a.steps;
-            polynomial_kernel<S><<<(unsigned)count, S::THREADS, 3 * square, stream>>>(a);
+            polynomial_kernel<W><<<(unsigned)count, W::THREADS, 3 * square, stream>>>(a);
             if (a.to == a.steps) apply_kernel<S, true><<<grid, S::THREADS, square + block, stream>>>(a);
             else apply_kernel<S, false><<<grid, S::THREADS, square + block + scratch, stream>>>(a);
         }
@@ -574,12 +556,13 @@ void launch_ortho_small(const MatrixShape &s, int steps, const float *schedule, 
     a.steps = steps;
     for (int k = 0; k < 3 * steps; ++k) a.schedule[k] = schedule[k];
     char *ws = static_cast<char *>(workspace);
-    // a wave a matrix where there is one tile and little to load
-    if (s.m() <= 16 && s.n() <= 256) launch<Small<16, 1>>(s, u, a, ws, stream);
-    else if (s.m() <= 16) launch<Small<16, 4>>(s, u, a, ws, stream);
-    else if (s.m() <= 32) launch<Small<32, 4>>(s, u, a, ws, stream);
-    else if (s.m() <= 48) launch<Small<48, 4>>(s, u, a, ws, stream);
-    else launch<Small<64, 4>>(s, u, a, ws, stream);
+    // A wave a matrix where there is one tile and little to load; as many waves as a symmetric product has tiles where
+    // a matrix has a compute unit to itself.
+    if (s.m() <= 16 && s.n() <= 256) launch<Small<16, 1>, Small<16, 4>>(s, u, a, ws, stream);
+    else if (s.m() <= 16) launch<Small<16, 4>, Small<16, 4>>(s, u, a, ws, stream);
+    else if (s.m() <= 32) launch<Small<32, 4>, Small<32, 4>>(s, u, a, ws, stream);
+    else if (s.m() <= 48) launch<Small<48, 8>, Small<48, 4>>(s, u, a, ws, stream);
+    else launch<Small<64, 12>, Small<64, 4>>(s, u, a, ws, stream);
 }
 
 }  // namespace lmkan

@@ -267,16 +267,35 @@ __device__ __forceinline__ void multiply(const Operand &rows, const Operand &col
 // tiles left over for less than a round are cut along the summed axis so that all workgroups get the same number
 // of stages.  What a workgroup has of a tile that it does not own whole goes to one of its two slots of a buffer,
 // where a second kernel joins the parts in order.
+// (Tiles are counted in 32 bits: a tile that is not at the end of a row of tiles stands for at least 64 x 64 results.)
 struct WorkSplit {
-    int64_t whole;    // tiles [0, whole) are taken whole, a multiple of `workers`
-    int64_t tiles;
+    int whole;     // tiles [0, whole) are taken whole, a multiple of `workers`
+    int tiles;
     int stages;
-    int workers;      // workgroups; a multiple of 8 when there are several rounds
-    int cutters;      // workgroups that share the tiles left over
-    __host__ __device__ int64_t left() const { return tiles - whole; }
-    // stages of the tiles left over, counted through, that workgroup w takes: [begin(w), begin(w + 1))
-    __host__ __device__ int64_t begin(int w) const { return left() * stages * w / cutters; }
-    __host__ __device__ int owner(int64_t stage) const { return (int)(((stage + 1) * cutters - 1) / (left() * stages)); }
+    int workers;   // workgroups, a multiple of 8
+    int cutters;   // workgroups that share the tiles left over
+    int each, more;   // their stages, counted through: `each` a workgroup, one more for the first `more`
+    __host__ __device__ int left() const { return tiles - whole; }
+    __host__ __device__ bool cut() const { return cutters > left(); }
+    __host__ __device__ int begin(int w) const { return w * each + (w < more ? w : more); }
+    __host__ __device__ int owner(int stage) const
+    {
+        const int first = more * (each + 1);
+        return stage < first ? stage / (each + 1) : more + (stage - first) / each;
+    }
+    // `shortest`: stages of a part, at least; 0: tiles are not cut
+    static WorkSplit of(int tiles, int stages, int workers, int shortest)
+    {
+        WorkSplit w;
+        w.tiles = tiles, w.stages = stages;
+        w.whole = tiles / workers * workers;
+        const int left = w.left();
+        const int64_t total = (int64_t)left * stages, pieces = shortest ? total / shortest : 0;
+        w.cutters = (int)(pieces < left ? left : pieces < workers ? pieces : workers);
+        w.each = left ? (int)(total / w.cutters) : 0, w.more = left ? (int)(total % w.cutters) : 0;
+        w.workers = w.whole ? workers : (w.cutters + 7) / 8 * 8;
+        return w;
+    }
 };
 
 // Calls f(tile, from, to, slot) for everything workgroup `id` takes; slot < 0: the whole tile.  Ids that run on the
@@ -284,18 +303,15 @@ struct WorkSplit {
 template <class F>
 __device__ __forceinline__ void for_work(const WorkSplit &w, int id, F &&f)
 {
-    const int each = w.workers / 8;
-    const int place = w.workers % 8 == 0 ? (id & 7) * each + (id >> 3) : id;
-    for (int64_t t = place; t < w.whole; t += w.workers) f(t, 0, w.stages, -1);
+    const int place = (id & 7) * (w.workers / 8) + (id >> 3);
+    for (int t = place; t < w.whole; t += w.workers) f(t, 0, w.stages, -1);
     if (place >= w.cutters) return;
-    int64_t s = w.begin(place);
-    const int64_t end = w.begin(place + 1);
+    int s = w.begin(place), tile = s / w.stages, from = s - tile * w.stages;
+    const int end = w.begin(place + 1);
     while (s < end) {
-        const int64_t tile = s / w.stages;
-        const int from = (int)(s - tile * w.stages);
-        const int to = end - tile * w.stages < w.stages ? (int)(end - tile * w.stages) : w.stages;
+        const int left = end - s, to = left < w.stages - from ? from + left : w.stages;
         f(w.whole + tile, uniform(from), uniform(to), from == 0 && to == w.stages ? -1 : 2 * place + (from == 0));
-        s += to - from;
+        s += to - from, ++tile, from = 0;
     }
 }
 
@@ -312,9 +328,9 @@ __device__ __forceinline__ void store_part(Acc *parts, int slot, const Acc (&acc
 // A wave's share of the parts of tile `tile` (counted from the first that is cut), summed in order; false when the
 // tile was taken whole
 template <class T, class Acc>
-__device__ __forceinline__ bool join_parts(const WorkSplit &w, int64_t tile, int wave, const Acc *parts, Acc (&acc)[T::CT][T::RT])
+__device__ __forceinline__ bool join_parts(const WorkSplit &w, int tile, int wave, const Acc *parts, Acc (&acc)[T::CT][T::RT])
 {
-    const int64_t first = tile * w.stages;
+    const int first = tile * w.stages;
     const int from = w.owner(first), to = w.owner(first + w.stages - 1);
     if (from == to) return false;
 #pragma unroll
