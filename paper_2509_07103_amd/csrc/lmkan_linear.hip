@@ -170,53 +170,82 @@ __device__ __forceinline__ void finish_tile(const LinearArgs &a, int tile, const
     const int ti = tile / a.tiles_across;
     const int64_t i0 = (int64_t)ti * T::ROWS;
     const int j0 = (tile - ti * a.tiles_across) * T::COLS;
-    for_wave_tiles<T>(acc, wave, [&](int row, int col, const intx4 (&v)[4]) {
+    // what a lane finishes of a 32 x 32 tile, after the tile went through LDS: rows 8 t + lane / 8, four columns
+    const int fr = lane >> 3, fc = (lane & 7) * 4;
+    struct Held {
+        floatx4 y[4];   // of 16-bit elements: two words
+        float scale[4];
+    };
+    // (rows and columns beyond the end: others are loaded, and not used)
+    const auto ahead = [&](int row, int col) {
+        Held h;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            int64_t i = i0 + row + 8 * t + fr;
+            i = i < a.batch ? i : a.batch - 1;
+            h.scale[t] = a.x_scale[i];
+            if (a.by_four && a.beta != 0.0f) {
+                const int64_t at = i * a.n_out + min(j0 + col + fc, a.n_out - 4);
+                if (a.y_dtype == LMKAN_F32) {
+                    h.y[t] = *reinterpret_cast<const floatx4 *>(static_cast<const float *>(a.y) + at);
+                } else {
+                    const uint2 u = *reinterpret_cast<const uint2 *>(static_cast<const uint16_t *>(a.y) + at);
+                    h.y[t][0] = __builtin_bit_cast(float, u.x), h.y[t][1] = __builtin_bit_cast(float, u.y);
+                }
+            }
+        }
+        return h;
+    };
+    for_wave_tiles<T>(acc, wave, ahead, [&](int row, int col, const intx4 (&v)[4], const Held &held) {
         if (i0 + row >= a.batch || j0 + col >= a.n_out) return;
 #pragma unroll
         for (int g = 0; g < 4; ++g) *reinterpret_cast<intx4 *>(scratch + ((16 * (g >> 1) + r) * kPitch + 16 * (g & 1) + 4 * q) * 4) = v[g];
-        const int j = j0 + col + (lane & 7) * 4;
-        float ws[4], b[4];
+        if (a.by_four) {
+            const int j = j0 + col + fc, seen = min(j, a.n_out - 4);
+            const floatx4 zero = {0, 0, 0, 0};
+            floatx4 ws, b;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const bool in = j + e < a.n_out;
-            ws[e] = in ? a.w_scale[j + e] : 0.0f;
-            b[e] = in && a.bias ? a.bias[j + e] : 0.0f;
-        }
+            for (int e = 0; e < 4; ++e) ws[e] = a.w_scale[seen + e];
+            b = zero;
+            if (a.bias)
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const int64_t i = i0 + row + 8 * t + (lane >> 3);
-            const intx4 sum = *reinterpret_cast<const intx4 *>(scratch + ((8 * t + (lane >> 3)) * kPitch + (lane & 7) * 4) * 4);
-            if (i >= a.batch || j >= a.n_out) continue;
-            const float xs = a.x_scale[i];
-            const int64_t at = i * a.n_out + j;
-            float o[4];
+                for (int e = 0; e < 4; ++e) b[e] = a.bias[seen + e];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] = (float)sum[e] * (xs * ws[e]) + b[e];
-            if (a.by_four) {
+            for (int t = 0; t < 4; ++t) {
+                const int64_t i = i0 + row + 8 * t + fr;
+                const intx4 sum = *reinterpret_cast<const intx4 *>(scratch + ((8 * t + fr) * kPitch + fc) * 4);
+                if (i >= a.batch || j >= a.n_out) continue;
+                const int64_t at = i * a.n_out + j;
+                floatx4 o;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] = (float)sum[e] * (held.scale[t] * ws[e]) + b[e];
                 if (a.y_dtype == LMKAN_F32) {
-                    float4 *to = reinterpret_cast<float4 *>(static_cast<float *>(a.y) + at);
-                    if (a.beta != 0.0f) {
-                        const float4 k = *to;
-                        o[0] += a.beta * k.x, o[1] += a.beta * k.y, o[2] += a.beta * k.z, o[3] += a.beta * k.w;
-                    }
-                    *to = make_float4(o[0], o[1], o[2], o[3]);
+                    if (a.beta != 0.0f) o += a.beta * held.y[t];
+                    *reinterpret_cast<floatx4 *>(static_cast<float *>(a.y) + at) = o;
                 } else {
-                    uint2 *to = reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.y) + at);
                     if (a.beta != 0.0f) {
-                        const uint2 k = *to;
-                        const uint16_t h[4] = {(uint16_t)k.x, (uint16_t)(k.x >> 16), (uint16_t)k.y, (uint16_t)(k.y >> 16)};
+                        const uint32_t u[2] = {__builtin_bit_cast(uint32_t, (float)held.y[t][0]), __builtin_bit_cast(uint32_t, (float)held.y[t][1])};
+                        const uint16_t h[4] = {(uint16_t)u[0], (uint16_t)(u[0] >> 16), (uint16_t)u[1], (uint16_t)(u[1] >> 16)};
 #pragma unroll
                         for (int e = 0; e < 4; ++e) o[e] += a.beta * load_as_float(h, e, a.y_dtype);
                     }
-                    *to = make_uint2(two_from_float(a.y_dtype, o[0], o[1]), two_from_float(a.y_dtype, o[2], o[3]));
+                    *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.y) + at) =
+                        make_uint2(two_from_float(a.y_dtype, o[0], o[1]), two_from_float(a.y_dtype, o[2], o[3]));
                 }
-            } else {
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (j + e < a.n_out) {
-                        if (a.beta != 0.0f) o[e] += a.beta * load_as_float(a.y, at + e, a.y_dtype);
-                        store_from_float(a.y, at + e, a.y_dtype, o[e]);
-                    }
+            }
+        } else {
+            // element by element, 32 adjacent ones of two rows at a time
+            const int j = j0 + col + (lane & 31);
+            if (j >= a.n_out) return;
+            const float ws = a.w_scale[j], b = a.bias ? a.bias[j] : 0.0f;
+#pragma unroll 2
+            for (int k = lane >> 5; k < 32; k += 2) {
+                const int64_t i = i0 + row + k;
+                if (i >= a.batch) break;
+                const int sum = *reinterpret_cast<const int *>(scratch + (k * kPitch + (lane & 31)) * 4);
+                float o = (float)sum * (a.x_scale[i] * ws) + b;
+                if (a.beta != 0.0f) o += a.beta * load_as_float(a.y, i * a.n_out + j, a.y_dtype);
+                store_from_float(a.y, i * a.n_out + j, a.y_dtype, o);
             }
         }
     });
@@ -247,12 +276,12 @@ __global__ __launch_bounds__(T::THREADS) void linear_kernel(LinearArgs a)
 
 // A wave's share of a tile that was cut, a workgroup each
 template <class T>
-__global__ __launch_bounds__(64) void linear_join_kernel(LinearArgs a)
+__global__ __launch_bounds__(64 * joiners<T>()) void linear_join_kernel(LinearArgs a)
 {
-    __shared__ __align__(16) char lds[kWaveScratch];
+    __shared__ __align__(16) char lds[kWaveScratch + join_lds<T>()];
     const int tile = blockIdx.x / T::WAVES, wave = blockIdx.x % T::WAVES;
     intx4 acc[T::CT][T::RT];
-    if (!join_parts<T>(a.work, tile, wave, a.parts, acc)) return;
+    if (!join_parts<T, joiners<T>()>(a.work, tile, wave, a.parts, reinterpret_cast<intx4 *>(lds + kWaveScratch), acc)) return;
     finish_tile<T>(a, a.work.whole + tile, acc, lds, wave);
 }
 
@@ -428,9 +457,8 @@ WorkSplit split_work(const LinearShape &s)
 {
     const int tiles = (int)(((s.batch + T::ROWS - 1) / T::ROWS) * ((s.n_out + T::COLS - 1) / T::COLS));
     const int stages = padded_row(s.n_in) / kLine, workers = kUnits * (160 * 1024 / T::LDS);
-    // Tiles are cut only where most compute units would be idle and the summed axis is long: joining the parts takes
-    // 5 us, a stage 0.35 (48 rows of 1024 -> 1024: 17 us cut, 11 whole).
-    return WorkSplit::of(tiles, stages, workers, tiles * 2 <= kUnits && stages >= 24 ? 8 : 0);
+    // (joining takes 5 us, a stage of the smaller tile 0.3: 48 rows of 1024 -> 1024, eight stages, 17 us cut, 11 whole)
+    return WorkSplit::of(tiles, stages, workers, T::ROWS == 64 ? 16 : 12);
 }
 
 // The larger tile reads half as much per product, and needs two tiles a compute unit to keep them busy.  Measured
@@ -465,7 +493,7 @@ void launch_tiles(LinearArgs &a, hipStream_t stream)
     a.tiles_across = (a.n_out + T::COLS - 1) / T::COLS;
     if (T::LDS > 65536) allow_large_lds(reinterpret_cast<const void *>(linear_kernel<T>), T::LDS);
     linear_kernel<T><<<a.work.workers, T::THREADS, T::LDS, stream>>>(a);
-    if (a.work.cut()) linear_join_kernel<T><<<(unsigned)a.work.left() * T::WAVES, 64, 0, stream>>>(a);
+    if (a.work.cut()) linear_join_kernel<T><<<a.work.left() * T::WAVES, 64 * joiners<T>(), 0, stream>>>(a);
 }
 
 template <int DTYPE, int ROWS>

@@ -256,38 +256,64 @@ __device__ __forceinline__ void finish_tile(const ProductArgs &a, const Place &w
     const int r = lane & 15, q = lane >> 4;
     const float unit = p.rows.inverse * p.cols.inverse;
     const int n_rows = p.rows.rows, n_cols = p.cols.rows;
-    for_wave_tiles<T>(acc, wave, [&](int row, int col, const floatx4 (&v)[4]) {
+    // what a lane finishes of a 32 x 32 tile of the result, after the tile went through LDS: rows 8 t + lane / 8, four columns
+    const int fr = lane >> 3, fc = (lane & 7) * 4;
+    const int64_t start = FINISH == kResult ? (a.first + w.matrix) * a.s.elems() : 0;
+    const char *gram = FINISH == kPoly ? p.gram.base + w.matrix * p.gram.stride : nullptr;
+    struct Held {
+        floatx4 w[4];        // kResult: weights
+        half4 hi[4], lo[4];  // kPoly: elements of A
+    };
+    // (rows and columns beyond the end: others are loaded, and not used)
+    const auto ahead = [&](int row, int col) {
+        Held h;
+        row += w.ti * T::ROWS, col += w.tj * T::COLS;
+        if (FINISH == kResult && a.u.weight && a.by_four) {
+            const int j = min(col + fc, n_cols - 4);
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+                h.w[t] = *reinterpret_cast<const floatx4 *>(a.u.weight + start + (int64_t)min(row + 8 * t + fr, n_rows - 1) * a.s.cols + j);
+        }
+        if (FINISH == kPoly) {
+            const int panel = min(col, n_cols - 1) / kPanel;
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int i = min(row + 16 * (g >> 1) + r, n_rows - 1), chunk = 2 * (g & 1) + (q >> 1);
+                h.hi[g] = *reinterpret_cast<const half4 *>(gram + pair_at(p.gram.rows, i, panel, chunk) + (q & 1) * 8);
+                h.lo[g] = *reinterpret_cast<const half4 *>(gram + pair_at(p.gram.rows, i, panel, 4 + chunk) + (q & 1) * 8);
+            }
+        }
+        return h;
+    };
+    for_wave_tiles<T>(acc, wave, ahead, [&](int row, int col, const floatx4 (&v)[4], const Held &held) {
         row += w.ti * T::ROWS, col += w.tj * T::COLS;
         if (FINISH == kResult) {
             if (row >= n_rows || col >= n_cols) return;
 #pragma unroll
             for (int g = 0; g < 4; ++g)
                 *reinterpret_cast<floatx4 *>(scratch + ((16 * (g >> 1) + r) * kPitch + 16 * (g & 1) + 4 * q) * 4) = v[g] * unit;
+            if (a.by_four) {
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                const int i = 8 * t + (lane >> 3), j = (lane & 7) * 4;
-                const float4 o = *reinterpret_cast<const float4 *>(scratch + (i * kPitch + j) * 4);
-                if (row + i >= n_rows || col + j >= n_cols) continue;
-                const int64_t at = (a.first + w.matrix) * a.s.elems() + (int64_t)(row + i) * a.s.cols + col + j;
-                if (a.by_four) {
-                    if (a.u.weight) {
-                        float4 *to = reinterpret_cast<float4 *>(a.u.weight + at);
-                        const float4 k = *to;
-                        *to = make_float4(a.u.keep * k.x + a.u.add * o.x, a.u.keep * k.y + a.u.add * o.y, a.u.keep * k.z + a.u.add * o.z, a.u.keep * k.w + a.u.add * o.w);
-                    } else if (a.s.dtype == LMKAN_F32) {
-                        *reinterpret_cast<float4 *>(static_cast<float *>(a.u.out) + at) = o;
-                    } else {
+                for (int t = 0; t < 4; ++t) {
+                    const int i = row + 8 * t + fr, j = col + fc;
+                    const floatx4 o = *reinterpret_cast<const floatx4 *>(scratch + ((8 * t + fr) * kPitch + fc) * 4);
+                    if (i >= n_rows || j >= n_cols) continue;
+                    const int64_t at = start + (int64_t)i * a.s.cols + j;
+                    if (a.u.weight) *reinterpret_cast<floatx4 *>(a.u.weight + at) = a.u.keep * held.w[t] + a.u.add * o;
+                    else if (a.s.dtype == LMKAN_F32) *reinterpret_cast<floatx4 *>(static_cast<float *>(a.u.out) + at) = o;
+                    else
                         *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.u.out) + at) =
-                            make_uint2(two_from_float(a.s.dtype, o.x, o.y), two_from_float(a.s.dtype, o.z, o.w));
-                    }
-                } else {
-                    const float one[4] = {o.x, o.y, o.z, o.w};
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (col + j + e < n_cols) {
-                            if (a.u.weight) a.u.weight[at + e] = a.u.keep * a.u.weight[at + e] + a.u.add * one[e];
-                            else store_from_float(a.u.out, at + e, a.s.dtype, one[e]);
-                        }
+                            make_uint2(two_from_float(a.s.dtype, o[0], o[1]), two_from_float(a.s.dtype, o[2], o[3]));
+                }
+            } else {
+                const int j = lane & 31;
+#pragma unroll 1
+                for (int i = lane >> 5; i < 32; i += 2) {
+                    if (row + i >= n_rows || col + j >= n_cols) continue;
+                    const int64_t at = start + (int64_t)(row + i) * a.s.cols + col + j;
+                    const float o = *reinterpret_cast<const float *>(scratch + (i * kPitch + j) * 4);
+                    if (a.u.weight) a.u.weight[at] = a.u.keep * a.u.weight[at] + a.u.add * o;
+                    else store_from_float(a.u.out, at, a.s.dtype, o);
                 }
             }
             return;
@@ -295,29 +321,29 @@ __device__ __forceinline__ void finish_tile(const ProductArgs &a, const Place &w
         const bool direct = row < n_rows && col < panels(n_cols) * kPanel;
         const bool turned = p.mirror.base && !(p.symmetric && w.ti == w.tj) && col < n_cols && row < panels(n_rows) * kPanel;
         if (!direct && !turned) return;
+        const bool inside = row + 32 <= n_rows && col + 32 <= n_cols;
+        const float scale = FINISH == kPoly ? p.out.scale : p.out.scale * unit;
         uint2 hi[4], lo[4];
-        const float scale = p.out.scale;
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
             const int i = row + 16 * (g >> 1) + r, j = col + 16 * (g & 1) + 4 * q;
-            floatx4 f = v[g] * unit;
-            if (FINISH == kPoly && i < n_rows && j < n_cols) {
-                const char *from = p.gram.base + w.matrix * p.gram.stride;
-                const int chunk = 2 * (g & 1) + (q >> 1);
-                const half4 gh = *reinterpret_cast<const half4 *>(from + pair_at(p.gram.rows, i, col / kPanel, chunk) + (q & 1) * 8);
-                const half4 gl = *reinterpret_cast<const half4 *>(from + pair_at(p.gram.rows, i, col / kPanel, 4 + chunk) + (q & 1) * 8);
-                const float s = p.gram.inverse;
+            floatx4 f = v[g];
+            if (FINISH == kPoly) {
+                const half4 gh = held.hi[g], gl = held.lo[g];
+                const float s = p.b * p.gram.inverse, c = p.c * unit;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) f[e] = p.c * f[e] + p.b * (((float)gh[e] + (float)gl[e]) * s) + (i == j + e ? p.a : 0.0f);
+                for (int e = 0; e < 4; ++e) f[e] = c * f[e] + s * ((float)gh[e] + (float)gl[e]) + (i == j + e ? p.a : 0.0f);
             }
+            f *= scale;
+            if (!inside)
+                // what lies beyond the matrix in a panel is zero
+#pragma unroll
+                for (int e = 0; e < 4; ++e) f[e] = i < n_rows && j + e < n_cols ? f[e] : 0.0f;
             half4 vh, vl;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                // what lies beyond the matrix in a panel is zero
-                _Float16 x, y;
-                split(i < n_rows && j + e < n_cols ? f[e] * scale : 0.0f, &x, &y);
-                vh[e] = x, vl[e] = y;
-            }
+            for (int e = 0; e < 4; ++e) vh[e] = (_Float16)f[e];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) vl[e] = (_Float16)__builtin_fmaf((float)vh[e], -1.0f, f[e]);
             hi[g] = __builtin_bit_cast(uint2, vh), lo[g] = __builtin_bit_cast(uint2, vl);
         }
         if (direct) store_pairs(p.out, p.out.base + w.matrix * p.out.stride, row, col, hi, lo, scratch, lane);
@@ -347,12 +373,12 @@ __global__ __launch_bounds__(T::THREADS) void product_kernel(ProductArgs a)
 
 // A wave's share of a tile that was cut, a workgroup each
 template <class T, int FINISH>
-__global__ __launch_bounds__(64) void join_kernel(ProductArgs a)
+__global__ __launch_bounds__(64 * joiners<T>()) void join_kernel(ProductArgs a)
 {
-    __shared__ __align__(16) char lds[kWaveScratch];
+    __shared__ __align__(16) char lds[kWaveScratch + join_lds<T>()];
     const int tile = blockIdx.x / T::WAVES, wave = blockIdx.x % T::WAVES;
     floatx4 acc[T::CT][T::RT];
-    if (!join_parts<T>(a.work, tile, wave, a.parts, acc)) return;
+    if (!join_parts<T, joiners<T>()>(a.work, tile, wave, a.parts, reinterpret_cast<floatx4 *>(lds + kWaveScratch), acc)) return;
     finish_tile<T, FINISH>(a, place_of(a, a.work.whole + tile), acc, lds, wave);
 }
 
@@ -370,6 +396,7 @@ __global__ __launch_bounds__(256) void unscaled_kernel(MatrixShape s, UpdateArgs
 }
 
 typedef TileShape<64, 64, 2, 2, 4> Tile64;
+typedef TileShape<64, 64, 2, 2, 9> Tile64Deep;
 typedef TileShape<128, 128, 2, 2, 2> Tile128;
 typedef TileShape<256, 256, 4, 2, 2> Tile256;
 
@@ -390,12 +417,12 @@ void launch_product_with(ProductArgs &a, hipStream_t stream)
     a.tiles = (int)tiles_of(p, T::ROWS);
     const int64_t tiles = (int64_t)a.tiles * a.matrices * a.problems;
     const int workers = kUnits * (T::LDS <= 80 * 1024 ? 2 : 1);
-    // a part shorter than four stages costs more to join than it saves
-    a.work = WorkSplit::of((int)tiles, panels(p.rows.depth), workers, 4);
+    // (joining takes 6 us, a stage of the smallest tile 0.25; 20 us and 1.8 for the largest)
+    a.work = WorkSplit::of((int)tiles, panels(p.rows.depth), workers, T::ROWS == 64 ? 24 : T::ROWS == 128 ? 20 : 12);
     const WorkSplit &w = a.work;
     if (T::LDS > 65536) allow_large_lds(reinterpret_cast<const void *>(product_kernel<T, FINISH>), T::LDS);
     product_kernel<T, FINISH><<<w.workers, T::THREADS, T::LDS, stream>>>(a);
-    if (w.cut()) join_kernel<T, FINISH><<<(unsigned)w.left() * T::WAVES, 64, 0, stream>>>(a);
+    if (w.cut()) join_kernel<T, FINISH><<<w.left() * T::WAVES, 64 * joiners<T>(), 0, stream>>>(a);
 }
 
 // The larger the tile, the less is read per product and the more of a tile that straddles the diagonal or the end is
@@ -408,7 +435,8 @@ void launch_product(ProductArgs &a, hipStream_t stream)
     const int shorter = a.s.m();
     if (shorter > 512 && tiles_of(a.p[0], 256) * n >= kUnits / 2) launch_product_with<Tile256, FINISH>(a, stream);
     else if (shorter > 256 && tiles_of(a.p[0], 128) * n >= 2 * kUnits) launch_product_with<Tile128, FINISH>(a, stream);
-    else launch_product_with<Tile64, FINISH>(a, stream);
+    else if (tiles_of(a.p[0], 64) * n > kUnits) launch_product_with<Tile64, FINISH>(a, stream);
+    else launch_product_with<Tile64Deep, FINISH>(a, stream);
 }
 
 // Matrices that share the workspace at a time: the batch in equal parts of at most 256 M elements (parts of 32 M and

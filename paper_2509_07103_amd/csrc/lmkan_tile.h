@@ -283,15 +283,17 @@ struct WorkSplit {
         const int first = more * (each + 1);
         return stage < first ? stage / (each + 1) : more + (stage - first) / each;
     }
-    // `shortest`: stages of a part, at least; 0: tiles are not cut
-    static WorkSplit of(int tiles, int stages, int workers, int shortest)
+    // `join`: what writing and joining parts takes, in stages; tiles are cut where that is less than the stages that
+    // the fullest workgroup is spared.  Parts have four stages at least.
+    static WorkSplit of(int tiles, int stages, int workers, int join)
     {
         WorkSplit w;
         w.tiles = tiles, w.stages = stages;
         w.whole = tiles / workers * workers;
         const int left = w.left();
-        const int64_t total = (int64_t)left * stages, pieces = shortest ? total / shortest : 0;
-        w.cutters = (int)(pieces < left ? left : pieces < workers ? pieces : workers);
+        const int64_t total = (int64_t)left * stages, pieces = total / 4;
+        const bool cut = (int64_t)stages * (workers - left) > (int64_t)workers * join && pieces > left;
+        w.cutters = (int)(!cut ? left : pieces < workers ? pieces : workers);
         w.each = left ? (int)(total / w.cutters) : 0, w.more = left ? (int)(total % w.cutters) : 0;
         w.workers = w.whole ? workers : (w.cutters + 7) / 8 * 8;
         return w;
@@ -304,14 +306,23 @@ template <class F>
 __device__ __forceinline__ void for_work(const WorkSplit &w, int id, F &&f)
 {
     const int place = (id & 7) * (w.workers / 8) + (id >> 3);
-    for (int t = place; t < w.whole; t += w.workers) f(t, 0, w.stages, -1);
-    if (place >= w.cutters) return;
-    int s = w.begin(place), tile = s / w.stages, from = s - tile * w.stages;
-    const int end = w.begin(place + 1);
-    while (s < end) {
-        const int left = end - s, to = left < w.stages - from ? from + left : w.stages;
-        f(w.whole + tile, uniform(from), uniform(to), from == 0 && to == w.stages ? -1 : 2 * place + (from == 0));
-        s += to - from, ++tile, from = 0;
+    const bool cuts = place < w.cutters;
+    int t = place, s = cuts ? w.begin(place) : 0;
+    const int end = cuts ? w.begin(place + 1) : 0;
+    while (true) {   // (one call: the body is long)
+        int tile, from = 0, to = w.stages, slot = -1;
+        if (t < w.whole) {
+            tile = t, t += w.workers;
+        } else if (s < end) {
+            const int k = s / w.stages, left = end - s;
+            tile = w.whole + k, from = s - k * w.stages;
+            to = left < w.stages - from ? from + left : w.stages;
+            if (from > 0 || to < w.stages) slot = 2 * place + (from == 0);
+            s += to - from;
+        } else {
+            break;
+        }
+        f(tile, uniform(from), uniform(to), slot);
     }
 }
 
@@ -325,42 +336,80 @@ __device__ __forceinline__ void store_part(Acc *parts, int slot, const Acc (&acc
         for (int i = 0; i < T::RT; ++i) to[(j * T::RT + i) * T::THREADS] = acc[j][i];
 }
 
-// A wave's share of the parts of tile `tile` (counted from the first that is cut), summed in order; false when the
-// tile was taken whole
-template <class T, class Acc>
-__device__ __forceinline__ bool join_parts(const WorkSplit &w, int tile, int wave, const Acc *parts, Acc (&acc)[T::CT][T::RT])
+// A wave's share of the parts of tile `tile` (counted from the first that is cut), summed in a fixed order by the
+// JOINERS waves of the workgroup; false when the tile was taken whole, or to all but the first of the waves.
+// `shared`: GROUPS * 64 * (JOINERS - 1) accumulators.
+template <class T, int JOINERS, class Acc>
+__device__ __forceinline__ bool join_parts(const WorkSplit &w, int tile, int wave, const Acc *parts, Acc *shared, Acc (&acc)[T::CT][T::RT])
 {
     const int first = tile * w.stages;
     const int from = w.owner(first), to = w.owner(first + w.stages - 1);
     if (from == to) return false;
+    const int lane = threadIdx.x & 63, joiner = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
     for (int j = 0; j < T::CT; ++j)
 #pragma unroll
         for (int i = 0; i < T::RT; ++i) acc[j][i] = Acc{0, 0, 0, 0};
-    for (int k = from; k <= to; ++k) {
-        const Acc *at = parts + (int64_t)(2 * k + (w.begin(k) <= first)) * T::GROUPS * T::THREADS + wave * 64 + (threadIdx.x & 63);
+    for (int k = from + joiner; k <= to; k += JOINERS) {
+        const Acc *at = parts + (int64_t)(2 * k + (w.begin(k) <= first)) * T::GROUPS * T::THREADS + wave * 64 + lane;
 #pragma unroll
         for (int j = 0; j < T::CT; ++j)
 #pragma unroll
             for (int i = 0; i < T::RT; ++i) acc[j][i] += at[(j * T::RT + i) * T::THREADS];
     }
+    if (JOINERS == 1) return true;
+    if (joiner > 0)
+#pragma unroll
+        for (int j = 0; j < T::CT; ++j)
+#pragma unroll
+            for (int i = 0; i < T::RT; ++i) shared[((joiner - 1) * T::GROUPS + j * T::RT + i) * 64 + lane] = acc[j][i];
+    __syncthreads();
+    if (joiner > 0) return false;
+    for (int k = 0; k < JOINERS - 1; ++k)
+#pragma unroll
+        for (int j = 0; j < T::CT; ++j)
+#pragma unroll
+            for (int i = 0; i < T::RT; ++i) acc[j][i] += shared[(k * T::GROUPS + j * T::RT + i) * 64 + lane];
     return true;
 }
 
+// Waves that join a wave's share: several where parts are small and may be many
+template <class T>
+constexpr int joiners() { return T::GROUPS <= 4 ? 8 : 1; }
+template <class T>
+constexpr int join_lds() { return T::GROUPS * 64 * 16 * (joiners<T>() - 1); }
+
 // Calls f(row, col, values) for every 32 x 32 tile of the wave, one after the other: row and col of its corner within
 // the workgroup's tile.  values[2 i + j][e] of a lane is at row 16 i + (lane & 15), column 16 j + 4 (lane >> 4) + e.
-template <class T, class Acc, class F>
-__device__ __forceinline__ void for_wave_tiles(const Acc (&acc)[T::CT][T::RT], int wave, F &&f)
+// ahead(row, col) is called one tile early, where registers allow; what it returns (loads under way) is passed to f.
+template <class T, class Acc, class A, class F>
+__device__ __forceinline__ void for_wave_tiles(const Acc (&acc)[T::CT][T::RT], int wave, A &&ahead, F &&f)
 {
+    constexpr int kTiles = T::CT / 2 * (T::RT / 2);
     const int row = wave / T::WC * T::RT * 16, col = wave % T::WC * T::CT * 16;
+    const auto values = [&](int i, int j, Acc (&v)[4]) { v[0] = acc[j][i], v[1] = acc[j + 1][i], v[2] = acc[j][i + 1], v[3] = acc[j + 1][i + 1]; };
+    if constexpr (T::GROUPS <= 16) {
+        auto next = ahead(row, col);
 #pragma unroll
-    for (int j = 0; j < T::CT; j += 2)
-#pragma unroll
-        for (int i = 0; i < T::RT; i += 2) {
-            const Acc v[4] = {acc[j][i], acc[j + 1][i], acc[j][i + 1], acc[j + 1][i + 1]};
-            f(row + 16 * i, col + 16 * j, v);
+        for (int t = 0; t < kTiles; ++t) {
+            const int i = t % (T::RT / 2) * 2, j = t / (T::RT / 2) * 2;
+            const auto now = next;
+            if (t + 1 < kTiles) next = ahead(row + (t + 1) % (T::RT / 2) * 32, col + (t + 1) / (T::RT / 2) * 32);
+            Acc v[4];
+            values(i, j, v);
+            f(row + 16 * i, col + 16 * j, v, now);
             __builtin_amdgcn_sched_barrier(0);   // (one tile's values at a time in registers)
         }
+    } else {
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) {
+            const int i = t % (T::RT / 2) * 2, j = t / (T::RT / 2) * 2;
+            Acc v[4];
+            values(i, j, v);
+            f(row + 16 * i, col + 16 * j, v, ahead(row + 16 * i, col + 16 * j));
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
 }
 
 // Four rows of a lane quad, four 16-bit values of adjacent columns each -> the lane's column (its place in the quad),
