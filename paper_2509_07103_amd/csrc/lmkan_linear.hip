@@ -1,9 +1,10 @@
 // The linear term in 8-bit whole numbers: rows scaled to codes one by one, products of codes summed exactly,
 //   y = beta y + xscale wscale sum(xcode wcode) + bias.
 //
-// Three kernels.  quantize_kernel reads rows once and writes codes and scales.  linear_kernel multiplies tiles of codes
-// on the matrix cores (lmkan_tile.h); few tiles with a long summed axis are cut along it and joined.  few_rows_kernel
-// answers single rows: it is bound by reading the weights, which every wave has on their way before it scales the rows.
+// quantize_kernel reads rows once and writes codes and scales; linear_kernel multiplies tiles of codes on the matrix
+// cores (lmkan_tile.h), few tiles with a long summed axis cut along it and joined.  Calls of few rows are bound by
+// launches and by reading the weights: one_row_kernel and some_rows_kernel (up to 64 short rows) take one launch, in
+// which every workgroup scales the rows for itself while its weights are on their way.
 #include "lmkan_dense.h"
 
 #include "lmkan_kernels.h"
@@ -66,6 +67,24 @@ __device__ __forceinline__ void load_four(const void *x, int64_t at, int left, b
     }
 }
 
+// Weights whose rows are not a multiple of 16 bytes, or start anywhere, to rows that are; a dword a thread
+struct AlignArgs {
+    const int8_t *w;
+    int n_in, n_out, pitch;
+    int8_t *to;
+};
+__device__ __forceinline__ void align_rows(const AlignArgs &a, unsigned block)
+{
+    const int64_t e = (int64_t)block * 256 + threadIdx.x;
+    const int64_t row = e / (a.pitch / 4);
+    const int k = (int)(e - row * (a.pitch / 4)) * 4;
+    if (row >= a.n_out) return;
+    int c[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c[i] = k + i < a.n_in ? a.w[row * a.n_in + k + i] : 0;
+    *reinterpret_cast<uint32_t *>(a.to + row * a.pitch + k) = packed(c);
+}
+
 constexpr int kHeld = 8;   // fours of a row that a thread keeps; longer rows are read again (from the L2)
 
 struct QuantizeArgs {
@@ -75,6 +94,8 @@ struct QuantizeArgs {
     const void *x;
     int8_t *codes;
     float *scale;
+    unsigned row_blocks;
+    AlignArgs align;   // the workgroups beyond row_blocks
 };
 
 // LANES threads a row (a wave, or a workgroup of 256)
@@ -82,6 +103,7 @@ template <int DTYPE, int LANES>
 __global__ __launch_bounds__(256) void quantize_kernel(QuantizeArgs a)
 {
     __shared__ uint32_t tops[4];
+    if (blockIdx.x >= a.row_blocks) return align_rows(a.align, blockIdx.x - a.row_blocks);
     const int64_t row = LANES == 64 ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
     if (LANES == 64 && row >= a.rows) return;
     const int t = LANES == 64 ? threadIdx.x & 63 : threadIdx.x;
@@ -238,7 +260,7 @@ __device__ __forceinline__ void finish_tile(const LinearArgs &a, int tile, const
             const int j = j0 + col + (lane & 31);
             if (j >= a.n_out) return;
             const float ws = a.w_scale[j], b = a.bias ? a.bias[j] : 0.0f;
-#pragma unroll 2
+#pragma unroll 8
             for (int k = lane >> 5; k < 32; k += 2) {
                 const int64_t i = i0 + row + k;
                 if (i >= a.batch) break;
@@ -285,34 +307,18 @@ __global__ __launch_bounds__(64 * joiners<T>()) void linear_join_kernel(LinearAr
     finish_tile<T>(a, a.work.whole + tile, acc, lds, wave);
 }
 
-// Weights whose rows are not a multiple of 16 bytes, or start anywhere, to rows that are; a dword a thread
-__global__ __launch_bounds__(256) void align_kernel(const int8_t *w, int n_in, int n_out, int pitch, int8_t *to)
-{
-    const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t row = e / (pitch / 4);
-    const int k = (int)(e - row * (pitch / 4)) * 4;
-    if (row >= n_out) return;
-    int c[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) c[i] = k + i < n_in ? w[row * n_in + k + i] : 0;
-    *reinterpret_cast<uint32_t *>(to + row * pitch + k) = packed(c);
-}
+// ---- one row ---------------------------------------------------------------------------------------------------------
 
-// ---- few rows --------------------------------------------------------------------------------------------------------
+constexpr int kRowHeld = 4;              // fours of the row that a thread keeps
 
-constexpr int kMostRows = 4;             // rows of a call that few_rows_kernel takes
-constexpr int kMostCodes = 48 * 1024;    // bytes of LDS for their codes
-constexpr int kFewHeld = 4;              // fours of a row that a thread keeps
-
-struct FewArgs {
+struct RowsArgs {
     const void *x;
     const int8_t *w;
     const float *w_scale, *bias;
     float beta;
     void *y;
-    int n_in, n_out, x_dtype, y_dtype;
+    int n_in, n_out, y_dtype;
     bool relu, w_aligned, x_by_four;
-    int padded;                          // n_in rounded up to the codes that a wave reads at a time
 };
 
 // 16 codes of a row from k on, zero beyond its end
@@ -329,12 +335,13 @@ __device__ __forceinline__ intx4 load_codes(const int8_t *row, int k, int n_in, 
     return v;
 }
 
-// A wave takes OUTS outputs of all ROWS rows; CHUNKS pieces of 1024 codes of each output are on their way at a time.
-template <int DTYPE, int ROWS, int OUTS, int CHUNKS>
-__global__ __launch_bounds__(256) void few_rows_kernel(FewArgs a)
+// A wave takes OUTS outputs; CHUNKS pieces of 1024 codes of each are on their way at a time, the first before the row
+// is scaled.  `padded`: n_in rounded up to pieces.
+template <int DTYPE, int OUTS, int CHUNKS>
+__global__ __launch_bounds__(256) void one_row_kernel(RowsArgs a, int padded)
 {
     extern __shared__ __align__(16) char lds[];
-    __shared__ uint32_t tops[ROWS][4];
+    __shared__ uint32_t tops[4];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int j0 = (blockIdx.x * 4 + wave) * OUTS;
     intx4 w[OUTS][CHUNKS];
@@ -348,93 +355,183 @@ __global__ __launch_bounds__(256) void few_rows_kernel(FewArgs a)
             }
     };
     fetch(0);
-    // the rows' codes, in LDS; a thread keeps the first kFewHeld fours of each row that it sees
+    // the row's codes, in LDS; a thread keeps the first kRowHeld fours that it sees
     const int fours = (a.n_in + 3) / 4;
-    float v[ROWS][kFewHeld][4];
-    const auto load = [&](int r, int f, float (&to)[4]) {
+    float v[kRowHeld][4];
+    const auto load = [&](int f, float (&to)[4]) {
         const int left = a.n_in - 4 * f;
-        load_four<DTYPE>(a.x, (int64_t)r * a.n_in + 4 * f, left, a.x_by_four && left >= 4, to);
+        load_four<DTYPE>(a.x, 4 * f, left, a.x_by_four && left >= 4, to);
 #pragma unroll
         for (int e = 0; e < 4; ++e) to[e] = rectified(to[e], a.relu);
     };
-    uint32_t top[ROWS] = {};
-    const auto see = [&](int r, const float (&from)[4]) {
+    uint32_t top = 0;
+    const auto see = [&](const float (&from)[4]) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) top[r] = larger(top[r], magnitude(from[e]));
+        for (int e = 0; e < 4; ++e) top = larger(top, magnitude(from[e]));
     };
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r)
+    for (int h = 0; h < kRowHeld; ++h)
+        if ((int)threadIdx.x + h * 256 < fours) load(threadIdx.x + h * 256, v[h]);
 #pragma unroll
-        for (int h = 0; h < kFewHeld; ++h)
-            if ((int)threadIdx.x + h * 256 < fours) load(r, threadIdx.x + h * 256, v[r][h]);
-#pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
-#pragma unroll
-        for (int h = 0; h < kFewHeld; ++h)
-            if ((int)threadIdx.x + h * 256 < fours) see(r, v[r][h]);
+    for (int h = 0; h < kRowHeld; ++h)
+        if ((int)threadIdx.x + h * 256 < fours) see(v[h]);
 #pragma unroll 4
-        for (int f = threadIdx.x + kFewHeld * 256; f < fours; f += 256) {
-            float w[4];
-            load(r, f, w);
-            see(r, w);
-        }
-        top[r] = wave_max(top[r]);
-        if (lane == 0) tops[r][wave] = top[r];
+    for (int f = threadIdx.x + kRowHeld * 256; f < fours; f += 256) {
+        float t[4];
+        load(f, t);
+        see(t);
     }
+    top = wave_max(top);
+    if (lane == 0) tops[wave] = top;
     __syncthreads();
-    float scale[ROWS];
+    const RowScale s(larger(larger(tops[0], tops[1]), larger(tops[2], tops[3])));
+    const auto store = [&](int f, const float (&from)[4]) {
+        int c[4];
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
-        const RowScale s(larger(larger(tops[r][0], tops[r][1]), larger(tops[r][2], tops[r][3])));
-        scale[r] = s.scale;
-        const auto store = [&](int f, const float (&from)[4]) {
-            int c[4];
+        for (int e = 0; e < 4; ++e) c[e] = s.code(from[e]);   // (beyond the row's end: of zero)
+        *reinterpret_cast<uint32_t *>(lds + 4 * f) = packed(c);
+    };
 #pragma unroll
-            for (int e = 0; e < 4; ++e) c[e] = s.code(from[e]);   // (beyond the row's end: of zero)
-            *reinterpret_cast<uint32_t *>(lds + r * a.padded + 4 * f) = packed(c);
-        };
-#pragma unroll
-        for (int h = 0; h < kFewHeld; ++h)
-            if ((int)threadIdx.x + h * 256 < fours) store(threadIdx.x + h * 256, v[r][h]);
+    for (int h = 0; h < kRowHeld; ++h)
+        if ((int)threadIdx.x + h * 256 < fours) store(threadIdx.x + h * 256, v[h]);
 #pragma unroll 4
-        for (int f = threadIdx.x + kFewHeld * 256; f < fours; f += 256) {
-            float w[4];
-            load(r, f, w);
-            store(f, w);
-        }
-        for (int f = fours + threadIdx.x; f < a.padded / 4; f += 256) *reinterpret_cast<uint32_t *>(lds + r * a.padded + 4 * f) = 0;
+    for (int f = threadIdx.x + kRowHeld * 256; f < fours; f += 256) {
+        float t[4];
+        load(f, t);
+        store(f, t);
     }
+    for (int f = fours + threadIdx.x; f < padded / 4; f += 256) *reinterpret_cast<uint32_t *>(lds + 4 * f) = 0;
     __syncthreads();
-    int sum[ROWS][OUTS] = {};
+    int sum[OUTS] = {};
     for (int k0 = 0; k0 < a.n_in; k0 += CHUNKS * 1024) {
         if (k0) fetch(k0);
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
             if (k0 + c * 1024 >= a.n_in) break;
+            const intx4 x = *reinterpret_cast<const intx4 *>(lds + k0 + c * 1024 + lane * 16);
 #pragma unroll
-            for (int r = 0; r < ROWS; ++r) {
-                const intx4 x = *reinterpret_cast<const intx4 *>(lds + r * a.padded + k0 + c * 1024 + lane * 16);
+            for (int o = 0; o < OUTS; ++o)
 #pragma unroll
-                for (int o = 0; o < OUTS; ++o)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) sum[r][o] = __builtin_amdgcn_sdot4(x[e], w[o][c][e], sum[r][o], false);
-            }
+                for (int e = 0; e < 4; ++e) sum[o] = __builtin_amdgcn_sdot4(x[e], w[o][c][e], sum[o], false);
         }
     }
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r)
+    for (int o = 0; o < OUTS; ++o) {
+        int t = sum[o];
 #pragma unroll
-        for (int o = 0; o < OUTS; ++o) {
-            int v = sum[r][o];
-#pragma unroll
-            for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d, 64);
-            if (lane == 0 && j0 + o < a.n_out) {
-                const int64_t at = (int64_t)r * a.n_out + j0 + o;
-                float y = (float)v * (scale[r] * a.w_scale[j0 + o]) + (a.bias ? a.bias[j0 + o] : 0.0f);
-                if (a.beta != 0.0f) y += a.beta * load_as_float(a.y, at, a.y_dtype);
-                store_from_float(a.y, at, a.y_dtype, y);
-            }
+        for (int d = 32; d > 0; d >>= 1) t += __shfl_xor(t, d, 64);
+        const int j = j0 + o;
+        if (lane == 0 && j < a.n_out) {
+            float y = (float)t * (s.scale * a.w_scale[j]) + (a.bias ? a.bias[j] : 0.0f);
+            if (a.beta != 0.0f) y += a.beta * load_as_float(a.y, j, a.y_dtype);
+            store_from_float(a.y, j, a.y_dtype, y);
         }
+    }
+}
+
+// ---- some rows -------------------------------------------------------------------------------------------------------
+
+constexpr int kSomeRows = 64;                // rows of a call that some_rows_kernel takes
+constexpr int kSomeWaves = 16;
+constexpr int kSomeLds = 128 * 1024;         // bytes of LDS for their codes
+constexpr int kSomeFetched = 4;              // pieces of 64 codes that a wave has on their way at the start
+
+// 64 codes are a piece of the summed axis; rows of codes are a piece apart from a multiple of LDS's banks
+int some_pitch(int n_in) { return (n_in + 63) / 64 * 64 + 16; }
+
+// A workgroup takes 16 outputs of all rows, RT tiles of 16.  A wave scales every sixteenth row, then multiplies every
+// sixteenth piece; the waves' sums meet in LDS, as whole numbers in any order.
+template <int DTYPE, int RT>
+__global__ __launch_bounds__(64 * kSomeWaves) void some_rows_kernel(RowsArgs a, int rows, int pitch)
+{
+    extern __shared__ __align__(16) char lds[];
+    __shared__ int sums[RT * 16][17];
+    __shared__ float scales[RT * 16];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int j0 = blockIdx.x * 16, pieces = (a.n_in + 63) / 64;
+    // weights: row lane & 15 of the 16 outputs, 16 codes from 16 (lane >> 4) on of a piece
+    const int8_t *w = a.w + (int64_t)min(j0 + (lane & 15), a.n_out - 1) * a.n_in;
+    const auto fetch = [&](int piece) { return load_codes(w, min(64 * piece + 16 * (lane >> 4), a.n_in), a.n_in, a.w_aligned); };
+    intx4 fetched[kSomeFetched];
+#pragma unroll
+    for (int k = 0; k < kSomeFetched; ++k)
+        if (wave + k * kSomeWaves < pieces) fetched[k] = fetch(wave + k * kSomeWaves);
+    for (int e = threadIdx.x; e < RT * 16 * 17; e += 64 * kSomeWaves) (&sums[0][0])[e] = 0;
+    const int fours = (a.n_in + 3) / 4;
+    for (int r = wave; r < rows; r += kSomeWaves) {
+        float v[kHeld][4];
+        uint32_t top = 0;
+        const auto load = [&](int f, float (&to)[4]) {
+            const int left = a.n_in - 4 * f;
+            load_four<DTYPE>(a.x, (int64_t)r * a.n_in + 4 * f, left, a.x_by_four && left >= 4, to);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) to[e] = rectified(to[e], a.relu);
+        };
+        const auto see = [&](const float (&from)[4]) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) top = larger(top, magnitude(from[e]));
+        };
+#pragma unroll
+        for (int h = 0; h < kHeld; ++h)
+            if (lane + h * 64 < fours) load(lane + h * 64, v[h]);
+#pragma unroll
+        for (int h = 0; h < kHeld; ++h)
+            if (lane + h * 64 < fours) see(v[h]);
+#pragma unroll 4
+        for (int f = lane + kHeld * 64; f < fours; f += 64) {
+            float t[4];
+            load(f, t);
+            see(t);
+        }
+        const RowScale s(wave_max(top));
+        if (lane == 0) scales[r] = s.scale;
+        char *to = lds + r * pitch;
+        const auto store = [&](int f, const float (&from)[4]) {
+            int c[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) c[e] = s.code(from[e]);   // (beyond the row's end: of zero)
+            *reinterpret_cast<uint32_t *>(to + 4 * f) = packed(c);
+        };
+#pragma unroll
+        for (int h = 0; h < kHeld; ++h)
+            if (lane + h * 64 < fours) store(lane + h * 64, v[h]);
+#pragma unroll 4
+        for (int f = lane + kHeld * 64; f < fours; f += 64) {
+            float t[4];
+            load(f, t);
+            store(f, t);
+        }
+        if (lane < 16 * pieces - fours) *reinterpret_cast<uint32_t *>(to + 4 * (fours + lane)) = 0;
+    }
+    __syncthreads();
+    intx4 acc[RT];
+#pragma unroll
+    for (int i = 0; i < RT; ++i) acc[i] = intx4{0, 0, 0, 0};
+    const auto multiply = [&](int piece, const intx4 &cols) {
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+            // (rows beyond the last repeat it: their outputs are dropped)
+            const intx4 x = *reinterpret_cast<const intx4 *>(lds + min(16 * i + (lane & 15), rows - 1) * pitch + 64 * piece + 16 * (lane >> 4));
+            acc[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(cols, x, acc[i], 0, 0, 0);
+        }
+    };
+#pragma unroll
+    for (int k = 0; k < kSomeFetched; ++k)
+        if (wave + k * kSomeWaves < pieces) multiply(wave + k * kSomeWaves, fetched[k]);
+    for (int piece = wave + kSomeFetched * kSomeWaves; piece < pieces; piece += kSomeWaves) multiply(piece, fetch(piece));
+    if (wave < pieces)
+#pragma unroll
+        for (int i = 0; i < RT; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) atomicAdd(&sums[16 * i + (lane & 15)][4 * (lane >> 4) + e], acc[i][e]);
+    __syncthreads();
+    const int r = threadIdx.x >> 4, j = j0 + (threadIdx.x & 15);
+    if (r < rows && j < a.n_out) {
+        const int64_t at = (int64_t)r * a.n_out + j;
+        float y = (float)sums[r][threadIdx.x & 15] * (scales[r] * a.w_scale[j]) + (a.bias ? a.bias[j] : 0.0f);
+        if (a.beta != 0.0f) y += a.beta * load_as_float(a.y, at, a.y_dtype);
+        store_from_float(a.y, at, a.y_dtype, y);
+    }
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------
@@ -443,9 +540,17 @@ size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 bool aligned_to(const void *p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 
 int padded_row(int n_in) { return (n_in + kLine - 1) / kLine * kLine; }
-int padded_few(int n_in) { return (n_in + 1023) / 1024 * 1024; }
+int padded_one(int n_in) { return (n_in + 1023) / 1024 * 1024; }
 
-bool few_rows(const LinearShape &s) { return s.batch <= kMostRows && s.batch * padded_few(s.n_in) <= kMostCodes; }
+// One launch, in which every workgroup scales all rows, or three.  The former takes 3.5 us and 0.14 for every 1024
+// elements of x and turn of a compute unit (a workgroup of 16 outputs at a time), the latter 7 to 17 us.  Measured (us, one
+// launch / three): 16 rows of 1024 -> 1024 5.7 / 10.7; 48 of 1024 -> 1024 10.1 / 11.4; 64 of 1024 -> 4096 13.1 / 11.4;
+// 64 of 256 -> 16384 30 / 8.3.
+bool some_rows(const LinearShape &s)
+{
+    const int64_t turns = (s.n_out + 16 * 256 - 1) / (16 * 256);
+    return s.batch > 1 && s.batch <= kSomeRows && s.batch * some_pitch(s.n_in) <= kSomeLds && s.batch * s.n_in * turns <= 50 * 1024;
+}
 
 typedef TileShape<64, 64, 2, 2, 3> Tile64;
 typedef TileShape<128, 128, 2, 2, 2> Tile128;
@@ -474,7 +579,7 @@ struct Layout {
 Layout layout_of(const LinearShape &s)
 {
     Layout l = {};
-    if (few_rows(s)) return l;
+    if (s.batch == 1 || some_rows(s)) return l;
     const WorkSplit w = split_work(s);
     const size_t tile = (large_tiles(s) ? Tile128::ROWS * Tile128::COLS : Tile64::ROWS * Tile64::COLS) * sizeof(int);
     size_t at = 0;
@@ -496,33 +601,50 @@ void launch_tiles(LinearArgs &a, hipStream_t stream)
     if (a.work.cut()) linear_join_kernel<T><<<a.work.left() * T::WAVES, 64 * joiners<T>(), 0, stream>>>(a);
 }
 
-template <int DTYPE, int ROWS>
-void launch_few_rows(const FewArgs &a, hipStream_t stream)
+template <int DTYPE>
+void launch_one(const RowsArgs &a, hipStream_t stream)
 {
     // one output a wave where four would leave compute units idle
-    if (a.n_out < 2048) few_rows_kernel<DTYPE, ROWS, 1, 8><<<(a.n_out + 3) / 4, 256, ROWS * a.padded, stream>>>(a);
-    else few_rows_kernel<DTYPE, ROWS, 4, 4><<<(a.n_out + 15) / 16, 256, ROWS * a.padded, stream>>>(a);
+    const int padded = padded_one(a.n_in);
+    if (padded > 56 * 1024) {
+        allow_large_lds(reinterpret_cast<const void *>(one_row_kernel<DTYPE, 1, 8>), padded_one(LMKAN_MAX_N_IN));
+        allow_large_lds(reinterpret_cast<const void *>(one_row_kernel<DTYPE, 4, 4>), padded_one(LMKAN_MAX_N_IN));
+    }
+    if (a.n_out < 2048) one_row_kernel<DTYPE, 1, 8><<<(a.n_out + 3) / 4, 256, padded, stream>>>(a, padded);
+    else one_row_kernel<DTYPE, 4, 4><<<(a.n_out + 15) / 16, 256, padded, stream>>>(a, padded);
+}
+
+template <int DTYPE, int RT>
+void launch_some_rows(int rows, const RowsArgs &a, hipStream_t stream)
+{
+    const int pitch = some_pitch(a.n_in), lds = rows * pitch;
+    if (lds > 56 * 1024) allow_large_lds(reinterpret_cast<const void *>(some_rows_kernel<DTYPE, RT>), kSomeLds);
+    some_rows_kernel<DTYPE, RT><<<(a.n_out + 15) / 16, 64 * kSomeWaves, lds, stream>>>(a, rows, pitch);
 }
 template <int DTYPE>
-void launch_few(int64_t rows, const FewArgs &a, hipStream_t stream)
+void launch_some(int rows, const RowsArgs &a, hipStream_t stream)
 {
-    if (rows == 1) launch_few_rows<DTYPE, 1>(a, stream);
-    else if (rows == 2) launch_few_rows<DTYPE, 2>(a, stream);
-    else if (rows == 3) launch_few_rows<DTYPE, 3>(a, stream);
-    else launch_few_rows<DTYPE, 4>(a, stream);
+    if (rows <= 16) launch_some_rows<DTYPE, 1>(rows, a, stream);
+    else if (rows <= 32) launch_some_rows<DTYPE, 2>(rows, a, stream);
+    else launch_some_rows<DTYPE, 4>(rows, a, stream);
 }
 
 template <int DTYPE>
-void launch_quantize(const QuantizeArgs &a, hipStream_t stream)
+void launch_quantize(QuantizeArgs a, hipStream_t stream)
 {
     // a wave a row while the row fits what its lanes hold
-    if (a.cols <= 64 * 4 * kHeld) quantize_kernel<DTYPE, 64><<<(unsigned)((a.rows + 3) / 4), 256, 0, stream>>>(a);
-    else quantize_kernel<DTYPE, 256><<<(unsigned)a.rows, 256, 0, stream>>>(a);
+    const bool wave = a.cols <= 64 * 4 * kHeld;
+    a.row_blocks = (unsigned)(wave ? (a.rows + 3) / 4 : a.rows);
+    const int64_t dwords = a.align.w ? (int64_t)a.align.n_out * (a.align.pitch / 4) : 0;
+    const unsigned blocks = a.row_blocks + (unsigned)((dwords + 255) / 256);
+    if (wave) quantize_kernel<DTYPE, 64><<<blocks, 256, 0, stream>>>(a);
+    else quantize_kernel<DTYPE, 256><<<blocks, 256, 0, stream>>>(a);
 }
 
-void quantize(int64_t rows, int cols, int pitch, int dtype, bool relu, const void *x, int8_t *codes, float *scale, hipStream_t stream)
+void quantize(int64_t rows, int cols, int pitch, int dtype, bool relu, const void *x, int8_t *codes, float *scale, const AlignArgs &align,
+              hipStream_t stream)
 {
-    QuantizeArgs a{rows, cols, pitch, relu, pitch > cols, false, false, x, codes, scale};
+    QuantizeArgs a{rows, cols, pitch, relu, pitch > cols, false, false, x, codes, scale, 0, align};
     a.by_four = cols % 4 == 0 && aligned_to(x, dtype == LMKAN_F32 ? 16 : 8);
     a.codes_by_four = pitch % 4 == 0 && aligned_to(codes, 4);
     if (dtype == LMKAN_F32) launch_quantize<LMKAN_F32>(a, stream);
@@ -534,7 +656,7 @@ void quantize(int64_t rows, int cols, int pitch, int dtype, bool relu, const voi
 
 void launch_quantize_rows(int64_t rows, int cols, int dtype, bool relu, const void *x, int8_t *codes, float *scale, hipStream_t stream)
 {
-    quantize(rows, cols, cols, dtype, relu, x, codes, scale, stream);
+    quantize(rows, cols, cols, dtype, relu, x, codes, scale, AlignArgs{}, stream);
 }
 
 size_t linear_i8_workspace_bytes(const LinearShape &s) { return layout_of(s).total; }
@@ -542,13 +664,13 @@ size_t linear_i8_workspace_bytes(const LinearShape &s) { return layout_of(s).tot
 void launch_linear_i8(const LinearShape &s, const void *x, const int8_t *w, const float *w_scale, const float *bias,
                       float beta, void *y, void *workspace, hipStream_t stream)
 {
-    if (few_rows(s)) {
-        const FewArgs a{x, w, w_scale, bias, beta, y, s.n_in, s.n_out, s.x_dtype, s.y_dtype, s.relu,
-                        s.n_in % 16 == 0 && aligned_to(w, 16), s.n_in % 4 == 0 && aligned_to(x, s.x_dtype == LMKAN_F32 ? 16 : 8),
-                        padded_few(s.n_in)};
-        if (s.x_dtype == LMKAN_F32) launch_few<LMKAN_F32>(s.batch, a, stream);
-        else if (s.x_dtype == LMKAN_F16) launch_few<LMKAN_F16>(s.batch, a, stream);
-        else launch_few<LMKAN_BF16>(s.batch, a, stream);
+    if (s.batch == 1 || some_rows(s)) {
+        const RowsArgs a{x, w, w_scale, bias, beta, y, s.n_in, s.n_out, s.y_dtype, s.relu, s.n_in % 16 == 0 && aligned_to(w, 16),
+                         s.n_in % 4 == 0 && aligned_to(x, s.x_dtype == LMKAN_F32 ? 16 : 8)};
+        const int rows = (int)s.batch;
+        if (s.x_dtype == LMKAN_F32) rows == 1 ? launch_one<LMKAN_F32>(a, stream) : launch_some<LMKAN_F32>(rows, a, stream);
+        else if (s.x_dtype == LMKAN_F16) rows == 1 ? launch_one<LMKAN_F16>(a, stream) : launch_some<LMKAN_F16>(rows, a, stream);
+        else rows == 1 ? launch_one<LMKAN_BF16>(a, stream) : launch_some<LMKAN_BF16>(rows, a, stream);
         return;
     }
     const Layout l = layout_of(s);
@@ -556,16 +678,15 @@ void launch_linear_i8(const LinearShape &s, const void *x, const int8_t *w, cons
     int8_t *codes = reinterpret_cast<int8_t *>(ws + l.codes);
     float *scale = reinterpret_cast<float *>(ws + l.scale);
     const int pitch = padded_row(s.n_in);
-    quantize(s.batch, s.n_in, pitch, s.x_dtype, s.relu, x, codes, scale, stream);
     LinearArgs a = {};
     a.x = codes, a.x_pitch = pitch;
     a.w = w, a.w_pitch = s.n_in;
+    AlignArgs align = {};
     if (s.n_in % 16 != 0 || !aligned_to(w, 16)) {
-        int8_t *to = reinterpret_cast<int8_t *>(ws + l.w);
-        const int64_t dwords = (int64_t)s.n_out * (pitch / 4);
-        align_kernel<<<(unsigned)((dwords + 255) / 256), 256, 0, stream>>>(w, s.n_in, s.n_out, pitch, to);
-        a.w = to, a.w_pitch = pitch;
+        align = {w, s.n_in, s.n_out, pitch, reinterpret_cast<int8_t *>(ws + l.w)};
+        a.w = align.to, a.w_pitch = pitch;
     }
+    quantize(s.batch, s.n_in, pitch, s.x_dtype, s.relu, x, codes, scale, align, stream);
     a.x_scale = scale, a.w_scale = w_scale, a.bias = bias, a.beta = beta;
     a.y = y, a.batch = s.batch, a.n_in = s.n_in, a.n_out = s.n_out, a.y_dtype = s.y_dtype;
     a.by_four = s.n_out % 4 == 0 && aligned_to(y, s.y_dtype == LMKAN_F32 ? 16 : 8);
