@@ -178,7 +178,7 @@ struct LinearArgs {
     int64_t batch;
     int n_in, n_out, y_dtype;
     bool by_four;              // rows of y take accesses of four elements
-    int tiles_across;
+    int tiles_down, tiles_across;
     WorkSplit work;
     intx4 *parts;
 };
@@ -189,9 +189,10 @@ __device__ __forceinline__ void finish_tile(const LinearArgs &a, int tile, const
     int lane = threadIdx.x & 63;
     asm volatile("" : "+v"(lane));   // (the addresses below are worked out here, not kept in registers through the main loop)
     const int r = lane & 15, q = lane >> 4;
-    const int ti = tile / a.tiles_across;
+    int ti, tj;
+    grouped_tile(tile, a.tiles_down, a.tiles_across, &ti, &tj);
     const int64_t i0 = (int64_t)ti * T::ROWS;
-    const int j0 = (tile - ti * a.tiles_across) * T::COLS;
+    const int j0 = tj * T::COLS;
     // what a lane finishes of a 32 x 32 tile, after the tile went through LDS: rows 8 t + lane / 8, four columns
     const int fr = lane >> 3, fc = (lane & 7) * 4;
     struct Held {
@@ -278,9 +279,10 @@ __global__ __launch_bounds__(T::THREADS) void linear_kernel(LinearArgs a)
 {
     extern __shared__ __align__(16) char lds[];
     for_work(a.work, blockIdx.x, [&](int tile, int from, int to, int slot) {
-        const int ti = tile / a.tiles_across;
-        const int64_t i0 = (int64_t)ti * T::ROWS;
-        const int j0 = (tile - ti * a.tiles_across) * T::COLS;
+        int ti, tj;
+        grouped_tile(tile, a.tiles_down, a.tiles_across, &ti, &tj);
+        const int64_t i0 = (int64_t)uniform(ti) * T::ROWS;
+        const int j0 = uniform(tj) * T::COLS;
         const int64_t last = a.batch - 1 - i0;
         const Operand x{reinterpret_cast<const char *>(uniform(a.x + i0 * a.x_pitch)), kLine, uniform((int)(last < T::ROWS ? last : T::ROWS)), false,
                         (unsigned)a.x_pitch, (int)a.x_pitch - 16};
@@ -288,7 +290,6 @@ __global__ __launch_bounds__(T::THREADS) void linear_kernel(LinearArgs a)
                         (int)a.w_pitch - 16};
         intx4 acc[T::CT][T::RT];
         multiply<T, CodeProduct>(x, w, from, to, lds, acc);
-        __syncthreads();
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         if (slot < 0) finish_tile<T>(a, tile, acc, lds + wave * kWaveScratch, wave);
         else store_part<T>(a.parts, slot, acc);
@@ -595,6 +596,7 @@ Layout layout_of(const LinearShape &s)
 template <class T>
 void launch_tiles(LinearArgs &a, hipStream_t stream)
 {
+    a.tiles_down = (int)((a.batch + T::ROWS - 1) / T::ROWS);
     a.tiles_across = (a.n_out + T::COLS - 1) / T::COLS;
     if (T::LDS > 65536) allow_large_lds(reinterpret_cast<const void *>(linear_kernel<T>), T::LDS);
     linear_kernel<T><<<a.work.workers, T::THREADS, T::LDS, stream>>>(a);

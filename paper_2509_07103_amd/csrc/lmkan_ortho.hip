@@ -204,7 +204,7 @@ struct ProductArgs {
     Product p[2];
     int problems;
     int matrices;
-    int tiles_across;
+    int tiles_down, tiles_across;
     int tiles;                 // of one matrix and problem
     WorkSplit work;
     floatx4 *parts;
@@ -215,16 +215,6 @@ struct ProductArgs {
     bool by_four;              // rows of the result take accesses of four elements
 };
 
-// Tile t of the upper triangle of n x n tiles, column by column: (0,0) (0,1) (1,1) (0,2) ...
-__device__ __forceinline__ void upper_tile(int t, int *i, int *j)
-{
-    int c = (int)((__builtin_amdgcn_sqrtf(8.0f * t + 1.0f) - 1.0f) * 0.5f);   // (about)
-    while ((c + 1) * (c + 2) / 2 <= t) ++c;
-    while (c * (c + 1) / 2 > t) --c;
-    *j = c;
-    *i = t - c * (c + 1) / 2;
-}
-
 // Where a tile of the launch is
 struct Place {
     int matrix, problem, ti, tj;
@@ -234,8 +224,8 @@ __device__ __forceinline__ Place place_of(const ProductArgs &a, int t)
     const int which = t / a.tiles, tile = t - which * a.tiles;
     const int matrix = a.problems == 1 ? which : which >> 1;
     int ti, tj;
-    if (a.p[0].symmetric) upper_tile(tile, &ti, &tj);
-    else ti = tile / a.tiles_across, tj = tile - ti * a.tiles_across;
+    if (a.p[0].symmetric) upper_tile(tile, a.tiles_across, &ti, &tj);
+    else grouped_tile(tile, a.tiles_down, a.tiles_across, &ti, &tj);
     return Place{uniform(matrix), uniform(which - matrix * a.problems), uniform(ti), uniform(tj)};
 }
 
@@ -364,12 +354,13 @@ __global__ __launch_bounds__(T::THREADS) void product_kernel(ProductArgs a)
         floatx4 acc[T::CT][T::RT];
         // (a workgroup that finishes a tile goes before one that multiplies: 1 to 3 %)
         __builtin_amdgcn_s_setprio(0);
-        multiply<T, PairProduct>(operand(p.rows, w.ti * T::ROWS), operand(p.cols, w.tj * T::COLS), from, to, lds, acc);
+        const bool holds = multiply<T, PairProduct>(operand(p.rows, w.ti * T::ROWS), operand(p.cols, w.tj * T::COLS), from, to, lds, acc);
         __builtin_amdgcn_s_setprio(2);
-        __syncthreads();
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        if (slot < 0) finish_tile<T, FINISH>(a, w, acc, lds + wave * kWaveScratch, wave);
-        else store_part<T>(a.parts, slot, acc);
+        if (holds) {
+            if (slot < 0) finish_tile<T, FINISH>(a, w, acc, lds + wave * kWaveScratch, wave);
+            else store_part<T>(a.parts, slot, acc);
+        }
         __syncthreads();
     });
 }
@@ -399,7 +390,7 @@ __global__ __launch_bounds__(256) void unscaled_kernel(MatrixShape s, UpdateArgs
 }
 
 typedef TileShape<64, 64, 2, 2, 4> Tile64;
-typedef TileShape<64, 64, 2, 2, 9> Tile64Deep;
+typedef TileShape<64, 64, 2, 2, 4, 2> Tile64Deep;
 typedef TileShape<128, 128, 2, 2, 2> Tile128;
 typedef TileShape<256, 256, 4, 2, 2> Tile256;
 
@@ -416,6 +407,7 @@ template <class T, int FINISH>
 void launch_product_with(ProductArgs &a, hipStream_t stream)
 {
     const Product &p = a.p[0];
+    a.tiles_down = (p.rows.rows + T::ROWS - 1) / T::ROWS;
     a.tiles_across = (p.cols.rows + T::COLS - 1) / T::COLS;
     a.tiles = (int)tiles_of(p, T::ROWS);
     const int64_t tiles = (int64_t)a.tiles * a.matrices * a.problems;

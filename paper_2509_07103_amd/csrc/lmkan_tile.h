@@ -72,15 +72,17 @@ __device__ __forceinline__ void landed()
     asm volatile("" ::: "memory");
 }
 
-// Tile shape: ROWS x COLS outputs of one workgroup, WR x WC waves, stages in BUFFERS buffers
-template <int ROWS_, int COLS_, int WR_, int WC_, int BUFFERS_>
+// Tile shape: ROWS x COLS outputs of one workgroup, WR x WC waves, stages in BUFFERS buffers.  TURNS groups of such
+// waves take stages in turn (each its own buffers) and add up at the end: for tiles that have a compute unit to
+// themselves, where one wave a SIMD would wait for its own reads.
+template <int ROWS_, int COLS_, int WR_, int WC_, int BUFFERS_, int TURNS_ = 1>
 struct TileShape {
-    static constexpr int ROWS = ROWS_, COLS = COLS_, WR = WR_, WC = WC_, BUFFERS = BUFFERS_;
-    static constexpr int WAVES = WR * WC, THREADS = 64 * WAVES;
+    static constexpr int ROWS = ROWS_, COLS = COLS_, WR = WR_, WC = WC_, BUFFERS = BUFFERS_, TURNS = TURNS_;
+    static constexpr int WAVES = WR * WC, THREADS = 64 * WAVES * TURNS;
     static constexpr int RT = ROWS / WR / 16, CT = COLS / WC / 16;   // 16 x 16 tiles of a wave
     static constexpr int STAGE = (ROWS + COLS) * kLine;              // bytes of a stage
     static constexpr int LOADS = (ROWS + COLS) / 8 / WAVES;          // loads of a wave a stage
-    static constexpr int LDS = BUFFERS * STAGE;
+    static constexpr int LDS = BUFFERS * TURNS * STAGE;
     static constexpr int GROUPS = RT * CT;                           // groups of four outputs of a lane
 };
 
@@ -175,33 +177,43 @@ struct CodeProduct {
 
 // The main loop: stages [from, to) of both operands, from < to.  While one buffer is multiplied the others fill; the
 // last columns of a stage are multiplied after the barrier that ends it, while the first fragments of the next are
-// on their way.  All waves have read what they need of LDS when it returns after one more barrier.
+// on their way.  Returns whether the wave holds the sums (the first group's do), with all of LDS free.
 template <class T, class Product>
-__device__ __forceinline__ void multiply(const Operand &rows, const Operand &cols, int from, int to, char *lds,
+__device__ __forceinline__ bool multiply(const Operand &rows, const Operand &cols, int from, int to, char *lds,
                                          typename Product::Acc (&acc)[T::CT][T::RT])
 {
     typedef typename Product::Acc Acc;
     typedef Fragment<typename Product::Element> Frag;
     constexpr int kAhead = T::BUFFERS - 1;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const unsigned at = lds_offset(lds);
+    const int all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int turn = T::TURNS == 1 ? 0 : all / T::WAVES, wave = T::TURNS == 1 ? all : all % T::WAVES;
+    char *own = lds + turn * T::BUFFERS * T::STAGE;
+    const unsigned at = lds_offset(own);
     const int wr = wave / T::WC, wc = wave % T::WC;
+    const int rounds = (to - from + T::TURNS - 1) / T::TURNS;                        // of all groups
+    const int n = T::TURNS == 1 ? rounds : (to - from - turn + T::TURNS - 1) / T::TURNS;   // stages of this one
 #pragma unroll
     for (int j = 0; j < T::CT; ++j)
 #pragma unroll
         for (int i = 0; i < T::RT; ++i) acc[j][i] = Acc{0, 0, 0, 0};
-    const auto fill = [&](int stage, int buffer) {
+    const auto fill = [&](int k, int buffer) {
+        const int stage = from + k * T::TURNS + turn;
         stage_operand<T::ROWS, T::WAVES>(rows, stage, at + buffer * T::STAGE, wave, lane);
         stage_operand<T::COLS, T::WAVES>(cols, stage, at + buffer * T::STAGE + T::ROWS * kLine, wave, lane);
     };
+    // stage k has landed (near the end fewer loads are under way: then all of them are awaited)
+    const auto await = [&](int k) {
+        if (k + kAhead <= n) landed<(kAhead - 1) * T::LOADS>();
+        else landed<0>();
+    };
     const FragmentPlace place(lane);
     for (int b = 0; b < kAhead; ++b)
-        if (from + b < to) fill(from + b, b);
+        if (b < n) fill(b, b);
     int buffer = 0;
     Frag r[T::RT], c[2];
     // the first fragments of a stage that has landed
     const auto begin = [&]() {
-        const char *p = lds + buffer * T::STAGE;
+        const char *p = own + buffer * T::STAGE;
         place.load(c[0], p + (T::ROWS + wc * T::CT * 16) * kLine, 0);
 #pragma unroll
         for (int i = 0; i < T::RT; ++i) place.load(r[i], p + wr * T::RT * 16 * kLine, i);
@@ -229,16 +241,18 @@ __device__ __forceinline__ void multiply(const Operand &rows, const Operand &col
     };
 #pragma unroll
     for (int i = 0; i < T::RT; ++i) sum[i] = Acc{0, 0, 0, 0};
-    if (from + kAhead <= to) landed<(kAhead - 1) * T::LOADS>();
-    else landed<0>();
-    if (from + kAhead < to) fill(from + kAhead, kAhead);
-    begin();
-    for (int s = from; s < to; ++s) {
-        const char *p = lds + buffer * T::STAGE + (T::ROWS + wc * T::CT * 16) * kLine;
+    await(0);
+    if (kAhead < n) fill(kAhead, kAhead);
+    if (T::TURNS == 1 || n > 0) begin();
+    for (int k = 0; k < rounds; ++k) {
+        const bool active = T::TURNS == 1 || k < n;
+        if (active) {
+            const char *p = own + buffer * T::STAGE + (T::ROWS + wc * T::CT * 16) * kLine;
 #pragma unroll
-        for (int j = 0; j + 1 < T::CT; ++j) {
-            place.load(c[(j + 1) & 1], p, j + 1);
-            multiply_by(r, c[j & 1], acc[j], acc[j == 0 ? T::CT - 1 : j - 1]);
+            for (int j = 0; j + 1 < T::CT; ++j) {
+                place.load(c[(j + 1) & 1], p, j + 1);
+                multiply_by(r, c[j & 1], acc[j], acc[j == 0 ? T::CT - 1 : j - 1]);
+            }
         }
         // own reads are done (told to the compiler: it would wait for the next stage's before the products below)
         __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0)
@@ -247,20 +261,62 @@ __device__ __forceinline__ void multiply(const Operand &rows, const Operand &col
         Frag held[T::RT];
 #pragma unroll
         for (int i = 0; i < T::RT; ++i) held[i] = r[i];
-        if (s + 1 < to) {
-            // (near the end fewer loads are under way: then all of them are awaited)
-            if (s + 1 + kAhead <= to) landed<(kAhead - 1) * T::LOADS>();
-            else landed<0>();
+        if (k + 1 < rounds) {
+            await(k + 1);
             const int done = buffer;
             buffer = buffer == kAhead ? 0 : buffer + 1;
-            if (s + 1 + kAhead < to) fill(s + 1 + kAhead, done);
-            begin();
+            if (k + 1 + kAhead < n) fill(k + 1 + kAhead, done);
+            if (T::TURNS == 1 || k + 1 < n) begin();
         }
-        multiply_by(held, last, acc[T::CT - 1], acc[T::CT - 2]);
+        if (active) multiply_by(held, last, acc[T::CT - 1], acc[T::CT - 2]);
     }
     if (Product::kBySum)
 #pragma unroll
         for (int i = 0; i < T::RT; ++i) acc[T::CT - 1][i] += sum[i];
+    __syncthreads();
+    if (T::TURNS == 1) return true;
+    Acc *shared = reinterpret_cast<Acc *>(lds) + wave * 64 + lane;
+    for (int t = 1; t < T::TURNS; ++t) {
+        if (turn == t)
+#pragma unroll
+            for (int j = 0; j < T::CT; ++j)
+#pragma unroll
+                for (int i = 0; i < T::RT; ++i) shared[(j * T::RT + i) * 64 * T::WAVES] = acc[j][i];
+        __syncthreads();
+        if (turn == 0)
+#pragma unroll
+            for (int j = 0; j < T::CT; ++j)
+#pragma unroll
+                for (int i = 0; i < T::RT; ++i) acc[j][i] += shared[(j * T::RT + i) * 64 * T::WAVES];
+        __syncthreads();
+    }
+    return turn == 0;
+}
+
+// The order of tiles: neighbours in the order, which run on one die, share rows and columns of their operands.
+// Rows are taken eight at a time, column by column.
+__host__ __device__ __forceinline__ void grouped_tile(int t, int down, int across, int *i, int *j)
+{
+    constexpr int kRows = 8;
+    const int group = t / (kRows * across), rest = t - group * kRows * across;
+    const int height = down - group * kRows < kRows ? down - group * kRows : kRows;
+    *j = rest / height;
+    *i = group * kRows + rest - *j * height;
+}
+// The upper triangle of n x n tiles, in blocks of 4 x 4, column of blocks by column of blocks
+__host__ __device__ __forceinline__ void upper_tile(int t, int n, int *i, int *j)
+{
+    int block = 0;
+    while (8 * (block + 1) * (block + 1) + 2 * (block + 1) <= t) ++block;   // (tiles in the columns of blocks before it: 8 b^2 + 2 b)
+    const int rest = t - 8 * block * block - 2 * block, width = n - 4 * block < 4 ? n - 4 * block : 4;
+    if (rest < 16 * block * width / 4) {
+        const int above = rest / (4 * width), in = rest - above * 4 * width;
+        *i = 4 * above + (in & 3), *j = 4 * block + (in >> 2);
+    } else {
+        int in = rest - 4 * width * block, c = 0;
+        while (in > c) in -= ++c;
+        *i = 4 * block + in, *j = 4 * block + c;
+    }
 }
 
 // A launch of W workgroups on `tiles` products of `stages` stages each.  Each takes whole tiles round by round; the
@@ -329,11 +385,11 @@ __device__ __forceinline__ void for_work(const WorkSplit &w, int id, F &&f)
 template <class T, class Acc>
 __device__ __forceinline__ void store_part(Acc *parts, int slot, const Acc (&acc)[T::CT][T::RT])
 {
-    Acc *to = parts + (int64_t)slot * T::GROUPS * T::THREADS + threadIdx.x;
+    Acc *to = parts + (int64_t)slot * T::GROUPS * 64 * T::WAVES + threadIdx.x;
 #pragma unroll
     for (int j = 0; j < T::CT; ++j)
 #pragma unroll
-        for (int i = 0; i < T::RT; ++i) to[(j * T::RT + i) * T::THREADS] = acc[j][i];
+        for (int i = 0; i < T::RT; ++i) to[(j * T::RT + i) * 64 * T::WAVES] = acc[j][i];
 }
 
 // A wave's share of the parts of tile `tile` (counted from the first that is cut), summed in a fixed order by the
@@ -351,11 +407,11 @@ __device__ __forceinline__ bool join_parts(const WorkSplit &w, int tile, int wav
 #pragma unroll
         for (int i = 0; i < T::RT; ++i) acc[j][i] = Acc{0, 0, 0, 0};
     for (int k = from + joiner; k <= to; k += JOINERS) {
-        const Acc *at = parts + (int64_t)(2 * k + (w.begin(k) <= first)) * T::GROUPS * T::THREADS + wave * 64 + lane;
+        const Acc *at = parts + (int64_t)(2 * k + (w.begin(k) <= first)) * T::GROUPS * 64 * T::WAVES + wave * 64 + lane;
 #pragma unroll
         for (int j = 0; j < T::CT; ++j)
 #pragma unroll
-            for (int i = 0; i < T::RT; ++i) acc[j][i] += at[(j * T::RT + i) * T::THREADS];
+            for (int i = 0; i < T::RT; ++i) acc[j][i] += at[(j * T::RT + i) * 64 * T::WAVES];
     }
     if (JOINERS == 1) return true;
     if (joiner > 0)
