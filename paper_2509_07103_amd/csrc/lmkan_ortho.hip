@@ -341,7 +341,7 @@ __device__ __forceinline__ void finish_tile(const ProductArgs &a, const Place &w
     });
 }
 
-template <class T, int FINISH>
+template <class T, int FINISH, bool ALONE>
 __global__ __launch_bounds__(T::THREADS) void product_kernel(ProductArgs a)
 {
     extern __shared__ __align__(16) char lds[];
@@ -354,13 +354,12 @@ __global__ __launch_bounds__(T::THREADS) void product_kernel(ProductArgs a)
         floatx4 acc[T::CT][T::RT];
         // (a workgroup that finishes a tile goes before one that multiplies: 1 to 3 %)
         __builtin_amdgcn_s_setprio(0);
-        const bool holds = multiply<T, PairProduct>(operand(p.rows, w.ti * T::ROWS), operand(p.cols, w.tj * T::COLS), from, to, lds, acc);
+        if constexpr (ALONE) multiply_alone<T, PairProduct>(operand(p.rows, w.ti * T::ROWS), operand(p.cols, w.tj * T::COLS), from, to, lds, acc);
+        else multiply<T, PairProduct>(operand(p.rows, w.ti * T::ROWS), operand(p.cols, w.tj * T::COLS), from, to, lds, acc);
         __builtin_amdgcn_s_setprio(2);
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        if (holds) {
-            if (slot < 0) finish_tile<T, FINISH>(a, w, acc, lds + wave * kWaveScratch, wave);
-            else store_part<T>(a.parts, slot, acc);
-        }
+        if (slot < 0) finish_tile<T, FINISH>(a, w, acc, lds + wave * kWaveScratch, wave);
+        else store_part<T>(a.parts, slot, acc);
         __syncthreads();
     });
 }
@@ -390,7 +389,7 @@ __global__ __launch_bounds__(256) void unscaled_kernel(MatrixShape s, UpdateArgs
 }
 
 typedef TileShape<64, 64, 2, 2, 4> Tile64;
-typedef TileShape<64, 64, 2, 2, 4, 2> Tile64Deep;
+typedef TileShape<64, 64, 2, 2, 2> Tile64Alone;
 typedef TileShape<128, 128, 2, 2, 2> Tile128;
 typedef TileShape<256, 256, 4, 2, 2> Tile256;
 
@@ -403,7 +402,7 @@ int64_t tiles_of(const Product &p, int tile)
     return p.symmetric ? down * (down + 1) / 2 : down * across;
 }
 
-template <class T, int FINISH>
+template <class T, int FINISH, bool ALONE = false>
 void launch_product_with(ProductArgs &a, hipStream_t stream)
 {
     const Product &p = a.p[0];
@@ -411,12 +410,13 @@ void launch_product_with(ProductArgs &a, hipStream_t stream)
     a.tiles_across = (p.cols.rows + T::COLS - 1) / T::COLS;
     a.tiles = (int)tiles_of(p, T::ROWS);
     const int64_t tiles = (int64_t)a.tiles * a.matrices * a.problems;
-    const int workers = kUnits * (T::LDS <= 80 * 1024 ? 2 : 1);
+    constexpr int kLds = ALONE ? Alone<T>::LDS : T::LDS;
+    const int workers = kUnits * (kLds <= 80 * 1024 ? 2 : 1);
     // (joining takes 6 us, a stage of the smallest tile 0.25; 20 us and 1.8 for the largest)
     a.work = WorkSplit::of((int)tiles, panels(p.rows.depth), workers, T::ROWS == 64 ? 24 : T::ROWS == 128 ? 20 : 12);
     const WorkSplit &w = a.work;
-    if (T::LDS > 65536) allow_large_lds(reinterpret_cast<const void *>(product_kernel<T, FINISH>), T::LDS);
-    product_kernel<T, FINISH><<<w.workers, T::THREADS, T::LDS, stream>>>(a);
+    if (kLds > 65536) allow_large_lds(reinterpret_cast<const void *>(product_kernel<T, FINISH, ALONE>), kLds);
+    product_kernel<T, FINISH, ALONE><<<w.workers, T::THREADS, kLds, stream>>>(a);
     if (w.cut()) join_kernel<T, FINISH><<<w.left() * T::WAVES, 64 * joiners<T>(), 0, stream>>>(a);
 }
 
@@ -431,7 +431,7 @@ void launch_product(ProductArgs &a, hipStream_t stream)
     if (shorter > 512 && tiles_of(a.p[0], 256) * n >= kUnits / 2) launch_product_with<Tile256, FINISH>(a, stream);
     else if (shorter > 256 && tiles_of(a.p[0], 128) * n >= 2 * kUnits) launch_product_with<Tile128, FINISH>(a, stream);
     else if (tiles_of(a.p[0], 64) * n > kUnits) launch_product_with<Tile64, FINISH>(a, stream);
-    else launch_product_with<Tile64Deep, FINISH>(a, stream);
+    else launch_product_with<Tile64Alone, FINISH, true>(a, stream);
 }
 
 // Matrices that share the workspace at a time: the batch in equal parts of at most 256 M elements (parts of 32 M and

@@ -63,26 +63,24 @@ __device__ __forceinline__ unsigned lds_offset(const void *p)
     return (unsigned)(size_t)(__attribute__((address_space(3))) const void *)p;
 }
 
-// All but the wave's last `LEFT` loads have landed and its own reads are done; then all waves' have
-template <int LEFT>
+// All but the wave's last `LEFT` loads have landed and its own reads are done; with several waves, then all waves' have
+template <int LEFT, int WAVES>
 __device__ __forceinline__ void landed()
 {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LEFT) : "memory");
-    __builtin_amdgcn_s_barrier();
+    if (WAVES > 1) __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 }
 
-// Tile shape: ROWS x COLS outputs of one workgroup, WR x WC waves, stages in BUFFERS buffers.  TURNS groups of such
-// waves take stages in turn (each its own buffers) and add up at the end: for tiles that have a compute unit to
-// themselves, where one wave a SIMD would wait for its own reads.
-template <int ROWS_, int COLS_, int WR_, int WC_, int BUFFERS_, int TURNS_ = 1>
+// Tile shape: ROWS x COLS outputs of one workgroup, WR x WC waves, stages in BUFFERS buffers
+template <int ROWS_, int COLS_, int WR_, int WC_, int BUFFERS_>
 struct TileShape {
-    static constexpr int ROWS = ROWS_, COLS = COLS_, WR = WR_, WC = WC_, BUFFERS = BUFFERS_, TURNS = TURNS_;
-    static constexpr int WAVES = WR * WC, THREADS = 64 * WAVES * TURNS;
+    static constexpr int ROWS = ROWS_, COLS = COLS_, WR = WR_, WC = WC_, BUFFERS = BUFFERS_;
+    static constexpr int WAVES = WR * WC, THREADS = 64 * WAVES;
     static constexpr int RT = ROWS / WR / 16, CT = COLS / WC / 16;   // 16 x 16 tiles of a wave
     static constexpr int STAGE = (ROWS + COLS) * kLine;              // bytes of a stage
     static constexpr int LOADS = (ROWS + COLS) / 8 / WAVES;          // loads of a wave a stage
-    static constexpr int LDS = BUFFERS * TURNS * STAGE;
+    static constexpr int LDS = BUFFERS * STAGE;
     static constexpr int GROUPS = RT * CT;                           // groups of four outputs of a lane
 };
 
@@ -175,36 +173,34 @@ struct CodeProduct {
     static constexpr bool kBySum = false;
 };
 
-// The main loop: stages [from, to) of both operands, from < to.  While one buffer is multiplied the others fill; the
-// last columns of a stage are multiplied after the barrier that ends it, while the first fragments of the next are
-// on their way.  Returns whether the wave holds the sums (the first group's do), with all of LDS free.
+// The main loop: stages from, from + step .. below `to` of both operands, by wave `wave` of T's.  While one buffer is
+// multiplied the others fill; the last columns of a stage are multiplied after the barrier that ends it, while the first
+// fragments of the next are on their way.
 template <class T, class Product>
-__device__ __forceinline__ bool multiply(const Operand &rows, const Operand &cols, int from, int to, char *lds,
-                                         typename Product::Acc (&acc)[T::CT][T::RT])
+__device__ __forceinline__ void multiply_stages(const Operand &rows, const Operand &cols, int from, int to, int step, char *lds, int wave,
+                                                typename Product::Acc (&acc)[T::CT][T::RT])
 {
     typedef typename Product::Acc Acc;
     typedef Fragment<typename Product::Element> Frag;
     constexpr int kAhead = T::BUFFERS - 1;
-    const int all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const int turn = T::TURNS == 1 ? 0 : all / T::WAVES, wave = T::TURNS == 1 ? all : all % T::WAVES;
-    char *own = lds + turn * T::BUFFERS * T::STAGE;
-    const unsigned at = lds_offset(own);
+    const int lane = threadIdx.x & 63;
+    const unsigned at = lds_offset(lds);
     const int wr = wave / T::WC, wc = wave % T::WC;
-    const int rounds = (to - from + T::TURNS - 1) / T::TURNS;                        // of all groups
-    const int n = T::TURNS == 1 ? rounds : (to - from - turn + T::TURNS - 1) / T::TURNS;   // stages of this one
+    const int n = (to - from + step - 1) / step;
 #pragma unroll
     for (int j = 0; j < T::CT; ++j)
 #pragma unroll
         for (int i = 0; i < T::RT; ++i) acc[j][i] = Acc{0, 0, 0, 0};
+    if (n <= 0) return;
     const auto fill = [&](int k, int buffer) {
-        const int stage = from + k * T::TURNS + turn;
+        const int stage = from + k * step;
         stage_operand<T::ROWS, T::WAVES>(rows, stage, at + buffer * T::STAGE, wave, lane);
         stage_operand<T::COLS, T::WAVES>(cols, stage, at + buffer * T::STAGE + T::ROWS * kLine, wave, lane);
     };
     // stage k has landed (near the end fewer loads are under way: then all of them are awaited)
     const auto await = [&](int k) {
-        if (k + kAhead <= n) landed<(kAhead - 1) * T::LOADS>();
-        else landed<0>();
+        if (k + kAhead <= n) landed<(kAhead - 1) * T::LOADS, T::WAVES>();
+        else landed<0, T::WAVES>();
     };
     const FragmentPlace place(lane);
     for (int b = 0; b < kAhead; ++b)
@@ -213,7 +209,7 @@ __device__ __forceinline__ bool multiply(const Operand &rows, const Operand &col
     Frag r[T::RT], c[2];
     // the first fragments of a stage that has landed
     const auto begin = [&]() {
-        const char *p = own + buffer * T::STAGE;
+        const char *p = lds + buffer * T::STAGE;
         place.load(c[0], p + (T::ROWS + wc * T::CT * 16) * kLine, 0);
 #pragma unroll
         for (int i = 0; i < T::RT; ++i) place.load(r[i], p + wr * T::RT * 16 * kLine, i);
@@ -243,16 +239,13 @@ __device__ __forceinline__ bool multiply(const Operand &rows, const Operand &col
     for (int i = 0; i < T::RT; ++i) sum[i] = Acc{0, 0, 0, 0};
     await(0);
     if (kAhead < n) fill(kAhead, kAhead);
-    if (T::TURNS == 1 || n > 0) begin();
-    for (int k = 0; k < rounds; ++k) {
-        const bool active = T::TURNS == 1 || k < n;
-        if (active) {
-            const char *p = own + buffer * T::STAGE + (T::ROWS + wc * T::CT * 16) * kLine;
+    begin();
+    for (int k = 0; k < n; ++k) {
+        const char *p = lds + buffer * T::STAGE + (T::ROWS + wc * T::CT * 16) * kLine;
 #pragma unroll
-            for (int j = 0; j + 1 < T::CT; ++j) {
-                place.load(c[(j + 1) & 1], p, j + 1);
-                multiply_by(r, c[j & 1], acc[j], acc[j == 0 ? T::CT - 1 : j - 1]);
-            }
+        for (int j = 0; j + 1 < T::CT; ++j) {
+            place.load(c[(j + 1) & 1], p, j + 1);
+            multiply_by(r, c[j & 1], acc[j], acc[j == 0 ? T::CT - 1 : j - 1]);
         }
         // own reads are done (told to the compiler: it would wait for the next stage's before the products below)
         __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0)
@@ -261,36 +254,67 @@ __device__ __forceinline__ bool multiply(const Operand &rows, const Operand &col
         Frag held[T::RT];
 #pragma unroll
         for (int i = 0; i < T::RT; ++i) held[i] = r[i];
-        if (k + 1 < rounds) {
+        if (k + 1 < n) {
             await(k + 1);
             const int done = buffer;
             buffer = buffer == kAhead ? 0 : buffer + 1;
             if (k + 1 + kAhead < n) fill(k + 1 + kAhead, done);
-            if (T::TURNS == 1 || k + 1 < n) begin();
+            begin();
         }
-        if (active) multiply_by(held, last, acc[T::CT - 1], acc[T::CT - 2]);
+        multiply_by(held, last, acc[T::CT - 1], acc[T::CT - 2]);
     }
     if (Product::kBySum)
 #pragma unroll
         for (int i = 0; i < T::RT; ++i) acc[T::CT - 1][i] += sum[i];
+}
+
+// Stages [from, to), from < to, by all waves of the workgroup together; LDS is free when it returns
+template <class T, class Product>
+__device__ __forceinline__ void multiply(const Operand &rows, const Operand &cols, int from, int to, char *lds,
+                                         typename Product::Acc (&acc)[T::CT][T::RT])
+{
+    multiply_stages<T, Product>(rows, cols, from, to, 1, lds, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), acc);
     __syncthreads();
-    if (T::TURNS == 1) return true;
-    Acc *shared = reinterpret_cast<Acc *>(lds) + wave * 64 + lane;
-    for (int t = 1; t < T::TURNS; ++t) {
-        if (turn == t)
+}
+
+// The same for a tile that has a compute unit to itself: each wave takes every WAVES-th stage of the whole tile, in
+// buffers of its own and without a barrier, and the sums are added up at the end, a quarter of the tile to a wave.
+// Half as much is read from LDS per product as where the waves share the tile.
+template <class T>
+struct Alone {
+    typedef TileShape<T::ROWS, T::COLS, 1, 1, T::BUFFERS> Whole;
+    static constexpr int LDS = T::WAVES * Whole::LDS;
+};
+template <class T, class Product>
+__device__ __forceinline__ void multiply_alone(const Operand &rows, const Operand &cols, int from, int to, char *lds,
+                                               typename Product::Acc (&acc)[T::CT][T::RT])
+{
+    typedef typename Product::Acc Acc;
+    typedef typename Alone<T>::Whole W;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    Acc own[W::CT][W::RT];
+    char *place = lds + wave * W::LDS;
+    multiply_stages<W, Product>(rows, cols, from + wave, to, T::WAVES, place, 0, own);
+    static_assert(W::LDS >= W::GROUPS * 64 * (int)sizeof(Acc), "the sums fit the buffers");
+    Acc *sums = reinterpret_cast<Acc *>(place) + lane;
 #pragma unroll
-            for (int j = 0; j < T::CT; ++j)
+    for (int j = 0; j < W::CT; ++j)
 #pragma unroll
-                for (int i = 0; i < T::RT; ++i) shared[(j * T::RT + i) * 64 * T::WAVES] = acc[j][i];
-        __syncthreads();
-        if (turn == 0)
+        for (int i = 0; i < W::RT; ++i) sums[(j * W::RT + i) * 64] = own[j][i];
+    __syncthreads();
+    const int wr = wave / T::WC, wc = wave % T::WC;
 #pragma unroll
-            for (int j = 0; j < T::CT; ++j)
+    for (int j = 0; j < T::CT; ++j)
 #pragma unroll
-                for (int i = 0; i < T::RT; ++i) acc[j][i] += shared[(j * T::RT + i) * 64 * T::WAVES];
-        __syncthreads();
+        for (int i = 0; i < T::RT; ++i) acc[j][i] = Acc{0, 0, 0, 0};
+    for (int w = 0; w < T::WAVES; ++w) {
+        const Acc *from_wave = reinterpret_cast<const Acc *>(lds + w * W::LDS) + lane;
+#pragma unroll
+        for (int j = 0; j < T::CT; ++j)
+#pragma unroll
+            for (int i = 0; i < T::RT; ++i) acc[j][i] += from_wave[((wc * T::CT + j) * W::RT + wr * T::RT + i) * 64];
     }
-    return turn == 0;
+    __syncthreads();
 }
 
 // The order of tiles: neighbours in the order, which run on one die, share rows and columns of their operands.
