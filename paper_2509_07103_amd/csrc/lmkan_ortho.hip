@@ -236,6 +236,28 @@ __device__ __forceinline__ const Product &product_of(const ProductArgs &a, const
     return FINISH == kKeep && w.problem ? a.p[1] : a.p[0];
 }
 
+// A wave's 32 x 32 tile at (row, col), values as in for_wave_tiles, to pairs; what lies beyond n_rows x n_cols is zero
+__device__ __forceinline__ void to_pairs(const floatx4 (&v)[4], float scale, int row, int col, int n_rows, int n_cols, int lane, uint2 (&hi)[4], uint2 (&lo)[4])
+{
+    const bool inside = row + 32 <= n_rows && col + 32 <= n_cols;
+    const int r = lane & 15, q = lane >> 4;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        floatx4 f = v[g] * scale;
+        if (!inside) {
+            const int i = row + 16 * (g >> 1) + r, j = col + 16 * (g & 1) + 4 * q;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) f[e] = i < n_rows && j + e < n_cols ? f[e] : 0.0f;
+        }
+        half4 vh, vl;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) vh[e] = (_Float16)f[e];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) vl[e] = (_Float16)__builtin_fmaf((float)vh[e], -1.0f, f[e]);
+        hi[g] = __builtin_bit_cast(uint2, vh), lo[g] = __builtin_bit_cast(uint2, vl);
+    }
+}
+
 // `scratch`: kWaveScratch bytes of LDS of the wave's own
 template <class T, int FINISH>
 __device__ __forceinline__ void finish_tile(const ProductArgs &a, const Place &w, const floatx4 (&acc)[T::CT][T::RT], char *scratch, int wave)
@@ -311,30 +333,19 @@ __device__ __forceinline__ void finish_tile(const ProductArgs &a, const Place &w
         const bool direct = row < n_rows && col < panels(n_cols) * kPanel;
         const bool turned = p.mirror.base && !(p.symmetric && w.ti == w.tj) && col < n_cols && row < panels(n_rows) * kPanel;
         if (!direct && !turned) return;
-        const bool inside = row + 32 <= n_rows && col + 32 <= n_cols;
-        const float scale = FINISH == kPoly ? p.out.scale : p.out.scale * unit;
         uint2 hi[4], lo[4];
+        if (FINISH == kPoly) {
+            floatx4 f[4];
+            const float s = p.b * p.gram.inverse, c = p.c * unit;
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const int i = row + 16 * (g >> 1) + r, j = col + 16 * (g & 1) + 4 * q;
-            floatx4 f = v[g];
-            if (FINISH == kPoly) {
-                const half4 gh = held.hi[g], gl = held.lo[g];
-                const float s = p.b * p.gram.inverse, c = p.c * unit;
+            for (int g = 0; g < 4; ++g) {
+                const int i = row + 16 * (g >> 1) + r, j = col + 16 * (g & 1) + 4 * q;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) f[e] = c * f[e] + s * ((float)gh[e] + (float)gl[e]) + (i == j + e ? p.a : 0.0f);
+                for (int e = 0; e < 4; ++e) f[g][e] = c * v[g][e] + s * ((float)held.hi[g][e] + (float)held.lo[g][e]) + (i == j + e ? p.a : 0.0f);
             }
-            f *= scale;
-            if (!inside)
-                // what lies beyond the matrix in a panel is zero
-#pragma unroll
-                for (int e = 0; e < 4; ++e) f[e] = i < n_rows && j + e < n_cols ? f[e] : 0.0f;
-            half4 vh, vl;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) vh[e] = (_Float16)f[e];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) vl[e] = (_Float16)__builtin_fmaf((float)vh[e], -1.0f, f[e]);
-            hi[g] = __builtin_bit_cast(uint2, vh), lo[g] = __builtin_bit_cast(uint2, vl);
+            to_pairs(f, p.out.scale, row, col, n_rows, n_cols, lane, hi, lo);
+        } else {
+            to_pairs(v, p.out.scale * unit, row, col, n_rows, n_cols, lane, hi, lo);
         }
         if (direct) store_pairs(p.out, p.out.base + w.matrix * p.out.stride, row, col, hi, lo, scratch, lane);
         if (turned) store_turned(p.mirror, p.mirror.base + w.matrix * p.mirror.stride, row, col, hi, lo, lane);
@@ -373,6 +384,153 @@ __global__ __launch_bounds__(64 * joiners<T>()) void join_kernel(ProductArgs a)
     floatx4 acc[T::CT][T::RT];
     if (!join_parts<T, joiners<T>()>(a.work, tile, wave, a.parts, reinterpret_cast<floatx4 *>(lds + kWaveScratch), acc)) return;
     finish_tile<T, FINISH>(a, place_of(a, a.work.whole + tile), acc, lds, wave);
+}
+
+// The steps on one Gram matrix of up to 128 x 128 in one launch: a workgroup per matrix, A and B in LDS, P in memory
+// (three matrices of pairs do not fit).  A wave has one 32 x 32 tile of the upper triangle; all read, then all write,
+// so that a product may take the place of a factor.  A product takes about 2 us, a launch for it 6.
+constexpr int kSide = 128, kSideTiles = kSide / 32, kChainWaves = kSideTiles * (kSideTiles + 1) / 2;
+constexpr int kSideBytes = kSide / kPanel * kSide * kLine;
+
+struct ChainArgs {
+    PairMatrix gram;           // scale of the first
+    PairMatrix p[2];           // P after every step by turns, the first in p[0] (scale, inverse: as below)
+    int steps;
+    float abc[3 * kStepsAtOnce];
+    float gram_scale[kStepsAtOnce], step_scale[kStepsAtOnce], w_scale[kStepsAtOnce], p_scale[kStepsAtOnce];
+};
+
+__device__ __forceinline__ void lds_store_tile(char *lds, int row, int col, const uint2 (&hi)[4], const uint2 (&lo)[4], bool turned, int lane)
+{
+    const int r = lane & 15, q = lane >> 4, k = r >> 2;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        const int line = row + 16 * (g >> 1) + r, chunk = 2 * (g & 1) + (q >> 1);
+        char *to = lds + (col / kPanel * kSide + line) * kLine + (q & 1) * 8;
+        *reinterpret_cast<uint2 *>(to + slot_of(line, chunk) * 16) = hi[g];
+        *reinterpret_cast<uint2 *>(to + slot_of(line, 4 + chunk) * 16) = lo[g];
+        if (turned) {
+            const int other = col + 16 * (g & 1) + 4 * q + (lane & 3), piece = 2 * (g >> 1) + (k >> 1);
+            char *back = lds + (row / kPanel * kSide + other) * kLine + (k & 1) * 8;
+            *reinterpret_cast<uint2 *>(back + slot_of(other, piece) * 16) = turn_quad(hi[g], lane);
+            *reinterpret_cast<uint2 *>(back + slot_of(other, 4 + piece) * 16) = turn_quad(lo[g], lane);
+        }
+    }
+}
+// the same to memory, lines of `d`
+__device__ __forceinline__ void memory_store_tile(const PairMatrix &d, char *to, int row, int col, const uint2 (&hi)[4], const uint2 (&lo)[4], bool turned, int lane)
+{
+    const int r = lane & 15, q = lane >> 4;
+    if (col < panels(d.depth) * kPanel)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int line = row + 16 * (g >> 1) + r, chunk = 2 * (g & 1) + (q >> 1);
+            if (line < d.rows) {
+                *reinterpret_cast<uint2 *>(to + pair_at(d.rows, line, col / kPanel, chunk) + (q & 1) * 8) = hi[g];
+                *reinterpret_cast<uint2 *>(to + pair_at(d.rows, line, col / kPanel, 4 + chunk) + (q & 1) * 8) = lo[g];
+            }
+        }
+    if (turned && row < panels(d.depth) * kPanel) store_turned(d, to, row, col, hi, lo, lane);
+}
+
+__global__ __launch_bounds__(64 * kChainWaves) void chain_kernel(ChainArgs a)
+{
+    extern __shared__ __align__(16) char lds[];
+    char *gram = lds, *step = lds + kSideBytes;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, q = lane >> 4;
+    const int m = a.gram.rows, lines = panels(m);
+    int ti, tj;
+    upper_tile(wave, kSideTiles, &ti, &tj);
+    const int row = uniform(ti) * 32, col = uniform(tj) * 32;
+    const bool there = row < m && col < lines * kPanel, turned = row != col;
+    const char *from = a.gram.base + (int64_t)blockIdx.x * a.gram.stride;
+    for (int e = threadIdx.x; e < 2 * kSideBytes / 16; e += 64 * kChainWaves) {
+        const int line = e / 8, at = line % kSide, panel = line / kSide;
+        const bool in = at < m && panel < lines;
+        *reinterpret_cast<uint4 *>(lds + e * 16) = in ? *reinterpret_cast<const uint4 *>(from + ((int64_t)panel * m + at) * kLine + e % 8 * 16) : make_uint4(0, 0, 0, 0);
+    }
+    __syncthreads();
+    const FragmentPlace place(lane);
+    typedef Fragment<half8> Frag;
+    const auto read = [&](const char *matrix, int panel, int first, Frag (&f)[2]) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) place.load(f[i], matrix + (panel * kSide + first) * kLine, i);
+    };
+    const auto read_memory = [&](const char *matrix, int panel, int first, Frag (&f)[2]) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int at = min(first + 16 * i + r, m - 1);
+            f[i].half[0] = *reinterpret_cast<const half8 *>(matrix + pair_at(m, at, panel, q));
+            f[i].half[1] = *reinterpret_cast<const half8 *>(matrix + pair_at(m, at, panel, 4 + q));
+        }
+    };
+    // the wave's tile of L R, R in LDS or in memory; v[2 i + j] as in for_wave_tiles
+    floatx4 v[4];
+    const auto product = [&](const char *l, auto &&read_right, const char *right) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) v[g] = floatx4{0, 0, 0, 0};
+        if (!there) return;
+        for (int k = 0; k < lines; ++k) {
+            Frag rows[2], cols[2];
+            read(l, k, row, rows);
+            read_right(right, k, col, cols);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                floatx4 sum[2];
+                PairProduct::line(rows, cols[j], sum);
+                v[j] += sum[0], v[2 + j] += sum[1];
+            }
+        }
+    };
+    uint2 hi[4], lo[4];
+    for (int k = 0; k < a.steps; ++k) {
+        const float c0 = a.abc[3 * k], c1 = a.abc[3 * k + 1], c2 = a.abc[3 * k + 2];
+        const float in_gram = 1.0f / a.gram_scale[k], in_step = 1.0f / a.step_scale[k];
+        char *p_now = a.p[k & 1].base + (int64_t)blockIdx.x * a.p[k & 1].stride;
+        product(gram, read, gram);
+        if (there) {
+            const float s = c1 * in_gram, c = c2 * in_gram * in_gram;
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int i = row + 16 * (g >> 1) + r, chunk = 2 * (g & 1) + (q >> 1), j = col + 16 * (g & 1) + 4 * q;
+                const char *at = gram + (col / kPanel * kSide + i) * kLine + (q & 1) * 8;
+                const half4 h = *reinterpret_cast<const half4 *>(at + slot_of(i, chunk) * 16), l = *reinterpret_cast<const half4 *>(at + slot_of(i, 4 + chunk) * 16);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[g][e] = c * v[g][e] + s * ((float)h[e] + (float)l[e]) + (i == j + e ? c0 : 0.0f);
+            }
+            // (B is not read by anybody at this point)
+            to_pairs(v, a.step_scale[k], row, col, m, m, lane, hi, lo);
+            lds_store_tile(step, row, col, hi, lo, turned, lane);
+            if (k == 0) memory_store_tile(a.p[0], p_now, row, col, hi, lo, turned, lane);
+        }
+        __syncthreads();
+        if (k > 0) {
+            // P in memory was written by this workgroup, before a barrier, to lines that it had not read
+            const char *before = a.p[(k - 1) & 1].base + (int64_t)blockIdx.x * a.p[0].stride;
+            product(step, read_memory, before);
+            if (there) {
+                to_pairs(v, in_step / a.p_scale[k - 1] * a.p_scale[k], row, col, m, m, lane, hi, lo);
+                memory_store_tile(a.p[k & 1], p_now, row, col, hi, lo, turned, lane);
+            }
+        }
+        if (k + 1 < a.steps) {
+            product(step, read, gram);
+            __syncthreads();
+            if (there) {
+                to_pairs(v, in_step * in_gram * a.w_scale[k], row, col, m, m, lane, hi, lo);
+                lds_store_tile(gram, row, col, hi, lo, turned, lane);
+            }
+            __syncthreads();
+            product(gram, read, step);
+            __syncthreads();
+            if (there) {
+                to_pairs(v, in_step / a.w_scale[k] * a.gram_scale[k + 1], row, col, m, m, lane, hi, lo);
+                lds_store_tile(gram, row, col, hi, lo, turned, lane);
+            }
+            __threadfence_block();
+            __syncthreads();
+        }
+    }
 }
 
 // No steps: X_0 itself is the result
@@ -560,6 +718,25 @@ void launch_ortho(const MatrixShape &s, int steps, const float *schedule, const 
             one(Product{x, x, gram, gram, none, 0, 0, 0, true});
             launch_product<kKeep>(args, stream);
             double factor = 1.0;
+            if (m <= kSide) {
+                ChainArgs chain = {};
+                chain.gram = gram;
+                chain.steps = end - k;
+                for (int i = 0; i < chain.steps; ++i) {
+                    const double now = bounds.singular[k + i], most_now = bounds.factor[k + i];
+                    factor *= most_now;
+                    for (int e = 0; e < 3; ++e) chain.abc[3 * i + e] = schedule[3 * (k + i) + e];
+                    chain.gram_scale[i] = scale_for(now * now);
+                    chain.step_scale[i] = scale_for(most_now);
+                    chain.w_scale[i] = scale_for(most_now * now * now);
+                    chain.p_scale[i] = scale_for(factor);
+                }
+                chain.p[0] = pairs(l.p[0], m, m, factor), chain.p[1] = pairs(l.p[1], m, m, factor);
+                allow_large_lds(reinterpret_cast<const void *>(chain_kernel), 2 * kSideBytes);
+                chain_kernel<<<(unsigned)count, 64 * kChainWaves, 2 * kSideBytes, stream>>>(chain);
+                so_far = chain.p[(chain.steps - 1) & 1];
+                k = end;
+            }
             for (const int begin = k; k < end; ++k) {
                 const float *abc = schedule + 3 * k;
                 const double now = bounds.singular[k], next = bounds.singular[k + 1];
