@@ -40,10 +40,12 @@ struct SmallArgs {
     UpdateArgs u;
     int steps, from, to;                   // steps [from, to) of the schedule
     float schedule[3 * LMKAN_MAX_ORTHO_STEPS];
+    int at_once;                           // steps on one Gram matrix
     int columns;                           // of X in LDS at a time, a multiple of 16
     Divide by_columns, by_m, by_n;
     int parts;                             // workgroups that share a matrix
     float *gram;                           // [matrices][parts][M][M], upper tiles
+    double *sum;                           // [matrices][M][M]: their sums, where they are many
     unsigned *scaled;                      // [matrices][parts]: whether kDown was applied
     float *poly;                           // [matrices][M][M]
     float *x;                              // [matrices][m][n]: X after a polynomial
@@ -299,7 +301,7 @@ __global__ __launch_bounds__(S::THREADS) void whole_kernel(SmallArgs a)
     const bool down = __syncthreads_or(large);
     if (down) scale_columns<S>(x, pitch, columns, kDown);
     for (int k = 0; k < a.steps;) {
-        const int end = k + kStepsAtOnce < a.steps ? k + kStepsAtOnce : a.steps;
+        const int end = k + a.at_once < a.steps ? k + a.at_once : a.steps;
         floatx4 acc[S::EACH];
 #pragma unroll
         for (int q = 0; q < S::EACH; ++q) acc[q] = floatx4{0, 0, 0, 0};
@@ -355,6 +357,46 @@ __global__ __launch_bounds__(S::THREADS) void gram_kernel(SmallArgs a)
     if (threadIdx.x == 0) a.scaled[matrix * a.parts + blockIdx.x] = down;
 }
 
+// Whether a part of the matrix's Gram matrix has scaled elements (they are those of the raw direction only)
+template <class S>
+__device__ __forceinline__ bool any_scaled(const SmallArgs &a, const unsigned *scaled)
+{
+    bool any = false;
+    if (a.from == 0)
+        for (int k = threadIdx.x; k < a.parts; k += S::THREADS) any |= scaled[k] != 0;
+    return __syncthreads_or(any);
+}
+
+// an element of a part, in float64, in the units of the scaled parts where there are any
+__device__ __forceinline__ double part_element(const float *from, const unsigned *scaled, bool any, int k, int64_t step, int e)
+{
+    const double v = from[k * step + e];
+    return any && !scaled[k] ? v * 0x1p-200 : v;
+}
+
+constexpr int kFewParts = 8;   // parts that the workgroup of the polynomial sums itself
+
+// Sums of many parts: grid (M M / 64, matrices), 64 elements a workgroup, every WAVES-th part to a wave
+template <class S>
+__global__ __launch_bounds__(S::THREADS) void sum_kernel(SmallArgs a)
+{
+    __shared__ double sums[S::WAVES][64];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int64_t matrix = blockIdx.y;
+    const float *from = a.gram + matrix * a.parts * S::M * S::M;
+    const unsigned *scaled = a.scaled + matrix * a.parts;
+    const bool any = any_scaled<S>(a, scaled);
+    const int e = blockIdx.x * 64 + lane;
+    double sum = 0.0;
+#pragma unroll 8
+    for (int k = wave; k < a.parts; k += S::WAVES) sum += part_element(from, scaled, any, k, S::M * S::M, e);
+    sums[wave][lane] = sum;
+    __syncthreads();
+    if (wave != 0) return;
+    for (int w = 1; w < S::WAVES; ++w) sum += sums[w][lane];
+    a.sum[matrix * S::M * S::M + e] = sum;
+}
+
 // The polynomial of a matrix from the parts of its Gram matrix: a workgroup per matrix.  The first is scaled by the
 // inverse of the norm.
 template <class S>
@@ -367,20 +409,15 @@ __global__ __launch_bounds__(S::THREADS) void polynomial_kernel(SmallArgs a)
     float *gram = lds, *b = gram + S::SQUARE, *p = b + S::SQUARE;
     const float *from = a.gram + matrix * a.parts * S::M * S::M;
     const unsigned *scaled = a.scaled + matrix * a.parts;
-    bool any = false;
-    if (a.from == 0)
-        for (int k = threadIdx.x; k < a.parts; k += S::THREADS) any |= scaled[k] != 0;
-    any = __syncthreads_or(any);
+    const bool any = any_scaled<S>(a, scaled);
+#pragma unroll 4
     for (int e = threadIdx.x; e < S::M * S::M; e += S::THREADS) {
         const int i = e / S::M, j = e % S::M;
-        if (i / 16 > j / 16) continue;
+        if (i / 16 > j / 16) continue;   // (below the diagonal: from above it)
         double sum = 0.0;
-        if (any) {
-            // all in the units of the scaled ones
-            for (int k = 0; k < a.parts; ++k) sum += (double)from[(int64_t)k * S::M * S::M + e] * (scaled[k] ? 1.0 : 0x1p-200);
-        } else {
-            for (int k = 0; k < a.parts; ++k) sum += (double)from[(int64_t)k * S::M * S::M + e];
-        }
+        if (a.parts > kFewParts) sum = a.sum[matrix * S::M * S::M + e];
+        else
+            for (int k = 0; k < a.parts; ++k) sum += part_element(from, scaled, any, k, S::M * S::M, e);
         gram[i * S::PITCH + j] = (float)sum;
         if (i / 16 != j / 16) gram[j * S::PITCH + i] = (float)sum;
     }
@@ -454,7 +491,7 @@ size_t whole_lds(const MatrixShape &s)
 {
     const size_t M = round16(s.m());
     // (the waves of a matrix of one tile share its sums)
-    return 3 * square_bytes((int)M) + M * (round16(s.n()) + 4) * sizeof(float) + (M == 16 ? 4 * 256 * sizeof(float) : 0);
+    return 3 * square_bytes((int)M) + M * (round16(s.n()) + 4) * sizeof(float) + (M == 16 ? 4 * 1024 * sizeof(float) : 0);
 }
 bool whole(const MatrixShape &s) { return s.n() <= 4096 && whole_lds(s) <= kSmallLds; }
 
@@ -471,7 +508,7 @@ int parts_of(const MatrixShape &s, int64_t count)
 }
 
 struct Layout {
-    size_t gram, scaled, poly, x, total;
+    size_t gram, scaled, sum, poly, x, total;
 };
 Layout layout_of(const MatrixShape &s, int64_t count)
 {
@@ -482,6 +519,7 @@ Layout layout_of(const MatrixShape &s, int64_t count)
     const auto take = [&](size_t bytes) { const size_t here = at; at += align256(bytes); return here; };
     l.gram = take(count * parts * M * M * sizeof(float));
     l.scaled = take(count * parts * sizeof(unsigned));
+    l.sum = take(parts > kFewParts ? count * M * M * sizeof(double) : 0);
     l.poly = take(count * M * M * sizeof(float));
     l.x = take(count * s.elems() * sizeof(float));
     l.total = at;
@@ -504,12 +542,15 @@ void launch(const MatrixShape &s, const UpdateArgs &update, SmallArgs a, char *w
 {
     if (whole(s)) {
         a.columns = round16(s.n());
+        // (of a matrix that is about square a new Gram matrix, which is the more exact, costs no more than the products it saves)
+        a.at_once = s.n() <= 2 * s.m() ? kStepsAtOnce - 1 : kStepsAtOnce;
         a.by_columns = Divide::by(a.columns), a.by_m = Divide::by(s.m()), a.by_n = Divide::by(s.n());
         const size_t lds = whole_lds(s);
         if (lds > 65536) allow_large_lds(reinterpret_cast<const void *>(whole_kernel<W>), kSmallLds);
         whole_kernel<W><<<(unsigned)s.batch, W::THREADS, lds, stream>>>(a);
         return;
     }
+    typedef Small<S::M, 16> Sum;
     const int64_t most = matrices_at_once(s);
     const size_t item = s.dtype == LMKAN_F32 ? 4 : 2;
     a.columns = columns_of(S::M);
@@ -520,6 +561,7 @@ void launch(const MatrixShape &s, const UpdateArgs &update, SmallArgs a, char *w
         const Layout l = layout_of(s, count);
         a.parts = parts_of(s, count);
         a.gram = reinterpret_cast<float *>(ws + l.gram), a.scaled = reinterpret_cast<unsigned *>(ws + l.scaled);
+        a.sum = reinterpret_cast<double *>(ws + l.sum);
         a.poly = reinterpret_cast<float *>(ws + l.poly), a.x = reinterpret_cast<float *>(ws + l.x);
         a.u.grad = static_cast<const char *>(update.grad) + skip * item;
         a.u.momentum = update.momentum ? update.momentum + skip : nullptr;
@@ -530,6 +572,7 @@ void launch(const MatrixShape &s, const UpdateArgs &update, SmallArgs a, char *w
         gram_kernel<S><<<grid, S::THREADS, block + scratch, stream>>>(a);
         for (; a.from < a.steps; a.from = a.to) {
             a.to = a.from + kStepsAtOnce < a.steps ? a.from + kStepsAtOnce : a.steps;
+            if (a.parts > kFewParts) sum_kernel<Sum><<<dim3(S::M * S::M / 64, (unsigned)count), Sum::THREADS, 0, stream>>>(a);
             polynomial_kernel<W><<<(unsigned)count, W::THREADS, 3 * square, stream>>>(a);
             if (a.to == a.steps) apply_kernel<S, true><<<grid, S::THREADS, square + block, stream>>>(a);
             else apply_kernel<S, false><<<grid, S::THREADS, square + block + scratch, stream>>>(a);
@@ -556,12 +599,22 @@ void launch_ortho_small(const MatrixShape &s, int steps, const float *schedule, 
     a.steps = steps;
     for (int k = 0; k < 3 * steps; ++k) a.schedule[k] = schedule[k];
     char *ws = static_cast<char *>(workspace);
-    // A wave a matrix where there is one tile and little to load; as many waves as a symmetric product has tiles where
-    // a matrix has a compute unit to itself.
-    if (s.m() <= 16 && s.n() <= 256) launch<Small<16, 1>, Small<16, 4>>(s, u, a, ws, stream);
-    else if (s.m() <= 16) launch<Small<16, 4>, Small<16, 4>>(s, u, a, ws, stream);
-    else if (s.m() <= 32) launch<Small<32, 4>, Small<32, 4>>(s, u, a, ws, stream);
-    else if (s.m() <= 48) launch<Small<48, 8>, Small<48, 4>>(s, u, a, ws, stream);
+    // Waves of a workgroup that has a matrix to itself: more for longer rows, fewer where one is small enough for several
+    // workgroups a compute unit.  Measured (us, 1 / 4 / 8 / 16 waves, 64: 8 / 12): 1681 of 8 x 16 9.7 / 16 / 23 / 52; 1000 of
+    // 16 x 100 22 / 19 / 20 / 37; 400 of 10 x 300 42 / 19 / 17 / 24; 25 of 12 x 900 114 / 36 / 24 / 20; 1600 of 30 x 60
+    // - / 44 / 53 / 89; 441 of 32 x 218 - / 36 / 32 / 40; one of 32 x 500 - / 49 / 35 / 29; 441 of 48 x 100 - / 45 / 39 / 47;
+    // 25 of 48 x 500 - / 80 / 54 / 46; 1600 of 64 x 64 156 / 186; 169 of 144 x 64 43 / 38.
+    const int m = s.m(), n = s.n();
+    if (m <= 16 && n <= 32) launch<Small<16, 1>, Small<16, 4>>(s, u, a, ws, stream);
+    else if (m <= 16 && n <= 160) launch<Small<16, 4>, Small<16, 4>>(s, u, a, ws, stream);
+    else if (m <= 16 && n <= 512) launch<Small<16, 8>, Small<16, 4>>(s, u, a, ws, stream);
+    else if (m <= 16) launch<Small<16, 16>, Small<16, 4>>(s, u, a, ws, stream);
+    else if (m <= 32 && n <= 64) launch<Small<32, 4>, Small<32, 4>>(s, u, a, ws, stream);
+    else if (m <= 32 && n <= 300) launch<Small<32, 8>, Small<32, 4>>(s, u, a, ws, stream);
+    else if (m <= 32) launch<Small<32, 16>, Small<32, 4>>(s, u, a, ws, stream);
+    else if (m <= 48 && n <= 200) launch<Small<48, 8>, Small<48, 4>>(s, u, a, ws, stream);
+    else if (m <= 48) launch<Small<48, 16>, Small<48, 4>>(s, u, a, ws, stream);
+    else if (n <= 64) launch<Small<64, 8>, Small<64, 4>>(s, u, a, ws, stream);
     else launch<Small<64, 12>, Small<64, 4>>(s, u, a, ws, stream);
 }
 
