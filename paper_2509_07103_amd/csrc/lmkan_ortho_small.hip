@@ -42,7 +42,8 @@ struct SmallArgs {
     float schedule[3 * LMKAN_MAX_ORTHO_STEPS];
     int at_once;                           // steps on one Gram matrix
     int columns;                           // of X in LDS at a time, a multiple of 16
-    Divide by_columns, by_m, by_n;
+    Divide by_fours;                       // columns / 4
+    bool whole_fours;                      // four adjacent elements from a multiple of four on are whole and aligned
     int parts;                             // workgroups that share a matrix
     float *gram;                           // [matrices][parts][M][M], upper tiles
     double *sum;                           // [matrices][M][M]: their sums, where they are many
@@ -57,10 +58,62 @@ __device__ __forceinline__ int64_t stored_at(const MatrixShape &s, int64_t matri
     return matrix * s.elems() + (s.flip() ? (int64_t)column * s.cols + row : (int64_t)row * s.cols + column);
 }
 
-__device__ __forceinline__ void store_result(const SmallArgs &a, int64_t at, float v)
+// Four adjacent elements of what is stored, `count` of which exist; `whole`: all four, aligned to their size together
+struct Raw4 {
+    floatx4 g, m;
+};
+__device__ __forceinline__ floatx4 load_four(const void *p, int dtype, int64_t at, int count, bool whole)
 {
-    if (a.u.weight) a.u.weight[at] = a.u.keep * a.u.weight[at] + a.u.add * v;
-    else store_from_float(a.u.out, at, a.s.dtype, v);
+    floatx4 v = {0, 0, 0, 0};
+    if (whole) {
+        if (dtype == LMKAN_F32) return *reinterpret_cast<const floatx4 *>(static_cast<const float *>(p) + at);
+        const uint2 u = *reinterpret_cast<const uint2 *>(static_cast<const uint16_t *>(p) + at);
+        const uint16_t h[4] = {(uint16_t)u.x, (uint16_t)(u.x >> 16), (uint16_t)u.y, (uint16_t)(u.y >> 16)};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = load_as_float(h, e, dtype);
+        return v;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (e < count) v[e] = load_as_float(p, at + e, dtype);
+    return v;
+}
+__device__ __forceinline__ void store_four(void *p, int dtype, int64_t at, int count, bool whole, const floatx4 &v)
+{
+    if (whole) {
+        if (dtype == LMKAN_F32) *reinterpret_cast<floatx4 *>(static_cast<float *>(p) + at) = v;
+        else *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(p) + at) = make_uint2(two_from_float(dtype, v[0], v[1]), two_from_float(dtype, v[2], v[3]));
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (e < count) store_from_float(p, at + e, dtype, v[e]);
+}
+// the direction's, in two halves as fetch() and direction() do one
+__device__ __forceinline__ Raw4 fetch_four(const UpdateArgs &u, int dtype, int64_t at, int count, bool whole, bool move)
+{
+    Raw4 r = {};
+    if (!u.momentum || u.nesterov || move) r.g = load_four(u.grad, dtype, at, count, whole);
+    if (u.momentum) r.m = load_four(u.momentum, LMKAN_F32, at, count, whole);
+    return r;
+}
+__device__ __forceinline__ floatx4 direction_four(const UpdateArgs &u, Raw4 r, int64_t at, int count, bool whole, bool move)
+{
+    if (!u.momentum) return r.g;
+    if (move) {
+        r.m = u.beta * r.m + (1.0f - u.beta) * r.g;
+        store_four(u.momentum, LMKAN_F32, at, count, whole, r.m);
+    }
+    return u.nesterov ? u.beta * r.m + (1.0f - u.beta) * r.g : r.m;
+}
+__device__ __forceinline__ void store_result_four(const SmallArgs &a, int64_t at, int count, bool whole, const floatx4 &v)
+{
+    if (a.u.weight) {
+        const floatx4 w = load_four(a.u.weight, LMKAN_F32, at, count, whole);
+        store_four(a.u.weight, LMKAN_F32, at, count, whole, a.u.keep * w + a.u.add * v);
+    } else {
+        store_four(a.u.out, a.s.dtype, at, count, whole, v);
+    }
 }
 
 // M: the shorter side rounded up to 16; WAVES of a workgroup
@@ -93,35 +146,76 @@ struct Small {
         return acc;
     }
 
-    // X: columns [first, first + columns) of all rows to LDS, zero beyond the matrix; returns whether one is large.
-    // get(row, column) loads, use(loaded, row, column) makes the element of it.
-    template <class G, class U>
-    static __device__ __forceinline__ bool load(float *x, int pitch, const MatrixShape &s, int first, int columns, const Divide &by_columns, G &&get, U &&use)
+    // Calls f(row, column, count) for every four adjacent elements of what is stored of columns [first, first + columns),
+    // kAtOnce of them at a time: f(first of them, ...) is for loads, g(...) for what follows.  `count` may be zero or negative.
+    template <class F, class G>
+    static __device__ __forceinline__ void for_fours(const MatrixShape &s, int first, int columns, const Divide &by_fours, F &&f, G &&g)
     {
-        constexpr int kAtOnce = 8;
-        bool large = false;
-        const int m = s.m(), n = s.n();
+        constexpr int kAtOnce = 4;
+        const int m = s.m(), n = s.n(), fours = M * columns / 4;
         const bool flip = s.flip();
-        for (int e0 = threadIdx.x; e0 < M * columns; e0 += kAtOnce * THREADS) {
-            Raw raw[kAtOnce];
+        for (int e0 = threadIdx.x; e0 < fours; e0 += kAtOnce * THREADS) {
 #pragma unroll
-            for (int u = 0; u < kAtOnce; ++u) {
-                // neighbouring lanes take neighbouring elements of what is stored
-                const int e = e0 + u * THREADS, q = flip ? e / M : by_columns.quotient(e);
-                const int r = flip ? e % M : q, c = flip ? q : e - q * columns;
-                if (e < M * columns && r < m && first + c < n) raw[u] = get(r, first + c);
-            }
+            for (int pass = 0; pass < 2; ++pass)
 #pragma unroll
-            for (int u = 0; u < kAtOnce; ++u) {
-                const int e = e0 + u * THREADS, q = flip ? e / M : by_columns.quotient(e);
-                const int r = flip ? e % M : q, c = flip ? q : e - q * columns;
-                if (e >= M * columns) break;
-                const float v = r < m && first + c < n ? use(raw[u], r, first + c) : 0.0f;
-                large |= !(fabsf(v) <= kLarge);
-                x[r * pitch + c] = v;
-            }
+                for (int u = 0; u < kAtOnce; ++u) {
+                    const int e = e0 + u * THREADS, q = flip ? e / (M / 4) : by_fours.quotient(e);
+                    const int r = flip ? 4 * (e % (M / 4)) : q, c = flip ? q : 4 * (e - q * (columns / 4));
+                    const int count = flip ? (first + c < n ? m - r : 0) : (r < m ? n - first - c : 0);
+                    if (e >= fours) break;
+                    if (pass == 0) f(u, r, c, count);
+                    else g(u, r, c, count);
+                }
         }
+    }
+
+    // X: columns [first, first + columns) of all rows to LDS, zero beyond the matrix; returns whether one is large.
+    // get(at, count, whole) loads the elements stored from `at` on, use(...) makes the direction of them.
+    template <class G, class U>
+    static __device__ __forceinline__ bool load(float *x, int pitch, const MatrixShape &s, int64_t matrix, int first, int columns, const Divide &by_fours, bool whole, G &&get, U &&use)
+    {
+        bool large = false;
+        Raw4 raw[4];
+        const bool flip = s.flip();
+        for_fours(s, first, columns, by_fours,
+            [&](int u, int r, int c, int count) {
+                if (count > 0) raw[u] = get(stored_at(s, matrix, r, first + c), count, whole && count >= 4);
+            },
+            [&](int u, int r, int c, int count) {
+                floatx4 v = {0, 0, 0, 0};
+                if (count > 0) v = use(raw[u], stored_at(s, matrix, r, first + c), count, whole && count >= 4);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (e >= count) v[e] = 0.0f;
+                    large |= !(fabsf(v[e]) <= kLarge);
+                }
+                if (!flip) {
+                    *reinterpret_cast<floatx4 *>(x + r * pitch + c) = v;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[(r + e) * pitch + c] = v[e];
+                }
+            });
         return large;
+    }
+
+    // Columns [first, first + columns) of X from LDS: put(at, count, whole, values) for every four adjacent stored elements
+    template <class P>
+    static __device__ __forceinline__ void store(const float *x, int pitch, const MatrixShape &s, int64_t matrix, int first, int columns, const Divide &by_fours, bool whole, P &&put)
+    {
+        const bool flip = s.flip();
+        for_fours(s, first, columns, by_fours, [](int, int, int, int) {},
+            [&](int, int r, int c, int count) {
+                if (count <= 0) return;
+                floatx4 v;
+                if (!flip) {
+                    v = *reinterpret_cast<const floatx4 *>(x + r * pitch + c);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] = x[(r + e) * pitch + c];
+                }
+                put(stored_at(s, matrix, r, first + c), count, whole && count >= 4, v);
+            });
     }
 
     // acc += X X^T over the columns in LDS, the wave's tiles
@@ -293,11 +387,11 @@ __global__ __launch_bounds__(S::THREADS) void whole_kernel(SmallArgs a)
     __shared__ double shared;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int64_t matrix = blockIdx.x;
-    const int columns = a.columns, pitch = columns + 4, m = a.s.m(), n = a.s.n();
+    const int columns = a.columns, pitch = columns + 4, m = a.s.m();
     float *gram = lds, *b = gram + S::SQUARE, *p = b + S::SQUARE, *x = p + S::SQUARE, *scratch = x + S::M * pitch;
     const bool large = S::load(
-        x, pitch, a.s, 0, columns, a.by_columns, [&](int r, int c) { return fetch(a.u, a.s.dtype, stored_at(a.s, matrix, r, c), true); },
-        [&](Raw v, int r, int c) { return direction(a.u, v, stored_at(a.s, matrix, r, c), true); });
+        x, pitch, a.s, matrix, 0, columns, a.by_fours, a.whole_fours, [&](int64_t at, int count, bool whole) { return fetch_four(a.u, a.s.dtype, at, count, whole, true); },
+        [&](const Raw4 &v, int64_t at, int count, bool whole) { return direction_four(a.u, v, at, count, whole, true); });
     const bool down = __syncthreads_or(large);
     if (down) scale_columns<S>(x, pitch, columns, kDown);
     for (int k = 0; k < a.steps;) {
@@ -317,12 +411,7 @@ __global__ __launch_bounds__(S::THREADS) void whole_kernel(SmallArgs a)
         __syncthreads();
         k = end;
     }
-    const bool flip = a.s.flip();
-#pragma unroll 4
-    for (int e = threadIdx.x; e < m * n; e += S::THREADS) {
-        const int q = flip ? a.by_m.quotient(e) : a.by_n.quotient(e), left = e - q * (flip ? m : n);
-        store_result(a, matrix * a.s.elems() + e, flip ? x[left * pitch + q] : x[q * pitch + left]);
-    }
+    S::store(x, pitch, a.s, matrix, 0, columns, a.by_fours, a.whole_fours, [&](int64_t at, int count, bool whole, const floatx4 &v) { store_result_four(a, at, count, whole, v); });
 }
 
 // Part of the Gram matrices of the raw direction: grid (parts, matrices)
@@ -340,8 +429,8 @@ __global__ __launch_bounds__(S::THREADS) void gram_kernel(SmallArgs a)
     bool down = false;
     for (int64_t first = (int64_t)blockIdx.x * columns; first < n; first += (int64_t)a.parts * columns) {
         const bool large = S::load(
-            x, pitch, a.s, (int)first, columns, a.by_columns, [&](int r, int c) { return fetch(a.u, a.s.dtype, stored_at(a.s, matrix, r, c), true); },
-            [&](Raw v, int r, int c) { return direction(a.u, v, stored_at(a.s, matrix, r, c), true); });
+            x, pitch, a.s, matrix, (int)first, columns, a.by_fours, a.whole_fours, [&](int64_t at, int count, bool whole) { return fetch_four(a.u, a.s.dtype, at, count, whole, true); },
+            [&](const Raw4 &v, int64_t at, int count, bool whole) { return direction_four(a.u, v, at, count, whole, true); });
         const bool now = __syncthreads_or(large);
         if (now && !down) {
             down = true;
@@ -374,7 +463,7 @@ __device__ __forceinline__ double part_element(const float *from, const unsigned
     return any && !scaled[k] ? v * 0x1p-200 : v;
 }
 
-constexpr int kFewParts = 8;   // parts that the workgroup of the polynomial sums itself
+constexpr int kFewParts = 16;  // parts that the workgroup of the polynomial sums itself
 
 // Sums of many parts: grid (M M / 64, matrices), 64 elements a workgroup, every WAVES-th part to a wave
 template <class S>
@@ -415,9 +504,12 @@ __global__ __launch_bounds__(S::THREADS) void polynomial_kernel(SmallArgs a)
         const int i = e / S::M, j = e % S::M;
         if (i / 16 > j / 16) continue;   // (below the diagonal: from above it)
         double sum = 0.0;
-        if (a.parts > kFewParts) sum = a.sum[matrix * S::M * S::M + e];
-        else
+        if (a.parts > kFewParts) {
+            sum = a.sum[matrix * S::M * S::M + e];
+        } else {
+#pragma unroll 4
             for (int k = 0; k < a.parts; ++k) sum += part_element(from, scaled, any, k, S::M * S::M, e);
+        }
         gram[i * S::PITCH + j] = (float)sum;
         if (i / 16 != j / 16) gram[j * S::PITCH + i] = (float)sum;
     }
@@ -444,35 +536,27 @@ __global__ __launch_bounds__(S::THREADS) void apply_kernel(SmallArgs a)
     floatx4 acc[S::EACH];
 #pragma unroll
     for (int q = 0; q < S::EACH; ++q) acc[q] = floatx4{0, 0, 0, 0};
-    const float *held = a.x + matrix * (int64_t)m * n;
     MatrixShape seen = a.s;   // X itself lies with the shorter side first
     if (a.from != 0) seen.rows = m, seen.cols = n;
+    MatrixShape kept = a.s;
+    kept.rows = m, kept.cols = n;
+    const bool x_fours = n % 4 == 0;
     for (int64_t first = (int64_t)blockIdx.x * columns; first < n; first += (int64_t)a.parts * columns) {
         S::load(
-            x, pitch, seen, (int)first, columns, a.by_columns,
-            [&](int r, int c) {
-                return a.from != 0 ? Raw{held[(int64_t)r * n + c], 0.0f} : fetch(a.u, a.s.dtype, stored_at(a.s, matrix, r, c), false);
+            x, pitch, seen, matrix, (int)first, columns, a.by_fours, a.from != 0 ? x_fours : a.whole_fours,
+            [&](int64_t at, int count, bool whole) {
+                return a.from != 0 ? Raw4{load_four(a.x, LMKAN_F32, at, count, whole), {}} : fetch_four(a.u, a.s.dtype, at, count, whole, false);
             },
-            [&](Raw v, int r, int c) { return a.from != 0 ? v.g : direction(a.u, v, 0, false); });
+            [&](const Raw4 &v, int64_t at, int count, bool whole) { return a.from != 0 ? v.g : direction_four(a.u, v, at, count, whole, false); });
         __syncthreads();
         S::apply(p, x, pitch, columns, wave, lane);
         __syncthreads();
-        const int count = n - first < columns ? (int)(n - first) : columns;
         if (LAST) {
-            const bool flip = a.s.flip();
-#pragma unroll 4
-            for (int e = threadIdx.x; e < S::M * columns; e += S::THREADS) {
-                const int q = flip ? e / S::M : a.by_columns.quotient(e);
-                const int r = flip ? e % S::M : q, c = flip ? q : e - q * columns;
-                if (r < m && c < count) store_result(a, stored_at(a.s, matrix, r, (int)first + c), x[r * pitch + c]);
-            }
+            S::store(x, pitch, a.s, matrix, (int)first, columns, a.by_fours, a.whole_fours,
+                     [&](int64_t at, int count, bool whole, const floatx4 &v) { store_result_four(a, at, count, whole, v); });
         } else {
-            float *to = a.x + matrix * (int64_t)m * n + first;
-#pragma unroll 4
-            for (int e = threadIdx.x; e < S::M * columns; e += S::THREADS) {
-                const int r = a.by_columns.quotient(e), c = e - r * columns;
-                if (r < m && c < count) to[(int64_t)r * n + c] = x[r * pitch + c];
-            }
+            S::store(x, pitch, kept, matrix, (int)first, columns, a.by_fours, x_fours,
+                     [&](int64_t at, int count, bool whole, const floatx4 &v) { store_four(a.x, LMKAN_F32, at, count, whole, v); });
             S::gram(x, pitch, columns, wave, lane, acc);
         }
         __syncthreads();
@@ -544,7 +628,7 @@ void launch(const MatrixShape &s, const UpdateArgs &update, SmallArgs a, char *w
         a.columns = round16(s.n());
         // (of a matrix that is about square a new Gram matrix, which is the more exact, costs no more than the products it saves)
         a.at_once = s.n() <= 2 * s.m() ? kStepsAtOnce - 1 : kStepsAtOnce;
-        a.by_columns = Divide::by(a.columns), a.by_m = Divide::by(s.m()), a.by_n = Divide::by(s.n());
+        a.by_fours = Divide::by(a.columns / 4);
         const size_t lds = whole_lds(s);
         if (lds > 65536) allow_large_lds(reinterpret_cast<const void *>(whole_kernel<W>), kSmallLds);
         whole_kernel<W><<<(unsigned)s.batch, W::THREADS, lds, stream>>>(a);
@@ -554,7 +638,7 @@ void launch(const MatrixShape &s, const UpdateArgs &update, SmallArgs a, char *w
     const int64_t most = matrices_at_once(s);
     const size_t item = s.dtype == LMKAN_F32 ? 4 : 2;
     a.columns = columns_of(S::M);
-    a.by_columns = Divide::by(a.columns);
+    a.by_fours = Divide::by(a.columns / 4);
     const size_t block = (size_t)S::M * (a.columns + 4) * sizeof(float), scratch = 4 * S::THREADS * sizeof(float), square = square_bytes(S::M);
     for (int64_t first = 0; first < s.batch; first += most) {
         const int64_t count = s.batch - first < most ? s.batch - first : most, skip = first * s.elems();
@@ -599,6 +683,9 @@ void launch_ortho_small(const MatrixShape &s, int steps, const float *schedule, 
     a.steps = steps;
     for (int k = 0; k < 3 * steps; ++k) a.schedule[k] = schedule[k];
     char *ws = static_cast<char *>(workspace);
+    const auto aligned = [](const void *p, size_t item) { return reinterpret_cast<uintptr_t>(p) % (4 * item) == 0; };
+    const size_t item = s.dtype == LMKAN_F32 ? 4 : 2;
+    a.whole_fours = s.cols % 4 == 0 && aligned(u.grad, item) && aligned(u.out, item) && aligned(u.momentum, 4) && aligned(u.weight, 4);
     // Waves of a workgroup that has a matrix to itself: more for longer rows, fewer where one is small enough for several
     // workgroups a compute unit.  Measured (us, 1 / 4 / 8 / 16 waves, 64: 8 / 12): 1681 of 8 x 16 9.7 / 16 / 23 / 52; 1000 of
     // 16 x 100 22 / 19 / 20 / 37; 400 of 10 x 300 42 / 19 / 17 / 24; 25 of 12 x 900 114 / 36 / 24 / 20; 1600 of 30 x 60
