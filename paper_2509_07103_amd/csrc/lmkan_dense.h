@@ -43,6 +43,12 @@ struct ScheduleBounds {
 };
 bool schedule_bounds(int steps, const float *schedule, ScheduleBounds *bounds);
 
+// Steps that are taken on one Gram matrix before the polynomial is applied and a new one is formed (lmkan_ortho.hip)
+int steps_at_once(const MatrixShape &s);
+
+// the power of two that brings values up to `bound` to the upper end of float16's range (65504), with room for rounding
+float pair_scale(double bound);
+
 size_t ortho_workspace_bytes(const MatrixShape &s);
 void launch_ortho(const MatrixShape &s, int steps, const float *schedule, const UpdateArgs &u, void *workspace,
                   hipStream_t stream);

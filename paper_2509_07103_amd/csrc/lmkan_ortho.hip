@@ -4,14 +4,13 @@
 //
 // with X of m x n, m <= n (the transpose of what is stored where that has more rows than columns).  Everything
 // between X_0 and the result is a polynomial of A_0, and polynomials of one symmetric matrix commute, so that
-// up to three steps are taken on m x m matrices alone,
+// several steps can be taken on m x m matrices alone,
 //   A_{k+1} = B_k A_k B_k,   P_{k+1} = B_k P_k,
-// and then X_{k+3} = P X_k.  All products but that one are symmetric: half their tiles are computed and mirrored.
-// For five steps that is 6 m^2 n + 14 m^3 multiply-adds instead of the 15 m^2 n + 5 m^3 of the steps as written,
-// and X is read and written twice instead of five times.  Three steps, not all: an error of A is relative to its
-// largest eigenvalue and grows by up to a^2 (11.9) a step where the eigenvalue is small; with a new Gram matrix
-// after three steps the result is as near to float64 as the steps as written are in float32 (strong directions a
-// hundred times the rest: 1.1e-5 and 1.9e-5 of the result; five steps on one Gram matrix: 6e-5).
+// and then X_{k+s} = P X_k.  All products but that one are symmetric: half their tiles are computed and mirrored.
+// Five steps take 15 m^2 n + 5 m^3 multiply-adds as written, 9 m^2 n + 11 m^3 two at a time and 6 m^2 n + 14 m^3 three
+// at a time, and X is read and written five, three or two times.  An error of A is relative to its largest eigenvalue
+// and grows by up to a^2 (11.9) a step where the eigenvalue is small, which is why not all are taken at once, and
+// steps_at_once() chooses.
 //
 // Factors are pairs of float16 (lmkan_tile.h): three instructions at the rate of float16 keep 22 bits, which
 // float32 instructions would do at a sixteenth of that rate.  The power of two that a matrix is scaled by follows
@@ -27,7 +26,7 @@ namespace lmkan {
 
 namespace {
 
-constexpr int kStepsAtOnce = 3;   // steps on one Gram matrix
+constexpr int kStepsAtOnce = 3;   // steps on one Gram matrix, at most
 constexpr int kAtOnce = 8;        // elements that a thread loads before it uses them
 constexpr int kNormParts = 1024;  // workgroups that sum the norm of one matrix, at most
 
@@ -623,10 +622,29 @@ Layout layout_of(const MatrixShape &s, int64_t count)
     return l;
 }
 
-// the power of two that brings values up to `bound` to the upper end of float16's range (65504), with room for rounding
-float scale_for(double bound) { return (float)exp2(floor(log2(32000.0 / bound))); }
-
 }  // namespace
+
+// The error against float64 is to stay near that of the steps as written in float32, which grows with m while that of
+// pairs summed line by line hardly does; long rows make small eigenvalues, and those suffer.  Measured, the error
+// relative to that of float32 for gradients with a few strong directions:
+//   m x n        one   two   three at once   |  m x n         two   three at once
+//   60 x 60      0.84  1.70  2.94            |  128 x 2000    0.70  2.28
+//   48 x 100     0.82  1.04  3.4             |  192 x 1537    0.58  2.31
+//   64 x 144     0.82  0.73  3.3             |  193 x 400     0.66  1.37
+//   48 x 400      -    0.84  1.99            |  193 x 1600    0.57  2.34
+//   33 x 270      -     -    1.59            |  256 x 256      -    1.20
+//   16 x 200      -     -    1.16            |  256 x 2100     -    1.87
+//   100 x 100    0.52  1.08  1.89            |  320 x 3000     -    1.03
+int steps_at_once(const MatrixShape &s)
+{
+    const int m = s.m(), n = s.n();
+    if (m <= 64 && (n < 2 * m || (m > 32 && m <= 40))) return 1;
+    if (m <= 32) return n <= 8 * m ? 2 : 3;
+    if (m <= 192) return 2;
+    return m <= 256 && n > 2 * m ? 2 : 3;
+}
+
+float pair_scale(double bound) { return (float)exp2(floor(log2(32000.0 / bound))); }
 
 bool schedule_bounds(int steps, const float *schedule, ScheduleBounds *bounds)
 {
@@ -680,14 +698,14 @@ void launch_ortho(const MatrixShape &s, int steps, const float *schedule, const 
     if (ortho_small_applicable(s, steps)) return launch_ortho_small(s, steps, schedule, u, workspace, stream);
     ScheduleBounds bounds;
     (void)schedule_bounds(steps, schedule, &bounds);
-    const int m = s.m(), n = s.n();
+    const int m = s.m(), n = s.n(), at_once = steps_at_once(s);
     const int64_t most = matrices_at_once(s);
     for (int64_t first = 0; first < s.batch; first += most) {
         const int64_t count = s.batch - first < most ? s.batch - first : most;
         const Layout l = layout_of(s, count);
         char *ws = static_cast<char *>(workspace);
         const auto pairs = [&](size_t at, int rows, int depth, double bound) {
-            const float scale = scale_for(bound);
+            const float scale = pair_scale(bound);
             return PairMatrix{ws + at, pair_bytes(rows, depth), rows, depth, scale, 1.0f / scale};
         };
         double *part = reinterpret_cast<double *>(ws + l.norm);
@@ -712,7 +730,7 @@ void launch_ortho(const MatrixShape &s, int steps, const float *schedule, const 
         args.parts = reinterpret_cast<floatx4 *>(ws + l.parts);
         const auto one = [&](const Product &p) { args.p[0] = p, args.problems = 1; };
         for (int k = 0; k < steps;) {
-            const int end = k + kStepsAtOnce < steps ? k + kStepsAtOnce : steps;
+            const int end = k + at_once < steps ? k + at_once : steps;
             const double r = bounds.singular[k];
             PairMatrix gram = pairs(l.a, m, m, r * r), so_far = none;
             one(Product{x, x, gram, gram, none, 0, 0, 0, true});
@@ -726,10 +744,10 @@ void launch_ortho(const MatrixShape &s, int steps, const float *schedule, const 
                     const double now = bounds.singular[k + i], most_now = bounds.factor[k + i];
                     factor *= most_now;
                     for (int e = 0; e < 3; ++e) chain.abc[3 * i + e] = schedule[3 * (k + i) + e];
-                    chain.gram_scale[i] = scale_for(now * now);
-                    chain.step_scale[i] = scale_for(most_now);
-                    chain.w_scale[i] = scale_for(most_now * now * now);
-                    chain.p_scale[i] = scale_for(factor);
+                    chain.gram_scale[i] = pair_scale(now * now);
+                    chain.step_scale[i] = pair_scale(most_now);
+                    chain.w_scale[i] = pair_scale(most_now * now * now);
+                    chain.p_scale[i] = pair_scale(factor);
                 }
                 chain.p[0] = pairs(l.p[0], m, m, factor), chain.p[1] = pairs(l.p[1], m, m, factor);
                 allow_large_lds(reinterpret_cast<const void *>(chain_kernel), 2 * kSideBytes);

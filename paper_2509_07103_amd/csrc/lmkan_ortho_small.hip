@@ -1,4 +1,4 @@
-// Orthogonalisation of matrices whose shorter side is at most 64, in float32 matrix instructions.
+// Orthogonalisation of matrices whose shorter side is at most 64.
 //
 // The steps are those of lmkan_ortho.hip: up to three on the m x m Gram matrix, applied together.  Here the Gram
 // matrix and its polynomials fit the LDS of one workgroup, so that a matrix costs
@@ -6,7 +6,8 @@
 //   five         where it is longer (five steps): Gram matrix in parts, polynomial, apply and next Gram matrix in
 //                parts, polynomial, apply.
 // The products with X take 2 m multiply-adds per element and pass; at m = 64 the float32 instructions (157 TFLOP/s)
-// take about as long for that as memory takes for the element, so nothing is gained by splitting factors.
+// take about as long for that as memory takes for the element, so nothing is gained by splitting factors.  The products
+// of the polynomials are a chain in one workgroup: from m = 33 on, pairs of float16 (lmkan_tile.h) make it shorter.
 //
 // Norms: |X|^2 is the trace of the Gram matrix of the raw direction D, A_0 = D D^T / (|D| + eps)^2 and the first
 // polynomial is scaled by 1 / (|D| + eps).  The trace and the sum of the parts are taken in float64.  Elements beyond
@@ -22,7 +23,6 @@ namespace lmkan {
 
 namespace {
 
-constexpr int kStepsAtOnce = 3;            // steps on one Gram matrix (as for larger matrices)
 constexpr float kLarge = 0x1p50f;          // elements beyond it are scaled in Gram matrices
 constexpr float kDown = 0x1p-100f;
 constexpr int kSmallLds = 150 * 1024;      // of 160 KiB
@@ -40,6 +40,8 @@ struct SmallArgs {
     UpdateArgs u;
     int steps, from, to;                   // steps [from, to) of the schedule
     float schedule[3 * LMKAN_MAX_ORTHO_STEPS];
+    // powers of two that pairs are held times: the Gram matrix, B, B A, and the polynomial so far
+    float gram_scale[LMKAN_MAX_ORTHO_STEPS], step_scale[LMKAN_MAX_ORTHO_STEPS], w_scale[LMKAN_MAX_ORTHO_STEPS], p_scale[LMKAN_MAX_ORTHO_STEPS];
     int at_once;                           // steps on one Gram matrix
     int columns;                           // of X in LDS at a time, a multiple of 16
     Divide by_fours;                       // columns / 4
@@ -125,6 +127,9 @@ struct Small {
     static constexpr int EACH = SHARE > 1 ? 1 : (TILES + WAVES - 1) / WAVES;  // tiles of a wave
     static constexpr int PITCH = M + 4;
     static constexpr int SQUARE = M * PITCH;                                  // floats of an M x M matrix in LDS
+    static constexpr bool PAIRS = M >= 48;                                    // products of polynomials in pairs
+    static constexpr int LINES = (M + kPanel - 1) / kPanel, PAIR_SQUARE = LINES * M * kLine;   // bytes of one of pairs
+    static constexpr int REST = PAIRS ? 3 * PAIR_SQUARE : 2 * SQUARE * (int)sizeof(float);     // bytes that polynomial() needs
 
     // tile t of the upper triangle, column by column
     static __device__ __forceinline__ void tile(int t, int *i, int *j)
@@ -294,9 +299,14 @@ struct Small {
         __syncthreads();
     }
 
-    // The steps [from, to) of the schedule on the Gram matrix `a` in LDS: leaves their polynomial in `p`
-    static __device__ __forceinline__ void polynomial(const SmallArgs &s, int from, int to, float *a, float *b, float *p, int wave, int lane)
+    // The steps [from, to) of the schedule on the Gram matrix `a` in LDS; returns their polynomial.  `rest`: REST bytes.
+    static __device__ __forceinline__ float *polynomial(const SmallArgs &s, int from, int to, float *a, char *rest, int wave, int lane)
     {
+        if constexpr (PAIRS) {
+            polynomial_of_pairs(s, from, to, a, rest, wave, lane);
+            return a;
+        }
+        float *b = reinterpret_cast<float *>(rest), *p = b + SQUARE;
         for (int k = from; k < to; ++k) {
             const float c0 = s.schedule[3 * k], c1 = s.schedule[3 * k + 1], c2 = s.schedule[3 * k + 2];
             float *step = k == from ? p : b;
@@ -313,6 +323,129 @@ struct Small {
             }
             if (k > from) product(p, b, p, wave, lane, same);
         }
+        return p;
+    }
+
+    // where the four adjacent columns of a lane's row of tile (i, j) lie in a square of pairs, hi; and turned, column
+    // 16 j + 4 (lane >> 4) + (lane & 3), four adjacent rows
+    static __device__ __forceinline__ int pair_place(int i, int j, int lane, bool lo)
+    {
+        const int r = 16 * i + (lane & 15), q = lane >> 4, chunk = 2 * (j & 1) + (q >> 1);
+        return (j / 2 * M + r) * kLine + slot_of(r, chunk + (lo ? 4 : 0)) * 16 + (q & 1) * 8;
+    }
+    static __device__ __forceinline__ int turned_place(int i, int j, int lane, bool lo)
+    {
+        const int r = 16 * j + 4 * (lane >> 4) + (lane & 3), k = (lane & 15) >> 2, chunk = 2 * (i & 1) + (k >> 1);
+        return (i / 2 * M + r) * kLine + slot_of(r, chunk + (lo ? 4 : 0)) * 16 + (k & 1) * 8;
+    }
+
+    // The same in pairs: `square` holds A and, at the end, the polynomial.  A wave has one tile of the upper triangle; all
+    // read, then all write.
+    static __device__ __forceinline__ void polynomial_of_pairs(const SmallArgs &s, int from, int to, float *square, char *rest, int wave, int lane)
+    {
+        static_assert(!PAIRS || TILES <= WAVES, "a tile a wave");
+        char *a = rest, *b = a + PAIR_SQUARE, *p = b + PAIR_SQUARE;
+        for (int e = threadIdx.x; e < M * LINES * 4; e += THREADS) {
+            // eight values a thread, zero beyond the last column
+            const int row = e / (LINES * 4), chunk = e % (LINES * 4);
+            half8 hi, lo;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float v = chunk * 8 < M ? square[row * PITCH + chunk * 8 + k] * s.gram_scale[from] : 0.0f;
+                hi[k] = (_Float16)v, lo[k] = (_Float16)(v - (float)hi[k]);
+            }
+            char *to = a + (chunk / 4 * M + row) * kLine;
+            *reinterpret_cast<half8 *>(to + slot_of(row, chunk % 4) * 16) = hi;
+            *reinterpret_cast<half8 *>(to + slot_of(row, 4 + chunk % 4) * 16) = lo;
+            if (M % kPanel != 0) {
+                // (what products never write of the others)
+                const half8 zero = {};
+                if (chunk * 8 >= M)
+                    for (int t = 1; t < 3; ++t) {
+                        *reinterpret_cast<half8 *>(to + t * PAIR_SQUARE + slot_of(row, chunk % 4) * 16) = zero;
+                        *reinterpret_cast<half8 *>(to + t * PAIR_SQUARE + slot_of(row, 4 + chunk % 4) * 16) = zero;
+                    }
+            }
+        }
+        __syncthreads();
+        const bool there = wave < TILES;
+        int i = 0, j = 0;
+        if (there) tile(wave, &i, &j);
+        const FragmentPlace place(lane);
+        floatx4 v;
+        const auto multiply_pairs = [&](const char *l, const char *r) {
+            v = floatx4{0, 0, 0, 0};
+            if (!there) return;
+#pragma unroll
+            for (int k = 0; k < LINES; ++k) {
+                Fragment<half8> rows[1], cols;
+                place.load(rows[0], l + k * M * kLine, i);
+                place.load(cols, r + k * M * kLine, j);
+                floatx4 sum[1];
+                PairProduct::line(rows, cols, sum);
+                v += sum[0];
+            }
+        };
+        const auto keep = [&](char *to, float scale) {
+            if (!there) return;
+            half4 h, l;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) h[e] = (_Float16)(v[e] * scale);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) l[e] = (_Float16)__builtin_fmaf((float)h[e], -1.0f, v[e] * scale);
+            const uint2 hi = __builtin_bit_cast(uint2, h), lo = __builtin_bit_cast(uint2, l);
+            *reinterpret_cast<uint2 *>(to + pair_place(i, j, lane, false)) = hi;
+            *reinterpret_cast<uint2 *>(to + pair_place(i, j, lane, true)) = lo;
+            if (i != j) {
+                *reinterpret_cast<uint2 *>(to + turned_place(i, j, lane, false)) = turn_quad(hi, lane);
+                *reinterpret_cast<uint2 *>(to + turned_place(i, j, lane, true)) = turn_quad(lo, lane);
+            }
+        };
+        const auto result = [&](float scale) {
+            if (there) put_square(square, 16 * i + (lane & 15), 16 * j + 4 * (lane >> 4), i != j, v * scale);
+        };
+        for (int k = from; k < to; ++k) {
+            const float c0 = s.schedule[3 * k], c1 = s.schedule[3 * k + 1], c2 = s.schedule[3 * k + 2];
+            const float in_gram = 1.0f / s.gram_scale[k], in_step = 1.0f / s.step_scale[k];
+            char *step = k == from ? p : b;
+            multiply_pairs(a, a);
+            if (there) {
+                const half4 h = *reinterpret_cast<const half4 *>(a + pair_place(i, j, lane, false)), l = *reinterpret_cast<const half4 *>(a + pair_place(i, j, lane, true));
+                const int row = 16 * i + (lane & 15), col = 16 * j + 4 * (lane >> 4);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = c2 * in_gram * in_gram * v[e] + c1 * in_gram * ((float)h[e] + (float)l[e]) + (row == col + e ? c0 : 0.0f);
+            }
+            if (k + 1 == to && k == from) return result(1.0f), __syncthreads();
+            keep(step, s.step_scale[k]);   // (B and P are read by nobody at this point)
+            __syncthreads();
+            if (k > from) {
+                multiply_pairs(b, p);
+                if (k + 1 == to) {
+                    result(in_step / s.p_scale[k - 1]);
+                } else {
+                    __syncthreads();
+                    keep(p, in_step / s.p_scale[k - 1] * s.p_scale[k]);
+                }
+            }
+            if (k + 1 < to) {
+                multiply_pairs(step, a);
+                __syncthreads();
+                keep(a, in_step * in_gram * s.w_scale[k]);
+                __syncthreads();
+                multiply_pairs(a, step);
+                __syncthreads();
+                keep(a, in_step / s.w_scale[k] * s.gram_scale[k + 1]);
+            }
+            __syncthreads();
+        }
+    }
+
+    static __device__ __forceinline__ void put_square(float *a, int row, int col, bool mirror, const floatx4 &v)
+    {
+        *reinterpret_cast<floatx4 *>(a + row * PITCH + col) = v;
+        if (mirror)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) a[(col + e) * PITCH + row] = v[e];
     }
 
     // X <- P X over the columns in LDS; a wave takes 16 columns at a time, in place
@@ -364,15 +497,6 @@ __device__ __forceinline__ void scale_square(float *p, float f)
 }
 
 template <class S>
-__device__ __forceinline__ void put_symmetric(float *a, int row, int col, bool mirror, const floatx4 &v)
-{
-    *reinterpret_cast<floatx4 *>(a + row * S::PITCH + col) = v;
-    if (mirror)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) a[(col + e) * S::PITCH + row] = v[e];
-}
-
-template <class S>
 __device__ __forceinline__ void scale_columns(float *x, int pitch, int columns, float f)
 {
     for (int e = threadIdx.x; e < S::M * pitch; e += S::THREADS) x[e] *= f;
@@ -388,7 +512,9 @@ __global__ __launch_bounds__(S::THREADS) void whole_kernel(SmallArgs a)
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int64_t matrix = blockIdx.x;
     const int columns = a.columns, pitch = columns + 4, m = a.s.m();
-    float *gram = lds, *b = gram + S::SQUARE, *p = b + S::SQUARE, *x = p + S::SQUARE, *scratch = x + S::M * pitch;
+    float *gram = lds;
+    char *rest = reinterpret_cast<char *>(gram + S::SQUARE);
+    float *x = reinterpret_cast<float *>(rest + S::REST), *scratch = x + S::M * pitch;
     const bool large = S::load(
         x, pitch, a.s, matrix, 0, columns, a.by_fours, a.whole_fours, [&](int64_t at, int count, bool whole) { return fetch_four(a.u, a.s.dtype, at, count, whole, true); },
         [&](const Raw4 &v, int64_t at, int count, bool whole) { return direction_four(a.u, v, at, count, whole, true); });
@@ -400,12 +526,12 @@ __global__ __launch_bounds__(S::THREADS) void whole_kernel(SmallArgs a)
 #pragma unroll
         for (int q = 0; q < S::EACH; ++q) acc[q] = floatx4{0, 0, 0, 0};
         S::gram(x, pitch, columns, wave, lane, acc);
-        S::for_tiles(acc, wave, lane, scratch, [&](int row, int col, bool mirror, const floatx4 &v) { put_symmetric<S>(gram, row, col, mirror, v); });
+        S::for_tiles(acc, wave, lane, scratch, [&](int row, int col, bool mirror, const floatx4 &v) { S::put_square(gram, row, col, mirror, v); });
         float inverse = 1.0f;
         // (the raw direction times 2^-100 has a norm that is so many times smaller, eps with it)
         if (k == 0) inverse = normalise<S>(gram, m, 1.0, down ? a.s.eps * kDown : a.s.eps, &shared, lane);
         else __syncthreads();
-        S::polynomial(a, k, end, gram, b, p, wave, lane);
+        float *p = S::polynomial(a, k, end, gram, rest, wave, lane);
         if (k == 0) scale_square<S>(p, inverse);
         S::apply(p, x, pitch, columns, wave, lane);
         __syncthreads();
@@ -495,7 +621,7 @@ __global__ __launch_bounds__(S::THREADS) void polynomial_kernel(SmallArgs a)
     __shared__ double shared;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int64_t matrix = blockIdx.x;
-    float *gram = lds, *b = gram + S::SQUARE, *p = b + S::SQUARE;
+    float *gram = lds;
     const float *from = a.gram + matrix * a.parts * S::M * S::M;
     const unsigned *scaled = a.scaled + matrix * a.parts;
     const bool any = any_scaled<S>(a, scaled);
@@ -516,7 +642,7 @@ __global__ __launch_bounds__(S::THREADS) void polynomial_kernel(SmallArgs a)
     float inverse = 1.0f;
     if (a.from == 0) inverse = normalise<S>(gram, a.s.m(), 1.0, any ? a.s.eps * kDown : a.s.eps, &shared, lane);
     else __syncthreads();
-    S::polynomial(a, a.from, a.to, gram, b, p, wave, lane);
+    const float *p = S::polynomial(a, a.from, a.to, gram, reinterpret_cast<char *>(gram + S::SQUARE), wave, lane);
     if (any) inverse *= kDown;   // (the direction itself is not scaled)
     float *to = a.poly + matrix * S::M * S::M;
     for (int e = threadIdx.x; e < S::M * S::M; e += S::THREADS) to[e] = p[e / S::M * S::PITCH + e % S::M] * inverse;
@@ -571,11 +697,16 @@ int round16(int n) { return (n + 15) / 16 * 16; }
 size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 size_t square_bytes(int M) { return (size_t)M * (M + 4) * sizeof(float); }
+// one square of float32 and what polynomial() needs
+size_t polynomial_lds(int M)
+{
+    return square_bytes(M) + (M == 16 ? Small<16, 1>::REST : M == 32 ? Small<32, 1>::REST : M == 48 ? Small<48, 8>::REST : Small<64, 12>::REST);
+}
 size_t whole_lds(const MatrixShape &s)
 {
     const size_t M = round16(s.m());
     // (the waves of a matrix of one tile share its sums)
-    return 3 * square_bytes((int)M) + M * (round16(s.n()) + 4) * sizeof(float) + (M == 16 ? 4 * 1024 * sizeof(float) : 0);
+    return polynomial_lds((int)M) + M * (round16(s.n()) + 4) * sizeof(float) + (M == 16 ? 4 * 1024 * sizeof(float) : 0);
 }
 bool whole(const MatrixShape &s) { return s.n() <= 4096 && whole_lds(s) <= kSmallLds; }
 
@@ -622,12 +753,17 @@ int64_t matrices_at_once(const MatrixShape &s)
 
 // W: the shape of workgroups that have a matrix to themselves, S: of those that share one
 template <class W, class S>
-void launch(const MatrixShape &s, const UpdateArgs &update, SmallArgs a, char *ws, hipStream_t stream)
+void launch(const MatrixShape &s, const UpdateArgs &update, SmallArgs a, const ScheduleBounds &bounds, char *ws, hipStream_t stream)
 {
+    a.at_once = steps_at_once(s);
+    double factor = 1.0;
+    for (int k = 0; k < a.steps; ++k) {
+        const double r = bounds.singular[k], most = bounds.factor[k];
+        factor = k % a.at_once == 0 ? most : factor * most;
+        a.gram_scale[k] = pair_scale(r * r), a.step_scale[k] = pair_scale(most), a.w_scale[k] = pair_scale(most * r * r), a.p_scale[k] = pair_scale(factor);
+    }
     if (whole(s)) {
         a.columns = round16(s.n());
-        // (of a matrix that is about square a new Gram matrix, which is the more exact, costs no more than the products it saves)
-        a.at_once = s.n() <= 2 * s.m() ? kStepsAtOnce - 1 : kStepsAtOnce;
         a.by_fours = Divide::by(a.columns / 4);
         const size_t lds = whole_lds(s);
         if (lds > 65536) allow_large_lds(reinterpret_cast<const void *>(whole_kernel<W>), kSmallLds);
@@ -655,9 +791,10 @@ void launch(const MatrixShape &s, const UpdateArgs &update, SmallArgs a, char *w
         a.from = 0;
         gram_kernel<S><<<grid, S::THREADS, block + scratch, stream>>>(a);
         for (; a.from < a.steps; a.from = a.to) {
-            a.to = a.from + kStepsAtOnce < a.steps ? a.from + kStepsAtOnce : a.steps;
+            a.to = a.from + a.at_once < a.steps ? a.from + a.at_once : a.steps;
+            if (polynomial_lds(S::M) > 65536) allow_large_lds(reinterpret_cast<const void *>(polynomial_kernel<W>), (int)polynomial_lds(S::M));
             if (a.parts > kFewParts) sum_kernel<Sum><<<dim3(S::M * S::M / 64, (unsigned)count), Sum::THREADS, 0, stream>>>(a);
-            polynomial_kernel<W><<<(unsigned)count, W::THREADS, 3 * square, stream>>>(a);
+            polynomial_kernel<W><<<(unsigned)count, W::THREADS, polynomial_lds(S::M), stream>>>(a);
             if (a.to == a.steps) apply_kernel<S, true><<<grid, S::THREADS, square + block, stream>>>(a);
             else apply_kernel<S, false><<<grid, S::THREADS, square + block + scratch, stream>>>(a);
         }
@@ -682,6 +819,8 @@ void launch_ortho_small(const MatrixShape &s, int steps, const float *schedule, 
     a.u = u;
     a.steps = steps;
     for (int k = 0; k < 3 * steps; ++k) a.schedule[k] = schedule[k];
+    ScheduleBounds bounds;
+    (void)schedule_bounds(steps, schedule, &bounds);
     char *ws = static_cast<char *>(workspace);
     const auto aligned = [](const void *p, size_t item) { return reinterpret_cast<uintptr_t>(p) % (4 * item) == 0; };
     const size_t item = s.dtype == LMKAN_F32 ? 4 : 2;
@@ -692,17 +831,16 @@ void launch_ortho_small(const MatrixShape &s, int steps, const float *schedule, 
     // - / 44 / 53 / 89; 441 of 32 x 218 - / 36 / 32 / 40; one of 32 x 500 - / 49 / 35 / 29; 441 of 48 x 100 - / 45 / 39 / 47;
     // 25 of 48 x 500 - / 80 / 54 / 46; 1600 of 64 x 64 156 / 186; 169 of 144 x 64 43 / 38.
     const int m = s.m(), n = s.n();
-    if (m <= 16 && n <= 32) launch<Small<16, 1>, Small<16, 4>>(s, u, a, ws, stream);
-    else if (m <= 16 && n <= 160) launch<Small<16, 4>, Small<16, 4>>(s, u, a, ws, stream);
-    else if (m <= 16 && n <= 512) launch<Small<16, 8>, Small<16, 4>>(s, u, a, ws, stream);
-    else if (m <= 16) launch<Small<16, 16>, Small<16, 4>>(s, u, a, ws, stream);
-    else if (m <= 32 && n <= 64) launch<Small<32, 4>, Small<32, 4>>(s, u, a, ws, stream);
-    else if (m <= 32 && n <= 300) launch<Small<32, 8>, Small<32, 4>>(s, u, a, ws, stream);
-    else if (m <= 32) launch<Small<32, 16>, Small<32, 4>>(s, u, a, ws, stream);
-    else if (m <= 48 && n <= 200) launch<Small<48, 8>, Small<48, 4>>(s, u, a, ws, stream);
-    else if (m <= 48) launch<Small<48, 16>, Small<48, 4>>(s, u, a, ws, stream);
-    else if (n <= 64) launch<Small<64, 8>, Small<64, 4>>(s, u, a, ws, stream);
-    else launch<Small<64, 12>, Small<64, 4>>(s, u, a, ws, stream);
+    if (m <= 16 && n <= 32) launch<Small<16, 1>, Small<16, 4>>(s, u, a, bounds, ws, stream);
+    else if (m <= 16 && n <= 160) launch<Small<16, 4>, Small<16, 4>>(s, u, a, bounds, ws, stream);
+    else if (m <= 16 && n <= 512) launch<Small<16, 8>, Small<16, 4>>(s, u, a, bounds, ws, stream);
+    else if (m <= 16) launch<Small<16, 16>, Small<16, 4>>(s, u, a, bounds, ws, stream);
+    else if (m <= 32 && n <= 64) launch<Small<32, 4>, Small<32, 4>>(s, u, a, bounds, ws, stream);
+    else if (m <= 32 && n <= 300) launch<Small<32, 8>, Small<32, 4>>(s, u, a, bounds, ws, stream);
+    else if (m <= 32) launch<Small<32, 16>, Small<32, 4>>(s, u, a, bounds, ws, stream);
+    else if (m <= 48 && n <= 200) launch<Small<48, 8>, Small<48, 4>>(s, u, a, bounds, ws, stream);
+    else if (m <= 48) launch<Small<48, 16>, Small<48, 4>>(s, u, a, bounds, ws, stream);
+    else launch<Small<64, 12>, Small<64, 4>>(s, u, a, bounds, ws, stream);
 }
 
 }  // namespace lmkan
