@@ -410,3 +410,38 @@ def test_empty_batches(dev):
     assert pkg.lmkan_linear_i8(pkg.LinearDesc(8, 4), torch.empty((0, 8), device=dev), w, s).shape == (0, 4)
     codes, scale = pkg.lmkan_quantize_rows(torch.empty((0, 8), device=dev))
     assert codes.shape == (0, 8) and scale.shape == (0,)
+
+
+
+def test_the_example_trains_and_answers(dev, oracle):
+    """Every loss against the same training in 64 bits on the host.  A gradient is off by 1e-5 at most, which a
+    schedule's a^5 (485) enlarges in the smallest directions to 5e-3 of a step; so the way down is off by no more
+    than 1 % of itself.  Codes are off by 0.29 of 1 / 127 of the largest value, on both factors: for rows and
+    weights about normally distributed (largest 3 to 4 deviations) 1.2 % of the linear term."""
+    from paper_2509_07103_amd import preconditioned
+    steps, batch, n_in, n_out, grid, gamma = 40, 512, 32, 24, 7, 0.3
+    losses, off = preconditioned.run(steps, batch, n_in, n_out, grid)
+    g = torch.Generator().manual_seed(0)
+    weight = (torch.randn((n_out, n_in), generator=g) / n_in ** 0.5).double()[None]
+    nodes = ((grid + 1) ** 2, n_in // 2, n_out)
+    table = torch.zeros(nodes, dtype=torch.float64)
+    momenta = torch.zeros_like(table), torch.zeros_like(weight)
+    g = torch.Generator().manual_seed(1)
+    mix = torch.randn((n_in, n_out), generator=g) / n_in ** 0.5
+    want = []
+    for step in range(steps):
+        x = torch.randn((batch, n_in), generator=g)
+        rectified = torch.relu(x).double()
+        coef = table.float().view(grid + 1, grid + 1, n_in // 2, n_out).contiguous().numpy()
+        y = gamma * torch.from_numpy(np.asarray(oracle.forward(x.numpy(), coef, grid))).double()
+        d = y + rectified @ weight[0].t() - torch.tanh(x @ mix).double()
+        want.append(float(d.square().mean()))
+        d *= 2.0 / d.numel()
+        grad_table = oracle.backward_coef(x.numpy(), (gamma * d).float().contiguous().numpy(), grid)
+        grads = torch.from_numpy(np.asarray(grad_table)).double().view(nodes), (d.t() @ rectified)[None]
+        for w, m, gw in zip((table, weight), momenta, grads):
+            m.mul_(0.9).add_(0.1 * gw)
+            w.sub_(0.02 * (1.0 - step / steps) * _reference(0.9 * m + 0.1 * gw, pkg.QUINTIC_SCHEDULE))
+    bound = 1e-2 * (want[0] - min(want))
+    assert max(abs(a - b) for a, b in zip(losses, want)) <= bound
+    assert off < 0.03
