@@ -387,7 +387,7 @@ __global__ __launch_bounds__(64 * joiners<T>()) void join_kernel(ProductArgs a)
 
 // The steps on one Gram matrix of up to 128 x 128 in one launch: a workgroup per matrix, A and B in LDS, P in memory
 // (three matrices of pairs do not fit).  A wave has one 32 x 32 tile of the upper triangle; all read, then all write,
-// so that a product may take the place of a factor.  A product takes about 2 us, a launch for it 6.
+// so that a product may take the place of a factor.  A product takes 3.7 us of 128 x 128, a launch for it 6.
 constexpr int kSide = 128, kSideTiles = kSide / 32, kChainWaves = kSideTiles * (kSideTiles + 1) / 2;
 constexpr int kSideBytes = kSide / kPanel * kSide * kLine;
 
@@ -578,15 +578,17 @@ void launch_product_with(ProductArgs &a, hipStream_t stream)
 }
 
 // The larger the tile, the less is read per product and the more of a tile that straddles the diagonal or the end is
-// wasted.  Measured (us, tiles of 64 / 128 / 256): 441 of 250 x 333 1900 / 1980 / 2400; 289 of 512 x 1024 7550 /
-// 6240 / 6540; one of 4096 x 4096 6500 / 4900 / 4350; one of 1024 x 1024 348 / 662 / 1020.
+// wasted.  Measured (us, tiles of 64 / 128 / 256): 441 of 250 x 333 1720 / 1640 / 1800; 289 of 512 x 1024 7000 /
+// 5480 / 5800; one of 4096 x 4096 5900 / 4770 / 4380; one of 1024 x 1024 300 / 563 / 997.  Rows of 193 to 256 fill two
+// tiles of 128, which pays where there are tiles for one and a half turns of the units (two workgroups each): 441 of
+// 200 x 300 1289 / 1178, 300 of 193 x 386 962 / 907, but 200 of 256 x 512 858 / 964.
 template <int FINISH>
 void launch_product(ProductArgs &a, hipStream_t stream)
 {
     const int64_t n = a.matrices * a.problems;
     const int shorter = a.s.m();
     if (shorter > 512 && tiles_of(a.p[0], 256) * n >= kUnits / 2) launch_product_with<Tile256, FINISH>(a, stream);
-    else if (shorter > 256 && tiles_of(a.p[0], 128) * n >= 2 * kUnits) launch_product_with<Tile128, FINISH>(a, stream);
+    else if (shorter > 192 && tiles_of(a.p[0], 128) * n >= (shorter > 256 ? 2 : 3) * kUnits) launch_product_with<Tile128, FINISH>(a, stream);
     else if (tiles_of(a.p[0], 64) * n > kUnits) launch_product_with<Tile64, FINISH>(a, stream);
     else launch_product_with<Tile64Alone, FINISH, true>(a, stream);
 }
@@ -631,10 +633,13 @@ Layout layout_of(const MatrixShape &s, int64_t count)
 //   60 x 60      0.84  1.70  2.94            |  128 x 2000    0.70  2.28
 //   48 x 100     0.82  1.04  3.4             |  192 x 1537    0.58  2.31
 //   64 x 144     0.82  0.73  3.3             |  193 x 400     0.66  1.37
-//   48 x 400      -    0.84  1.99            |  193 x 1600    0.57  2.34
-//   33 x 270      -     -    1.59            |  256 x 256      -    1.20
-//   16 x 200      -     -    1.16            |  256 x 2100     -    1.87
+//   48 x 400      -    0.84  1.99            |  250 x 333      -    1.14
+//   33 x 270      -    1.82  1.59            |  256 x 2100    0.52  1.87
+//   16 x 200      -     -    1.16            |  256 x 256      -    1.20
 //   100 x 100    0.52  1.08  1.89            |  320 x 3000     -    1.03
+//   33 x 66       -    1.63   -              |  257 x 2200     -    1.31
+//   40 x 80      0.90   -     -              |  193 x 386      -    1.43
+//   41 x 82       -    1.30   -              |  32 x 1500      -    1.47
 int steps_at_once(const MatrixShape &s)
 {
     const int m = s.m(), n = s.n();

@@ -826,10 +826,10 @@ void launch_ortho_small(const MatrixShape &s, int steps, const float *schedule, 
     const size_t item = s.dtype == LMKAN_F32 ? 4 : 2;
     a.whole_fours = s.cols % 4 == 0 && aligned(u.grad, item) && aligned(u.out, item) && aligned(u.momentum, 4) && aligned(u.weight, 4);
     // Waves of a workgroup that has a matrix to itself: more for longer rows, fewer where one is small enough for several
-    // workgroups a compute unit.  Measured (us, 1 / 4 / 8 / 16 waves, 64: 8 / 12): 1681 of 8 x 16 9.7 / 16 / 23 / 52; 1000 of
-    // 16 x 100 22 / 19 / 20 / 37; 400 of 10 x 300 42 / 19 / 17 / 24; 25 of 12 x 900 114 / 36 / 24 / 20; 1600 of 30 x 60
-    // - / 44 / 53 / 89; 441 of 32 x 218 - / 36 / 32 / 40; one of 32 x 500 - / 49 / 35 / 29; 441 of 48 x 100 - / 45 / 39 / 47;
-    // 25 of 48 x 500 - / 80 / 54 / 46; 1600 of 64 x 64 156 / 186; 169 of 144 x 64 43 / 38.
+    // workgroups a compute unit.  Measured (us, 1 / 4 / 8 / 16 waves): 1681 of 8 x 16 8.9 / 14 / 22 / 50; 1000 of
+    // 16 x 100 18 / 13 / 19 / 33; 400 of 10 x 300 27 / 20 / 21 / 22; 25 of 12 x 900 68 / 24 / 17 / 15; 1600 of 30 x 60
+    // - / 40 / 48 / 79; 441 of 32 x 218 - / 35 / 31 / 41; one of 32 x 500 - / 33 / 26 / 23; 441 of 48 x 100 - / - / 35 / 45;
+    // 25 of 48 x 500 - / - / 51 / 46; and 1600 of 64 x 64 takes 172, 169 of 144 x 64 34 (twelve waves).
     const int m = s.m(), n = s.n();
     if (m <= 16 && n <= 32) launch<Small<16, 1>, Small<16, 4>>(s, u, a, bounds, ws, stream);
     else if (m <= 16 && n <= 160) launch<Small<16, 4>, Small<16, 4>>(s, u, a, bounds, ws, stream);

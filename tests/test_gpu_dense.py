@@ -445,3 +445,9 @@ def test_the_example_trains_and_answers(dev, oracle):
     bound = 1e-2 * (want[0] - min(want))
     assert max(abs(a - b) for a, b in zip(losses, want)) <= bound
     assert off < 0.03
+
+
+def test_many_matrices_of_two_larger_tiles(dev):
+    x = _gradient(260, 193, 200, seed=41)
+    got = pkg.lmkan_orthogonalize(pkg.MatrixDesc(260, 193, 200), x.to(dev))
+    assert _far(got, _reference(x, pkg.QUINTIC_SCHEDULE)) <= TOL
