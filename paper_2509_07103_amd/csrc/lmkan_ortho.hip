@@ -7,7 +7,7 @@
 // several steps can be taken on m x m matrices alone,
 //   A_{k+1} = B_k A_k B_k,   P_{k+1} = B_k P_k,
 // and then X_{k+s} = P X_k.  All products but that one are symmetric: half their tiles are computed and mirrored.
-// Five steps take 15 m^2 n + 5 m^3 multiply-adds as written, 9 m^2 n + 11 m^3 two at a time and 6 m^2 n + 14 m^3 three
+// Five steps take 15 m^2 n + 5 m^3 operations as written, 9 m^2 n + 11 m^3 two at a time and 6 m^2 n + 14 m^3 three
 // at a time, and X is read and written five, three or two times.  An error of A is relative to its largest eigenvalue
 // and grows by up to a^2 (11.9) a step where the eigenvalue is small, which is why not all are taken at once, and
 // steps_at_once() chooses.
