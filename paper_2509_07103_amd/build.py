@@ -91,3 +91,4 @@ if __name__ == "__main__":
     from paper_2509_07103_amd import check_codegen
     check_codegen.check(verbose=True)
     check_codegen.check(verbose=True, sources=check_codegen.SPARSE_SOURCES)
+    check_codegen.check_lds_loads(verbose=True)

@@ -131,9 +131,89 @@ def check(verbose: bool = False, sources=CHECKED_SOURCES) -> dict[str, int]:
     return counts
 
 
+# wait states that the instruction set asks for before a load straight to LDS
+AFTER_M0, AFTER_VECTOR_WRITE = 1, 5
+
+
+def _scalars(text: str) -> frozenset[str]:
+    """Scalar registers named in `text`."""
+    out = set(re.findall(r"\b(?:s\d+|m0|vcc_lo|vcc_hi)\b", text))
+    if re.search(r"\bvcc\b", text):
+        out |= {"vcc_lo", "vcc_hi"}
+    for m in re.finditer(r"\bs\[(\d+):(\d+)\]", text):
+        out |= {f"s{i}" for i in range(int(m.group(1)), int(m.group(2)) + 1)}
+    return frozenset(out)
+
+
+def check_lds_load_waits(text: str) -> dict[str, int]:
+    """Every path to every load to LDS in a disassembly; returns {symbol: loads}, raises on one that comes too soon."""
+    counts, bad = {}, []
+    for part in re.split(r"(?m)^(?=<[^>]+>:$)", re.sub(r"(?m)^<(L\d+)>:", r"\1:", text)):
+        head, _, body = part.partition("\n")
+        symbol = head.strip("<>:\n ")
+        code = [line for line in (re.split(r"//|;", l)[0].strip() for l in body.split("\n")) if line]
+        label_at = {l[:-1]: i for i, l in enumerate(code) if l.endswith(":")}
+        jumps: dict[int, list[int]] = {}
+        for i, l in enumerate(code):
+            if re.match(r"s_c?branch", l) and l.split()[1] in label_at:
+                jumps.setdefault(label_at[l.split()[1]], []).append(i)
+        for at, load in enumerate(code):
+            if not (re.match(r"global_load_lds_", load) or re.match(r"buffer_load_.*\blds$", load)):
+                continue
+            counts[symbol] = counts.get(symbol, 0) + 1
+            base = _scalars(load)
+            todo, seen = [(at, 0)], set()
+            while todo:
+                i, waited = todo.pop()
+                before = list(jumps.get(i, []))
+                if i > 0 and not re.match(r"s_branch|s_endpgm|s_setpc", code[i - 1]):
+                    before.append(i - 1)
+                for j in before:
+                    l = code[j]
+                    if (j, waited) in seen:
+                        continue
+                    seen.add((j, waited))
+                    if l.endswith(":"):
+                        todo.append((j, waited))
+                        continue
+                    operands = (l.split(None, 1) + [""])[1].split(",")
+                    written = _scalars(",".join(operands[:2 if re.match(r"v_\w*(_co_|div_scale)", l) else 1]))
+                    if waited < AFTER_M0 and "m0" in written and l.startswith("s_"):
+                        bad.append(f"{symbol}: '{load}' follows '{l}' without a wait state")
+                    elif l.startswith("v_") and written & base:
+                        bad.append(f"{symbol}: '{load}' follows '{l}' after {waited} wait states")
+                    nop = re.match(r"s_nop (\d+)", l)
+                    if waited + (int(nop.group(1)) + 1 if nop else 1) < AFTER_VECTOR_WRITE:
+                        todo.append((j, waited + (int(nop.group(1)) + 1 if nop else 1)))
+    if bad:
+        raise RuntimeError(f"{len(bad)} loads to LDS come too soon:\n  " + "\n  ".join(bad[:8]))
+    return counts
+
+
+def check_lds_loads(library: str | None = None, verbose: bool = False) -> dict[str, int]:
+    """Disassembles the device code of the built library and checks it."""
+    objdump = os.path.join(os.path.dirname(os.path.dirname(hip_build.HIPCC)), "llvm", "bin", "llvm-objdump")
+    counts: dict[str, int] = {}
+    with tempfile.TemporaryDirectory() as tmp:
+        copy = os.path.join(tmp, "library.so")
+        os.symlink(os.path.abspath(library or hip_build.LIB), copy)
+        subprocess.run([objdump, "--offloading", copy], check=True, capture_output=True, cwd=tmp)
+        for name in sorted(os.listdir(tmp)):
+            if "gfx950" in name:
+                res = subprocess.run([objdump, "-d", "--no-show-raw-insn", "--no-leading-addr", "--symbolize-operands",
+                                      "--mcpu=gfx950", os.path.join(tmp, name)], check=True, capture_output=True, text=True)
+                counts.update(check_lds_load_waits(res.stdout))
+    if not counts:
+        raise RuntimeError("no loads to LDS found; the check no longer sees the kernels")
+    if verbose:
+        print(f"codegen check: {sum(counts.values())} loads to LDS in {len(counts)} kernels, none of them too soon", flush=True)
+    return counts
+
+
 if __name__ == "__main__":
     check(verbose=True)
     check(verbose=True, sources=SPARSE_SOURCES)
+    check_lds_loads(verbose=True)
 
 
 # Kernels that must not touch scratch memory at all (substrings of the mangled names), and the

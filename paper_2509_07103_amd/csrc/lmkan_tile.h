@@ -51,10 +51,12 @@ __device__ __forceinline__ V uniform(V v)
 
 // 16 bytes per lane from global memory (a wave-uniform base, 32 bits of offset per lane) to LDS at lds + 16 lane.
 // The compiler does not know of the load (it cannot make reads of the other buffer wait for it); it is awaited
-// with landed().  m0 is a reserved register to the compiler, which sets it before any use of its own.
+// with landed().  m0 is a reserved register to the compiler, which sets it before any use of its own.  The instruction
+// set asks for one wait state between a scalar write of m0 and a load that takes its place from it; the compiler adds
+// none inside a statement of ours (s_nop: without it a line may go to the place of the one before).
 __device__ __forceinline__ void load_to_lds(const void *base, unsigned offset, unsigned lds)
 {
-    asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" :
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" :
                  : "v"(offset), "s"(uniform(base)), "s"(uniform(lds)) : "memory");
 }
 
