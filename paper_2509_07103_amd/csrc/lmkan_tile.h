@@ -96,6 +96,15 @@ struct Operand {
     int limit;       // codes: the last 16 bytes of a row; lines that end beyond read them there (the other operand is zero)
 };
 
+// Where a lane's 16 bytes of the eight lines from row r0 on lie in a panel, for a tile of N rows that exist up to row
+// `last`; lanes beyond the last line read its last bytes.  (A panel may have 2^26 lines, a tile no more than N.)
+template <int N>
+__host__ __device__ __forceinline__ unsigned panel_offset(int last, int r0, int lane)
+{
+    const unsigned end = (unsigned)(last < N - 1 ? last : N - 1) * kLine + kLine - 16, at = (unsigned)(r0 * kLine + lane * 16);
+    return at < end ? at : end;
+}
+
 // Brings the lines of a stage of one operand to LDS, N rows, from wave `wave` of WAVES.
 template <int N, int WAVES>
 __device__ __forceinline__ void stage_operand(const Operand &o, int stage, unsigned lds, int wave, int lane)
@@ -107,10 +116,7 @@ __device__ __forceinline__ void stage_operand(const Operand &o, int stage, unsig
         const int r0 = (g * WAVES + wave) * 8;
         unsigned at;
         if (o.panels) {
-            // one piece; lanes beyond its end read its last bytes
-            const unsigned end = (unsigned)o.last * kLine + kLine - 16;
-            at = (unsigned)(r0 * kLine + lane * 16);
-            at = at < end ? at : end;
+            at = panel_offset<N>(o.last, r0, lane);
         } else {
             const int r = r0 + (lane >> 3), c = slot_of(r, lane & 7) * 16, most = o.limit - stage * kLine;
             at = (unsigned)(r < o.last ? r : o.last) * o.pitch + (unsigned)(c < most ? c : most);
