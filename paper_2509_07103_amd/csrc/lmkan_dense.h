@@ -49,6 +49,9 @@ int steps_at_once(const MatrixShape &s);
 // the power of two that brings values up to `bound` to the upper end of float16's range (65504), with room for rounding
 float pair_scale(double bound);
 
+// Workgroups of a launch at most, of up to 1024 threads: the runtime takes fewer than 2^32 threads along a dimension
+constexpr int64_t kMostGroups = 1 << 21;
+
 size_t ortho_workspace_bytes(const MatrixShape &s);
 void launch_ortho(const MatrixShape &s, int steps, const float *schedule, const UpdateArgs &u, void *workspace,
                   hipStream_t stream);

@@ -72,10 +72,11 @@ struct AlignArgs {
     const int8_t *w;
     int n_in, n_out, pitch;
     int8_t *to;
+    int64_t first;   // block of the launch's first
 };
 __device__ __forceinline__ void align_rows(const AlignArgs &a, unsigned block)
 {
-    const int64_t e = (int64_t)block * 256 + threadIdx.x;
+    const int64_t e = (a.first + block) * 256 + threadIdx.x;
     const int64_t row = e / (a.pitch / 4);
     const int k = (int)(e - row * (a.pitch / 4)) * 4;
     if (row >= a.n_out) return;
@@ -636,11 +637,19 @@ void launch_quantize(QuantizeArgs a, hipStream_t stream)
 {
     // a wave a row while the row fits what its lanes hold
     const bool wave = a.cols <= 64 * 4 * kHeld;
-    a.row_blocks = (unsigned)(wave ? (a.rows + 3) / 4 : a.rows);
-    const int64_t dwords = a.align.w ? (int64_t)a.align.n_out * (a.align.pitch / 4) : 0;
-    const unsigned blocks = a.row_blocks + (unsigned)((dwords + 255) / 256);
-    if (wave) quantize_kernel<DTYPE, 64><<<blocks, 256, 0, stream>>>(a);
-    else quantize_kernel<DTYPE, 256><<<blocks, 256, 0, stream>>>(a);
+    const int64_t rows = a.rows, most = kMostGroups * (wave ? 4 : 1), item = DTYPE == LMKAN_F32 ? 4 : 2;
+    const int64_t aligning = a.align.w ? ((int64_t)a.align.n_out * (a.align.pitch / 4) + 255) / 256 : 0;
+    for (int64_t row = 0, block = 0; row < rows || block < aligning; row += a.rows) {
+        a.rows = rows - row < most ? rows - row : most;
+        a.row_blocks = (unsigned)(wave ? (a.rows + 3) / 4 : a.rows);
+        const int64_t room = kMostGroups - a.row_blocks, now = aligning - block < room ? aligning - block : room;
+        const unsigned blocks = a.row_blocks + (unsigned)now;
+        if (wave) quantize_kernel<DTYPE, 64><<<blocks, 256, 0, stream>>>(a);
+        else quantize_kernel<DTYPE, 256><<<blocks, 256, 0, stream>>>(a);
+        a.x = static_cast<const char *>(a.x) + a.rows * a.cols * item;
+        a.codes += a.rows * a.pitch, a.scale += a.rows;
+        block += now, a.align.first = block;
+    }
 }
 
 void quantize(int64_t rows, int cols, int pitch, int dtype, bool relu, const void *x, int8_t *codes, float *scale, const AlignArgs &align,

@@ -741,10 +741,10 @@ Layout layout_of(const MatrixShape &s, int64_t count)
     return l;
 }
 
-// matrices that share the workspace at a time: 512 M elements, and what a grid takes
+// matrices of a launch; those that share the workspace at a time: 512 M elements, and what a grid takes
 int64_t matrices_at_once(const MatrixShape &s)
 {
-    if (whole(s)) return s.batch;
+    if (whole(s)) return s.batch < kMostGroups ? s.batch : kMostGroups;
     int64_t most = ((int64_t)512 << 20) / s.elems();
     most = most < 1 ? 1 : most > 32768 ? 32768 : most;
     const int64_t parts = (s.batch + most - 1) / most;
@@ -762,31 +762,36 @@ void launch(const MatrixShape &s, const UpdateArgs &update, SmallArgs a, const S
         factor = k % a.at_once == 0 ? most : factor * most;
         a.gram_scale[k] = pair_scale(r * r), a.step_scale[k] = pair_scale(most), a.w_scale[k] = pair_scale(most * r * r), a.p_scale[k] = pair_scale(factor);
     }
+    const int64_t most_matrices = matrices_at_once(s);
+    const size_t item = s.dtype == LMKAN_F32 ? 4 : 2;
+    const auto from_matrix = [&](int64_t first) {
+        const int64_t skip = first * s.elems();
+        a.u.grad = static_cast<const char *>(update.grad) + skip * item;
+        a.u.momentum = update.momentum ? update.momentum + skip : nullptr;
+        a.u.weight = update.weight ? update.weight + skip : nullptr;
+        a.u.out = update.out ? static_cast<char *>(update.out) + skip * item : nullptr;
+        return s.batch - first < most_matrices ? s.batch - first : most_matrices;
+    };
     if (whole(s)) {
         a.columns = round16(s.n());
         a.by_fours = Divide::by(a.columns / 4);
         const size_t lds = whole_lds(s);
         if (lds > 65536) allow_large_lds(reinterpret_cast<const void *>(whole_kernel<W>), kSmallLds);
-        whole_kernel<W><<<(unsigned)s.batch, W::THREADS, lds, stream>>>(a);
+        for (int64_t first = 0; first < s.batch; first += most_matrices)
+            whole_kernel<W><<<(unsigned)from_matrix(first), W::THREADS, lds, stream>>>(a);
         return;
     }
     typedef Small<S::M, 16> Sum;
-    const int64_t most = matrices_at_once(s);
-    const size_t item = s.dtype == LMKAN_F32 ? 4 : 2;
     a.columns = columns_of(S::M);
     a.by_fours = Divide::by(a.columns / 4);
     const size_t block = (size_t)S::M * (a.columns + 4) * sizeof(float), scratch = 4 * S::THREADS * sizeof(float), square = square_bytes(S::M);
-    for (int64_t first = 0; first < s.batch; first += most) {
-        const int64_t count = s.batch - first < most ? s.batch - first : most, skip = first * s.elems();
+    for (int64_t first = 0; first < s.batch; first += most_matrices) {
+        const int64_t count = from_matrix(first);
         const Layout l = layout_of(s, count);
         a.parts = parts_of(s, count);
         a.gram = reinterpret_cast<float *>(ws + l.gram), a.scaled = reinterpret_cast<unsigned *>(ws + l.scaled);
         a.sum = reinterpret_cast<double *>(ws + l.sum);
         a.poly = reinterpret_cast<float *>(ws + l.poly), a.x = reinterpret_cast<float *>(ws + l.x);
-        a.u.grad = static_cast<const char *>(update.grad) + skip * item;
-        a.u.momentum = update.momentum ? update.momentum + skip : nullptr;
-        a.u.weight = update.weight ? update.weight + skip : nullptr;
-        a.u.out = update.out ? static_cast<char *>(update.out) + skip * item : nullptr;
         const dim3 grid(a.parts, (unsigned)count);
         a.from = 0;
         gram_kernel<S><<<grid, S::THREADS, block + scratch, stream>>>(a);

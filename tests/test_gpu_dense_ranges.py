@@ -54,3 +54,59 @@ def test_rows_of_more_than_2_to_the_25(dev):
                 o, w = (t[:, part].reshape(m, -1, min(64, part.stop - part.start)).square().sum(dim=(0, 2)) for t in (off, want))
                 worst = max(worst, float((o / w).max()) ** 0.5)
     assert worst <= TOL
+
+
+def test_more_matrices_than_a_launch_takes(dev):
+    """2^21 matrices of one workgroup each to a launch: the second launch starts where the first ended."""
+    n = (1 << 21) + 77
+    g = torch.Generator(device=dev).manual_seed(2)
+    x = torch.randn((n, 1, 3), device=dev, generator=g)
+
+    def steps(v):
+        v = v / (v.norm(dim=2, keepdim=True) + 1e-7)
+        for a, b, c in pkg.QUINTIC_SCHEDULE:
+            s2 = v.square().sum(dim=2, keepdim=True)
+            v = (a + b * s2 + c * s2 * s2) * v
+        return v
+    want = steps(x.double())
+    got = pkg.lmkan_orthogonalize(pkg.MatrixDesc(n, 1, 3), x)
+    assert float(((got.double() - want).norm(dim=2) / want.norm(dim=2)).max()) <= TOL
+    m, w = torch.zeros_like(x), x.clone()
+    pkg.lmkan_muon_step(pkg.MatrixDesc(n, 1, 3), pkg.MuonParams(lr=0.5, momentum=0.5, nesterov=False), x, m, w)
+    assert torch.equal(m, 0.5 * x)
+    want = steps(0.5 * x.double())
+    off = (w.double() - (x.double() - 0.5 * want)).norm(dim=2)
+    assert bool((off <= 4 * 2.0 ** -24 * x.double().norm(dim=2) + 0.5 * TOL * want.norm(dim=2)).all())
+
+
+@pytest.mark.parametrize("rows,cols", [((1 << 23) + 21, 3), ((1 << 21) + 13, 2049)])
+def test_more_rows_than_a_launch_takes(dev, rows, cols):
+    """Four rows of up to 2048 values to a workgroup, or one longer one, 2^21 workgroups to a launch."""
+    g = torch.Generator(device=dev).manual_seed(3)
+    x = torch.empty((rows, cols), dtype=torch.float16, device=dev).normal_(generator=g)
+    codes, scale = pkg.lmkan_quantize_rows(x)
+    for at in range(0, rows, 1 << 19):
+        v = x[at:at + (1 << 19)].float()
+        top = v.abs().amax(dim=1, keepdim=True)
+        full = torch.full_like(top, 127.0)
+        f = torch.where(top > 0, full / top, torch.zeros_like(top))
+        assert torch.equal(codes[at:at + (1 << 19)].float(), torch.round(v * f))
+        assert torch.equal(scale[at:at + (1 << 19)], (top / full)[:, 0])
+
+
+def test_linear_i8_of_more_rows_and_weights_than_a_launch_takes(dev):
+    """Rows to codes in two launches, and weights to aligned rows in two."""
+    for batch, n_in, n_out in (((1 << 23) + 21, 3, 2), (70, 2051, (1 << 20) + 5)):
+        g = torch.Generator(device=dev).manual_seed(4)
+        x = torch.empty((batch, n_in), dtype=torch.float16, device=dev).normal_(generator=g)
+        w = torch.randint(-127, 128, (n_out, n_in), device=dev, generator=g, dtype=torch.int8)
+        ws = torch.rand((n_out,), device=dev, generator=g)
+        got = pkg.lmkan_linear_i8(pkg.LinearDesc(n_in, n_out, pkg.LMKAN_F16, pkg.LMKAN_F32), x, w, ws)
+        codes, scale = pkg.lmkan_quantize_rows(x)
+        codes = codes.float()                            # sums below 2^24 or exact in float64
+        for at in range(0, n_out, 1 << 17):
+            for r in range(0, batch, 1 << 21):
+                part = slice(r, r + (1 << 21)), slice(at, at + (1 << 17))
+                want = codes[part[0]].double() @ w[part[1]].double().t().contiguous() * scale[part[0]].double()[:, None] * ws[part[1]].double()
+                off = (got[part].double() - want).abs()
+                assert bool((off <= 4 * 2.0 ** -24 * want.abs() + 1e-30).all())
