@@ -2,14 +2,14 @@
 
 Tolerances are those of test_gpu_dense.py: 4e-5 of the result's norm for five steps, and the unit roundoff of a
 16-bit result."""
+import numpy as np
 import pytest
 import torch
 
 import paper_2509_07103_amd as pkg
+from test_gpu_dense import CODE, DT, TOL, UNIT, _codes, _far, _gradient, _reference, _rows
 
 pytestmark = pytest.mark.gpu
-
-TOL = 4e-5
 
 
 @pytest.fixture(scope="module")
@@ -110,3 +110,73 @@ def test_linear_i8_of_more_rows_and_weights_than_a_launch_takes(dev):
                 want = codes[part[0]].double() @ w[part[1]].double().t().contiguous() * scale[part[0]].double()[:, None] * ws[part[1]].double()
                 off = (got[part].double() - want).abs()
                 assert bool((off <= 4 * 2.0 ** -24 * want.abs() + 1e-30).all())
+
+
+def _on_device(x, schedule, eps=1e-7):
+    """_reference for larger shapes: the same steps in float64 on the device, factors contiguous."""
+    x = x.double()
+    flip = x.shape[1] > x.shape[2]
+    x = x.mT.contiguous() if flip else x
+    x = x / (x.square().sum(dim=(1, 2), keepdim=True).sqrt() + eps)
+    for a, b, c in np.asarray(schedule, dtype=np.float32).astype(np.float64).reshape(-1, 3):
+        gram = x @ x.mT.contiguous()
+        x = a * x + (b * gram + c * gram @ gram) @ x
+    return x.mT.contiguous() if flip else x
+
+
+# short sides above 512 with 128 tiles of 256 or more, 257 to 512 with 512 tiles of 128; joins of both
+@pytest.mark.parametrize("shape", [(1, 4097, 4099), (16, 1025, 1100), (40, 700, 513), (100, 300, 420), (90, 500, 290)],
+                         ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_orthogonalize_in_the_larger_tiles(dev, shape, dtype):
+    g = torch.Generator(device=dev).manual_seed(sum(shape))
+    x = torch.randn(shape, device=dev, generator=g)
+    x += 0.5 * torch.randn((*shape[:2], 2), device=dev, generator=g) @ torch.randn((shape[0], 2, shape[2]), device=dev, generator=g)
+    x = x.to(DT[dtype])
+    got = pkg.lmkan_orthogonalize(pkg.MatrixDesc(*shape, dtype=CODE[dtype]), x)
+    assert _far(got, _on_device(x, pkg.QUINTIC_SCHEDULE).cpu()) <= TOL + (UNIT[dtype] if dtype != "f32" else 0.0)
+    assert torch.equal(got, pkg.lmkan_orthogonalize(pkg.MatrixDesc(*shape, dtype=CODE[dtype]), x))
+
+
+@pytest.mark.parametrize("shape", [(16500, 65, 66), (16390, 70, 68), (32800, 1, 4097), (32780, 4100, 2)], ids=lambda s: "x".join(map(str, s)))
+def test_batches_in_parts(dev, shape):
+    """More matrices than share the workspace at a time."""
+    g = torch.Generator(device=dev).manual_seed(6)
+    grad = torch.randn(shape, device=dev, generator=g).to(torch.bfloat16)
+    m, w = torch.randn(shape, device=dev, generator=g), torch.zeros(shape, device=dev)
+    held = m.clone()
+    p = pkg.MuonParams(lr=0.5, momentum=0.5, nesterov=True)
+    pkg.lmkan_muon_step(pkg.MatrixDesc(*shape, dtype=pkg.LMKAN_BF16), p, grad, m, w)
+    for at in range(0, shape[0], 2048):
+        part = slice(at, at + 2048)
+        moved = 0.5 * held[part].double() + 0.5 * grad[part].double()
+        assert float((m[part].double() - moved).abs().max()) <= 4 * 2.0 ** -24 * float(held.abs().max() + grad.abs().max())
+        want = -0.5 * _on_device(0.5 * moved + 0.5 * grad[part].double(), pkg.QUINTIC_SCHEDULE)
+        assert _far(w[part], want.cpu()) <= TOL
+
+
+@pytest.mark.parametrize("batch,n_in,n_out", [(8200, 1000, 1030), (4097, 2050, 2052), (9001, 16, 1025), (3000, 333, 4101)])
+@pytest.mark.parametrize("x_dtype,y_dtype", [("f32", "f32"), ("bf16", "bf16"), ("f16", "f32")])
+@pytest.mark.parametrize("relu,bias,beta", [(False, False, 0.0), (True, True, 0.25)])
+def test_linear_i8_in_the_larger_tiles(dev, batch, n_in, n_out, x_dtype, y_dtype, relu, bias, beta):
+    """512 tiles of 128 and more."""
+    g = torch.Generator().manual_seed(batch + n_in + n_out)
+    x = _rows(batch, n_in, 41, x_dtype)
+    w = torch.randint(-127, 128, (n_out, n_in), generator=g, dtype=torch.int8)
+    ws = (0.5 + torch.rand((n_out,), generator=g)) / (73.0 * n_in ** 0.5)
+    b = torch.randn((n_out,), generator=g).to(dev) if bias else None
+    y = torch.randn((batch, n_out), generator=g).to(DT[y_dtype]).to(dev) if beta else None
+    codes, _ = _codes(x, relu)
+    top = x.float().clamp(min=0) if relu else x.float().abs()
+    want = torch.from_numpy(codes).to(dev).double() @ w.to(dev).double().t().contiguous()
+    want *= (top.amax(dim=1).double()[:, None] / 127.0).to(dev) * ws.to(dev).double()
+    size = want.abs()
+    if bias:
+        want, size = want + b.double(), size + b.double().abs()
+    if beta:
+        want, size = want + beta * y.double(), size + beta * y.double().abs()
+    got = pkg.lmkan_linear_i8(pkg.LinearDesc(n_in, n_out, CODE[x_dtype], CODE[y_dtype], relu=relu), x.to(dev), w.to(dev), ws.to(dev),
+                              bias=b, beta=beta, y=y)
+    most = 8 * 2.0 ** -24 * size + (UNIT[y_dtype] if y_dtype != "f32" else 0.0) * want.abs() * 1.001
+    off = (got.double() - want).abs()
+    assert bool((off <= most + 1e-30).all()), float((off / (most + 1e-30)).max())
