@@ -46,8 +46,20 @@ bool schedule_bounds(int steps, const float *schedule, ScheduleBounds *bounds);
 // Steps that are taken on one Gram matrix before the polynomial is applied and a new one is formed (lmkan_ortho.hip)
 int steps_at_once(const MatrixShape &s);
 
-// the power of two that brings values up to `bound` to the upper end of float16's range (65504), with room for rounding
+// The power of two that brings values up to `bound` to the upper end of float16's range (65504), with room for rounding.
+// Bounds end at 2^-113, so that every scale and every inverse of one is a float32 value: what a schedule takes below
+// that has fewer bits, and none from 2^-152 on.
 float pair_scale(double bound);
+
+// A step on a Gram matrix A held in pairs: what takes products of pairs to pairs of their results.  (Worked out in
+// float64: of scales that are far apart no two may be multiplied in float32 first.)
+struct ChainStep {
+    float a, b, c;                   // B = a I + b A + c A^2, from pairs of A and their products
+    float to_w, to_gram, to_p;       // B A, (B A) B and B P
+    float step_inverse, p_inverse;   // of the scales of B, and of P before the step
+};
+// `factor`: the product of the factors of the steps before on the same Gram matrix, and of this one afterwards
+ChainStep chain_step(const ScheduleBounds &bounds, const float *schedule, int k, double *factor);
 
 // Workgroups of a launch at most, of up to 1024 threads: the runtime takes fewer than 2^32 threads along a dimension
 constexpr int64_t kMostGroups = 1 << 21;

@@ -196,8 +196,9 @@ struct Product {
     PairMatrix rows, cols;     // the factors: by the rows and by the columns of the output
     PairMatrix out, mirror;    // mirror: the output's transpose (the same matrix when symmetric); no base: none
     PairMatrix gram;           // kPoly: A
-    float a, b, c;
     bool symmetric;
+    float a, b, c;             // kPoly: from products and pairs of A to pairs
+    float to_out;              // kKeep: from products to pairs
 };
 struct ProductArgs {
     Product p[2];
@@ -265,7 +266,6 @@ __device__ __forceinline__ void finish_tile(const ProductArgs &a, const Place &w
     int lane = threadIdx.x & 63;
     asm volatile("" : "+v"(lane));   // (the addresses below are worked out here, not kept in registers through the main loop)
     const int r = lane & 15, q = lane >> 4;
-    const float unit = p.rows.inverse * p.cols.inverse;
     const int n_rows = p.rows.rows, n_cols = p.cols.rows;
     // what a lane finishes of a 32 x 32 tile of the result, after the tile went through LDS: rows 8 t + lane / 8, four columns
     const int fr = lane >> 3, fc = (lane & 7) * 4;
@@ -302,7 +302,7 @@ __device__ __forceinline__ void finish_tile(const ProductArgs &a, const Place &w
             if (row >= n_rows || col >= n_cols) return;
 #pragma unroll
             for (int g = 0; g < 4; ++g)
-                *reinterpret_cast<floatx4 *>(scratch + ((16 * (g >> 1) + r) * kPitch + 16 * (g & 1) + 4 * q) * 4) = v[g] * unit;
+                *reinterpret_cast<floatx4 *>(scratch + ((16 * (g >> 1) + r) * kPitch + 16 * (g & 1) + 4 * q) * 4) = v[g] * p.rows.inverse * p.cols.inverse;
             if (a.by_four) {
 #pragma unroll
                 for (int t = 0; t < 4; ++t) {
@@ -335,16 +335,15 @@ __device__ __forceinline__ void finish_tile(const ProductArgs &a, const Place &w
         uint2 hi[4], lo[4];
         if (FINISH == kPoly) {
             floatx4 f[4];
-            const float s = p.b * p.gram.inverse, c = p.c * unit;
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 const int i = row + 16 * (g >> 1) + r, j = col + 16 * (g & 1) + 4 * q;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) f[g][e] = c * v[g][e] + s * ((float)held.hi[g][e] + (float)held.lo[g][e]) + (i == j + e ? p.a : 0.0f);
+                for (int e = 0; e < 4; ++e) f[g][e] = p.c * v[g][e] + p.b * ((float)held.hi[g][e] + (float)held.lo[g][e]) + (i == j + e ? p.a : 0.0f);
             }
-            to_pairs(f, p.out.scale, row, col, n_rows, n_cols, lane, hi, lo);
+            to_pairs(f, 1.0f, row, col, n_rows, n_cols, lane, hi, lo);
         } else {
-            to_pairs(v, p.out.scale * unit, row, col, n_rows, n_cols, lane, hi, lo);
+            to_pairs(v, p.to_out, row, col, n_rows, n_cols, lane, hi, lo);
         }
         if (direct) store_pairs(p.out, p.out.base + w.matrix * p.out.stride, row, col, hi, lo, scratch, lane);
         if (turned) store_turned(p.mirror, p.mirror.base + w.matrix * p.mirror.stride, row, col, hi, lo, lane);
@@ -392,11 +391,10 @@ constexpr int kSide = 128, kSideTiles = kSide / 32, kChainWaves = kSideTiles * (
 constexpr int kSideBytes = kSide / kPanel * kSide * kLine;
 
 struct ChainArgs {
-    PairMatrix gram;           // scale of the first
-    PairMatrix p[2];           // P after every step by turns, the first in p[0] (scale, inverse: as below)
+    PairMatrix gram;           // of the first step
+    PairMatrix p[2];           // P after every step by turns, the first in p[0]
     int steps;
-    float abc[3 * kStepsAtOnce];
-    float gram_scale[kStepsAtOnce], step_scale[kStepsAtOnce], w_scale[kStepsAtOnce], p_scale[kStepsAtOnce];
+    ChainStep step[kStepsAtOnce];
 };
 
 __device__ __forceinline__ void lds_store_tile(char *lds, int row, int col, const uint2 (&hi)[4], const uint2 (&lo)[4], bool turned, int lane)
@@ -483,22 +481,20 @@ __global__ __launch_bounds__(64 * kChainWaves) void chain_kernel(ChainArgs a)
     };
     uint2 hi[4], lo[4];
     for (int k = 0; k < a.steps; ++k) {
-        const float c0 = a.abc[3 * k], c1 = a.abc[3 * k + 1], c2 = a.abc[3 * k + 2];
-        const float in_gram = 1.0f / a.gram_scale[k], in_step = 1.0f / a.step_scale[k];
+        const ChainStep &now = a.step[k];
         char *p_now = a.p[k & 1].base + (int64_t)blockIdx.x * a.p[k & 1].stride;
         product(gram, read, gram);
         if (there) {
-            const float s = c1 * in_gram, c = c2 * in_gram * in_gram;
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 const int i = row + 16 * (g >> 1) + r, chunk = 2 * (g & 1) + (q >> 1), j = col + 16 * (g & 1) + 4 * q;
                 const char *at = gram + (col / kPanel * kSide + i) * kLine + (q & 1) * 8;
                 const half4 h = *reinterpret_cast<const half4 *>(at + slot_of(i, chunk) * 16), l = *reinterpret_cast<const half4 *>(at + slot_of(i, 4 + chunk) * 16);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[g][e] = c * v[g][e] + s * ((float)h[e] + (float)l[e]) + (i == j + e ? c0 : 0.0f);
+                for (int e = 0; e < 4; ++e) v[g][e] = now.c * v[g][e] + now.b * ((float)h[e] + (float)l[e]) + (i == j + e ? now.a : 0.0f);
             }
             // (B is not read by anybody at this point)
-            to_pairs(v, a.step_scale[k], row, col, m, m, lane, hi, lo);
+            to_pairs(v, 1.0f, row, col, m, m, lane, hi, lo);
             lds_store_tile(step, row, col, hi, lo, turned, lane);
             if (k == 0) memory_store_tile(a.p[0], p_now, row, col, hi, lo, turned, lane);
         }
@@ -508,7 +504,7 @@ __global__ __launch_bounds__(64 * kChainWaves) void chain_kernel(ChainArgs a)
             const char *before = a.p[(k - 1) & 1].base + (int64_t)blockIdx.x * a.p[0].stride;
             product(step, read_memory, before);
             if (there) {
-                to_pairs(v, in_step / a.p_scale[k - 1] * a.p_scale[k], row, col, m, m, lane, hi, lo);
+                to_pairs(v, now.to_p, row, col, m, m, lane, hi, lo);
                 memory_store_tile(a.p[k & 1], p_now, row, col, hi, lo, turned, lane);
             }
         }
@@ -516,14 +512,14 @@ __global__ __launch_bounds__(64 * kChainWaves) void chain_kernel(ChainArgs a)
             product(step, read, gram);
             __syncthreads();
             if (there) {
-                to_pairs(v, in_step * in_gram * a.w_scale[k], row, col, m, m, lane, hi, lo);
+                to_pairs(v, now.to_w, row, col, m, m, lane, hi, lo);
                 lds_store_tile(gram, row, col, hi, lo, turned, lane);
             }
             __syncthreads();
             product(gram, read, step);
             __syncthreads();
             if (there) {
-                to_pairs(v, in_step / a.w_scale[k] * a.gram_scale[k + 1], row, col, m, m, lane, hi, lo);
+                to_pairs(v, now.to_gram, row, col, m, m, lane, hi, lo);
                 lds_store_tile(gram, row, col, hi, lo, turned, lane);
             }
             __threadfence_block();
@@ -649,7 +645,23 @@ int steps_at_once(const MatrixShape &s)
     return m <= 256 && n > 2 * m ? 2 : 3;
 }
 
-float pair_scale(double bound) { return (float)exp2(floor(log2(32000.0 / bound))); }
+float pair_scale(double bound) { return (float)exp2(floor(log2(32000.0 / fmax(bound, 0x1p-113)))); }
+
+ChainStep chain_step(const ScheduleBounds &bounds, const float *schedule, int k, double *factor)
+{
+    const double r = bounds.singular[k], next = bounds.singular[k + 1], most = bounds.factor[k];
+    const double gram = pair_scale(r * r), step = pair_scale(most), w = pair_scale(most * r * r), before = pair_scale(*factor);
+    *factor *= most;
+    ChainStep c;
+    c.a = (float)(schedule[3 * k] * step);
+    c.b = (float)(schedule[3 * k + 1] * step / gram);
+    c.c = (float)(schedule[3 * k + 2] * step / (gram * gram));
+    c.to_w = (float)(w / (step * gram));
+    c.to_gram = (float)(pair_scale(next * next) / (step * w));
+    c.to_p = (float)(pair_scale(*factor) / (step * before));
+    c.step_inverse = (float)(1.0 / step), c.p_inverse = (float)(1.0 / before);
+    return c;
+}
 
 bool schedule_bounds(int steps, const float *schedule, ScheduleBounds *bounds)
 {
@@ -734,26 +746,21 @@ void launch_ortho(const MatrixShape &s, int steps, const float *schedule, const 
         args.by_four = s.cols % 4 == 0 && reinterpret_cast<uintptr_t>(u.weight ? (const void *)u.weight : u.out) % (u.weight || s.dtype == LMKAN_F32 ? 16 : 8) == 0;
         args.parts = reinterpret_cast<floatx4 *>(ws + l.parts);
         const auto one = [&](const Product &p) { args.p[0] = p, args.problems = 1; };
+        const auto kept = [&](const PairMatrix &rows, const PairMatrix &cols, const PairMatrix &out, const PairMatrix &mirror, bool symmetric) {
+            return Product{rows, cols, out, mirror, none, symmetric, 0, 0, 0, (float)((double)out.scale * rows.inverse * cols.inverse)};
+        };
         for (int k = 0; k < steps;) {
             const int end = k + at_once < steps ? k + at_once : steps;
             const double r = bounds.singular[k];
             PairMatrix gram = pairs(l.a, m, m, r * r), so_far = none;
-            one(Product{x, x, gram, gram, none, 0, 0, 0, true});
+            one(kept(x, x, gram, gram, true));
             launch_product<kKeep>(args, stream);
             double factor = 1.0;
             if (m <= kSide) {
                 ChainArgs chain = {};
                 chain.gram = gram;
                 chain.steps = end - k;
-                for (int i = 0; i < chain.steps; ++i) {
-                    const double now = bounds.singular[k + i], most_now = bounds.factor[k + i];
-                    factor *= most_now;
-                    for (int e = 0; e < 3; ++e) chain.abc[3 * i + e] = schedule[3 * (k + i) + e];
-                    chain.gram_scale[i] = pair_scale(now * now);
-                    chain.step_scale[i] = pair_scale(most_now);
-                    chain.w_scale[i] = pair_scale(most_now * now * now);
-                    chain.p_scale[i] = pair_scale(factor);
-                }
+                for (int i = 0; i < chain.steps; ++i) chain.step[i] = chain_step(bounds, schedule, k + i, &factor);
                 chain.p[0] = pairs(l.p[0], m, m, factor), chain.p[1] = pairs(l.p[1], m, m, factor);
                 allow_large_lds(reinterpret_cast<const void *>(chain_kernel), 2 * kSideBytes);
                 chain_kernel<<<(unsigned)count, 64 * kChainWaves, 2 * kSideBytes, stream>>>(chain);
@@ -761,18 +768,17 @@ void launch_ortho(const MatrixShape &s, int steps, const float *schedule, const 
                 k = end;
             }
             for (const int begin = k; k < end; ++k) {
-                const float *abc = schedule + 3 * k;
                 const double now = bounds.singular[k], next = bounds.singular[k + 1];
                 const PairMatrix step = pairs(l.b[k & 1], m, m, bounds.factor[k]);
-                one(Product{gram, gram, step, step, gram, abc[0], abc[1], abc[2], true});
+                const ChainStep c = chain_step(bounds, schedule, k, &factor);
+                one(Product{gram, gram, step, step, gram, true, c.a, c.b, c.c, 0});
                 launch_product<kPoly>(args, stream);
-                factor *= bounds.factor[k];
                 const PairMatrix w = pairs(l.w, m, m, bounds.factor[k] * now * now);
                 args.problems = 0;
-                if (k + 1 < end) args.p[args.problems++] = Product{step, gram, w, w, none, 0, 0, 0, true};
+                if (k + 1 < end) args.p[args.problems++] = kept(step, gram, w, w, true);
                 if (k > begin) {
                     const PairMatrix longer = pairs(l.p[k & 1], m, m, factor);
-                    args.p[args.problems++] = Product{step, so_far, longer, longer, none, 0, 0, 0, true};
+                    args.p[args.problems++] = kept(step, so_far, longer, longer, true);
                     so_far = longer;
                 } else {
                     so_far = step;
@@ -780,18 +786,18 @@ void launch_ortho(const MatrixShape &s, int steps, const float *schedule, const 
                 if (args.problems) launch_product<kKeep>(args, stream);
                 if (k + 1 < end) {
                     gram = pairs(l.a, m, m, next * next);
-                    one(Product{w, step, gram, gram, none, 0, 0, 0, true});
+                    one(kept(w, step, gram, gram, true));
                     launch_product<kKeep>(args, stream);
                 }
             }
             if (k < steps) {
                 const PairMatrix y = pairs(l.u, m, n, bounds.singular[k]);
                 const PairMatrix yt = pairs(l.v[turned ^ 1], n, m, bounds.singular[k]);
-                one(Product{so_far, xt, y, yt, none, 0, 0, 0, false});
+                one(kept(so_far, xt, y, yt, false));
                 launch_product<kKeep>(args, stream);
                 x = y, xt = yt, turned ^= 1;
             } else {
-                one(s.flip() ? Product{xt, so_far, none, none, none, 0, 0, 0, false} : Product{so_far, xt, none, none, none, 0, 0, 0, false});
+                one(s.flip() ? Product{xt, so_far, none, none, none, false, 0, 0, 0, 0} : Product{so_far, xt, none, none, none, false, 0, 0, 0, 0});
                 launch_product<kResult>(args, stream);
             }
         }

@@ -40,8 +40,8 @@ struct SmallArgs {
     UpdateArgs u;
     int steps, from, to;                   // steps [from, to) of the schedule
     float schedule[3 * LMKAN_MAX_ORTHO_STEPS];
-    // powers of two that pairs are held times: the Gram matrix, B, B A, and the polynomial so far
-    float gram_scale[LMKAN_MAX_ORTHO_STEPS], step_scale[LMKAN_MAX_ORTHO_STEPS], w_scale[LMKAN_MAX_ORTHO_STEPS], p_scale[LMKAN_MAX_ORTHO_STEPS];
+    ChainStep step[LMKAN_MAX_ORTHO_STEPS];        // in pairs
+    float gram_scale[LMKAN_MAX_ORTHO_STEPS];      // the power of two that pairs of the Gram matrix are held times
     int at_once;                           // steps on one Gram matrix
     int columns;                           // of X in LDS at a time, a multiple of 16
     Divide by_fours;                       // columns / 4
@@ -401,40 +401,39 @@ struct Small {
                 *reinterpret_cast<uint2 *>(to + turned_place(i, j, lane, true)) = turn_quad(lo, lane);
             }
         };
-        const auto result = [&](float scale) {
-            if (there) put_square(square, 16 * i + (lane & 15), 16 * j + 4 * (lane >> 4), i != j, v * scale);
+        const auto result = [&](float first, float second) {
+            if (there) put_square(square, 16 * i + (lane & 15), 16 * j + 4 * (lane >> 4), i != j, v * first * second);
         };
         for (int k = from; k < to; ++k) {
-            const float c0 = s.schedule[3 * k], c1 = s.schedule[3 * k + 1], c2 = s.schedule[3 * k + 2];
-            const float in_gram = 1.0f / s.gram_scale[k], in_step = 1.0f / s.step_scale[k];
+            const ChainStep &now = s.step[k];
             char *step = k == from ? p : b;
             multiply_pairs(a, a);
             if (there) {
                 const half4 h = *reinterpret_cast<const half4 *>(a + pair_place(i, j, lane, false)), l = *reinterpret_cast<const half4 *>(a + pair_place(i, j, lane, true));
                 const int row = 16 * i + (lane & 15), col = 16 * j + 4 * (lane >> 4);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = c2 * in_gram * in_gram * v[e] + c1 * in_gram * ((float)h[e] + (float)l[e]) + (row == col + e ? c0 : 0.0f);
+                for (int e = 0; e < 4; ++e) v[e] = now.c * v[e] + now.b * ((float)h[e] + (float)l[e]) + (row == col + e ? now.a : 0.0f);
             }
-            if (k + 1 == to && k == from) return result(1.0f), __syncthreads();
-            keep(step, s.step_scale[k]);   // (B and P are read by nobody at this point)
+            if (k + 1 == to && k == from) return result(now.step_inverse, 1.0f), __syncthreads();
+            keep(step, 1.0f);   // (B and P are read by nobody at this point)
             __syncthreads();
             if (k > from) {
                 multiply_pairs(b, p);
                 if (k + 1 == to) {
-                    result(in_step / s.p_scale[k - 1]);
+                    result(now.step_inverse, now.p_inverse);
                 } else {
                     __syncthreads();
-                    keep(p, in_step / s.p_scale[k - 1] * s.p_scale[k]);
+                    keep(p, now.to_p);
                 }
             }
             if (k + 1 < to) {
                 multiply_pairs(step, a);
                 __syncthreads();
-                keep(a, in_step * in_gram * s.w_scale[k]);
+                keep(a, now.to_w);
                 __syncthreads();
                 multiply_pairs(a, step);
                 __syncthreads();
-                keep(a, in_step / s.w_scale[k] * s.gram_scale[k + 1]);
+                keep(a, now.to_gram);
             }
             __syncthreads();
         }
@@ -758,9 +757,9 @@ void launch(const MatrixShape &s, const UpdateArgs &update, SmallArgs a, const S
     a.at_once = steps_at_once(s);
     double factor = 1.0;
     for (int k = 0; k < a.steps; ++k) {
-        const double r = bounds.singular[k], most = bounds.factor[k];
-        factor = k % a.at_once == 0 ? most : factor * most;
-        a.gram_scale[k] = pair_scale(r * r), a.step_scale[k] = pair_scale(most), a.w_scale[k] = pair_scale(most * r * r), a.p_scale[k] = pair_scale(factor);
+        const double r = bounds.singular[k];
+        if (k % a.at_once == 0) factor = 1.0;
+        a.gram_scale[k] = pair_scale(r * r), a.step[k] = chain_step(bounds, a.schedule, k, &factor);
     }
     const int64_t most_matrices = matrices_at_once(s);
     const size_t item = s.dtype == LMKAN_F32 ? 4 : 2;

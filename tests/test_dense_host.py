@@ -123,3 +123,17 @@ def test_python_refuses_tensors_that_do_not_fit():
 def test_workspace_of_large_batches_is_bounded():
     """A table of 1089 matrices of 2048 x 4096 is worked on in parts."""
     assert 0 < pkg.lmkan_orthogonalize_workspace_bytes(pkg.MatrixDesc(1089, 2048, 4096)) < 8 << 30
+
+
+def _pair_scale(bound):
+    f = pkg.lib()._ZN5lmkan10pair_scaleEd
+    f.restype, f.argtypes = C.c_float, [C.c_double]
+    return f(bound)
+
+
+def test_scales_of_pairs_are_finite_powers_of_two():
+    """Whatever a schedule makes of its bounds; values up to the bound stay below what float16 holds."""
+    for bound in [0.0, 5e-324, 1e-40, 1e-30, 2.0 ** -114, 2.0 ** -113, 2.0 ** -100, 1e-20, 1e-3, 0.5, 1.0, 1.25, 16.0, 1024.0, 64.0 ** 3]:
+        s = _pair_scale(bound)
+        assert np.isfinite(s) and np.frexp(s)[0] == 0.5 and np.float32(1.0) / np.float32(s) * np.float32(s) == 1, bound
+        assert bound * s <= 32000 and (bound < 2.0 ** -113 or bound * s > 15999)

@@ -180,3 +180,22 @@ def test_linear_i8_in_the_larger_tiles(dev, batch, n_in, n_out, x_dtype, y_dtype
     most = 8 * 2.0 ** -24 * size + (UNIT[y_dtype] if y_dtype != "f32" else 0.0) * want.abs() * 1.001
     off = (got.double() - want).abs()
     assert bool((off <= most + 1e-30).all()), float((off / (most + 1e-30)).max())
+
+
+SHRINKING = [[(0.0, 0.0, 0.0)], [(0.0, 0.0, 0.0)] + list(pkg.QUINTIC_SCHEDULE[:2]), list(pkg.QUINTIC_SCHEDULE[:2]) + [(0.0, 0.0, 0.0)],
+             [(1e-20, 0.0, 0.0)], [(1e-20, 0.0, 0.0), (2.0, -1.5, 0.5)], [(1e-12, -5e-13, 0.0), (1e-12, 0.0, 0.0), (60.0, 0.0, 0.0)],
+             [(0.0, 1e-3, 0.0)] * 2, [(1.5, -0.5, 0.0)] * 2 + [(1e-19, 0.0, 0.0)] * 2, [(0.5, 0.0, 0.0)] * 32]
+
+
+@pytest.mark.parametrize("schedule", SHRINKING, ids=range(len(SHRINKING)))
+@pytest.mark.parametrize("shape", [(3, 24, 40), (3, 40, 70), (2, 64, 64), (1, 48, 6000), (1, 30, 6000), (2, 100, 70), (2, 150, 130), (1, 600, 700)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_schedules_that_shrink(dev, schedule, shape):
+    """Steps of nothing, and steps that take singular values down to 1e-38."""
+    x = _gradient(*shape, seed=15)
+    got = pkg.lmkan_orthogonalize(pkg.MatrixDesc(*shape), x.to(dev), schedule=schedule)
+    want = _reference(x, schedule)
+    if not want.any():
+        assert torch.equal(got.cpu(), torch.zeros_like(x))
+    else:
+        assert _far(got, want) <= TOL
