@@ -682,13 +682,11 @@ bool schedule_bounds(int steps, const float *schedule, ScheduleBounds *bounds)
         visit(0.0);
         visit(end);
         if (c != 0.0) visit(-b / (2.0 * c));
-        const double root = sqrt(9.0 * b * b - 20.0 * a * c);  // of a + 3 b u + 5 c u^2 (NaN: none)
-        if (c != 0.0) {
-            visit((-3.0 * b + root) / (10.0 * c));
-            visit((-3.0 * b - root) / (10.0 * c));
-        } else if (b != 0.0) {
-            visit(-a / (3.0 * b));
-        }
+        // a + 3 b u + 5 c u^2 = 0 (no root: NaN).  The sum has terms of one sign: the difference would lose the smaller root
+        // where c is small.
+        const double sum = -0.5 * (3.0 * b + copysign(sqrt(9.0 * b * b - 20.0 * a * c), b));
+        if (c != 0.0) visit(sum / (5.0 * c));
+        if (sum != 0.0) visit(a / sum);
         if (!(singular <= kMaxSingular) || !(factor <= kMaxFactor)) return false;
         r = singular;
         bounds->factor[k] = (float)factor;

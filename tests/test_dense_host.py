@@ -137,3 +137,33 @@ def test_scales_of_pairs_are_finite_powers_of_two():
         s = _pair_scale(bound)
         assert np.isfinite(s) and np.frexp(s)[0] == 0.5 and np.float32(1.0) / np.float32(s) * np.float32(s) == 1, bound
         assert bound * s <= 32000 and (bound < 2.0 ** -113 or bound * s > 15999)
+
+
+class _Bounds(C.Structure):
+    _fields_ = [("singular", C.c_float * 33), ("factor", C.c_float * 32)]
+
+
+def _bounds(schedule):
+    f = pkg.lib()._ZN5lmkan15schedule_boundsEiPKfPNS_14ScheduleBoundsE
+    f.restype, f.argtypes = C.c_bool, [C.c_int, C.c_void_p, C.c_void_p]
+    steps, rows = _schedule(schedule)
+    b = _Bounds()
+    return list(b.singular[:steps + 1]) if f(steps, rows.ctypes.data, C.byref(b)) else None, list(b.factor[:steps])
+
+
+@pytest.mark.parametrize("schedule", [
+    pkg.QUINTIC_SCHEDULE, [(1.7, 0.0, 0.0), (1.5, -0.5, 0.0)], [(2.0, -1.5, 0.5)] * 4, [(-1.5, 0.5, 0.0)],
+    [(1.7, 0.0, 0.0), (1.5, -0.5, 1e-17)], [(1.7, 0.0, 0.0), (1.5, -0.5, -1e-17)], [(1.7, 0.0, 0.0), (-1.5, 0.5, 1e-20)],
+    [(1.7, 0.0, 0.0), (1.5, -0.5, 1e-9)], [(1.7, 0.0, 0.0), (1.5, -0.5, 1e-30)], [(1.7, 0.0, 0.0), (1.5, -0.5, 1e-44)],
+    [(0.0, 1.0, -1e-12)], [(1.5, 0.0, 0.0), (2.0, 1e-20, -0.2)], [(0.0, 0.0, 1.0)], [(0.0, 0.0, 0.0)],
+], ids=str)
+def test_bounds_of_a_schedule_are_those_of_its_polynomials(schedule):
+    """Extremes of s (a + b s^2 + c s^4) and of the factor against many points between the ends; a last coefficient may
+    be far smaller than the others."""
+    singular, factor = _bounds(schedule)
+    r = 1.0
+    for k, (a, b, c) in enumerate(np.asarray(schedule, dtype=np.float32).astype(np.float64)):
+        s = np.linspace(0.0, r, 200001)
+        f = np.abs(a + b * s ** 2 + c * s ** 4)
+        r = float((f * s).max())
+        assert abs(factor[k] - f.max()) <= 1e-6 * f.max() and abs(singular[k + 1] - r) <= 1e-6 * r, k
