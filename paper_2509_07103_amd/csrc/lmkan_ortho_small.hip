@@ -10,8 +10,10 @@
 // of the polynomials are a chain in one workgroup: from m = 33 on, pairs of float16 (lmkan_tile.h) make it shorter.
 //
 // Norms: |X|^2 is the trace of the Gram matrix of the raw direction D, A_0 = D D^T / (|D| + eps)^2 and the first
-// polynomial is scaled by 1 / (|D| + eps).  The trace and the sum of the parts are taken in float64.  Elements beyond
-// 2^50, whose squares might exceed float32, are scaled by 2^-100 in the Gram matrix of their part.
+// polynomial is scaled by 1 / (|D| + eps).  The squares are float32 products, so that D is held times a power of two by its
+// largest element: beyond 2^50 times 2^-90, up to 2^-40 times 2^90.  Squares then leave float32's normal range only for
+// elements of less than 2^-23 of the largest.  Every workgroup goes by the elements it sees; the trace and the sums of
+// parts, in the range of the largest, are taken in float64.
 #include "lmkan_dense.h"
 
 #include <math.h>
@@ -23,8 +25,18 @@ namespace lmkan {
 
 namespace {
 
-constexpr float kLarge = 0x1p50f;          // elements beyond it are scaled in Gram matrices
-constexpr float kDown = 0x1p-100f;
+// Ranges by the largest element: 0 up to 2^-40, 1 up to 2^50, 2 beyond (or not a number)
+constexpr uint32_t kTiny = (127 - 40) << 23, kLarge = (127 + 50) << 23;   // bits of 2^-40 and 2^50
+__device__ __forceinline__ float range_scale(int range) { return range == 0 ? 0x1p90f : range == 1 ? 1.0f : 0x1p-90f; }
+__device__ __forceinline__ double range_units(int ranges) { return ranges == 0 ? 1.0 : ranges == 1 ? 0x1p-180 : 0x1p-360; }   // of products, so many ranges down
+// the bits of a magnitude are ordered like the values, NaN above infinity
+__device__ __forceinline__ uint32_t magnitude(float v) { return __builtin_bit_cast(uint32_t, v) & 0x7fffffffu; }
+// The range of what all threads have seen, `before` of what they saw earlier, from each one's largest magnitude
+__device__ __forceinline__ int range_of_all(uint32_t top, int before)
+{
+    if (__syncthreads_or(top > kLarge)) return 2;
+    return before > 0 ? before : __syncthreads_or(top > kTiny);
+}
 constexpr int kSmallLds = 150 * 1024;      // of 160 KiB
 constexpr int kMostParts = 512;            // parts of a Gram matrix
 
@@ -49,8 +61,9 @@ struct SmallArgs {
     int parts;                             // workgroups that share a matrix
     float *gram;                           // [matrices][parts][M][M], upper tiles
     double *sum;                           // [matrices][M][M]: their sums, where they are many
-    unsigned *scaled;                      // [matrices][parts]: whether kDown was applied
+    int *range;                            // [matrices][parts]: of the elements in a part
     float *poly;                           // [matrices][M][M]
+    float *unit;                           // [matrices]: what the direction is to be scaled by, by its range
     float *x;                              // [matrices][m][n]: X after a polynomial
 };
 
@@ -174,12 +187,12 @@ struct Small {
         }
     }
 
-    // X: columns [first, first + columns) of all rows to LDS, zero beyond the matrix; returns whether one is large.
+    // X: columns [first, first + columns) of all rows to LDS, zero beyond the matrix; returns the thread's largest magnitude.
     // get(at, count, whole) loads the elements stored from `at` on, use(...) makes the direction of them.
     template <class G, class U>
-    static __device__ __forceinline__ bool load(float *x, int pitch, const MatrixShape &s, int64_t matrix, int first, int columns, const Divide &by_fours, bool whole, G &&get, U &&use)
+    static __device__ __forceinline__ uint32_t load(float *x, int pitch, const MatrixShape &s, int64_t matrix, int first, int columns, const Divide &by_fours, bool whole, G &&get, U &&use)
     {
-        bool large = false;
+        uint32_t top = 0;
         Raw4 raw[4];
         const bool flip = s.flip();
         for_fours(s, first, columns, by_fours,
@@ -192,7 +205,7 @@ struct Small {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     if (e >= count) v[e] = 0.0f;
-                    large |= !(fabsf(v[e]) <= kLarge);
+                    top = max(top, magnitude(v[e]));
                 }
                 if (!flip) {
                     *reinterpret_cast<floatx4 *>(x + r * pitch + c) = v;
@@ -201,7 +214,7 @@ struct Small {
                     for (int e = 0; e < 4; ++e) x[(r + e) * pitch + c] = v[e];
                 }
             });
-        return large;
+        return top;
     }
 
     // Columns [first, first + columns) of X from LDS: put(at, count, whole, values) for every four adjacent stored elements
@@ -468,21 +481,21 @@ struct Small {
     }
 };
 
-// The Gram matrix of the raw direction to that of X_0, in place, from its trace; returns 1 / (norm + eps).
-// `unit`: what it has to be multiplied by (scaled elements).
+// The Gram matrix of the scaled direction to that of X_0, in place, from its trace; returns what takes the scaled
+// direction to X_0.  `eps`: times the same scale.
 template <class S>
-__device__ __forceinline__ float normalise(float *a, int m, double unit, float eps, double *shared, int lane)
+__device__ __forceinline__ float normalise(float *a, int m, double eps, double *shared, int lane)
 {
     __syncthreads();
     if (threadIdx.x < 64) {
         double trace = lane < m ? (double)a[lane * S::PITCH + lane] : 0.0;
 #pragma unroll
         for (int d = 32; d > 0; d >>= 1) trace += __shfl_xor(trace, d, 64);
-        if (lane == 0) *shared = 1.0 / (sqrt(trace * unit) + (double)eps);
+        if (lane == 0) *shared = 1.0 / (sqrt(trace) + eps);
     }
     __syncthreads();
     const double inverse = *shared;
-    const double f = inverse * inverse * unit;
+    const double f = inverse * inverse;
     for (int e = threadIdx.x; e < S::SQUARE; e += S::THREADS) a[e] = (float)((double)a[e] * f);
     __syncthreads();
     return (float)inverse;
@@ -514,11 +527,12 @@ __global__ __launch_bounds__(S::THREADS) void whole_kernel(SmallArgs a)
     float *gram = lds;
     char *rest = reinterpret_cast<char *>(gram + S::SQUARE);
     float *x = reinterpret_cast<float *>(rest + S::REST), *scratch = x + S::M * pitch;
-    const bool large = S::load(
+    const uint32_t top = S::load(
         x, pitch, a.s, matrix, 0, columns, a.by_fours, a.whole_fours, [&](int64_t at, int count, bool whole) { return fetch_four(a.u, a.s.dtype, at, count, whole, true); },
         [&](const Raw4 &v, int64_t at, int count, bool whole) { return direction_four(a.u, v, at, count, whole, true); });
-    const bool down = __syncthreads_or(large);
-    if (down) scale_columns<S>(x, pitch, columns, kDown);
+    const int range = range_of_all(top, 0);
+    const float scale = range_scale(range);
+    if (range != 1) scale_columns<S>(x, pitch, columns, scale);
     for (int k = 0; k < a.steps;) {
         const int end = k + a.at_once < a.steps ? k + a.at_once : a.steps;
         floatx4 acc[S::EACH];
@@ -527,8 +541,7 @@ __global__ __launch_bounds__(S::THREADS) void whole_kernel(SmallArgs a)
         S::gram(x, pitch, columns, wave, lane, acc);
         S::for_tiles(acc, wave, lane, scratch, [&](int row, int col, bool mirror, const floatx4 &v) { S::put_square(gram, row, col, mirror, v); });
         float inverse = 1.0f;
-        // (the raw direction times 2^-100 has a norm that is so many times smaller, eps with it)
-        if (k == 0) inverse = normalise<S>(gram, m, 1.0, down ? a.s.eps * kDown : a.s.eps, &shared, lane);
+        if (k == 0) inverse = normalise<S>(gram, m, (double)a.s.eps * scale, &shared, lane);
         else __syncthreads();
         float *p = S::polynomial(a, k, end, gram, rest, wave, lane);
         if (k == 0) scale_square<S>(p, inverse);
@@ -551,41 +564,39 @@ __global__ __launch_bounds__(S::THREADS) void gram_kernel(SmallArgs a)
     floatx4 acc[S::EACH];
 #pragma unroll
     for (int q = 0; q < S::EACH; ++q) acc[q] = floatx4{0, 0, 0, 0};
-    bool down = false;
+    int range = 0;
     for (int64_t first = (int64_t)blockIdx.x * columns; first < n; first += (int64_t)a.parts * columns) {
-        const bool large = S::load(
+        const uint32_t top = S::load(
             x, pitch, a.s, matrix, (int)first, columns, a.by_fours, a.whole_fours, [&](int64_t at, int count, bool whole) { return fetch_four(a.u, a.s.dtype, at, count, whole, true); },
             [&](const Raw4 &v, int64_t at, int count, bool whole) { return direction_four(a.u, v, at, count, whole, true); });
-        const bool now = __syncthreads_or(large);
-        if (now && !down) {
-            down = true;
+        // (what there is of the sum goes over to a larger range)
+        const int now = range_of_all(top, range);
+        for (; range < now; ++range)
 #pragma unroll
-            for (int q = 0; q < S::EACH; ++q) acc[q] *= kDown, acc[q] *= kDown;
-        }
-        if (down) scale_columns<S>(x, pitch, columns, kDown);
+            for (int q = 0; q < S::EACH; ++q) acc[q] *= 0x1p-90f, acc[q] *= 0x1p-90f;
+        if (range != 1) scale_columns<S>(x, pitch, columns, range_scale(range));
         S::gram(x, pitch, columns, wave, lane, acc);
         __syncthreads();
     }
     float *to = a.gram + (matrix * a.parts + blockIdx.x) * S::M * S::M;
     S::for_tiles(acc, wave, lane, scratch, [&](int row, int col, bool, const floatx4 &v) { *reinterpret_cast<floatx4 *>(to + row * S::M + col) = v; });
-    if (threadIdx.x == 0) a.scaled[matrix * a.parts + blockIdx.x] = down;
+    if (threadIdx.x == 0) a.range[matrix * a.parts + blockIdx.x] = range;
 }
 
-// Whether a part of the matrix's Gram matrix has scaled elements (they are those of the raw direction only)
+// The range of a matrix's direction, from those of the parts (1 for an X between polynomials)
 template <class S>
-__device__ __forceinline__ bool any_scaled(const SmallArgs &a, const unsigned *scaled)
+__device__ __forceinline__ int matrix_range(const SmallArgs &a, const int *ranges)
 {
-    bool any = false;
-    if (a.from == 0)
-        for (int k = threadIdx.x; k < a.parts; k += S::THREADS) any |= scaled[k] != 0;
-    return __syncthreads_or(any);
+    if (a.from != 0) return 1;
+    int range = 0;
+    for (int k = threadIdx.x; k < a.parts; k += S::THREADS) range = max(range, ranges[k]);
+    return __syncthreads_or(range == 2) ? 2 : __syncthreads_or(range == 1);
 }
 
-// an element of a part, in float64, in the units of the scaled parts where there are any
-__device__ __forceinline__ double part_element(const float *from, const unsigned *scaled, bool any, int k, int64_t step, int e)
+// an element of a part, in float64, in the units of the range `range`; `first`: of the direction
+__device__ __forceinline__ double part_element(const float *from, const int *ranges, int range, bool first, int k, int64_t step, int e)
 {
-    const double v = from[k * step + e];
-    return any && !scaled[k] ? v * 0x1p-200 : v;
+    return (double)from[k * step + e] * range_units(first ? range - ranges[k] : 0);
 }
 
 constexpr int kFewParts = 16;  // parts that the workgroup of the polynomial sums itself
@@ -598,12 +609,12 @@ __global__ __launch_bounds__(S::THREADS) void sum_kernel(SmallArgs a)
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int64_t matrix = blockIdx.y;
     const float *from = a.gram + matrix * a.parts * S::M * S::M;
-    const unsigned *scaled = a.scaled + matrix * a.parts;
-    const bool any = any_scaled<S>(a, scaled);
+    const int *ranges = a.range + matrix * a.parts;
+    const int range = matrix_range<S>(a, ranges);
     const int e = blockIdx.x * 64 + lane;
     double sum = 0.0;
 #pragma unroll 8
-    for (int k = wave; k < a.parts; k += S::WAVES) sum += part_element(from, scaled, any, k, S::M * S::M, e);
+    for (int k = wave; k < a.parts; k += S::WAVES) sum += part_element(from, ranges, range, a.from == 0, k, S::M * S::M, e);
     sums[wave][lane] = sum;
     __syncthreads();
     if (wave != 0) return;
@@ -622,8 +633,8 @@ __global__ __launch_bounds__(S::THREADS) void polynomial_kernel(SmallArgs a)
     const int64_t matrix = blockIdx.x;
     float *gram = lds;
     const float *from = a.gram + matrix * a.parts * S::M * S::M;
-    const unsigned *scaled = a.scaled + matrix * a.parts;
-    const bool any = any_scaled<S>(a, scaled);
+    const int *ranges = a.range + matrix * a.parts;
+    const int range = matrix_range<S>(a, ranges);
 #pragma unroll 4
     for (int e = threadIdx.x; e < S::M * S::M; e += S::THREADS) {
         const int i = e / S::M, j = e % S::M;
@@ -633,16 +644,16 @@ __global__ __launch_bounds__(S::THREADS) void polynomial_kernel(SmallArgs a)
             sum = a.sum[matrix * S::M * S::M + e];
         } else {
 #pragma unroll 4
-            for (int k = 0; k < a.parts; ++k) sum += part_element(from, scaled, any, k, S::M * S::M, e);
+            for (int k = 0; k < a.parts; ++k) sum += part_element(from, ranges, range, a.from == 0, k, S::M * S::M, e);
         }
         gram[i * S::PITCH + j] = (float)sum;
         if (i / 16 != j / 16) gram[j * S::PITCH + i] = (float)sum;
     }
     float inverse = 1.0f;
-    if (a.from == 0) inverse = normalise<S>(gram, a.s.m(), 1.0, any ? a.s.eps * kDown : a.s.eps, &shared, lane);
+    if (a.from == 0) inverse = normalise<S>(gram, a.s.m(), (double)a.s.eps * range_scale(range), &shared, lane);
     else __syncthreads();
     const float *p = S::polynomial(a, a.from, a.to, gram, reinterpret_cast<char *>(gram + S::SQUARE), wave, lane);
-    if (any) inverse *= kDown;   // (the direction itself is not scaled)
+    if (threadIdx.x == 0) a.unit[matrix] = range_scale(range);
     float *to = a.poly + matrix * S::M * S::M;
     for (int e = threadIdx.x; e < S::M * S::M; e += S::THREADS) to[e] = p[e / S::M * S::PITCH + e % S::M] * inverse;
 }
@@ -666,13 +677,14 @@ __global__ __launch_bounds__(S::THREADS) void apply_kernel(SmallArgs a)
     MatrixShape kept = a.s;
     kept.rows = m, kept.cols = n;
     const bool x_fours = n % 4 == 0;
+    const float unit = a.unit[matrix];
     for (int64_t first = (int64_t)blockIdx.x * columns; first < n; first += (int64_t)a.parts * columns) {
         S::load(
             x, pitch, seen, matrix, (int)first, columns, a.by_fours, a.from != 0 ? x_fours : a.whole_fours,
             [&](int64_t at, int count, bool whole) {
                 return a.from != 0 ? Raw4{load_four(a.x, LMKAN_F32, at, count, whole), {}} : fetch_four(a.u, a.s.dtype, at, count, whole, false);
             },
-            [&](const Raw4 &v, int64_t at, int count, bool whole) { return a.from != 0 ? v.g : direction_four(a.u, v, at, count, whole, false); });
+            [&](const Raw4 &v, int64_t at, int count, bool whole) { return a.from != 0 ? v.g : unit * direction_four(a.u, v, at, count, whole, false); });
         __syncthreads();
         S::apply(p, x, pitch, columns, wave, lane);
         __syncthreads();
@@ -722,7 +734,7 @@ int parts_of(const MatrixShape &s, int64_t count)
 }
 
 struct Layout {
-    size_t gram, scaled, sum, poly, x, total;
+    size_t gram, range, sum, poly, unit, x, total;
 };
 Layout layout_of(const MatrixShape &s, int64_t count)
 {
@@ -732,9 +744,10 @@ Layout layout_of(const MatrixShape &s, int64_t count)
     size_t at = 0;
     const auto take = [&](size_t bytes) { const size_t here = at; at += align256(bytes); return here; };
     l.gram = take(count * parts * M * M * sizeof(float));
-    l.scaled = take(count * parts * sizeof(unsigned));
+    l.range = take(count * parts * sizeof(int));
     l.sum = take(parts > kFewParts ? count * M * M * sizeof(double) : 0);
     l.poly = take(count * M * M * sizeof(float));
+    l.unit = take(count * sizeof(float));
     l.x = take(count * s.elems() * sizeof(float));
     l.total = at;
     return l;
@@ -788,9 +801,9 @@ void launch(const MatrixShape &s, const UpdateArgs &update, SmallArgs a, const S
         const int64_t count = from_matrix(first);
         const Layout l = layout_of(s, count);
         a.parts = parts_of(s, count);
-        a.gram = reinterpret_cast<float *>(ws + l.gram), a.scaled = reinterpret_cast<unsigned *>(ws + l.scaled);
+        a.gram = reinterpret_cast<float *>(ws + l.gram), a.range = reinterpret_cast<int *>(ws + l.range);
         a.sum = reinterpret_cast<double *>(ws + l.sum);
-        a.poly = reinterpret_cast<float *>(ws + l.poly), a.x = reinterpret_cast<float *>(ws + l.x);
+        a.poly = reinterpret_cast<float *>(ws + l.poly), a.unit = reinterpret_cast<float *>(ws + l.unit), a.x = reinterpret_cast<float *>(ws + l.x);
         const dim3 grid(a.parts, (unsigned)count);
         a.from = 0;
         gram_kernel<S><<<grid, S::THREADS, block + scratch, stream>>>(a);

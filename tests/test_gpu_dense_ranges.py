@@ -199,3 +199,37 @@ def test_schedules_that_shrink(dev, schedule, shape):
         assert torch.equal(got.cpu(), torch.zeros_like(x))
     else:
         assert _far(got, want) <= TOL
+
+
+SMALL = [(3, 16, 8), (2, 40, 70), (3, 64, 64), (1, 3, 5000), (1, 64, 6000), (6000, 30, 1), (1, 1, 70001)]
+
+
+@pytest.mark.parametrize("scale,eps", [(1e-18, 1e-30), (1e-24, 1e-30), (1e-30, 1e-36), (1e-36, 1e-40), (1e-24, 1e-24)])
+@pytest.mark.parametrize("shape", SMALL + [(2, 65, 70), (2, 250, 333)], ids=lambda s: "x".join(map(str, s)))
+def test_small_magnitudes_with_a_smaller_eps(dev, shape, scale, eps):
+    """Squares below float32's range; eps is a float32 value.  (Denormals hold fewer bits: they are the input here.)"""
+    x = _gradient(*shape, seed=14, scale=scale)
+    got = pkg.lmkan_orthogonalize(pkg.MatrixDesc(*shape, eps=eps), x.to(dev))
+    assert _far(got, _reference(x, pkg.QUINTIC_SCHEDULE, float(np.float32(eps)))) <= TOL
+
+
+@pytest.mark.parametrize("shape", [(1, 3, 5000), (1, 64, 6000), (2, 40, 70), (1, 70, 6000)], ids=lambda s: "x".join(map(str, s)))
+def test_magnitudes_that_differ_within_a_matrix(dev, shape):
+    """Small, ordinary and large columns, in this and the other order: the norm is that of the largest."""
+    n = shape[2]
+    for order in ((1e-28, 1.0, 1e25), (1e25, 1.0, 1e-28), (1e-28, 1e-27, 1e-28), (1.0, 1e-28, 1.0)):
+        x = _gradient(*shape, seed=16, scale=1.0)
+        for k, s in enumerate(order):
+            x[:, :, k * n // 3:(k + 1) * n // 3] *= s
+        got = pkg.lmkan_orthogonalize(pkg.MatrixDesc(*shape, eps=1e-36), x.to(dev))
+        assert _far(got, _reference(x, pkg.QUINTIC_SCHEDULE, float(np.float32(1e-36)))) <= TOL
+
+
+@pytest.mark.parametrize("shape", SMALL + [(2, 65, 70), (2, 250, 333)], ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("steps", [0, 5])
+def test_the_largest_magnitudes(dev, shape, steps):
+    """Norms beyond float32."""
+    x = _gradient(*shape, seed=17, scale=1.0)
+    x *= 3e38 / x.abs().max()
+    got = pkg.lmkan_orthogonalize(pkg.MatrixDesc(*shape), x.to(dev), schedule=pkg.QUINTIC_SCHEDULE[:steps])
+    assert _far(got, _reference(x, pkg.QUINTIC_SCHEDULE[:steps])) <= TOL
