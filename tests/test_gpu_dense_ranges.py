@@ -233,3 +233,11 @@ def test_the_largest_magnitudes(dev, shape, steps):
     x *= 3e38 / x.abs().max()
     got = pkg.lmkan_orthogonalize(pkg.MatrixDesc(*shape), x.to(dev), schedule=pkg.QUINTIC_SCHEDULE[:steps])
     assert _far(got, _reference(x, pkg.QUINTIC_SCHEDULE[:steps])) <= TOL
+
+
+@pytest.mark.parametrize("steps", [0, 1, 5])
+@pytest.mark.parametrize("eps", [1e-38, 1e-39, 1e-42, 1e-45])
+@pytest.mark.parametrize("shape", SMALL + [(2, 65, 70), (2, 250, 333)], ids=lambda s: "x".join(map(str, s)))
+def test_zeros_with_the_smallest_eps(dev, shape, eps, steps):
+    got = pkg.lmkan_orthogonalize(pkg.MatrixDesc(*shape, eps=eps), torch.zeros(shape, device=dev), schedule=pkg.QUINTIC_SCHEDULE[:steps])
+    assert torch.equal(got, torch.zeros_like(got))
