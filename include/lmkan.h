@@ -411,8 +411,9 @@ typedef struct lmkan_matrices {
  *   x_dev, out_dev  desc->dtype; out is overwritten and may be x_dev itself
  *   workspace_dev / workspace_bytes: at least lmkan_orthogonalize_workspace_bytes(desc)
  *                 bytes, 256-byte aligned
- * Every product keeps 22 bits of its factors or more and is summed in float32, norms are
- * summed in float64; out is rounded to desc->dtype once.  A matrix of zeros stays zero; one
+ * Every product keeps 22 bits of its factors or more (elements below 2^-16 of what bounds
+ * their matrix: 2^-38 of that) and is summed in float32, norms are summed in float64 and
+ * hold for any eps; out is rounded to desc->dtype once.  A matrix of zeros stays zero; one
  * with a NaN or an infinity becomes NaN (steps > 0) and leaves the others of the batch alone.
  * The result repeats bit for bit between runs.
  */

@@ -14,7 +14,8 @@
 //
 // Factors are pairs of float16 (lmkan_tile.h): three instructions at the rate of float16 keep 22 bits, which
 // float32 instructions would do at a sixteenth of that rate.  The power of two that a matrix is scaled by follows
-// from the bound of its singular values (schedule_bounds).
+// from the bound of its singular values (schedule_bounds); for X, which is smaller where |U| is not large beside eps,
+// also from |X_0| and the factors of the steps behind it (extra_bits).
 #include "lmkan_dense.h"
 
 #include <math.h>
@@ -37,6 +38,20 @@ struct PairMatrix {
     int rows, depth;
     float scale, inverse;   // a power of two, and one over it
 };
+
+// X is held times a power of two of its own besides: its norm is at most |X_0| times `grow`, and `bound`
+struct Extra {
+    float grow, bound;
+    int most;          // bits
+};
+// How many bits a matrix X with |X_0| = size stays below its bound
+__device__ __forceinline__ int extra_bits(const Extra &x, float size)
+{
+    const float now = size * x.grow;
+    if (!(now > 0.0f && now < x.bound)) return 0;
+    const int bits = (int)(__builtin_bit_cast(uint32_t, x.bound) >> 23) - (int)(__builtin_bit_cast(uint32_t, now) >> 23) - 1;
+    return min(max(bits, 0), x.most);
+}
 
 // Sum over the 256 threads in a fixed order, for all of them
 __device__ __forceinline__ double sum_of_threads(double v, double *shared)
@@ -74,21 +89,24 @@ __global__ __launch_bounds__(256) void norm_kernel(MatrixShape s, UpdateArgs u, 
     if (threadIdx.x == 0) part[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = sum;
 }
 
-// times / (norm + eps), which may be beyond float32 either way, in two factors: a power of two that brings elements near
-// one without a rounding, and the rest (in scalar registers: two vector registers more and split_kernel has six waves a
-// SIMD instead of seven, 132 us instead of 124 for 441 of 250 x 333)
+// What takes elements to X_0 (a matrix of pairs: to what they are held as), in two factors, as it may be beyond float32
+// either way: a power of two that brings elements near one without a rounding, and the rest.  (In scalar registers: two
+// vector registers more and split_kernel has six waves a SIMD instead of seven, 132 us instead of 124 for 441 of 250 x 333.)
 struct Inverse {
-    float power, rest;
+    float power, rest, size;   // size: |X_0|
     __device__ __forceinline__ float of(float v) const { return v * power * rest; }
 };
-__device__ __forceinline__ Inverse inverse_norm(const MatrixShape &s, const double *part, int parts, int64_t matrix, float times, double *shared)
+__device__ __forceinline__ Inverse inverse_norm(const MatrixShape &s, const double *part, int parts, int64_t matrix, float scale, const Extra &extra, double *shared)
 {
     double sum = 0.0;
     for (int i = threadIdx.x; i < parts; i += 256) sum += part[matrix * parts + i];
-    const double norm = sqrt(sum_of_threads(sum, shared));
+    const double norm = sqrt(sum_of_threads(sum, shared)), inverse = 1.0 / (norm + (double)s.eps);
     const int exponent = (int)(__builtin_bit_cast(uint64_t, norm) >> 52) - 1023;   // (not below zero)
-    const float power = __builtin_bit_cast(float, (uint32_t)(127 - min(max(exponent, -127), 126)) << 23);
-    return {uniform(power), uniform((float)(times / ((norm + (double)s.eps) * power)))};
+    const int power = min(max(exponent, -127), 126);                               // elements times 2^-power
+    const float size = uniform((float)(norm * inverse));
+    const int up = power + extra_bits(extra, size);
+    const double rest = inverse * scale * __builtin_bit_cast(double, (uint64_t)(1023 + up) << 52);
+    return {uniform(__builtin_bit_cast(float, (uint32_t)(127 - power) << 23)), uniform((float)rest), size};
 }
 
 __device__ __forceinline__ void split(float v, _Float16 *hi, _Float16 *lo)
@@ -106,6 +124,8 @@ struct SplitArgs {
     const double *part;
     int parts;
     PairMatrix by_rows, by_cols;
+    Extra extra;
+    float *size;
 };
 __global__ __launch_bounds__(256) void split_kernel(SplitArgs a)
 {
@@ -114,7 +134,8 @@ __global__ __launch_bounds__(256) void split_kernel(SplitArgs a)
     const int64_t matrix = blockIdx.z, per = a.s.elems();
     const int across = (a.s.cols + 63) / 64;
     const int r0 = (int)(blockIdx.x / across) * 64, c0 = (int)(blockIdx.x % across) * 64;
-    const Inverse f = inverse_norm(a.s, a.part, a.parts, matrix, a.by_rows.scale, sums);
+    const Inverse f = inverse_norm(a.s, a.part, a.parts, matrix, a.by_rows.scale, a.extra, sums);
+    if (blockIdx.x == 0 && threadIdx.x == 0) a.size[matrix] = f.size;
     const int c = threadIdx.x & 63;
     const int64_t from = (a.first + matrix) * per + (int64_t)r0 * a.s.cols + c0 + c;
     for (int b = threadIdx.x >> 6; b < 64; b += 4 * kAtOnce) {
@@ -197,8 +218,9 @@ __device__ __forceinline__ void store_turned(const PairMatrix &d, char *to, int 
 // What becomes of a product
 enum Finish {
     kKeep,      // pairs, both ways round
+    kKeepX,     // the same, with X among the factors
     kPoly,      // a I + b A + c (product), pairs
-    kResult,    // the result of the call
+    kResult,    // the result of the call (X is a factor)
 };
 
 struct Product {
@@ -217,6 +239,9 @@ struct ProductArgs {
     int tiles;                 // of one matrix and problem
     WorkSplit work;
     floatx4 *parts;
+    const float *size;         // |X_0| of every matrix
+    int x_factors;             // kKeepX, kResult: how many of the factors are X
+    Extra in, out;             // of X as a factor, and as the product
     // kResult
     MatrixShape s;
     UpdateArgs u;
@@ -267,15 +292,21 @@ __device__ __forceinline__ void to_pairs(const floatx4 (&v)[4], float scale, int
     }
 }
 
+// |X_0| of a tile's matrix, for products with X
+template <int FINISH>
+__device__ __forceinline__ float size_of(const ProductArgs &a, const Place &w) { return FINISH == kKeepX || FINISH == kResult ? a.size[w.matrix] : 0.0f; }
+
 // `scratch`: kWaveScratch bytes of LDS of the wave's own
 template <class T, int FINISH>
-__device__ __forceinline__ void finish_tile(const ProductArgs &a, const Place &w, const floatx4 (&acc)[T::CT][T::RT], char *scratch, int wave)
+__device__ __forceinline__ void finish_tile(const ProductArgs &a, const Place &w, const floatx4 (&acc)[T::CT][T::RT], float size, char *scratch, int wave)
 {
     const Product &p = product_of<FINISH>(a, w);
     int lane = threadIdx.x & 63;
     asm volatile("" : "+v"(lane));   // (the addresses below are worked out here, not kept in registers through the main loop)
     const int r = lane & 15, q = lane >> 4;
     const int n_rows = p.rows.rows, n_cols = p.cols.rows;
+    // for what X is held times besides its scale
+    const float adjust = FINISH == kKeepX || FINISH == kResult ? uniform(ldexpf(1.0f, extra_bits(a.out, size) - a.x_factors * extra_bits(a.in, size))) : 1.0f;
     // what a lane finishes of a 32 x 32 tile of the result, after the tile went through LDS: rows 8 t + lane / 8, four columns
     const int fr = lane >> 3, fc = (lane & 7) * 4;
     const int64_t start = FINISH == kResult ? (a.first + w.matrix) * a.s.elems() : 0;
@@ -311,7 +342,7 @@ __device__ __forceinline__ void finish_tile(const ProductArgs &a, const Place &w
             if (row >= n_rows || col >= n_cols) return;
 #pragma unroll
             for (int g = 0; g < 4; ++g)
-                *reinterpret_cast<floatx4 *>(scratch + ((16 * (g >> 1) + r) * kPitch + 16 * (g & 1) + 4 * q) * 4) = v[g] * p.rows.inverse * p.cols.inverse;
+                *reinterpret_cast<floatx4 *>(scratch + ((16 * (g >> 1) + r) * kPitch + 16 * (g & 1) + 4 * q) * 4) = v[g] * p.rows.inverse * p.cols.inverse * adjust;
             if (a.by_four) {
 #pragma unroll
                 for (int t = 0; t < 4; ++t) {
@@ -352,7 +383,7 @@ __device__ __forceinline__ void finish_tile(const ProductArgs &a, const Place &w
             }
             to_pairs(f, 1.0f, row, col, n_rows, n_cols, lane, hi, lo);
         } else {
-            to_pairs(v, p.to_out, row, col, n_rows, n_cols, lane, hi, lo);
+            to_pairs(v, p.to_out * adjust, row, col, n_rows, n_cols, lane, hi, lo);
         }
         if (direct) store_pairs(p.out, p.out.base + w.matrix * p.out.stride, row, col, hi, lo, scratch, lane);
         if (turned) store_turned(p.mirror, p.mirror.base + w.matrix * p.mirror.stride, row, col, hi, lo, lane);
@@ -369,6 +400,7 @@ __global__ __launch_bounds__(T::THREADS) void product_kernel(ProductArgs a)
         const auto operand = [&](const PairMatrix &m, int first_row) {
             return Operand{uniform(m.base + w.matrix * m.stride + (int64_t)first_row * kLine), uniform((int64_t)m.rows * kLine), m.rows - 1 - first_row, true, 0, 0};
         };
+        const float size = size_of<FINISH>(a, w);   // (under way through the main loop)
         floatx4 acc[T::CT][T::RT];
         // (a workgroup that finishes a tile goes before one that multiplies: 1 to 3 %)
         __builtin_amdgcn_s_setprio(0);
@@ -376,7 +408,7 @@ __global__ __launch_bounds__(T::THREADS) void product_kernel(ProductArgs a)
         else multiply<T, PairProduct>(operand(p.rows, w.ti * T::ROWS), operand(p.cols, w.tj * T::COLS), from, to, lds, acc);
         __builtin_amdgcn_s_setprio(2);
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        if (slot < 0) finish_tile<T, FINISH>(a, w, acc, lds + wave * kWaveScratch, wave);
+        if (slot < 0) finish_tile<T, FINISH>(a, w, acc, size, lds + wave * kWaveScratch, wave);
         else store_part<T>(a.parts, slot, acc);
         __syncthreads();
     });
@@ -388,9 +420,11 @@ __global__ __launch_bounds__(64 * joiners<T>()) void join_kernel(ProductArgs a)
 {
     __shared__ __align__(16) char lds[kWaveScratch + join_lds<T>()];
     const int tile = blockIdx.x / T::WAVES, wave = blockIdx.x % T::WAVES;
+    const Place w = place_of(a, a.work.whole + tile);
+    const float size = size_of<FINISH>(a, w);
     floatx4 acc[T::CT][T::RT];
     if (!join_parts<T, joiners<T>()>(a.work, tile, wave, a.parts, reinterpret_cast<floatx4 *>(lds + kWaveScratch), acc)) return;
-    finish_tile<T, FINISH>(a, place_of(a, a.work.whole + tile), acc, lds, wave);
+    finish_tile<T, FINISH>(a, w, acc, size, lds, wave);
 }
 
 // The steps on one Gram matrix of up to 128 x 128 in one launch: a workgroup per matrix, A and B in LDS, P in memory
@@ -542,7 +576,7 @@ __global__ __launch_bounds__(256) void unscaled_kernel(MatrixShape s, UpdateArgs
 {
     __shared__ double sums[256];
     const int64_t per = s.elems(), base = (first + blockIdx.y) * per;
-    const Inverse f = inverse_norm(s, part, parts, blockIdx.y, 1.0f, sums);
+    const Inverse f = inverse_norm(s, part, parts, blockIdx.y, 1.0f, Extra{}, sums);
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < per; i += (int64_t)gridDim.x * 256) {
         const float v = f.of(direction(u, fetch(u, s.dtype, base + i, false), base + i, false));
         if (u.weight) u.weight[base + i] = u.keep * u.weight[base + i] + u.add * v;
@@ -612,7 +646,7 @@ size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // the workspace of `count` matrices
 struct Layout {
-    size_t norm, u, v[2], a, w, b[2], p[2], parts, total;
+    size_t norm, u, v[2], a, w, b[2], p[2], parts, size, total;
 };
 Layout layout_of(const MatrixShape &s, int64_t count)
 {
@@ -625,6 +659,8 @@ Layout layout_of(const MatrixShape &s, int64_t count)
     l.u = take(u), l.v[0] = take(v), l.v[1] = take(v);
     l.a = take(g), l.w = take(g), l.b[0] = take(g), l.b[1] = take(g), l.p[0] = take(g), l.p[1] = take(g);
     l.parts = take(kPartsBytes);
+    // (last: matrices of pairs that start 256 bytes off multiples of 8 KiB make products 2 % slower)
+    l.size = take(align256(count * sizeof(float)));
     l.total = at;
     return l;
 }
@@ -732,6 +768,12 @@ void launch_ortho(const MatrixShape &s, int steps, const float *schedule, const 
             const float scale = pair_scale(bound);
             return PairMatrix{ws + at, pair_bytes(rows, depth), rows, depth, scale, 1.0f / scale};
         };
+        // of X before step k; the scale and the bits besides end at 2^114
+        double grow = 1.0;
+        const auto extra_of_x = [&](int k) {
+            const int most = 114 - ilogbf(pair_scale(bounds.singular[k]));
+            return Extra{(float)grow, bounds.singular[k], most < 0 ? 0 : most};
+        };
         double *part = reinterpret_cast<double *>(ws + l.norm);
         const int64_t some = (s.elems() + 4095) / 4096;
         const int parts = (int)(some < kNormParts ? some : kNormParts);
@@ -741,10 +783,11 @@ void launch_ortho(const MatrixShape &s, int steps, const float *schedule, const 
             continue;
         }
         const PairMatrix none{};
+        float *size = reinterpret_cast<float *>(ws + l.size);
         PairMatrix x = pairs(l.u, m, n, 1.0), xt = pairs(l.v[0], n, m, 1.0);
         int turned = 0;
         const unsigned tiles = (unsigned)(((s.rows + 63) / 64) * (int64_t)((s.cols + 63) / 64));
-        split_kernel<<<dim3(tiles, 1, (unsigned)count), 256, 0, stream>>>(SplitArgs{s, u, first, part, parts, s.flip() ? xt : x, s.flip() ? x : xt});
+        split_kernel<<<dim3(tiles, 1, (unsigned)count), 256, 0, stream>>>(SplitArgs{s, u, first, part, parts, s.flip() ? xt : x, s.flip() ? x : xt, extra_of_x(0), size});
         ProductArgs args = {};
         args.matrices = (int)count;
         args.s = s;
@@ -752,6 +795,8 @@ void launch_ortho(const MatrixShape &s, int steps, const float *schedule, const 
         args.first = first;
         args.by_four = s.cols % 4 == 0 && reinterpret_cast<uintptr_t>(u.weight ? (const void *)u.weight : u.out) % (u.weight || s.dtype == LMKAN_F32 ? 16 : 8) == 0;
         args.parts = reinterpret_cast<floatx4 *>(ws + l.parts);
+        args.size = size;
+        args.in = extra_of_x(0);
         const auto one = [&](const Product &p) { args.p[0] = p, args.problems = 1; };
         const auto kept = [&](const PairMatrix &rows, const PairMatrix &cols, const PairMatrix &out, const PairMatrix &mirror, bool symmetric) {
             return Product{rows, cols, out, mirror, none, symmetric, 0, 0, 0, (float)((double)out.scale * rows.inverse * cols.inverse)};
@@ -761,7 +806,8 @@ void launch_ortho(const MatrixShape &s, int steps, const float *schedule, const 
             const double r = bounds.singular[k];
             PairMatrix gram = pairs(l.a, m, m, r * r), so_far = none;
             one(kept(x, x, gram, gram, true));
-            launch_product<kKeep>(args, stream);
+            args.x_factors = 2, args.out = Extra{};
+            launch_product<kKeepX>(args, stream);
             double factor = 1.0;
             if (m <= kSide) {
                 ChainArgs chain = {};
@@ -798,13 +844,16 @@ void launch_ortho(const MatrixShape &s, int steps, const float *schedule, const 
                 }
             }
             if (k < steps) {
-                const PairMatrix y = pairs(l.u, m, n, bounds.singular[k]);
-                const PairMatrix yt = pairs(l.v[turned ^ 1], n, m, bounds.singular[k]);
+                const PairMatrix y = pairs(l.u, m, n, bounds.singular[k]), yt = pairs(l.v[turned ^ 1], n, m, bounds.singular[k]);
                 one(kept(so_far, xt, y, yt, false));
-                launch_product<kKeep>(args, stream);
+                grow *= factor;
+                args.x_factors = 1, args.out = extra_of_x(k);
+                launch_product<kKeepX>(args, stream);
+                args.in = args.out;
                 x = y, xt = yt, turned ^= 1;
             } else {
                 one(s.flip() ? Product{xt, so_far, none, none, none, false, 0, 0, 0, 0} : Product{so_far, xt, none, none, none, false, 0, 0, 0, 0});
+                args.x_factors = 1, args.out = Extra{};
                 launch_product<kResult>(args, stream);
             }
         }

@@ -241,3 +241,12 @@ def test_the_largest_magnitudes(dev, shape, steps):
 def test_zeros_with_the_smallest_eps(dev, shape, eps, steps):
     got = pkg.lmkan_orthogonalize(pkg.MatrixDesc(*shape, eps=eps), torch.zeros(shape, device=dev), schedule=pkg.QUINTIC_SCHEDULE[:steps])
     assert torch.equal(got, torch.zeros_like(got))
+
+
+@pytest.mark.parametrize("scale", [1e-9, 1e-12, 1e-15, 1e-20])
+@pytest.mark.parametrize("shape", [(2, 40, 70), (2, 65, 70), (3, 100, 90), (1, 1500, 96), (2, 250, 333), (1, 600, 700)], ids=lambda s: "x".join(map(str, s)))
+def test_gradients_far_below_eps(dev, shape, scale):
+    """|U| << eps: X_0 is small and the steps multiply it by a, every product with 22 bits all the same."""
+    x = _gradient(*shape, seed=18, scale=scale)
+    got = pkg.lmkan_orthogonalize(pkg.MatrixDesc(*shape), x.to(dev))
+    assert _far(got, _reference(x, pkg.QUINTIC_SCHEDULE, float(np.float32(1e-7)))) <= TOL
