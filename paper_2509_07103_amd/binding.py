@@ -541,7 +541,9 @@ def lmkan_fold(desc: LayerDesc, coef: torch.Tensor, gamma: float = 1.0, lin_w: t
 
 @functools.lru_cache(maxsize=64)
 def _schedule_bytes(schedule: tuple) -> bytes:
-    return np.ascontiguousarray(np.asarray(schedule, dtype=np.float32).reshape(-1, 3)).tobytes()
+    if any(len(row) != 3 for row in schedule):
+        raise ValueError("schedule: expected a sequence of (a, b, c)")
+    return np.asarray(schedule, dtype=np.float32).tobytes()
 
 
 def _schedule(schedule) -> bytes:

@@ -167,3 +167,12 @@ def test_bounds_of_a_schedule_are_those_of_its_polynomials(schedule):
         f = np.abs(a + b * s ** 2 + c * s ** 4)
         r = float((f * s).max())
         assert abs(factor[k] - f.max()) <= 1e-6 * f.max() and abs(singular[k + 1] - r) <= 1e-6 * r, k
+
+
+@pytest.mark.parametrize("schedule", [[(1.5, -0.5), (1.5, -0.5), (1.5, -0.5)], [(1.5, -0.5, 0.0, 1.5, -0.5, 0.0)], [(1.5, -0.5, 0.0), ()]], ids=str)
+def test_python_refuses_schedules_that_are_not_triples(schedule):
+    """Six numbers in threes by accident are not two steps."""
+    with pytest.raises(ValueError, match="schedule"):
+        pkg.lmkan_orthogonalize(pkg.MatrixDesc(2, 8, 8), torch.zeros((2, 8, 8)), schedule=schedule)
+    with pytest.raises(ValueError, match="schedule"):
+        pkg.lmkan_muon_step(pkg.MatrixDesc(2, 8, 8), pkg.MuonParams(0.1), *(torch.zeros((2, 8, 8)) for _ in range(3)), schedule=schedule)
