@@ -43,8 +43,9 @@ struct ScheduleBounds {
 };
 bool schedule_bounds(int steps, const float *schedule, ScheduleBounds *bounds);
 
-// Steps that are taken on one Gram matrix before the polynomial is applied and a new one is formed (lmkan_ortho.hip)
-int steps_at_once(const MatrixShape &s);
+// Steps that are taken on one Gram matrix before the polynomial is applied and a new one is formed: the step after the
+// last of those that begin with step k (lmkan_ortho.hip)
+int steps_until(const MatrixShape &s, const ScheduleBounds &bounds, int steps, int k);
 
 // The power of two that brings values up to `bound` to the upper end of float16's range (65504), with room for rounding.
 // Bounds end at 2^-113, so that every scale and every inverse of one is a float32 value: what a schedule takes below

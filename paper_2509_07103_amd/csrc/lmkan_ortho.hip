@@ -10,7 +10,7 @@
 // Five steps take 15 m^2 n + 5 m^3 operations as written, 9 m^2 n + 11 m^3 two at a time and 6 m^2 n + 14 m^3 three
 // at a time, and X is read and written five, three or two times.  An error of A is relative to its largest eigenvalue
 // and grows by up to a^2 (11.9) a step where the eigenvalue is small, which is why not all are taken at once, and
-// steps_at_once() chooses.
+// steps_until() chooses.
 //
 // Factors are pairs of float16 (lmkan_tile.h): three instructions at the rate of float16 keep 22 bits, which
 // float32 instructions would do at a sixteenth of that rate.  The power of two that a matrix is scaled by follows
@@ -681,13 +681,19 @@ Layout layout_of(const MatrixShape &s, int64_t count)
 //   33 x 66       -    1.63   -              |  257 x 2200     -    1.31
 //   40 x 80      0.90   -     -              |  193 x 386      -    1.43
 //   41 x 82       -    1.30   -              |  32 x 1500      -    1.47
-int steps_at_once(const MatrixShape &s)
+// A step with a larger factor than these have (3.44) is not followed by others: with factors of 8.2, 4.1, 3.9, 3.3, 2.3 two at
+// once had 2.3 (100 x 100), three 1.9 (250 x 333) and 2.2 (256 x 256).
+int steps_until(const MatrixShape &s, const ScheduleBounds &bounds, int steps, int k)
 {
     const int m = s.m(), n = s.n();
-    if (m <= 64 && (n < 2 * m || (m > 32 && m <= 40))) return 1;
-    if (m <= 32) return n <= 8 * m ? 2 : 3;
-    if (m <= 192) return 2;
-    return m <= 256 && n > 2 * m ? 2 : 3;
+    int most;
+    if (m <= 64 && (n < 2 * m || (m > 32 && m <= 40))) most = 1;
+    else if (m <= 32) most = n <= 8 * m ? 2 : 3;
+    else if (m <= 192) most = 2;
+    else most = m <= 256 && n > 2 * m ? 2 : 3;
+    int end = k + 1;
+    while (end < steps && end < k + most && bounds.factor[end - 1] <= 3.5f) ++end;
+    return end;
 }
 
 float pair_scale(double bound) { return (float)exp2(floor(log2(32000.0 / fmax(bound, 0x1p-113)))); }
@@ -758,7 +764,7 @@ void launch_ortho(const MatrixShape &s, int steps, const float *schedule, const 
     if (ortho_small_applicable(s, steps)) return launch_ortho_small(s, steps, schedule, u, workspace, stream);
     ScheduleBounds bounds;
     (void)schedule_bounds(steps, schedule, &bounds);
-    const int m = s.m(), n = s.n(), at_once = steps_at_once(s);
+    const int m = s.m(), n = s.n();
     const int64_t most = matrices_at_once(s);
     for (int64_t first = 0; first < s.batch; first += most) {
         const int64_t count = s.batch - first < most ? s.batch - first : most;
@@ -802,7 +808,7 @@ void launch_ortho(const MatrixShape &s, int steps, const float *schedule, const 
             return Product{rows, cols, out, mirror, none, symmetric, 0, 0, 0, (float)((double)out.scale * rows.inverse * cols.inverse)};
         };
         for (int k = 0; k < steps;) {
-            const int end = k + at_once < steps ? k + at_once : steps;
+            const int end = steps_until(s, bounds, steps, k);
             const double r = bounds.singular[k];
             PairMatrix gram = pairs(l.a, m, m, r * r), so_far = none;
             one(kept(x, x, gram, gram, true));

@@ -54,7 +54,7 @@ struct SmallArgs {
     float schedule[3 * LMKAN_MAX_ORTHO_STEPS];
     ChainStep step[LMKAN_MAX_ORTHO_STEPS];        // in pairs
     float gram_scale[LMKAN_MAX_ORTHO_STEPS];      // the power of two that pairs of the Gram matrix are held times
-    int at_once;                           // steps on one Gram matrix
+    int end[LMKAN_MAX_ORTHO_STEPS];        // the step after those on one Gram matrix, by the first of them
     int columns;                           // of X in LDS at a time, a multiple of 16
     Divide by_fours;                       // columns / 4
     bool whole_fours;                      // four adjacent elements from a multiple of four on are whole and aligned
@@ -534,7 +534,7 @@ __global__ __launch_bounds__(S::THREADS) void whole_kernel(SmallArgs a)
     const float scale = range_scale(range);
     if (range != 1) scale_columns<S>(x, pitch, columns, scale);
     for (int k = 0; k < a.steps;) {
-        const int end = k + a.at_once < a.steps ? k + a.at_once : a.steps;
+        const int end = a.end[k];
         floatx4 acc[S::EACH];
 #pragma unroll
         for (int q = 0; q < S::EACH; ++q) acc[q] = floatx4{0, 0, 0, 0};
@@ -767,11 +767,10 @@ int64_t matrices_at_once(const MatrixShape &s)
 template <class W, class S>
 void launch(const MatrixShape &s, const UpdateArgs &update, SmallArgs a, const ScheduleBounds &bounds, char *ws, hipStream_t stream)
 {
-    a.at_once = steps_at_once(s);
     double factor = 1.0;
-    for (int k = 0; k < a.steps; ++k) {
+    for (int k = 0, end = 0; k < a.steps; ++k) {
         const double r = bounds.singular[k];
-        if (k % a.at_once == 0) factor = 1.0;
+        if (k == end) factor = 1.0, end = a.end[k] = steps_until(s, bounds, a.steps, k);
         a.gram_scale[k] = pair_scale(r * r), a.step[k] = chain_step(bounds, a.schedule, k, &factor);
     }
     const int64_t most_matrices = matrices_at_once(s);
@@ -808,7 +807,7 @@ void launch(const MatrixShape &s, const UpdateArgs &update, SmallArgs a, const S
         a.from = 0;
         gram_kernel<S><<<grid, S::THREADS, block + scratch, stream>>>(a);
         for (; a.from < a.steps; a.from = a.to) {
-            a.to = a.from + a.at_once < a.steps ? a.from + a.at_once : a.steps;
+            a.to = a.end[a.from];
             if (polynomial_lds(S::M) > 65536) allow_large_lds(reinterpret_cast<const void *>(polynomial_kernel<W>), (int)polynomial_lds(S::M));
             if (a.parts > kFewParts) sum_kernel<Sum><<<dim3(S::M * S::M / 64, (unsigned)count), Sum::THREADS, 0, stream>>>(a);
             polynomial_kernel<W><<<(unsigned)count, W::THREADS, polynomial_lds(S::M), stream>>>(a);

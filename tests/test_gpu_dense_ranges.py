@@ -250,3 +250,25 @@ def test_gradients_far_below_eps(dev, shape, scale):
     x = _gradient(*shape, seed=18, scale=scale)
     got = pkg.lmkan_orthogonalize(pkg.MatrixDesc(*shape), x.to(dev))
     assert _far(got, _reference(x, pkg.QUINTIC_SCHEDULE, float(np.float32(1e-7)))) <= TOL
+
+
+LARGE_FACTORS = ((8.205, -22.9, 16.46), (4.066, -2.861, 0.5184), (3.910, -2.823, 0.5250), (3.286, -2.415, 0.4853), (2.278, -1.620, 0.3985))
+
+
+@pytest.mark.parametrize("schedule", [LARGE_FACTORS], ids=["large_factors"])
+@pytest.mark.parametrize("m,n", [(20, 160), (32, 256), (33, 66), (41, 328), (45, 90), (46, 115), (48, 384), (48, 576), (49, 147), (60, 60), (64, 144), (100, 100),
+                                 (128, 2000), (193, 193), (250, 333), (256, 256), (512, 512), (1024, 1024)])
+def test_errors_stay_near_those_of_float32_steps(dev, m, n, schedule):
+    """At most 1.5 times, geometric mean over matrices: what the steps on one Gram matrix are chosen by."""
+    count = max(2, min(64, int(2e6 / (m * n))))
+    g = torch.Generator(device=dev).manual_seed(m * 7919 + n)
+    x = torch.randn((count, m, n), device=dev, generator=g)
+    x += 0.5 * torch.randn((count, m, 2), device=dev, generator=g) @ torch.randn((count, 2, n), device=dev, generator=g)
+    want = _on_device(x, schedule)
+    plain = x / (x.double().square().sum(dim=(1, 2), keepdim=True).sqrt() + 1e-7).float()
+    for a, b, c in schedule:
+        gram = plain @ plain.mT.contiguous()
+        plain = a * plain + (b * gram + c * (gram @ gram)) @ plain
+    got = pkg.lmkan_orthogonalize(pkg.MatrixDesc(count, m, n), x, schedule=schedule)
+    far, far_plain = ((t.double() - want).flatten(1).norm(dim=1) / want.flatten(1).norm(dim=1) for t in (got, plain))
+    assert float((far / far_plain).log().mean().exp()) <= 1.5
