@@ -667,27 +667,36 @@ Layout layout_of(const MatrixShape &s, int64_t count)
 
 }  // namespace
 
-// The error against float64 is to stay near that of the steps as written in float32, which grows with m while that of
-// pairs summed line by line hardly does; long rows make small eigenvalues, and those suffer.  Measured, the error
-// relative to that of float32 for gradients with a few strong directions:
-//   m x n        one   two   three at once   |  m x n         two   three at once
-//   60 x 60      0.84  1.70  2.94            |  128 x 2000    0.70  2.28
-//   48 x 100     0.82  1.04  3.4             |  192 x 1537    0.58  2.31
-//   64 x 144     0.82  0.73  3.3             |  193 x 400     0.66  1.37
-//   48 x 400      -    0.84  1.99            |  250 x 333      -    1.14
-//   33 x 270      -    1.82  1.59            |  256 x 2100    0.52  1.87
-//   16 x 200      -     -    1.16            |  256 x 256      -    1.20
-//   100 x 100    0.52  1.08  1.89            |  320 x 3000     -    1.03
-//   33 x 66       -    1.63   -              |  257 x 2200     -    1.31
-//   40 x 80      0.90   -     -              |  193 x 386      -    1.43
-//   41 x 82       -    1.30   -              |  32 x 1500      -    1.47
-// A step with a larger factor than these have (3.44) is not followed by others: with factors of 8.2, 4.1, 3.9, 3.3, 2.3 two at
-// once had 2.3 (100 x 100), three 1.9 (250 x 333) and 2.2 (256 x 256).
+// The error against float64 is to stay within 1.5 times that of the steps as written in float32, for schedules that leave
+// singular values apart (one that converges ends nearer to it than pairs are held: below).  float32's error grows with m,
+// as its sums get longer; that of pairs comes from their rounding (2^-23 of a factor, float32 2^-24) and hardly grows.  So
+// float32 wins where m is small: from 33 rows, where the polynomials go over to pairs, to 48 a step by itself already costs
+// up to 1.3 times float32's error, two of them 1.3 to 2.  The error of a Gram matrix is multiplied by the square of a step's
+// factor where the singular value is small, and so is that of long rows, whose eigenvalues are small.  Measured, the error
+// relative to that of float32 for gradients with a few strong directions and five steps of a factor of 3.44 (64 and fewer
+// matrices a shape, geometric mean):
+//   m x n       one   two   three at once  |  m x n       one   two   three at once
+//   16 x 200    0.80  1.21  1.06           |  64 x 144    0.77  0.89  2.61
+//   28 x 56     0.90  1.18  1.83           |  100 x 100   0.52  1.16  1.67
+//   32 x 256    0.96  1.35  0.93           |  128 x 2000  0.63  0.63  1.29
+//   33 x 66     1.19  1.82  2.70           |  192 x 1537  0.59  0.57  1.65
+//   40 x 80     1.06  1.67  2.66           |  193 x 400   0.52  0.58  1.21
+//   41 x 328    1.22  1.80  1.27           |  250 x 333   0.41  0.68  0.99
+//   44 x 110    1.07  1.55  2.25           |  256 x 256   0.38  0.75  1.14
+//   46 x 115    1.02  1.48  2.26           |  256 x 2100  0.38  0.31  1.12
+//   46 x 138    1.07  1.53  1.90           |  320 x 3000  0.36  0.28  1.03
+//   48 x 384    1.18  1.53  1.54           |  512 x 512   0.29  0.46  0.87
+//   46 x 552    0.99  1.37  1.21           |  1024 x 1024 0.26  0.37  0.72
+//   60 x 60     0.81  1.72  2.48           |  50 x 300    1.11  1.46  1.61
+// With the rule below the largest of 681 shapes from 2 x 2 to 700 x 5600 is 1.46 (20 x 160).  A step with a larger factor
+// is not followed by others: with factors of 8.2, 4.1, 3.9, 3.3, 2.3 two at once had 2.3 (100 x 100), three 1.9 (250 x 333)
+// and 2.2 (256 x 256).  Eight steps (1.5, -0.5, 0), which converge: 2.2 to 2.8 times float32's 1.7e-7 to 2.2e-7, however
+// many are taken at once.
 int steps_until(const MatrixShape &s, const ScheduleBounds &bounds, int steps, int k)
 {
     const int m = s.m(), n = s.n();
     int most;
-    if (m <= 64 && (n < 2 * m || (m > 32 && m <= 40))) most = 1;
+    if (m <= 64 && (n < 2 * m || (m > 32 && m < 46) || (m >= 46 && m <= 48 && 2 * n >= 5 * m && n < 12 * m))) most = 1;
     else if (m <= 32) most = n <= 8 * m ? 2 : 3;
     else if (m <= 192) most = 2;
     else most = m <= 256 && n > 2 * m ? 2 : 3;

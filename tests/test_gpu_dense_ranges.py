@@ -255,7 +255,7 @@ def test_gradients_far_below_eps(dev, shape, scale):
 LARGE_FACTORS = ((8.205, -22.9, 16.46), (4.066, -2.861, 0.5184), (3.910, -2.823, 0.5250), (3.286, -2.415, 0.4853), (2.278, -1.620, 0.3985))
 
 
-@pytest.mark.parametrize("schedule", [LARGE_FACTORS], ids=["large_factors"])
+@pytest.mark.parametrize("schedule", [pkg.QUINTIC_SCHEDULE, LARGE_FACTORS], ids=["quintic", "large_factors"])
 @pytest.mark.parametrize("m,n", [(20, 160), (32, 256), (33, 66), (41, 328), (45, 90), (46, 115), (48, 384), (48, 576), (49, 147), (60, 60), (64, 144), (100, 100),
                                  (128, 2000), (193, 193), (250, 333), (256, 256), (512, 512), (1024, 1024)])
 def test_errors_stay_near_those_of_float32_steps(dev, m, n, schedule):
