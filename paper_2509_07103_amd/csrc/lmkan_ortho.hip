@@ -590,45 +590,69 @@ typedef TileShape<128, 128, 2, 2, 2> Tile128;
 typedef TileShape<256, 256, 4, 2, 2> Tile256;
 
 constexpr int kUnits = 256;      // compute units
-constexpr size_t kPartsBytes = (size_t)128 << 20;   // slots of 256 workgroups with the largest tile
 
-int64_t tiles_of(const Product &p, int tile)
-{
-    const int64_t down = (p.rows.rows + tile - 1) / tile, across = (p.cols.rows + tile - 1) / tile;
-    return p.symmetric ? down * (down + 1) / 2 : down * across;
-}
+// `count` products of rows x cols, summed over `depth`
+struct Batch {
+    int rows, cols, depth;
+    bool symmetric;
+    int64_t count;
+    int64_t tiles(int tile) const
+    {
+        const int64_t down = (rows + tile - 1) / tile, across = (cols + tile - 1) / tile;
+        return symmetric ? down * (down + 1) / 2 : down * across;
+    }
+};
 
-template <class T, int FINISH, bool ALONE = false>
-void launch_product_with(ProductArgs &a, hipStream_t stream)
-{
-    const Product &p = a.p[0];
-    a.tiles_down = (p.rows.rows + T::ROWS - 1) / T::ROWS;
-    a.tiles_across = (p.cols.rows + T::COLS - 1) / T::COLS;
-    a.tiles = (int)tiles_of(p, T::ROWS);
-    const int64_t tiles = (int64_t)a.tiles * a.matrices * a.problems;
-    constexpr int kLds = ALONE ? Alone<T>::LDS : T::LDS;
-    const int workers = kUnits * (kLds <= 80 * 1024 ? 2 : 1);
-    // (joining takes 6 us, a stage of the smallest tile 0.25; 20 us and 1.8 for the largest)
-    a.work = WorkSplit::of((int)tiles, panels(p.rows.depth), workers, T::ROWS == 64 ? 24 : T::ROWS == 128 ? 20 : 12);
-    const WorkSplit &w = a.work;
-    if (kLds > 65536) allow_large_lds(reinterpret_cast<const void *>(product_kernel<T, FINISH, ALONE>), kLds);
-    product_kernel<T, FINISH, ALONE><<<w.workers, T::THREADS, kLds, stream>>>(a);
-    if (w.cut()) join_kernel<T, FINISH><<<w.left() * T::WAVES, 64 * joiners<T>(), 0, stream>>>(a);
-}
-
+// How a batch of products is launched: the tiles, and who takes which of them.
 // The larger the tile, the less is read per product and the more of a tile that straddles the diagonal or the end is
 // wasted.  Measured (us, tiles of 64 / 128 / 256): 441 of 250 x 333 1720 / 1640 / 1800; 289 of 512 x 1024 7000 /
 // 5480 / 5800; one of 4096 x 4096 5900 / 4770 / 4380; one of 1024 x 1024 300 / 563 / 997.  Rows of 193 to 256 fill two
 // tiles of 128, which pays where there are tiles for one and a half turns of the units (two workgroups each): 441 of
 // 200 x 300 1289 / 1178, 300 of 193 x 386 962 / 907, but 200 of 256 x 512 858 / 964.
+struct Plan {
+    int tile;
+    bool alone;
+    WorkSplit work;
+    size_t parts() const { return work.cut() ? (size_t)2 * work.cutters * tile * tile * sizeof(float) : 0; }
+};
+// (joining takes 6 us, a stage of the smallest tile 0.25; 20 us and 1.8 for the largest)
+template <class T, bool ALONE = false>
+Plan plan_with(const Batch &b)
+{
+    const int workers = kUnits * ((ALONE ? Alone<T>::LDS : T::LDS) <= 80 * 1024 ? 2 : 1);
+    return {T::ROWS, ALONE, WorkSplit::of((int)(b.tiles(T::ROWS) * b.count), panels(b.depth), workers, T::ROWS == 64 ? 24 : T::ROWS == 128 ? 20 : 12)};
+}
+Plan plan_of(const MatrixShape &s, const Batch &b)
+{
+    const int shorter = s.m();
+    if (shorter > 512 && b.tiles(256) * b.count >= kUnits / 2) return plan_with<Tile256>(b);
+    if (shorter > 192 && b.tiles(128) * b.count >= (shorter > 256 ? 2 : 3) * kUnits) return plan_with<Tile128>(b);
+    if (b.tiles(64) * b.count > kUnits) return plan_with<Tile64>(b);
+    return plan_with<Tile64Alone, true>(b);
+}
+
+template <class T, int FINISH, bool ALONE = false>
+void launch_product_with(const ProductArgs &a, hipStream_t stream)
+{
+    constexpr int kLds = ALONE ? Alone<T>::LDS : T::LDS;
+    if (kLds > 65536) allow_large_lds(reinterpret_cast<const void *>(product_kernel<T, FINISH, ALONE>), kLds);
+    product_kernel<T, FINISH, ALONE><<<a.work.workers, T::THREADS, kLds, stream>>>(a);
+    if (a.work.cut()) join_kernel<T, FINISH><<<a.work.left() * T::WAVES, 64 * joiners<T>(), 0, stream>>>(a);
+}
+
 template <int FINISH>
 void launch_product(ProductArgs &a, hipStream_t stream)
 {
-    const int64_t n = a.matrices * a.problems;
-    const int shorter = a.s.m();
-    if (shorter > 512 && tiles_of(a.p[0], 256) * n >= kUnits / 2) launch_product_with<Tile256, FINISH>(a, stream);
-    else if (shorter > 192 && tiles_of(a.p[0], 128) * n >= (shorter > 256 ? 2 : 3) * kUnits) launch_product_with<Tile128, FINISH>(a, stream);
-    else if (tiles_of(a.p[0], 64) * n > kUnits) launch_product_with<Tile64, FINISH>(a, stream);
+    const Product &p = a.p[0];
+    const Batch b{p.rows.rows, p.cols.rows, p.rows.depth, p.symmetric, (int64_t)a.matrices * a.problems};
+    const Plan plan = plan_of(a.s, b);
+    a.tiles_down = (b.rows + plan.tile - 1) / plan.tile;
+    a.tiles_across = (b.cols + plan.tile - 1) / plan.tile;
+    a.tiles = (int)b.tiles(plan.tile);
+    a.work = plan.work;
+    if (plan.tile == 256) launch_product_with<Tile256, FINISH>(a, stream);
+    else if (plan.tile == 128) launch_product_with<Tile128, FINISH>(a, stream);
+    else if (!plan.alone) launch_product_with<Tile64, FINISH>(a, stream);
     else launch_product_with<Tile64Alone, FINISH, true>(a, stream);
 }
 
@@ -658,7 +682,15 @@ Layout layout_of(const MatrixShape &s, int64_t count)
     l.norm = take(align256(count * kNormParts * sizeof(double)));
     l.u = take(u), l.v[0] = take(v), l.v[1] = take(v);
     l.a = take(g), l.w = take(g), l.b[0] = take(g), l.b[1] = take(g), l.p[0] = take(g), l.p[1] = take(g);
-    l.parts = take(kPartsBytes);
+    // what the products of a call have of parts at most: Gram matrices, products of polynomials, one or two at a time, X
+    const int m = s.m(), n = s.n();
+    size_t parts = 0;
+    for (const Batch &b : {Batch{m, m, n, true, count}, Batch{m, m, m, true, count}, Batch{m, m, m, true, 2 * count}, Batch{s.flip() ? n : m, s.flip() ? m : n, m, false, count},
+                           Batch{m, n, m, false, count}}) {
+        const size_t bytes = plan_of(s, b).parts();
+        parts = bytes > parts ? bytes : parts;
+    }
+    l.parts = take(align256(parts));
     // (last: matrices of pairs that start 256 bytes off multiples of 8 KiB make products 2 % slower)
     l.size = take(align256(count * sizeof(float)));
     l.total = at;

@@ -176,3 +176,13 @@ def test_python_refuses_schedules_that_are_not_triples(schedule):
         pkg.lmkan_orthogonalize(pkg.MatrixDesc(2, 8, 8), torch.zeros((2, 8, 8)), schedule=schedule)
     with pytest.raises(ValueError, match="schedule"):
         pkg.lmkan_muon_step(pkg.MatrixDesc(2, 8, 8), pkg.MuonParams(0.1), *(torch.zeros((2, 8, 8)) for _ in range(3)), schedule=schedule)
+
+
+@pytest.mark.parametrize("shape,parts", [((1, 65, 65), 0.5), ((1, 100, 100), 0.5), ((20, 65, 65), 4), ((1, 1024, 1024), 32), ((441, 250, 333), 64)], ids=str)
+def test_workspace_follows_the_matrices(shape, parts):
+    """X by rows, X by columns twice and six square matrices in pairs (128 bytes for 32 values), and MiB for parts of tiles
+    that are cut: as many as the launches of the call have, not the most that any call has."""
+    batch, m, n = shape[0], min(shape[1:]), max(shape[1:])
+    pairs = batch * 128 * (-(-n // 32) * m + 2 * -(-m // 32) * n + 6 * -(-m // 32) * m)
+    need = pkg.lmkan_orthogonalize_workspace_bytes(pkg.MatrixDesc(*shape))
+    assert pairs < need < pairs + batch * (8192 + 4) + (1 << 14) + parts * (1 << 20)
