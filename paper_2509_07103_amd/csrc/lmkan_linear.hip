@@ -31,6 +31,10 @@ struct RowScale {
     __device__ __forceinline__ int code(float v) const { return finite ? (int)rintf(v * factor) : 0; }
 };
 
+// A sum of codes to the term.  (The sum first: the product of both scales may lie below float32's range where the term
+// does not; rows may have any magnitude, the scale of an output is that of weights)
+__device__ __forceinline__ float scaled(int sum, float w_scale, float x_scale) { return (float)sum * w_scale * x_scale; }
+
 __device__ __forceinline__ uint32_t magnitude(float v) { return __builtin_bit_cast(uint32_t, v) & 0x7fffffffu; }
 __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return a > b ? a : b; }
 __device__ __forceinline__ float rectified(float v, bool relu) { return relu && v < 0.0f ? 0.0f : v; }
@@ -242,7 +246,7 @@ __device__ __forceinline__ void finish_tile(const LinearArgs &a, int tile, const
                 const int64_t at = i * a.n_out + j;
                 floatx4 o;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[e] = (float)sum[e] * (held.scale[t] * ws[e]) + b[e];
+                for (int e = 0; e < 4; ++e) o[e] = scaled(sum[e], ws[e], held.scale[t]) + b[e];
                 if (a.y_dtype == LMKAN_F32) {
                     if (a.beta != 0.0f) o += a.beta * held.y[t];
                     *reinterpret_cast<floatx4 *>(static_cast<float *>(a.y) + at) = o;
@@ -267,7 +271,7 @@ __device__ __forceinline__ void finish_tile(const LinearArgs &a, int tile, const
                 const int64_t i = i0 + row + k;
                 if (i >= a.batch) break;
                 const int sum = *reinterpret_cast<const int *>(scratch + (k * kPitch + (lane & 31)) * 4);
-                float o = (float)sum * (a.x_scale[i] * ws) + b;
+                float o = scaled(sum, ws, a.x_scale[i]) + b;
                 if (a.beta != 0.0f) o += a.beta * load_as_float(a.y, i * a.n_out + j, a.y_dtype);
                 store_from_float(a.y, i * a.n_out + j, a.y_dtype, o);
             }
@@ -424,7 +428,7 @@ __global__ __launch_bounds__(256) void one_row_kernel(RowsArgs a, int padded)
         for (int d = 32; d > 0; d >>= 1) t += __shfl_xor(t, d, 64);
         const int j = j0 + o;
         if (lane == 0 && j < a.n_out) {
-            float y = (float)t * (s.scale * a.w_scale[j]) + (a.bias ? a.bias[j] : 0.0f);
+            float y = scaled(t, a.w_scale[j], s.scale) + (a.bias ? a.bias[j] : 0.0f);
             if (a.beta != 0.0f) y += a.beta * load_as_float(a.y, j, a.y_dtype);
             store_from_float(a.y, j, a.y_dtype, y);
         }
@@ -530,7 +534,7 @@ __global__ __launch_bounds__(64 * kSomeWaves) void some_rows_kernel(RowsArgs a, 
     const int r = threadIdx.x >> 4, j = j0 + (threadIdx.x & 15);
     if (r < rows && j < a.n_out) {
         const int64_t at = (int64_t)r * a.n_out + j;
-        float y = (float)sums[r][threadIdx.x & 15] * (scales[r] * a.w_scale[j]) + (a.bias ? a.bias[j] : 0.0f);
+        float y = scaled(sums[r][threadIdx.x & 15], a.w_scale[j], scales[r]) + (a.bias ? a.bias[j] : 0.0f);
         if (a.beta != 0.0f) y += a.beta * load_as_float(a.y, at, a.y_dtype);
         store_from_float(a.y, at, a.y_dtype, y);
     }

@@ -272,3 +272,20 @@ def test_errors_stay_near_those_of_float32_steps(dev, m, n, schedule):
     got = pkg.lmkan_orthogonalize(pkg.MatrixDesc(count, m, n), x, schedule=schedule)
     far, far_plain = ((t.double() - want).flatten(1).norm(dim=1) / want.flatten(1).norm(dim=1) for t in (got, plain))
     assert float((far / far_plain).log().mean().exp()) <= 1.5
+
+
+@pytest.mark.parametrize("x_size,w_size", [(1e-36, 1e-4), (1e-35, 1e-6), (1e30, 1e-3), (1.0, 1e-30)])
+@pytest.mark.parametrize("batch,n_in,n_out", [(1, 300, 64), (1, 4096, 2100), (5, 300, 64), (300, 300, 64), (300, 300, 61), (70, 4096, 64), (70, 4096, 33)])
+def test_linear_i8_of_rows_of_any_magnitude(dev, batch, n_in, n_out, x_size, w_size):
+    """Scales whose product lies below float32's normal range: the sum brings it back."""
+    g = torch.Generator().manual_seed(batch + n_in + n_out)
+    x = x_size * torch.randn((batch, n_in), generator=g)
+    w = torch.randint(-127, 128, (n_out, n_in), generator=g, dtype=torch.int8)
+    ws = w_size * (0.5 + torch.rand((n_out,), generator=g))
+    codes, scale = _codes(x)
+    product = codes.astype(np.float64) @ w.numpy().astype(np.float64).T
+    want = product * scale.astype(np.float64)[:, None] * ws.numpy().astype(np.float64)
+    got = pkg.lmkan_linear_i8(pkg.LinearDesc(n_in, n_out), x.to(dev), w.to(dev), ws.to(dev)).cpu().double().numpy()
+    off = np.abs(got - want)
+    most = 4 * 2.0 ** -24 * np.abs(want) + 2.0 ** -149
+    assert (off <= most).all(), float((off / most).max())
