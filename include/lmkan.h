@@ -412,8 +412,11 @@ typedef struct lmkan_matrices {
  *   workspace_dev / workspace_bytes: at least lmkan_orthogonalize_workspace_bytes(desc)
  *                 bytes, 256-byte aligned
  * Every product keeps 22 bits of its factors or more (elements below 2^-16 of what bounds
- * their matrix: 2^-38 of that) and is summed in float32, norms are summed in float64 and
- * hold for any eps; out is rounded to desc->dtype once.  A matrix of zeros stays zero; one
+ * their matrix: 2^-38 of that) and is summed in float32.  Norms hold for any eps; they are
+ * summed in float64, up to 64 rows (the shorter side) from sums of float32 products.  On
+ * the shapes measured the error is at most 1.5 times that of the same steps in float32, and
+ * less on larger matrices; for schedules that converge, up to 3 times (there 6e-7 of the
+ * result's norm).  out is rounded to desc->dtype once.  A matrix of zeros stays zero; one
  * with a NaN or an infinity becomes NaN (steps > 0) and leaves the others of the batch alone.
  * The result repeats bit for bit between runs.
  */

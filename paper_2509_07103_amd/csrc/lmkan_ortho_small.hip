@@ -3,8 +3,10 @@
 // The steps are those of lmkan_ortho.hip: up to three on the m x m Gram matrix, applied together.  Here the Gram
 // matrix and its polynomials fit the LDS of one workgroup, so that a matrix costs
 //   one launch   where X fits LDS too (whole_kernel): X is read once and the result written once;
-//   five         where it is longer (five steps): Gram matrix in parts, polynomial, apply and next Gram matrix in
-//                parts, polynomial, apply.
+//   1 + 2 g      where it is longer, for g groups of steps that share a Gram matrix (steps_until): Gram matrix in parts,
+//                then polynomial, and apply with the next Gram matrix in parts; 1 + 3 g where more than 16 parts are summed
+//                by a launch of their own.  Five steps: g = 2 up to 32 rows, 5 up to 45, 3 from 46 on.
+//                One of 16 x 70001 takes 49 us, one of 48 x 20000 76, one of 64 x 65536 129, four of 64 x 16384 118.
 // The products with X take 2 m multiply-adds per element and pass; at m = 64 the float32 instructions (157 TFLOP/s)
 // take about as long for that as memory takes for the element, so nothing is gained by splitting factors.  The products
 // of the polynomials are a chain in one workgroup: from m = 33 on, pairs of float16 (lmkan_tile.h) make it shorter.
@@ -845,7 +847,8 @@ void launch_ortho_small(const MatrixShape &s, int steps, const float *schedule, 
     // workgroups a compute unit.  Measured (us, 1 / 4 / 8 / 16 waves): 1681 of 8 x 16 8.9 / 14 / 22 / 50; 1000 of
     // 16 x 100 18 / 13 / 19 / 33; 400 of 10 x 300 27 / 20 / 21 / 22; 25 of 12 x 900 68 / 24 / 17 / 15; 1600 of 30 x 60
     // - / 40 / 48 / 79; 441 of 32 x 218 - / 35 / 31 / 41; one of 32 x 500 - / 33 / 26 / 23; 441 of 48 x 100 - / - / 35 / 45;
-    // 25 of 48 x 500 - / - / 51 / 46; and 1600 of 64 x 64 takes 172, 169 of 144 x 64 34 (twelve waves).
+    // 441 of 48 x 150 - / - / 53 / 66; 441 of 48 x 200 - / - / 76 / 72; 25 of 48 x 500 - / - / 69 / 64; and 1600 of 64 x 64
+    // takes 172, 169 of 144 x 64 35 (twelve waves).
     const int m = s.m(), n = s.n();
     if (m <= 16 && n <= 32) launch<Small<16, 1>, Small<16, 4>>(s, u, a, bounds, ws, stream);
     else if (m <= 16 && n <= 160) launch<Small<16, 4>, Small<16, 4>>(s, u, a, bounds, ws, stream);
