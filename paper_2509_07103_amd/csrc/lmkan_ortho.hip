@@ -12,10 +12,10 @@
 // and grows by up to a^2 (11.9) a step where the eigenvalue is small, which is why not all are taken at once, and
 // steps_until() chooses.
 //
-// Factors are pairs of float16 (lmkan_tile.h): three instructions at the rate of float16 keep 22 bits, which
-// float32 instructions do at a seventh of that rate (library products: 154 against 1130 to 1240 TFLOP/s).  The power of two that a matrix is scaled by follows
-// from the bound of its singular values (schedule_bounds); for X, which is smaller where |U| is not large beside eps,
-// also from |X_0| and the factors of the steps behind it (extra_bits).
+// Factors are pairs of float16 (lmkan_tile.h): three instructions at the rate of float16 keep 22 bits, which float32
+// instructions do at a seventh of that rate (library products: 154 against 1130 to 1240 TFLOP/s).  The power of two that
+// a matrix is scaled by follows from the bound of its singular values (schedule_bounds); for X, which is smaller where
+// |U| is not large beside eps, also from |X_0| and the factors of the steps behind it (extra_bits).
 #include "lmkan_dense.h"
 
 #include <math.h>
