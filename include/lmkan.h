@@ -18,8 +18,8 @@
  *   - Every function that can fail returns an lmkan_status.  Argument errors
  *     are found on the host before anything is launched, so nothing has been
  *     written when a status other than LMKAN_OK or LMKAN_ERR_HIP comes back.
- *   - batch == 0 is legal: nothing is read, and only lmkan_backward writes
- *     (an overwritten grad_coef becomes all zeros).
+ *   - batch == 0 is legal: nothing is read, and only the backward calls write
+ *     (an overwritten gradient that is summed over the batch becomes all zeros).
  *   - Alignment: every tensor its element size.  Faster kernels are chosen at
  *     run time when pointers and widths allow wider accesses (8 bytes for x_dev
  *     and grad_x_dev, 16 bytes for the other tensors).
@@ -487,6 +487,155 @@ size_t lmkan_linear_i8_workspace_bytes(const lmkan_linear *desc, int64_t batch);
 lmkan_status lmkan_linear_i8(const lmkan_linear *desc, int64_t batch, const void *x_dev, const int8_t *w_codes_dev,
                              const float *w_scale_dev, const float *bias_dev, float beta, void *y_dev,
                              void *workspace_dev, size_t workspace_bytes, void *stream);
+
+/*
+ * A normalised layer, z = LayerNorm(x), y = gamma lmKAN(z) + Linear(ReLU(z)): the norm in
+ * front of the layer, whose grid is made for rows of mean 0 and variance 1, activations
+ * kept in 8 bits between the passes, the linear term's gradient from them, and the linear
+ * term as it answers requests that each have an adapter of their own.
+ */
+
+/*
+ * Checkpoints.  A matrix [rows][cols] of activations is held as
+ *   codes [rows][cols] int8, in [-127, 127]
+ *   exps  [rows][ceil(cols / LMKAN_CHECKPOINT_BLOCK)] uint8: a byte for 32 adjacent
+ *         columns of a row (the last block of a row may be shorter)
+ * and stands for value[n][c] = codes[n][c] 2^(exps[n][c / 32] - 133): eight-bit elements of
+ * 1/64 with a shared power of two of bias 127, as in the OCP microscaling formats.
+ * A byte of 255 stands for a NaN in every column of its block.
+ */
+#define LMKAN_CHECKPOINT_BLOCK 32
+
+/* Bytes of exps for a matrix; 0 on a size that is refused below. */
+size_t lmkan_checkpoint_exps_bytes(int64_t rows, int32_t cols);
+
+/*
+ * Rows to a checkpoint.  With m the largest magnitude of a block, the block's power of two
+ * is the least with rint(m / 2^e) <= 127 (at least 2^-133, at most 2^121, where codes end at
+ * 127); codes[n][c] = rint(x[n][c] / 2^e), ties to even.  A block of zeros has a byte of 0, a
+ * block with a NaN or an infinity a byte of 255 and codes of 0.  With LMKAN_LINEAR_RELU
+ * max(x, 0) takes the place of x.
+ *   x_dtype 16-bit rows are widened to float32 first; cols 1 .. LMKAN_MAX_N_IN
+ * codes and exps are overwritten and must not overlap x or each other.
+ */
+lmkan_status lmkan_checkpoint_rows(int64_t rows, int32_t cols, int32_t x_dtype, int32_t flags, const void *x_dev,
+                                   int8_t *codes_dev, uint8_t *exps_dev, void *stream);
+
+/*
+ * Rows back from a checkpoint:
+ *     y[n][c] = f(weight[c] value[n][c] + bias[c]),  f = max(., 0) with LMKAN_LINEAR_RELU
+ * in float32, rounded to y_dtype once: with the weight and bias of a norm its output from the
+ * checkpoint that it wrote.
+ *   weight_dev, bias_dev  [cols] float32; NULL = 1 and 0
+ */
+lmkan_status lmkan_restore_rows(int64_t rows, int32_t cols, int32_t y_dtype, int32_t flags, const int8_t *codes_dev,
+                                const uint8_t *exps_dev, const float *weight_dev, const float *bias_dev, void *y_dev,
+                                void *stream);
+
+/* Layer norm over the columns of a row. */
+typedef struct lmkan_norm {
+    int32_t cols;      /* 1 .. LMKAN_MAX_N_IN                                          */
+    int32_t x_dtype;   /* lmkan_dtype of x and grad_x                                  */
+    int32_t y_dtype;   /* lmkan_dtype of y and grad_y                                  */
+    int32_t flags;     /* LMKAN_NORM_ACCUMULATE or 0                                   */
+    float eps;         /* added to the variance, > 0                                   */
+} lmkan_norm;
+
+#define LMKAN_NORM_ACCUMULATE 1 /* backward adds into grad_weight and grad_bias instead of overwriting */
+
+/*
+ * For every row, with mean and variance (divided by cols) summed in float64,
+ *     mean and rstd = 1 / sqrt(variance + eps), rounded to float32,
+ *     hat[c] = (x[c] - mean) rstd          (float32, two roundings)
+ *     y[c] = weight[c] hat[c] + bias[c]    (rounded to y_dtype once)
+ *   weight_dev, bias_dev  [cols] float32; NULL = 1 and 0
+ *   y_dev                 [rows][cols], overwritten; may be x_dev itself when the types are equal
+ *   stats_dev             [rows][2] float32, mean and rstd, what the backward pass needs; NULL
+ *                         skips them
+ *   codes_dev, exps_dev   checkpoint of hat, as lmkan_checkpoint_rows makes it; NULL (both) skips it
+ * (Statistics in float64: hat does not depend on the order of a sum, so that codes repeat.)
+ */
+lmkan_status lmkan_layer_norm(const lmkan_norm *desc, int64_t rows, const void *x_dev, const float *weight_dev,
+                              const float *bias_dev, void *y_dev, float *stats_dev, int8_t *codes_dev,
+                              uint8_t *exps_dev, void *stream);
+
+/*
+ * Gradients of the norm.  With hat[n][c] = (x[n][c] - mean[n]) rstd[n], or what the checkpoint of it
+ * stands for, d = weight grad_y, and <.> the mean over a row's columns,
+ *     grad_x = rstd (d - <d> - hat <d hat>)
+ *     grad_weight[c] = sum_n grad_y[n][c] hat[n][c],  grad_bias[c] = sum_n grad_y[n][c]
+ *   x_dev                 what the forward call was given, or NULL: then codes_dev and exps_dev, the
+ *                         checkpoint that it wrote (one of the two, not both)
+ *   stats_dev             what the forward call wrote
+ *   weight_dev            NULL = 1
+ *   grad_x_dev            [rows][cols] in x_dtype, overwritten; NULL skips it.  It must not overlap
+ *                         the inputs
+ *   grad_weight_dev, grad_bias_dev  [cols] float32, overwritten, or added to with
+ *                         LMKAN_NORM_ACCUMULATE; NULL skips either.  rows == 0 is a sum of nothing
+ *   workspace_dev / workspace_bytes: at least lmkan_layer_norm_backward_workspace_bytes(desc, rows)
+ *                         bytes, 256-byte aligned (NULL allowed when 0, and when neither grad_weight nor
+ *                         grad_bias is wanted)
+ * Sums are float32, in an order that the sizes fix: the results repeat bit for bit.
+ */
+size_t lmkan_layer_norm_backward_workspace_bytes(const lmkan_norm *desc, int64_t rows);
+lmkan_status lmkan_layer_norm_backward(const lmkan_norm *desc, int64_t rows, const void *x_dev, const int8_t *codes_dev,
+                                       const uint8_t *exps_dev, const float *stats_dev, const float *weight_dev,
+                                       const void *grad_y_dev, void *grad_x_dev, float *grad_weight_dev,
+                                       float *grad_bias_dev, void *workspace_dev, size_t workspace_bytes, void *stream);
+
+/*
+ * Gradients of the linear term's weights and bias from a checkpoint of its input:
+ *     grad_weight[j][e] = sum_n grad_y[n][j] f(value[n][e]),  grad_bias[j] = sum_n grad_y[n][j]
+ * with f = max(., 0) under LMKAN_LINEAR_RELU.  Of the descriptor y_dtype is the type of grad_y;
+ * x_dtype is not used.
+ *   grad_y_dev       [batch][n_out] in y_dtype
+ *   grad_weight_dev  [n_out][n_in] float32, grad_bias_dev [n_out] float32 or NULL; both are
+ *                    overwritten, or added to with LMKAN_LINEAR_ACCUMULATE in the descriptor's flags
+ *   workspace_dev / workspace_bytes: at least lmkan_linear_grad_workspace_bytes(desc, batch)
+ *                    bytes, 256-byte aligned (NULL allowed when 0)
+ * Products keep 24 bits of grad_y (all of a 16-bit one) and all of the values, and are summed in
+ * float32 in an order that the sizes fix: the results repeat bit for bit.  Factors below 2^-126 may
+ * count as zeros.
+ */
+#define LMKAN_LINEAR_ACCUMULATE 2
+size_t lmkan_linear_grad_workspace_bytes(const lmkan_linear *desc, int64_t batch);
+lmkan_status lmkan_linear_grad(const lmkan_linear *desc, int64_t batch, const int8_t *codes_dev, const uint8_t *exps_dev,
+                               const void *grad_y_dev, float *grad_weight_dev, float *grad_bias_dev,
+                               void *workspace_dev, size_t workspace_bytes, void *stream);
+
+/* Low-rank adapters of one linear term. */
+#define LMKAN_MAX_ADAPTERS 65536
+#define LMKAN_MAX_ADAPTER_RANK 256
+typedef struct lmkan_adapters {
+    int32_t count;    /* 1 .. LMKAN_MAX_ADAPTERS                                       */
+    int32_t rank;     /* 1 .. LMKAN_MAX_ADAPTER_RANK                                   */
+    int32_t n_in;     /* 1 .. LMKAN_MAX_N_IN                                           */
+    int32_t n_out;    /* 1 .. LMKAN_MAX_N_OUT                                          */
+    int32_t dtype;    /* lmkan_dtype of a and b                                        */
+    int32_t x_dtype;  /* lmkan_dtype of x                                              */
+    int32_t y_dtype;  /* lmkan_dtype of y                                              */
+    int32_t flags;    /* LMKAN_LINEAR_RELU or 0                                        */
+} lmkan_adapters;
+
+/*
+ * Adds to every row of y what the adapter of its request makes of its row of x:
+ *     y[n] += scale[r] B_r (A_r f(x[n])),  r = index[n],  f = max(., 0) with LMKAN_LINEAR_RELU
+ *   x_dev      [batch][n_in] in x_dtype
+ *   index_dev  [batch] int32; a row whose index is not in [0, count) has no adapter and stays as it is
+ *   a_dev      [count][rank][n_in], b_dev [count][n_out][rank], both in dtype; of lower ranks the rest
+ *              is zero
+ *   scale_dev  [count] float32; NULL = 1
+ *   y_dev      [batch][n_out] in y_dtype, added to in place (lmkan_linear_i8 has written the shared
+ *              projection there); it must not overlap the inputs
+ *   workspace_dev / workspace_bytes: at least lmkan_adapters_workspace_bytes(desc, batch) bytes,
+ *              256-byte aligned
+ * Products and sums are float32 (products of 16-bit factors are exact), y is rounded to its type
+ * once.  The results repeat bit for bit.
+ */
+size_t lmkan_adapters_workspace_bytes(const lmkan_adapters *desc, int64_t batch);
+lmkan_status lmkan_adapters_add(const lmkan_adapters *desc, int64_t batch, const void *x_dev, const int32_t *index_dev,
+                                const void *a_dev, const void *b_dev, const float *scale_dev, void *y_dev,
+                                void *workspace_dev, size_t workspace_bytes, void *stream);
 
 #ifdef __cplusplus
 }

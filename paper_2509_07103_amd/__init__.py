@@ -8,7 +8,12 @@ from .binding import (LMKAN_BF16, LMKAN_F16, LMKAN_F32, LMKAN_FLAG_ACCUMULATE_GR
                       lmkan_locate, lmkan_microbench, MICROBENCH, lmkan_pack, lmkan_time_next_kernel, lmkan_packed_bytes, lmkan_status_string,
                       lmkan_version, lmkan_workspace_bytes,
                       lmkan_orthogonalize, lmkan_orthogonalize_workspace_bytes, lmkan_muon_step, lmkan_quantize_rows,
-                      lmkan_linear_i8, lmkan_linear_i8_workspace_bytes)
+                      lmkan_linear_i8, lmkan_linear_i8_workspace_bytes,
+                      LMKAN_CHECKPOINT_BLOCK, LMKAN_LINEAR_ACCUMULATE, LMKAN_MAX_ADAPTER_RANK, LMKAN_MAX_ADAPTERS,
+                      LMKAN_NORM_ACCUMULATE, AdapterDesc, NormDesc, lmkan_adapters_add, lmkan_adapters_workspace_bytes,
+                      lmkan_checkpoint_exps_bytes, lmkan_checkpoint_rows, lmkan_layer_norm, lmkan_layer_norm_backward,
+                      lmkan_layer_norm_backward_workspace_bytes, lmkan_linear_grad, lmkan_linear_grad_workspace_bytes,
+                      lmkan_restore_rows)
 
 __all__ = [n for n in dir() if n.startswith(("lmkan_", "LMKAN_", "Layer", "Lmkan", "Conv2d", "lib", "MICROBENCH",
-                                            "Linear", "Matrix", "Muon", "QUINTIC"))]
+                                            "Linear", "Matrix", "Muon", "QUINTIC", "Norm", "Adapter"))]

@@ -6,7 +6,7 @@ the current stream.  There is no CPU fallback: if the library is missing or a
 call fails, an exception is raised.
 
 The calls that a program makes per step (forward, backward, pack, the
-convolution, the optimiser's step, the linear term) first go to ``_native`` (csrc/lmkan_torch.cpp), which does the same
+convolution, the optimiser's step, the linear term, the norm, checkpoints, adapters) first go to ``_native`` (csrc/lmkan_torch.cpp), which does the same
 marshalling in native code for the ordinary case and returns None for any
 other; the code here then takes over and raises what there is to raise.
 """
@@ -31,6 +31,11 @@ LMKAN_PACK_TILE = 64
 LMKAN_MAX_GRID = 64
 LMKAN_STATIC_SCRATCH_BYTES = 32 << 20
 LMKAN_LINEAR_RELU = 1
+LMKAN_LINEAR_ACCUMULATE = 2
+LMKAN_NORM_ACCUMULATE = 1
+LMKAN_CHECKPOINT_BLOCK = 32
+LMKAN_MAX_ADAPTERS = 65536
+LMKAN_MAX_ADAPTER_RANK = 256
 LMKAN_MAX_ORTHO_STEPS = 32
 
 _TORCH_DTYPE = {LMKAN_F32: torch.float32, LMKAN_F16: torch.float16, LMKAN_BF16: torch.bfloat16}
@@ -111,6 +116,16 @@ class _Linear(C.Structure):
                 ("flags", C.c_int32)]
 
 
+class _Norm(C.Structure):
+    _fields_ = [("cols", C.c_int32), ("x_dtype", C.c_int32), ("y_dtype", C.c_int32), ("flags", C.c_int32),
+                ("eps", C.c_float)]
+
+
+class _Adapters(C.Structure):
+    _fields_ = [("count", C.c_int32), ("rank", C.c_int32), ("n_in", C.c_int32), ("n_out", C.c_int32),
+                ("dtype", C.c_int32), ("x_dtype", C.c_int32), ("y_dtype", C.c_int32), ("flags", C.c_int32)]
+
+
 @dataclass
 class MatrixDesc:
     """Mirror of ``lmkan_matrices``: a batch of dense matrices [batch][rows][cols].  A table in the layout of
@@ -152,6 +167,42 @@ class LinearDesc:
 
     def c(self) -> _Linear:
         return _Linear(self.n_in, self.n_out, self.x_dtype, self.y_dtype, LMKAN_LINEAR_RELU if self.relu else 0)
+
+
+@dataclass
+class NormDesc:
+    """Mirror of ``lmkan_norm`` (its flag is an argument of the backward call)."""
+    cols: int
+    x_dtype: int = LMKAN_F32
+    y_dtype: int = LMKAN_F32
+    eps: float = 1e-5
+
+    def c(self, accumulate: bool = False) -> _Norm:
+        return _Norm(self.cols, self.x_dtype, self.y_dtype, LMKAN_NORM_ACCUMULATE if accumulate else 0, self.eps)
+
+
+@dataclass
+class AdapterDesc:
+    """Mirror of ``lmkan_adapters``: ``count`` adapters of one rank for a linear term n_in -> n_out; ``dtype`` is that
+    of the adapters."""
+    count: int
+    rank: int
+    n_in: int
+    n_out: int
+    dtype: int = LMKAN_F32
+    x_dtype: int = LMKAN_F32
+    y_dtype: int = LMKAN_F32
+    relu: bool = False
+
+    def c(self) -> _Adapters:
+        return _Adapters(self.count, self.rank, self.n_in, self.n_out, self.dtype, self.x_dtype, self.y_dtype,
+                         LMKAN_LINEAR_RELU if self.relu else 0)
+
+    def a_shape(self):
+        return (self.count, self.rank, self.n_in)
+
+    def b_shape(self):
+        return (self.count, self.n_out, self.rank)
 
 
 # five steps of the quintic that brings singular values from a few thousandths up near one
@@ -218,6 +269,27 @@ def lib() -> C.CDLL:
     L.lmkan_linear_i8.restype = C.c_int
     L.lmkan_linear_i8.argtypes = [np_, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_float,
                                   C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+    vp, lp, ap = C.c_void_p, C.POINTER(_Norm), C.POINTER(_Adapters)
+    L.lmkan_checkpoint_exps_bytes.restype = C.c_size_t
+    L.lmkan_checkpoint_exps_bytes.argtypes = [C.c_int64, C.c_int32]
+    L.lmkan_checkpoint_rows.restype = C.c_int
+    L.lmkan_checkpoint_rows.argtypes = [C.c_int64, C.c_int32, C.c_int32, C.c_int32, vp, vp, vp, vp]
+    L.lmkan_restore_rows.restype = C.c_int
+    L.lmkan_restore_rows.argtypes = [C.c_int64, C.c_int32, C.c_int32, C.c_int32, vp, vp, vp, vp, vp, vp]
+    L.lmkan_layer_norm.restype = C.c_int
+    L.lmkan_layer_norm.argtypes = [lp, C.c_int64, vp, vp, vp, vp, vp, vp, vp, vp]
+    L.lmkan_layer_norm_backward_workspace_bytes.restype = C.c_size_t
+    L.lmkan_layer_norm_backward_workspace_bytes.argtypes = [lp, C.c_int64]
+    L.lmkan_layer_norm_backward.restype = C.c_int
+    L.lmkan_layer_norm_backward.argtypes = [lp, C.c_int64, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
+    L.lmkan_linear_grad_workspace_bytes.restype = C.c_size_t
+    L.lmkan_linear_grad_workspace_bytes.argtypes = [np_, C.c_int64]
+    L.lmkan_linear_grad.restype = C.c_int
+    L.lmkan_linear_grad.argtypes = [np_, C.c_int64, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
+    L.lmkan_adapters_workspace_bytes.restype = C.c_size_t
+    L.lmkan_adapters_workspace_bytes.argtypes = [ap, C.c_int64]
+    L.lmkan_adapters_add.restype = C.c_int
+    L.lmkan_adapters_add.argtypes = [ap, C.c_int64, vp, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
     cp = C.POINTER(_Conv2d)
     L.lmkan_conv2d_rows.restype = C.c_int64
     L.lmkan_conv2d_rows.argtypes = [cp, C.POINTER(C.c_int32), C.POINTER(C.c_int32)]
@@ -231,7 +303,10 @@ def lib() -> C.CDLL:
     native.init(*(C.cast(f, C.c_void_p).value for f in (
         L.lmkan_workspace_bytes, L.lmkan_packed_bytes, L.lmkan_forward, L.lmkan_backward, L.lmkan_conv2d_rows,
         L.lmkan_conv2d_forward, L.lmkan_conv2d_backward, L.lmkan_pack, L.lmkan_orthogonalize_workspace_bytes,
-        L.lmkan_orthogonalize, L.lmkan_muon_step, L.lmkan_linear_i8_workspace_bytes, L.lmkan_linear_i8)))
+        L.lmkan_orthogonalize, L.lmkan_muon_step, L.lmkan_linear_i8_workspace_bytes, L.lmkan_linear_i8,
+        L.lmkan_checkpoint_rows, L.lmkan_restore_rows, L.lmkan_layer_norm, L.lmkan_layer_norm_backward_workspace_bytes,
+        L.lmkan_layer_norm_backward, L.lmkan_linear_grad_workspace_bytes, L.lmkan_linear_grad,
+        L.lmkan_adapters_workspace_bytes, L.lmkan_adapters_add)))
     _native = native
     _lib = L
     return L
@@ -648,4 +723,220 @@ def lmkan_linear_i8(desc: LinearDesc, x: torch.Tensor, w_codes: torch.Tensor, w_
     _check(lib().lmkan_linear_i8(C.byref(desc.c()), batch, xp, wp, sp, bp, beta, yp, _ptr(ws), wsz, _stream(stream)),
            "lmkan_linear_i8")
     _used_on(stream, ws, y)
+    return y
+
+
+def _rows(t: torch.Tensor, dtype: int, cols: int, name: str) -> int:
+    """Rows of a matrix that is checked with ``_here`` later on."""
+    if t.dim() != 2:
+        raise ValueError(f"{name}: expected a matrix {_TORCH_DTYPE[dtype]} (rows, {cols}), got {t.dtype} {tuple(t.shape)}")
+    return t.shape[0]
+
+
+def _here(t: torch.Tensor | None, dtype, shape, name: str) -> int | None:
+    """``_dev``, and the tensor is on the current device, where the library launches."""
+    p = _dev(t, dtype, shape, name)
+    if t is not None and t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name}: on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+    return p
+
+
+def _own_workspace(workspace: torch.Tensor | None, need: int, device):
+    """``_call_workspace``; the caller's is on the current device."""
+    if workspace is not None:
+        _here(workspace, workspace.dtype, workspace.shape, "workspace")
+    return _call_workspace(workspace, need, device)
+
+
+def _exps_shape(rows: int, cols: int):
+    return (rows, (cols + LMKAN_CHECKPOINT_BLOCK - 1) // LMKAN_CHECKPOINT_BLOCK)
+
+
+def lmkan_checkpoint_exps_bytes(rows: int, cols: int) -> int:
+    return lib().lmkan_checkpoint_exps_bytes(rows, cols)
+
+
+def lmkan_checkpoint_rows(x: torch.Tensor, relu: bool = False, stream=None):
+    """x [rows][cols] -> its 8-bit checkpoint (codes int8 [rows][cols], exps uint8 [rows][ceil(cols / 32)])."""
+    if stream is None:
+        done = (_native or _fast()).checkpoint_rows(x, relu)
+        if done is not None:
+            return done
+    if x.dim() != 2 or x.dtype not in _DTYPE_CODE:
+        raise ValueError(f"x: expected a matrix of float32, float16 or bfloat16, got {x.dtype} {tuple(x.shape)}")
+    rows, cols = x.shape
+    xp = _here(x, x.dtype, (rows, cols), "x")
+    codes = torch.empty((rows, cols), dtype=torch.int8, device=x.device)
+    exps = torch.empty(_exps_shape(rows, cols), dtype=torch.uint8, device=x.device)
+    _check(lib().lmkan_checkpoint_rows(rows, cols, _DTYPE_CODE[x.dtype], LMKAN_LINEAR_RELU if relu else 0, xp,
+                                       codes.data_ptr(), exps.data_ptr(), _stream(stream)), "lmkan_checkpoint_rows")
+    _used_on(stream, codes, exps)
+    return codes, exps
+
+
+def lmkan_restore_rows(codes: torch.Tensor, exps: torch.Tensor, weight: torch.Tensor | None = None,
+                       bias: torch.Tensor | None = None, relu: bool = False, dtype: int = LMKAN_F32,
+                       y: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """Rows in ``dtype`` from a checkpoint: f(weight value + bias), f = max(., 0) with ``relu``."""
+    if stream is None:
+        done = (_native or _fast()).restore_rows(codes, exps, weight, bias, relu, dtype, y)
+        if done is not None:
+            return done
+    if codes.dim() != 2:
+        raise ValueError(f"codes: expected a matrix of int8, got {codes.dtype} {tuple(codes.shape)}")
+    if dtype not in _TORCH_DTYPE:
+        raise ValueError(f"dtype: expected LMKAN_F32, LMKAN_F16 or LMKAN_BF16, got {dtype}")
+    rows, cols = codes.shape
+    cp = _here(codes, torch.int8, (rows, cols), "codes")
+    ep = _here(exps, torch.uint8, _exps_shape(rows, cols), "exps")
+    wp = _here(weight, torch.float32, (cols,), "weight")
+    bp = _here(bias, torch.float32, (cols,), "bias")
+    if y is None:
+        y = torch.empty((rows, cols), dtype=_TORCH_DTYPE[dtype], device=codes.device)
+    yp = _here(y, _TORCH_DTYPE[dtype], (rows, cols), "y")
+    _check(lib().lmkan_restore_rows(rows, cols, dtype, LMKAN_LINEAR_RELU if relu else 0, cp, ep, wp, bp, yp,
+                                    _stream(stream)), "lmkan_restore_rows")
+    _used_on(stream, y)
+    return y
+
+
+def lmkan_layer_norm(desc: NormDesc, x: torch.Tensor, weight: torch.Tensor | None = None,
+                     bias: torch.Tensor | None = None, y: torch.Tensor | None = None, keep: bool = False, stream=None):
+    """Returns (y, stats [rows][2], kept): rows normalised over their columns, what the backward call needs of the
+    statistics, and with ``keep`` the checkpoint (codes, exps) of the normalised rows before weight and bias, else
+    None.  ``y`` may be ``x``."""
+    if stream is None:
+        done = (_native or _fast()).layer_norm(desc, x, weight, bias, y, keep)
+        if done is not None:
+            return done
+    rows = _rows(x, desc.x_dtype, desc.cols, "x")
+    xp = _here(x, _TORCH_DTYPE[desc.x_dtype], (rows, desc.cols), "x")
+    wp = _here(weight, torch.float32, (desc.cols,), "weight")
+    bp = _here(bias, torch.float32, (desc.cols,), "bias")
+    if y is None:
+        y = torch.empty((rows, desc.cols), dtype=_TORCH_DTYPE[desc.y_dtype], device=x.device)
+    yp = _here(y, _TORCH_DTYPE[desc.y_dtype], (rows, desc.cols), "y")
+    stats = torch.empty((rows, 2), dtype=torch.float32, device=x.device)
+    codes = torch.empty((rows, desc.cols), dtype=torch.int8, device=x.device) if keep else None
+    exps = torch.empty(_exps_shape(rows, desc.cols), dtype=torch.uint8, device=x.device) if keep else None
+    _check(lib().lmkan_layer_norm(C.byref(desc.c()), rows, xp, wp, bp, yp, stats.data_ptr(), _ptr(codes), _ptr(exps),
+                                  _stream(stream)), "lmkan_layer_norm")
+    _used_on(stream, y, stats, codes, exps)
+    return y, stats, ((codes, exps) if keep else None)
+
+
+def lmkan_layer_norm_backward_workspace_bytes(desc: NormDesc, rows: int) -> int:
+    return lib().lmkan_layer_norm_backward_workspace_bytes(C.byref(desc.c()), rows)
+
+
+def lmkan_layer_norm_backward(desc: NormDesc, grad_y: torch.Tensor, stats: torch.Tensor, x: torch.Tensor | None = None,
+                              kept=None, weight: torch.Tensor | None = None, need_grad_x: bool = True,
+                              need_grad_weight: bool = True, need_grad_bias: bool = True,
+                              grad_x: torch.Tensor | None = None, grad_weight: torch.Tensor | None = None,
+                              grad_bias: torch.Tensor | None = None, accumulate: bool = False, stream=None,
+                              workspace: torch.Tensor | None = None):
+    """Returns (grad_x, grad_weight, grad_bias), None for those not needed, from the rows ``x`` of the forward call or
+    from the checkpoint ``kept`` that it made (one of them).  With ``accumulate`` the last two are added to the tensors
+    given."""
+    if (x is None) == (kept is None):
+        raise ValueError("the backward call takes the rows x or their checkpoint kept, one of the two")
+    if accumulate and ((need_grad_weight and grad_weight is None) or (need_grad_bias and grad_bias is None)):
+        raise ValueError("accumulating into grad_weight and grad_bias needs existing tensors")
+    codes, exps = kept if kept is not None else (None, None)
+    if stream is None:
+        done = (_native or _fast()).layer_norm_backward(desc, grad_y, stats, x, codes, exps, weight, need_grad_x,
+                                                        need_grad_weight, need_grad_bias, grad_x, grad_weight, grad_bias,
+                                                        accumulate, workspace)
+        if done is not None:
+            return done
+    rows, cols, dev = _rows(grad_y, desc.y_dtype, desc.cols, "grad_y"), desc.cols, grad_y.device
+    gp = _here(grad_y, _TORCH_DTYPE[desc.y_dtype], (rows, cols), "grad_y")
+    sp = _here(stats, torch.float32, (rows, 2), "stats")
+    xp = _here(x, _TORCH_DTYPE[desc.x_dtype], (rows, cols), "x")
+    cp = _here(codes, torch.int8, (rows, cols), "codes")
+    ep = _here(exps, torch.uint8, _exps_shape(rows, cols), "exps")
+    wp = _here(weight, torch.float32, (cols,), "weight")
+    if need_grad_x and grad_x is None:
+        grad_x = torch.empty((rows, cols), dtype=_TORCH_DTYPE[desc.x_dtype], device=dev)
+    if need_grad_weight and grad_weight is None:
+        grad_weight = torch.empty((cols,), dtype=torch.float32, device=dev)
+    if need_grad_bias and grad_bias is None:
+        grad_bias = torch.empty((cols,), dtype=torch.float32, device=dev)
+    gxp = _here(grad_x, _TORCH_DTYPE[desc.x_dtype], (rows, cols), "grad_x") if need_grad_x else None
+    gwp = _here(grad_weight, torch.float32, (cols,), "grad_weight") if need_grad_weight else None
+    gbp = _here(grad_bias, torch.float32, (cols,), "grad_bias") if need_grad_bias else None
+    need = lmkan_layer_norm_backward_workspace_bytes(desc, rows) if need_grad_weight or need_grad_bias else 0
+    ws, wsz = _own_workspace(workspace, need, dev)
+    _check(lib().lmkan_layer_norm_backward(C.byref(desc.c(accumulate)), rows, xp, cp, ep, sp, wp, gp, gxp, gwp, gbp,
+                                           _ptr(ws), wsz, _stream(stream)), "lmkan_layer_norm_backward")
+    _used_on(stream, ws, grad_x, grad_weight, grad_bias)
+    return (grad_x if need_grad_x else None, grad_weight if need_grad_weight else None,
+            grad_bias if need_grad_bias else None)
+
+
+def _linear_grad_desc(desc: LinearDesc, accumulate: bool = False) -> _Linear:
+    d = desc.c()
+    d.flags |= LMKAN_LINEAR_ACCUMULATE if accumulate else 0
+    return d
+
+
+def lmkan_linear_grad_workspace_bytes(desc: LinearDesc, batch: int) -> int:
+    return lib().lmkan_linear_grad_workspace_bytes(C.byref(_linear_grad_desc(desc)), batch)
+
+
+def lmkan_linear_grad(desc: LinearDesc, codes: torch.Tensor, exps: torch.Tensor, grad_y: torch.Tensor,
+                      need_grad_bias: bool = True, grad_weight: torch.Tensor | None = None,
+                      grad_bias: torch.Tensor | None = None, accumulate: bool = False, stream=None,
+                      workspace: torch.Tensor | None = None):
+    """Returns (grad_weight [n_out][n_in], grad_bias [n_out] or None), float32, of the linear term whose input is held
+    in the checkpoint (codes, exps); ``grad_y`` is in the descriptor's y_dtype.  With ``accumulate`` they are added to the
+    tensors given."""
+    if accumulate and (grad_weight is None or (need_grad_bias and grad_bias is None)):
+        raise ValueError("accumulating into grad_weight and grad_bias needs existing tensors")
+    if stream is None:
+        done = (_native or _fast()).linear_grad(desc, codes, exps, grad_y, need_grad_bias, grad_weight, grad_bias,
+                                                accumulate, workspace)
+        if done is not None:
+            return done
+    batch, dev = _rows(grad_y, desc.y_dtype, desc.n_out, "grad_y"), grad_y.device
+    gp = _here(grad_y, _TORCH_DTYPE[desc.y_dtype], (batch, desc.n_out), "grad_y")
+    cp = _here(codes, torch.int8, (batch, desc.n_in), "codes")
+    ep = _here(exps, torch.uint8, _exps_shape(batch, desc.n_in), "exps")
+    if grad_weight is None:
+        grad_weight = torch.empty((desc.n_out, desc.n_in), dtype=torch.float32, device=dev)
+    if need_grad_bias and grad_bias is None:
+        grad_bias = torch.empty((desc.n_out,), dtype=torch.float32, device=dev)
+    gwp = _here(grad_weight, torch.float32, (desc.n_out, desc.n_in), "grad_weight")
+    gbp = _here(grad_bias, torch.float32, (desc.n_out,), "grad_bias") if need_grad_bias else None
+    ws, wsz = _own_workspace(workspace, lmkan_linear_grad_workspace_bytes(desc, batch), dev)
+    _check(lib().lmkan_linear_grad(C.byref(_linear_grad_desc(desc, accumulate)), batch, cp, ep, gp, gwp, gbp, _ptr(ws),
+                                   wsz, _stream(stream)), "lmkan_linear_grad")
+    _used_on(stream, ws, grad_weight, grad_bias)
+    return grad_weight, (grad_bias if need_grad_bias else None)
+
+
+def lmkan_adapters_workspace_bytes(desc: AdapterDesc, batch: int) -> int:
+    return lib().lmkan_adapters_workspace_bytes(C.byref(desc.c()), batch)
+
+
+def lmkan_adapters_add(desc: AdapterDesc, x: torch.Tensor, index: torch.Tensor, a: torch.Tensor, b: torch.Tensor,
+                       y: torch.Tensor, scale: torch.Tensor | None = None, stream=None,
+                       workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """y[n] += scale[r] B_r (A_r f(x[n])) in place, r = index[n] (int32); rows whose index is not in [0, count) stay."""
+    if stream is None:
+        done = (_native or _fast()).adapters_add(desc, x, index, a, b, y, scale, workspace)
+        if done is not None:
+            return done
+    batch = _rows(x, desc.x_dtype, desc.n_in, "x")
+    dt = _TORCH_DTYPE[desc.dtype]
+    xp = _here(x, _TORCH_DTYPE[desc.x_dtype], (batch, desc.n_in), "x")
+    ip = _here(index, torch.int32, (batch,), "index")
+    ap = _here(a, dt, desc.a_shape(), "a")
+    bp = _here(b, dt, desc.b_shape(), "b")
+    yp = _here(y, _TORCH_DTYPE[desc.y_dtype], (batch, desc.n_out), "y")
+    sp = _here(scale, torch.float32, (desc.count,), "scale")
+    ws, wsz = _own_workspace(workspace, lmkan_adapters_workspace_bytes(desc, batch), x.device)
+    _check(lib().lmkan_adapters_add(C.byref(desc.c()), batch, xp, ip, ap, bp, sp, yp, _ptr(ws), wsz, _stream(stream)),
+           "lmkan_adapters_add")
+    _used_on(stream, ws)
     return y

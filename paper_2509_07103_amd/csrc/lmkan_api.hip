@@ -9,6 +9,7 @@
 
 #include "lmkan.h"
 #include "lmkan_dense.h"
+#include "lmkan_rows.h"
 #include "lmkan_gather.h"
 #include "lmkan_kernels.h"
 #include "lmkan_sorted.h"
@@ -782,6 +783,218 @@ lmkan_status lmkan_linear_i8(const lmkan_linear *desc, int64_t batch, const void
     drop_stale_error();
     launch_linear_i8(s, x_dev, w_codes_dev, w_scale_dev, bias_dev, beta, y_dev, workspace_dev,
                      static_cast<hipStream_t>(stream));
+    return launch_status();
+}
+
+}  // extern "C"
+
+namespace {
+
+bool apart(const void *p, size_t n, const void *q, size_t m)
+{
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+    return !p || !q || a + n <= b || b + m <= a;
+}
+
+bool rows_ok(int64_t rows, int32_t cols) { return rows >= 0 && rows <= LMKAN_MAX_BATCH && cols >= 1 && cols <= LMKAN_MAX_N_IN; }
+
+lmkan_status check_norm(const lmkan_norm *d, int64_t rows, NormShape *s)
+{
+    if (!d) return LMKAN_ERR_NULL;
+    if (!rows_ok(rows, d->cols)) return LMKAN_ERR_SHAPE;
+    if (!known_dtype(d->x_dtype) || !known_dtype(d->y_dtype) || (d->flags & ~LMKAN_NORM_ACCUMULATE) || !(d->eps > 0.0f) || !isfinite(d->eps))
+        return LMKAN_ERR_UNSUPPORTED;
+    *s = {rows, d->cols, d->x_dtype, d->y_dtype, d->eps, (d->flags & LMKAN_NORM_ACCUMULATE) != 0};
+    return LMKAN_OK;
+}
+
+lmkan_status check_linear_grad(const lmkan_linear *d, int64_t batch, LinearShape *s)
+{
+    if (!d) return LMKAN_ERR_NULL;
+    lmkan_linear plain = *d;
+    plain.flags &= ~LMKAN_LINEAR_ACCUMULATE;
+    return check_linear(&plain, batch, s);
+}
+
+lmkan_status check_adapters(const lmkan_adapters *d, int64_t batch, AdapterShape *s)
+{
+    if (!d) return LMKAN_ERR_NULL;
+    if (batch < 0 || batch > LMKAN_MAX_BATCH || d->count < 1 || d->count > LMKAN_MAX_ADAPTERS || d->rank < 1 || d->rank > LMKAN_MAX_ADAPTER_RANK ||
+        d->n_in < 1 || d->n_in > LMKAN_MAX_N_IN || d->n_out < 1 || d->n_out > LMKAN_MAX_N_OUT)
+        return LMKAN_ERR_SHAPE;
+    if (!known_dtype(d->dtype) || !known_dtype(d->x_dtype) || !known_dtype(d->y_dtype) || (d->flags & ~LMKAN_LINEAR_RELU)) return LMKAN_ERR_UNSUPPORTED;
+    *s = {batch, d->count, d->rank, d->n_in, d->n_out, d->dtype, d->x_dtype, d->y_dtype, (d->flags & LMKAN_LINEAR_RELU) != 0};
+    return LMKAN_OK;
+}
+
+lmkan_status check_workspace(const void *workspace, size_t bytes, size_t need)
+{
+    if (need > 0 && (!workspace || bytes < need)) return LMKAN_ERR_WORKSPACE;
+    return need > 0 && !aligned(workspace, 256) ? LMKAN_ERR_ALIGN : LMKAN_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t lmkan_checkpoint_exps_bytes(int64_t rows, int32_t cols) { return rows_ok(rows, cols) ? (size_t)rows * exp_blocks(cols) : 0; }
+
+lmkan_status lmkan_checkpoint_rows(int64_t rows, int32_t cols, int32_t x_dtype, int32_t flags, const void *x_dev,
+                                   int8_t *codes_dev, uint8_t *exps_dev, void *stream)
+{
+    if (!rows_ok(rows, cols)) return LMKAN_ERR_SHAPE;
+    if (!known_dtype(x_dtype) || (flags & ~LMKAN_LINEAR_RELU)) return LMKAN_ERR_UNSUPPORTED;
+    if (rows == 0) return LMKAN_OK;
+    if (!x_dev || !codes_dev || !exps_dev) return LMKAN_ERR_NULL;
+    if (!aligned(x_dev, dtype_size(x_dtype))) return LMKAN_ERR_ALIGN;
+    const size_t n = (size_t)rows * cols, blocks = (size_t)rows * exp_blocks(cols), x = n * dtype_size(x_dtype);
+    if (!apart(x_dev, x, codes_dev, n) || !apart(x_dev, x, exps_dev, blocks) || !apart(codes_dev, n, exps_dev, blocks)) return LMKAN_ERR_UNSUPPORTED;
+    drop_stale_error();
+    launch_checkpoint(rows, cols, x_dtype, (flags & LMKAN_LINEAR_RELU) != 0, x_dev, codes_dev, exps_dev, static_cast<hipStream_t>(stream));
+    return launch_status();
+}
+
+lmkan_status lmkan_restore_rows(int64_t rows, int32_t cols, int32_t y_dtype, int32_t flags, const int8_t *codes_dev,
+                                const uint8_t *exps_dev, const float *weight_dev, const float *bias_dev, void *y_dev,
+                                void *stream)
+{
+    if (!rows_ok(rows, cols)) return LMKAN_ERR_SHAPE;
+    if (!known_dtype(y_dtype) || (flags & ~LMKAN_LINEAR_RELU)) return LMKAN_ERR_UNSUPPORTED;
+    if (rows == 0) return LMKAN_OK;
+    if (!codes_dev || !exps_dev || !y_dev) return LMKAN_ERR_NULL;
+    if (!aligned(y_dev, dtype_size(y_dtype)) || !aligned(weight_dev, 4) || !aligned(bias_dev, 4)) return LMKAN_ERR_ALIGN;
+    const size_t n = (size_t)rows * cols, y = n * dtype_size(y_dtype), columns = (size_t)cols * 4;
+    if (!apart(y_dev, y, codes_dev, n) || !apart(y_dev, y, exps_dev, (size_t)rows * exp_blocks(cols)) || !apart(y_dev, y, weight_dev, columns) ||
+        !apart(y_dev, y, bias_dev, columns))
+        return LMKAN_ERR_UNSUPPORTED;
+    drop_stale_error();
+    launch_restore(rows, cols, y_dtype, (flags & LMKAN_LINEAR_RELU) != 0, codes_dev, exps_dev, weight_dev, bias_dev, y_dev,
+                   static_cast<hipStream_t>(stream));
+    return launch_status();
+}
+
+lmkan_status lmkan_layer_norm(const lmkan_norm *desc, int64_t rows, const void *x_dev, const float *weight_dev,
+                              const float *bias_dev, void *y_dev, float *stats_dev, int8_t *codes_dev,
+                              uint8_t *exps_dev, void *stream)
+{
+    NormShape s;
+    const lmkan_status st = check_norm(desc, rows, &s);
+    if (st != LMKAN_OK) return st;
+    if (rows == 0) return LMKAN_OK;
+    if (!x_dev || !y_dev || !codes_dev != !exps_dev) return LMKAN_ERR_NULL;
+    if (!aligned(x_dev, dtype_size(s.x_dtype)) || !aligned(y_dev, dtype_size(s.y_dtype)) || !aligned(weight_dev, 4) || !aligned(bias_dev, 4) ||
+        !aligned(stats_dev, 4))
+        return LMKAN_ERR_ALIGN;
+    const struct { const void *p; size_t n; } in[] = {{x_dev, (size_t)rows * s.cols * dtype_size(s.x_dtype)}, {weight_dev, (size_t)s.cols * 4}, {bias_dev, (size_t)s.cols * 4}},
+                                              out[] = {{y_dev, (size_t)rows * s.cols * dtype_size(s.y_dtype)}, {stats_dev, (size_t)rows * 8},
+                                                       {codes_dev, (size_t)rows * s.cols}, {exps_dev, (size_t)rows * exp_blocks(s.cols)}};
+    for (int i = 0; i < 4; ++i) {
+        for (const auto &from : in)
+            if (!apart(from.p, from.n, out[i].p, out[i].n) && !(from.p == x_dev && out[i].p == y_dev && x_dev == y_dev && s.x_dtype == s.y_dtype))
+                return LMKAN_ERR_UNSUPPORTED;
+        for (int k = 0; k < i; ++k)
+            if (!apart(out[k].p, out[k].n, out[i].p, out[i].n)) return LMKAN_ERR_UNSUPPORTED;
+    }
+    drop_stale_error();
+    launch_layer_norm(s, x_dev, weight_dev, bias_dev, y_dev, stats_dev, codes_dev, exps_dev, static_cast<hipStream_t>(stream));
+    return launch_status();
+}
+
+size_t lmkan_layer_norm_backward_workspace_bytes(const lmkan_norm *desc, int64_t rows)
+{
+    NormShape s;
+    return check_norm(desc, rows, &s) == LMKAN_OK ? layer_norm_backward_workspace_bytes(s) : 0;
+}
+
+lmkan_status lmkan_layer_norm_backward(const lmkan_norm *desc, int64_t rows, const void *x_dev, const int8_t *codes_dev,
+                                       const uint8_t *exps_dev, const float *stats_dev, const float *weight_dev,
+                                       const void *grad_y_dev, void *grad_x_dev, float *grad_weight_dev,
+                                       float *grad_bias_dev, void *workspace_dev, size_t workspace_bytes, void *stream)
+{
+    NormShape s;
+    lmkan_status st = check_norm(desc, rows, &s);
+    if (st != LMKAN_OK) return st;
+    const size_t x_size = dtype_size(s.x_dtype), y_size = dtype_size(s.y_dtype), n = (size_t)rows * s.cols, columns = (size_t)s.cols * 4;
+    if (!aligned(x_dev, x_size) || !aligned(grad_x_dev, x_size) || !aligned(grad_y_dev, y_size) || !aligned(stats_dev, 4) || !aligned(weight_dev, 4) ||
+        !aligned(grad_weight_dev, 4) || !aligned(grad_bias_dev, 4))
+        return LMKAN_ERR_ALIGN;
+    if (rows > 0) {
+        if (!stats_dev || !grad_y_dev || !codes_dev != !exps_dev || (!x_dev && !codes_dev)) return LMKAN_ERR_NULL;
+        if (x_dev && codes_dev) return LMKAN_ERR_UNSUPPORTED;
+        const struct { const void *p; size_t n; } in[] = {{x_dev, n * x_size}, {codes_dev, n}, {exps_dev, (size_t)rows * exp_blocks(s.cols)}, {stats_dev, (size_t)rows * 8},
+                                                          {weight_dev, columns}, {grad_y_dev, n * y_size}},
+                                                  out[] = {{grad_x_dev, n * x_size}, {grad_weight_dev, columns}, {grad_bias_dev, columns}};
+        for (const auto &to : out)
+            for (const auto &from : in)
+                if (!apart(from.p, from.n, to.p, to.n)) return LMKAN_ERR_UNSUPPORTED;
+    }
+    if (!apart(grad_weight_dev, columns, grad_bias_dev, columns) || !apart(grad_x_dev, n * x_size, grad_weight_dev, columns) ||
+        !apart(grad_x_dev, n * x_size, grad_bias_dev, columns))
+        return LMKAN_ERR_UNSUPPORTED;
+    st = check_workspace(workspace_dev, workspace_bytes, grad_weight_dev || grad_bias_dev ? layer_norm_backward_workspace_bytes(s) : 0);
+    if (st != LMKAN_OK) return st;
+    drop_stale_error();
+    const NormBackwardArgs a{x_dev, codes_dev, exps_dev, stats_dev, weight_dev, grad_y_dev, grad_x_dev, grad_weight_dev, grad_bias_dev};
+    launch_layer_norm_backward(s, a, workspace_dev, static_cast<hipStream_t>(stream));
+    return launch_status();
+}
+
+size_t lmkan_linear_grad_workspace_bytes(const lmkan_linear *desc, int64_t batch)
+{
+    LinearShape s;
+    return check_linear_grad(desc, batch, &s) == LMKAN_OK ? linear_grad_workspace_bytes(s) : 0;
+}
+
+lmkan_status lmkan_linear_grad(const lmkan_linear *desc, int64_t batch, const int8_t *codes_dev, const uint8_t *exps_dev,
+                               const void *grad_y_dev, float *grad_weight_dev, float *grad_bias_dev,
+                               void *workspace_dev, size_t workspace_bytes, void *stream)
+{
+    LinearShape s;
+    lmkan_status st = check_linear_grad(desc, batch, &s);
+    if (st != LMKAN_OK) return st;
+    if (!grad_weight_dev || (batch > 0 && (!codes_dev || !exps_dev || !grad_y_dev))) return LMKAN_ERR_NULL;
+    if (!aligned(grad_y_dev, dtype_size(s.y_dtype)) || !aligned(grad_weight_dev, 4) || !aligned(grad_bias_dev, 4)) return LMKAN_ERR_ALIGN;
+    const size_t weight = (size_t)s.n_out * s.n_in * 4, bias = (size_t)s.n_out * 4;
+    const struct { const void *p; size_t n; } in[] = {{codes_dev, (size_t)batch * s.n_in}, {exps_dev, (size_t)batch * exp_blocks(s.n_in)},
+                                                      {grad_y_dev, (size_t)batch * s.n_out * dtype_size(s.y_dtype)}};
+    for (const auto &from : in)
+        if (!apart(from.p, from.n, grad_weight_dev, weight) || !apart(from.p, from.n, grad_bias_dev, bias)) return LMKAN_ERR_UNSUPPORTED;
+    if (!apart(grad_weight_dev, weight, grad_bias_dev, bias)) return LMKAN_ERR_UNSUPPORTED;
+    st = check_workspace(workspace_dev, workspace_bytes, linear_grad_workspace_bytes(s));
+    if (st != LMKAN_OK) return st;
+    drop_stale_error();
+    launch_linear_grad(s, (desc->flags & LMKAN_LINEAR_ACCUMULATE) != 0, codes_dev, exps_dev, grad_y_dev, grad_weight_dev, grad_bias_dev,
+                       workspace_dev, static_cast<hipStream_t>(stream));
+    return launch_status();
+}
+
+size_t lmkan_adapters_workspace_bytes(const lmkan_adapters *desc, int64_t batch)
+{
+    AdapterShape s;
+    return check_adapters(desc, batch, &s) == LMKAN_OK && batch > 0 ? adapters_workspace_bytes(s) : 0;
+}
+
+lmkan_status lmkan_adapters_add(const lmkan_adapters *desc, int64_t batch, const void *x_dev, const int32_t *index_dev,
+                                const void *a_dev, const void *b_dev, const float *scale_dev, void *y_dev,
+                                void *workspace_dev, size_t workspace_bytes, void *stream)
+{
+    AdapterShape s;
+    lmkan_status st = check_adapters(desc, batch, &s);
+    if (st != LMKAN_OK) return st;
+    if (batch == 0) return LMKAN_OK;
+    if (!x_dev || !index_dev || !a_dev || !b_dev || !y_dev) return LMKAN_ERR_NULL;
+    const size_t size = dtype_size(s.dtype), x_size = dtype_size(s.x_dtype), y_size = dtype_size(s.y_dtype);
+    if (!aligned(x_dev, x_size) || !aligned(y_dev, y_size) || !aligned(index_dev, 4) || !aligned(a_dev, size) || !aligned(b_dev, size) ||
+        !aligned(scale_dev, 4))
+        return LMKAN_ERR_ALIGN;
+    const size_t y = (size_t)batch * s.n_out * y_size, of_adapters = (size_t)s.count * s.rank * size;
+    if (!apart(y_dev, y, x_dev, (size_t)batch * s.n_in * x_size) || !apart(y_dev, y, index_dev, (size_t)batch * 4) ||
+        !apart(y_dev, y, a_dev, of_adapters * s.n_in) || !apart(y_dev, y, b_dev, of_adapters * s.n_out) || !apart(y_dev, y, scale_dev, (size_t)s.count * 4))
+        return LMKAN_ERR_UNSUPPORTED;
+    st = check_workspace(workspace_dev, workspace_bytes, adapters_workspace_bytes(s));
+    if (st != LMKAN_OK) return st;
+    drop_stale_error();
+    launch_adapters(s, x_dev, index_dev, a_dev, b_dev, scale_dev, y_dev, workspace_dev, static_cast<hipStream_t>(stream));
     return launch_status();
 }
 

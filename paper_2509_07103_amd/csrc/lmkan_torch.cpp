@@ -32,6 +32,15 @@ struct Library {
     decltype(&lmkan_muon_step) muon_step;
     decltype(&lmkan_linear_i8_workspace_bytes) linear_i8_workspace_bytes;
     decltype(&lmkan_linear_i8) linear_i8;
+    decltype(&lmkan_checkpoint_rows) checkpoint_rows;
+    decltype(&lmkan_restore_rows) restore_rows;
+    decltype(&lmkan_layer_norm) layer_norm;
+    decltype(&lmkan_layer_norm_backward_workspace_bytes) layer_norm_backward_workspace_bytes;
+    decltype(&lmkan_layer_norm_backward) layer_norm_backward;
+    decltype(&lmkan_linear_grad_workspace_bytes) linear_grad_workspace_bytes;
+    decltype(&lmkan_linear_grad) linear_grad;
+    decltype(&lmkan_adapters_workspace_bytes) adapters_workspace_bytes;
+    decltype(&lmkan_adapters_add) adapters_add;
 } g_lib;
 
 // attribute names, interned once
@@ -42,6 +51,9 @@ enum { kLinIn, kLinOut, kXDtype, kYDtype, kRelu, kLinearNames };
 PyObject *g_desc_names[kDescNames], *g_conv_names[kConvNames], *g_matrix_names[kMatrixNames], *g_linear_names[kLinearNames], *g_eps_name;
 enum { kLr, kMomentum, kDecay, kScale, kNesterov, kMuonNames };
 PyObject *g_muon_names[kMuonNames];
+enum { kNormCols, kNormX, kNormY, kNormNames };
+enum { kCount, kRank, kAdapterIn, kAdapterOut, kAdapterDtype, kAdapterX, kAdapterY, kAdapterRelu, kAdapterNames };
+PyObject *g_norm_names[kNormNames], *g_adapter_names[kAdapterNames];
 
 template <int N>
 bool read_ints(PyObject *obj, PyObject *const (&names)[N], int32_t (&out)[N])
@@ -397,6 +409,262 @@ PyObject *linear_i8(PyObject *, PyObject *const *args, Py_ssize_t n)
     LMKAN_GUARDED_END
 }
 
+// The operators on rows.  Tensors are on the current device, where the library launches; every output that the caller
+// did not bring is allocated like `like`.
+bool here(const at::Tensor *t, at::ScalarType type, at::IntArrayRef shape)
+{
+    return fits(t, type, shape) && t->device().index() == c10::hip::current_device();
+}
+bool here_or_none(PyObject *o, at::ScalarType type, at::IntArrayRef shape) { return o == Py_None || here(tensor(o), type, shape); }
+
+bool made(PyObject *given, at::ScalarType type, at::IntArrayRef shape, const at::Tensor &like, at::Tensor &out)
+{
+    if (given == Py_None) {
+        out = at::empty(shape, like.options().dtype(type));
+        return true;
+    }
+    const at::Tensor *t = tensor(given);
+    if (!here(t, type, shape)) return false;
+    out = *t;
+    return true;
+}
+
+bool workspace_here(PyObject *given, size_t need, const at::Tensor &like, at::Tensor &ws, size_t &bytes)
+{
+    return any_workspace(given, need, like, ws, bytes) && (given == Py_None || ws.device().index() == c10::hip::current_device());
+}
+
+template <class T>
+T *data_or_null(PyObject *o)
+{
+    const at::Tensor *t = o == Py_None ? nullptr : tensor(o);
+    return t ? static_cast<T *>(t->data_ptr()) : nullptr;
+}
+
+bool truth(PyObject *o, bool &v)
+{
+    v = o == Py_True;
+    return v || o == Py_False;
+}
+
+int64_t exps_of(int64_t cols) { return (cols + LMKAN_CHECKPOINT_BLOCK - 1) / LMKAN_CHECKPOINT_BLOCK; }
+
+// a tuple of objects, which it takes
+template <class... P>
+PyObject *tuple_of(P... objects)
+{
+    PyObject *all[] = {objects...};
+    bool whole = true;
+    for (PyObject *o : all) whole = whole && o;
+    PyObject *t = whole ? PyTuple_Pack((Py_ssize_t)sizeof...(P), objects...) : nullptr;
+    for (PyObject *o : all) Py_XDECREF(o);
+    return t;
+}
+
+// checkpoint_rows(x, relu) -> (codes, exps)
+PyObject *checkpoint_rows(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    if (n != 2) Py_RETURN_NONE;
+    LMKAN_GUARDED_BEGIN
+    const at::Tensor *x = tensor(args[0]);
+    bool relu;
+    if (!x || x->dim() != 2 || !truth(args[1], relu)) Py_RETURN_NONE;
+    const int dtype = x->scalar_type() == at::kFloat ? LMKAN_F32 : x->scalar_type() == at::kHalf ? LMKAN_F16 : LMKAN_BF16;
+    const int64_t rows = x->size(0), cols = x->size(1);
+    if (!here(x, type_of(dtype), {rows, cols}) || cols > LMKAN_MAX_N_IN) Py_RETURN_NONE;
+    const at::Tensor codes = at::empty({rows, cols}, x->options().dtype(at::kChar)), exps = at::empty({rows, exps_of(cols)}, x->options().dtype(at::kByte));
+    lmkan_status st;
+    void *s = current_stream(), *xp = data(*x);
+    int8_t *cp = static_cast<int8_t *>(data(codes));
+    uint8_t *ep = static_cast<uint8_t *>(data(exps));
+    Py_BEGIN_ALLOW_THREADS
+    st = g_lib.checkpoint_rows(rows, (int32_t)cols, dtype, relu ? LMKAN_LINEAR_RELU : 0, xp, cp, ep, s);
+    Py_END_ALLOW_THREADS
+    if (st != LMKAN_OK) Py_RETURN_NONE;
+    return tuple_of(wrap(codes), wrap(exps));
+    LMKAN_GUARDED_END
+}
+
+// restore_rows(codes, exps, weight, bias, relu, dtype, y) -> y
+PyObject *restore_rows(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    if (n != 7) Py_RETURN_NONE;
+    LMKAN_GUARDED_BEGIN
+    const at::Tensor *codes = tensor(args[0]), *exps = tensor(args[1]);
+    bool relu;
+    if (!codes || codes->dim() != 2 || !truth(args[4], relu) || !PyLong_Check(args[5])) Py_RETURN_NONE;
+    const long dtype = PyLong_AsLong(args[5]);
+    if (dtype == -1 && PyErr_Occurred()) PyErr_Clear();
+    const int64_t rows = codes->size(0), cols = codes->size(1);
+    if (dtype < 0 || dtype > 2 || cols > LMKAN_MAX_N_IN || !here(codes, at::kChar, {rows, cols}) || !here(exps, at::kByte, {rows, exps_of(cols)}) ||
+        !here_or_none(args[2], at::kFloat, {cols}) || !here_or_none(args[3], at::kFloat, {cols}))
+        Py_RETURN_NONE;
+    at::Tensor y;
+    if (!made(args[6], type_of((int)dtype), {rows, cols}, *codes, y)) Py_RETURN_NONE;
+    lmkan_status st;
+    void *s = current_stream(), *yp = data(y);
+    const int8_t *cp = static_cast<int8_t *>(data(*codes));
+    const uint8_t *ep = static_cast<uint8_t *>(data(*exps));
+    const float *wp = data_or_null<float>(args[2]), *bp = data_or_null<float>(args[3]);
+    Py_BEGIN_ALLOW_THREADS
+    st = g_lib.restore_rows(rows, (int32_t)cols, (int32_t)dtype, relu ? LMKAN_LINEAR_RELU : 0, cp, ep, wp, bp, yp, s);
+    Py_END_ALLOW_THREADS
+    if (st != LMKAN_OK) Py_RETURN_NONE;
+    return wrap(y);
+    LMKAN_GUARDED_END
+}
+
+bool read_norm(PyObject *desc, bool accumulate, lmkan_norm &d)
+{
+    int32_t v[kNormNames];
+    double eps;
+    if (!read_ints(desc, g_norm_names, v) || !read_double(desc, g_eps_name, eps)) return false;
+    d = {v[kNormCols], v[kNormX], v[kNormY], accumulate ? LMKAN_NORM_ACCUMULATE : 0, (float)eps};
+    return d.cols >= 1 && d.cols <= LMKAN_MAX_N_IN && known_dtype(d.x_dtype) && known_dtype(d.y_dtype);
+}
+
+// layer_norm(desc, x, weight, bias, y, keep) -> (y, stats, (codes, exps) or None)
+PyObject *layer_norm(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    if (n != 6) Py_RETURN_NONE;
+    LMKAN_GUARDED_BEGIN
+    lmkan_norm d;
+    bool keep;
+    const at::Tensor *x = tensor(args[1]);
+    if (!read_norm(args[0], false, d) || !truth(args[5], keep) || !x || x->dim() != 2) Py_RETURN_NONE;
+    const int64_t rows = x->size(0);
+    if (!here(x, type_of(d.x_dtype), {rows, d.cols}) || !here_or_none(args[2], at::kFloat, {d.cols}) || !here_or_none(args[3], at::kFloat, {d.cols}))
+        Py_RETURN_NONE;
+    at::Tensor y, codes, exps;
+    if (!made(args[4], type_of(d.y_dtype), {rows, d.cols}, *x, y)) Py_RETURN_NONE;
+    const at::Tensor stats = at::empty({rows, 2}, x->options().dtype(at::kFloat));
+    if (keep) {
+        codes = at::empty({rows, d.cols}, x->options().dtype(at::kChar));
+        exps = at::empty({rows, exps_of(d.cols)}, x->options().dtype(at::kByte));
+    }
+    lmkan_status st;
+    void *s = current_stream(), *xp = data(*x), *yp = data(y);
+    const float *wp = data_or_null<float>(args[2]), *bp = data_or_null<float>(args[3]);
+    float *sp = static_cast<float *>(data(stats));
+    int8_t *cp = static_cast<int8_t *>(data(codes));
+    uint8_t *ep = static_cast<uint8_t *>(data(exps));
+    Py_BEGIN_ALLOW_THREADS
+    st = g_lib.layer_norm(&d, rows, xp, wp, bp, yp, sp, cp, ep, s);
+    Py_END_ALLOW_THREADS
+    if (st != LMKAN_OK) Py_RETURN_NONE;
+    PyObject *kept = Py_None;
+    if (keep) kept = tuple_of(wrap(codes), wrap(exps));
+    else Py_INCREF(kept);
+    return tuple_of(wrap(y), wrap(stats), kept);
+    LMKAN_GUARDED_END
+}
+
+// layer_norm_backward(desc, grad_y, stats, x, codes, exps, weight, need_x, need_weight, need_bias, grad_x, grad_weight,
+//                     grad_bias, accumulate, workspace) -> (grad_x, grad_weight, grad_bias)
+PyObject *layer_norm_backward(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    if (n != 15) Py_RETURN_NONE;
+    LMKAN_GUARDED_BEGIN
+    lmkan_norm d;
+    bool need_x, need_weight, need_bias, accumulate;
+    const at::Tensor *gy = tensor(args[1]), *stats = tensor(args[2]);
+    if (!truth(args[7], need_x) || !truth(args[8], need_weight) || !truth(args[9], need_bias) || !truth(args[13], accumulate) ||
+        !read_norm(args[0], accumulate, d) || !gy || gy->dim() != 2)
+        Py_RETURN_NONE;
+    const int64_t rows = gy->size(0);
+    const at::ScalarType type = type_of(d.x_dtype);
+    if (!here(gy, type_of(d.y_dtype), {rows, d.cols}) || !here(stats, at::kFloat, {rows, 2}) || !here_or_none(args[3], type, {rows, d.cols}) ||
+        !here_or_none(args[4], at::kChar, {rows, d.cols}) || !here_or_none(args[5], at::kByte, {rows, exps_of(d.cols)}) ||
+        !here_or_none(args[6], at::kFloat, {d.cols}))
+        Py_RETURN_NONE;
+    at::Tensor gx, gw, gb, ws;
+    size_t bytes = 0;
+    if ((need_x && !made(args[10], type, {rows, d.cols}, *gy, gx)) || (need_weight && !made(args[11], at::kFloat, {d.cols}, *gy, gw)) ||
+        (need_bias && !made(args[12], at::kFloat, {d.cols}, *gy, gb)) ||
+        !workspace_here(args[14], need_weight || need_bias ? g_lib.layer_norm_backward_workspace_bytes(&d, rows) : 0, *gy, ws, bytes))
+        Py_RETURN_NONE;
+    lmkan_status st;
+    void *s = current_stream(), *gyp = data(*gy), *gxp = data(gx), *wsp = data(ws);
+    const void *xp = data_or_null<void>(args[3]);
+    const int8_t *cp = data_or_null<int8_t>(args[4]);
+    const uint8_t *ep = data_or_null<uint8_t>(args[5]);
+    const float *sp = static_cast<float *>(data(*stats)), *wp = data_or_null<float>(args[6]);
+    float *gwp = static_cast<float *>(data(gw)), *gbp = static_cast<float *>(data(gb));
+    Py_BEGIN_ALLOW_THREADS
+    st = g_lib.layer_norm_backward(&d, rows, xp, cp, ep, sp, wp, gyp, gxp, gwp, gbp, wsp, bytes, s);
+    Py_END_ALLOW_THREADS
+    if (st != LMKAN_OK) Py_RETURN_NONE;
+    return tuple_of(wrap(gx), wrap(gw), wrap(gb));
+    LMKAN_GUARDED_END
+}
+
+// linear_grad(desc, codes, exps, grad_y, need_bias, grad_weight, grad_bias, accumulate, workspace) -> (grad_weight, grad_bias)
+PyObject *linear_grad(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    if (n != 9) Py_RETURN_NONE;
+    LMKAN_GUARDED_BEGIN
+    int32_t v[kLinearNames];
+    bool need_bias, accumulate;
+    const at::Tensor *codes = tensor(args[1]), *exps = tensor(args[2]), *gy = tensor(args[3]);
+    if (!read_ints(args[0], g_linear_names, v) || !known_dtype(v[kXDtype]) || !known_dtype(v[kYDtype]) || !truth(args[4], need_bias) ||
+        !truth(args[7], accumulate) || !gy || gy->dim() != 2)
+        Py_RETURN_NONE;
+    const lmkan_linear d = {v[kLinIn], v[kLinOut], v[kXDtype], v[kYDtype], (v[kRelu] ? LMKAN_LINEAR_RELU : 0) | (accumulate ? LMKAN_LINEAR_ACCUMULATE : 0)};
+    const int64_t batch = gy->size(0);
+    if (d.n_in < 1 || d.n_out < 1 || !here(gy, type_of(d.y_dtype), {batch, d.n_out}) || !here(codes, at::kChar, {batch, d.n_in}) ||
+        !here(exps, at::kByte, {batch, exps_of(d.n_in)}))
+        Py_RETURN_NONE;
+    at::Tensor gw, gb, ws;
+    size_t bytes = 0;
+    if (!made(args[5], at::kFloat, {d.n_out, d.n_in}, *gy, gw) || (need_bias && !made(args[6], at::kFloat, {d.n_out}, *gy, gb)) ||
+        !workspace_here(args[8], g_lib.linear_grad_workspace_bytes(&d, batch), *gy, ws, bytes))
+        Py_RETURN_NONE;
+    lmkan_status st;
+    void *s = current_stream(), *gyp = data(*gy), *wsp = data(ws);
+    const int8_t *cp = static_cast<int8_t *>(data(*codes));
+    const uint8_t *ep = static_cast<uint8_t *>(data(*exps));
+    float *gwp = static_cast<float *>(data(gw)), *gbp = static_cast<float *>(data(gb));
+    Py_BEGIN_ALLOW_THREADS
+    st = g_lib.linear_grad(&d, batch, cp, ep, gyp, gwp, gbp, wsp, bytes, s);
+    Py_END_ALLOW_THREADS
+    if (st != LMKAN_OK) Py_RETURN_NONE;
+    return tuple_of(wrap(gw), wrap(gb));
+    LMKAN_GUARDED_END
+}
+
+// adapters_add(desc, x, index, a, b, y, scale, workspace) -> y
+PyObject *adapters_add(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    if (n != 8) Py_RETURN_NONE;
+    LMKAN_GUARDED_BEGIN
+    int32_t v[kAdapterNames];
+    const at::Tensor *x = tensor(args[1]), *index = tensor(args[2]), *a = tensor(args[3]), *b = tensor(args[4]), *y = tensor(args[5]);
+    if (!read_ints(args[0], g_adapter_names, v) || !known_dtype(v[kAdapterDtype]) || !known_dtype(v[kAdapterX]) || !known_dtype(v[kAdapterY]) || !x ||
+        x->dim() != 2)
+        Py_RETURN_NONE;
+    const lmkan_adapters d = {v[kCount], v[kRank], v[kAdapterIn], v[kAdapterOut], v[kAdapterDtype], v[kAdapterX], v[kAdapterY],
+                              v[kAdapterRelu] ? LMKAN_LINEAR_RELU : 0};
+    const int64_t batch = x->size(0);
+    const at::ScalarType type = type_of(d.dtype);
+    if (!here(x, type_of(d.x_dtype), {batch, d.n_in}) || !here(index, at::kInt, {batch}) || !here(a, type, {d.count, d.rank, d.n_in}) ||
+        !here(b, type, {d.count, d.n_out, d.rank}) || !here(y, type_of(d.y_dtype), {batch, d.n_out}) || !here_or_none(args[6], at::kFloat, {d.count}))
+        Py_RETURN_NONE;
+    at::Tensor ws;
+    size_t bytes = 0;
+    if (!workspace_here(args[7], g_lib.adapters_workspace_bytes(&d, batch), *x, ws, bytes)) Py_RETURN_NONE;
+    lmkan_status st;
+    void *s = current_stream(), *xp = data(*x), *ap = data(*a), *bp = data(*b), *yp = data(*y), *wsp = data(ws);
+    const int32_t *ip = static_cast<int32_t *>(data(*index));
+    const float *sp = data_or_null<float>(args[6]);
+    Py_BEGIN_ALLOW_THREADS
+    st = g_lib.adapters_add(&d, batch, xp, ip, ap, bp, sp, yp, wsp, bytes, s);
+    Py_END_ALLOW_THREADS
+    if (st != LMKAN_OK) Py_RETURN_NONE;
+    Py_INCREF(args[5]);
+    return args[5];
+    LMKAN_GUARDED_END
+}
+
 // init(the addresses, in the order of Library)
 PyObject *init(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
@@ -422,6 +690,12 @@ PyMethodDef g_methods[] = {{"init", (PyCFunction)(void (*)(void))init, METH_FAST
                            {"orthogonalize", (PyCFunction)(void (*)(void))orthogonalize, METH_FASTCALL, nullptr},
                            {"muon_step", (PyCFunction)(void (*)(void))muon_step, METH_FASTCALL, nullptr},
                            {"linear_i8", (PyCFunction)(void (*)(void))linear_i8, METH_FASTCALL, nullptr},
+                           {"checkpoint_rows", (PyCFunction)(void (*)(void))checkpoint_rows, METH_FASTCALL, nullptr},
+                           {"restore_rows", (PyCFunction)(void (*)(void))restore_rows, METH_FASTCALL, nullptr},
+                           {"layer_norm", (PyCFunction)(void (*)(void))layer_norm, METH_FASTCALL, nullptr},
+                           {"layer_norm_backward", (PyCFunction)(void (*)(void))layer_norm_backward, METH_FASTCALL, nullptr},
+                           {"linear_grad", (PyCFunction)(void (*)(void))linear_grad, METH_FASTCALL, nullptr},
+                           {"adapters_add", (PyCFunction)(void (*)(void))adapters_add, METH_FASTCALL, nullptr},
                            {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
@@ -440,6 +714,10 @@ PyMODINIT_FUNC PyInit__native(void)
     for (int i = 0; i < kMatrixNames; ++i) g_matrix_names[i] = PyUnicode_InternFromString(matrix[i]);
     for (int i = 0; i < kMuonNames; ++i) g_muon_names[i] = PyUnicode_InternFromString(muon[i]);
     for (int i = 0; i < kLinearNames; ++i) g_linear_names[i] = PyUnicode_InternFromString(linear[i]);
+    static const char *norm[] = {"cols", "x_dtype", "y_dtype"};
+    static const char *adapter[] = {"count", "rank", "n_in", "n_out", "dtype", "x_dtype", "y_dtype", "relu"};
+    for (int i = 0; i < kNormNames; ++i) g_norm_names[i] = PyUnicode_InternFromString(norm[i]);
+    for (int i = 0; i < kAdapterNames; ++i) g_adapter_names[i] = PyUnicode_InternFromString(adapter[i]);
     g_eps_name = PyUnicode_InternFromString("eps");
     return PyModule_Create(&g_module);
 }
