@@ -1,65 +1,496 @@
-// Gradients of the linear term's weights and bias from a checkpoint of its input.
+// Gradients of the linear term's weights and bias from a checkpoint of its input:
+//   grad_weight[j][e] = sum_n g[n][j] f(value[n][e]),  grad_bias[j] = sum_n g[n][j].
 #include "lmkan_rows.h"
+
+#include "lmkan_tile.h"
 
 namespace lmkan {
 
 namespace {
 
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+typedef float floatx2 __attribute__((ext_vector_type(2)));
+
+constexpr int kDepth = 64;            // rows of the batch in a stage
+constexpr int kCols = 128;            // inputs of a tile
+constexpr int kWaveRows = 64;         // outputs of a wave
+constexpr int kStageBytes = kCols * kLine;
+constexpr int kScalePitch = kDepth + 4, kScaleFloats = kCols / kBlock * kScalePitch;   // powers of two of a stage
+
+// slot of chunk `chunk` (eight rows of the batch) in the line of input `e`
+__device__ __forceinline__ int grad_slot(int e, int chunk) { return chunk ^ ((e >> 1) & 7) ^ ((e >> 4) & 1); }
+
 struct GradArgs {
     int64_t batch;
-    int n_in, n_out, dtype;
+    int n_in, n_out;
     bool relu, accumulate;
     const int8_t *codes;
     const uint8_t *exps;
     const void *grad_y;
     float *grad_weight, *grad_bias;
+    int down, across;      // tiles
+    int first;             // of the launch, counted through tiles and splits
+    int splits, stages;    // stages: of 64 rows in all
+    int each, more;        // of a split: `each`, one more for the first `more`
+    floatx4 *parts;        // [splits][tiles][wave][GROUPS][lane], or null: one split
+    double *bias_parts;    // [splits][n_out]
+    bool out_by_four;
+    __host__ __device__ int begin(int s) const { return s * each + (s < more ? s : more); }
 };
 
-// 32 x 32 results of a workgroup, four a thread, 32 rows of the batch at a time
-__global__ __launch_bounds__(256) void linear_grad_kernel(GradArgs a)
+// WJ waves lie along the outputs, WAVES / WJ along the inputs: a tile of 64 WJ outputs and 128 inputs
+template <int WJ>
+struct GradTile {
+    static constexpr int WAVES = 4, THREADS = 64 * WAVES, WE = WAVES / WJ, ROWS = kWaveRows * WJ, TE = kCols / WE / 32;   // TE: tiles of 32 inputs of a wave
+    static constexpr int GROUPS = 2 * TE * 4;                                             // groups of four results of a lane
+    static constexpr int CODED = kDepth * kCols / 4 / THREADS;                            // rows of codes of a thread in a stage
+};
+
+// Group q of a lane's results: adjacent inputs e .. e + 3 of output j, within the workgroup's tile
+template <int WJ>
+__device__ __forceinline__ void place_of(int wave, int lane, int q, int *j, int *e)
 {
-    __shared__ float g[32][33], v[32][33];
-    const int across = (a.n_in + 31) / 32, ti = blockIdx.x / across, tj = blockIdx.x - ti * across;
-    const int j0 = ti * 32, e0 = tj * 32, lane = threadIdx.x & 31, part = threadIdx.x >> 5;
-    float acc[4] = {}, bias[4] = {};
-    for (int64_t n0 = 0; n0 < a.batch; n0 += 32) {
-        for (int k = part; k < 32; k += 8) {
-            const int64_t n = n0 + k;
-            const int j = j0 + lane, e = e0 + lane;
-            g[k][lane] = n < a.batch && j < a.n_out ? load_as_float(a.grad_y, n * a.n_out + j, a.dtype) : 0.0f;
-            v[k][lane] = n < a.batch && e < a.n_in
-                             ? rectify(value_of(a.codes[n * a.n_in + e], a.exps[n * exp_blocks(a.n_in) + e / kBlock]), a.relu)
-                             : 0.0f;
-        }
-        __syncthreads();
-        for (int k = 0; k < 32; ++k)
-            for (int i = 0; i < 4; ++i) {
-                acc[i] = fmaf(g[k][part * 4 + i], v[k][lane], acc[i]);
-                bias[i] += g[k][part * 4 + i];
-            }
-        __syncthreads();
-    }
-    for (int i = 0; i < 4; ++i) {
-        const int j = j0 + part * 4 + i, e = e0 + lane;
-        if (j >= a.n_out) continue;
-        if (e < a.n_in) {
-            float *to = a.grad_weight + (int64_t)j * a.n_in + e;
-            *to = a.accumulate ? *to + acc[i] : acc[i];
-        }
-        if (a.grad_bias && e == 0) a.grad_bias[j] = a.accumulate ? a.grad_bias[j] + bias[i] : bias[i];
+    typedef GradTile<WJ> T;
+    const int wj = wave / T::WE, we = wave % T::WE, part = q & 3, et = (q >> 2) % T::TE, jt = (q >> 2) / T::TE;
+    *j = wj * kWaveRows + 2 * (lane & 31) + jt;
+    *e = (we * T::TE + et) * 32 + 8 * part + 4 * (lane >> 5);
+}
+
+__device__ __forceinline__ void store_group(const GradArgs &a, int j, int e, floatx4 v)
+{
+    if (j >= a.n_out || e >= a.n_in) return;
+    float *to = a.grad_weight + (int64_t)j * a.n_in + e;
+    if (a.out_by_four) {
+        floatx4 *p = reinterpret_cast<floatx4 *>(to);
+        *p = a.accumulate ? *p + v : v;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (e + i < a.n_in) to[i] = a.accumulate ? to[i] + v[i] : v[i];
     }
 }
 
+// Eight adjacent rows of two adjacent outputs, as they lie in memory
+template <int DTYPE>
+struct RawPair {
+    floatx2 v[8];
+};
+template <>
+struct RawPair<LMKAN_F16> {
+    uint32_t v[8];
+};
+template <>
+struct RawPair<LMKAN_BF16> {
+    uint32_t v[8];
+};
+template <int DTYPE>
+constexpr int parts_of() { return DTYPE == LMKAN_F32 ? 3 : DTYPE == LMKAN_F16 ? 2 : 1; }
+
+// the upper halves of two words, `a` in the lower half
+__device__ __forceinline__ uint32_t upper_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
+__device__ __forceinline__ uint32_t bits(float v) { return __builtin_bit_cast(uint32_t, v); }
+__device__ __forceinline__ float cut(float v) { return __builtin_bit_cast(float, bits(v) & 0xffff0000u); }
+
+// Eight values to parts of bfloat16, of 8 bits each, cut off one after the other: their sum is the value, exactly
+template <int N>
+__device__ __forceinline__ void to_parts(const float (&v)[8], bf16x8 (&to)[N])
+{
+    uint32_t w[N][4];
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+        float a = v[i], b = v[i + 1];
+#pragma unroll
+        for (int p = 0; p < N; ++p) {
+            w[p][i / 2] = upper_halves(bits(a), bits(b));
+            if (p + 1 < N) a -= cut(a), b -= cut(b);
+        }
+    }
+#pragma unroll
+    for (int p = 0; p < N; ++p) to[p] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const intx4 *>(w[p]));
+}
+
+// Those of output t (0 or 1) of a pair
+template <int DTYPE>
+__device__ __forceinline__ float value_in(const RawPair<DTYPE> &r, int i, int t)
+{
+    if constexpr (DTYPE == LMKAN_F32) return r.v[i][t];
+    else if constexpr (DTYPE == LMKAN_F16) return (float)__builtin_bit_cast(_Float16, (uint16_t)(r.v[i] >> (16 * t)));
+    else return __builtin_bit_cast(float, t ? r.v[i] & 0xffff0000u : r.v[i] << 16);
+}
+template <int DTYPE>
+__device__ __forceinline__ float sum_of(const RawPair<DTYPE> &r, int t)
+{
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = value_in(r, i, t);
+    return ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+}
+template <int DTYPE, int N>
+__device__ __forceinline__ void to_parts(const RawPair<DTYPE> &r, bf16x8 (&to)[2][N])
+{
+    if constexpr (DTYPE == LMKAN_BF16) {
+        intx4 w[2];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            w[0][i] = (int)__builtin_amdgcn_perm(r.v[2 * i + 1], r.v[2 * i], 0x05040100u);
+            w[1][i] = (int)upper_halves(r.v[2 * i], r.v[2 * i + 1]);
+        }
+        to[0][0] = __builtin_bit_cast(bf16x8, w[0]), to[1][0] = __builtin_bit_cast(bf16x8, w[1]);
+    } else {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = value_in(r, i, t);
+            to_parts(v, to[t]);
+        }
+    }
+}
+
+// max(., 0) of four codes (a block that stands for NaN has codes of zero and a scale of NaN)
+__device__ __forceinline__ uint32_t positive_codes(uint32_t four)
+{
+    const uint32_t sign = four & 0x80808080u;
+    return four & ~(sign | (sign - (sign >> 7)));
+}
+
+// Reads of `bytes` of memory: beyond its end, and everywhere where `bytes` is negative, they give zero
+struct Buffer {
+    __amdgpu_buffer_rsrc_t rsrc;
+    __device__ __forceinline__ Buffer(const char *base, int bytes)
+        : rsrc(__builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base), 0, bytes > 0 ? bytes : 0, 0x00027000))
+    {
+    }
+    __device__ __forceinline__ uint32_t word(unsigned at) const { return __builtin_amdgcn_raw_buffer_load_b32(rsrc, at, 0, 0); }
+    __device__ __forceinline__ uint32_t half(unsigned at) const { return (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rsrc, at, 0, 0); }
+    __device__ __forceinline__ uint32_t byte(unsigned at) const { return (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(rsrc, at, 0, 0); }
+    __device__ __forceinline__ floatx2 two_floats(unsigned at) const
+    {
+        return __builtin_bit_cast(floatx2, __builtin_amdgcn_raw_buffer_load_b64(rsrc, at, 0, 0));
+    }
+};
+
+// The rows of one matrix, stage by stage: 64 rows take at most 2^30 + 2^11 bytes
+struct Stages {
+    const char *base;
+    int64_t left;   // bytes
+    int pitch;
+    __device__ __forceinline__ Stages(const void *p, int64_t batch, int bytes, int stage)
+        : base(static_cast<const char *>(p) + (int64_t)stage * kDepth * bytes), left((batch - (int64_t)stage * kDepth) * bytes), pitch(bytes)
+    {
+    }
+    __device__ __forceinline__ void next()
+    {
+        base += (int64_t)(kDepth * pitch), left -= (int64_t)(kDepth * pitch);
+    }
+    // rows from `row` of the stage on
+    __device__ __forceinline__ Buffer at(int row) const
+    {
+        const int most = left < 0x7fffffff ? (int)left : 0x7fffffff;
+        return Buffer(base + row * pitch, most - row * pitch);
+    }
+};
+
+// ALIGNED: pairs of outputs and fours of codes lie at multiples of their size
+template <int DTYPE, int WJ, bool ALIGNED>
+__global__ __launch_bounds__(GradTile<WJ>::THREADS, 2) void linear_grad_kernel(GradArgs a)
+{
+    typedef GradTile<WJ> T;
+    constexpr int P = parts_of<DTYPE>();
+    constexpr int AHEAD = 2;   // steps of 16 rows that are under way
+    __shared__ __align__(16) char lds[2 * kStageBytes + 2 * kScaleFloats * (int)sizeof(float)];
+    const int tiles = a.down * a.across, total = tiles * a.splits;
+    const int id = a.first + (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);   // (workgroups on one die: adjacent tiles of the same rows)
+    if (id >= total) return;
+    const int split = id / tiles, tile = id - split * tiles;
+    int ti, tj;
+    grouped_tile(tile, a.down, a.across, &ti, &tj);
+    const int j0 = ti * T::ROWS, e0 = tj * kCols;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wj = wave / T::WE, we = wave % T::WE;
+    const int from = a.begin(split), to = a.begin(split + 1);
+
+    // Gradients: outputs j, j + 1, rows 8 (lane / 32) on of every 16.  What lies beyond the last row reads as zero; what lies
+    // beyond the last column belongs to results that are dropped.
+    constexpr unsigned kSize = DTYPE == LMKAN_F32 ? 4 : 2;
+    const int j = j0 + wj * kWaveRows + 2 * (lane & 31);
+    const int pitch = a.n_out * (int)kSize;
+    const unsigned at = (unsigned)(lane >> 5) * 8 * (unsigned)pitch + (unsigned)j * kSize;
+    const auto load_pair = [&](const Stages &rows, int step) {
+        RawPair<DTYPE> r;
+        const Buffer b = rows.at(16 * step);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const unsigned to = at + i * (unsigned)pitch;
+            if constexpr (DTYPE == LMKAN_F32) r.v[i] = b.two_floats(to);
+            else r.v[i] = ALIGNED ? b.word(to) : b.half(to) | b.half(to + 2) << 16;
+        }
+        return r;
+    };
+
+    // codes: inputs e .. e + 3, some adjacent rows of a stage
+    const int per_row = exp_blocks(a.n_in);
+    const int row0 = (threadIdx.x >> 5) * T::CODED, ec = 4 * (threadIdx.x & 31), e = e0 + ec;
+    struct Codes {
+        uint32_t v[T::CODED];
+    };
+    const auto load_codes = [&](const Stages &rows) {
+        Codes c;
+        const Buffer b = rows.at(0);
+#pragma unroll
+        for (int i = 0; i < T::CODED; ++i) {
+            const unsigned from = (unsigned)(row0 + i) * (unsigned)a.n_in + (unsigned)e;
+            c.v[i] = ALIGNED ? b.word(from) : b.byte(from) | b.byte(from + 1) << 8 | b.byte(from + 2) << 16 | b.byte(from + 3) << 24;
+        }
+        return c;
+    };
+    const auto rectified = [&](Codes c) {
+        if (a.relu)
+#pragma unroll
+            for (int i = 0; i < T::CODED; ++i) c.v[i] = positive_codes(c.v[i]);
+        return c;
+    };
+    // powers of two: a row and a block of inputs a thread, for all threads in LDS [block][row]
+    float *const scales = reinterpret_cast<float *>(lds + 2 * kStageBytes);
+    const bool scaling = threadIdx.x < kDepth * 4;
+    const auto load_exp = [&](const Stages &rows) {
+        return scaling ? rows.at(0).byte((threadIdx.x >> 2) * (unsigned)per_row + (unsigned)e0 / kBlock + (threadIdx.x & 3)) : 0;
+    };
+    const auto store_scale = [&](uint32_t byte, float *to) {
+        if (scaling) to[(threadIdx.x & 3) * kScalePitch + (threadIdx.x >> 2)] = value_of(1, (int)byte);
+    };
+    // column k of a thread's codes, as bfloat16
+    const auto store_column = [&](const Codes &c, int k, const float *scale, char *buffer) {
+        float v[T::CODED], by[T::CODED];
+#pragma unroll
+        for (int i = 0; i < T::CODED; i += 4)
+            *reinterpret_cast<floatx4 *>(by + i) = *reinterpret_cast<const floatx4 *>(scale + (ec / kBlock) * kScalePitch + row0 + i);
+#pragma unroll
+        for (int i = 0; i < T::CODED; ++i) v[i] = (float)(int8_t)(c.v[i] >> (8 * k)) * by[i];
+        uint32_t w[T::CODED / 2];
+#pragma unroll
+        for (int i = 0; i < T::CODED / 2; ++i) w[i] = upper_halves(bits(v[2 * i]), bits(v[2 * i + 1]));
+        char *to = buffer + (ec + k) * kLine + grad_slot(ec + k, row0 / 8) * 16 + row0 % 8 * 2;
+        if constexpr (T::CODED == 8) *reinterpret_cast<uint4 *>(to) = make_uint4(w[0], w[1], w[2], w[3]);
+        else *reinterpret_cast<uint2 *>(to) = make_uint2(w[0], w[1]);
+    };
+
+    const auto load_fragments = [&](const char *buffer, int step, bf16x8 (&v)[T::TE]) {
+#pragma unroll
+        for (int k = 0; k < T::TE; ++k) {
+            const int row = (we * T::TE + k) * 32 + (lane & 31);
+            v[k] = *reinterpret_cast<const bf16x8 *>(buffer + row * kLine + grad_slot(row, 2 * step + (lane >> 5)) * 16);
+        }
+    };
+
+    floatx16 acc[2][T::TE];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int k = 0; k < T::TE; ++k) acc[t][k] = floatx16{};
+    const bool with_bias = a.grad_bias && tj == 0 && we == 0;
+    double bias[2] = {};
+    if (from < to) {
+        // (stages beyond the last are read too, as zeros beyond the last row, and not used)
+        Stages rows(a.grad_y, a.batch, pitch, from), codes(a.codes, a.batch, a.n_in, from), exps(a.exps, a.batch, per_row, from);
+        RawPair<DTYPE> raw[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) raw[k] = load_pair(rows, k);
+        const Codes first = rectified(load_codes(codes));
+        store_scale(load_exp(exps), scales);
+        exps.next();
+        store_scale(load_exp(exps), scales + kScaleFloats);
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < 4; ++k) store_column(first, k, scales, lds);
+        codes.next();
+        Codes c = load_codes(codes);
+        __syncthreads();
+        for (int s = from; s < to; ++s) {
+            const int now = s - from & 1;
+            const char *buffer = lds + now * kStageBytes;
+            codes.next(), exps.next();
+            Stages ahead = rows;
+            ahead.next();
+            const Codes later = load_codes(codes);
+            c = rectified(c);
+            const uint32_t byte = load_exp(exps);
+            bf16x8 v[T::TE];
+            load_fragments(buffer, 0, v);
+#pragma unroll
+            for (int step = 0; step < 4; ++step) {
+                bf16x8 g[2][P];
+                to_parts(raw[step % AHEAD], g);
+                if (with_bias)
+#pragma unroll
+                    for (int t = 0; t < 2; ++t)
+                        bias[t] += (double)sum_of(raw[step % AHEAD], t);
+                raw[step % AHEAD] = load_pair(step + AHEAD < 4 ? rows : ahead, (step + AHEAD) & 3);
+                store_column(c, step, scales + (now ^ 1) * kScaleFloats, lds + (now ^ 1) * kStageBytes);
+                bf16x8 then[T::TE];
+                if (step < 3) load_fragments(buffer, step + 1, then);
+#pragma unroll
+                for (int p = P - 1; p >= 0; --p)
+#pragma unroll
+                    for (int k = 0; k < T::TE; ++k)
+#pragma unroll
+                        for (int t = 0; t < 2; ++t) acc[t][k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[k], g[t][p], acc[t][k], 0, 0, 0);
+                if (step < 3)
+#pragma unroll
+                    for (int k = 0; k < T::TE; ++k) v[k] = then[k];
+            }
+            rows = ahead;
+            c = later;
+            store_scale(byte, scales + now * kScaleFloats);
+            __syncthreads();
+        }
+    }
+    if (with_bias)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            bias[t] += __shfl_xor(bias[t], 32, 64);
+            if (lane < 32 && j + t < a.n_out) {
+                if (a.parts) a.bias_parts[(int64_t)split * a.n_out + j + t] = bias[t];
+                else a.grad_bias[j + t] = a.accumulate ? a.grad_bias[j + t] + (float)bias[t] : (float)bias[t];
+            }
+        }
+#pragma unroll
+    for (int q = 0; q < T::GROUPS; ++q) {
+        const floatx16 &t = acc[(q >> 2) / T::TE][(q >> 2) % T::TE];
+        const floatx4 v = {t[4 * (q & 3)], t[4 * (q & 3) + 1], t[4 * (q & 3) + 2], t[4 * (q & 3) + 3]};
+        if (a.parts) {
+            a.parts[(((int64_t)split * tiles + tile) * T::WAVES + wave) * (T::GROUPS * 64) + q * 64 + lane] = v;
+        } else {
+            int jo, eo;
+            place_of<WJ>(wave, lane, q, &jo, &eo);
+            store_group(a, j0 + jo, e0 + eo, v);
+        }
+    }
+}
+
+// The sums of 64 groups' parts a workgroup: a wave takes every fourth split, and the waves' sums meet in LDS
+template <int WJ>
+__global__ __launch_bounds__(256) void linear_grad_join_kernel(GradArgs a)
+{
+    typedef GradTile<WJ> T;
+    __shared__ floatx4 sums[3][64];
+    __shared__ double bias_sums[3][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t groups = (int64_t)a.down * a.across * T::WAVES * T::GROUPS * 64, i = (int64_t)blockIdx.x * 64 + lane;
+    const bool biased = a.grad_bias && i < a.n_out;
+    floatx4 sum = {0, 0, 0, 0};
+    double bias = 0.0;
+#pragma unroll 8
+    for (int s = wave; s < a.splits; s += 4) sum += a.parts[s * groups + i];
+    if (biased)
+        for (int s = wave; s < a.splits; s += 4) bias += a.bias_parts[(int64_t)s * a.n_out + i];
+    if (wave > 0) sums[wave - 1][lane] = sum, bias_sums[wave - 1][lane] = bias;
+    __syncthreads();
+    if (wave > 0) return;
+#pragma unroll
+    for (int w = 0; w < 3; ++w) sum += sums[w][lane], bias += bias_sums[w][lane];
+    const int tile = (int)(blockIdx.x / (T::WAVES * T::GROUPS)), rest = (int)(blockIdx.x % (T::WAVES * T::GROUPS));
+    int ti, tj, j, e;
+    grouped_tile(tile, a.down, a.across, &ti, &tj);
+    place_of<WJ>(rest / T::GROUPS, lane, rest % T::GROUPS, &j, &e);
+    store_group(a, ti * T::ROWS + j, tj * kCols + e, sum);
+    if (biased) a.grad_bias[i] = a.accumulate ? a.grad_bias[i] + (float)bias : (float)bias;
+}
+
+// ---- host ------------------------------------------------------------------------------------------------------------
+
+constexpr int kUnits = 256;   // compute units
+
+struct Plan {
+    int wj, down, across, splits, stages;
+};
+
+// Tile and splits by what a call takes in us: stages of a workgroup, fitted to 18 shapes (8192 rows of 1024 -> 1024, float32:
+// 3.7 a stage of 256 outputs alone on a compute unit and 6.5 two at a time, 2.0 of 128 outputs; bfloat16 1.5), parts written
+// and joined at 8.5 TB/s (64 MiB 11 us a launch, 16 MiB 5).  Measured (us, best / next other tile / next other number of
+// splits): 8192 of 1024 -> 1024 float32 64 / 67 / 65; 5000 of 500 -> 333 29 / 35 / 32; 65536 of 128 -> 128 32 / 33 / 40;
+// 4096 of 4096 -> 4096 bfloat16 139 / 203 / 174.
+Plan plan_of(const LinearShape &s, bool whole)
+{
+    Plan best = {};
+    double least = 1e300;
+    const int stages = (int)((s.batch + kDepth - 1) / kDepth);
+    const int parts = s.y_dtype == LMKAN_F32 ? 3 : s.y_dtype == LMKAN_F16 ? 2 : 1;
+    for (int wj = whole ? 4 : 2; wj >= 1; wj /= 2) {
+        const int down = (s.n_out + kWaveRows * wj - 1) / (kWaveRows * wj), across = (s.n_in + kCols - 1) / kCols;
+        const int64_t tiles = (int64_t)down * across;
+        const double stage = wj == 4 ? 0.4 + 1.1 * parts : wj == 2 ? 0.5 + 0.5 * parts : 0.6 + 0.45 * parts;
+        for (int splits = 1; splits <= 512 && splits <= (stages > 0 ? stages : 1); splits *= 2) {
+            if (splits > 1 && tiles * splits > 4 * kUnits) break;
+            const int64_t turns = (tiles * splits + kUnits - 1) / kUnits;
+            const double bytes = (double)tiles * splits * wj * kWaveRows * kCols * sizeof(float);
+            const double cost = ((turns / 2) * 1.75 + turns % 2) * ((stages + splits - 1) / splits + 1) * stage + (splits > 1 ? 3.0 + bytes / 8e6 : 0.0);
+            if (cost < least) least = cost, best = {wj, down, across, splits, stages};
+        }
+    }
+    return best;
+}
+
+size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
+
+size_t parts_bytes(const Plan &p) { return align256((size_t)p.splits * p.down * p.across * p.wj * kWaveRows * kCols * sizeof(float)); }
+
+size_t plan_bytes(const LinearShape &s, const Plan &p)
+{
+    return p.splits > 1 ? parts_bytes(p) + align256((size_t)p.splits * s.n_out * sizeof(double)) : 0;
+}
+
+bool whole_shape(const LinearShape &s) { return s.n_out % 2 == 0 && s.n_in % 4 == 0; }
+
+template <int DTYPE, int WJ>
+void launch(GradArgs a, bool whole, hipStream_t stream)
+{
+    const int64_t total = (int64_t)a.down * a.across * a.splits;
+    for (int64_t first = 0; first < total; first += kMostGroups) {
+        const unsigned groups = (unsigned)((total - first < kMostGroups ? total - first : kMostGroups) + 7) / 8 * 8;
+        a.first = (int)first;
+        if (whole) linear_grad_kernel<DTYPE, WJ, true><<<groups, GradTile<WJ>::THREADS, 0, stream>>>(a);
+        else if constexpr (WJ < 4) linear_grad_kernel<DTYPE, WJ, false><<<groups, GradTile<WJ>::THREADS, 0, stream>>>(a);
+    }
+    if (!a.parts) return;
+    // (a group of the join for every four results of the tiles, which are at least as many as the outputs)
+    linear_grad_join_kernel<WJ><<<(unsigned)(a.down * a.across * GradTile<WJ>::WAVES * GradTile<WJ>::GROUPS), 256, 0, stream>>>(a);
+}
+
+template <int DTYPE>
+void launch_type(int wj, const GradArgs &a, bool whole, hipStream_t stream)
+{
+    if (wj == 4) launch<DTYPE, 4>(a, whole, stream);
+    else if (wj == 2) launch<DTYPE, 2>(a, whole, stream);
+    else launch<DTYPE, 1>(a, whole, stream);
+}
+
+bool aligned_to(const void *p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+
 }  // namespace
 
-size_t linear_grad_workspace_bytes(const LinearShape &) { return 0; }
+size_t linear_grad_workspace_bytes(const LinearShape &s)
+{
+    // (whether the tensors are aligned is not known here)
+    const size_t some = plan_bytes(s, plan_of(s, false)), all = whole_shape(s) ? plan_bytes(s, plan_of(s, true)) : 0;
+    return some > all ? some : all;
+}
 
 void launch_linear_grad(const LinearShape &s, bool accumulate, const int8_t *codes, const uint8_t *exps, const void *grad_y,
-                        float *grad_weight, float *grad_bias, void *, hipStream_t stream)
+                        float *grad_weight, float *grad_bias, void *workspace, hipStream_t stream)
 {
-    const GradArgs a{s.batch, s.n_in, s.n_out, s.y_dtype, s.relu, accumulate, codes, exps, grad_y, grad_weight, grad_bias};
-    const int64_t tiles = (int64_t)((s.n_in + 31) / 32) * ((s.n_out + 31) / 32);
-    linear_grad_kernel<<<(unsigned)tiles, 256, 0, stream>>>(a);
+    const bool whole = whole_shape(s) && aligned_to(grad_y, s.y_dtype == LMKAN_F32 ? 8 : 4) && aligned_to(codes, 4);
+    const Plan p = plan_of(s, whole);
+    GradArgs a{s.batch, s.n_in, s.n_out, s.relu, accumulate, codes, exps, grad_y, grad_weight, grad_bias, p.down, p.across, 0, p.splits, p.stages,
+               p.stages / p.splits, p.stages % p.splits, nullptr, nullptr, s.n_in % 4 == 0 && aligned_to(grad_weight, 16)};
+    if (p.splits > 1) {
+        a.parts = static_cast<floatx4 *>(workspace);
+        a.bias_parts = reinterpret_cast<double *>(static_cast<char *>(workspace) + parts_bytes(p));
+    }
+    if (s.y_dtype == LMKAN_F32) launch_type<LMKAN_F32>(p.wj, a, whole, stream);
+    else if (s.y_dtype == LMKAN_F16) launch_type<LMKAN_F16>(p.wj, a, whole, stream);
+    else launch_type<LMKAN_BF16>(p.wj, a, whole, stream);
 }
 
 }  // namespace lmkan
