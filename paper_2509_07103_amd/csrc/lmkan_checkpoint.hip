@@ -1,58 +1,153 @@
 // Activations to 8-bit checkpoints and back.  A block of 32 columns shares a power of two, so that both directions are
 // exact but for the one rounding to a whole number, and a value (7 bits and a sign) is exact in 16-bit types too.
+//
+// Both are bound by memory.  A lane takes pieces of 4 or 8 adjacent elements (16 bytes; one element where rows are not
+// aligned), 8 or 4 lanes a block; a row goes to as many lanes as give each up to four pieces, which are under way together.
 #include "lmkan_rows.h"
 
 namespace lmkan {
 
 namespace {
 
-// 32 lanes a block of a row
-__global__ __launch_bounds__(256) void checkpoint_kernel(int64_t blocks, int cols, int dtype, bool relu, const void *x, int8_t *codes, uint8_t *exps)
+constexpr int kTaken = 4;   // pieces of a lane that are under way
+
+struct RowsArgs {
+    int64_t rows;
+    int cols, dtype;
+    bool relu;
+    int lanes_log;   // of a row
+    const void *x;
+    int8_t *codes;
+    uint8_t *exps;
+    const float *weight, *bias;
+    void *y;
+};
+
+template <int E, int DTYPE>
+__global__ __launch_bounds__(256) void checkpoint_kernel(RowsArgs a)
 {
-    const int per_row = exp_blocks(cols);
-    for (int64_t b = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); b < blocks; b += (int64_t)gridDim.x * 8) {
-        const int64_t row = b / per_row;
-        const int col = (int)(b - row * per_row) * kBlock + (threadIdx.x & 31);
-        const float v = col < cols ? rectify(load_as_float(x, row * cols + col, dtype), relu) : 0.0f;
-        uint32_t top = magnitude_bits(v);
-        for (int d = 16; d > 0; d >>= 1) {
-            const uint32_t other = (uint32_t)__shfl_xor((int)top, d, 64);
-            top = top > other ? top : other;
+    const int lanes = 1 << a.lanes_log, per_row = exp_blocks(a.cols), pieces = per_row * (kBlock / E);
+    const int lane = threadIdx.x & (lanes - 1), rows = 256 >> a.lanes_log;
+    for (int64_t row = (int64_t)blockIdx.x * rows + (threadIdx.x >> a.lanes_log); row < a.rows; row += (int64_t)gridDim.x * rows) {
+        const void *x = row_at(a.x, row * a.cols, DTYPE);
+        int8_t *codes = a.codes + row * a.cols;
+        uint8_t *exps = a.exps + row * per_row;
+        for (int p0 = lane; p0 < pieces; p0 += kTaken * lanes) {
+            float v[kTaken][E];
+#pragma unroll
+            for (int k = 0; k < kTaken; ++k) {
+                const int c = (p0 + k * lanes) * E;
+                load_piece<E, DTYPE>(x, c < a.cols ? c : 0, v[k]);   // (beyond the end: zeros instead)
+            }
+#pragma unroll
+            for (int k = 0; k < kTaken; ++k) {
+                const int c = (p0 + k * lanes) * E;
+                if (p0 + k * lanes >= pieces) break;
+#pragma unroll
+                for (int i = 0; i < E; ++i) v[k][i] = c < a.cols ? rectify(v[k][i], a.relu) : 0.0f;
+                uint32_t w[(E + 3) / 4];
+                const int byte = encode_piece(v[k], w);
+                if (c < a.cols) {
+                    store_codes_piece<E>(codes + c, w);
+                    if (c % kBlock == 0) exps[c / kBlock] = (uint8_t)byte;
+                }
+            }
         }
-        const int byte = block_byte(top);
-        if (col < cols) codes[row * cols + col] = (int8_t)code_of(v, byte);
-        if ((threadIdx.x & 31) == 0) exps[b] = (uint8_t)byte;
     }
 }
 
-__global__ __launch_bounds__(256) void restore_kernel(int64_t elems, int cols, int dtype, bool relu, const int8_t *codes, const uint8_t *exps,
-                                                      const float *weight, const float *bias, void *y)
+template <int E>
+__global__ __launch_bounds__(256) void restore_kernel(RowsArgs a)
 {
-    const int per_row = exp_blocks(cols);
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < elems; i += (int64_t)gridDim.x * 256) {
-        const int64_t row = i / cols;
-        const int col = (int)(i - row * cols);
-        float v = value_of(codes[i], exps[row * per_row + col / kBlock]);
-        v = fmaf(weight ? weight[col] : 1.0f, v, bias ? bias[col] : 0.0f);
-        store_from_float(y, i, dtype, rectify(v, relu));
+    const int lanes = 1 << a.lanes_log, per_row = exp_blocks(a.cols);
+    const int lane = threadIdx.x & (lanes - 1), rows = 256 >> a.lanes_log;
+    for (int64_t row = (int64_t)blockIdx.x * rows + (threadIdx.x >> a.lanes_log); row < a.rows; row += (int64_t)gridDim.x * rows) {
+        const int8_t *codes = a.codes + row * a.cols;
+        void *y = row_at(a.y, row * a.cols, a.dtype);
+        const uint8_t *exps = a.exps + row * per_row;
+        for (int c0 = lane * E; c0 < a.cols; c0 += kTaken * lanes * E) {
+            uint32_t w[kTaken][(E + 3) / 4];
+            int byte[kTaken];
+#pragma unroll
+            for (int k = 0; k < kTaken; ++k) {
+                const int c = c0 + k * lanes * E, from = c < a.cols ? c : c0;
+                load_codes_piece<E>(codes + from, w[k]);
+                byte[k] = exps[from / kBlock];
+            }
+#pragma unroll
+            for (int k = 0; k < kTaken; ++k) {
+                const int c = c0 + k * lanes * E;
+                if (c >= a.cols) break;
+                float v[E];
+                values_of<E>(w[k], byte[k], v);
+                if (a.weight || a.bias) {
+                    float m[E], b[E];
+                    if (a.weight) load_piece<E, LMKAN_F32>(a.weight, c, m);
+                    if (a.bias) load_piece<E, LMKAN_F32>(a.bias, c, b);
+#pragma unroll
+                    for (int i = 0; i < E; ++i) v[i] = fmaf(a.weight ? m[i] : 1.0f, v[i], a.bias ? b[i] : 0.0f);
+                }
+#pragma unroll
+                for (int i = 0; i < E; ++i) v[i] = rectify(v[i], a.relu);
+                store_piece(y, c, a.dtype, v);
+            }
+        }
     }
 }
 
-int64_t at_most(int64_t n, int64_t most) { return n < most ? n : most; }
+// Lanes of a row: each has up to kTaken pieces, and blocks are whole
+int lanes_log(int cols, int e)
+{
+    int log = e == 1 ? 5 : e == 4 ? 3 : 2;
+    while (log < 8 && cols > (kTaken * e) << log) ++log;
+    return log;
+}
+
+unsigned groups(int64_t rows, int log)
+{
+    const int64_t n = (rows + (256 >> log) - 1) / (256 >> log);
+    return (unsigned)(n < kMostGroups ? n : kMostGroups);
+}
+
+template <int E>
+void launch_checkpoint_type(const RowsArgs &a, hipStream_t stream)
+{
+    const unsigned n = groups(a.rows, a.lanes_log);
+    if (a.dtype == LMKAN_F32) {
+        if constexpr (E < 8) checkpoint_kernel<E, LMKAN_F32><<<n, 256, 0, stream>>>(a);
+    } else if (a.dtype == LMKAN_F16) {
+        checkpoint_kernel<E, LMKAN_F16><<<n, 256, 0, stream>>>(a);
+    } else {
+        checkpoint_kernel<E, LMKAN_BF16><<<n, 256, 0, stream>>>(a);
+    }
+}
 
 }  // namespace
 
 void launch_checkpoint(int64_t rows, int cols, int dtype, bool relu, const void *x, int8_t *codes, uint8_t *exps, hipStream_t stream)
 {
-    const int64_t blocks = rows * exp_blocks(cols);
-    checkpoint_kernel<<<(unsigned)at_most((blocks + 7) / 8, 8192), 256, 0, stream>>>(blocks, cols, dtype, relu, x, codes, exps);
+    RowsArgs a{rows, cols, dtype, relu, 0, x, codes, exps};
+    const auto fits = [&](int e) { return pieces_ok(e, cols, x, dtype) && reinterpret_cast<uintptr_t>(codes) % e == 0; };
+    const int e = dtype != LMKAN_F32 && fits(8) ? 8 : fits(4) ? 4 : 1;
+    a.lanes_log = lanes_log(cols, e);
+    if (e == 8) launch_checkpoint_type<8>(a, stream);
+    else if (e == 4) launch_checkpoint_type<4>(a, stream);
+    else launch_checkpoint_type<1>(a, stream);
 }
 
 void launch_restore(int64_t rows, int cols, int dtype, bool relu, const int8_t *codes, const uint8_t *exps, const float *weight,
                     const float *bias, void *y, hipStream_t stream)
 {
-    const int64_t elems = rows * cols;
-    restore_kernel<<<(unsigned)at_most((elems + 255) / 256, 8192), 256, 0, stream>>>(elems, cols, dtype, relu, codes, exps, weight, bias, y);
+    RowsArgs a{rows, cols, dtype, relu, 0, nullptr, const_cast<int8_t *>(codes), const_cast<uint8_t *>(exps), weight, bias, y};
+    const auto fits = [&](int e) {
+        return pieces_ok(e, cols, y, dtype) && reinterpret_cast<uintptr_t>(codes) % e == 0 && pieces_ok(4, 4, weight, LMKAN_F32) && pieces_ok(4, 4, bias, LMKAN_F32);
+    };
+    const int e = dtype != LMKAN_F32 && fits(8) ? 8 : fits(4) ? 4 : 1;
+    a.lanes_log = lanes_log(cols, e);
+    const unsigned n = groups(rows, a.lanes_log);
+    if (e == 8) restore_kernel<8><<<n, 256, 0, stream>>>(a);
+    else if (e == 4) restore_kernel<4><<<n, 256, 0, stream>>>(a);
+    else restore_kernel<1><<<n, 256, 0, stream>>>(a);
 }
 
 }  // namespace lmkan

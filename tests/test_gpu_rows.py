@@ -517,7 +517,7 @@ def _guarded(t, dev, shift):
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("shift", [1, 3, 8])
 def test_pointers_anywhere_and_nothing_written_beyond(dev, shape, dtype, shift):
-    """Tensors that start on an element's boundary only give the same bits, and nothing around an output changes."""
+    """Tensors that start on an element's boundary only: the same results, and nothing around an output changes."""
     rows, cols = shape
     code, n_out = CODE[dtype], 37
     x, w, b = _rows(rows, cols, dtype, seed=220).to(dev), _randn(cols, seed=221).to(dev), _randn(cols, seed=222).to(dev)
@@ -546,9 +546,22 @@ def test_pointers_anywhere_and_nothing_written_beyond(dev, shape, dtype, shift):
     added2, check = _guarded(gl, dev, shift)
     checks.append(check)
     pkg.lmkan_adapters_add(adapters, put(x), put(index), put(a), put(bb), added2)
-    for got, want in [(y2, y), (stats2, stats), (kept2[0], kept[0]), (kept2[1], kept[1]), (gx2, gx), (gw2, gw), (gb2, gb), (back2, back), (lw2, lw),
-                      (lb2, lb), (added2, added)]:
+    for got, want in [(y2, y), (stats2, stats), (kept2[0], kept[0]), (kept2[1], kept[1]), (back2, back)]:
         assert torch.equal(got, want)
+    # sums whose order may go by the alignment: both within their bounds of the exact sum
+    hat = (x.cpu().double() - stats[:, :1].cpu().double()) * stats[:, 1:].cpu().double()
+    g, k = gy.cpu().double(), 2 * (min(rows, 1300) + 11) * U
+    want, tol = _norm_gradients(hat, stats[:, 1:].cpu().double(), g, w.cpu().double())
+    _within(gx2, gx.cpu().double(), 2 * tol + 2 * _out(want, dtype), "grad_x")
+    _within(gw2, gw.cpu().double(), k * (g * hat).abs().sum(dim=0), "grad_weight")
+    _within(gb2, gb.cpu().double(), k * g.abs().sum(dim=0), "grad_bias")
+    v, g = _values(kept[0].cpu(), kept[1].cpu()), gl.cpu().double()
+    _within(lw2, lw.cpu().double(), 2 * (rows / 4 + 64) * U * torch.sqrt(g.square().T @ v.square()), "the linear term's weight")
+    _within(lb2, lb.cpu().double(), 2 * (rows / 4 + 64) * U * g.square().sum(dim=0).sqrt(), "the linear term's bias")
+    r = index.cpu().long()
+    low = torch.einsum("nki,ni->nk", a.cpu().double().abs()[r], x.cpu().double().abs())
+    size = torch.einsum("njk,nk->nj", bb.cpu().double().abs()[r], low)
+    _within(added2, added.cpu().double(), 2 * ((cols + 5 + 16) * U * size + 2 * U * added.cpu().double().abs() + _out(added.cpu().double(), dtype)), "y")
     assert all(c() for c in checks)
 
 
