@@ -604,7 +604,7 @@ lmkan_status lmkan_linear_grad(const lmkan_linear *desc, int64_t batch, const in
                                void *workspace_dev, size_t workspace_bytes, void *stream);
 
 /* Low-rank adapters of one linear term. */
-#define LMKAN_MAX_ADAPTERS 65536
+#define LMKAN_MAX_ADAPTERS 16384
 #define LMKAN_MAX_ADAPTER_RANK 256
 typedef struct lmkan_adapters {
     int32_t count;    /* 1 .. LMKAN_MAX_ADAPTERS                                       */
@@ -628,7 +628,7 @@ typedef struct lmkan_adapters {
  *   y_dev      [batch][n_out] in y_dtype, added to in place (lmkan_linear_i8 has written the shared
  *              projection there); it must not overlap the inputs
  *   workspace_dev / workspace_bytes: at least lmkan_adapters_workspace_bytes(desc, batch) bytes,
- *              256-byte aligned
+ *              256-byte aligned (NULL allowed when 0)
  * Products and sums are float32 (products of 16-bit factors are exact), y is rounded to its type
  * once.  The results repeat bit for bit.
  */

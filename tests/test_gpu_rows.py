@@ -458,7 +458,7 @@ def _check_adapters(dev, data, relu, scaled, w="f32", x_type="f32", y_type="f32"
 
 ADAPTERS = [(1, 1, 1, 1, 1), (1, 64, 64, 8, 4), (1, 4096, 100, 16, 3), (3, 37, 19, 5, 2), (16, 128, 128, 16, 4), (17, 130, 70, 17, 3), (48, 256, 300, 33, 20),
             (65, 100, 33, 64, 65), (200, 64, 500, 100, 5), (130, 500, 40, 256, 2), (1000, 96, 72, 7, 300), (600, 1000, 16, 1, 1), (33, 7, 1100, 128, 1),
-            (2049, 40, 24, 12, 6), (300, 16, 16, 4, 65536)]
+            (2049, 40, 24, 12, 6), (300, 16, 16, 4, 16384), (3000, 64, 48, 8, 16384), (40000, 24, 20, 3, 50)]
 
 
 @pytest.mark.parametrize("shape", ADAPTERS, ids=str)

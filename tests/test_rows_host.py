@@ -122,18 +122,24 @@ def _adapters(batch=4, x=_at(0), index=_at(1), a=_at(2), b=_at(3), scale=_at(4),
 
 
 @pytest.mark.parametrize("kw,status", [
-    (dict(batch=-1), SHAPE), (dict(count=0), SHAPE), (dict(count=65537), SHAPE), (dict(rank=0), SHAPE), (dict(rank=257), SHAPE),
+    (dict(batch=-1), SHAPE), (dict(count=0), SHAPE), (dict(count=16385), SHAPE), (dict(rank=0), SHAPE), (dict(rank=257), SHAPE),
     (dict(n_in=0), SHAPE), (dict(n_out=0), SHAPE), (dict(n_in=131071), SHAPE), (dict(n_out=4194241), SHAPE),
     (dict(dtype=3), UNSUPPORTED), (dict(x_dtype=-1), UNSUPPORTED), (dict(y_dtype=5), UNSUPPORTED), (dict(flags=2), UNSUPPORTED),
     (dict(x=None), NULL), (dict(index=None), NULL), (dict(a=None), NULL), (dict(b=None), NULL), (dict(y=None), NULL),
     (dict(x=ODD), ALIGN), (dict(index=ODD), ALIGN), (dict(a=ODD), ALIGN), (dict(b=ODD), ALIGN), (dict(scale=ODD), ALIGN), (dict(y=ODD), ALIGN),
     (dict(y=_at(0)), UNSUPPORTED), (dict(y=_at(1)), UNSUPPORTED), (dict(y=_at(2)), UNSUPPORTED), (dict(y=_at(3)), UNSUPPORTED),
-    (dict(y=_at(4)), UNSUPPORTED), (dict(ws=None), WORKSPACE), (dict(nbytes=C.c_size_t(0)), WORKSPACE),
-    (dict(ws=C.c_void_p(0xa00000010)), ALIGN),
-    (dict(batch=0, x=None, index=None, a=None, b=None, y=None, ws=None, nbytes=C.c_size_t(0)), OK),
+    (dict(y=_at(4)), UNSUPPORTED), (dict(batch=0, x=None, index=None, a=None, b=None, y=None, ws=None, nbytes=C.c_size_t(0)), OK),
 ])
 def test_adapters_refuse(kw, status):
     assert _adapters(**kw) == status
+
+
+def test_adapters_refuse_workspaces():
+    big = dict(batch=4096, n_in=1024, n_out=1024, rank=32, count=8)
+    assert pkg.lmkan_adapters_workspace_bytes(pkg.AdapterDesc(8, 32, 1024, 1024), 4096) > 256
+    assert _adapters(ws=None, **big) == WORKSPACE and _adapters(nbytes=C.c_size_t(256), **big) == WORKSPACE
+    assert _adapters(ws=C.c_void_p(0xa00000010), **big) == ALIGN
+    assert pkg.lmkan_adapters_workspace_bytes(pkg.AdapterDesc(0, 32, 1024, 1024), 4096) == 0
 
 
 def test_missing_descriptors():
