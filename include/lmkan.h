@@ -604,7 +604,7 @@ lmkan_status lmkan_linear_grad(const lmkan_linear *desc, int64_t batch, const in
                                void *workspace_dev, size_t workspace_bytes, void *stream);
 
 /* Low-rank adapters of one linear term. */
-#define LMKAN_MAX_ADAPTERS 16384
+#define LMKAN_MAX_ADAPTERS 8192
 #define LMKAN_MAX_ADAPTER_RANK 256
 typedef struct lmkan_adapters {
     int32_t count;    /* 1 .. LMKAN_MAX_ADAPTERS                                       */

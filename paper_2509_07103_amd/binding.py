@@ -34,7 +34,7 @@ LMKAN_LINEAR_RELU = 1
 LMKAN_LINEAR_ACCUMULATE = 2
 LMKAN_NORM_ACCUMULATE = 1
 LMKAN_CHECKPOINT_BLOCK = 32
-LMKAN_MAX_ADAPTERS = 16384
+LMKAN_MAX_ADAPTERS = 8192
 LMKAN_MAX_ADAPTER_RANK = 256
 LMKAN_MAX_ORTHO_STEPS = 32
 

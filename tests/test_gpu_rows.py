@@ -458,7 +458,7 @@ def _check_adapters(dev, data, relu, scaled, w="f32", x_type="f32", y_type="f32"
 
 ADAPTERS = [(1, 1, 1, 1, 1), (1, 64, 64, 8, 4), (1, 4096, 100, 16, 3), (3, 37, 19, 5, 2), (16, 128, 128, 16, 4), (17, 130, 70, 17, 3), (48, 256, 300, 33, 20),
             (65, 100, 33, 64, 65), (200, 64, 500, 100, 5), (130, 500, 40, 256, 2), (1000, 96, 72, 7, 300), (600, 1000, 16, 1, 1), (33, 7, 1100, 128, 1),
-            (2049, 40, 24, 12, 6), (300, 16, 16, 4, 16384), (3000, 64, 48, 8, 16384), (40000, 24, 20, 3, 50)]
+            (2049, 40, 24, 12, 6), (300, 16, 16, 4, 8192), (3000, 64, 48, 8, 8192), (40000, 24, 20, 3, 50)]
 
 
 @pytest.mark.parametrize("shape", ADAPTERS, ids=str)
@@ -474,6 +474,15 @@ def test_adapters_match_float64(dev, shape):
 def test_adapters_in_every_type(dev, w, x, y):
     for shape in [(5, 100, 60, 6, 3), (70, 128, 96, 16, 3), (300, 64, 130, 40, 2)]:
         _check_adapters(dev, _adapters(*shape, w=w, x=x, y=y, seed=190), True, True, w, x, y)
+
+
+@pytest.mark.parametrize("rank", [1, 6, 8, 16, 20, 32, 48, 64, 65, 100, 128, 129, 200, 256])
+@pytest.mark.parametrize("types", ["f32 f32 f32", "bf16 bf16 bf16", "f16 f16 f32", "bf16 f32 f32", "f32 f16 bf16"])
+def test_adapters_of_every_rank_with_many_rows(dev, rank, types):
+    """More rows than one launch takes: sorted by adapter, a few hundred of each and some tiles not full."""
+    w, x, y = types.split()
+    for n_in, n_out, relu in [(256, 160, True), (333, 77, False), (1200, 520, False)]:
+        _check_adapters(dev, _adapters(700, n_in, n_out, rank, 3, w=w, x=x, y=y, seed=195), relu, True, w, x, y)
 
 
 @pytest.mark.parametrize("kind", ["one", "none", "runs", "last", "beyond"])
