@@ -41,8 +41,6 @@ struct AdapterArgs {
     int outputs;        // of a workgroup of the kernel `up`
 };
 
-typedef uint32_t uintx2 __attribute__((ext_vector_type(2)));
-
 // Four elements as they lie in memory, and as float32.  WIDE: float32; else 16 bits, float16 when `half`
 template <bool WIDE>
 struct Raw;
@@ -64,6 +62,10 @@ __device__ __forceinline__ Raw<WIDE> fetch_four(const void *row, int at, int lef
         if constexpr (TOGETHER) {
             r.v = *reinterpret_cast<const floatx4 *>(p + (left > 0 ? at : 0));
         } else {
+            if (left >= 4) {
+                r.v = load_words<floatx4, true>(p + at);
+                return r;
+            }
             float e[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) e[i] = p[i < left ? at + i : 0];
@@ -74,6 +76,10 @@ __device__ __forceinline__ Raw<WIDE> fetch_four(const void *row, int at, int lef
         if constexpr (TOGETHER) {
             r.v = *reinterpret_cast<const uintx2 *>(p + (left > 0 ? at : 0));
         } else {
+            if (left >= 4) {
+                r.v = load_words<uintx2, true>(p + at);
+                return r;
+            }
             uint32_t e[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) e[i] = p[i < left ? at + i : 0];
@@ -115,14 +121,13 @@ __device__ __forceinline__ floatx4 rectify_four(floatx4 f, bool relu)
 template <bool X, bool W, bool IN4, bool RANK4>
 __global__ __launch_bounds__(kFewOutputs) void adapters_few_kernel(AdapterArgs a)
 {
-    constexpr int kRanks = 16, kAhead = 4;   // values of A f(x) at a time; fours of B that are fetched before they are known
-    __shared__ float parts[kFewOutputs / 64][kRanks];
+    constexpr int kWaves = kFewOutputs / 64, kRanks = W ? 4 : 8, kPieces = 4, kAhead = 4;   // kAhead: fours of B that are fetched before A f(x) is known
     __shared__ float low[LMKAN_MAX_ADAPTER_RANK];
     const AdapterShape &s = a.s;
     const int64_t n = blockIdx.x;
     const int r = a.index[n];
     if (r < 0 || r >= s.count) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int j = blockIdx.y * kFewOutputs + threadIdx.x, seen = j < s.n_out ? j : s.n_out - 1;
     const bool x_half = s.x_dtype == LMKAN_F16, w_half = s.dtype == LMKAN_F16;
     const void *const up = row_at(a.b, ((int64_t)r * s.n_out + seen) * s.rank, s.dtype);
@@ -131,37 +136,44 @@ __global__ __launch_bounds__(kFewOutputs) void adapters_few_kernel(AdapterArgs a
     for (int k = 0; k < kAhead; ++k) ahead[k] = fetch_four<W, RANK4>(up, 4 * k, s.rank - 4 * k);
     const float before = load_as_float(a.y, n * s.n_out + seen, s.y_dtype);
     const void *const x = row_at(a.x, n * s.n_in, s.x_dtype);
-    for (int k0 = 0; k0 < s.rank; k0 += kRanks) {
+    // a wave takes every eighth rank, kRanks of them and kPieces pieces of the row at a time
+    for (int k0 = wave; k0 < s.rank; k0 += kWaves * kRanks) {
         const void *const down = row_at(a.a, ((int64_t)r * s.rank + k0) * s.n_in, s.dtype);
-        const int most = s.rank - k0 - 1;
         float sum[kRanks] = {};
-        for (int c = threadIdx.x * 4; c < s.n_in; c += 4 * kFewOutputs) {
-            const int left = s.n_in - c;
-            const floatx4 v = rectify_four(widen(fetch_four<X, IN4>(x, c, left), left, x_half), s.relu);
-            Raw<W> w[kRanks];
+        for (int c0 = 4 * lane; c0 < s.n_in; c0 += 256 * kPieces) {
+            Raw<X> v[kPieces];
+            Raw<W> w[kRanks][kPieces];
 #pragma unroll
-            for (int k = 0; k < kRanks; ++k) w[k] = fetch_four<W, IN4>(row_at(down, (int64_t)(k < most ? k : most) * s.n_in, W ? LMKAN_F32 : LMKAN_F16), c, left);
+            for (int p = 0; p < kPieces; ++p) v[p] = fetch_four<X, IN4>(x, c0 + 256 * p, s.n_in - c0 - 256 * p);
 #pragma unroll
             for (int k = 0; k < kRanks; ++k) {
-                const floatx4 f = widen(w[k], left, w_half);
+                if (k0 + kWaves * k >= s.rank) break;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) sum[k] = fmaf(f[i], v[i], sum[k]);
+                for (int p = 0; p < kPieces; ++p)
+                    w[k][p] = fetch_four<W, IN4>(row_at(down, (int64_t)(kWaves * k) * s.n_in, W ? LMKAN_F32 : LMKAN_F16), c0 + 256 * p, s.n_in - c0 - 256 * p);
+            }
+            floatx4 f[kPieces];
+#pragma unroll
+            for (int p = 0; p < kPieces; ++p) f[p] = rectify_four(widen(v[p], s.n_in - c0 - 256 * p, x_half), s.relu);
+#pragma unroll
+            for (int k = 0; k < kRanks; ++k) {
+                if (k0 + kWaves * k >= s.rank) break;
+#pragma unroll
+                for (int p = 0; p < kPieces; ++p) {
+                    const floatx4 g = widen(w[k][p], s.n_in - c0 - 256 * p, w_half);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) sum[k] = fmaf(g[i], f[p][i], sum[k]);
+                }
             }
         }
 #pragma unroll
         for (int k = 0; k < kRanks; ++k) {
+            if (k0 + kWaves * k >= s.rank) break;
             sum[k] = over_lanes(sum[k], 64, [](float p, float q) { return p + q; });
-            if (lane == k) parts[wave][k] = sum[k];
+            if (lane == 0) low[k0 + kWaves * k] = sum[k];
         }
-        __syncthreads();
-        if (threadIdx.x < kRanks) {
-            float total = parts[0][threadIdx.x];
-#pragma unroll
-            for (int w = 1; w < kFewOutputs / 64; ++w) total += parts[w][threadIdx.x];
-            low[k0 + threadIdx.x] = total;   // (beyond the rank: the last one's again, not used)
-        }
-        __syncthreads();
     }
+    __syncthreads();
     float sum = 0.0f;
     const auto add = [&](const Raw<W> &w, int k) {
         const floatx4 f = widen(w, s.rank - k, w_half);
@@ -300,7 +312,9 @@ __device__ __forceinline__ intx4 fetch_piece(const void *row, int at, int end)
         const intx4 v = *reinterpret_cast<const intx4 *>(static_cast<const char *>(row) + (at < end ? at : 0) * (16 / N));
         return at < end ? v : intx4{0, 0, 0, 0};
     } else {
-        intx4 v;
+        if (at + N <= end) return load_words<intx4, true>(static_cast<const char *>(row) + at * (16 / N));
+        intx4 v = {0, 0, 0, 0};
+        if (at >= end) return v;
         if constexpr (WIDE) {
             const int *p = static_cast<const int *>(row);
 #pragma unroll
@@ -660,11 +674,13 @@ __global__ __launch_bounds__(256) void adapters_up_kernel(AdapterArgs a)
             }
             if (p >= tile.rows) continue;
             if (ALIGNED) {
-                if (j < s.n_out) store_piece(y[u], j, s.y_dtype, o);
+                if (j < s.n_out) store_piece<kYPiece>(y[u], j, s.n_out, s.y_dtype, o);
             } else {
 #pragma unroll
-                for (int e = 0; e < kYPiece; ++e)
-                    if (j + e < s.n_out) store_from_float(y[u], j + e, s.y_dtype, o[e]);
+                for (int e = 0; e < kYPiece; e += 4) {
+                    const float four[4] = {o[e], o[e + 1], o[e + 2], o[e + 3]};
+                    if (j + e < s.n_out) store_piece<-4>(y[u], j + e, s.n_out, s.y_dtype, four);
+                }
             }
         }
         wave_sync();

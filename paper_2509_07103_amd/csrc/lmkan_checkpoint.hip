@@ -1,8 +1,7 @@
 // Activations to 8-bit checkpoints and back.  A block of 32 columns shares a power of two, so that both directions are
 // exact but for the one rounding to a whole number, and a value (7 bits and a sign) is exact in 16-bit types too.
 //
-// Both are bound by memory.  A lane takes pieces of 4 or 8 adjacent elements (16 bytes; one element where rows are not
-// aligned), 8 or 4 lanes a block; a row goes to as many lanes as give each up to four pieces, which are under way together.
+// Both are bound by memory.  A lane takes pieces of 4 or 8 adjacent elements (16 bytes), 8 or 4 lanes a block; a row goes to as many lanes as give each up to four pieces, which are under way together.
 #include "lmkan_rows.h"
 
 namespace lmkan {
@@ -23,9 +22,10 @@ struct RowsArgs {
     void *y;
 };
 
-template <int E, int DTYPE>
+template <int K, int DTYPE>
 __global__ __launch_bounds__(256) void checkpoint_kernel(RowsArgs a)
 {
+    constexpr int E = elements_of(K);
     const int lanes = 1 << a.lanes_log, per_row = exp_blocks(a.cols), pieces = per_row * (kBlock / E);
     const int lane = threadIdx.x & (lanes - 1), rows = 256 >> a.lanes_log;
     for (int64_t row = (int64_t)blockIdx.x * rows + (threadIdx.x >> a.lanes_log); row < a.rows; row += (int64_t)gridDim.x * rows) {
@@ -35,20 +35,18 @@ __global__ __launch_bounds__(256) void checkpoint_kernel(RowsArgs a)
         for (int p0 = lane; p0 < pieces; p0 += kTaken * lanes) {
             float v[kTaken][E];
 #pragma unroll
-            for (int k = 0; k < kTaken; ++k) {
-                const int c = (p0 + k * lanes) * E;
-                load_piece<E, DTYPE>(x, c < a.cols ? c : 0, v[k]);   // (beyond the end: zeros instead)
-            }
+            for (int k = 0; k < kTaken; ++k) load_piece_as<K, DTYPE>(x, (p0 + k * lanes) * E, a.cols, v[k]);
 #pragma unroll
             for (int k = 0; k < kTaken; ++k) {
                 const int c = (p0 + k * lanes) * E;
                 if (p0 + k * lanes >= pieces) break;
+                settle<K>(v[k], c, a.cols);
 #pragma unroll
-                for (int i = 0; i < E; ++i) v[k][i] = c < a.cols ? rectify(v[k][i], a.relu) : 0.0f;
+                for (int i = 0; i < E; ++i) v[k][i] = rectify(v[k][i], a.relu);
                 uint32_t w[(E + 3) / 4];
                 const int byte = encode_piece(v[k], w);
                 if (c < a.cols) {
-                    store_codes_piece<E>(codes + c, w);
+                    store_codes_piece<K>(codes, c, a.cols, w);
                     if (c % kBlock == 0) exps[c / kBlock] = (uint8_t)byte;
                 }
             }
@@ -56,9 +54,10 @@ __global__ __launch_bounds__(256) void checkpoint_kernel(RowsArgs a)
     }
 }
 
-template <int E>
+template <int K>
 __global__ __launch_bounds__(256) void restore_kernel(RowsArgs a)
 {
+    constexpr int E = elements_of(K);
     const int lanes = 1 << a.lanes_log, per_row = exp_blocks(a.cols);
     const int lane = threadIdx.x & (lanes - 1), rows = 256 >> a.lanes_log;
     for (int64_t row = (int64_t)blockIdx.x * rows + (threadIdx.x >> a.lanes_log); row < a.rows; row += (int64_t)gridDim.x * rows) {
@@ -70,9 +69,9 @@ __global__ __launch_bounds__(256) void restore_kernel(RowsArgs a)
             int byte[kTaken];
 #pragma unroll
             for (int k = 0; k < kTaken; ++k) {
-                const int c = c0 + k * lanes * E, from = c < a.cols ? c : c0;
-                load_codes_piece<E>(codes + from, w[k]);
-                byte[k] = exps[from / kBlock];
+                const int c = c0 + k * lanes * E;
+                load_codes_piece<K>(codes, c, a.cols, w[k]);
+                byte[k] = exps[(c < a.cols ? c : 0) / kBlock];
             }
 #pragma unroll
             for (int k = 0; k < kTaken; ++k) {
@@ -80,16 +79,17 @@ __global__ __launch_bounds__(256) void restore_kernel(RowsArgs a)
                 if (c >= a.cols) break;
                 float v[E];
                 values_of<E>(w[k], byte[k], v);
+                settle<K>(v, c, a.cols);
                 if (a.weight || a.bias) {
                     float m[E], b[E];
-                    if (a.weight) load_piece<E, LMKAN_F32>(a.weight, c, m);
-                    if (a.bias) load_piece<E, LMKAN_F32>(a.bias, c, b);
+                    if (a.weight) load_piece_as<K, LMKAN_F32>(a.weight, c, a.cols, m), settle<K>(m, c, a.cols);
+                    if (a.bias) load_piece_as<K, LMKAN_F32>(a.bias, c, a.cols, b), settle<K>(b, c, a.cols);
 #pragma unroll
                     for (int i = 0; i < E; ++i) v[i] = fmaf(a.weight ? m[i] : 1.0f, v[i], a.bias ? b[i] : 0.0f);
                 }
 #pragma unroll
                 for (int i = 0; i < E; ++i) v[i] = rectify(v[i], a.relu);
-                store_piece(y, c, a.dtype, v);
+                store_piece<K>(y, c, a.cols, a.dtype, v);
             }
         }
     }
@@ -109,16 +109,16 @@ unsigned groups(int64_t rows, int log)
     return (unsigned)(n < kMostGroups ? n : kMostGroups);
 }
 
-template <int E>
+template <int K>
 void launch_checkpoint_type(const RowsArgs &a, hipStream_t stream)
 {
     const unsigned n = groups(a.rows, a.lanes_log);
     if (a.dtype == LMKAN_F32) {
-        if constexpr (E < 8) checkpoint_kernel<E, LMKAN_F32><<<n, 256, 0, stream>>>(a);
+        if constexpr (K < 8) checkpoint_kernel<K, LMKAN_F32><<<n, 256, 0, stream>>>(a);
     } else if (a.dtype == LMKAN_F16) {
-        checkpoint_kernel<E, LMKAN_F16><<<n, 256, 0, stream>>>(a);
+        checkpoint_kernel<K, LMKAN_F16><<<n, 256, 0, stream>>>(a);
     } else {
-        checkpoint_kernel<E, LMKAN_BF16><<<n, 256, 0, stream>>>(a);
+        checkpoint_kernel<K, LMKAN_BF16><<<n, 256, 0, stream>>>(a);
     }
 }
 
@@ -128,10 +128,11 @@ void launch_checkpoint(int64_t rows, int cols, int dtype, bool relu, const void 
 {
     RowsArgs a{rows, cols, dtype, relu, 0, x, codes, exps};
     const auto fits = [&](int e) { return pieces_ok(e, cols, x, dtype) && reinterpret_cast<uintptr_t>(codes) % e == 0; };
-    const int e = dtype != LMKAN_F32 && fits(8) ? 8 : fits(4) ? 4 : 1;
-    a.lanes_log = lanes_log(cols, e);
-    if (e == 8) launch_checkpoint_type<8>(a, stream);
-    else if (e == 4) launch_checkpoint_type<4>(a, stream);
+    const int kind = dtype != LMKAN_F32 && fits(8) ? 8 : fits(4) ? 4 : unaligned_kind(cols);
+    a.lanes_log = lanes_log(cols, elements_of(kind));
+    if (kind == 8) launch_checkpoint_type<8>(a, stream);
+    else if (kind == 4) launch_checkpoint_type<4>(a, stream);
+    else if (kind == -4) launch_checkpoint_type<-4>(a, stream);
     else launch_checkpoint_type<1>(a, stream);
 }
 
@@ -142,11 +143,12 @@ void launch_restore(int64_t rows, int cols, int dtype, bool relu, const int8_t *
     const auto fits = [&](int e) {
         return pieces_ok(e, cols, y, dtype) && reinterpret_cast<uintptr_t>(codes) % e == 0 && pieces_ok(4, 4, weight, LMKAN_F32) && pieces_ok(4, 4, bias, LMKAN_F32);
     };
-    const int e = dtype != LMKAN_F32 && fits(8) ? 8 : fits(4) ? 4 : 1;
-    a.lanes_log = lanes_log(cols, e);
+    const int kind = dtype != LMKAN_F32 && fits(8) ? 8 : fits(4) ? 4 : unaligned_kind(cols);
+    a.lanes_log = lanes_log(cols, elements_of(kind));
     const unsigned n = groups(rows, a.lanes_log);
-    if (e == 8) restore_kernel<8><<<n, 256, 0, stream>>>(a);
-    else if (e == 4) restore_kernel<4><<<n, 256, 0, stream>>>(a);
+    if (kind == 8) restore_kernel<8><<<n, 256, 0, stream>>>(a);
+    else if (kind == 4) restore_kernel<4><<<n, 256, 0, stream>>>(a);
+    else if (kind == -4) restore_kernel<-4><<<n, 256, 0, stream>>>(a);
     else restore_kernel<1><<<n, 256, 0, stream>>>(a);
 }
 

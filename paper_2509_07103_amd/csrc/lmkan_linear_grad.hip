@@ -1,7 +1,8 @@
 // Gradients of the linear term's weights and bias from a checkpoint of its input:
 //   grad_weight[j][e] = sum_n g[n][j] f(value[n][e]),  grad_bias[j] = sum_n g[n][j].
-#include "lmkan_rows.h"
+#include <type_traits>
 
+#include "lmkan_rows.h"
 #include "lmkan_tile.h"
 
 namespace lmkan {
@@ -157,8 +158,8 @@ __device__ __forceinline__ uint32_t positive_codes(uint32_t four)
 // Reads of `bytes` of memory: beyond its end, and everywhere where `bytes` is negative, they give zero
 struct Buffer {
     __amdgpu_buffer_rsrc_t rsrc;
-    __device__ __forceinline__ Buffer(const char *base, int bytes)
-        : rsrc(__builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base), 0, bytes > 0 ? bytes : 0, 0x00027000))
+    __device__ __forceinline__ Buffer(const char *p, int bytes)
+        : rsrc(__builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(p), 0, bytes > 0 ? bytes : 0, 0x00027000))
     {
     }
     __device__ __forceinline__ uint32_t word(unsigned at) const { return __builtin_amdgcn_raw_buffer_load_b32(rsrc, at, 0, 0); }
@@ -191,13 +192,17 @@ struct Stages {
     }
 };
 
-// ALIGNED: pairs of outputs and fours of codes lie at multiples of their size
+// How pairs of 16-bit gradients and fours of codes are read: as words (at any address, but then inside the matrix: at its end
+// a word may be there in part), or element by element
+enum Reads { kWords, kElements };
+
+// ALIGNED: pairs of 16-bit outputs and fours of codes lie at multiples of their size
 template <int DTYPE, int WJ, bool ALIGNED>
 __global__ __launch_bounds__(GradTile<WJ>::THREADS, 2) void linear_grad_kernel(GradArgs a)
 {
     typedef GradTile<WJ> T;
     constexpr int P = parts_of<DTYPE>();
-    constexpr int AHEAD = 2;   // steps of 16 rows that are under way
+    constexpr int AHEAD = WJ < 4 ? 4 : 2;   // steps of 16 rows whose gradients are under way   // steps of 16 rows that are under way
     __shared__ __align__(16) char lds[2 * kStageBytes + 2 * kScaleFloats * (int)sizeof(float)];
     const int tiles = a.down * a.across, total = tiles * a.splits;
     const int id = a.first + (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);   // (workgroups on one die: adjacent tiles of the same rows)
@@ -216,14 +221,15 @@ __global__ __launch_bounds__(GradTile<WJ>::THREADS, 2) void linear_grad_kernel(G
     const int j = j0 + wj * kWaveRows + 2 * (lane & 31);
     const int pitch = a.n_out * (int)kSize;
     const unsigned at = (unsigned)(lane >> 5) * 8 * (unsigned)pitch + (unsigned)j * kSize;
-    const auto load_pair = [&](const Stages &rows, int step) {
+    const auto load_pair = [&](auto reads, const Stages &rows, int step) {
+        constexpr Reads kReads = decltype(reads)::value;
         RawPair<DTYPE> r;
         const Buffer b = rows.at(16 * step);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const unsigned to = at + i * (unsigned)pitch;
             if constexpr (DTYPE == LMKAN_F32) r.v[i] = b.two_floats(to);
-            else r.v[i] = ALIGNED ? b.word(to) : b.half(to) | b.half(to + 2) << 16;
+            else r.v[i] = kReads == kWords ? b.word(to) : b.half(to) | b.half(to + 2) << 16;
         }
         return r;
     };
@@ -234,13 +240,14 @@ __global__ __launch_bounds__(GradTile<WJ>::THREADS, 2) void linear_grad_kernel(G
     struct Codes {
         uint32_t v[T::CODED];
     };
-    const auto load_codes = [&](const Stages &rows) {
+    const auto load_codes = [&](auto reads, const Stages &rows) {
+        constexpr Reads kReads = decltype(reads)::value;
         Codes c;
         const Buffer b = rows.at(0);
 #pragma unroll
         for (int i = 0; i < T::CODED; ++i) {
-            const unsigned from = (unsigned)(row0 + i) * (unsigned)a.n_in + (unsigned)e;
-            c.v[i] = ALIGNED ? b.word(from) : b.byte(from) | b.byte(from + 1) << 8 | b.byte(from + 2) << 16 | b.byte(from + 3) << 24;
+            const unsigned f = (unsigned)(row0 + i) * (unsigned)a.n_in + (unsigned)e;
+            c.v[i] = kReads == kWords ? b.word(f) : b.byte(f) | b.byte(f + 1) << 8 | b.byte(f + 2) << 16 | b.byte(f + 3) << 24;
         }
         return c;
     };
@@ -290,29 +297,33 @@ __global__ __launch_bounds__(GradTile<WJ>::THREADS, 2) void linear_grad_kernel(G
         for (int k = 0; k < T::TE; ++k) acc[t][k] = floatx16{};
     const bool with_bias = a.grad_bias && tj == 0 && we == 0;
     double bias[2] = {};
-    if (from < to) {
-        // (stages beyond the last are read too, as zeros beyond the last row, and not used)
+    const auto run = [&](int from, int to) {
+        if (from >= to) return;
+        const auto reads = std::integral_constant<Reads, kWords>();
+        // (powers of two are read two stages ahead, as zeros beyond the last row; what else would be beyond the last stage is that
+        // stage again, and not used)
         Stages rows(a.grad_y, a.batch, pitch, from), codes(a.codes, a.batch, a.n_in, from), exps(a.exps, a.batch, per_row, from);
         RawPair<DTYPE> raw[AHEAD];
 #pragma unroll
-        for (int k = 0; k < AHEAD; ++k) raw[k] = load_pair(rows, k);
-        const Codes first = rectified(load_codes(codes));
+        for (int k = 0; k < AHEAD; ++k) raw[k] = load_pair(reads, rows, k);
+        const Codes first = rectified(load_codes(reads, codes));
         store_scale(load_exp(exps), scales);
         exps.next();
         store_scale(load_exp(exps), scales + kScaleFloats);
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < 4; ++k) store_column(first, k, scales, lds);
-        codes.next();
-        Codes c = load_codes(codes);
+        if (from + 1 < to) codes.next();
+        Codes c = load_codes(reads, codes);
         __syncthreads();
         for (int s = from; s < to; ++s) {
             const int now = s - from & 1;
             const char *buffer = lds + now * kStageBytes;
-            codes.next(), exps.next();
+            exps.next();
+            if (s + 2 < to) codes.next();
             Stages ahead = rows;
-            ahead.next();
-            const Codes later = load_codes(codes);
+            if (s + 1 < to) ahead.next();
+            const Codes later = load_codes(reads, codes);
             c = rectified(c);
             const uint32_t byte = load_exp(exps);
             bf16x8 v[T::TE];
@@ -323,9 +334,8 @@ __global__ __launch_bounds__(GradTile<WJ>::THREADS, 2) void linear_grad_kernel(G
                 to_parts(raw[step % AHEAD], g);
                 if (with_bias)
 #pragma unroll
-                    for (int t = 0; t < 2; ++t)
-                        bias[t] += (double)sum_of(raw[step % AHEAD], t);
-                raw[step % AHEAD] = load_pair(step + AHEAD < 4 ? rows : ahead, (step + AHEAD) & 3);
+                    for (int t = 0; t < 2; ++t) bias[t] += (double)sum_of(raw[step % AHEAD], t);
+                raw[step % AHEAD] = load_pair(reads, step + AHEAD < 4 ? rows : ahead, (step + AHEAD) & 3);
                 store_column(c, step, scales + (now ^ 1) * kScaleFloats, lds + (now ^ 1) * kStageBytes);
                 bf16x8 then[T::TE];
                 if (step < 3) load_fragments(buffer, step + 1, then);
@@ -344,6 +354,48 @@ __global__ __launch_bounds__(GradTile<WJ>::THREADS, 2) void linear_grad_kernel(G
             store_scale(byte, scales + now * kScaleFloats);
             __syncthreads();
         }
+    };
+    // the last stages, one thing after the other
+    const auto run_elements = [&](int from, int to) {
+        const auto reads = std::integral_constant<Reads, kElements>();
+        for (int s = from; s < to; ++s) {
+            const Stages rows(a.grad_y, a.batch, pitch, s);
+            store_scale(load_exp(Stages(a.exps, a.batch, per_row, s)), scales);
+            __syncthreads();
+            const Codes c = rectified(load_codes(reads, Stages(a.codes, a.batch, a.n_in, s)));
+#pragma unroll
+            for (int k = 0; k < 4; ++k) store_column(c, k, scales, lds);
+            __syncthreads();
+#pragma unroll 1
+            for (int step = 0; step < 4; ++step) {
+                const RawPair<DTYPE> raw = load_pair(reads, rows, step);
+                bf16x8 g[2][P], v[T::TE];
+                to_parts(raw, g);
+                if (with_bias)
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) bias[t] += (double)sum_of(raw, t);
+                load_fragments(lds, step, v);
+#pragma unroll
+                for (int p = P - 1; p >= 0; --p)
+#pragma unroll
+                    for (int k = 0; k < T::TE; ++k)
+#pragma unroll
+                        for (int t = 0; t < 2; ++t) acc[t][k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[k], g[t][p], acc[t][k], 0, 0, 0);
+            }
+            __syncthreads();
+        }
+    };
+    if constexpr (ALIGNED) {
+        run(from, to);
+    } else {
+        // stages whose reads of whole tiles stay inside both matrices
+        const auto inside = [&](int bytes, int past) {
+            const int64_t rows = a.batch - (past + bytes - 1) / bytes;
+            return rows > 0 ? (int)(rows / kDepth) : 0;
+        };
+        const int both = min(inside(pitch, 2 * T::ROWS + 4), inside(a.n_in, kCols + 4)), middle = both < from ? from : both < to ? both : to;
+        run(from, middle);
+        run_elements(middle, to);
     }
     if (with_bias)
 #pragma unroll
@@ -406,8 +458,8 @@ struct Plan {
 };
 
 // Tile and splits by what a call takes in us: stages of a workgroup, fitted to 18 shapes (8192 rows of 1024 -> 1024, float32:
-// 3.7 a stage of 256 outputs alone on a compute unit and 6.5 two at a time, 2.0 of 128 outputs; bfloat16 1.5), parts written
-// and joined at 8.5 TB/s (64 MiB 11 us a launch, 16 MiB 5).  Measured (us, best / next other tile / next other number of
+// 3.7 a stage of 256 outputs alone on a compute unit and 6.5 two at a time, 2.2 of 128 outputs; bfloat16 1.5; one and a half to
+// begin with), parts written and joined at 8 TB/s.  Measured (us, best / next other tile / next other number of
 // splits): 8192 of 1024 -> 1024 float32 64 / 67 / 65; 5000 of 500 -> 333 29 / 35 / 32; 65536 of 128 -> 128 32 / 33 / 40;
 // 4096 of 4096 -> 4096 bfloat16 139 / 203 / 174.
 Plan plan_of(const LinearShape &s, bool whole)
@@ -416,15 +468,15 @@ Plan plan_of(const LinearShape &s, bool whole)
     double least = 1e300;
     const int stages = (int)((s.batch + kDepth - 1) / kDepth);
     const int parts = s.y_dtype == LMKAN_F32 ? 3 : s.y_dtype == LMKAN_F16 ? 2 : 1;
-    for (int wj = whole ? 4 : 2; wj >= 1; wj /= 2) {
+    for (int wj = 4; wj >= 1; wj /= 2) {
         const int down = (s.n_out + kWaveRows * wj - 1) / (kWaveRows * wj), across = (s.n_in + kCols - 1) / kCols;
         const int64_t tiles = (int64_t)down * across;
-        const double stage = wj == 4 ? 0.4 + 1.1 * parts : wj == 2 ? 0.5 + 0.5 * parts : 0.6 + 0.45 * parts;
+        const double stage = wj == 4 ? 0.4 + 1.1 * parts : wj == 2 ? 0.5 + 0.55 * parts : 0.6 + 0.45 * parts;
         for (int splits = 1; splits <= 512 && splits <= (stages > 0 ? stages : 1); splits *= 2) {
             if (splits > 1 && tiles * splits > 4 * kUnits) break;
             const int64_t turns = (tiles * splits + kUnits - 1) / kUnits;
             const double bytes = (double)tiles * splits * wj * kWaveRows * kCols * sizeof(float);
-            const double cost = ((turns / 2) * 1.75 + turns % 2) * ((stages + splits - 1) / splits + 1) * stage + (splits > 1 ? 3.0 + bytes / 8e6 : 0.0);
+            const double cost = ((turns / 2) * 1.75 + turns % 2) * ((stages + splits - 1) / splits + 1.5) * stage + (splits > 1 ? 3.0 + bytes / 8e6 : 0.0);
             if (cost < least) least = cost, best = {wj, down, across, splits, stages};
         }
     }
@@ -440,7 +492,8 @@ size_t plan_bytes(const LinearShape &s, const Plan &p)
     return p.splits > 1 ? parts_bytes(p) + align256((size_t)p.splits * s.n_out * sizeof(double)) : 0;
 }
 
-bool whole_shape(const LinearShape &s) { return s.n_out % 2 == 0 && s.n_in % 4 == 0; }
+// (two float32 need no more than their own alignment)
+bool whole_shape(const LinearShape &s) { return (s.y_dtype == LMKAN_F32 || s.n_out % 2 == 0) && s.n_in % 4 == 0; }
 
 template <int DTYPE, int WJ>
 void launch(GradArgs a, bool whole, hipStream_t stream)
@@ -450,7 +503,7 @@ void launch(GradArgs a, bool whole, hipStream_t stream)
         const unsigned groups = (unsigned)((total - first < kMostGroups ? total - first : kMostGroups) + 7) / 8 * 8;
         a.first = (int)first;
         if (whole) linear_grad_kernel<DTYPE, WJ, true><<<groups, GradTile<WJ>::THREADS, 0, stream>>>(a);
-        else if constexpr (WJ < 4) linear_grad_kernel<DTYPE, WJ, false><<<groups, GradTile<WJ>::THREADS, 0, stream>>>(a);
+        else linear_grad_kernel<DTYPE, WJ, false><<<groups, GradTile<WJ>::THREADS, 0, stream>>>(a);
     }
     if (!a.parts) return;
     // (a group of the join for every four results of the tiles, which are at least as many as the outputs)
@@ -479,7 +532,7 @@ size_t linear_grad_workspace_bytes(const LinearShape &s)
 void launch_linear_grad(const LinearShape &s, bool accumulate, const int8_t *codes, const uint8_t *exps, const void *grad_y,
                         float *grad_weight, float *grad_bias, void *workspace, hipStream_t stream)
 {
-    const bool whole = whole_shape(s) && aligned_to(grad_y, s.y_dtype == LMKAN_F32 ? 8 : 4) && aligned_to(codes, 4);
+    const bool whole = whole_shape(s) && aligned_to(grad_y, 4) && aligned_to(codes, 4);
     const Plan p = plan_of(s, whole);
     GradArgs a{s.batch, s.n_in, s.n_out, s.relu, accumulate, codes, exps, grad_y, grad_weight, grad_bias, p.down, p.across, 0, p.splits, p.stages,
                p.stages / p.splits, p.stages % p.splits, nullptr, nullptr, s.n_in % 4 == 0 && aligned_to(grad_weight, 16)};

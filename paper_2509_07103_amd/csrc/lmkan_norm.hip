@@ -15,10 +15,10 @@ struct Plus {
     __device__ __forceinline__ V operator()(V a, V b) const { return a + b; }
 };
 
-// How a row lies over lanes: `lanes` of them (a power of two), or a workgroup of THREADS when GROUP
-template <int E, int H, int THREADS, bool GROUP>
+// How a row lies over lanes: `lanes` of them (a power of two), or a workgroup of THREADS when GROUP; H pieces of kind K a lane
+template <int K, int H, int THREADS, bool GROUP>
 struct Spread {
-    static constexpr int kWaves = THREADS / 64;
+    static constexpr int kWaves = THREADS / 64, E = elements_of(K);
     int lanes, lane, row, rows;   // rows: of the workgroup at a time
     __device__ __forceinline__ explicit Spread(int lanes_log)
     {
@@ -57,36 +57,54 @@ struct Spread {
             for (int w = 1; w < kWaves; ++w) a += shared[2 * w], b += shared[2 * w + 1];
         }
     }
-};
-
-template <int E, int H, int DTYPE>
-__device__ __forceinline__ void load_row_as(const void *p, int64_t first, int lanes, int lane, int cols, float (&v)[H][E])
-{
-    p = row_at(p, first, DTYPE);
+    // A lane's pieces of a row, as they lie in memory
+    __device__ __forceinline__ void load(const void *p, int64_t first, int dtype, int cols, uint32_t (&w)[H][E]) const
+    {
+        p = row_at(p, first, dtype);
+        if (dtype == LMKAN_F32) {
 #pragma unroll
-    for (int h = 0; h < H; ++h) {
-        const int c = (h * lanes + lane) * E;
-        load_piece<E, DTYPE>(p, c < cols ? c : 0, v[h]);
+            for (int h = 0; h < H; ++h) load_raw<K, true>(p, column(h), cols, w[h]);
+        } else {
+#pragma unroll
+            for (int h = 0; h < H; ++h) load_raw<K, false>(p, column(h), cols, w[h]);
+        }
     }
-}
-// A lane's pieces of a row that begins at `first`; what lies beyond the end is anything that the row holds
-template <int E, int H>
-__device__ __forceinline__ void load_row(const void *p, int64_t first, int dtype, int lanes, int lane, int cols, float (&v)[H][E])
-{
-    if (dtype == LMKAN_F32) load_row_as<E, H, LMKAN_F32>(p, first, lanes, lane, cols, v);
-    else if (dtype == LMKAN_F16) load_row_as<E, H, LMKAN_F16>(p, first, lanes, lane, cols, v);
-    else load_row_as<E, H, LMKAN_BF16>(p, first, lanes, lane, cols, v);
-}
-// columns' weights or the like: `other` where there are none, zero beyond the end
-template <int E, int H>
-__device__ __forceinline__ void load_columns(const float *p, float other, int lanes, int lane, int cols, float (&v)[H][E])
-{
-    if (p) load_row_as<E, H, LMKAN_F32>(p, 0, lanes, lane, cols, v);
+    // ... and as float32, in place
+    __device__ __forceinline__ void take(const uint32_t (&w)[H][E], int dtype, int cols, float (&v)[H][E]) const
+    {
+        if (dtype == LMKAN_F32) {
 #pragma unroll
-    for (int h = 0; h < H; ++h)
+            for (int h = 0; h < H; ++h) convert<LMKAN_F32>(w[h], v[h]);
+        } else if (dtype == LMKAN_F16) {
 #pragma unroll
-        for (int i = 0; i < E; ++i) v[h][i] = (h * lanes + lane) * E < cols ? (p ? v[h][i] : other) : 0.0f;
-}
+            for (int h = 0; h < H; ++h) convert<LMKAN_F16>(w[h], v[h]);
+        } else {
+#pragma unroll
+            for (int h = 0; h < H; ++h) convert<LMKAN_BF16>(w[h], v[h]);
+        }
+        place(v, cols);
+    }
+    // (pieces that are aligned exist or do not: who takes them asks)
+    __device__ __forceinline__ void place(float (&v)[H][E], int cols) const
+    {
+        if constexpr (K < 0)
+#pragma unroll
+            for (int h = 0; h < H; ++h) settle<K>(v[h], column(h), cols);
+    }
+    // columns' weights or the like: `other` where there are none, zero beyond the end
+    __device__ __forceinline__ void load_columns(const float *p, float other, int cols, float (&v)[H][E]) const
+    {
+        if (p)
+#pragma unroll
+            for (int h = 0; h < H; ++h) load_piece_as<K, LMKAN_F32>(p, column(h), cols, v[h]);
+#pragma unroll
+        for (int h = 0; h < H; ++h) {
+            if (K < 0) settle<K>(v[h], column(h), cols);
+#pragma unroll
+            for (int i = 0; i < E; ++i) v[h][i] = exists<K>(column(h), i, cols) ? (p ? v[h][i] : other) : 0.0f;
+        }
+    }
+};
 
 struct NormArgs {
     int64_t rows;
@@ -103,18 +121,21 @@ struct NormArgs {
 // (x - mean) rstd: two roundings, as the checkpoint's definition has it
 __device__ __forceinline__ float normal(float x, float mean, float rstd) { return __fmul_rn(__fsub_rn(x, mean), rstd); }
 
-template <int E, int H, int THREADS, bool GROUP>
+template <int K, int H, int THREADS, bool GROUP>
 __global__ __launch_bounds__(THREADS) void norm_kernel(NormArgs a)
 {
+    constexpr int E = elements_of(K);
     __shared__ double sums[THREADS / 64];
-    const Spread<E, H, THREADS, GROUP> s(a.lanes_log);
+    const Spread<K, H, THREADS, GROUP> s(a.lanes_log);
     float w[H][E], b[H][E];
-    load_columns(a.weight, 1.0f, s.lanes, s.lane, a.cols, w);
-    load_columns(a.bias, 0.0f, s.lanes, s.lane, a.cols, b);
+    s.load_columns(a.weight, 1.0f, a.cols, w);
+    s.load_columns(a.bias, 0.0f, a.cols, b);
     for (int64_t row = (int64_t)blockIdx.x * s.rows + s.row; row < a.rows; row += (int64_t)gridDim.x * s.rows) {
         const int64_t first = row * a.cols;
+        uint32_t raw[H][E];
+        s.load(a.x, first, a.x_dtype, a.cols, raw);
         float x[H][E];
-        load_row(a.x, first, a.x_dtype, s.lanes, s.lane, a.cols, x);
+        s.take(raw, a.x_dtype, a.cols, x);
         double sum = 0.0;
 #pragma unroll
         for (int h = 0; h < H; ++h) {
@@ -130,7 +151,8 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(NormArgs a)
             double part = 0.0;
 #pragma unroll
             for (int i = 0; i < E; ++i) {
-                const double d = (double)x[h][i] - centre;
+                double d = (double)x[h][i] - centre;
+                if (K < 0 && i > 0) d = exists<K>(s.column(h), i, a.cols) ? d : 0.0;
                 part = fma(d, d, part);
             }
             sum += s.column(h) < a.cols ? part : 0.0;
@@ -145,30 +167,31 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(NormArgs a)
             const int c = s.column(h);
             float hat[E];
 #pragma unroll
-            for (int i = 0; i < E; ++i) hat[i] = c < a.cols ? normal(x[h][i], mean, rstd) : 0.0f;
+            for (int i = 0; i < E; ++i) hat[i] = exists<K>(c, i, a.cols) ? normal(x[h][i], mean, rstd) : 0.0f;
             if (a.codes) {
                 uint32_t coded[(E + 3) / 4];
                 const int byte = encode_piece(hat, coded);
                 if (c < a.cols) {
-                    store_codes_piece<E>(codes + c, coded);
+                    store_codes_piece<K>(codes, c, a.cols, coded);
                     if (c % kBlock == 0) exps[c / kBlock] = (uint8_t)byte;
                 }
             }
             if (c < a.cols) {
 #pragma unroll
                 for (int i = 0; i < E; ++i) hat[i] = fmaf(w[h][i], hat[i], b[h][i]);
-                store_piece(y, c, a.y_dtype, hat);
+                store_piece<K>(y, c, a.cols, a.y_dtype, hat);
             }
         }
     }
 }
 
 // Rows that registers do not hold are read three times (from the L2 or the last cache after the first)
-template <int E>
+template <int K>
 __global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs a)
 {
+    constexpr int E = elements_of(K);
     __shared__ double sums[16];
-    const Spread<E, 1, 1024, true> s(0);
+    const Spread<K, 1, 1024, true> s(0);
     const int lane = threadIdx.x * E;
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const void *const x = row_at(a.x, row * a.cols, a.x_dtype);
@@ -177,7 +200,8 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs a)
 #pragma unroll 4
         for (int c = lane; c < a.cols; c += 1024 * E) {
             float v[E];
-            load_piece(x, c, a.x_dtype, v);
+            load_piece<K>(x, c, a.cols, a.x_dtype, v);
+            settle<K>(v, c, a.cols);
 #pragma unroll
             for (int i = 0; i < E; ++i) sum += (double)v[i];
         }
@@ -186,10 +210,11 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs a)
 #pragma unroll 4
         for (int c = lane; c < a.cols; c += 1024 * E) {
             float v[E];
-            load_piece(x, c, a.x_dtype, v);
+            load_piece<K>(x, c, a.cols, a.x_dtype, v);
+            settle<K>(v, c, a.cols);
 #pragma unroll
             for (int i = 0; i < E; ++i) {
-                const double d = (double)v[i] - centre;
+                const double d = exists<K>(c, i, a.cols) ? (double)v[i] - centre : 0.0;
                 sum = fma(d, d, sum);
             }
         }
@@ -198,21 +223,25 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs a)
         for (int c0 = 0; c0 < a.cols; c0 += 1024 * E) {
             const int c = c0 + lane;
             float hat[E];
-            load_piece(x, c < a.cols ? c : 0, a.x_dtype, hat);
+            load_piece<K>(x, c, a.cols, a.x_dtype, hat);
+            settle<K>(hat, c, a.cols);
 #pragma unroll
-            for (int i = 0; i < E; ++i) hat[i] = c < a.cols ? normal(hat[i], mean, rstd) : 0.0f;
+            for (int i = 0; i < E; ++i) hat[i] = exists<K>(c, i, a.cols) ? normal(hat[i], mean, rstd) : 0.0f;
             if (a.codes) {
                 uint32_t coded[(E + 3) / 4];
                 const int byte = encode_piece(hat, coded);
                 if (c < a.cols) {
-                    store_codes_piece<E>(a.codes + row * a.cols + c, coded);
+                    store_codes_piece<K>(a.codes + row * a.cols, c, a.cols, coded);
                     if (c % kBlock == 0) a.exps[row * exp_blocks(a.cols) + c / kBlock] = (uint8_t)byte;
                 }
             }
             if (c < a.cols) {
 #pragma unroll
-                for (int i = 0; i < E; ++i) hat[i] = fmaf(a.weight ? a.weight[c + i] : 1.0f, hat[i], a.bias ? a.bias[c + i] : 0.0f);
-                store_piece(y, c, a.y_dtype, hat);
+                for (int i = 0; i < E; ++i) {
+                    const int at = c + i < a.cols ? c + i : c;
+                    hat[i] = fmaf(a.weight ? a.weight[at] : 1.0f, hat[i], a.bias ? a.bias[at] : 0.0f);
+                }
+                store_piece<K>(y, c, a.cols, a.y_dtype, hat);
             }
         }
     }
@@ -227,44 +256,52 @@ struct GradArgs {
     float *parts;   // [workgroups][2][cols], or null: no gradients of weight and bias
 };
 
-template <int E, int H, int THREADS, bool GROUP>
+template <int K, int H, int THREADS, bool GROUP>
 __global__ __launch_bounds__(THREADS) void norm_grad_kernel(GradArgs g)
 {
+    constexpr int E = elements_of(K);
     const NormBackwardArgs &a = g.a;
     const int cols = g.s.cols;
     __shared__ float sums[2 * (THREADS / 64)];
     __shared__ float joined[GROUP ? 1 : THREADS * E];
-    const Spread<E, H, THREADS, GROUP> s(g.lanes_log);
+    const Spread<K, H, THREADS, GROUP> s(g.lanes_log);
+    const float part = 1.0f / (float)cols;
     float w[H][E], gw[H][E], gb[H][E];
-    load_columns(a.weight, 1.0f, s.lanes, s.lane, cols, w);
+    s.load_columns(a.weight, 1.0f, cols, w);
 #pragma unroll
     for (int h = 0; h < H; ++h)
 #pragma unroll
         for (int i = 0; i < E; ++i) gw[h][i] = gb[h][i] = 0.0f;
     for (int64_t row = (int64_t)blockIdx.x * s.rows + s.row; row < g.s.rows; row += (int64_t)gridDim.x * s.rows) {
         const int64_t first = row * cols;
-        float d[H][E], hat[H][E];
-        load_row(a.grad_y, first, g.s.y_dtype, s.lanes, s.lane, cols, d);
+        // (all loads of the row are under way before the first is used)
+        uint32_t raw_d[H][E], raw_x[H][E], coded[H][(E + 3) / 4];
+        int byte[H];
+        s.load(a.grad_y, first, g.s.y_dtype, cols, raw_d);
         const float mean = a.stats[2 * row], rstd = a.stats[2 * row + 1];
         if (a.x) {
-            load_row(a.x, first, g.s.x_dtype, s.lanes, s.lane, cols, hat);
+            s.load(a.x, first, g.s.x_dtype, cols, raw_x);
+        } else {
+            const int8_t *codes = a.codes + first;
+            const uint8_t *exps = a.exps + row * exp_blocks(cols);
+#pragma unroll
+            for (int h = 0; h < H; ++h) {
+                load_codes_piece<K>(codes, s.column(h), cols, coded[h]);
+                byte[h] = exps[(s.column(h) < cols ? s.column(h) : 0) / kBlock];
+            }
+        }
+        float d[H][E], hat[H][E];
+        s.take(raw_d, g.s.y_dtype, cols, d);
+        if (a.x) {
+            s.take(raw_x, g.s.x_dtype, cols, hat);
 #pragma unroll
             for (int h = 0; h < H; ++h)
 #pragma unroll
                 for (int i = 0; i < E; ++i) hat[h][i] = (hat[h][i] - mean) * rstd;
         } else {
-            const int8_t *codes = a.codes + first;
-            const uint8_t *exps = a.exps + row * exp_blocks(cols);
-            uint32_t coded[H][(E + 3) / 4];
-            int byte[H];
-#pragma unroll
-            for (int h = 0; h < H; ++h) {
-                const int c = s.column(h) < cols ? s.column(h) : 0;
-                load_codes_piece<E>(codes + c, coded[h]);
-                byte[h] = exps[c / kBlock];
-            }
 #pragma unroll
             for (int h = 0; h < H; ++h) values_of<E>(coded[h], byte[h], hat[h]);
+            s.place(hat, cols);
         }
         float of_d = 0.0f, of_dh = 0.0f;
 #pragma unroll
@@ -282,7 +319,7 @@ __global__ __launch_bounds__(THREADS) void norm_grad_kernel(GradArgs g)
         }
         if (a.grad_x) {
             s.two_sums(of_d, of_dh, sums);
-            of_d /= cols, of_dh /= cols;
+            of_d *= part, of_dh *= part;
             void *const grad_x = row_at(a.grad_x, first, g.s.x_dtype);
 #pragma unroll
             for (int h = 0; h < H; ++h) {
@@ -290,7 +327,7 @@ __global__ __launch_bounds__(THREADS) void norm_grad_kernel(GradArgs g)
                 if (c < cols) {
 #pragma unroll
                     for (int i = 0; i < E; ++i) d[h][i] = rstd * (d[h][i] - of_d - hat[h][i] * of_dh);
-                    store_piece(grad_x, c, g.s.x_dtype, d[h]);
+                    store_piece<K>(grad_x, c, cols, g.s.x_dtype, d[h]);
                 }
             }
         }
@@ -316,42 +353,46 @@ __global__ __launch_bounds__(THREADS) void norm_grad_kernel(GradArgs g)
             }
             if (s.row == 0 && c < cols)
 #pragma unroll
-                for (int i = 0; i < E; ++i) to[which * cols + c + i] = v[i];
+                for (int i = 0; i < E; ++i)
+                    if (exists<K>(c, i, cols)) to[which * cols + c + i] = v[i];
         }
     }
 }
 
-template <int E>
+template <int K, int E>
 __device__ __forceinline__ void load_hat(const NormShape &s, const NormBackwardArgs &a, int64_t row, int c, float (&hat)[E])
 {
     if (a.x) {
         const float mean = a.stats[2 * row], rstd = a.stats[2 * row + 1];
-        load_piece(row_at(a.x, row * s.cols, s.x_dtype), c, s.x_dtype, hat);
+        load_piece<K>(row_at(a.x, row * s.cols, s.x_dtype), c, s.cols, s.x_dtype, hat);
 #pragma unroll
         for (int i = 0; i < E; ++i) hat[i] = (hat[i] - mean) * rstd;
     } else {
         uint32_t coded[(E + 3) / 4];
-        load_codes_piece<E>(a.codes + row * s.cols + c, coded);
+        load_codes_piece<K>(a.codes + row * s.cols, c, s.cols, coded);
         values_of<E>(coded, a.exps[row * exp_blocks(s.cols) + c / kBlock], hat);
     }
+    settle<K>(hat, c, s.cols);
 }
 
 // Rows that registers do not hold: the rows' gradients, read twice ..
-template <int E>
+template <int K>
 __global__ __launch_bounds__(1024) void norm_long_grad_x_kernel(NormShape s, NormBackwardArgs a)
 {
+    constexpr int E = elements_of(K);
     __shared__ float sums[32];
-    const Spread<E, 1, 1024, true> spread(0);
+    const Spread<K, 1, 1024, true> spread(0);
     for (int64_t row = blockIdx.x; row < s.rows; row += gridDim.x) {
         const float rstd = a.stats[2 * row + 1];
         const void *const gy = row_at(a.grad_y, row * s.cols, s.y_dtype);
         void *const gx = row_at(a.grad_x, row * s.cols, s.x_dtype);
         const auto load = [&](int c, float (&d)[E], float (&hat)[E]) {
-            load_piece(gy, c, s.y_dtype, d);
-            load_hat(s, a, row, c, hat);
+            load_piece<K>(gy, c, s.cols, s.y_dtype, d);
+            settle<K>(d, c, s.cols);
+            load_hat<K>(s, a, row, c, hat);
             if (a.weight)
 #pragma unroll
-                for (int i = 0; i < E; ++i) d[i] *= a.weight[c + i];
+                for (int i = 0; i < E; ++i) d[i] *= a.weight[c + i < s.cols ? c + i : c];
         };
         float of_d = 0.0f, of_dh = 0.0f;
         for (int c = threadIdx.x * E; c < s.cols; c += 1024 * E) {
@@ -367,28 +408,31 @@ __global__ __launch_bounds__(1024) void norm_long_grad_x_kernel(NormShape s, Nor
             load(c, d, hat);
 #pragma unroll
             for (int i = 0; i < E; ++i) d[i] = rstd * (d[i] - of_d - hat[i] * of_dh);
-            store_piece(gx, c, s.x_dtype, d);
+            store_piece<K>(gx, c, s.cols, s.x_dtype, d);
         }
     }
 }
 
 // .. and the columns' sums, a piece of columns a thread
-template <int E>
+template <int K>
 __global__ __launch_bounds__(256) void norm_long_columns_kernel(NormShape s, NormBackwardArgs a, float *parts)
 {
+    constexpr int E = elements_of(K);
     const int c = (blockIdx.x * 256 + threadIdx.x) * E;
     if (c >= s.cols) return;
     float w[E] = {}, b[E] = {};
     for (int64_t row = blockIdx.y; row < s.rows; row += gridDim.y) {
         float g[E], hat[E];
-        load_piece(row_at(a.grad_y, row * s.cols, s.y_dtype), c, s.y_dtype, g);
-        load_hat(s, a, row, c, hat);
+        load_piece<K>(row_at(a.grad_y, row * s.cols, s.y_dtype), c, s.cols, s.y_dtype, g);
+        settle<K>(g, c, s.cols);
+        load_hat<K>(s, a, row, c, hat);
 #pragma unroll
         for (int i = 0; i < E; ++i) b[i] += g[i], w[i] = fmaf(g[i], hat[i], w[i]);
     }
     float *const to = parts + (int64_t)blockIdx.y * 2 * s.cols;
 #pragma unroll
-    for (int i = 0; i < E; ++i) to[c + i] = w[i], to[s.cols + c + i] = b[i];
+    for (int i = 0; i < E; ++i)
+        if (c + i < s.cols) to[c + i] = w[i], to[s.cols + c + i] = b[i];
 }
 
 // The parts' sums: 32 columns a workgroup, every 32nd part a thread
@@ -401,7 +445,7 @@ __global__ __launch_bounds__(1024) void norm_join_kernel(NormShape s, NormBackwa
     if (!to) return;
     double sum = 0.0;
     if (c < s.cols)
-#pragma unroll 8
+#pragma unroll 16
         for (int p = slice; p < parts; p += 32) sum += (double)from[((int64_t)p * 2 + blockIdx.y) * s.cols + c];
     sums[slice][col] = sum;
     __syncthreads();
@@ -412,55 +456,53 @@ __global__ __launch_bounds__(1024) void norm_join_kernel(NormShape s, NormBackwa
 
 // ---- host ------------------------------------------------------------------------------------------------------------
 
-// Elements of a row that a lane holds (8 where they lie one by one), and a workgroup of 512; workgroups of 1024 would leave
-// 128 registers a lane, which spill.
-constexpr int lane_holds(int e) { return e == 1 ? 8 : 16; }
-constexpr int most_held(int e) { return 512 * lane_holds(e); }
+// Elements of a row that a lane holds, and a workgroup of 512; workgroups of 1024 would leave 128 registers a lane, which spill
+constexpr int kLaneHolds = 16, kMostHeld = 512 * kLaneHolds;
 constexpr int kUnits = 256;                       // compute units
 
-// How a row of `cols` columns is spread: pieces of e elements; its lanes, or the threads of a workgroup
+// How a row of `cols` columns is spread: pieces of a kind; its lanes, or the threads of a workgroup
 struct Plan {
-    int e, held, lanes_log, threads;   // threads: 0, lanes of a wave
+    int kind, held, lanes_log, threads;   // threads: 0, lanes of a wave
 };
 
-Plan plan_of(int cols, int e)
+Plan plan_of(int cols, int kind)
 {
-    Plan p = {e, 1, e == 1 ? 5 : e == 4 ? 3 : 2, 0};
-    while (p.lanes_log < 6 && cols > lane_holds(e) << p.lanes_log) ++p.lanes_log;
+    const int e = elements_of(kind);
+    Plan p = {kind, 1, e == 1 ? 5 : e == 4 ? 3 : 2, 0};
+    while (p.lanes_log < 6 && cols > kLaneHolds << p.lanes_log) ++p.lanes_log;
     int lanes = 1 << p.lanes_log;
-    if (cols > lane_holds(e) * 64) {
-        p.threads = 256;
-        while (cols > lane_holds(e) * p.threads) p.threads *= 2;
+    if (cols > kLaneHolds * 64) {
+        p.threads = cols > kLaneHolds * 256 ? 512 : 256;
         lanes = p.threads;
     }
     while (p.held * e * lanes < cols) p.held *= 2;
     return p;
 }
 
-// calls f with E, H, THREADS and GROUP as constants
-template <int E, int H, int THREADS, bool GROUP>
+// calls f with K, H, THREADS and GROUP as constants
+template <int K, int H, int THREADS, bool GROUP>
 struct Sizes {
-    static constexpr int e = E, h = H, threads = THREADS;
+    static constexpr int k = K, h = H, threads = THREADS;
     static constexpr bool group = GROUP;
 };
-template <int E, class F>
+template <int K, class F>
 void with_held(const Plan &p, F &&f)
 {
-    constexpr int kMost = lane_holds(E) / E;
-    if (p.threads == 512) f(Sizes<E, kMost, 512, true>());
-    else if (p.threads == 256 && p.held == kMost) f(Sizes<E, kMost, 256, true>());
-    else if (p.threads == 256) f(Sizes<E, kMost / 2, 256, true>());
-    else if (p.held == kMost) f(Sizes<E, kMost, 256, false>());
-    else if (p.held == kMost / 2) f(Sizes<E, kMost / 2, 256, false>());
-    else if constexpr (E == 4) f(Sizes<E, 1, 256, false>());
-    else if constexpr (E == 1) f(Sizes<E, 2, 256, false>());
+    constexpr int kMost = kLaneHolds / elements_of(K);
+    if (p.threads == 512) f(Sizes<K, kMost, 512, true>());
+    else if (p.threads == 256 && p.held == kMost) f(Sizes<K, kMost, 256, true>());
+    else if (p.threads == 256) f(Sizes<K, kMost / 2, 256, true>());
+    else if (p.held == kMost) f(Sizes<K, kMost, 256, false>());
+    else if (p.held == kMost / 2) f(Sizes<K, kMost / 2, 256, false>());
+    else if constexpr (kMost == 4) f(Sizes<K, 1, 256, false>());
 }
 template <class F>
 void with_sizes(const Plan &p, F &&f)
 {
-    if (p.e == 8) with_held<8>(p, f);
-    else if (p.e == 4) with_held<4>(p, f);
-    else with_held<1>(p, f);
+    if (p.kind == 8) with_held<8>(p, f);
+    else if (p.kind == 4) with_held<4>(p, f);
+    else if (p.kind == -4) with_held<-4>(p, f);
+    else f(Sizes<1, 1, 256, false>());   // (fewer than four columns)
 }
 
 unsigned groups_of(const Plan &p, int64_t rows, int most)
@@ -469,17 +511,17 @@ unsigned groups_of(const Plan &p, int64_t rows, int most)
     return (unsigned)(n < most ? n : most);
 }
 
-int piece_of(int cols, const void *const (&p)[4], const int (&dtypes)[4], const float *w, const float *b, const int8_t *codes, bool narrow)
+int kind_of(int cols, const void *const (&p)[4], const int (&dtypes)[4], const float *w, const float *b, const int8_t *codes, bool narrow)
 {
     const auto fits = [&](int e) {
         for (int i = 0; i < 4; ++i)
             if (p[i] && !pieces_ok(e, cols, p[i], dtypes[i])) return false;
         return cols % e == 0 && reinterpret_cast<uintptr_t>(codes) % e == 0 && reinterpret_cast<uintptr_t>(w) % 16 == 0 && reinterpret_cast<uintptr_t>(b) % 16 == 0;
     };
-    return narrow && fits(8) ? 8 : fits(4) ? 4 : 1;
+    return narrow && fits(8) ? 8 : fits(4) ? 4 : unaligned_kind(cols);
 }
 
-constexpr int kGradGroups = 2 * kUnits;   // workgroups of the backward pass, and parts
+constexpr int kGradGroups = 2 * kUnits;   // workgroups of the backward pass at most, and parts
 
 }  // namespace
 
@@ -487,19 +529,19 @@ void launch_layer_norm(const NormShape &s, const void *x, const float *weight, c
                        uint8_t *exps, hipStream_t stream)
 {
     NormArgs a{s.rows, s.cols, s.x_dtype, s.y_dtype, 0, s.eps, x, weight, bias, y, stats, codes, exps};
-    const int e = piece_of(s.cols, {x, y, nullptr, nullptr}, {s.x_dtype, s.y_dtype}, weight, bias, codes, s.x_dtype != LMKAN_F32);
-    if (s.cols > most_held(e)) {
+    const int kind = kind_of(s.cols, {x, y, nullptr, nullptr}, {s.x_dtype, s.y_dtype}, weight, bias, codes, s.x_dtype != LMKAN_F32);
+    if (s.cols > kMostHeld) {
         const unsigned groups = (unsigned)(s.rows < kMostGroups ? s.rows : kMostGroups);
-        if (e > 1) norm_long_kernel<4><<<groups, 1024, 0, stream>>>(a);
-        else norm_long_kernel<1><<<groups, 1024, 0, stream>>>(a);
+        if (kind > 0) norm_long_kernel<4><<<groups, 1024, 0, stream>>>(a);
+        else norm_long_kernel<-4><<<groups, 1024, 0, stream>>>(a);
         return;
     }
-    const Plan p = plan_of(s.cols, e);
+    const Plan p = plan_of(s.cols, kind);
     a.lanes_log = p.lanes_log;
     with_sizes(p, [&](auto sizes) {
         typedef decltype(sizes) S;
         const int most = 8 * kUnits * 256 / S::threads;
-        norm_kernel<S::e, S::h, S::threads, S::group><<<groups_of(p, s.rows, most), S::threads, 0, stream>>>(a);
+        norm_kernel<S::k, S::h, S::threads, S::group><<<groups_of(p, s.rows, most), S::threads, 0, stream>>>(a);
     });
 }
 
@@ -515,26 +557,27 @@ void launch_layer_norm_backward(const NormShape &s, const NormBackwardArgs &a, v
     float *const parts = static_cast<float *>(workspace);
     unsigned groups = 0;
     const bool narrow = s.y_dtype != LMKAN_F32 && (!a.x || s.x_dtype != LMKAN_F32);
-    const int e = piece_of(s.cols, {a.x, a.grad_y, a.grad_x, nullptr}, {s.x_dtype, s.y_dtype, s.x_dtype}, a.weight, nullptr, a.codes, narrow);
-    if (s.rows > 0 && s.cols > most_held(e)) {
+    const int kind = kind_of(s.cols, {a.x, a.grad_y, a.grad_x, nullptr}, {s.x_dtype, s.y_dtype, s.x_dtype}, a.weight, nullptr, a.codes, narrow);
+    if (s.rows > 0 && s.cols > kMostHeld) {
         const unsigned rows = (unsigned)(s.rows < kMostGroups ? s.rows : kMostGroups);
         if (a.grad_x) {
-            if (e > 1) norm_long_grad_x_kernel<4><<<rows, 1024, 0, stream>>>(s, a);
-            else norm_long_grad_x_kernel<1><<<rows, 1024, 0, stream>>>(s, a);
+            if (kind > 0) norm_long_grad_x_kernel<4><<<rows, 1024, 0, stream>>>(s, a);
+            else norm_long_grad_x_kernel<-4><<<rows, 1024, 0, stream>>>(s, a);
         }
         groups = rows < 64 ? rows : 64;
         if (columns) {
-            if (e > 1) norm_long_columns_kernel<4><<<dim3((s.cols / 4 + 255) / 256, groups), 256, 0, stream>>>(s, a, parts);
-            else norm_long_columns_kernel<1><<<dim3((s.cols + 255) / 256, groups), 256, 0, stream>>>(s, a, parts);
+            const dim3 across((s.cols + 1023) / 1024, groups);
+            if (kind > 0) norm_long_columns_kernel<4><<<across, 256, 0, stream>>>(s, a, parts);
+            else norm_long_columns_kernel<-4><<<across, 256, 0, stream>>>(s, a, parts);
         }
     } else if (s.rows > 0) {
         GradArgs g{s, a, 0, columns ? parts : nullptr};
-        const Plan p = plan_of(s.cols, e);
+        const Plan p = plan_of(s.cols, kind);
         g.lanes_log = p.lanes_log;
         groups = groups_of(p, s.rows, kGradGroups);
         with_sizes(p, [&](auto sizes) {
             typedef decltype(sizes) S;
-            norm_grad_kernel<S::e, S::h, S::threads, S::group><<<groups, S::threads, 0, stream>>>(g);
+            norm_grad_kernel<S::k, S::h, S::threads, S::group><<<groups, S::threads, 0, stream>>>(g);
         });
     }
     if (columns) norm_join_kernel<<<dim3((s.cols + 31) / 32, 2), 1024, 0, stream>>>(s, a, (int)groups, parts);

@@ -99,83 +99,164 @@ __device__ __forceinline__ V over_lanes(V v, int lanes, F &&f)
 __device__ __forceinline__ const void *row_at(const void *p, int64_t first, int dtype) { return static_cast<const char *>(p) + first * (dtype == LMKAN_F32 ? 4 : 2); }
 __device__ __forceinline__ void *row_at(void *p, int64_t first, int dtype) { return static_cast<char *>(p) + first * (dtype == LMKAN_F32 ? 4 : 2); }
 
-// E adjacent elements of a row: 1, or 4 or 8 that are aligned to their size together
-template <int E, int DTYPE>
-__device__ __forceinline__ void load_piece(const void *p, unsigned at, float (&v)[E])
+// Pieces of adjacent elements, of kind K:
+//   4, 8   aligned to their size together; a row is a whole number of them
+//   -4     four that start anywhere (the loads take any address that elements may have); at the end of a row the last four
+//          elements are read and moved down, and the rest is zero.  Rows of four elements at least
+//   1      one by one
+constexpr int elements_of(int kind) { return kind < 0 ? -kind : kind; }
+
+template <class V>
+struct __attribute__((packed, aligned(1))) Anywhere {
+    V v;
+};
+typedef uint32_t uintx2 __attribute__((ext_vector_type(2)));
+typedef uint32_t uintx4 __attribute__((ext_vector_type(4)));
+template <class V, bool ANYWHERE>
+__device__ __forceinline__ V load_words(const void *p)
 {
-    if constexpr (E == 1) {
-        v[0] = load_as_float(p, at, DTYPE);
-    } else if constexpr (DTYPE == LMKAN_F32) {
-#pragma unroll
-        for (int i = 0; i < E; i += 4) {
-            const float4 f = *reinterpret_cast<const float4 *>(static_cast<const float *>(p) + at + i);
-            v[i] = f.x, v[i + 1] = f.y, v[i + 2] = f.z, v[i + 3] = f.w;
+    if constexpr (ANYWHERE) return reinterpret_cast<const Anywhere<V> *>(p)->v;
+    else return *static_cast<const V *>(p);
+}
+template <bool ANYWHERE, class V>
+__device__ __forceinline__ void store_words(void *p, V v)
+{
+    if constexpr (ANYWHERE) reinterpret_cast<Anywhere<V> *>(p)->v = v;
+    else *static_cast<V *>(p) = v;
+}
+
+// Where the elements of the piece at column `at` are read: in the row in any case
+template <int K>
+__device__ __forceinline__ unsigned read_at(int at, int cols)
+{
+    return (unsigned)(K < 0 ? (at + 4 <= cols ? at : cols - 4) : (at < cols ? at : 0));
+}
+// What belongs to the columns at .. of what was read (beyond the end: zeros)
+template <int K, int E>
+__device__ __forceinline__ void settle(float (&v)[E], int at, int cols)
+{
+    if constexpr (K < 0) {
+        const int move = at + 4 - cols;
+        if (move > 0) {
+            if (move & 1) v[0] = v[1], v[1] = v[2], v[2] = v[3], v[3] = 0.0f;
+            if (move & 2) v[0] = v[2], v[1] = v[3], v[2] = v[3] = 0.0f;
+            if (move >= 4) v[0] = v[1] = v[2] = v[3] = 0.0f;
         }
     } else {
-        uint32_t w[E / 2];
-        const uint16_t *from = static_cast<const uint16_t *>(p) + at;
-        if constexpr (E == 8) {
-            const uint4 u = *reinterpret_cast<const uint4 *>(from);
-            w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w;
-        } else {
-            const uint2 u = *reinterpret_cast<const uint2 *>(from);
-            w[0] = u.x, w[1] = u.y;
-        }
 #pragma unroll
-        for (int i = 0; i < E; ++i) {
-            const uint16_t b = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
-            v[i] = load_as_float(&b, 0, DTYPE);
-        }
+        for (int i = 0; i < E; ++i) v[i] = at < cols ? v[i] : 0.0f;
     }
 }
-template <int E>
-__device__ __forceinline__ void load_piece(const void *p, unsigned at, int dtype, float (&v)[E])
+template <int K>
+__device__ __forceinline__ bool exists(int at, int i, int cols) { return K < 0 ? at + i < cols : at < cols; }
+
+// A piece as it lies in memory (WIDE: float32), and then as float32
+template <int K, bool WIDE, int E>
+__device__ __forceinline__ void load_raw(const void *row, int at, int cols, uint32_t (&w)[E])
 {
-    if (dtype == LMKAN_F32) load_piece<E, LMKAN_F32>(p, at, v);
-    else if (dtype == LMKAN_F16) load_piece<E, LMKAN_F16>(p, at, v);
-    else load_piece<E, LMKAN_BF16>(p, at, v);
+    const unsigned from = read_at<K>(at, cols);
+    if constexpr (E == 1) {
+        w[0] = WIDE ? static_cast<const uint32_t *>(row)[from] : static_cast<const uint16_t *>(row)[from];
+    } else {
+        const char *p = static_cast<const char *>(row) + from * (WIDE ? 4u : 2u);
+        constexpr int kWords = WIDE ? E : E / 2;
+        if constexpr (kWords == 2) {
+            const uintx2 u = load_words<uintx2, K < 0>(p);
+            w[0] = u[0], w[1] = u[1];
+        } else {
+#pragma unroll
+            for (int i = 0; i < kWords; i += 4) {
+                const uintx4 u = load_words<uintx4, K < 0>(p + 4 * i);
+                w[i] = u[0], w[i + 1] = u[1], w[i + 2] = u[2], w[i + 3] = u[3];
+            }
+        }
+#pragma unroll
+        for (int i = kWords; i < E; ++i) w[i] = 0;
+    }
 }
-template <int E>
-__device__ __forceinline__ void store_piece(void *p, unsigned at, int dtype, const float (&v)[E])
+template <int DTYPE, int E>
+__device__ __forceinline__ void convert(const uint32_t (&w)[E], float (&v)[E])
+{
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+        const uint32_t word = E == 1 || DTYPE == LMKAN_F32 ? w[i] : w[i / 2];
+        if (DTYPE == LMKAN_F32) v[i] = __builtin_bit_cast(float, word);
+        else if (DTYPE == LMKAN_F16) v[i] = (float)__builtin_bit_cast(_Float16, (uint16_t)(word >> (16 * (i & 1))));
+        else v[i] = __builtin_bit_cast(float, i & 1 ? word & 0xffff0000u : word << 16);
+    }
+}
+// (what was read; `settle` makes columns of it)
+template <int K, int DTYPE, int E>
+__device__ __forceinline__ void load_piece_as(const void *row, int at, int cols, float (&v)[E])
+{
+    uint32_t w[E];
+    load_raw<K, DTYPE == LMKAN_F32>(row, at, cols, w);
+    convert<DTYPE>(w, v);
+}
+template <int K, int E>
+__device__ __forceinline__ void load_piece(const void *row, int at, int cols, int dtype, float (&v)[E])
+{
+    if (dtype == LMKAN_F32) load_piece_as<K, LMKAN_F32>(row, at, cols, v);
+    else if (dtype == LMKAN_F16) load_piece_as<K, LMKAN_F16>(row, at, cols, v);
+    else load_piece_as<K, LMKAN_BF16>(row, at, cols, v);
+}
+
+// Two adjacent 16-bit elements, the first in the lower half (bfloat16 by the instruction that rounds two at a time)
+__device__ __forceinline__ uint32_t two_narrow(int dtype, float a, float b)
+{
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    if (dtype == LMKAN_F16) return two_from_float(LMKAN_F16, a, b);
+    return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
+}
+
+// A piece that exists, in part at the end of a row
+template <int K, int E>
+__device__ __forceinline__ void store_piece(void *row, int at, int cols, int dtype, const float (&v)[E])
 {
     if constexpr (E == 1) {
-        store_from_float(p, at, dtype, v[0]);
+        store_from_float(row, at, dtype, v[0]);
+        return;
+    }
+    if (K < 0 && at + E > cols) {
+#pragma unroll
+        for (int i = 0; i < E; ++i)
+            if (at + i < cols) store_from_float(row, at + i, dtype, v[i]);
     } else if (dtype == LMKAN_F32) {
 #pragma unroll
-        for (int i = 0; i < E; i += 4) *reinterpret_cast<float4 *>(static_cast<float *>(p) + at + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
-    } else {
-        uint32_t w[E / 2];
+        for (int i = 0; i + 3 < E; i += 4) {
+            uintx4 u;
 #pragma unroll
-        for (int i = 0; i < E / 2; ++i) w[i] = two_from_float(dtype, v[2 * i], v[2 * i + 1]);
-        uint16_t *to = static_cast<uint16_t *>(p) + at;
-        if constexpr (E == 8) *reinterpret_cast<uint4 *>(to) = make_uint4(w[0], w[1], w[2], w[3]);
-        else *reinterpret_cast<uint2 *>(to) = make_uint2(w[0], w[1]);
+            for (int e = 0; e < 4; ++e) u[e] = __builtin_bit_cast(uint32_t, v[i + e]);
+            store_words<K < 0>(static_cast<float *>(row) + at + i, u);
+        }
+    } else {
+        char *to = reinterpret_cast<char *>(static_cast<uint16_t *>(row) + at);
+        if constexpr (E == 8) store_words<false>(to, uintx4{two_narrow(dtype, v[0], v[1]), two_narrow(dtype, v[2], v[3]), two_narrow(dtype, v[4], v[5]), two_narrow(dtype, v[6], v[7])});
+        else if constexpr (E == 4) store_words<K < 0>(to, uintx2{two_narrow(dtype, v[0], v[1]), two_narrow(dtype, v[2], v[3])});
     }
 }
 
-// E adjacent codes as they lie in memory, four to a word
-template <int E>
-__device__ __forceinline__ void load_codes_piece(const int8_t *p, uint32_t (&w)[(E + 3) / 4])
+// A piece of codes as it was read, four to a word; then the values, which `settle` puts in place
+template <int K, int W>
+__device__ __forceinline__ void load_codes_piece(const int8_t *row, int at, int cols, uint32_t (&w)[W])
 {
-    if constexpr (E == 1) {
+    const int8_t *p = row + read_at<K>(at, cols);
+    if constexpr (K == 1) {
         w[0] = (uint8_t)*p;
-    } else if constexpr (E == 4) {
-        w[0] = *reinterpret_cast<const uint32_t *>(p);
+    } else if constexpr (K == 8) {
+        const uintx2 u = load_words<uintx2, false>(p);
+        w[0] = u[0], w[1] = u[1];
     } else {
-        const uint2 u = *reinterpret_cast<const uint2 *>(p);
-        w[0] = u.x, w[1] = u.y;
+        w[0] = load_words<uint32_t, K < 0>(p);
     }
 }
-// The power of two of a block in float32 (NaN for 255); times a code it is the value, exactly, where it is not below 2^-126
-// (there the value itself is worked out)
+// (a code times its block's power of two is exact, 2^-133 times 127 too; the power is NaN for 255)
 template <int E>
 __device__ __forceinline__ void values_of(const uint32_t (&w)[(E + 3) / 4], int byte, float (&v)[E])
 {
+    const float power = value_of(1, byte);
 #pragma unroll
-    for (int i = 0; i < E; ++i) v[i] = (float)(int8_t)(w[i / 4] >> (8 * (i & 3)));
-    const int e = byte - kExpBias;
-#pragma unroll
-    for (int i = 0; i < E; ++i) v[i] = __builtin_amdgcn_ldexpf(byte == kExpNan ? __builtin_nanf("") : v[i], e);
+    for (int i = 0; i < E; ++i) v[i] = (float)(int8_t)(w[i / 4] >> (8 * (i & 3))) * power;
 }
 
 // A piece of a block to codes: its byte, from the largest magnitude over the lanes of the block, and the codes.  All lanes of
@@ -203,20 +284,29 @@ __device__ __forceinline__ int encode_piece(const float (&v)[E], uint32_t (&w)[(
     }
     return byte;
 }
-template <int E>
-__device__ __forceinline__ void store_codes_piece(int8_t *p, const uint32_t (&w)[(E + 3) / 4])
+template <int K, int W>
+__device__ __forceinline__ void store_codes_piece(int8_t *row, int at, int cols, const uint32_t (&w)[W])
 {
-    if constexpr (E == 1) *p = (int8_t)w[0];
-    else if constexpr (E == 4) *reinterpret_cast<uint32_t *>(p) = w[0];
-    else *reinterpret_cast<uint2 *>(p) = make_uint2(w[0], w[1]);
+    if constexpr (K == 1) {
+        row[at] = (int8_t)w[0];
+    } else if constexpr (K == 8) {
+        store_words<false>(row + at, uintx2{w[0], w[1]});
+    } else if (K < 0 && at + 4 > cols) {
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+            if (at + i < cols) row[at + i] = (int8_t)(w[0] >> (8 * i));
+    } else {
+        store_words<K < 0>(row + at, w[0]);
+    }
 }
 
-// Whether pieces of E elements of a matrix of rows of `cols` may be taken together
+// Whether pieces of 4 or 8 elements of a matrix of rows of `cols` are aligned
 inline bool pieces_ok(int e, int cols, const void *p, int dtype)
 {
     const size_t size = dtype == LMKAN_F32 ? 16 : 2 * e;
     return cols % e == 0 && reinterpret_cast<uintptr_t>(p) % size == 0;
 }
+inline int unaligned_kind(int cols) { return cols < 4 ? 1 : -4; }
 
 struct NormShape {
     int64_t rows;
