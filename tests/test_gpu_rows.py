@@ -655,3 +655,43 @@ def test_chain_against_autograd(dev):
     exact = x.double().requires_grad_()
     torch.nn.functional.layer_norm(exact, (n_in,), w.double(), b.double(), EPS).backward(gz.double())
     assert float((gx.cpu().double() - exact.grad).norm() / exact.grad.norm()) <= 0.01
+
+
+def test_normalised_layer_of_the_example(dev):
+    """The example's training step runs, and its gradients are those of the formulas at the values that the checkpoint
+    stands for; its answers with adapters are the plain ones plus the adapters' products."""
+    from paper_2509_07103_amd import preconditioned
+    losses, off = preconditioned.run(3, 256, 32, 24, 7, normalised=True)
+    assert len(losses) == 3 and all(np.isfinite(losses)) and off < 0.1
+    rows, n_in, n_out = 200, 64, 40
+    model = preconditioned.NormalisedLayer(n_in, n_out, 8, 0.3, dev)
+    x, gy = _rows(rows, n_in, seed=250), 1e-2 * _randn(rows, n_out, seed=251)
+    _, saved = model.forward(x.to(dev))
+    grad_x, grad_table, grad_weight = model.gradients(saved, gy.to(dev))
+    stats, kept = saved
+    z = _values(kept[0].cpu(), kept[1].cpu())
+    w, g = model.weight.cpu().double(), gy.double()
+    relu = z.clamp(min=0.0)
+    _within(grad_weight, g.T @ relu, (rows / 4 + 64) * U * torch.sqrt(g.square().T @ relu.square()) + 1e-44, "grad_weight")
+    # (a table of zeros: the layer itself passes nothing back); the product of float32 on the way is off by n_out u of the
+    # magnitudes, which the norm's backward pass takes to at most three times that of a row
+    gz = (g @ w) * (z > 0)
+    want, tol = _norm_gradients(z, stats[:, 1:].cpu().double(), gz, None)
+    size = (g.abs() @ w.abs()).amax(dim=1, keepdim=True) * stats[:, 1:].cpu().double() * (1 + z.abs())
+    _within(grad_x, want, tol + 3 * n_out * U * size, "grad_x")
+    _, table = pkg.lmkan_backward(model.layer, pkg.lmkan_restore_rows(*kept), model.table, (0.3 * gy).to(dev), need_grad_x=False)
+    assert float((table - grad_table).norm() / table.norm()) <= 1e-5
+    model.freeze()
+    adapters = preconditioned.random_adapters(3, 8, n_in, n_out, dev)
+    index = (torch.arange(rows) % 4 - 1).int()
+    plain, adapted = model.answer(x.to(dev)), model.answer(x.to(dev), adapters, index.to(dev))
+    assert torch.equal(plain[::4], adapted[::4])                        # no adapter
+    zf, _, _ = pkg.lmkan_layer_norm(model.norm, x.to(dev))
+    zd, a, b = zf.cpu().double().clamp(min=0.0), adapters[1].cpu().double(), adapters[2].cpu().double()
+    for n in range(1, rows, 17):
+        r = int(index[n])
+        if r >= 0:
+            add = b[r] @ (a[r] @ zd[n])
+            size = b[r].abs() @ (a[r].abs() @ zd[n])
+            want = plain[n].cpu().double() + add
+            _within(adapted[n], want, (n_in + 8 + 16) * U * size + 2 * U * want.abs())
