@@ -575,7 +575,8 @@ lmkan_status lmkan_layer_norm(const lmkan_norm *desc, int64_t rows, const void *
  *   workspace_dev / workspace_bytes: at least lmkan_layer_norm_backward_workspace_bytes(desc, rows)
  *                         bytes, 256-byte aligned (NULL allowed when 0, and when neither grad_weight nor
  *                         grad_bias is wanted)
- * Sums are float32, in an order that the sizes fix: the results repeat bit for bit.
+ * Sums are float32, in an order that the sizes and the tensors' alignment fix: the results repeat bit
+ * for bit.
  */
 size_t lmkan_layer_norm_backward_workspace_bytes(const lmkan_norm *desc, int64_t rows);
 lmkan_status lmkan_layer_norm_backward(const lmkan_norm *desc, int64_t rows, const void *x_dev, const int8_t *codes_dev,
@@ -594,8 +595,8 @@ lmkan_status lmkan_layer_norm_backward(const lmkan_norm *desc, int64_t rows, con
  *   workspace_dev / workspace_bytes: at least lmkan_linear_grad_workspace_bytes(desc, batch)
  *                    bytes, 256-byte aligned (NULL allowed when 0)
  * Products keep 24 bits of grad_y (all of a 16-bit one) and all of the values, and are summed in
- * float32 in an order that the sizes fix: the results repeat bit for bit.  Factors below 2^-126 may
- * count as zeros.
+ * float32 in an order that the sizes and the tensors' alignment fix: the results repeat bit for bit.
+ * Factors below 2^-126 may count as zeros.  An infinite grad_y makes what it enters infinite or NaN.
  */
 #define LMKAN_LINEAR_ACCUMULATE 2
 size_t lmkan_linear_grad_workspace_bytes(const lmkan_linear *desc, int64_t batch);
@@ -630,7 +631,8 @@ typedef struct lmkan_adapters {
  *   workspace_dev / workspace_bytes: at least lmkan_adapters_workspace_bytes(desc, batch) bytes,
  *              256-byte aligned (NULL allowed when 0)
  * Products and sums are float32 (products of 16-bit factors are exact), y is rounded to its type
- * once.  The results repeat bit for bit.
+ * once.  The results repeat bit for bit.  Float32 and bfloat16 factors below 2^-126 may count as zeros;
+ * an infinite factor makes what it enters infinite or NaN.
  */
 size_t lmkan_adapters_workspace_bytes(const lmkan_adapters *desc, int64_t batch);
 lmkan_status lmkan_adapters_add(const lmkan_adapters *desc, int64_t batch, const void *x_dev, const int32_t *index_dev,

@@ -510,6 +510,37 @@ def test_adapters_with_values_that_are_not_finite_stay_in_their_rows(dev):
             assert torch.equal(got[n], clean[n])
 
 
+@pytest.mark.parametrize("types", ["f32 f32 f32", "bf16 bf16 bf16", "f16 f16 f32", "f32 f16 bf16"])
+def test_many_rows_with_values_that_are_not_finite_stay_in_their_rows(dev, types):
+    w, x_type, y_type = types.split()
+    data = _adapters(900, 128, 64, 24, 3, w=w, x=x_type, y=y_type, seed=212, index=torch.arange(900) % 3)
+    x, index, a, b, y, scale = data
+    desc, clean = _check_adapters(dev, data, False, True, w, x_type, y_type)
+    x, a, b, y = x.clone(), a.clone(), b.clone(), y.clone()
+    x[7, 5] = float("nan")
+    x[9, 127] = float("-inf")
+    a[2, 0, 0] = float("inf")
+    b[1, 63, 23] = float("inf")
+    y[12, 3] = float("nan")
+    got = pkg.lmkan_adapters_add(desc, x.to(dev), index.to(dev), a.to(dev), b.to(dev), y.to(dev), scale=scale.to(dev)).cpu()
+    bad = ~torch.isfinite(got)
+    want = torch.zeros(900, 64, dtype=torch.bool)
+    want[7] = want[9] = want[2::3] = True
+    want[1::3, 63] = want[12, 3] = True
+    assert torch.equal(bad, want)
+    assert torch.equal(got[~want], clean.cpu()[~want])
+
+
+@pytest.mark.parametrize("small", ["x", "a", "b"])
+@pytest.mark.parametrize("batch", [6, 900])
+def test_float16_numbers_below_the_smallest_normal_one_count(dev, small, batch):
+    """Multiples of 2^-24 are factors like any other."""
+    x, index, a, b, y, scale = _adapters(batch, 128, 64, 16, 3, w="f16", x="f16", y="f32", seed=215, index=torch.arange(batch) % 3)
+    tiny = {"x": x, "a": a, "b": b}[small]
+    tiny.copy_(tiny * 2.0 ** -18)
+    _check_adapters(dev, (x, index, a, b, torch.zeros_like(y), scale), False, True, "f16", "f16", "f32")
+
+
 # ---- all of them -----------------------------------------------------------------------------------------------------
 
 def _guarded(t, dev, shift):
@@ -695,3 +726,47 @@ def test_normalised_layer_of_the_example(dev):
             size = b[r].abs() @ (a[r].abs() @ zd[n])
             want = plain[n].cpu().double() + add
             _within(adapted[n], want, (n_in + 8 + 16) * U * size + 2 * U * want.abs())
+
+
+def test_offsets_beyond_32_bits(dev):
+    """Matrices of more than 2^31 elements: their last rows come out as they do alone."""
+    rows, cols, last = 16 * 1024 + 256, 131070, 4
+    gen = torch.Generator(device=dev).manual_seed(260)
+    x = torch.empty((rows, cols), dtype=torch.float16, device=dev).normal_(generator=gen)
+    end = x[-last:]                                                     # (aligned as the first row is)
+    assert x.numel() > 2 ** 31 and end.data_ptr() % 16 == x.data_ptr() % 16
+    desc = pkg.NormDesc(cols, x_dtype=pkg.LMKAN_F16, y_dtype=pkg.LMKAN_F16)
+    y, stats, kept = pkg.lmkan_layer_norm(desc, x, keep=True)
+    y_end, stats_end, kept_end = pkg.lmkan_layer_norm(desc, end, keep=True)
+    for got, want in [(y, y_end), (stats, stats_end), (kept[0], kept_end[0]), (kept[1], kept_end[1])]:
+        assert torch.equal(got[-last:], want)
+    codes, exps = pkg.lmkan_checkpoint_rows(x, relu=True)
+    of_end = pkg.lmkan_checkpoint_rows(end, relu=True)
+    assert torch.equal(codes[-last:], of_end[0]) and torch.equal(exps[-last:], of_end[1])
+    pkg.lmkan_restore_rows(codes, exps, dtype=pkg.LMKAN_F16, y=y)
+    assert torch.equal(y[-last:], pkg.lmkan_restore_rows(*of_end, dtype=pkg.LMKAN_F16))
+    for given in ({"x": x}, {"kept": kept}):
+        alone = {"x": end} if "x" in given else {"kept": kept_end}
+        grad_x, grad_weight, grad_bias = pkg.lmkan_layer_norm_backward(desc, y, stats, **given)
+        assert torch.equal(grad_x[-last:], pkg.lmkan_layer_norm_backward(desc, y[-last:], stats_end, **alone)[0])
+        del grad_x
+    # one row that is not zero: each sum is one product
+    linear = pkg.LinearDesc(cols, 3)
+    gy = torch.zeros((rows, 3), device=dev)
+    gy[-1] = torch.tensor([1.5, -0.3, 7.0], device=dev)
+    for got, want in zip(pkg.lmkan_linear_grad(linear, codes, exps, gy), pkg.lmkan_linear_grad(linear, of_end[0], of_end[1], gy[-last:])):
+        assert torch.equal(got, want)
+    y.zero_()                                                           # .. and with the gradient's own offsets
+    y[-1] = x[0]
+    few = pkg.lmkan_checkpoint_rows(_randn(rows, 3, seed=261).to(dev))
+    got = pkg.lmkan_linear_grad(pkg.LinearDesc(3, cols, y_dtype=pkg.LMKAN_F16), *few, y)[0]
+    assert torch.equal(got, x[0].float()[:, None] * pkg.lmkan_restore_rows(*few)[-1])   # (11 bits times 7: exact)
+    # adapters: n_in u of the sum of magnitudes and the rest, as ever
+    a = (_randn(2, 3, cols, seed=262) / cols ** 0.5).half()
+    b, index = _randn(2, 5, 3, seed=263).half(), torch.arange(rows, dtype=torch.int32) % 2
+    out = pkg.lmkan_adapters_add(pkg.AdapterDesc(2, 3, cols, 5, dtype=pkg.LMKAN_F16, x_dtype=pkg.LMKAN_F16), x, index.to(dev), a.to(dev), b.to(dev),
+                                 torch.zeros((rows, 5), device=dev))
+    for n in list(range(3)) + list(range(rows - 3, rows)):
+        xd, ad, bd = x[n].cpu().double(), a[n % 2].double(), b[n % 2].double()
+        size = bd.abs() @ (ad.abs() @ xd.abs())
+        _within(out[n], bd @ (ad @ xd), (cols + 3 + 16) * U * size, f"row {n}")
