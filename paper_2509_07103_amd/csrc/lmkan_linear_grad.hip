@@ -202,7 +202,7 @@ __global__ __launch_bounds__(GradTile<WJ>::THREADS, 2) void linear_grad_kernel(G
 {
     typedef GradTile<WJ> T;
     constexpr int P = parts_of<DTYPE>();
-    constexpr int AHEAD = WJ < 4 ? 4 : 2;   // steps of 16 rows whose gradients are under way   // steps of 16 rows that are under way
+    constexpr int AHEAD = WJ < 4 ? 4 : 2;   // steps of 16 rows whose gradients are under way
     __shared__ __align__(16) char lds[2 * kStageBytes + 2 * kScaleFloats * (int)sizeof(float)];
     const int tiles = a.down * a.across, total = tiles * a.splits;
     const int id = a.first + (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);   // (workgroups on one die: adjacent tiles of the same rows)
@@ -303,18 +303,24 @@ __global__ __launch_bounds__(GradTile<WJ>::THREADS, 2) void linear_grad_kernel(G
         // (powers of two are read two stages ahead, as zeros beyond the last row; what else would be beyond the last stage is that
         // stage again, and not used)
         Stages rows(a.grad_y, a.batch, pitch, from), codes(a.codes, a.batch, a.n_in, from), exps(a.exps, a.batch, per_row, from);
+        // (loads in the order in which the loop leaves them under way: a wait counts back from the last one)
+        Codes first = load_codes(reads, codes);
+        const uint32_t byte0 = load_exp(exps);
+        exps.next();
+        const uint32_t byte1 = load_exp(exps);
+        if (from + 1 < to) codes.next();
+        Codes c = load_codes(reads, codes);
+        __builtin_amdgcn_sched_barrier(0);
         RawPair<DTYPE> raw[AHEAD];
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) raw[k] = load_pair(reads, rows, k);
-        const Codes first = rectified(load_codes(reads, codes));
-        store_scale(load_exp(exps), scales);
-        exps.next();
-        store_scale(load_exp(exps), scales + kScaleFloats);
+        __builtin_amdgcn_sched_barrier(0);
+        store_scale(byte0, scales);
+        store_scale(byte1, scales + kScaleFloats);
+        first = rectified(first);
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < 4; ++k) store_column(first, k, scales, lds);
-        if (from + 1 < to) codes.next();
-        Codes c = load_codes(reads, codes);
         __syncthreads();
         for (int s = from; s < to; ++s) {
             const int now = s - from & 1;
@@ -435,6 +441,7 @@ __global__ __launch_bounds__(256) void linear_grad_join_kernel(GradArgs a)
 #pragma unroll 8
     for (int s = wave; s < a.splits; s += 4) sum += a.parts[s * groups + i];
     if (biased)
+#pragma unroll 8
         for (int s = wave; s < a.splits; s += 4) bias += a.bias_parts[(int64_t)s * a.n_out + i];
     if (wave > 0) sums[wave - 1][lane] = sum, bias_sums[wave - 1][lane] = bias;
     __syncthreads();
