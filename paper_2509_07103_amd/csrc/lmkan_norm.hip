@@ -92,19 +92,24 @@ struct Spread {
             for (int h = 0; h < H; ++h) settle<K>(v[h], column(h), cols);
     }
     // columns' weights or the like: `other` where there are none, zero beyond the end
+    __device__ __forceinline__ void load_columns(const float *p, float other, int h, int cols, float (&v)[E]) const
+    {
+        if (p) load_piece_as<K, LMKAN_F32>(p, column(h), cols, v);
+        if (K < 0) settle<K>(v, column(h), cols);
+#pragma unroll
+        for (int i = 0; i < E; ++i) v[i] = exists<K>(column(h), i, cols) ? (p ? v[i] : other) : 0.0f;
+    }
     __device__ __forceinline__ void load_columns(const float *p, float other, int cols, float (&v)[H][E]) const
     {
-        if (p)
 #pragma unroll
-            for (int h = 0; h < H; ++h) load_piece_as<K, LMKAN_F32>(p, column(h), cols, v[h]);
-#pragma unroll
-        for (int h = 0; h < H; ++h) {
-            if (K < 0) settle<K>(v[h], column(h), cols);
-#pragma unroll
-            for (int i = 0; i < E; ++i) v[h][i] = exists<K>(column(h), i, cols) ? (p ? v[h][i] : other) : 0.0f;
-        }
+        for (int h = 0; h < H; ++h) load_columns(p, other, h, cols, v[h]);
     }
 };
+
+// Elements of a row that a lane holds, and of the longest rows that registers hold
+constexpr int kLaneHolds = 16, kLaneHoldsMost = 32, kMostHeld = 512 * kLaneHoldsMost;
+// Weights stay in registers beside 16 elements of the row; beside 32 they are read for every row
+constexpr bool weights_held(int held) { return held <= kLaneHolds; }
 
 struct NormArgs {
     int64_t rows;
@@ -127,9 +132,12 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(NormArgs a)
     constexpr int E = elements_of(K);
     __shared__ double sums[THREADS / 64];
     const Spread<K, H, THREADS, GROUP> s(a.lanes_log);
+    constexpr bool kHeld = weights_held(H * E);
     float w[H][E], b[H][E];
-    s.load_columns(a.weight, 1.0f, a.cols, w);
-    s.load_columns(a.bias, 0.0f, a.cols, b);
+    if (kHeld) {
+        s.load_columns(a.weight, 1.0f, a.cols, w);
+        s.load_columns(a.bias, 0.0f, a.cols, b);
+    }
     for (int64_t row = (int64_t)blockIdx.x * s.rows + s.row; row < a.rows; row += (int64_t)gridDim.x * s.rows) {
         const int64_t first = row * a.cols;
         uint32_t raw[H][E];
@@ -177,8 +185,16 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(NormArgs a)
                 }
             }
             if (c < a.cols) {
+                float wh[E], bh[E];
+                if constexpr (kHeld) {
 #pragma unroll
-                for (int i = 0; i < E; ++i) hat[i] = fmaf(w[h][i], hat[i], b[h][i]);
+                    for (int i = 0; i < E; ++i) wh[i] = w[h][i], bh[i] = b[h][i];
+                } else {
+                    s.load_columns(a.weight, 1.0f, h, a.cols, wh);
+                    s.load_columns(a.bias, 0.0f, h, a.cols, bh);
+                }
+#pragma unroll
+                for (int i = 0; i < E; ++i) hat[i] = fmaf(wh[i], hat[i], bh[i]);
                 store_piece<K>(y, c, a.cols, a.y_dtype, hat);
             }
         }
@@ -256,7 +272,8 @@ struct GradArgs {
     float *parts;   // [workgroups][2][cols], or null: no gradients of weight and bias
 };
 
-template <int K, int H, int THREADS, bool GROUP>
+// KEPT: from the checkpoint (one kernel for both would hold the registers of both)
+template <bool KEPT, int K, int H, int THREADS, bool GROUP>
 __global__ __launch_bounds__(THREADS) void norm_grad_kernel(GradArgs g)
 {
     constexpr int E = elements_of(K);
@@ -267,19 +284,26 @@ __global__ __launch_bounds__(THREADS) void norm_grad_kernel(GradArgs g)
     const Spread<K, H, THREADS, GROUP> s(g.lanes_log);
     const float part = 1.0f / (float)cols;
     float w[H][E], gw[H][E], gb[H][E];
-    s.load_columns(a.weight, 1.0f, cols, w);
+    if (weights_held(H * E)) s.load_columns(a.weight, 1.0f, cols, w);
 #pragma unroll
     for (int h = 0; h < H; ++h)
 #pragma unroll
         for (int i = 0; i < E; ++i) gw[h][i] = gb[h][i] = 0.0f;
     for (int64_t row = (int64_t)blockIdx.x * s.rows + s.row; row < g.s.rows; row += (int64_t)gridDim.x * s.rows) {
         const int64_t first = row * cols;
-        // (all loads of the row are under way before the first is used)
+        // (all loads of the row are under way before the first is used, but for the longest unaligned rows, for which registers
+        // are short)
+        constexpr bool kOneByOne = KEPT && K < 0 && !weights_held(H * E);
         uint32_t raw_d[H][E], raw_x[H][E], coded[H][(E + 3) / 4];
         int byte[H];
+        float d[H][E], hat[H][E];
         s.load(a.grad_y, first, g.s.y_dtype, cols, raw_d);
+        if constexpr (kOneByOne) {
+            s.take(raw_d, g.s.y_dtype, cols, d);
+            __builtin_amdgcn_sched_barrier(0);
+        }
         const float mean = a.stats[2 * row], rstd = a.stats[2 * row + 1];
-        if (a.x) {
+        if constexpr (!KEPT) {
             s.load(a.x, first, g.s.x_dtype, cols, raw_x);
         } else {
             const int8_t *codes = a.codes + first;
@@ -290,9 +314,8 @@ __global__ __launch_bounds__(THREADS) void norm_grad_kernel(GradArgs g)
                 byte[h] = exps[(s.column(h) < cols ? s.column(h) : 0) / kBlock];
             }
         }
-        float d[H][E], hat[H][E];
-        s.take(raw_d, g.s.y_dtype, cols, d);
-        if (a.x) {
+        if constexpr (!kOneByOne) s.take(raw_d, g.s.y_dtype, cols, d);
+        if constexpr (!KEPT) {
             s.take(raw_x, g.s.x_dtype, cols, hat);
 #pragma unroll
             for (int h = 0; h < H; ++h)
@@ -307,11 +330,18 @@ __global__ __launch_bounds__(THREADS) void norm_grad_kernel(GradArgs g)
 #pragma unroll
         for (int h = 0; h < H; ++h) {
             if (s.column(h) < cols) {
+                float of_h[E];
+                if constexpr (weights_held(H * E)) {
+#pragma unroll
+                    for (int i = 0; i < E; ++i) of_h[i] = w[h][i];
+                } else {
+                    s.load_columns(a.weight, 1.0f, h, cols, of_h);
+                }
 #pragma unroll
                 for (int i = 0; i < E; ++i) {
                     gb[h][i] += d[h][i];
                     gw[h][i] = fmaf(d[h][i], hat[h][i], gw[h][i]);
-                    d[h][i] *= w[h][i];
+                    d[h][i] *= of_h[i];
                     of_d += d[h][i];
                     of_dh = fmaf(d[h][i], hat[h][i], of_dh);
                 }
@@ -456,8 +486,6 @@ __global__ __launch_bounds__(1024) void norm_join_kernel(NormShape s, NormBackwa
 
 // ---- host ------------------------------------------------------------------------------------------------------------
 
-// Elements of a row that a lane holds, and a workgroup of 512; workgroups of 1024 would leave 128 registers a lane, which spill
-constexpr int kLaneHolds = 16, kMostHeld = 512 * kLaneHolds;
 constexpr int kUnits = 256;                       // compute units
 
 // How a row of `cols` columns is spread: pieces of a kind; its lanes, or the threads of a workgroup
@@ -489,7 +517,8 @@ template <int K, class F>
 void with_held(const Plan &p, F &&f)
 {
     constexpr int kMost = kLaneHolds / elements_of(K);
-    if (p.threads == 512) f(Sizes<K, kMost, 512, true>());
+    if (p.held == 2 * kMost) f(Sizes<K, 2 * kMost, 512, true>());
+    else if (p.threads == 512) f(Sizes<K, kMost, 512, true>());
     else if (p.threads == 256 && p.held == kMost) f(Sizes<K, kMost, 256, true>());
     else if (p.threads == 256) f(Sizes<K, kMost / 2, 256, true>());
     else if (p.held == kMost) f(Sizes<K, kMost, 256, false>());
@@ -574,10 +603,11 @@ void launch_layer_norm_backward(const NormShape &s, const NormBackwardArgs &a, v
         GradArgs g{s, a, 0, columns ? parts : nullptr};
         const Plan p = plan_of(s.cols, kind);
         g.lanes_log = p.lanes_log;
-        groups = groups_of(p, s.rows, kGradGroups);
+        groups = groups_of(p, s.rows, s.cols > kLaneHolds * 512 ? kUnits : kGradGroups);
         with_sizes(p, [&](auto sizes) {
             typedef decltype(sizes) S;
-            norm_grad_kernel<S::k, S::h, S::threads, S::group><<<groups, S::threads, 0, stream>>>(g);
+            if (a.x) norm_grad_kernel<false, S::k, S::h, S::threads, S::group><<<groups, S::threads, 0, stream>>>(g);
+            else norm_grad_kernel<true, S::k, S::h, S::threads, S::group><<<groups, S::threads, 0, stream>>>(g);
         });
     }
     if (columns) norm_join_kernel<<<dim3((s.cols + 31) / 32, 2), 1024, 0, stream>>>(s, a, (int)groups, parts);

@@ -282,6 +282,18 @@ def test_layer_norm_backward_matches_float64(dev, shape, kept):
     _check_norm_backward(dev, shape, "bf16", "bf16", kept, affine=False, seed=40)
 
 
+@pytest.mark.parametrize("shape", [(3, 8200), (5, 9001), (2, 12345), (530, 8193), (300, 16384), (4, 16385)], ids=str)
+@pytest.mark.parametrize("types", ["f32 f32", "bf16 bf16", "f16 f32"])
+def test_rows_on_either_side_of_what_registers_hold(dev, shape, types):
+    x_dtype, y_dtype = types.split()
+    x = _rows(*shape, dtype=x_dtype, seed=65)
+    w, b = _randn(shape[1], seed=66), _randn(shape[1], seed=67)
+    _check_norm(dev, x, y_dtype, w, b, keep=True)
+    _check_norm(dev, x, y_dtype, None, None, keep=False)
+    for kept in (False, True):
+        _check_norm_backward(dev, shape, x_dtype, y_dtype, kept, affine=True, seed=68)
+
+
 @pytest.mark.parametrize("x_dtype", TYPES)
 @pytest.mark.parametrize("y_dtype", TYPES)
 @pytest.mark.parametrize("shape", [(37, 50), (6, 640), (3, 5000), (2, 40000)], ids=str)
