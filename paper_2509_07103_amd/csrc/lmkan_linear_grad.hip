@@ -1,5 +1,18 @@
 // Gradients of the linear term's weights and bias from a checkpoint of its input:
 //   grad_weight[j][e] = sum_n g[n][j] f(value[n][e]),  grad_bias[j] = sum_n g[n][j].
+//
+// A value has 7 bits and a power of two: it is exact in bfloat16.  A gradient is cut into parts of 8 bits, three of a float32, two of
+// a float16, which are exact as well, so that 32 x 32 x 16 bfloat16 instructions make exact products and float32 sums: three of
+// them take 3/8 of the time of float32 instructions.  The axis that is summed is the batch, across which neither matrix is
+// contiguous: gradients go from memory to the instruction's operands directly (a lane has two adjacent outputs of eight rows),
+// codes are turned on their way through LDS.  A tile of 64 to 256 outputs and 128 inputs a workgroup; the batch is cut where tiles are
+// few, and a second launch adds the parts.
+//
+// Measured (us; TFLOP/s of 2 n j e; in brackets counted with the parts, where the library's bfloat16 product reaches 1225):
+// 16384 of 4096 -> 4096 float32 1300 (1270), 8192 of 1024 -> 1024 float32 62 to 72 (720 to 840), of which 8.8 add the parts; 4096 of
+// 4096 -> 4096 bfloat16 140 to 150 (910 to 980); 5000 of 500 -> 333 float32 25, 131072 of 64 -> 10 bfloat16 25.  What bounds a
+// workgroup alone on its unit is its reads on their way through the texture unit (8 bytes a lane, busy for 55 % of the time) and
+// their latency, not the matrix instructions (36 %).
 #include <type_traits>
 
 #include "lmkan_rows.h"
@@ -467,9 +480,10 @@ struct Plan {
 // Tile and splits by what a call takes in us: stages of a workgroup, fitted to 18 shapes (8192 rows of 1024 -> 1024, float32:
 // 3.7 a stage of 256 outputs alone on a compute unit and 6.5 two at a time, 2.2 of 128 outputs; bfloat16 1.5; one and a half to
 // begin with), parts written and joined at 8 TB/s.  Measured (us, best / next other tile / next other number of
-// splits): 8192 of 1024 -> 1024 float32 64 / 67 / 65; 5000 of 500 -> 333 29 / 35 / 32; 65536 of 128 -> 128 32 / 33 / 40;
+// splits): 8192 of 1024 -> 1024 float32 64 / 67 / 65; 5000 of 500 -> 333 29 / 35 / 32; 65536 of 128 -> 128 32 / 33 / 40 (the join has since
+// made that 26);
 // 4096 of 4096 -> 4096 bfloat16 139 / 203 / 174.
-Plan plan_of(const LinearShape &s, bool whole)
+Plan plan_of(const LinearShape &s)
 {
     Plan best = {};
     double least = 1e300;
@@ -531,16 +545,14 @@ bool aligned_to(const void *p, size_t a) { return reinterpret_cast<uintptr_t>(p)
 
 size_t linear_grad_workspace_bytes(const LinearShape &s)
 {
-    // (whether the tensors are aligned is not known here)
-    const size_t some = plan_bytes(s, plan_of(s, false)), all = whole_shape(s) ? plan_bytes(s, plan_of(s, true)) : 0;
-    return some > all ? some : all;
+    return plan_bytes(s, plan_of(s));
 }
 
 void launch_linear_grad(const LinearShape &s, bool accumulate, const int8_t *codes, const uint8_t *exps, const void *grad_y,
                         float *grad_weight, float *grad_bias, void *workspace, hipStream_t stream)
 {
     const bool whole = whole_shape(s) && aligned_to(grad_y, 4) && aligned_to(codes, 4);
-    const Plan p = plan_of(s, whole);
+    const Plan p = plan_of(s);
     GradArgs a{s.batch, s.n_in, s.n_out, s.relu, accumulate, codes, exps, grad_y, grad_weight, grad_bias, p.down, p.across, 0, p.splits, p.stages,
                p.stages / p.splits, p.stages % p.splits, nullptr, nullptr, s.n_in % 4 == 0 && aligned_to(grad_weight, 16)};
     if (p.splits > 1) {
