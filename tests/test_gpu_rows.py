@@ -639,8 +639,9 @@ def _chain(dev, rows=96, n_in=64, n_out=40, seed=230):
     return run
 
 
-def test_chain_on_other_streams(dev):
-    run = _chain(dev)
+@pytest.mark.parametrize("rows", [96, 3000])
+def test_chain_on_other_streams(dev, rows):
+    run = _chain(dev, rows)
     want = run()
     torch.cuda.synchronize()
     side, other = torch.cuda.Stream(), torch.cuda.Stream()
@@ -652,8 +653,9 @@ def test_chain_on_other_streams(dev):
         assert all(torch.equal(g, t) for g, t in zip(got, want))
 
 
-def test_chain_in_a_graph(dev):
-    run = _chain(dev)
+@pytest.mark.parametrize("rows", [96, 3000])
+def test_chain_in_a_graph(dev, rows):
+    run = _chain(dev, rows)
     want = run()
     torch.cuda.synchronize()
     side = torch.cuda.Stream()
