@@ -8,11 +8,10 @@
 // codes are turned on their way through LDS.  A tile of 64 to 256 outputs and 128 inputs a workgroup; the batch is cut where tiles are
 // few, and a second launch adds the parts.
 //
-// Measured (us; TFLOP/s of 2 n j e; in brackets counted with the parts, where the library's bfloat16 product reaches 1225):
-// 16384 of 4096 -> 4096 float32 1300 (1270), 8192 of 1024 -> 1024 float32 62 to 72 (720 to 840), of which 8.8 add the parts; 4096 of
-// 4096 -> 4096 bfloat16 140 to 150 (910 to 980); 5000 of 500 -> 333 float32 25, 131072 of 64 -> 10 bfloat16 25.  What bounds a
-// workgroup alone on its unit is its reads on their way through the texture unit (8 bytes a lane, busy for 55 % of the time) and
-// their latency, not the matrix instructions (36 %).
+// Measured (us; TFLOP/s counted with the parts, where the library's bfloat16 product reaches 1225): 16384 of 4096 -> 4096 float32
+// 1300 (1270), 8192 of 1024 -> 1024 float32 57 to 64 (810 to 900), of which 8.8 add the parts; 4096 of 4096 -> 4096 bfloat16 140 to
+// 150 (910 to 980), bound by reads of four bytes a lane; 5000 of 500 -> 333 float32 24, 131072 of 64 -> 10 bfloat16 22, bound by the
+// start of a workgroup (3 to 4) and the second launch.
 #include <type_traits>
 
 #include "lmkan_rows.h"
@@ -52,21 +51,24 @@ struct GradArgs {
     __host__ __device__ int begin(int s) const { return s * each + (s < more ? s : more); }
 };
 
-// WJ waves lie along the outputs, WAVES / WJ along the inputs: a tile of 64 WJ outputs and 128 inputs
-template <int WJ>
+// WJ waves lie along the outputs, 4 / WJ along the inputs: a tile of 64 WJ outputs and 128 inputs.  H = 2: twice as many, and of a
+// stage's four steps of 16 rows each half takes two, so that two waves share a matrix unit, one making parts while the other
+// multiplies.  H = 1: two workgroups on a unit do the same for each other, where tiles are that many
+template <int WJ, int H>
 struct GradTile {
-    static constexpr int WAVES = 4, THREADS = 64 * WAVES, WE = WAVES / WJ, ROWS = kWaveRows * WJ, TE = kCols / WE / 32;   // TE: tiles of 32 inputs of a wave
-    static constexpr int GROUPS = 2 * TE * 4;                                             // groups of four results of a lane
+    static constexpr int HALF = 4, WAVES = H * HALF, THREADS = 64 * WAVES, WE = HALF / WJ, ROWS = kWaveRows * WJ, TE = kCols / WE / 32;   // TE: tiles of 32 inputs of a wave
+    static constexpr int OUT = 2 / H, GROUPS = OUT * TE * 4;                              // outputs of a pair and groups of four results that a lane ends with
+    static constexpr int STEPS = kDepth / 16 / H;                                         // of a wave in a stage
     static constexpr int CODED = kDepth * kCols / 4 / THREADS;                            // rows of codes of a thread in a stage
 };
 
 // Group q of a lane's results: adjacent inputs e .. e + 3 of output j, within the workgroup's tile
-template <int WJ>
+template <int WJ, int H>
 __device__ __forceinline__ void place_of(int wave, int lane, int q, int *j, int *e)
 {
-    typedef GradTile<WJ> T;
-    const int wj = wave / T::WE, we = wave % T::WE, part = q & 3, et = (q >> 2) % T::TE, jt = (q >> 2) / T::TE;
-    *j = wj * kWaveRows + 2 * (lane & 31) + jt;
+    typedef GradTile<WJ, H> T;
+    const int wj = wave % T::HALF / T::WE, we = wave % T::WE, part = q & 3, et = (q >> 2) % T::TE, jt = (q >> 2) / T::TE;
+    *j = wj * kWaveRows + 2 * (lane & 31) + (H == 2 ? wave / T::HALF : jt);
     *e = (we * T::TE + et) * 32 + 8 * part + 4 * (lane >> 5);
 }
 
@@ -210,12 +212,12 @@ struct Stages {
 enum Reads { kWords, kElements };
 
 // ALIGNED: pairs of 16-bit outputs and fours of codes lie at multiples of their size
-template <int DTYPE, int WJ, bool ALIGNED>
-__global__ __launch_bounds__(GradTile<WJ>::THREADS, 2) void linear_grad_kernel(GradArgs a)
+template <int DTYPE, int WJ, int H, bool ALIGNED>
+__global__ __launch_bounds__((GradTile<WJ, H>::THREADS), H == 1 ? 2 : 1) void linear_grad_kernel(GradArgs a)
 {
-    typedef GradTile<WJ> T;
+    typedef GradTile<WJ, H> T;
     constexpr int P = parts_of<DTYPE>();
-    constexpr int AHEAD = WJ < 4 ? 4 : 2;   // steps of 16 rows whose gradients are under way
+    constexpr int kSteps = T::STEPS, AHEAD = kSteps < 2 ? kSteps : 2;   // steps whose gradients are under way
     __shared__ __align__(16) char lds[2 * kStageBytes + 2 * kScaleFloats * (int)sizeof(float)];
     const int tiles = a.down * a.across, total = tiles * a.splits;
     const int id = a.first + (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);   // (workgroups on one die: adjacent tiles of the same rows)
@@ -225,7 +227,7 @@ __global__ __launch_bounds__(GradTile<WJ>::THREADS, 2) void linear_grad_kernel(G
     grouped_tile(tile, a.down, a.across, &ti, &tj);
     const int j0 = ti * T::ROWS, e0 = tj * kCols;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wj = wave / T::WE, we = wave % T::WE;
+    const int half = wave / T::HALF, wj = wave % T::HALF / T::WE, we = wave % T::WE;
     const int from = a.begin(split), to = a.begin(split + 1);
 
     // Gradients: outputs j, j + 1, rows 8 (lane / 32) on of every 16.  What lies beyond the last row reads as zero; what lies
@@ -326,7 +328,7 @@ __global__ __launch_bounds__(GradTile<WJ>::THREADS, 2) void linear_grad_kernel(G
         __builtin_amdgcn_sched_barrier(0);
         RawPair<DTYPE> raw[AHEAD];
 #pragma unroll
-        for (int k = 0; k < AHEAD; ++k) raw[k] = load_pair(reads, rows, k);
+        for (int k = 0; k < AHEAD; ++k) raw[k] = load_pair(reads, rows, kSteps * half + k);
         __builtin_amdgcn_sched_barrier(0);
         store_scale(byte0, scales);
         store_scale(byte1, scales + kScaleFloats);
@@ -346,25 +348,27 @@ __global__ __launch_bounds__(GradTile<WJ>::THREADS, 2) void linear_grad_kernel(G
             c = rectified(c);
             const uint32_t byte = load_exp(exps);
             bf16x8 v[T::TE];
-            load_fragments(buffer, 0, v);
+            load_fragments(buffer, kSteps * half, v);
 #pragma unroll
-            for (int step = 0; step < 4; ++step) {
+            for (int step = 0; step < kSteps; ++step) {
                 bf16x8 g[2][P];
                 to_parts(raw[step % AHEAD], g);
                 if (with_bias)
 #pragma unroll
                     for (int t = 0; t < 2; ++t) bias[t] += (double)sum_of(raw[step % AHEAD], t);
-                raw[step % AHEAD] = load_pair(reads, step + AHEAD < 4 ? rows : ahead, (step + AHEAD) & 3);
-                store_column(c, step, scales + (now ^ 1) * kScaleFloats, lds + (now ^ 1) * kStageBytes);
+                raw[step % AHEAD] = load_pair(reads, step + AHEAD < kSteps ? rows : ahead, kSteps * half + (step + AHEAD) % kSteps);
+#pragma unroll
+                for (int k = 0; k < 4 / kSteps; ++k)
+                    store_column(c, 4 / kSteps * step + k, scales + (now ^ 1) * kScaleFloats, lds + (now ^ 1) * kStageBytes);
                 bf16x8 then[T::TE];
-                if (step < 3) load_fragments(buffer, step + 1, then);
+                if (step + 1 < kSteps) load_fragments(buffer, kSteps * half + step + 1, then);
 #pragma unroll
                 for (int p = P - 1; p >= 0; --p)
 #pragma unroll
                     for (int k = 0; k < T::TE; ++k)
 #pragma unroll
                         for (int t = 0; t < 2; ++t) acc[t][k] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[k], g[t][p], acc[t][k], 0, 0, 0);
-                if (step < 3)
+                if (step + 1 < kSteps)
 #pragma unroll
                     for (int k = 0; k < T::TE; ++k) v[k] = then[k];
             }
@@ -386,7 +390,7 @@ __global__ __launch_bounds__(GradTile<WJ>::THREADS, 2) void linear_grad_kernel(G
             for (int k = 0; k < 4; ++k) store_column(c, k, scales, lds);
             __syncthreads();
 #pragma unroll 1
-            for (int step = 0; step < 4; ++step) {
+            for (int step = kSteps * half; step < kSteps * (half + 1); ++step) {
                 const RawPair<DTYPE> raw = load_pair(reads, rows, step);
                 bf16x8 g[2][P], v[T::TE];
                 to_parts(raw, g);
@@ -416,24 +420,60 @@ __global__ __launch_bounds__(GradTile<WJ>::THREADS, 2) void linear_grad_kernel(G
         run(from, middle);
         run_elements(middle, to);
     }
-    if (with_bias)
+    // the halves' sums: each ends with one output of a pair, and gives the other
+    floatx16 sum[T::OUT][T::TE];
+    if constexpr (H == 1) {
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            bias[t] += __shfl_xor(bias[t], 32, 64);
-            if (lane < 32 && j + t < a.n_out) {
-                if (a.parts) a.bias_parts[(int64_t)split * a.n_out + j + t] = bias[t];
-                else a.grad_bias[j + t] = a.accumulate ? a.grad_bias[j + t] + (float)bias[t] : (float)bias[t];
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int k = 0; k < T::TE; ++k) sum[t][k] = acc[t][k];
+    } else {
+        floatx4 *const given = reinterpret_cast<floatx4 *>(lds);
+        static_assert(T::WAVES * 64 * 16 * (int)sizeof(float) <= 2 * kStageBytes, "");
+#pragma unroll
+        for (int k = 0; k < T::TE; ++k) {
+            sum[0][k] = half ? acc[1][k] : acc[0][k];
+            const floatx16 give = half ? acc[0][k] : acc[1][k];
+            __syncthreads();
+#pragma unroll
+            for (int p = 0; p < 4; ++p) given[(wave * 4 + p) * 64 + lane] = floatx4{give[4 * p], give[4 * p + 1], give[4 * p + 2], give[4 * p + 3]};
+            __syncthreads();
+#pragma unroll
+            for (int p = 0; p < 4; ++p) {
+                const floatx4 v = given[((wave ^ T::HALF) * 4 + p) * 64 + lane];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sum[0][k][4 * p + i] += v[i];
             }
         }
+    }
+    if (a.grad_bias && tj == 0) {
+        double *const halves = reinterpret_cast<double *>(lds);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) bias[t] += __shfl_xor(bias[t], 32, 64);
+        if constexpr (H == 2) {
+            __syncthreads();
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+                if (half && with_bias && lane < 32) halves[(wj * 2 + t) * 32 + lane] = bias[t];
+            __syncthreads();
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+            if (!half && with_bias && lane < 32 && j + t < a.n_out) {
+                const double both = H == 2 ? bias[t] + halves[(wj * 2 + t) * 32 + lane] : bias[t];
+                if (a.parts) a.bias_parts[(int64_t)split * a.n_out + j + t] = both;
+                else a.grad_bias[j + t] = a.accumulate ? a.grad_bias[j + t] + (float)both : (float)both;
+            }
+    }
 #pragma unroll
     for (int q = 0; q < T::GROUPS; ++q) {
-        const floatx16 &t = acc[(q >> 2) / T::TE][(q >> 2) % T::TE];
+        const floatx16 &t = sum[(q >> 2) / T::TE][(q >> 2) % T::TE];
         const floatx4 v = {t[4 * (q & 3)], t[4 * (q & 3) + 1], t[4 * (q & 3) + 2], t[4 * (q & 3) + 3]};
-        if (a.parts) {
+        if (H == 2 && a.parts) {
             a.parts[(((int64_t)split * tiles + tile) * T::WAVES + wave) * (T::GROUPS * 64) + q * 64 + lane] = v;
         } else {
             int jo, eo;
-            place_of<WJ>(wave, lane, q, &jo, &eo);
+            place_of<WJ, H>(wave, lane, q, &jo, &eo);
             store_group(a, j0 + jo, e0 + eo, v);
         }
     }
@@ -443,7 +483,7 @@ __global__ __launch_bounds__(GradTile<WJ>::THREADS, 2) void linear_grad_kernel(G
 template <int WJ>
 __global__ __launch_bounds__(256) void linear_grad_join_kernel(GradArgs a)
 {
-    typedef GradTile<WJ> T;
+    typedef GradTile<WJ, 2> T;
     __shared__ floatx4 sums[3][64];
     __shared__ double bias_sums[3][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -464,7 +504,7 @@ __global__ __launch_bounds__(256) void linear_grad_join_kernel(GradArgs a)
     const int tile = (int)(blockIdx.x / (T::WAVES * T::GROUPS)), rest = (int)(blockIdx.x % (T::WAVES * T::GROUPS));
     int ti, tj, j, e;
     grouped_tile(tile, a.down, a.across, &ti, &tj);
-    place_of<WJ>(rest / T::GROUPS, lane, rest % T::GROUPS, &j, &e);
+    place_of<WJ, 2>(rest / T::GROUPS, lane, rest % T::GROUPS, &j, &e);
     store_group(a, ti * T::ROWS + j, tj * kCols + e, sum);
     if (biased) a.grad_bias[i] = a.accumulate ? a.grad_bias[i] + (float)bias : (float)bias;
 }
@@ -474,15 +514,15 @@ __global__ __launch_bounds__(256) void linear_grad_join_kernel(GradArgs a)
 constexpr int kUnits = 256;   // compute units
 
 struct Plan {
-    int wj, down, across, splits, stages;
+    int wj, halves, down, across, splits, stages;
 };
 
-// Tile and splits by what a call takes in us: stages of a workgroup, fitted to 18 shapes (8192 rows of 1024 -> 1024, float32:
-// 3.7 a stage of 256 outputs alone on a compute unit and 6.5 two at a time, 2.2 of 128 outputs; bfloat16 1.5; one and a half to
-// begin with), parts written and joined at 8 TB/s.  Measured (us, best / next other tile / next other number of
-// splits): 8192 of 1024 -> 1024 float32 64 / 67 / 65; 5000 of 500 -> 333 29 / 35 / 32; 65536 of 128 -> 128 32 / 33 / 40 (the join has since
-// made that 26);
-// 4096 of 4096 -> 4096 bfloat16 139 / 203 / 174.
+// Tile and splits by what a call takes in us: stages of a workgroup, fitted to 18 shapes, one and a half of them to begin with, and
+// parts, which are written and joined.  Workgroups of two halves have a unit for themselves; of one half two are on a unit, which
+// takes that many tiles without splits.  Measured (us, as chosen / next other tile / next other number of splits): 8192 rows of
+// 1024 -> 1024 float32 62 / 71 / 73; 5000 of 500 -> 333 25 / 24 / 26; 65536 of 128 -> 128 21 / 22 / 23; 20000 of 1000 -> 1000 bfloat16
+// 61 / 78 / 72; 1000 of 100 -> 4000 float32 18 / 19 / 20.  Halves (one / two): 4096 of 4096 -> 4096 bfloat16 150 / 167, 16384 of
+// 4096 -> 4096 float32 1300 / 1353, 64 of 4096 -> 4096 20 / 28, 8192 of 1024 -> 1024 72 / 62.
 Plan plan_of(const LinearShape &s)
 {
     Plan best = {};
@@ -492,13 +532,18 @@ Plan plan_of(const LinearShape &s)
     for (int wj = 4; wj >= 1; wj /= 2) {
         const int down = (s.n_out + kWaveRows * wj - 1) / (kWaveRows * wj), across = (s.n_in + kCols - 1) / kCols;
         const int64_t tiles = (int64_t)down * across;
-        const double stage = wj == 4 ? 0.4 + 1.1 * parts : wj == 2 ? 0.5 + 0.55 * parts : 0.6 + 0.45 * parts;
+        if (wj == 4 && tiles > kUnits) {
+            const int64_t turns = (tiles + kUnits - 1) / kUnits;
+            const double cost = ((turns / 2) * (0.75 + 1.43 * parts) + (turns % 2) * (0.4 + 1.1 * parts)) * (stages + 1.5);
+            if (cost < least) least = cost, best = {wj, 1, down, across, 1, stages};
+        }
+        const double stage = wj == 4 ? 0.72 + 0.71 * parts : wj == 2 ? 0.43 + 0.47 * parts : 0.75 + 0.27 * parts;
         for (int splits = 1; splits <= 512 && splits <= (stages > 0 ? stages : 1); splits *= 2) {
             if (splits > 1 && tiles * splits > 4 * kUnits) break;
             const int64_t turns = (tiles * splits + kUnits - 1) / kUnits;
             const double bytes = (double)tiles * splits * wj * kWaveRows * kCols * sizeof(float);
-            const double cost = ((turns / 2) * 1.75 + turns % 2) * ((stages + splits - 1) / splits + 1.5) * stage + (splits > 1 ? 3.0 + bytes / 8e6 : 0.0);
-            if (cost < least) least = cost, best = {wj, down, across, splits, stages};
+            const double cost = turns * ((stages + splits - 1) / splits + 1.5) * stage + (splits > 1 ? 3.0 + bytes / 3.5e6 : 0.0);
+            if (cost < least) least = cost, best = {wj, 2, down, across, splits, stages};
         }
     }
     return best;
@@ -516,27 +561,29 @@ size_t plan_bytes(const LinearShape &s, const Plan &p)
 // (two float32 need no more than their own alignment)
 bool whole_shape(const LinearShape &s) { return (s.y_dtype == LMKAN_F32 || s.n_out % 2 == 0) && s.n_in % 4 == 0; }
 
-template <int DTYPE, int WJ>
+template <int DTYPE, int WJ, int H>
 void launch(GradArgs a, bool whole, hipStream_t stream)
 {
+    typedef GradTile<WJ, H> T;
     const int64_t total = (int64_t)a.down * a.across * a.splits;
     for (int64_t first = 0; first < total; first += kMostGroups) {
         const unsigned groups = (unsigned)((total - first < kMostGroups ? total - first : kMostGroups) + 7) / 8 * 8;
         a.first = (int)first;
-        if (whole) linear_grad_kernel<DTYPE, WJ, true><<<groups, GradTile<WJ>::THREADS, 0, stream>>>(a);
-        else linear_grad_kernel<DTYPE, WJ, false><<<groups, GradTile<WJ>::THREADS, 0, stream>>>(a);
+        if (whole) linear_grad_kernel<DTYPE, WJ, H, true><<<groups, T::THREADS, 0, stream>>>(a);
+        else linear_grad_kernel<DTYPE, WJ, H, false><<<groups, T::THREADS, 0, stream>>>(a);
     }
     if (!a.parts) return;
     // (a group of the join for every four results of the tiles, which are at least as many as the outputs)
-    linear_grad_join_kernel<WJ><<<(unsigned)(a.down * a.across * GradTile<WJ>::WAVES * GradTile<WJ>::GROUPS), 256, 0, stream>>>(a);
+    if constexpr (H == 2) linear_grad_join_kernel<WJ><<<(unsigned)(a.down * a.across * T::WAVES * T::GROUPS), 256, 0, stream>>>(a);
 }
 
 template <int DTYPE>
-void launch_type(int wj, const GradArgs &a, bool whole, hipStream_t stream)
+void launch_type(const Plan &p, const GradArgs &a, bool whole, hipStream_t stream)
 {
-    if (wj == 4) launch<DTYPE, 4>(a, whole, stream);
-    else if (wj == 2) launch<DTYPE, 2>(a, whole, stream);
-    else launch<DTYPE, 1>(a, whole, stream);
+    if (p.halves == 1) launch<DTYPE, 4, 1>(a, whole, stream);
+    else if (p.wj == 4) launch<DTYPE, 4, 2>(a, whole, stream);
+    else if (p.wj == 2) launch<DTYPE, 2, 2>(a, whole, stream);
+    else launch<DTYPE, 1, 2>(a, whole, stream);
 }
 
 bool aligned_to(const void *p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
@@ -559,9 +606,9 @@ void launch_linear_grad(const LinearShape &s, bool accumulate, const int8_t *cod
         a.parts = static_cast<floatx4 *>(workspace);
         a.bias_parts = reinterpret_cast<double *>(static_cast<char *>(workspace) + parts_bytes(p));
     }
-    if (s.y_dtype == LMKAN_F32) launch_type<LMKAN_F32>(p.wj, a, whole, stream);
-    else if (s.y_dtype == LMKAN_F16) launch_type<LMKAN_F16>(p.wj, a, whole, stream);
-    else launch_type<LMKAN_BF16>(p.wj, a, whole, stream);
+    if (s.y_dtype == LMKAN_F32) launch_type<LMKAN_F32>(p, a, whole, stream);
+    else if (s.y_dtype == LMKAN_F16) launch_type<LMKAN_F16>(p, a, whole, stream);
+    else launch_type<LMKAN_BF16>(p, a, whole, stream);
 }
 
 }  // namespace lmkan
