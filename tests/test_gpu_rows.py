@@ -384,6 +384,15 @@ def test_linear_grad_matches_float64(dev, shape, dtype):
     _check_grad(dev, *shape, dtype, relu=False, bias=False, seed=120)
 
 
+@pytest.mark.parametrize("shape", [(70, 2048, 4352), (130, 2049, 4101), (1, 4096, 4160)], ids=str)
+@pytest.mark.parametrize("dtype", TYPES)
+def test_linear_grad_of_more_tiles_than_units(dev, shape, dtype):
+    desc, codes, exps, gy, gw, gb = _check_grad(dev, *shape, dtype, relu=True, bias=True, seed=125)
+    base = torch.ones_like(gw), torch.ones_like(gb)
+    pkg.lmkan_linear_grad(desc, codes, exps, gy, grad_weight=base[0], grad_bias=base[1], accumulate=True)
+    assert torch.equal(base[0], 1 + gw) and torch.equal(base[1], 1 + gb)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_products_keep_the_bits_of_the_gradient(dev, dtype):
     """One row: every element is one product, off by 2^-24 for the bits of a float32 gradient that are kept and 2^-24 for
