@@ -3,7 +3,7 @@
 //
 // A value has 7 bits and a power of two: it is exact in bfloat16.  A gradient is cut into parts of 8 bits, three of a float32, two of
 // a float16, which are exact as well, so that 32 x 32 x 16 bfloat16 instructions make exact products and float32 sums: three of
-// them take 3/8 of the time of float32 instructions.  The axis that is summed is the batch, across which neither matrix is
+// them take a third of the time of float32 instructions.  The axis that is summed is the batch, across which neither matrix is
 // contiguous: gradients go from memory to the instruction's operands directly (a lane has two adjacent outputs of eight rows),
 // codes are turned on their way through LDS.  A tile of 64 to 256 outputs and 128 inputs a workgroup; the batch is cut where tiles are
 // few, and a second launch adds the parts.
@@ -217,7 +217,7 @@ __global__ __launch_bounds__((GradTile<WJ, H>::THREADS), H == 1 ? 2 : 1) void li
 {
     typedef GradTile<WJ, H> T;
     constexpr int P = parts_of<DTYPE>();
-    constexpr int kSteps = T::STEPS, AHEAD = kSteps < 2 ? kSteps : 2;   // steps whose gradients are under way
+    constexpr int kSteps = T::STEPS, AHEAD = 2;   // AHEAD: steps whose gradients are under way
     __shared__ __align__(16) char lds[2 * kStageBytes + 2 * kScaleFloats * (int)sizeof(float)];
     const int tiles = a.down * a.across, total = tiles * a.splits;
     const int id = a.first + (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);   // (workgroups on one die: adjacent tiles of the same rows)
