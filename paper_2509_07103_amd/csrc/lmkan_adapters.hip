@@ -516,8 +516,8 @@ __device__ __forceinline__ void cut_eight(const float (&v)[8], bf16x8 (&to)[N])
 
 // y[place][j] += scale sum_k B[j][k] low[place][k]: 32 outputs of all places of a tile at a time for a wave, while B and y of
 // the next 32 are on their way.  The results go through LDS to lanes that lie along the outputs.
-// NATIVE: 16-bit adapters, on bfloat16 instructions: low in three parts, B as it is or (float16) in two.  Three or five
-// products of 32 terms take 48 or 80 clocks where float32 instructions take 256.
+// NATIVE: 16-bit adapters, on bfloat16 instructions: low in three parts, B as it is or (float16) in two.  Three or six
+// products of 32 terms take 48 or 96 clocks where float32 instructions take 256.
 template <bool W, bool Y, bool ALIGNED, bool NATIVE, int RT>
 __global__ __launch_bounds__(256) void adapters_up_kernel(AdapterArgs a)
 {
@@ -625,10 +625,10 @@ __global__ __launch_bounds__(256) void adapters_up_kernel(AdapterArgs a)
                         } else {
                             f[0] = __builtin_bit_cast(bf16x8, T < 32 && part > 1 ? intx4{0, 0, 0, 0} : w);
                         }
-                        // small products first; the last part of low times the second of B is 2^-24 of the whole and left out
+                        // small products first, all of them: the last part of low times the second of B is up to 2^-22 of the whole
 #pragma unroll
                         for (int q = 2; q >= 0; --q) {
-                            if (w_half && q < 2)
+                            if (w_half)
 #pragma unroll
                                 for (int i = 0; i < kRowTiles; ++i) acc[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[1], parts[i][at][q], acc[t][i], 0, 0, 0);
 #pragma unroll
