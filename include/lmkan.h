@@ -594,7 +594,8 @@ lmkan_status lmkan_layer_norm_backward(const lmkan_norm *desc, int64_t rows, con
  *                    overwritten, or added to with LMKAN_LINEAR_ACCUMULATE in the descriptor's flags
  *   workspace_dev / workspace_bytes: at least lmkan_linear_grad_workspace_bytes(desc, batch)
  *                    bytes, 256-byte aligned (NULL allowed when 0)
- * Products keep 24 bits of grad_y (all of a 16-bit one) and all of the values, and are summed in
+ * Products keep 24 bits of grad_y, those of them that stand for 2^-133 or more (all 24 from 2^-110 on;
+ * all of a 16-bit one), and all of the values, and are summed in
  * float32 in an order that the sizes and the tensors' alignment fix: the results repeat bit for bit.
  * Factors below 2^-126 may count as zeros.  An infinite grad_y makes what it enters infinite or NaN.
  */
@@ -631,7 +632,9 @@ typedef struct lmkan_adapters {
  *   workspace_dev / workspace_bytes: at least lmkan_adapters_workspace_bytes(desc, batch) bytes,
  *              256-byte aligned (NULL allowed when 0)
  * Products and sums are float32 (products of 16-bit factors are exact), y is rounded to its type
- * once.  The results repeat bit for bit.  Float32 and bfloat16 factors below 2^-126 may count as zeros;
+ * once.  The results repeat bit for bit.  Float32 and bfloat16 factors below 2^-126 may count as zeros,
+ * and so may, with 16-bit adapters, the bits of A f(x) that stand for less than 2^-133; sums that a
+ * float16 factor below 2^-14 enters may be rounded as if it were that large;
  * an infinite factor makes what it enters infinite or NaN.
  */
 size_t lmkan_adapters_workspace_bytes(const lmkan_adapters *desc, int64_t batch);
