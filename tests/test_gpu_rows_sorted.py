@@ -117,3 +117,119 @@ def test_float16_numbers_below_the_smallest_normal_one_count_in_many_rows(dev, s
         _within(got[r::3], want, (128 / 4 + 16 / 4 + 64) * U * size + 2 * U * want.abs(), "y")
         # (a factor of ten leading zeros: u 2^10 of its product, twice that where a sum cuts)
         assert float((got[r::3].cpu().double() - want).norm() / want.norm()) < 2.0 ** -13
+
+
+def _check_sorted(dev, data, relu, scaled, w="f32", x_type="f32", y_type="f32", shift=None):
+    """Against float64 within the root of the sum of squares; `shift`: every tensor starts that many elements into a buffer, of
+    which nothing around the result may change."""
+    x, index, a, b, y, scale = data
+    count, rank, n_in = a.shape
+    desc = pkg.AdapterDesc(count, rank, n_in, b.shape[1], dtype=CODE[w], x_dtype=CODE[x_type], y_dtype=CODE[y_type], relu=relu)
+    _sorted(desc, x.shape[0])
+    put = (lambda t: t.to(dev)) if shift is None else (lambda t: _guarded(t, dev, shift)[0])
+    got, whole = (y.clone().to(dev), lambda: True) if shift is None else _guarded(y, dev, shift)
+    pkg.lmkan_adapters_add(desc, put(x), put(index), put(a), put(b), got, scale=put(scale) if scaled else None)
+    xd = x.double().clamp(min=0.0) if relu else x.double()
+    want, size = y.double().clone(), torch.zeros(y.shape, dtype=torch.float64)
+    has = (index >= 0) & (index < count)
+    for r in index[has].unique().tolist():
+        n = torch.nonzero(index == r)[:, 0]
+        s = float(scale[r]) if scaled else 1.0
+        ad, bd = a[r].double(), b[r].double()
+        want[n] += s * ((xd[n] @ ad.T) @ bd.T)
+        size[n] = s * ((xd[n].square() @ ad.square().T) @ bd.square().T).sqrt()
+    assert torch.equal(got[~has].cpu(), y[~has])                       # bit for bit
+    _within(got[has], want[has], ((n_in / 4 + rank / 4 + 64) * U * size + 2 * U * want.abs() + _out(want, y_type))[has], "y")
+    assert whole()
+    return desc, got.cpu()
+
+
+@pytest.mark.parametrize("types", ["f32 f32 f32", "bf16 bf16 bf16", "f16 f16 f32", "bf16 f32 f32", "f32 f16 bf16"])
+@pytest.mark.parametrize("rank", [1, 3, 6, 8, 16, 17, 20, 32, 33, 48, 64])
+def test_small_ranks_of_many_rows(dev, rank, types):
+    w, x, y = types.split()
+    for n_in, n_out, relu in [(256, 160, True), (333, 77, False)]:
+        _check_sorted(dev, _adapters(1500, n_in, n_out, rank, 3, w=w, x=x, y=y, seed=320), relu, True, w, x, y)
+
+
+@pytest.mark.parametrize("kind", ["one", "none", "first", "last", "waves", "runs", "turns", "beyond"])
+@pytest.mark.parametrize("batch", [3000, 40001])
+def test_arrangements_of_many_requests(dev, kind, batch):
+    """Rows of one adapter, of none, runs that fill waves of 64 and runs that do not, indices far out of range; 40001 rows are
+    sorted in two parts."""
+    at, none = torch.arange(batch), torch.full((batch,), -1)
+    index = {"one": torch.full((batch,), 4), "none": none, "first": torch.where(at == 0, 0, none), "last": torch.where(at == batch - 1, 8, none),
+             "waves": at // 256 % 11 - 1, "runs": at // 77 % 9, "turns": at % 9, "beyond": torch.tensor([-2 ** 31, 2 ** 31 - 1, 9, 8, 0])[at % 5]}[kind]
+    _check_sorted(dev, _adapters(batch, 80, 50, 10, 9, index=index, seed=325), False, True)
+
+
+@pytest.mark.parametrize("count", [1, 2, 1023, 1025, 8191, 8192])
+def test_many_adapters_of_many_rows(dev, count):
+    index = (torch.arange(2500) * 7919) % (count + 1) - int(count > 1)
+    index[::5] = count - 1
+    _check_sorted(dev, _adapters(2500, 24, 20, 4, count, index=index, seed=330), True, False)
+
+
+@pytest.mark.parametrize("types", ["f32 f32 f32", "bf16 bf16 bf16", "f16 f16 f32", "bf16 f32 f16", "f32 f16 bf16"])
+@pytest.mark.parametrize("shape", [(128, 96, 16), (131, 45, 5), (333, 77, 130)], ids=str)
+@pytest.mark.parametrize("shift", [1, 3, 8])
+def test_many_rows_anywhere_and_nothing_written_beyond(dev, shape, types, shift):
+    w, x, y = types.split()
+    n_in, n_out, rank = shape
+    _check_sorted(dev, _adapters(1100, n_in, n_out, rank, 5, w=w, x=x, y=y, seed=335), True, True, w, x, y, shift=shift)
+
+
+@pytest.mark.parametrize("types", ["f32 f32 f32", "bf16 bf16 bf16", "f16 f16 f32", "f32 f16 bf16"])
+@pytest.mark.parametrize("shape", [(128, 64, 24), (131, 65, 23)], ids=str)
+def test_values_that_are_not_finite_stay_in_their_rows_of_a_tile(dev, shape, types):
+    w, x_type, y_type = types.split()
+    n_in, n_out, rank = shape
+    rows = 1500
+    data = _adapters(rows, n_in, n_out, rank, 3, w=w, x=x_type, y=y_type, seed=340, index=torch.arange(rows) % 3)
+    x, index, a, b, y, scale = data
+    desc, clean = _check_sorted(dev, data, False, True, w, x_type, y_type)
+    x, a, b, y = x.clone(), a.clone(), b.clone(), y.clone()
+    x[7, 5] = float("nan")
+    x[9, n_in - 1] = float("-inf")
+    a[2, 0, 0] = float("inf")
+    b[1, n_out - 1, rank - 1] = float("inf")
+    y[12, 3] = float("nan")
+    got = pkg.lmkan_adapters_add(desc, x.to(dev), index.to(dev), a.to(dev), b.to(dev), y.to(dev), scale=scale.to(dev)).cpu()
+    want = torch.zeros(rows, n_out, dtype=torch.bool)
+    want[7] = want[9] = want[2::3] = True
+    want[1::3, n_out - 1] = want[12, 3] = True
+    assert torch.equal(~torch.isfinite(got), want)
+    assert torch.equal(got[~want], clean[~want])
+
+
+def test_many_rows_twice_in_a_workspace_and_in_a_graph(dev):
+    """The same workspace for two calls one after the other, eager and replayed, gives what workspaces of their own give."""
+    first, second = _adapters(1500, 96, 64, 12, 4, seed=350), _adapters(2900, 96, 64, 12, 4, seed=360)
+    desc = pkg.AdapterDesc(4, 12, 96, 64)
+    ws = torch.empty(max(pkg.lmkan_adapters_workspace_bytes(desc, n) for n in (1500, 2900)), dtype=torch.uint8, device=dev)
+    data = [[t.to(dev) for t in d] for d in (first, second)]
+    want = [pkg.lmkan_adapters_add(desc, x, i, a, b, y.clone(), scale=s) for x, i, a, b, y, s in data]
+    out = [torch.empty_like(t) for t in want]
+
+    def both():
+        for (x, i, a, b, y, s), to in zip(data, out):
+            to.copy_(y)
+            pkg.lmkan_adapters_add(desc, x, i, a, b, to, scale=s, workspace=ws)
+    both()
+    assert all(torch.equal(o, t) for o, t in zip(out, want))
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        both()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both()
+    for _ in range(4):
+        ws.fill_(0x5a)
+        for o in out:
+            o.fill_(7)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, t) for o, t in zip(out, want))
