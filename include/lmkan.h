@@ -20,6 +20,8 @@
  *     written when a status other than LMKAN_OK or LMKAN_ERR_HIP comes back.
  *   - batch == 0 is legal: nothing is read, and only the backward calls write
  *     (an overwritten gradient that is summed over the batch becomes all zeros).
+ *   - Workspace sizes are those of the batch that is asked for: another one, a smaller
+ *     one too, may need more, unless the comment of the call says otherwise.
  *   - Alignment: every tensor its element size.  Faster kernels are chosen at
  *     run time when pointers and widths allow wider accesses (8 bytes for x_dev
  *     and grad_x_dev, 16 bytes for the other tensors).
@@ -630,7 +632,7 @@ typedef struct lmkan_adapters {
  *   y_dev      [batch][n_out] in y_dtype, added to in place (lmkan_linear_i8 has written the shared
  *              projection there); it must not overlap the inputs
  *   workspace_dev / workspace_bytes: at least lmkan_adapters_workspace_bytes(desc, batch) bytes,
- *              256-byte aligned (NULL allowed when 0)
+ *              256-byte aligned (NULL allowed when 0).  The size covers every smaller batch too
  * Products and sums are float32 (products of 16-bit factors are exact), y is rounded to its type
  * once.  The results repeat bit for bit.  Float32 and bfloat16 factors below 2^-126 may count as zeros,
  * and so may, with 16-bit adapters, the bits of A f(x) that stand for less than 2^-133; sums that a

@@ -714,11 +714,12 @@ int rank_tiles(int rank) { return rank <= 16 ? 1 : rank <= 32 ? 2 : rank <= 64 ?
 // Pieces of the inputs: as many as keep two workgroups on a compute unit, of 256 inputs at least; of the outputs (below) for four.
 // Measured (us, for half as many / as they are / twice as many): 8192 rows of 1024 -> 1024, rank 32, float32 41 / 39 / 44; bfloat16
 // 16384 of 4096 -> 1024, rank 64, 79 / 76 / 67; 4096 of 4096 -> 4096, rank 128, 66 / 68 / 87.
+constexpr int kMostSplits = 32;
 void split_inputs(const AdapterShape &s, int rows, int *splits, int *each)
 {
     const int tiles = (rows + kTileRows - 1) / kTileRows;
     int n = 1;
-    while (n < 32 && tiles * n < 2 * kUnits && s.n_in > 256 * n) n *= 2;
+    while (n < kMostSplits && tiles * n < 2 * kUnits && s.n_in > 256 * n) n *= 2;
     *each = ((s.n_in + n - 1) / n + 255) / 256 * 256;
     *splits = (s.n_in + *each - 1) / *each;
 }
@@ -764,6 +765,20 @@ void with_rank(int rank, F &&f)
 }  // namespace
 
 size_t adapters_workspace_bytes(const AdapterShape &s) { return few_rows(s) ? 0 : layout_of(s).total; }
+
+// (fewer tiles have more pieces of the inputs: of each number of pieces the batch with the most rows)
+size_t adapters_workspace_most(const AdapterShape &s)
+{
+    size_t most = adapters_workspace_bytes(s);
+    for (int n = 2; n <= kMostSplits; n *= 2) {
+        AdapterShape smaller = s;
+        const int64_t rows = (2 * 2 * kUnits - 1) / n * kTileRows;   // tiles n / 2 < 2 kUnits: the last that `split_inputs` cuts in n
+        if (rows < s.batch) smaller.batch = rows;
+        const size_t bytes = adapters_workspace_bytes(smaller);
+        if (bytes > most) most = bytes;
+    }
+    return most;
+}
 
 void launch_adapters(const AdapterShape &s, const void *x, const int32_t *index, const void *a, const void *b, const float *scale, void *y,
                      void *workspace, hipStream_t stream)

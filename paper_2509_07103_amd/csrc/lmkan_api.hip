@@ -971,7 +971,7 @@ lmkan_status lmkan_linear_grad(const lmkan_linear *desc, int64_t batch, const in
 size_t lmkan_adapters_workspace_bytes(const lmkan_adapters *desc, int64_t batch)
 {
     AdapterShape s;
-    return check_adapters(desc, batch, &s) == LMKAN_OK && batch > 0 ? adapters_workspace_bytes(s) : 0;
+    return check_adapters(desc, batch, &s) == LMKAN_OK && batch > 0 ? adapters_workspace_most(s) : 0;
 }
 
 lmkan_status lmkan_adapters_add(const lmkan_adapters *desc, int64_t batch, const void *x_dev, const int32_t *index_dev,

@@ -346,7 +346,8 @@ struct AdapterShape {
     int dtype, x_dtype, y_dtype;
     bool relu;
 };
-size_t adapters_workspace_bytes(const AdapterShape &s);
+size_t adapters_workspace_bytes(const AdapterShape &s);   // of this batch
+size_t adapters_workspace_most(const AdapterShape &s);    // of this and every smaller batch
 void launch_adapters(const AdapterShape &s, const void *x, const int32_t *index, const void *a, const void *b, const float *scale, void *y,
                      void *workspace, hipStream_t stream);
 
