@@ -595,7 +595,7 @@ lmkan_status lmkan_layer_norm_backward(const lmkan_norm *desc, int64_t rows, con
  *   grad_weight_dev  [n_out][n_in] float32, grad_bias_dev [n_out] float32 or NULL; both are
  *                    overwritten, or added to with LMKAN_LINEAR_ACCUMULATE in the descriptor's flags
  *   workspace_dev / workspace_bytes: at least lmkan_linear_grad_workspace_bytes(desc, batch)
- *                    bytes, 256-byte aligned (NULL allowed when 0)
+ *                    bytes, 256-byte aligned (NULL allowed when 0).  The size covers every smaller batch too
  * Products keep 24 bits of grad_y, those of them that stand for 2^-133 or more (all 24 from 2^-110 on;
  * all of a 16-bit one), and all of the values, and are summed in
  * float32 in an order that the sizes and the tensors' alignment fix: the results repeat bit for bit.

@@ -942,7 +942,7 @@ lmkan_status lmkan_layer_norm_backward(const lmkan_norm *desc, int64_t rows, con
 size_t lmkan_linear_grad_workspace_bytes(const lmkan_linear *desc, int64_t batch)
 {
     LinearShape s;
-    return check_linear_grad(desc, batch, &s) == LMKAN_OK ? linear_grad_workspace_bytes(s) : 0;
+    return check_linear_grad(desc, batch, &s) == LMKAN_OK ? linear_grad_workspace_most(s) : 0;
 }
 
 lmkan_status lmkan_linear_grad(const lmkan_linear *desc, int64_t batch, const int8_t *codes_dev, const uint8_t *exps_dev,

@@ -517,35 +517,46 @@ struct Plan {
     int wj, halves, down, across, splits, stages;
 };
 
+// Workgroups that a unit takes one after the other
+int64_t turns_of(int64_t workgroups) { return (workgroups + kUnits - 1) / kUnits; }
+
 // Tile and splits by what a call takes in us: stages of a workgroup, fitted to 18 shapes, one and a half of them to begin with, and
 // parts, which are written and joined.  Workgroups of two halves have a unit for themselves; of one half two are on a unit, which
 // takes that many tiles without splits.  Measured (us, as chosen / next other tile / next other number of splits): 8192 rows of
 // 1024 -> 1024 float32 62 / 71 / 73; 5000 of 500 -> 333 25 / 24 / 26; 65536 of 128 -> 128 21 / 22 / 23; 20000 of 1000 -> 1000 bfloat16
 // 61 / 78 / 72; 1000 of 100 -> 4000 float32 18 / 19 / 20.  Halves (one / two): 4096 of 4096 -> 4096 bfloat16 150 / 167, 16384 of
 // 4096 -> 4096 float32 1300 / 1353, 64 of 4096 -> 4096 20 / 28, 8192 of 1024 -> 1024 72 / 62.
-Plan plan_of(const LinearShape &s)
+// Calls f(plan, cost) with every tile and number of splits that is considered.
+template <class F>
+void candidates(const LinearShape &s, F &&f)
 {
-    Plan best = {};
-    double least = 1e300;
     const int stages = (int)((s.batch + kDepth - 1) / kDepth);
     const int parts = s.y_dtype == LMKAN_F32 ? 3 : s.y_dtype == LMKAN_F16 ? 2 : 1;
     for (int wj = 4; wj >= 1; wj /= 2) {
         const int down = (s.n_out + kWaveRows * wj - 1) / (kWaveRows * wj), across = (s.n_in + kCols - 1) / kCols;
         const int64_t tiles = (int64_t)down * across;
         if (wj == 4 && tiles > kUnits) {
-            const int64_t turns = (tiles + kUnits - 1) / kUnits;
+            const int64_t turns = turns_of(tiles);
             const double cost = ((turns / 2) * (0.75 + 1.43 * parts) + (turns % 2) * (0.4 + 1.1 * parts)) * (stages + 1.5);
-            if (cost < least) least = cost, best = {wj, 1, down, across, 1, stages};
+            f(Plan{wj, 1, down, across, 1, stages}, cost);
         }
         const double stage = wj == 4 ? 0.72 + 0.71 * parts : wj == 2 ? 0.43 + 0.47 * parts : 0.75 + 0.27 * parts;
         for (int splits = 1; splits <= 512 && splits <= (stages > 0 ? stages : 1); splits *= 2) {
             if (splits > 1 && tiles * splits > 4 * kUnits) break;
-            const int64_t turns = (tiles * splits + kUnits - 1) / kUnits;
             const double bytes = (double)tiles * splits * wj * kWaveRows * kCols * sizeof(float);
-            const double cost = turns * ((stages + splits - 1) / splits + 1.5) * stage + (splits > 1 ? 3.0 + bytes / 3.5e6 : 0.0);
-            if (cost < least) least = cost, best = {wj, 2, down, across, splits, stages};
+            const double cost = turns_of(tiles * splits) * ((stages + splits - 1) / splits + 1.5) * stage + (splits > 1 ? 3.0 + bytes / 3.5e6 : 0.0);
+            f(Plan{wj, 2, down, across, splits, stages}, cost);
         }
     }
+}
+
+Plan plan_of(const LinearShape &s)
+{
+    Plan best = {};
+    double least = 1e300;
+    candidates(s, [&](const Plan &p, double cost) {
+        if (cost < least) least = cost, best = p;
+    });
     return best;
 }
 
@@ -590,9 +601,22 @@ bool aligned_to(const void *p, size_t a) { return reinterpret_cast<uintptr_t>(p)
 
 }  // namespace
 
-size_t linear_grad_workspace_bytes(const LinearShape &s)
+size_t linear_grad_workspace_bytes(const LinearShape &s) { return plan_bytes(s, plan_of(s)); }
+
+// The most that this and any smaller batch needs.  A smaller one considers no plan that this one does not; of those that cut the
+// batch none is taken that has more splits than another of its tile but no fewer turns a split (s = m s' splits with
+// turns(s) >= m turns(s') take ceil(n / s) turns(s) >= ceil(n / s') turns(s') for any n stages, and have more parts).
+size_t linear_grad_workspace_most(const LinearShape &s)
 {
-    return plan_bytes(s, plan_of(s));
+    size_t most = 0;
+    candidates(s, [&](const Plan &p, double) {
+        const int64_t tiles = (int64_t)p.down * p.across;
+        for (int fewer = 1; fewer < p.splits; fewer *= 2)
+            if (turns_of(tiles * p.splits) >= p.splits / fewer * turns_of(tiles * fewer)) return;
+        const size_t bytes = plan_bytes(s, p);
+        if (bytes > most) most = bytes;
+    });
+    return most;
 }
 
 void launch_linear_grad(const LinearShape &s, bool accumulate, const int8_t *codes, const uint8_t *exps, const void *grad_y,

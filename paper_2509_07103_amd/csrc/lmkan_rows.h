@@ -336,7 +336,8 @@ size_t layer_norm_backward_workspace_bytes(const NormShape &s);
 void launch_layer_norm_backward(const NormShape &s, const NormBackwardArgs &a, void *workspace, hipStream_t stream);
 
 // y_dtype: of grad_y
-size_t linear_grad_workspace_bytes(const LinearShape &s);
+size_t linear_grad_workspace_bytes(const LinearShape &s);   // of this batch
+size_t linear_grad_workspace_most(const LinearShape &s);    // of this and every smaller batch
 void launch_linear_grad(const LinearShape &s, bool accumulate, const int8_t *codes, const uint8_t *exps, const void *grad_y,
                         float *grad_weight, float *grad_bias, void *workspace, hipStream_t stream);
 

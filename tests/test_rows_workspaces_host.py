@@ -29,3 +29,19 @@ def test_adapters(shape):
         desc = pkg.AdapterDesc(*shape, dtype=dtype)
         _never_shrinks(lambda n: pkg.lmkan_adapters_workspace_bytes(desc, n), _batches(1))
     assert pkg.lmkan_adapters_workspace_bytes(desc, 0) == 0
+
+
+@pytest.mark.parametrize("shape", [(500, 333), (4096, 1024), (4096, 333), (1024, 1024), (64, 10), (1, 1), (1000, 1000), (2048, 2048), (4096, 4096),
+                                   (130, 4000), (8000, 3000)], ids=str)
+@pytest.mark.parametrize("y_dtype", [pkg.LMKAN_F32, pkg.LMKAN_F16, pkg.LMKAN_BF16])
+def test_linear_gradient(shape, y_dtype):
+    desc = pkg.LinearDesc(*shape, y_dtype=y_dtype)
+    _never_shrinks(lambda n: pkg.lmkan_linear_grad_workspace_bytes(desc, n), _batches(2))
+    # never more than the parts of four workgroups a unit, 256 x 128 float32 each, and their biases
+    assert pkg.lmkan_linear_grad_workspace_bytes(desc, 70000) <= 1024 * 256 * 128 * 4 + 512 * shape[1] * 8 + 512
+
+
+def test_norm_gradients():
+    for cols in (1, 333, 1024, 20011):
+        desc = pkg.NormDesc(cols)
+        _never_shrinks(lambda n: pkg.lmkan_layer_norm_backward_workspace_bytes(desc, n), range(0, 3000))
