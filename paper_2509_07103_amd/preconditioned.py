@@ -104,8 +104,16 @@ class NormalisedLayer(PreconditionedLayer):
             lmkan_adapters_add(desc, z, index, a, b, y, scale=scale)
         return y
 
-    def answer_in_float(self, x: torch.Tensor) -> torch.Tensor:
-        return self.forward(x)[0]
+    def answer_in_float(self, x: torch.Tensor, adapters=None, index: torch.Tensor | None = None) -> torch.Tensor:
+        y = self.forward(x)[0]
+        if adapters is not None:
+            desc, a, b, scale = adapters
+            z = torch.relu(lmkan_layer_norm(self.norm, x)[0])
+            for r in range(desc.count):
+                rows = torch.nonzero(index == r)[:, 0]
+                add = (z[rows] @ a[r].t()) @ b[r].t()
+                y[rows] += add if scale is None else scale[r] * add
+        return y
 
 
 def random_adapters(count: int, rank: int, n_in: int, n_out: int, device, seed: int = 2):
@@ -118,7 +126,8 @@ def random_adapters(count: int, rank: int, n_in: int, n_out: int, device, seed: 
 
 def run(steps: int = 60, batch: int = 2048, n_in: int = 64, n_out: int = 64, grid: int = 9, device="cuda:0",
         normalised: bool = False):
-    """Trains on a fixed random function; returns (losses, relative difference of the 8-bit answer)."""
+    """Trains on a fixed random function; returns (losses, relative difference of the 8-bit answer).  A normalised layer
+    answers requests with adapters, of which every ninth row has none."""
     g = torch.Generator(device="cpu").manual_seed(1)
     mix = (torch.randn((n_in, n_out), generator=g) / n_in ** 0.5).to(device)
     model = (NormalisedLayer if normalised else PreconditionedLayer)(n_in, n_out, grid, 0.3, device)
@@ -129,8 +138,11 @@ def run(steps: int = 60, batch: int = 2048, n_in: int = 64, n_out: int = 64, gri
         losses.append(float(model.train_step(x, torch.tanh(x @ mix), muon)))
     model.freeze()
     x = torch.randn((batch, n_in), generator=g).to(device)
-    want = model.answer_in_float(x)
-    return losses, float((model.answer(x) - want).norm() / want.norm())
+    requests = ()
+    if normalised:
+        requests = random_adapters(8, 8, n_in, n_out, device), (torch.arange(batch, device=device) % 9 - 1).int()
+    want = model.answer_in_float(x, *requests)
+    return losses, float((model.answer(x, *requests) - want).norm() / want.norm())
 
 
 def main() -> None:

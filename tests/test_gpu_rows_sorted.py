@@ -233,3 +233,23 @@ def test_many_rows_twice_in_a_workspace_and_in_a_graph(dev):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(o, t) for o, t in zip(out, want))
+
+
+def test_the_example_answers_with_adapters(dev, monkeypatch):
+    """The command's run of a normalised layer goes through the operators that the package's description names, on many rows,
+    and its answers in 8 bits are those in float32 but for the rounding of rows and weights."""
+    from paper_2509_07103_amd import preconditioned
+    names = ["lmkan_layer_norm", "lmkan_layer_norm_backward", "lmkan_restore_rows", "lmkan_linear_grad", "lmkan_linear_i8", "lmkan_adapters_add"]
+    calls = []
+
+    def spy(name, call):
+        def recorded(*args, **kw):
+            calls.append(name)
+            return call(*args, **kw)
+        return recorded
+    for name in names:
+        monkeypatch.setattr(preconditioned, name, spy(name, getattr(preconditioned, name)))
+    losses, off = preconditioned.run(2, 1100, 32, 24, 7, normalised=True)
+    assert len(losses) == 2 and set(calls) == set(names)
+    # codes are off by half a step of 1/127 of the largest in a row, of which there are two factors
+    assert off < 0.05
