@@ -492,7 +492,8 @@ lmkan_status lmkan_linear_i8(const lmkan_linear *desc, int64_t batch, const void
 
 /*
  * A normalised layer, z = LayerNorm(x), y = gamma lmKAN(z) + Linear(ReLU(z)): the norm in
- * front of the layer, whose grid is made for rows of mean 0 and variance 1, activations
+ * front of the layer (the grid's cells are laid out for inputs around 0 of variance 1, which
+ * a norm of rows gives a row as a whole, not each of its columns), activations
  * kept in 8 bits between the passes, the linear term's gradient from them, and the linear
  * term as it answers requests that each have an adapter of their own.
  */
