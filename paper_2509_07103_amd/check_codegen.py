@@ -221,8 +221,13 @@ if __name__ == "__main__":
 # in the others, a spilled main loop is hundreds of bytes).
 NO_SCRATCH = ("forward_slab_kernelIf", "forward_slab_f16_kernel", "backward_input_lane_kernel",
               "backward_input_slab_f16_kernel", "backward_coef_stream_kernel", "backward_fused_kernel",
-              "hessian_reg_kernel", "head_kernel")
+              "hessian_reg_kernel", "head_kernel", "norm_kernelI", "norm_grad_kernelI", "norm_long_", "norm_join_kernel",
+              "checkpoint_kernelI", "restore_kernelI", "linear_grad_", "adapters_")
 MAX_SCRATCH_BYTES = 64
+# Of those the ones that do, and how much: the float32 gradient of the linear term with two workgroups on a unit (pairs at any
+# address, or not), and gradients of the longest norms from a checkpoint at any address.
+KNOWN_SCRATCH = {"linear_grad_kernelILi0ELi4ELi1ELb1E": 24, "linear_grad_kernelILi0ELi4ELi1ELb0E": 44,
+                 "norm_grad_kernelILb1ELin4ELi8ELi512ELb1E": 60}
 
 
 def check_resources(report: str) -> dict[str, int]:
@@ -241,8 +246,12 @@ def check_resources(report: str) -> dict[str, int]:
             scratch[name] = int(m.group(1))
     if not scratch:
         raise RuntimeError("resource check: the compiler's report names no kernel")
-    bad = [f"{k}: {v} bytes of scratch per lane" for k, v in scratch.items()
-           if v > MAX_SCRATCH_BYTES or (v > 0 and any(t in k for t in NO_SCRATCH))]
+    def most(kernel: str) -> int:
+        for name, bytes_ in KNOWN_SCRATCH.items():
+            if name in kernel:
+                return bytes_
+        return 0 if any(t in kernel for t in NO_SCRATCH) else MAX_SCRATCH_BYTES
+    bad = [f"{k}: {v} bytes of scratch per lane, {most(k)} allowed" for k, v in scratch.items() if v > most(k)]
     if bad:
         raise RuntimeError("resource check: kernels spill registers to scratch memory\n  " + "\n  ".join(bad))
     return scratch

@@ -53,7 +53,8 @@ struct GradArgs {
 
 // WJ waves lie along the outputs, 4 / WJ along the inputs: a tile of 64 WJ outputs and 128 inputs.  H = 2: twice as many, and of a
 // stage's four steps of 16 rows each half takes two, so that two waves share a matrix unit, one making parts while the other
-// multiplies.  H = 1: two workgroups on a unit do the same for each other, where tiles are that many
+// multiplies.  H = 1: two workgroups on a unit do the same for each other, where tiles are that many; float32 gradients then need 6
+// to 11 registers more than the 256 that a lane has, which go to memory and back in every stage
 template <int WJ, int H>
 struct GradTile {
     static constexpr int HALF = 4, WAVES = H * HALF, THREADS = 64 * WAVES, WE = HALF / WJ, ROWS = kWaveRows * WJ, TE = kCols / WE / 32;   // TE: tiles of 32 inputs of a wave

@@ -301,7 +301,7 @@ __global__ __launch_bounds__(THREADS) void norm_grad_kernel(GradArgs g)
     for (int64_t row = (int64_t)blockIdx.x * s.rows + s.row; row < g.s.rows; row += (int64_t)gridDim.x * s.rows) {
         const int64_t first = row * cols;
         // (all loads of the row are under way before the first is used, but for the longest unaligned rows, for which registers
-        // are short)
+        // are short: 60 bytes a lane of theirs go to memory and back for every row all the same)
         constexpr bool kOneByOne = KEPT && K < 0 && !weights_held(H * E);
         uint32_t raw_d[H][E], raw_x[H][E], coded[H][(E + 3) / 4];
         int byte[H];
