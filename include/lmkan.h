@@ -556,7 +556,8 @@ typedef struct lmkan_norm {
  *   stats_dev             [rows][2] float32, mean and rstd, what the backward pass needs; NULL
  *                         skips them
  *   codes_dev, exps_dev   checkpoint of hat, as lmkan_checkpoint_rows makes it; NULL (both) skips it
- * (Statistics in float64: hat does not depend on the order of a sum, so that codes repeat.)
+ * The results repeat bit for bit for tensors of the same sizes and alignment.  (Statistics in float64: on another alignment,
+ * which sums in another order, hat and codes differ only where that falls on both sides of the border of two float32 numbers.)
  */
 lmkan_status lmkan_layer_norm(const lmkan_norm *desc, int64_t rows, const void *x_dev, const float *weight_dev,
                               const float *bias_dev, void *y_dev, float *stats_dev, int8_t *codes_dev,

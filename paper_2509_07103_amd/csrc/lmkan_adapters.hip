@@ -5,13 +5,14 @@
 //   order  one workgroup sorts the rows by adapter, by counting, into tiles of up to 32 rows of one adapter
 //   down   low = A f(x): a tile and a piece of the inputs a workgroup, whose waves take every fourth 16 inputs
 //   up     y += scale B low: a tile and a piece of the outputs a workgroup
-// Products are those of float32 matrix instructions, 16 x 16 results of 4 terms, or where the types allow it of 16-bit ones;
-// reading x and y once each bounds them as long as the rank is below a hundred.  A row's result does not depend on the rows that
+// Products are those of float32 matrix instructions, 16 x 16 results of 4 terms, or where the types allow it of 16-bit ones.
+// Reading x and y once each would bound them as long as the rank is below a hundred; they take twice that at low ranks and three
+// times at 128, as every tile of 32 rows reads its adapter again and three launches wait for each other.  A row's result does not depend on the rows that
 // share its tile, so that the order within an adapter, which atomics decide, changes nothing.
 //
-// Measured (us): one row of 4096 -> 4096, rank 16, bfloat16 8.3; 48 rows of 1024 -> 1024, rank 16, 4.3 (an empty launch 3.4); 8192 rows
-// of 1024 -> 1024, rank 32, float32 38: 7.8 for the order (one workgroup, a chain of loads, counters and stores), 13.7 down (x at
-// 2.4 TB/s), 16.0 up (y at 4.2 TB/s); 16384 rows of 4096 -> 1024, rank 64, bfloat16 76.
+// Measured (us): one row of 4096 -> 4096, rank 16, bfloat16 8.3; 48 rows of 1024 -> 1024, rank 16, 4.2 in a loop of that call (an empty
+// launch 3.4); 8192 rows of 1024 -> 1024, rank 32, float32 39: 7.7 for the order (one workgroup, a chain of loads, counters and
+// stores), 13.8 down (x at 2.4 TB/s), 16.3 up (y at 4.1 TB/s); 16384 rows of 4096 -> 1024, rank 64, bfloat16 76, float16 80.
 #include <type_traits>
 
 #include "lmkan_rows.h"
@@ -700,9 +701,9 @@ constexpr int kUnits = 256;   // compute units
 
 size_t item_of(int dtype) { return dtype == LMKAN_F32 ? 4 : 2; }
 
-// One launch while what its workgroups read of A, each for itself, is little.  Measured (us, one launch / three): 48 rows of
-// 1024 -> 1024, rank 16, 5.5 / 12.9; 512 rows 10.7 / 13.0; 2000 of 333 -> 100, rank 20, 42 / 17; 128 of 2048 -> 2048, rank 64,
-// 33 / 19; one of 4096 -> 4096, rank 128, in float32 40 / 24.
+// One launch while what its workgroups read of A, each for itself, is little.  Measured (us, one launch / three; bfloat16 adapters):
+// 48 rows of 1024 -> 1024, rank 16, 4.2 / 12.9; 512 rows 9.3 / 13.5; 2000 of 333 -> 100, rank 20, 24 / 17; 128 of 2048 -> 2048, rank
+// 64, 26 / 17; one of 4096 -> 4096, rank 128, in float32 29 / 24.
 bool few_rows(const AdapterShape &s)
 {
     const int64_t a = (int64_t)s.rank * s.n_in * item_of(s.dtype), groups = s.batch * ((s.n_out + kFewOutputs - 1) / kFewOutputs);
@@ -790,7 +791,7 @@ void launch_adapters(const AdapterShape &s, const void *x, const int32_t *index,
     const auto whole = [](int n, const void *p, int dtype) { return n % (16 / item_of(dtype)) == 0 && aligned_to(p, 16); };
     const bool in_whole = whole(s.n_in, x, s.x_dtype) && whole(s.n_in, a, s.dtype), out_whole = whole(s.rank, b, s.dtype) && whole(s.n_out, y, s.y_dtype);
     // 16-bit instructions here and on the way up.  Measured (us, float32 / 16-bit): 16384 rows of 4096 -> 1024, rank 64, bfloat16
-    // 172 / 76; 4096 of 4096 -> 4096, rank 128, 136 / 68; 16384 of 1024 -> 1024, rank 16, 49 / 42
+    // 172 / 76; 4096 of 4096 -> 4096, rank 128, 136 / 69; 16384 of 1024 -> 1024, rank 16, 49 / 41
     const bool native = s.x_dtype == s.dtype && s.dtype != LMKAN_F32;
     const bool xw = s.x_dtype == LMKAN_F32, ww = s.dtype == LMKAN_F32;
     if (few_rows(s)) {

@@ -1,10 +1,12 @@
 // Activations to 8-bit checkpoints and back.  A block of 32 columns shares a power of two, so that both directions are
-// exact but for the one rounding to a whole number, and a value (7 bits and a sign) is exact in 16-bit types too.
+// exact but for the one rounding to a whole number, and a value (7 bits and a sign) is exact in 16-bit types too (float16: within
+// its range).
 //
 // Both are bound by memory.  A lane takes pieces of 4 or 8 adjacent elements (16 bytes), 8 or 4 lanes a block, whose largest
 // magnitude they find without LDS; a row goes to as many lanes as give each a few pieces, which are under way together.
-// 16384 x 4096 float32: to codes 62 us (5.5 TB/s of what is read and written; a copy reaches 5.2 to 5.4), back 61 (5.5);
-// 5000 x 500 float16 4.4 and 4.2 us a launch, hardly more than an empty one.
+// 16384 x 4096 float32, each in a loop of its own: to codes 62 us (5.4 TB/s of what is read and written; a copy reaches 5.2 to 5.4),
+// back 61 (5.5).  One after the other, on rows that the last cache no longer holds in part, 83 and 57, 140 in all (4.8); 5000 x 500
+// float16 9.5, two launches that take hardly more than empty ones.
 #include "lmkan_rows.h"
 
 namespace lmkan {

@@ -9,9 +9,9 @@
 // few, and a second launch adds the parts.
 //
 // Measured (us; TFLOP/s counted with the parts, where the library's bfloat16 product reaches 1225): 16384 of 4096 -> 4096 float32
-// 1300 (1270), 8192 of 1024 -> 1024 float32 57 to 64 (810 to 900), of which 8.8 add the parts; 4096 of 4096 -> 4096 bfloat16 140 to
-// 150 (910 to 980), bound by reads of four bytes a lane; 5000 of 500 -> 333 float32 24, 131072 of 64 -> 10 bfloat16 22, bound by the
-// start of a workgroup (3 to 4) and the second launch.
+// 1330 (1240), 8192 of 1024 -> 1024 float32 58 (890), of which 8.8 add the parts, float16 47 (730); 4096 of 4096 -> 4096 bfloat16 143
+// (960), bound by reads of four bytes a lane; 5000 of 500 -> 333 float32 24, 131072 of 64 -> 10 bfloat16 22 with the bias and 18
+// without, bound by the start of a workgroup (3 to 4) and the second launch.
 #include <type_traits>
 
 #include "lmkan_rows.h"

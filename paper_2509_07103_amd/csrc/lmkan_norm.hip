@@ -7,10 +7,11 @@
 // row after row, with the columns' weights in registers; the backward pass keeps its sums over rows there too, writes one
 // part a workgroup, and a second launch adds the parts.  Statistics in float64 take no time beside the memory.
 //
-// Measured (us; TB/s of what has to be read and written, of which a copy reaches 5.2 to 5.4): 65536 x 1024 float32 forward 99
-// (5.4), with a checkpoint 121 (5.0), backward 153 (5.3), from the checkpoint 114 (5.3); 8192 x 1024 backward 23 (4.4), of which
-// 4.7 are the second launch; 262144 x 128 bfloat16 from the checkpoint 39 (4.4); 100000 x 333 from bfloat16 to float32, rows at any
-// address, forward 49 (4.1), backward 63 (4.2); 4096 x 16384 float32 forward 135 (4.0), backward 182 (4.4).
+// Measured (us; TB/s of what has to be read and written, of which a copy reaches 5.2 to 5.4): 65536 x 1024 float32 forward 100
+// (5.4), with a checkpoint 116 (5.2), backward 151 (5.3), from the checkpoint 113 (5.4); 8192 x 1024 backward 23 (4.4), of which
+// 3.9 are the second launch; 262144 x 128 bfloat16 from the checkpoint 39 (4.3); 100000 x 333 from bfloat16 to float32, rows at any
+// address, forward 48 (4.1), backward 63 (4.2); 4096 x 16384 float32 forward 130 (4.1), backward 185 (4.4); 2000 x 40000, which
+// registers do not hold, 266 (2.4) and 419 (2.3).
 #include "lmkan_rows.h"
 
 namespace lmkan {
@@ -209,7 +210,7 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(NormArgs a)
 }
 
 // Rows that registers do not hold are read three times (from the L2 or the last cache after the first).  4096 x 16384 float32
-// would take 216 us this way where rows in registers take 135, and 330 instead of 182 in the backward pass.
+// would take 216 us this way where rows in registers take 130, and 330 instead of 185 in the backward pass.
 template <int K>
 __global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs a)
 {
