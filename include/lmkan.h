@@ -578,7 +578,7 @@ lmkan_status lmkan_layer_norm(const lmkan_norm *desc, int64_t rows, const void *
  *                         LMKAN_NORM_ACCUMULATE; NULL skips either.  rows == 0 is a sum of nothing
  *   workspace_dev / workspace_bytes: at least lmkan_layer_norm_backward_workspace_bytes(desc, rows)
  *                         bytes, 256-byte aligned (NULL allowed when 0, and when neither grad_weight nor
- *                         grad_bias is wanted)
+ *                         grad_bias is wanted).  The size covers every smaller number of rows too
  * Sums are float32, in an order that the sizes and the tensors' alignment fix: the results repeat bit
  * for bit.
  */

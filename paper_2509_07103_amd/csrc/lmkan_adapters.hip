@@ -7,8 +7,8 @@
 //   up     y += scale B low: a tile and a piece of the outputs a workgroup
 // Products are those of float32 matrix instructions, 16 x 16 results of 4 terms, or where the types allow it of 16-bit ones.
 // Reading x and y once each would bound them as long as the rank is below a hundred; they take twice that at low ranks and three
-// times at 128, as every tile of 32 rows reads its adapter again and three launches wait for each other.  A row's result does not depend on the rows that
-// share its tile, so that the order within an adapter, which atomics decide, changes nothing.
+// times at 128, as every tile of 32 rows reads its adapter again and three launches wait for each other.  A row's result does not
+// depend on the rows that share its tile, so that the order within an adapter, which atomics decide, changes nothing.
 //
 // Measured (us): one row of 4096 -> 4096, rank 16, bfloat16 8.3; 48 rows of 1024 -> 1024, rank 16, 4.2 in a loop of that call (an empty
 // launch 3.4); 8192 rows of 1024 -> 1024, rank 32, float32 39: 7.7 for the order (one workgroup, a chain of loads, counters and
